@@ -336,7 +336,7 @@ PLAIN = {"head": _plain_head, "controls": _plain_controls, "grammar": _plain_gra
 # ------------------------------------------------------------------ the package's calls
 def _own_head(s):
     from paper_2510_26527_b200 import binding
-    out, _ = binding.polyspec_lm_head_w4(s["hidden"], s["qweight"], s["scales"], s["zero_points"], out=s["logits"])
+    out, _ = binding.polyspec_lm_head_quantized(s["hidden"], s["qweight"], s["scales"], s["zero_points"], out=s["logits"])
     return {"logits": out}
 
 
