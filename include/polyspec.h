@@ -67,7 +67,8 @@ typedef enum {
     POLYSPEC_ERR_CUDA = 4,
     POLYSPEC_ERR_TIMEOUT = 5,
     POLYSPEC_ERR_BAD_INPUT_ON_DEVICE = 6,
-    POLYSPEC_ERR_SCRATCH_LIMIT = 7      /* problem too large for the built-in scratch of a *_static call */
+    POLYSPEC_ERR_SCRATCH_LIMIT = 7,     /* problem too large for the built-in scratch of a *_static call */
+    POLYSPEC_ERR_NO_PAGES = 8           /* a cache pool has too few free pages (reported on the device) */
 } polyspec_status;
 
 typedef enum { POLYSPEC_F32 = 0, POLYSPEC_BF16 = 1 } polyspec_dtype;
@@ -401,6 +402,123 @@ polyspec_status polyspec_staged_accumulate(const polyspec_staged_state* s /* hos
                                            int32_t* pos1, int32_t* tokens1, float* uniforms1, int32_t* block_len1, void* cuda_stream);
 polyspec_status polyspec_staged_commit(const polyspec_staged_state* s /* host */, const int32_t* block_len1, const int32_t* accepted_len1,
                                        const int32_t* next_token1, void* cuda_stream);
+
+/*
+ * polyspec_lm_head_quantized -- polyspec_lm_head for a verifier whose LM head is held in 4 bits with group scales (the paper's M_2
+ * is a 4-bit copy of M_1 with groups of 128, Section 4.1):
+ *   logits[r, v] = sum_g scales[v, g] * sum_{k in group g} hidden[r, k] * (q[v, k] - z[v, g])
+ *
+ *   hidden       [rows, d] bf16, 16-byte aligned; any number of rows
+ *   qweight      [V, d/8] 32-bit words, 16-byte aligned: word i of a row holds q[v, 8i .. 8i+7], weight 8i + e in the four
+ *                bits from bit 4 * (e / 2) + 16 * (e % 2) on (polyspec_pack_quantized makes it from one code per byte)
+ *   scales       [V, d/group] bf16; group 32, 64 or 128, d a multiple of group
+ *   zero_points  [V, d/group] bytes, or NULL for 8 everywhere; the low four bits of a byte count
+ *   logits       out [rows, V] fp32 or bf16 (logits_dt), 16-byte aligned; any V
+ *   q - z is multiplied exactly, a group's sum and the sum over the groups are held in fp32; bf16 logits are rounded once.
+ *   The result of a row does not depend on timing.  No workspace; nothing outside [rows, V] is written.
+ *   device_status as in polyspec_lm_head.
+ */
+polyspec_status polyspec_pack_quantized(const void* codes /* [V, d] bytes, 16-byte aligned, low four bits count */, int V, int d /* a multiple of 32 */,
+                                 void* qweight /* out [V, d/8] words */, void* cuda_stream);
+polyspec_status polyspec_lm_head_quantized(const void* hidden, const void* qweight, const void* scales, const void* zero_points,
+                                    int rows, int V, int d, int group, polyspec_dtype logits_dt, void* logits,
+                                    int32_t* device_status, void* cuda_stream);
+
+/*
+ * polyspec_process_logits -- a request's sampling controls on the logits rows of a block, before they are verified: penalties
+ * for repeated tokens, biases and allowed-token masks.  Every row of a block has a context of its own, the text so far and
+ * the drafted tokens before the row, so row j of sequence b is controlled with history[b, 0 .. history_len) followed by
+ * draft_tokens[b, 0 .. j); give the rows of every model of the chain the same controls, and the chain verifies controlled
+ * distributions.  With n(v) the occurrences of v in that context behind the prompt:
+ *     z1 = v occurs in the context ? (z > 0 ? z / repetition : z * repetition) : z
+ *     z2 = n(v) > 0 ? z1 - frequency * n(v) - presence : z1
+ *     z3 = z2 + the biases listed for v (a token listed twice counts twice)
+ *     z4 = v allowed ? z3 : -inf            (whatever z3 is, NaN included)
+ * in fp32, rounded once to the storage type.  Entries that no control touches keep their bits.  A row whose mask allows
+ * nothing becomes -inf throughout, which the verification calls report as unusable.
+ *
+ *   logits [B, rows, V] fp32 or bf16, out [B, rows, V]: either the same buffer (in place) or one that does not overlap it;
+ *   both 16-byte aligned, V a multiple of 8
+ *   draft_tokens [B, k] or NULL (every row then has the history alone as its context), rows <= k + 1
+ *   controls (host struct of device pointers; a NULL pointer leaves that control out):
+ *     history       [B, history_cap] token ids; history_len [B] (NULL: history_cap), prompt_len [B] (NULL: 0): the first
+ *                   prompt_len tokens are the prompt, which counts for the repetition penalty only
+ *     repetition, frequency, presence   [B] (NULL: 1, 0, 0); repetition > 0
+ *     bias_tokens, bias_values          [B, n_bias]
+ *     mask          [B, rows, ceil(V/32)] words: entry v is allowed iff bit v % 32 of word v / 32 is set
+ *     vocab_begin, vocab_size           where the logits are one rank's slice of a sharded vocabulary: their first entry and
+ *                   the whole size; token ids are always whole-vocabulary ids, mask bits are the slice's.  0, 0: not sharded
+ *   A negative token id is padding and counts nowhere.  An id >= vocab_size, a length outside its bounds (it is clamped) or
+ *   a repetition that is not > 0 (1 is used) sets *device_status to POLYSPEC_ERR_BAD_INPUT_ON_DEVICE.
+ */
+typedef struct {
+    const int32_t* history;
+    const int32_t* history_len;
+    const int32_t* prompt_len;
+    const float* repetition;
+    const float* frequency;
+    const float* presence;
+    const int32_t* bias_tokens;
+    const float* bias_values;
+    const uint32_t* mask;
+    int history_cap, n_bias, vocab_begin, vocab_size;
+} polyspec_logit_controls;
+polyspec_status polyspec_process_logits(const void* logits, const polyspec_logit_controls* controls /* host */, const int32_t* draft_tokens,
+                                        int k, int B, int rows, int V, polyspec_dtype dt, void* out, int32_t* device_status,
+                                        void* cuda_stream);
+
+/*
+ * Page tables of a model's cache around a verified block (Algorithm 1 commits a prefix and rolls the rest back), kept on the
+ * device like the staged loop's state: no call is read back.
+ *
+ *   table [n_seqs, max_pages]  the pages a sequence holds, in order (-1 behind them); len [n_seqs] tokens held, in pages of
+ *   page_tokens; refs [n_pages] table entries naming each page; free_bits [ceil(n_pages/32)] bit p % 32 of word p / 32 set iff
+ *   refs[p] == 0, no bits set past n_pages.  Caller-owned device arrays, filled by polyspec_cache_init.
+ *   n_pages <= 1048576, max_pages * page_tokens < 2^31.
+ *   A pool is the contents: n_planes planes (layers, keys and values) of n_pages pages of page_bytes, page p of plane i at
+ *   data + (i * n_pages + p) * page_bytes; page_bytes a multiple of 16, data 16-byte aligned.
+ *   In reserve and rollback the target length of sequence b is base[b] + (extra ? extra[b] : 0) + plus; base or extra may be
+ *   the staged loop's t and cnt, or len itself.
+ *
+ *   polyspec_cache_reserve   sequences whose target is above their length grow to it.  Pages are taken lowest number first,
+ *        sequences in order; where the first new token falls into a last page that other sequences hold too, the page is
+ *        replaced by a copy of its own first (in every pool given).  A sequence for which the free pages, counted off in
+ *        order, do not suffice stays as it was, with all after it that need a page (POLYSPEC_ERR_NO_PAGES in *device_status);
+ *        so does one whose target exceeds max_pages * page_tokens (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE).  len tells what was granted.
+ *   polyspec_cache_rollback  sequences whose target is below their length (and not negative) fall back to it; pages wholly
+ *        behind it are given back.  Others stay as they are.
+ *   polyspec_cache_fork      for n pairs: sequence dst[i], which holds nothing, becomes a copy of src[i] that shares its pages.
+ *        Both negative: unused.  A pair is left out (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE) if a number is out of range, dst holds
+ *        tokens, src is a dst of the list, or an earlier pair has the same dst.
+ *   polyspec_cache_compact   moves pages so that those in use are numbered 0 .. n_live-1: the i-th used page from n_live on
+ *        goes to the i-th free page below n_live, its contents in every pool with it; tables follow.  moved_to [n_pages] (or
+ *        NULL): the new number of every page in use, -1 for free ones.
+ *   Reserve and compact need a workspace of polyspec_cache_workspace bytes.  Calls on one state must be ordered by the
+ *   caller (one stream); the outcome depends on the state alone.  A page number out of range or a reference too many found on
+ *   the way is skipped and reported as POLYSPEC_ERR_BAD_INPUT_ON_DEVICE.
+ */
+#define POLYSPEC_CACHE_MAX_POOLS 8
+typedef struct {
+    int n_seqs, max_pages, n_pages, page_tokens;
+    int32_t *table, *len, *refs;
+    uint32_t* free_bits;
+} polyspec_cache_pages;
+typedef struct {
+    void* data;
+    int n_planes;
+    size_t page_bytes;
+} polyspec_cache_pool;
+polyspec_status polyspec_cache_workspace(int n_seqs, int n_pages, size_t* bytes /* host out */);
+polyspec_status polyspec_cache_init(const polyspec_cache_pages* s /* host */, void* cuda_stream);
+polyspec_status polyspec_cache_reserve(const polyspec_cache_pages* s /* host */, const int32_t* base, const int32_t* extra, int plus,
+                                       const polyspec_cache_pool* pools /* host */, int n_pools, int32_t* device_status,
+                                       void* workspace, size_t workspace_bytes, void* cuda_stream);
+polyspec_status polyspec_cache_rollback(const polyspec_cache_pages* s /* host */, const int32_t* base, const int32_t* extra, int plus,
+                                        int32_t* device_status, void* cuda_stream);
+polyspec_status polyspec_cache_fork(const polyspec_cache_pages* s /* host */, const int32_t* src, const int32_t* dst, int n,
+                                    int32_t* device_status, void* cuda_stream);
+polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */, const polyspec_cache_pool* pools /* host */, int n_pools,
+                                       int32_t* moved_to, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
  * polyspec_verify_level_static -- polyspec_verify_level without a workspace argument.

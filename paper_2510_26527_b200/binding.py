@@ -17,7 +17,7 @@ LIB_PATH = os.path.join(_HERE, "libpolyspec.so")
 
 OK = 0
 ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, ERR_BAD_INPUT_ON_DEVICE = 1, 2, 3, 4, 5, 6
-ERR_SCRATCH_LIMIT = 7
+ERR_SCRATCH_LIMIT, ERR_NO_PAGES = 7, 8
 F32, BF16 = 0, 1
 MAX_K, MAX_MODELS = 32, 8
 
@@ -37,6 +37,9 @@ EXPORTS = (
     "polyspec_sharded_chain_sizes", "polyspec_sharded_chain_stats", "polyspec_sharded_chain_gather",
     "polyspec_sharded_chain_decide", "polyspec_sharded_chain_pick", "polyspec_sharded_chain_handoff",
     "polyspec_staged_init", "polyspec_staged_round_begin", "polyspec_staged_accumulate", "polyspec_staged_commit",
+    "polyspec_pack_quantized", "polyspec_lm_head_quantized", "polyspec_process_logits",
+    "polyspec_cache_workspace", "polyspec_cache_init", "polyspec_cache_reserve", "polyspec_cache_rollback", "polyspec_cache_fork",
+    "polyspec_cache_compact",
 )
 
 
@@ -62,6 +65,26 @@ class StagedState(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int) for n in ("B", "K", "mu", "kcap", "N", "R", "C", "cap", "n_tokens")] + \
                [(n, ctypes.c_void_p) for n in STAGED_ARRAYS]
 
+
+class LogitControls(ctypes.Structure):
+    """polyspec_logit_controls."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("history", "history_len", "prompt_len", "repetition", "frequency", "presence",
+                                               "bias_tokens", "bias_values", "mask")] + \
+               [(n, ctypes.c_int) for n in ("history_cap", "n_bias", "vocab_begin", "vocab_size")]
+
+
+class CachePagesStruct(ctypes.Structure):
+    """polyspec_cache_pages."""
+    _fields_ = [(n, ctypes.c_int) for n in ("n_seqs", "max_pages", "n_pages", "page_tokens")] + \
+               [(n, ctypes.c_void_p) for n in ("table", "len", "refs", "free_bits")]
+
+
+class CachePool(ctypes.Structure):
+    """polyspec_cache_pool."""
+    _fields_ = [("data", ctypes.c_void_p), ("n_planes", ctypes.c_int), ("page_bytes", ctypes.c_size_t)]
+
+
+CACHE_MAX_POOLS = 8
 
 _lib = None
 
@@ -162,6 +185,25 @@ def load_library() -> ctypes.CDLL:
     lib.polyspec_staged_accumulate.argtypes = [ssp, i32p, i32p, i32p, i32p, f32p, i32p, i32p, f32p, i32p, vp]
     lib.polyspec_staged_commit.restype = ci
     lib.polyspec_staged_commit.argtypes = [ssp, i32p, i32p, i32p, vp]
+    lib.polyspec_pack_quantized.restype = ci
+    lib.polyspec_pack_quantized.argtypes = [vp, ci, ci, vp, vp]
+    lib.polyspec_lm_head_quantized.restype = ci
+    lib.polyspec_lm_head_quantized.argtypes = [vp, vp, vp, vp, ci, ci, ci, ci, ci, vp, i32p, vp]
+    lib.polyspec_process_logits.restype = ci
+    lib.polyspec_process_logits.argtypes = [vp, ctypes.POINTER(LogitControls), i32p, ci, ci, ci, ci, ci, vp, i32p, vp]
+    cpp, poolp = ctypes.POINTER(CachePagesStruct), ctypes.POINTER(CachePool)
+    lib.polyspec_cache_workspace.restype = ci
+    lib.polyspec_cache_workspace.argtypes = [ci, ci, szp]
+    lib.polyspec_cache_init.restype = ci
+    lib.polyspec_cache_init.argtypes = [cpp, vp]
+    lib.polyspec_cache_reserve.restype = ci
+    lib.polyspec_cache_reserve.argtypes = [cpp, i32p, i32p, ci, poolp, ci, i32p, vp, sz, vp]
+    lib.polyspec_cache_rollback.restype = ci
+    lib.polyspec_cache_rollback.argtypes = [cpp, i32p, i32p, ci, i32p, vp]
+    lib.polyspec_cache_fork.restype = ci
+    lib.polyspec_cache_fork.argtypes = [cpp, i32p, i32p, ci, i32p, vp]
+    lib.polyspec_cache_compact.restype = ci
+    lib.polyspec_cache_compact.argtypes = [cpp, poolp, ci, i32p, vp, sz, vp]
     _lib = lib
     return lib
 
@@ -772,3 +814,270 @@ class ShardedChainCall:
         _check(self.lib.polyspec_sharded_chain_handoff(self.n, self._k, level, self.B, _ptr(self.out["accepted_len"]), _ptr(token),
                                                        _ptr(self.block_tokens), _ptr(self.block_len), _ptr(self.out["out_tokens"]),
                                                        _ptr(self.out["out_len"]), _stream(self.stream)), "polyspec_sharded_chain_handoff")
+
+
+# ------------------------------------------------------------------ 4-bit LM head, sampling controls, cache pages
+class _On:
+    """The device and the stream of a call: every tensor contiguous on one CUDA device, which is made current while the call is
+    enqueued; what the call allocated stays alive for a stream other than the current one."""
+
+    def __init__(self, stream, *tensors):
+        self.device = None
+        for t in tensors:
+            if t is None:
+                continue
+            if not t.is_cuda or not t.is_contiguous():
+                raise ValueError("device-pointer arguments must be contiguous CUDA tensors")
+            if self.device is None:
+                self.device = t.device
+            elif t.device != self.device:
+                raise ValueError("all tensors of a call must be on one device")
+        self.stream = stream
+        self._guard = None
+
+    def __enter__(self):
+        if torch.cuda.current_device() != self.device.index:
+            self._guard = torch.cuda.device(self.device)
+            self._guard.__enter__()
+        return self
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+    def handle(self) -> int:
+        return _stream(self.stream)
+
+    def empty(self, shape, dtype) -> torch.Tensor:
+        """A tensor for the call's stream."""
+        if self.stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        s = self.stream if isinstance(self.stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.handle(), device=self.device)
+        with torch.cuda.stream(s):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def status(self) -> torch.Tensor:
+        """A zeroed status word, zeroed on the call's stream."""
+        t = self.empty(1, torch.int32)
+        if self.stream is None:
+            return t.zero_()
+        s = self.stream if isinstance(self.stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.handle(), device=self.device)
+        with torch.cuda.stream(s):
+            return t.zero_()
+
+
+def _typed(dtype, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+
+
+def _status_arg(device_status):
+    if device_status is not None and (device_status.dtype != torch.int32 or device_status.numel() < 1):
+        raise TypeError("device_status must be an int32 tensor")
+
+
+def polyspec_pack_quantized(codes, out=None, stream=None):
+    """codes [V, d] uint8 (one 4-bit code per byte, d a multiple of 32) -> qweight [V, d/8] int32, the words
+    polyspec_lm_head_quantized reads."""
+    lib = load_library()
+    _typed(torch.uint8, codes=codes)
+    _typed(torch.int32, out=out)
+    V, d = codes.shape
+    with _On(stream, codes, out) as on:
+        if out is None:
+            out = on.empty((V, d // 8), torch.int32)
+        if tuple(out.shape) != (V, d // 8):
+            raise ValueError("out must be [V, d/8]")
+        _check(lib.polyspec_pack_quantized(_ptr(codes), V, d, _ptr(out), on.handle()), "polyspec_pack_quantized")
+    return out
+
+
+def polyspec_lm_head_quantized(hidden, qweight, scales, zero_points=None, out=None, out_dtype=torch.float32, device_status=None, stream=None):
+    """logits[r, v] = sum_d hidden[r, d] * scales[v, d // group] * (code[v, d] - zero_point[v, d // group]).
+
+    hidden [rows, d] bf16, qweight [V, d/8] int32 (polyspec_pack_quantized), scales [V, d/group] bf16, zero_points
+    [V, d/group] uint8 or None (8 everywhere); out [rows, V] fp32 or bf16 (out_dtype, where out is not given)."""
+    lib = load_library()
+    _typed(torch.bfloat16, hidden=hidden, scales=scales)
+    _typed(torch.int32, qweight=qweight)
+    _typed(torch.uint8, zero_points=zero_points)
+    _status_arg(device_status)
+    rows, d = hidden.shape
+    V, groups = scales.shape
+    if tuple(qweight.shape) != (V, d // 8) or groups < 1 or d % groups or (zero_points is not None and zero_points.shape != scales.shape):
+        raise ValueError("shapes must be hidden [rows,d], qweight [V,d/8], scales [V,d/group], zero_points [V,d/group]")
+    with _On(stream, hidden, qweight, scales, zero_points, out, device_status) as on:
+        if out is None:
+            out = on.empty((rows, V), out_dtype)
+        if tuple(out.shape) != (rows, V):
+            raise ValueError("out must be [rows, V]")
+        dt = _dt(out)
+        if device_status is None:
+            device_status = on.status()
+        _check(lib.polyspec_lm_head_quantized(_ptr(hidden), _ptr(qweight), _ptr(scales), _ptr(zero_points), rows, V, d, d // groups, dt,
+                                              _ptr(out), _ptr(device_status), on.handle()), "polyspec_lm_head_quantized")
+    return out, device_status
+
+
+def polyspec_process_logits(logits, draft_tokens=None, history=None, history_len=None, prompt_len=None, repetition=None, frequency=None,
+                            presence=None, bias_tokens=None, bias_values=None, mask=None, out=None, vocab_begin=0, vocab_size=0,
+                            device_status=None, stream=None):
+    """Sampling controls on logits [B, rows, V] of a block: penalties for repeated tokens, biases, allowed-token masks; row j has
+    the history and draft_tokens[:, :j] as its context.
+
+    draft_tokens [B, k >= rows-1], history [B, cap], history_len and prompt_len [B], bias_tokens [B, n]: int32; repetition,
+    frequency, presence [B], bias_values [B, n]: float32; mask [B, rows, ceil(V/32)] int32 (bit v % 32 of word v // 32 set:
+    allowed).  out: a tensor of its own (made if None) or logits itself.  Returns (out, status word)."""
+    lib = load_library()
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, rows, V]")
+    B, rows, V = logits.shape
+    dt = _dt(logits)
+    _typed(torch.int32, draft_tokens=draft_tokens, history=history, history_len=history_len, prompt_len=prompt_len, bias_tokens=bias_tokens,
+           mask=mask)
+    _typed(torch.float32, repetition=repetition, frequency=frequency, presence=presence, bias_values=bias_values)
+    _typed(logits.dtype, out=out)
+    _status_arg(device_status)
+    for name, t in (("history_len", history_len), ("prompt_len", prompt_len), ("repetition", repetition), ("frequency", frequency),
+                    ("presence", presence)):
+        if t is not None and tuple(t.shape) != (B,):
+            raise ValueError(f"{name} must be [B]")
+    if any(t is not None and (t.dim() != 2 or t.shape[0] != B) for t in (draft_tokens, history, bias_tokens)):
+        raise ValueError("draft_tokens, history and bias_tokens must be [B, n]")
+    if (bias_tokens is None) != (bias_values is None) or (bias_tokens is not None and bias_values.shape != bias_tokens.shape):
+        raise ValueError("bias_tokens and bias_values must have one shape")
+    if mask is not None and tuple(mask.shape) != (B, rows, (V + 31) // 32):
+        raise ValueError("mask must be [B, rows, ceil(V/32)]")
+    if out is not None and out.shape != logits.shape:
+        raise ValueError("out must have the shape of logits")
+    if history is None and (history_len is not None or prompt_len is not None):
+        raise ValueError("history_len and prompt_len need a history")
+    if history is not None and history.shape[1] == 0:
+        history = history_len = prompt_len = None
+    if bias_tokens is not None and bias_tokens.shape[1] == 0:
+        bias_tokens = bias_values = None
+    with _On(stream, logits, draft_tokens, history, history_len, prompt_len, repetition, frequency, presence, bias_tokens, bias_values,
+             mask, out, device_status) as on:
+        if out is None:
+            out = on.empty(logits.shape, logits.dtype)
+        if device_status is None:
+            device_status = on.status()
+        c = LogitControls(_ptr(history), _ptr(history_len), _ptr(prompt_len), _ptr(repetition), _ptr(frequency), _ptr(presence),
+                          _ptr(bias_tokens), _ptr(bias_values), _ptr(mask), 0 if history is None else history.shape[1],
+                          0 if bias_tokens is None else bias_tokens.shape[1], int(vocab_begin), int(vocab_size))
+        _check(lib.polyspec_process_logits(_ptr(logits), ctypes.byref(c), _ptr(draft_tokens),
+                                           0 if draft_tokens is None else draft_tokens.shape[1], B, rows, V, dt, _ptr(out),
+                                           _ptr(device_status), on.handle()), "polyspec_process_logits")
+    return out, device_status
+
+
+def polyspec_cache_workspace(n_seqs: int, n_pages: int) -> int:
+    n = ctypes.c_size_t(0)
+    _check(load_library().polyspec_cache_workspace(n_seqs, n_pages, ctypes.byref(n)), "polyspec_cache_workspace")
+    return n.value
+
+
+class CachePages:
+    """Page tables of one model's cache: table [n_seqs, max_pages], len [n_seqs], refs [n_pages] (int32) and free_bits
+    [ceil(n_pages/32)] (int32), on the device.  CachePages.new allocates and initialises them; the constructor takes tensors
+    that hold a state already.  The calls' workspace is allocated at the first call that needs one."""
+
+    def __init__(self, table, len, refs, free_bits, page_tokens):
+        _typed(torch.int32, table=table, len=len, refs=refs, free_bits=free_bits)
+        n_seqs, max_pages = table.shape
+        n_pages = refs.numel()
+        if tuple(len.shape) != (n_seqs,) or refs.dim() != 1 or tuple(free_bits.shape) != ((n_pages + 31) // 32,):
+            raise ValueError("shapes must be table [n_seqs,max_pages], len [n_seqs], refs [n_pages], free_bits [ceil(n_pages/32)]")
+        _On(None, table, len, refs, free_bits)
+        self.table, self.len, self.refs, self.free_bits = table, len, refs, free_bits
+        self.n_seqs, self.max_pages, self.n_pages, self.page_tokens = n_seqs, max_pages, n_pages, int(page_tokens)
+        self.c = CachePagesStruct(n_seqs, max_pages, n_pages, self.page_tokens, _ptr(table), _ptr(len), _ptr(refs), _ptr(free_bits))
+        self._workspace = None
+
+    @classmethod
+    def new(cls, n_seqs, max_pages, n_pages, page_tokens, device="cuda", stream=None):
+        i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=device)
+        pages = cls(i32(n_seqs, max_pages), i32(n_seqs), i32(n_pages), i32((n_pages + 31) // 32), page_tokens)
+        with _On(stream, pages.table) as on:
+            _check(load_library().polyspec_cache_init(ctypes.byref(pages.c), on.handle()), "polyspec_cache_init")
+        return pages
+
+    def workspace(self, on):
+        if self._workspace is None:
+            self._workspace = on.empty(polyspec_cache_workspace(self.n_seqs, self.n_pages), torch.uint8)
+        return self._workspace
+
+
+def _targets(pages, base, extra):
+    _typed(torch.int32, base=base, extra=extra)
+    if any(t is not None and tuple(t.shape) != (pages.n_seqs,) for t in (base, extra)):
+        raise ValueError("base and extra must be [n_seqs]")
+
+
+def _pools(pages, pools):
+    """pools: tensors [n_planes, n_pages, ...], each plane's page contiguous."""
+    if len(pools) > CACHE_MAX_POOLS:
+        raise ValueError(f"at most {CACHE_MAX_POOLS} pools")
+    for t in pools:
+        if t.dim() < 3 or t.shape[1] != pages.n_pages:
+            raise ValueError("a pool must be [n_planes, n_pages, ...]")
+    return (CachePool * max(1, len(pools)))(*[CachePool(t.data_ptr(), t.shape[0], t.stride(1) * t.element_size()) for t in pools])
+
+
+def polyspec_cache_reserve(pages, base, extra=None, plus=0, pools=(), device_status=None, workspace=None, stream=None):
+    """Grow every sequence to base[b] + extra[b] + plus tokens; a last page that others hold too is replaced by a copy of its
+    own, in every pool ([n_planes, n_pages, ...] tensors).  pages.len tells what was granted.  Returns the status word."""
+    lib = load_library()
+    _targets(pages, base, extra)
+    _status_arg(device_status)
+    with _On(stream, pages.table, base, extra, workspace, device_status, *pools) as on:
+        if workspace is None:
+            workspace = pages.workspace(on)
+        if device_status is None:
+            device_status = on.status()
+        _check(lib.polyspec_cache_reserve(ctypes.byref(pages.c), _ptr(base), _ptr(extra), int(plus), _pools(pages, pools), len(pools),
+                                          _ptr(device_status), _ptr(workspace), workspace.numel(), on.handle()), "polyspec_cache_reserve")
+    return device_status
+
+
+def polyspec_cache_rollback(pages, base, extra=None, plus=0, device_status=None, stream=None):
+    """Let every sequence fall back to base[b] + extra[b] + plus tokens (never up); returns the status word."""
+    lib = load_library()
+    _targets(pages, base, extra)
+    _status_arg(device_status)
+    with _On(stream, pages.table, base, extra, device_status) as on:
+        if device_status is None:
+            device_status = on.status()
+        _check(lib.polyspec_cache_rollback(ctypes.byref(pages.c), _ptr(base), _ptr(extra), int(plus), _ptr(device_status), on.handle()),
+               "polyspec_cache_rollback")
+    return device_status
+
+
+def polyspec_cache_fork(pages, src, dst, device_status=None, stream=None):
+    """Sequence dst[i], which holds nothing, becomes a copy of src[i] on the same pages; returns the status word."""
+    lib = load_library()
+    _typed(torch.int32, src=src, dst=dst)
+    _status_arg(device_status)
+    if src.dim() != 1 or src.shape != dst.shape:
+        raise ValueError("src and dst must be [n]")
+    with _On(stream, pages.table, src, dst, device_status) as on:
+        if device_status is None:
+            device_status = on.status()
+        _check(lib.polyspec_cache_fork(ctypes.byref(pages.c), _ptr(src), _ptr(dst), src.numel(), _ptr(device_status), on.handle()),
+               "polyspec_cache_fork")
+    return device_status
+
+
+def polyspec_cache_compact(pages, pools=(), moved_to=None, workspace=None, stream=None):
+    """Renumber the pages in use to 0 .. n_live-1, moving their contents in every pool; moved_to [n_pages] int32 takes the new
+    numbers (-1 for free pages)."""
+    lib = load_library()
+    _typed(torch.int32, moved_to=moved_to)
+    if moved_to is not None and tuple(moved_to.shape) != (pages.n_pages,):
+        raise ValueError("moved_to must be [n_pages]")
+    with _On(stream, pages.table, moved_to, workspace, *pools) as on:
+        if workspace is None:
+            workspace = pages.workspace(on)
+        _check(lib.polyspec_cache_compact(ctypes.byref(pages.c), _pools(pages, pools), len(pools), _ptr(moved_to), _ptr(workspace),
+                                          workspace.numel(), on.handle()), "polyspec_cache_compact")

@@ -217,11 +217,12 @@ const char* polyspec_status_string(polyspec_status s)
         case POLYSPEC_ERR_TIMEOUT: return "bounded wait expired on the device";
         case POLYSPEC_ERR_BAD_INPUT_ON_DEVICE: return "unusable input found on the device (token out of range or unusable logits row)";
         case POLYSPEC_ERR_SCRATCH_LIMIT: return "problem too large for the built-in scratch of a *_static call";
+        case POLYSPEC_ERR_NO_PAGES: return "too few free cache pages (found on the device)";
     }
     return "unknown status";
 }
 
-int polyspec_version(void) { return 310; }      // 0.3.1: staged verification and the second insertion condition in the ABI
+int polyspec_version(void) { return 400; }      // 0.4.0: 4-bit LM head, sampling controls on logits, cache pages in the ABI
 
 const char* polyspec_last_cuda_error(void) { return cudaGetErrorString(g_last_cuda_error); }
 

@@ -1,0 +1,157 @@
+"""The LM head with 4-bit weights against its 64-bit statement.
+
+Tolerance per element: q - z is exact in bf16 and bf16 products are exact in fp32, so what is rounded are additions.  A group's
+sum of G products takes at most G additions in any order, the sum over the groups one fused multiply-add each, each off by at
+most 2^-23 (an addition inside the tensor core may truncate) of a partial sum that the sum of magnitudes bounds: (G + groups)
+2^-23 sum |h| |w|.  A bf16 logit is rounded once more, by at most 2^-8 of its value."""
+import pytest
+import torch
+
+from paper_2510_26527_b200 import binding, buildlib
+from tests import plain_operators as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    buildlib.build()
+    binding.load_library()
+    assert torch.cuda.is_available()
+
+
+def _case(rows, V, d, group, zeros, seed):
+    g = torch.Generator().manual_seed(seed)
+    hidden = torch.randn((rows, d), generator=g).to(torch.bfloat16)
+    codes = torch.randint(0, 16, (V, d), generator=g, dtype=torch.uint8)
+    scales = (torch.rand((V, d // group), generator=g) * 0.02 + 0.001).to(torch.bfloat16)
+    zp = torch.randint(0, 16, (V, d // group), generator=g, dtype=torch.uint8) if zeros else None
+    return hidden, codes, scales, zp
+
+
+def _close(got, hidden, codes, scales, zp):
+    ref, size = plain.head(hidden, codes, scales, zp)
+    d = codes.shape[1]
+    groups = scales.shape[1]
+    tol = (d // groups + groups) * 2.0 ** -23 * size + 1e-30
+    if got.dtype == torch.bfloat16:
+        tol = tol + 2.0 ** -8 * (ref.abs() + tol)
+    err = (got.cpu().double() - ref).abs()
+    worst = float((err / tol).max())
+    assert worst <= 1.0, worst
+    assert float(ref.abs().max()) > 0.01
+
+
+def _to(*ts):
+    return [None if t is None else t.to(DEV) for t in ts]
+
+
+@pytest.mark.parametrize("rows", [1, 2, 7, 8, 9, 15, 16, 17, 33, 64, 65, 100, 144, 193, 288, 300])
+@pytest.mark.parametrize("V,d,group,zeros,dtype", [
+    (257, 256, 128, True, torch.float32),
+    (130, 96, 32, True, torch.bfloat16),
+    (64, 192, 64, False, torch.float32),
+])
+def test_rows(rows, V, d, group, zeros, dtype):
+    hidden, codes, scales, zp = _case(rows, V, d, group, zeros, rows * 7 + V)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    out, status = binding.polyspec_lm_head_quantized(h, binding.polyspec_pack_quantized(c), s, z, out_dtype=dtype)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and out.dtype == dtype
+    _close(out, hidden, codes, scales, zp)
+
+
+@pytest.mark.parametrize("rows", [1, 9, 40])
+@pytest.mark.parametrize("V,d,group", [
+    (1, 32, 32), (1, 128, 128), (7, 64, 64), (31, 160, 32), (33, 128, 32), (127, 320, 64), (128, 384, 128), (129, 1152, 128),
+    (1000, 2080, 32), (513, 4096, 128), (300, 8192, 64), (257, 16384, 128), (40, 12800, 32), (5000, 448, 64), (20001, 256, 32),
+])
+def test_shapes(rows, V, d, group):
+    hidden, codes, scales, zp = _case(rows, V, d, group, V % 2 == 1, V + d)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    q = binding.polyspec_pack_quantized(c)
+    out, status = binding.polyspec_lm_head_quantized(h, q, s, z)
+    low, _ = binding.polyspec_lm_head_quantized(h, q, s, z, out_dtype=torch.bfloat16)
+    torch.cuda.synchronize()
+    assert int(status) == 0
+    _close(out, hidden, codes, scales, zp)
+    assert torch.equal(low, out.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("rows,V,d,group", [(1, 3001, 1024, 128), (12, 3001, 1024, 64), (70, 3001, 1024, 128), (200, 3001, 1056, 32)])
+def test_writes_nothing_else_and_repeats(rows, V, d, group):
+    hidden, codes, scales, zp = _case(rows, V, d, group, True, 3)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    q = binding.polyspec_pack_quantized(c)
+    room = torch.full((rows * V + 64,), -7.0, device=DEV)
+    first = None
+    for _ in range(3):
+        out, _ = binding.polyspec_lm_head_quantized(h, q, s, z, out=room[: rows * V].view(rows, V))
+        torch.cuda.synchronize()
+        assert (room[rows * V:] == -7.0).all()
+        assert first is None or torch.equal(first, out)
+        first = out.clone()
+    # a row's logits do not depend on where the vocabulary is cut
+    cut = 1504
+    for a, b in ((0, cut), (cut, V)):
+        part, _ = binding.polyspec_lm_head_quantized(h, q[a:b].contiguous(), s[a:b].contiguous(), z[a:b].contiguous())
+        assert torch.equal(part, first[:, a:b])
+
+
+def test_pack_layout_and_high_bits():
+    codes = torch.arange(2 * 32, dtype=torch.uint8).view(2, 32)             # codes above 15: the low four bits count
+    q = binding.polyspec_pack_quantized(codes.to(DEV)).cpu().numpy().view("uint32")
+    for v in range(2):
+        for k in range(32):
+            e = k % 8
+            assert (int(q[v, k // 8]) >> (4 * (e // 2) + 16 * (e % 2))) & 15 == int(codes[v, k]) & 15
+    hidden, codes, scales, zp = _case(3, 40, 128, 32, True, 5)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    q = binding.polyspec_pack_quantized(c)
+    a, _ = binding.polyspec_lm_head_quantized(h, q, s, z)
+    b, _ = binding.polyspec_lm_head_quantized(h, q, s, z + 16)
+    assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows", [1, 20, 130])
+def test_special_values_stay_in_their_rows_and_columns(rows):
+    hidden, codes, scales, zp = _case(rows, 300, 256, 128, True, 11)
+    hidden[0, 5] = float("inf")
+    scales[17, 1] = float("nan")
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    out, _ = binding.polyspec_lm_head_quantized(h, binding.polyspec_pack_quantized(c), s, z)
+    out = out.cpu()
+    assert out[:, 17].isnan().all()
+    keep = torch.ones(300, dtype=torch.bool)
+    keep[17] = False
+    if rows > 1:
+        ref, size = plain.head(hidden[1:], codes[keep], scales[keep], zp[keep])
+        assert ((out[1:][:, keep].double() - ref).abs() <= (128 + 2) * 2.0 ** -23 * size).all()
+    # inf * (q - z): +-inf by the sign of q - z, NaN where it is zero
+    sign = (codes[:, 5].float() - zp[:, 0].float())
+    assert torch.equal(out[0, keep & (sign > 0)], torch.full((int((keep & (sign > 0)).sum()),), float("inf")))
+    assert out[0, keep & (sign == 0)].isnan().all()
+
+
+@pytest.mark.parametrize("rows", [1, 36, 150])
+def test_captured_and_on_another_stream(rows):
+    hidden, codes, scales, zp = _case(rows, 2000, 512, 128, True, 21)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    q = binding.polyspec_pack_quantized(c)
+    want, status = binding.polyspec_lm_head_quantized(h, q, s, z)
+    out = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.polyspec_lm_head_quantized(h, q, s, z, out=out, device_status=status)
+    h2 = h.clone()
+    h.mul_(2.0)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(out, want * 2)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got, _ = binding.polyspec_lm_head_quantized(h2, q, s, z, stream=side)
+    side.synchronize()
+    assert torch.equal(got, want)
