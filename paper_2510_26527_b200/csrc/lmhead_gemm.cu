@@ -44,9 +44,12 @@
 #include <mutex>
 
 #include "polyspec_kernels.cuh"
+#include "tensor_device.cuh"
 
 namespace polyspec {
 namespace {
+
+using namespace tensordev;
 
 constexpr int kTileV = 128;                 // vocabulary entries per CTA and tile (MMA M per CTA)
 constexpr int kPairV = 2 * kTileV;          // vocabulary entries per CTA pair and tile (MMA M)
@@ -60,7 +63,6 @@ constexpr int kStageBytes = kBytesA + kBytesBMax;            // 34 KiB
 constexpr int kEpiWarps = 8;                // warps 2..9: two per TMEM lane quarter, alternating 16-column chunks
 constexpr int kGemmThreads = 32 * (2 + kEpiWarps);
 constexpr int kTmemCols = 512;
-constexpr uint32_t kSpinLimitG = 1u << 20;
 constexpr int kScratchPitch = 32;                            // an epilogue warp's staging tile: [16 hidden rows][32 vocabulary entries] fp32
 constexpr int kStatStageBytes = kEpiWarps * 16 * kScratchPitch * 4;
 constexpr int kStatMergeBytes = 4 * kMaxCols * 8;            // (E, s) of every column from each of the four lane quarters
@@ -96,8 +98,6 @@ struct GemmParams {
     int32_t* status;
 };
 
-__device__ __forceinline__ uint32_t smem_addr(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
 // The shared::cluster address of `addr` (a shared::cta address of this CTA) in CTA `rank` of the cluster.
 __device__ __forceinline__ uint32_t cluster_addr(uint32_t addr, uint32_t rank)
 {
@@ -117,51 +117,11 @@ __device__ __forceinline__ void cluster_sync_all()
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
-__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count)
-{
-    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
-}
-__device__ __forceinline__ void mbar_expect_tx(uint32_t bar, uint32_t bytes)
-{
-    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
 // Arrive on a barrier of any CTA of the cluster (`bar` is a shared::cluster address).
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
-__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
-}
-// Bounded wait that also gives up when a role of either CTA has raised the abort flag.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag)
-{
-    for (uint32_t i = 0; i < kSpinLimitG; ++i) {
-        if (mbar_try(bar, parity)) return true;
-        if ((i & 63u) == 63u && *abort_flag) return false;
-    }
-    return false;
-}
-
-// The same for waits that are known to be long (an epilogue warp waiting for a whole K loop): the
-// lanes sleep between polls instead of competing with the issuing warps for instruction slots.
-__device__ __forceinline__ bool mbar_wait_relaxed(uint32_t bar, uint32_t parity, volatile int* abort_flag)
-{
-    for (uint32_t i = 0; i < kSpinLimitG; ++i) {
-        if (mbar_try(bar, parity)) return true;
-        __nanosleep(256);
-        if ((i & 63u) == 63u && *abort_flag) return false;
-    }
-    return false;
-}
-
 // 2-D tiled TMA load into this CTA's shared memory; completion is counted on `bar`, a
 // shared::cluster address that may belong to the peer CTA of the pair.
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
@@ -182,20 +142,11 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, int x, int 
 __device__ __forceinline__ void tma_store_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 __device__ __forceinline__ void tma_store_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 
-// Shared-memory matrix descriptor (64 bits) of a K-major tile stored as rows of 128 bytes with
-// the 128-byte swizzle: start address >> 4 in bits 0..13, leading byte offset (unused here, 1) in
-// bits 16..29, stride byte offset 1024 >> 4 (8-row groups 1024 bytes apart) in bits 32..45,
-// descriptor version 1 in bits 46..47, layout type 2 in bits 61..63.  The address may point
-// 32 * i bytes into the first row to select the i-th 16-element K slice.
 // Instruction descriptor: D fp32, A and B bf16, both K-major, M = 256 over the CTA pair, N = n.
 __device__ __forceinline__ uint32_t instr_desc_bf16(int n)
 {
     return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(kPairV >> 4) << 24);
 }
-
-// The upper word of smem_desc_sw128 is the same for every tile; MMAs are issued from the lower words.
-constexpr uint32_t kDescHi = (1024u >> 4) | (1u << 14) | (2u << 29);
-__device__ __forceinline__ uint32_t smem_desc_lo(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | (1u << 16); }
 
 __device__ __forceinline__ void umma_bf16(uint32_t tmem_d, uint32_t adesc_lo, uint32_t bdesc_lo, uint32_t idesc, uint32_t accumulate)
 {
@@ -214,30 +165,6 @@ __device__ __forceinline__ void umma_commit_pair(uint32_t bar)
     asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                  ::"r"(bar), "h"(mask) : "memory");
 }
-// True in exactly one lane of a fully active warp.  The role loops are run by whole warps
-// (every lane polls the barriers) and only the issue of an asynchronous instruction is
-// elected, so that loop state and descriptors stay warp-uniform.
-__device__ __forceinline__ bool elect_one()
-{
-    uint32_t pred;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "elect.sync _|p, 0xffffffff;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(pred));
-    return pred != 0;
-}
-__device__ __forceinline__ void tc_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-
-__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t* r)
-{
-    asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
-          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-        : "r"(taddr) : "memory");
-}
 __device__ __forceinline__ float ex2f(float x)
 {
     float y;
@@ -249,12 +176,6 @@ __device__ __forceinline__ float pow2_neg(float d)
 {
     return (d < -126.0f) ? 0.0f : __int_as_float((static_cast<int>(d) + 127) << 23);
 }
-__device__ __forceinline__ void mbar_arrive_local(uint32_t bar)
-{
-    asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-
 // Work item -> (job, vocabulary tile, column block).  Items of job 0 come first; inside a job
 // the column blocks of one vocabulary tile are neighbours, so they run at about the same time
 // and share the W tile in L2.
@@ -540,26 +461,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) lmh
     }
 }
 
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
-                                  const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
-                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 std::mutex g_init_mutex;
 EncodeTiledFn g_encode = nullptr;
 bool g_attr_set[64] = {false};
 int g_pairs[64] = {0};      // CTA pairs the device can hold at once
 
-cudaError_t get_encoder()
-{
-    if (g_encode) return cudaSuccess;
-    void* fn = nullptr;
-    cudaDriverEntryPointQueryResult q;
-    cudaError_t e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &q);
-    if (e != cudaSuccess) return e;
-    if (q != cudaDriverEntryPointSuccess || !fn) return cudaErrorNotSupported;
-    g_encode = reinterpret_cast<EncodeTiledFn>(fn);
-    return cudaSuccess;
-}
+cudaError_t get_encoder() { return g_encode ? cudaSuccess : find_encoder(&g_encode); }
 
 // [n_rows, d] bf16 row-major; box = 64 elements of d (128 bytes) by box_rows rows; 128-byte swizzle;
 // rows past n_rows read as zero.

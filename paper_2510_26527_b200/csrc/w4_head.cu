@@ -28,6 +28,7 @@ namespace {
 constexpr int kWarpsS = 16;                     // warps per CTA, one CTA per SM
 constexpr int kThreadsS = 32 * kWarpsS;
 constexpr int kTileS = 32;                      // vocabulary entries per tile (two m16 tiles)
+constexpr int kStreamRows = 16;                 // more rows go to the tensor-core kernel
 constexpr int kChunk = 128;                     // d elements per step: 16 bytes of codes per lane and row
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -69,7 +70,6 @@ struct StreamParams {
     int split;                          // warps per tile, a divisor of kWarpsS
     int chunks_per_warp;                // ceil(chunks / split)
     int tiles;
-    int staged;                         // 0: the hidden rows do not fit shared memory and are read from global memory
     void* out;
 };
 
@@ -86,7 +86,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
 
     // hidden rows in fragment order: the 16 bytes of (chunk, n tile, word, lane) are the eight elements of row nt * 8 + g
     // that multiply word `word` of the codes lane (g, t) holds
-    const int kept = p.staged ? chunks * NT * 4 * 32 : 0;
+    const int kept = chunks * NT * 4 * 32;
     for (int i = threadIdx.x; i < kept; i += kThreadsS) {
         const int l = i & 31, word = (i >> 5) & 3, nt = (i >> 7) % NT, c = (i >> 7) / NT;
         const int n = nt * 8 + (l >> 2), q = l & 3;
@@ -162,13 +162,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
                         const int word = gi * (4 / GPC) + wi;
                         uint4 h[NT];
 #pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) {
-                            if (p.staged) { h[nt] = hid[(nt * 4 + word) * 32]; continue; }
-                            const int n = nt * 8 + g;
-                            const int k = c * kChunk + (G == 128 ? t * 32 + word * 8 : G == 64 ? (word >> 1) * 64 + t * 16 + (word & 1) * 8 : word * 32 + t * 8);
-                            h[nt] = n < rows && k < p.d ? __ldg(reinterpret_cast<const uint4*>(p.hidden + static_cast<size_t>(row0 + n) * p.d + k))
-                                                        : make_uint4(0, 0, 0, 0);
-                        }
+                        for (int nt = 0; nt < NT; ++nt) h[nt] = hid[(nt * 4 + word) * 32];
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
                             uint32_t lo[4], hi[4];
@@ -225,9 +219,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
 
 constexpr size_t kMaxSmem = 227 * 1024;
 
-size_t stream_smem(int d, int nt, bool staged = true)
+size_t stream_smem(int d, int nt)
 {
-    if (!staged) d = 0;
     const size_t chunks = (d + kChunk - 1) / kChunk;
     return chunks * nt * 4 * 512 + 2 * kWarpsS * (2 * nt * 4 * 32) * sizeof(float);
 }
@@ -235,7 +228,7 @@ size_t stream_smem(int d, int nt, bool staged = true)
 template <int G, int NT, int DT>
 cudaError_t launch_stream_t(const StreamParams& p, int grid_y, int sms, cudaStream_t stream)
 {
-    const size_t smem = stream_smem(p.d, NT, p.staged != 0);
+    const size_t smem = stream_smem(p.d, NT);
     cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<G, NT, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
     const dim3 grid(static_cast<unsigned>(std::min(sms, p.tiles)), static_cast<unsigned>(grid_y));
@@ -267,7 +260,6 @@ cudaError_t launch_stream(const W4Problem& q, int nt, polyspec_dtype dt, cudaStr
     p.d = q.d;
     p.groups = q.d / q.group;
     p.out = q.out;
-    p.staged = stream_smem(q.d, nt) <= kMaxSmem;
     p.tiles = (q.V + kTileS - 1) / kTileS;
     const int chunks = (q.d + kChunk - 1) / kChunk;
     // as many warps per tile as leave each two chunks (the prefetch depth) to work on
@@ -326,7 +318,6 @@ polyspec_status polyspec_lm_head_quantized(const void* hidden, const void* qweig
         return POLYSPEC_ERR_INVALID_ARG;
     if (group != 32 && group != 64 && group != 128) return POLYSPEC_ERR_UNSUPPORTED;
     if (d % group != 0 || V > 0x7fffffff - 1024) return POLYSPEC_ERR_UNSUPPORTED;
-    (void)device_status;
     W4Problem q;
     q.hidden = hidden;
     q.codes = static_cast<const uint32_t*>(qweight);
@@ -338,7 +329,9 @@ polyspec_status polyspec_lm_head_quantized(const void* hidden, const void* qweig
     q.group = group;
     q.out = logits;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    const int nt = rows > 8 && stream_smem(d, 2) <= kMaxSmem ? 2 : 1;
+    if (rows > kStreamRows || stream_smem(d, rows > 8 ? 2 : 1) > kMaxSmem)
+        return cuda_failed(launch_w4_tensor(q, dt, device_status, s)) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
+    const int nt = rows > 8 ? 2 : 1;
     return cuda_failed(launch_stream(q, nt, dt, s)) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }
 

@@ -16,6 +16,9 @@ struct W4Problem {
     void* out;                      // [rows, V]
 };
 
+// The tensor-core kernel (w4_tensor.cu): any number of rows.
+cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* device_status, cudaStream_t stream);
+
 namespace w4 {
 
 // The eight weights of a word as four bf16 pairs (0,1) (2,3) (4,5) (6,7), the zero point subtracted.

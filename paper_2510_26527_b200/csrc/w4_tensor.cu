@@ -1,0 +1,416 @@
+// LM-head projection with 4-bit weights on the fifth-generation tensor cores, for more rows than the streaming kernel takes
+// (formula, numerics and weight format: w4_head.cu).
+//
+// The vocabulary is the MMA's M axis (128 entries per tile = the 128 lanes of tensor memory), the hidden rows its N axis.
+// The expanded weights never touch shared memory: dequantising warps read the packed tile, turn codes into exact bf16
+// integers q - z and write them with tcgen05.st into tensor memory, from where the MMA takes its A operand.  Each group of
+// weights is accumulated by the tensor core into a slot of its own, and the epilogue warps multiply the slot's fp32 sums by
+// the group's scale -- one scale per lane, since a lane is a vocabulary entry -- and add them to the running sums in their
+// registers.  So the scale costs one FMA per (entry, row, group) instead of a rounding per weight.
+//
+// Persistent, one CTA per SM; work items are (vocabulary tile, block of hidden rows), the row blocks of one tile neighbours so
+// that its codes come from L2 the second time.  Warp roles (18 warps):
+//   0        TMA producer: per K block of 128, the packed tile (128 rows x 64 bytes, 64-byte swizzle) and the hidden tile
+//            (two boxes of 64 elements, 128-byte swizzle)
+//   1        MMA issuer; allocates and frees tensor memory
+//   2..9     dequantisers, two warps per lane quarter, each half of the K block
+//   10..17   epilogue, two warps per lane quarter, each half of the columns
+// Tensor memory: kept[] A blocks of 64 columns in a ring, then accumulator slots of N columns in a ring.
+//
+// Every wait on an mbarrier is bounded: one that runs out raises an abort flag that all roles poll, sets POLYSPEC_ERR_TIMEOUT,
+// and the kernel still lets its copies land, frees tensor memory and returns.
+#include <cuda.h>
+
+#include <algorithm>
+#include <mutex>
+
+#include "polyspec_kernels.cuh"
+#include "tensor_device.cuh"
+#include "w4_kernels.cuh"
+
+namespace polyspec {
+namespace {
+
+using namespace tensordev;
+
+constexpr int kTileV = 128;
+constexpr int kBlock = 128;                             // K elements per block
+constexpr int kCodeBytes = kTileV * kBlock / 2;         // 8 KiB
+constexpr int kDequantWarps = 8, kEpilogueWarps = 8;
+constexpr int kThreads = 32 * (2 + kDequantWarps + kEpilogueWarps);
+constexpr int kMaxStages = 12, kMaxSlots = 8, kMaxABlocks = 4;
+constexpr int kTmemCols = 512;
+constexpr int kABlockCols = kBlock / 2;                 // two bf16 per 32-bit column
+constexpr int kMaxRowsPerItem = 144;                    // accumulators of an epilogue thread: half of them
+constexpr size_t kSmemLimit = 227 * 1024;
+
+struct TensorParams {
+    CUtensorMap map_codes;      // [V, d / 2] bytes, box {64, 128}
+    CUtensorMap map_hidden;     // [rows, d] bf16, box {64, N}
+    const __nv_bfloat16* scales;
+    const unsigned char* zeros;
+    void* out;
+    int out_bf16;
+    int rows, V, groups, group; // groups per row of d
+    int kblocks;
+    int row_blocks, items;
+    int stages, a_blocks, slots;
+    uint32_t idesc;
+    int32_t* status;
+};
+
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+// D (tensor memory) = or += A (tensor memory) B (shared memory descriptor)
+__device__ __forceinline__ void umma_from_tmem(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 db;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "mov.b64 db, {%2, %5};\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %3, p;\n\t}"
+        ::"r"(d), "r"(a), "r"(b_lo), "r"(idesc), "r"(accumulate), "r"(kDescHi) : "memory");
+}
+__device__ __forceinline__ void umma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+__device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+        ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+          "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
+          "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_ld8(uint32_t addr, uint32_t* r)
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr) : "memory");
+}
+
+__device__ __forceinline__ void raise_abort(int* abort_flag, int32_t* status)
+{
+    if (!*reinterpret_cast<volatile int*>(abort_flag) && status) atomicCAS(status, 0, static_cast<int>(POLYSPEC_ERR_TIMEOUT));
+    *reinterpret_cast<volatile int*>(abort_flag) = 1;
+}
+
+// A bounded wait that the whole warp passes or the whole warp gives up (what follows are warp-wide instructions).
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag)
+{
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+}
+
+// A position in a ring of n: its index and the parity a consumer waits for.
+struct Ring {
+    uint32_t at = 0, phase = 0;
+    __device__ __forceinline__ void next(uint32_t n)
+    {
+        if (++at == n) { at = 0; phase ^= 1u; }
+    }
+};
+
+// NC: columns (hidden rows) per epilogue warp, half of the item's N.
+template <int NC>
+__global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_constant__ TensorParams p)
+{
+    constexpr int N = 2 * NC;
+    constexpr uint32_t kHiddenBytes = N * kBlock * 2;
+    constexpr uint32_t kStage = kCodeBytes + kHiddenBytes;
+    extern __shared__ unsigned char smem_tensor[];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    __shared__ __align__(8) uint64_t barriers[2 * kMaxStages + 2 * kMaxABlocks + 2 * kMaxSlots];
+
+    const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const uint32_t tiles = (smem_addr(smem_tensor) + 1023u) & ~1023u;
+    const uint32_t full = smem_addr(barriers), empty = full + 8u * kMaxStages, a_full = empty + 8u * kMaxStages, a_empty = a_full + 8u * kMaxABlocks,
+                   acc_full = a_empty + 8u * kMaxABlocks, acc_empty = acc_full + 8u * kMaxSlots;
+    const uint32_t n_stages = p.stages, n_a = p.a_blocks, n_slots = p.slots;
+
+    if (threadIdx.x == 0) {
+        abort_flag = 0;
+        for (int i = 0; i < kMaxStages; ++i) { mbar_init(full + 8u * i, 1); mbar_init(empty + 8u * i, kDequantWarps + 1); }
+        for (int i = 0; i < kMaxABlocks; ++i) { mbar_init(a_full + 8u * i, kDequantWarps); mbar_init(a_empty + 8u * i, 1); }
+        for (int i = 0; i < kMaxSlots; ++i) { mbar_init(acc_full + 8u * i, 1); mbar_init(acc_empty + 8u * i, kEpilogueWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tmem_slot)), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot, tmem_acc = tmem + n_a * kABlockCols;
+    volatile int* abort_p = &abort_flag;
+    const int per_block = kBlock / p.group;             // groups per K block: 1, 2 or 4
+
+    if (warp == 0) {
+        // ------------------------------------------------------------------ TMA producer
+        Ring st;
+        st.phase = 1;                                   // a fresh "empty" barrier passes a wait on parity 1
+        uint32_t it = 0;
+        bool ok = true;
+        for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
+            const int v0 = item / p.row_blocks * kTileV, row0 = item % p.row_blocks * N;
+            for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
+                if (!warp_wait(empty + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
+                const uint32_t bar = full + 8u * st.at, dst = tiles + st.at * kStage;
+                if (elect_one()) {
+                    mbar_expect_tx(bar, kStage);
+                    tma_load(dst, &p.map_codes, kb * (kBlock / 2), v0, bar);
+                    tma_load(dst + kCodeBytes, &p.map_hidden, kb * kBlock, row0, bar);
+                    tma_load(dst + kCodeBytes + kHiddenBytes / 2, &p.map_hidden, kb * kBlock + 64, row0, bar);
+                }
+                __syncwarp();
+                st.next(n_stages);
+            }
+        }
+        if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
+        __syncwarp();
+        // the copies must have landed before the CTA may exit, also when it gives up
+        for (uint32_t q = it > n_stages ? it - n_stages : 0u; q < it; ++q)
+            for (uint32_t i = 0; i < kSpinLimitG; ++i)
+                if (mbar_try(full + 8u * (q % n_stages), (q / n_stages) & 1u)) break;
+    } else if (warp == 1) {
+        // ------------------------------------------------------------------ MMA issuer
+        Ring st, ab, slot;
+        slot.phase = 1;
+        bool ok = true;
+        uint32_t last_stage = 0, last_stage_phase = 0, last_a = 0, last_a_phase = 0;
+        const int mmas = p.group / 16;                  // MMAs per group
+        for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
+            int groups_left = p.groups;
+            for (int kb = 0; ok && kb < p.kblocks; ++kb, groups_left -= per_block) {
+                if (!warp_wait(full + 8u * st.at, st.phase, abort_p) || !warp_wait(a_full + 8u * ab.at, ab.phase, abort_p)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t b_lo = smem_desc_lo(tiles + st.at * kStage + kCodeBytes);
+                const uint32_t a = tmem + ab.at * kABlockCols;
+                const int n = min(per_block, groups_left);
+                for (int gi = 0; gi < n; ++gi) {
+                    if (!warp_wait(acc_empty + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
+                    tc_fence_after();
+                    if (elect_one()) {
+                        for (int m = 0; m < mmas; ++m) {
+                            const int kk = gi * mmas + m;           // 16-element slice of the block
+                            umma_from_tmem(tmem_acc + slot.at * N, a + kk * 8, b_lo + (kk >> 2) * (kHiddenBytes / 2 >> 4) + (kk & 3) * 2, p.idesc, m != 0);
+                        }
+                        umma_commit(acc_full + 8u * slot.at);
+                    }
+                    __syncwarp();
+                    slot.next(n_slots);
+                }
+                if (!ok) break;
+                if (elect_one()) {
+                    umma_commit(empty + 8u * st.at);
+                    umma_commit(a_empty + 8u * ab.at);
+                }
+                __syncwarp();
+                last_stage = st.at; last_stage_phase = st.phase;
+                last_a = ab.at; last_a_phase = ab.phase;
+                st.next(n_stages);
+                ab.next(n_a);
+            }
+        }
+        // the last commits arrive on barriers of this CTA: it must not exit before
+        if (ok) ok = warp_wait(empty + 8u * last_stage, last_stage_phase, abort_p) && warp_wait(a_empty + 8u * last_a, last_a_phase, abort_p);
+        if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
+    } else if (warp < 2 + kDequantWarps) {
+        // ------------------------------------------------------------------ dequantisers
+        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const int r = quarter * 32 + lane;              // row of the tile
+        Ring st, ab;
+        ab.phase = 1;
+        bool ok = true;
+        const uint32_t swizzle = (static_cast<uint32_t>(r) >> 1) & 3u;
+        for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
+            const size_t v = static_cast<size_t>(min(item / p.row_blocks * kTileV + r, p.V - 1));
+            const unsigned char* zero = p.zeros ? p.zeros + v * p.groups : nullptr;
+            // the zero points of the two 32-element runs this thread expands, one block ahead
+            auto magic_of = [&](int kb, int run) {
+                const int g = min(kb * per_block + (half * 2 + run) * 32 / p.group, p.groups - 1);
+                return 0x43004300u | (zero ? (__ldg(zero + g) & 15u) * 0x00010001u : 0x00080008u);
+            };
+            uint32_t magic[2] = {magic_of(0, 0), magic_of(0, 1)};
+            for (int kb = 0; kb < p.kblocks; ++kb) {
+                uint32_t next[2] = {magic[0], magic[1]};
+                if (kb + 1 < p.kblocks) { next[0] = magic_of(kb + 1, 0); next[1] = magic_of(kb + 1, 1); }
+                if (!warp_wait(full + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
+                uint32_t w[8];
+                const uint32_t row = tiles + st.at * kStage + static_cast<uint32_t>(r) * 64u;
+#pragma unroll
+                for (int c = 0; c < 2; ++c)
+                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[4 * c]), "=r"(w[4 * c + 1]), "=r"(w[4 * c + 2]), "=r"(w[4 * c + 3])
+                                 : "r"(row + (((half * 2 + c) ^ swizzle) << 4)));
+                uint32_t x[32];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t pairs[4];
+                    w4::expand(w[i], magic[i >> 2], pairs);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[4 * i + j] = pairs[j];
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive_local(empty + 8u * st.at);           // the codes are in registers
+                st.next(n_stages);
+                if (!warp_wait(a_empty + 8u * ab.at, ab.phase, abort_p)) { ok = false; break; }
+                tc_fence_after();
+                tmem_st32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + ab.at * kABlockCols + half * 32, x);
+                tmem_st_wait();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_local(a_full + 8u * ab.at);
+                ab.next(n_a);
+                magic[0] = next[0];
+                magic[1] = next[1];
+            }
+        }
+        if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
+    } else {
+        // ------------------------------------------------------------------ epilogue
+        const int quarter = warp & 3, half = (warp - 2 - kDequantWarps) >> 2;
+        Ring slot;
+        bool ok = true;
+        const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + half * NC;
+        for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
+            const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * N + half * NC;
+            const __nv_bfloat16* scale = p.scales + static_cast<size_t>(min(v, p.V - 1)) * p.groups;
+            float sum[NC];
+#pragma unroll
+            for (int i = 0; i < NC; ++i) sum[i] = 0.0f;
+            float s = __bfloat162float(scale[0]);
+            for (int g = 0; g < p.groups; ++g) {
+                const float next = __bfloat162float(scale[min(g + 1, p.groups - 1)]);
+                if (!warp_wait(acc_full + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t t = t0 + slot.at * N;
+#pragma unroll
+                for (int c = 0; c < NC; c += 24) {
+                    uint32_t x[24];
+#pragma unroll
+                    for (int q = 0; q < 24; q += 8)
+                        if (c + q < NC) tmem_ld8(t + c + q, x + q);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 24; ++i)
+                        if (c + i < NC) sum[c + i] = fmaf(s, __uint_as_float(x[i]), sum[c + i]);
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_local(acc_empty + 8u * slot.at);
+                slot.next(n_slots);
+                s = next;
+            }
+            if (!ok || v >= p.V) continue;
+            const int n = min(NC, p.rows - row0);
+#pragma unroll
+            for (int i = 0; i < NC; ++i) {
+                if (i >= n) continue;
+                const size_t at = static_cast<size_t>(row0 + i) * p.V + v;
+                if (p.out_bf16) w4::store_logit<POLYSPEC_BF16>(p.out, at, sum[i]);
+                else w4::store_logit<POLYSPEC_F32>(p.out, at, sum[i]);
+            }
+        }
+        if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
+    }
+
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    if (warp == 1) {
+        if (*abort_p) __nanosleep(1000000);             // giving up: MMAs in flight get a bounded moment
+        __syncwarp();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
+std::mutex g_mutex;
+EncodeTiledFn g_encode = nullptr;
+
+bool encode(CUtensorMap* map, CUtensorMapDataType type, const void* base, size_t inner, size_t outer, size_t pitch, int box_inner, int box_outer,
+            CUtensorMapSwizzle swizzle)
+{
+    const cuuint64_t dims[2] = {inner, outer};
+    const cuuint64_t strides[1] = {pitch};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(box_inner), static_cast<cuuint32_t>(box_outer)};
+    const cuuint32_t one[2] = {1, 1};
+    return g_encode(map, type, 2, const_cast<void*>(base), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
+                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int NC>
+cudaError_t launch_nc(TensorParams& p, int grid, cudaStream_t stream)
+{
+    constexpr size_t stage = kCodeBytes + static_cast<size_t>(2 * NC) * kBlock * 2;
+    p.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemLimit - 4096) / stage));
+    const size_t smem = 1024 + p.stages * stage;
+    // tensor memory: two blocks of A at least, then as many accumulator slots as fit
+    p.a_blocks = 2 * NC * 4 + 4 * kABlockCols <= kTmemCols ? 4 : 2;
+    p.slots = std::min(kMaxSlots, (kTmemCols - p.a_blocks * kABlockCols) / (2 * NC));
+    cudaError_t e = cudaFuncSetAttribute(w4_tensor_kernel<NC>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    if (e != cudaSuccess) return e;
+    w4_tensor_kernel<NC><<<grid, kThreads, smem, stream>>>(p);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* device_status, cudaStream_t stream)
+{
+    {
+        std::lock_guard<std::mutex> lock(g_mutex);
+        if (!g_encode) {
+            const cudaError_t e = find_encoder(&g_encode);
+            if (e != cudaSuccess) return e;
+        }
+    }
+    int dev = 0, sms = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (e != cudaSuccess) return e;
+    TensorParams p;
+    p.scales = static_cast<const __nv_bfloat16*>(q.scales);
+    p.zeros = q.zeros;
+    p.out = q.out;
+    p.out_bf16 = dt == POLYSPEC_BF16;
+    p.rows = q.rows;
+    p.V = q.V;
+    p.group = q.group;
+    p.groups = q.d / q.group;
+    p.kblocks = (q.d + kBlock - 1) / kBlock;
+    p.status = device_status;
+    p.row_blocks = (q.rows + kMaxRowsPerItem - 1) / kMaxRowsPerItem;
+    const int cols = (q.rows + p.row_blocks - 1) / p.row_blocks;
+    const int nc = (cols + 15) / 16 * 8;                // N in steps of 16
+    const int n = nc <= 32 ? 2 * nc : nc <= 48 ? 96 : nc <= 64 ? 128 : 144;
+    p.row_blocks = (q.rows + n - 1) / n;
+    const long long items = static_cast<long long>((q.V + kTileV - 1) / kTileV) * p.row_blocks;
+    if (items > 0x7fffffffLL) return cudaErrorInvalidValue;
+    p.items = static_cast<int>(items);
+    // D fp32, A and B bf16, both K-major, M = 128, N = n
+    p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(kTileV >> 4) << 24);
+    if (!encode(&p.map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, q.codes, q.d / 2, q.V, q.d / 2, kBlock / 2, kTileV, CU_TENSOR_MAP_SWIZZLE_64B) ||
+        !encode(&p.map_hidden, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, q.hidden, q.d, q.rows, static_cast<size_t>(q.d) * 2, 64, n, CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorInvalidValue;
+    const int grid = std::min(sms, p.items);
+    switch (n) {
+        case 16: return launch_nc<8>(p, grid, stream);
+        case 32: return launch_nc<16>(p, grid, stream);
+        case 48: return launch_nc<24>(p, grid, stream);
+        case 64: return launch_nc<32>(p, grid, stream);
+        case 96: return launch_nc<48>(p, grid, stream);
+        case 128: return launch_nc<64>(p, grid, stream);
+        default: return launch_nc<72>(p, grid, stream);
+    }
+}
+
+}  // namespace polyspec
