@@ -11,11 +11,13 @@
 // HBM-bound: every logit is read and written once, except that a vector of eight entries that the mask forbids as a whole
 // is written without being read, and that in place (out == logits) only what a control touches moves at all.
 // A CTA owns a slice of the vocabulary of one sequence and walks rows of the block.  It counts the history's tokens that
-// fall into its slice in shared memory once (32-bit words: bit 31 seen in the prompt, bit 30 biased, below them n(v)),
-// so the counts cost one read of the history per slice from L2 and no memory traffic.  Every vector of the slice belongs
-// to one thread for all rows: which of its vectors hold anything is a few bits in a register, and the drafted token that
-// joins the context between two rows is counted by its owner without a barrier.  Counting with integer atomics and adding
-// listed biases in list order make the result independent of timing.
+// fall into its slice in shared memory once (a 32-bit word per entry: bits 31..29 flags, below them n(v)), and whoever is first to touch an
+// entry puts it on a list.  Rows are then streamed as vectors with nothing but the mask applied, and the few listed entries
+// are computed and stored one by one after them: a text of thousands of tokens touches a few entries of every 256 a warp
+// moves, so computing them where the vectors pass by had the whole warp take the slow path almost every time.
+// Counting with integer atomics and adding listed biases in list order make the result independent of timing.
+#include <cuda_bf16.h>
+
 #include <algorithm>
 
 #include "polyspec_kernels.cuh"
@@ -26,7 +28,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVec = 8;                                 // entries per vector: one byte of the mask
-constexpr uint32_t kSeenInPrompt = 1u << 31, kBiased = 1u << 30, kCountMask = kBiased - 1;
+constexpr uint32_t kSeenInPrompt = 1u << 31, kBiased = 1u << 30, kDrafted = 1u << 29, kCountMask = kDrafted - 1;
 
 struct ControlParams {
     const void* logits;
@@ -45,33 +47,32 @@ __device__ __forceinline__ void bad_input(int32_t* status)
     if (status) atomicCAS(status, 0, static_cast<int>(POLYSPEC_ERR_BAD_INPUT_ON_DEVICE));
 }
 
+// Four mask bits as the top bits of four bytes (the product puts bit i at 8 i + 7; other bits are not looked at).
+__device__ __forceinline__ uint32_t spread4(uint32_t bits) { return (bits & 15u) * 0x10204080u; }
+
+// Each byte of the result is a byte's top bit eight times: nibble i of the selector, less 8, says which.
+__device__ __forceinline__ uint32_t top_bits(uint32_t x, uint32_t selector)
+{
+    uint32_t r;
+    asm("prmt.b32 %0, %1, 0, %2;" : "=r"(r) : "r"(x), "r"(selector));
+    return r;
+}
+
 // Eight logits as raw 16-byte words: one for 2-byte types, two for 4-byte types.
 template <int DT> struct Vec8;
 template <> struct Vec8<POLYSPEC_BF16> {
     uint4 a;
     __device__ __forceinline__ void load(const void* p, size_t e) { a = *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + e * 2); }
     __device__ __forceinline__ void store(void* p, size_t e) const { *reinterpret_cast<uint4*>(static_cast<char*>(p) + e * 2) = a; }
-    __device__ __forceinline__ void fill_neg_inf() { a = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
+    // entries whose bit is clear become -inf, whatever they hold
     __device__ __forceinline__ void forbid(uint32_t allowed)
     {
-        uint32_t* w = &a.x;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (!(allowed >> (2 * i) & 1u)) w[i] = (w[i] & 0xffff0000u) | 0xff80u;
-            if (!(allowed >> (2 * i + 1) & 1u)) w[i] = (w[i] & 0xffffu) | 0xff800000u;
-        }
-    }
-    __device__ __forceinline__ float get(int i) const
-    {
-        const uint32_t w = (&a.x)[i >> 1];
-        return __uint_as_float((i & 1) ? (w & 0xffff0000u) : (w << 16));
-    }
-    __device__ __forceinline__ void set(int i, float v)
-    {
-        uint32_t& w = (&a.x)[i >> 1];
-        unsigned short h;
-        asm("cvt.rn.bf16.f32 %0, %1;" : "=h"(h) : "f"(v));
-        w = (i & 1) ? ((w & 0xffffu) | (static_cast<uint32_t>(h) << 16)) : ((w & 0xffff0000u) | h);
+        const uint32_t lo = spread4(allowed), hi = spread4(allowed >> 4);
+        auto pick = [](uint32_t w, uint32_t keep) { return (w & keep) | (0xff80ff80u & ~keep); };
+        a.x = pick(a.x, top_bits(lo, 0x9988));
+        a.y = pick(a.y, top_bits(lo, 0xbbaa));
+        a.z = pick(a.z, top_bits(hi, 0x9988));
+        a.w = pick(a.w, top_bits(hi, 0xbbaa));
     }
 };
 template <> struct Vec8<POLYSPEC_F32> {
@@ -88,27 +89,63 @@ template <> struct Vec8<POLYSPEC_F32> {
         q[0] = a;
         q[1] = b;
     }
-    __device__ __forceinline__ void fill_neg_inf() { a = b = make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
-    __device__ __forceinline__ uint32_t& word(int i) { return i < 4 ? (&a.x)[i] : (&b.x)[i - 4]; }
     __device__ __forceinline__ void forbid(uint32_t allowed)
     {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (!(allowed >> i & 1u)) word(i) = 0xff800000u;
+        const uint32_t lo = spread4(allowed), hi = spread4(allowed >> 4);
+        auto pick = [](uint32_t w, uint32_t keep) { return (w & keep) | (0xff800000u & ~keep); };
+        a.x = pick(a.x, top_bits(lo, 0x8888));
+        a.y = pick(a.y, top_bits(lo, 0x9999));
+        a.z = pick(a.z, top_bits(lo, 0xaaaa));
+        a.w = pick(a.w, top_bits(lo, 0xbbbb));
+        b.x = pick(b.x, top_bits(hi, 0x8888));
+        b.y = pick(b.y, top_bits(hi, 0x9999));
+        b.z = pick(b.z, top_bits(hi, 0xaaaa));
+        b.w = pick(b.w, top_bits(hi, 0xbbbb));
     }
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float(i < 4 ? (&a.x)[i] : (&b.x)[i - 4]); }
-    __device__ __forceinline__ void set(int i, float v) { word(i) = __float_as_uint(v); }
 };
 
-// One sequence's slice [v0, v0 + n) of the vocabulary, counted into `count` (and `bias`) by the whole CTA.
-__device__ __forceinline__ void count_context(const ControlParams& p, int b, int v0, int n, bool report, uint32_t* count, float* bias)
+template <int DT> __device__ __forceinline__ float load_logit(const void* p, size_t e)
+{
+    if (DT == POLYSPEC_F32) return static_cast<const float*>(p)[e];
+    return __uint_as_float(static_cast<uint32_t>(static_cast<const unsigned short*>(p)[e]) << 16);
+}
+template <int DT> __device__ __forceinline__ void store_logit(void* p, size_t e, float x)
+{
+    if (DT == POLYSPEC_F32) static_cast<float*>(p)[e] = x;
+    else static_cast<__nv_bfloat16*>(p)[e] = __float2bfloat16_rn(x);
+}
+
+// What a CTA knows of its slice.
+struct Slice {
+    uint32_t* count;            // [slice]
+    float* bias;                // [slice] or nullptr
+    unsigned short* list;       // [slice]: the touched entries
+    int* n_list;
+    const int32_t* draft;       // [rows - 1]: entries of the slice the drafted tokens are, -1 where they lie outside
+};
+
+// One sequence's slice [v0, v0 + n) of the vocabulary, counted by the whole CTA.
+__device__ __forceinline__ void count_context(const ControlParams& p, int b, int v0, int n, bool report, const Slice& s, int32_t* drafted)
 {
     const int tid = threadIdx.x;
-    for (int i = tid; i < n; i += kThreads) count[i] = 0;
-    if (bias)
-        for (int i = tid; i < n; i += kThreads) bias[i] = 0.0f;
+    for (int i = tid; i < n / 4; i += kThreads) reinterpret_cast<uint4*>(s.count)[i] = make_uint4(0, 0, 0, 0);      // n is a multiple of 8
+    if (s.bias)
+        for (int i = tid; i < n / 4; i += kThreads) reinterpret_cast<uint4*>(s.bias)[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) *s.n_list = 0;
     __syncthreads();
-    const int first = p.c.vocab_begin + v0;
+    const unsigned first = static_cast<unsigned>(p.c.vocab_begin + v0);
+    // the first to touch an entry lists it
+    auto touch = [&](unsigned at, uint32_t was) {
+        if (was == 0) s.list[atomicAdd(s.n_list, 1)] = static_cast<unsigned short>(at);
+    };
+    if (p.draft && tid < p.rows - 1) {
+        const int t = p.draft[static_cast<size_t>(b) * p.k + tid];
+        if (report && t >= p.c.vocab_size) bad_input(p.status);
+        const unsigned at = static_cast<unsigned>(t) - first;
+        const bool mine = t >= 0 && at < static_cast<unsigned>(n);
+        drafted[tid] = mine ? static_cast<int>(at) : -1;
+        if (mine) touch(at, atomicOr(&s.count[at], kDrafted));
+    }
     if (p.c.history) {
         int len = p.c.history_len ? p.c.history_len[b] : p.c.history_cap;
         int prompt = p.c.prompt_len ? p.c.prompt_len[b] : 0;
@@ -118,11 +155,8 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
         const int32_t* text = p.c.history + static_cast<size_t>(b) * p.c.history_cap;
         auto add = [&](int i, int t) {
             if (report && t >= p.c.vocab_size) bad_input(p.status);
-            const unsigned at = static_cast<unsigned>(t) - static_cast<unsigned>(first);
-            if (t >= 0 && at < static_cast<unsigned>(n)) {
-                if (i < prompt) atomicOr(&count[at], kSeenInPrompt);
-                else atomicAdd(&count[at], 1u);
-            }
+            const unsigned at = static_cast<unsigned>(t) - first;
+            if (t >= 0 && at < static_cast<unsigned>(n)) touch(at, i < prompt ? atomicOr(&s.count[at], kSeenInPrompt) : atomicAdd(&s.count[at], 1u));
         };
         int i = tid;
         for (; i + 7 * kThreads < len; i += 8 * kThreads) {
@@ -134,30 +168,31 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
         }
         for (; i < len; i += kThreads) add(i, text[i]);
     }
-    if (bias && tid < 32) {
-        // one warp walks the list 32 entries at a time; entries of one batch that name the same token are summed by the
-        // first of them in list order
+    if (s.bias && tid >= kThreads - 32) {
+        // one warp walks the list 32 biases at a time; those of one batch that name the same token are summed, in list order,
+        // by the first of them
+        const int lane = tid & 31;
         const int32_t* toks = p.c.bias_tokens + static_cast<size_t>(b) * p.c.n_bias;
         const float* vals = p.c.bias_values + static_cast<size_t>(b) * p.c.n_bias;
         for (int i0 = 0; i0 < p.c.n_bias; i0 += 32) {
-            const int i = i0 + tid;
+            const int i = i0 + lane;
             const int t = i < p.c.n_bias ? toks[i] : -1;
             const float x = i < p.c.n_bias ? vals[i] : 0.0f;
             if (report && t >= p.c.vocab_size) bad_input(p.status);
-            const unsigned at = static_cast<unsigned>(t) - static_cast<unsigned>(first);
+            const unsigned at = static_cast<unsigned>(t) - first;
             const bool mine = t >= 0 && at < static_cast<unsigned>(n);
             const unsigned any = __ballot_sync(0xffffffffu, mine);
             if (!any) continue;
-            const unsigned same = __match_any_sync(0xffffffffu, mine ? t : -1 - tid);
-            float sum = mine ? bias[at] : 0.0f;
+            const unsigned same = __match_any_sync(0xffffffffu, mine ? t : -1 - lane);
+            float sum = mine ? s.bias[at] : 0.0f;
             for (unsigned left = any; left; left &= left - 1) {      // list order, every lane the same number of turns
                 const int src = __ffs(left) - 1;
                 const float y = __shfl_sync(0xffffffffu, x, src);
                 if (same >> src & 1u) sum += y;
             }
-            if (mine && tid == __ffs(same) - 1) {
-                bias[at] = sum;
-                atomicOr(&count[at], kBiased);
+            if (mine && lane == __ffs(same) - 1) {
+                s.bias[at] = sum;
+                touch(at, atomicOr(&s.count[at], kBiased));
             }
             __syncwarp();
         }
@@ -166,11 +201,13 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
 }
 
 // VPT vectors of eight entries per thread: a slice of kThreads * VPT * 8 entries.
-// COUNTS: penalties or biases are there (the counts are needed); otherwise only a mask.
+// COUNTS: penalties or biases are there; otherwise only a mask.
 template <int DT, int VPT, bool COUNTS>
 __global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
 {
     extern __shared__ uint4 smem_controls[];
+    __shared__ int n_list;
+    __shared__ int32_t drafted[kMaxK];
     constexpr int kSlice = kThreads * VPT * kVec;
     const int tid = threadIdx.x;
     int at = blockIdx.x;
@@ -180,23 +217,20 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
     const int v0 = slice * kSlice;
     const int n = min(kSlice, p.V - v0);
     const int j0 = group * p.rows_per_group, j1 = min(p.rows, j0 + p.rows_per_group);
-    const bool report = slice == 0 && group == 0;
     const bool in_place = p.out == p.logits;
+    const unsigned char* mask = reinterpret_cast<const unsigned char*>(p.c.mask);
+    const bool streams = !in_place || mask;             // whether vectors move at all
 
-    uint32_t* count = reinterpret_cast<uint32_t*>(smem_controls);
-    float* bias = COUNTS && p.c.bias_tokens ? reinterpret_cast<float*>(count + kSlice) : nullptr;
-    uint32_t touched = 0;                               // bit u: vector u * kThreads + tid holds a counted or biased entry
+    Slice s;
     float r = 1.0f, f = 0.0f, pr = 0.0f;
+    int listed = 0;
     if (COUNTS) {
-        count_context(p, b, v0, n, report, count, bias);
-#pragma unroll
-        for (int u = 0; u < VPT; ++u) {
-            const int e = (u * kThreads + tid) * kVec;
-            if (e < n) {
-                const uint4 x = *reinterpret_cast<const uint4*>(count + e), y = *reinterpret_cast<const uint4*>(count + e + 4);
-                if (x.x | x.y | x.z | x.w | y.x | y.y | y.z | y.w) touched |= 1u << u;
-            }
-        }
+        const bool report = slice == 0 && group == 0;
+        s.count = reinterpret_cast<uint32_t*>(smem_controls);
+        s.list = reinterpret_cast<unsigned short*>(s.count + kSlice);
+        s.bias = p.c.bias_tokens ? reinterpret_cast<float*>(s.list + kSlice) : nullptr;
+        s.n_list = &n_list;
+        s.draft = drafted;
         if (p.c.repetition) r = p.c.repetition[b];
         if (p.c.frequency) f = p.c.frequency[b];
         if (p.c.presence) pr = p.c.presence[b];
@@ -204,22 +238,10 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
             if (report && tid == 0) bad_input(p.status);
             r = 1.0f;
         }
-    }
-    // the drafted token at position j joins the context of the rows after it; its owner counts it
-    auto join = [&](int j) {
-        const int t = p.draft[static_cast<size_t>(b) * p.k + j];
-        const unsigned e = static_cast<unsigned>(t) - static_cast<unsigned>(p.c.vocab_begin + v0);
-        if (t >= 0 && e < static_cast<unsigned>(n) && static_cast<int>(e / kVec) % kThreads == tid) {
-            count[e] += 1u;
-            touched |= 1u << (e / kVec / kThreads);
-        }
-    };
-    if (COUNTS && p.draft) {
-        if (report && tid + 1 < p.rows && p.draft[static_cast<size_t>(b) * p.k + tid] >= p.c.vocab_size) bad_input(p.status);
-        for (int j = 0; j < j0; ++j) join(j);
+        count_context(p, b, v0, n, report, s, drafted);
+        listed = n_list;
     }
 
-    const unsigned char* mask = reinterpret_cast<const unsigned char*>(p.c.mask);
     auto mask_of = [&](int j, uint32_t (&m)[VPT]) {
 #pragma unroll
         for (int u = 0; u < VPT; ++u) {
@@ -232,43 +254,42 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
     mask_of(j0, allowed);
     for (int j = j0; j < j1; ++j) {
         const size_t row = (static_cast<size_t>(b) * p.rows + j) * p.V + v0;
-        Vec8<DT> z[VPT];
-        uint32_t next[VPT];
+        if (streams) {
+            Vec8<DT> z[VPT];
+            uint32_t next[VPT];
 #pragma unroll
-        for (int u = 0; u < VPT; ++u) {
-            const int e = (u * kThreads + tid) * kVec;
-            const bool moves = !in_place || (touched >> u & 1u) || allowed[u] != 0xffu;
-            if (e < n && moves && allowed[u] != 0) z[u].load(p.logits, row + e);
-        }
-        mask_of(j + 1, next);
-#pragma unroll
-        for (int u = 0; u < VPT; ++u) {
-            const int e = (u * kThreads + tid) * kVec;
-            const bool moves = !in_place || (touched >> u & 1u) || allowed[u] != 0xffu;
-            if (e >= n || !moves) continue;
-            if (allowed[u] == 0) {
-                z[u].fill_neg_inf();
-            } else {
-                if (COUNTS && (touched >> u & 1u)) {
-#pragma unroll
-                    for (int i = 0; i < kVec; ++i) {
-                        const uint32_t w = count[e + i];
-                        if (w == 0) continue;
-                        float x = z[u].get(i);
-                        const uint32_t times = w & kCountMask;
-                        if (times || (w & kSeenInPrompt)) x = x > 0.0f ? x / r : x * r;
-                        if (times) x = x - f * static_cast<float>(times) - pr;
-                        if (w & kBiased) x += bias[e + i];
-                        z[u].set(i, x);
-                    }
-                }
-                if (allowed[u] != 0xffu) z[u].forbid(allowed[u]);
+            for (int u = 0; u < VPT; ++u) {
+                const int e = (u * kThreads + tid) * kVec;
+                if (e < n && allowed[u] != 0 && (!in_place || allowed[u] != 0xffu)) z[u].load(p.logits, row + e);
             }
-            z[u].store(p.out, row + e);
-        }
-        if (COUNTS && p.draft && j + 1 < j1) join(j);
+            mask_of(j + 1, next);
 #pragma unroll
-        for (int u = 0; u < VPT; ++u) allowed[u] = next[u];
+            for (int u = 0; u < VPT; ++u) {
+                const int e = (u * kThreads + tid) * kVec;
+                if (e < n && (!in_place || allowed[u] != 0xffu)) {
+                    if (allowed[u] != 0xffu) z[u].forbid(allowed[u]);
+                    z[u].store(p.out, row + e);
+                }
+                allowed[u] = next[u];
+            }
+        }
+        if (COUNTS && listed) {
+            if (streams) __syncthreads();               // the listed entries are stored over the vectors
+            for (int i = tid; i < listed; i += kThreads) {
+                const int e = s.list[i];
+                const uint32_t w = s.count[e];
+                uint32_t times = w & kCountMask;
+                if (w & kDrafted)
+                    for (int q = 0; q < j; ++q) times += s.draft[q] == e;
+                if (!times && !(w & (kSeenInPrompt | kBiased))) continue;          // drafted later than this row
+                if (mask && !(mask[(static_cast<size_t>(b) * p.rows + j) * p.mask_bytes + (v0 + e) / 8] >> (e & 7) & 1u)) continue;
+                float x = load_logit<DT>(p.logits, row + e);
+                if (times || (w & kSeenInPrompt)) x = x > 0.0f ? x / r : x * r;
+                if (times) x = x - f * static_cast<float>(times) - pr;
+                if (w & kBiased) x += s.bias[e];
+                store_logit<DT>(p.out, row + e, x);
+            }
+        }
     }
 }
 
@@ -280,7 +301,7 @@ cudaError_t launch_vpt(ControlParams& p, bool counts, cudaStream_t stream)
     p.row_groups = (p.rows + p.rows_per_group - 1) / p.rows_per_group;
     const long long blocks = static_cast<long long>(p.slices) * p.row_groups * p.B;
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
-    const size_t smem = counts ? static_cast<size_t>(kSlice) * (p.c.bias_tokens ? 8 : 4) : 0;
+    const size_t smem = counts ? static_cast<size_t>(kSlice) * (p.c.bias_tokens ? 10 : 6) : 0;
     if (counts) {
         if (smem > 48 * 1024) {
             cudaError_t e = cudaFuncSetAttribute(logits_kernel<DT, VPT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
@@ -296,20 +317,19 @@ cudaError_t launch_vpt(ControlParams& p, bool counts, cudaStream_t stream)
 template <int DT>
 cudaError_t launch_controls(ControlParams& p, bool counts, cudaStream_t stream)
 {
-    // Few sequences: smaller slices, then fewer rows per CTA, until there are about four CTAs for each of 148 SMs; many:
-    // the largest slice and all rows of a sequence, so that the history is counted as seldom as possible.
-    const long long want = 4 * 148;
+    // Few sequences: smaller slices, then fewer rows per CTA, until there are about eight CTAs for each of 148 SMs; many: the
+    // largest slice and all rows of a sequence, so that the history is counted as seldom as possible.  Without counts there
+    // is nothing to share between rows, and a CTA takes one.
+    const long long want = 8 * 148;
     auto ctas = [&](int vpt, int rpg) {
         const long long s = (p.V + kThreads * vpt * kVec - 1) / (kThreads * vpt * kVec);
         return s * ((p.rows + rpg - 1) / rpg) * p.B;
     };
-    int vpt = 4, rpg = p.rows;
+    int vpt = 2, rpg = counts ? p.rows : 1;
     while (vpt > 1 && ctas(vpt, rpg) < want) vpt >>= 1;
     while (rpg > 1 && ctas(vpt, rpg) < want) rpg = (rpg + 1) / 2;
     p.rows_per_group = rpg;
-    if (vpt == 4) return launch_vpt<DT, 4>(p, counts, stream);
-    if (vpt == 2) return launch_vpt<DT, 2>(p, counts, stream);
-    return launch_vpt<DT, 1>(p, counts, stream);
+    return vpt == 2 ? launch_vpt<DT, 2>(p, counts, stream) : launch_vpt<DT, 1>(p, counts, stream);
 }
 
 }  // namespace

@@ -103,15 +103,22 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
     uint32_t turn = 0;
     for (int tile = blockIdx.x + team * gridDim.x; tile < p.tiles; tile += teams * gridDim.x, turn ^= 1u) {
         const uint32_t* codes[4];
-        const __nv_bfloat16* scale[4];
-        const unsigned char* zero[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {           // the lane's four entries: g, g + 8, g + 16, g + 24 (those past V read the last one)
-            const size_t v = static_cast<size_t>(min(tile * kTileS + i * 8 + g, p.V - 1));
-            codes[i] = p.codes + v * (p.d / 8);
-            scale[i] = p.scales + v * p.groups;
-            zero[i] = p.zeros ? p.zeros + v * p.groups : nullptr;
-        }
+        for (int i = 0; i < 4; ++i)             // the lane's four entries: g, g + 8, g + 16, g + 24 (those past V read the last one)
+            codes[i] = p.codes + static_cast<size_t>(min(tile * kTileS + i * 8 + g, p.V - 1)) * (p.d / 8);
+        // scale and zero point of entry g + 8 t, which the quad's lanes hand one another when they use them
+        const size_t own = static_cast<size_t>(min(tile * kTileS + t * 8 + g, p.V - 1)) * p.groups;
+        struct Raw { unsigned short scale[GPC]; unsigned char zero[GPC]; };
+        auto load_raw = [&](int c) {
+            Raw r;
+#pragma unroll
+            for (int gi = 0; gi < GPC; ++gi) {
+                const int group = GPC == 1 ? c : min(c * GPC + gi, p.groups - 1);
+                r.scale[gi] = __ldg(reinterpret_cast<const unsigned short*>(p.scales) + own + group);
+                r.zero[gi] = p.zeros ? __ldg(p.zeros + own + group) : 8;
+            }
+            return r;
+        };
         float sum[2][NT][4];
 #pragma unroll
         for (int m = 0; m < 2; ++m)
@@ -122,11 +129,14 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
 
         constexpr int kAhead = 2;               // chunks of codes in flight
         uint4 w[kAhead][4];
+        Raw raw[kAhead];
 #pragma unroll
         for (int a = 0; a < kAhead; ++a)
-            if (c_first + a < c_end)
+            if (c_first + a < c_end) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) w[a][i] = load_codes<G>(codes[i], c_first + a, t, p.groups - (c_first + a) * GPC);
+                raw[a] = load_raw(c_first + a);
+            }
         for (int c0 = c_first; c0 < c_end; c0 += kAhead) {
 #pragma unroll
             for (int a = 0; a < kAhead; ++a) {
@@ -135,9 +145,14 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
                 uint32_t x[4][4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) { x[i][0] = w[a][i].x; x[i][1] = w[a][i].y; x[i][2] = w[a][i].z; x[i][3] = w[a][i].w; }
-                if (c + kAhead < c_end)
+                uint32_t sz[GPC];
+#pragma unroll
+                for (int gi = 0; gi < GPC; ++gi) sz[gi] = static_cast<uint32_t>(raw[a].scale[gi]) << 16 | (raw[a].zero[gi] & 15u);
+                if (c + kAhead < c_end) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) w[a][i] = load_codes<G>(codes[i], c + kAhead, t, p.groups - (c + kAhead) * GPC);
+                    raw[a] = load_raw(c + kAhead);
+                }
                 const uint4* hid = smem_w4 + c * NT * 4 * 32 + lane;
 #pragma unroll
                 for (int gi = 0; gi < GPC; ++gi) {
@@ -147,8 +162,9 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
                     uint32_t z[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        s[i] = __bfloat162float(scale[i][group]);
-                        z[i] = 0x43004300u | (zero[i] ? (zero[i][group] & 15u) * 0x00010001u : 0x00080008u);
+                        const uint32_t x = __shfl_sync(0xffffffffu, sz[gi], g * 4 + i);
+                        s[i] = __uint_as_float(x & 0xffff0000u);
+                        z[i] = 0x43004300u | (x & 15u) * 0x00010001u;
                     }
                     float acc[2][NT][4];
 #pragma unroll

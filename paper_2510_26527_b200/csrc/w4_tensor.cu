@@ -235,15 +235,15 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_con
         for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
             const size_t v = static_cast<size_t>(min(item / p.row_blocks * kTileV + r, p.V - 1));
             const unsigned char* zero = p.zeros ? p.zeros + v * p.groups : nullptr;
-            // the zero points of the two 32-element runs this thread expands, one block ahead
-            auto magic_of = [&](int kb, int run) {
+            // the zero points of the two 32-element runs this thread expands, as loaded, two blocks ahead: arithmetic on a
+            // fresh load would wait for it
+            auto zero_of = [&](int kb, int run) -> uint32_t {
                 const int g = min(kb * per_block + (half * 2 + run) * 32 / p.group, p.groups - 1);
-                return 0x43004300u | (zero ? (__ldg(zero + g) & 15u) * 0x00010001u : 0x00080008u);
+                return zero ? __ldg(zero + g) : 8u;
             };
-            uint32_t magic[2] = {magic_of(0, 0), magic_of(0, 1)};
+            uint32_t z0[2] = {zero_of(0, 0), zero_of(0, 1)}, z1[2] = {zero_of(1, 0), zero_of(1, 1)};
             for (int kb = 0; kb < p.kblocks; ++kb) {
-                uint32_t next[2] = {magic[0], magic[1]};
-                if (kb + 1 < p.kblocks) { next[0] = magic_of(kb + 1, 0); next[1] = magic_of(kb + 1, 1); }
+                const uint32_t next[2] = {zero_of(kb + 2, 0), zero_of(kb + 2, 1)};
                 if (!warp_wait(full + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
                 uint32_t w[8];
                 const uint32_t row = tiles + st.at * kStage + static_cast<uint32_t>(r) * 64u;
@@ -251,6 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_con
                 for (int c = 0; c < 2; ++c)
                     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[4 * c]), "=r"(w[4 * c + 1]), "=r"(w[4 * c + 2]), "=r"(w[4 * c + 3])
                                  : "r"(row + (((half * 2 + c) ^ swizzle) << 4)));
+                const uint32_t magic[2] = {0x43004300u | (z0[0] & 15u) * 0x00010001u, 0x43004300u | (z0[1] & 15u) * 0x00010001u};
                 uint32_t x[32];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -270,8 +271,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_con
                 __syncwarp();
                 if (lane == 0) mbar_arrive_local(a_full + 8u * ab.at);
                 ab.next(n_a);
-                magic[0] = next[0];
-                magic[1] = next[1];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) { z0[i] = z1[i]; z1[i] = next[i]; }
             }
         }
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
@@ -287,12 +288,14 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_con
             float sum[NC];
 #pragma unroll
             for (int i = 0; i < NC; ++i) sum[i] = 0.0f;
-            float s = __bfloat162float(scale[0]);
+            // scales as loaded, two groups ahead (as the zero points above)
+            __nv_bfloat16 s0 = scale[0], s1 = scale[min(1, p.groups - 1)];
             for (int g = 0; g < p.groups; ++g) {
-                const float next = __bfloat162float(scale[min(g + 1, p.groups - 1)]);
+                const __nv_bfloat16 next = scale[min(g + 2, p.groups - 1)];
                 if (!warp_wait(acc_full + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t t = t0 + slot.at * N;
+                const float s = __bfloat162float(s0);
 #pragma unroll
                 for (int c = 0; c < NC; c += 24) {
                     uint32_t x[24];
@@ -308,7 +311,8 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_con
                 __syncwarp();
                 if (lane == 0) mbar_arrive_local(acc_empty + 8u * slot.at);
                 slot.next(n_slots);
-                s = next;
+                s0 = s1;
+                s1 = next;
             }
             if (!ok || v >= p.V) continue;
             const int n = min(NC, p.rows - row0);
