@@ -13,9 +13,11 @@
 //   0        TMA producer: per K block of 128, the packed tile (128 rows x 64 bytes, 64-byte swizzle) and the hidden tile
 //            (two boxes of 64 elements, 128-byte swizzle)
 //   1        MMA issuer; allocates and frees tensor memory
-//   2..9     dequantisers, two warps per lane quarter, each half of the K block
-//   10..17   epilogue, two warps per lane quarter, each half of the columns
-// Tensor memory: kept[] A blocks of 64 columns in a ring, then accumulator slots of N columns in a ring.
+//   then     dequantisers, in sets of four warps (one per lane quarter): a set takes every second or third K block, so that the
+//            latencies of one (shared-memory reads, tensor-memory stores, barriers) pass behind the arithmetic of another
+//   last     epilogue, one or two warps per lane quarter, each its share of the columns
+// Up to 64 rows, where expanding codes is what takes the time, three sets and four epilogue warps; above, two and eight.
+// Tensor memory: A blocks of 64 columns in a ring, then accumulator slots of N columns in a ring.
 //
 // Every wait on an mbarrier is bounded: one that runs out raises an abort flag that all roles poll, sets POLYSPEC_ERR_TIMEOUT,
 // and the kernel still lets its copies land, frees tensor memory and returns.
@@ -36,12 +38,11 @@ using namespace tensordev;
 constexpr int kTileV = 128;
 constexpr int kBlock = 128;                             // K elements per block
 constexpr int kCodeBytes = kTileV * kBlock / 2;         // 8 KiB
-constexpr int kDequantWarps = 8, kEpilogueWarps = 8;
-constexpr int kThreads = 32 * (2 + kDequantWarps + kEpilogueWarps);
+constexpr int kSetWarps = 4;                            // dequantising warps per K block
 constexpr int kMaxStages = 12, kMaxSlots = 8, kMaxABlocks = 4;
 constexpr int kTmemCols = 512;
 constexpr int kABlockCols = kBlock / 2;                 // two bf16 per 32-bit column
-constexpr int kMaxRowsPerItem = 144;                    // accumulators of an epilogue thread: half of them
+constexpr int kMaxRowsPerItem = 144;                    // an epilogue thread holds half of them as accumulators
 constexpr size_t kSmemLimit = 227 * 1024;
 
 struct TensorParams {
@@ -51,7 +52,7 @@ struct TensorParams {
     const unsigned char* zeros;
     void* out;
     int out_bf16;
-    int rows, V, groups, group; // groups per row of d
+    int rows, V, group, groups; // groups: of a whole row
     int kblocks;
     int row_blocks, items;
     int stages, a_blocks, slots;
@@ -117,11 +118,62 @@ struct Ring {
     }
 };
 
-// NC: columns (hidden rows) per epilogue warp, half of the item's N.
-template <int NC>
-__global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_constant__ TensorParams p)
+// The MMA issuer's whole run.  The number of groups per K block is a template argument so that a block's MMAs are straight-line
+// code on uniform registers: with the loop bounds read from the parameters the issue alone took 750 cycles per block.
+template <int N, int GROUPS>
+__device__ __forceinline__ bool issue_all(const TensorParams& p, uint32_t tiles, uint32_t tmem, uint32_t tmem_acc, uint32_t full, uint32_t empty,
+                                          uint32_t a_full, uint32_t a_empty, uint32_t acc_full, uint32_t acc_empty, volatile int* abort_p)
 {
-    constexpr int N = 2 * NC;
+    constexpr uint32_t kHiddenBytes = N * kBlock * 2, kStage = kCodeBytes + kHiddenBytes;
+    constexpr int kMmas = kBlock / 16 / GROUPS;         // per group
+    const uint32_t n_stages = p.stages, n_a = p.a_blocks, n_slots = p.slots;
+    Ring st, ab, slot;
+    slot.phase = 1;
+    uint32_t last_stage = 0, last_stage_phase = 0, last_a = 0, last_a_phase = 0;
+    for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
+        for (int kb = 0; kb < p.kblocks; ++kb) {
+            if (!warp_wait(full + 8u * st.at, st.phase, abort_p) || !warp_wait(a_full + 8u * ab.at, ab.phase, abort_p)) return false;
+            const uint32_t b_lo = smem_desc_lo(tiles + st.at * kStage + kCodeBytes);
+            const uint32_t a = tmem + ab.at * kABlockCols;
+#pragma unroll
+            for (int gi = 0; gi < GROUPS; ++gi) {
+                if (GROUPS > 1 && kb * GROUPS + gi >= p.groups) break;
+                if (!warp_wait(acc_empty + 8u * slot.at, slot.phase, abort_p)) return false;
+                tc_fence_after();
+                const uint32_t d = tmem_acc + slot.at * N;
+                if (elect_one()) {
+#pragma unroll
+                    for (int m = 0; m < kMmas; ++m) {
+                        const int kk = gi * kMmas + m;              // 16-element slice of the block
+                        umma_from_tmem(d, a + kk * 8, b_lo + (kk >> 2) * (kHiddenBytes / 2 >> 4) + (kk & 3) * 2, p.idesc, m != 0);
+                    }
+                    umma_commit(acc_full + 8u * slot.at);
+                }
+                __syncwarp();
+                slot.next(n_slots);
+            }
+            if (elect_one()) {
+                umma_commit(empty + 8u * st.at);
+                umma_commit(a_empty + 8u * ab.at);
+            }
+            __syncwarp();
+            last_stage = st.at; last_stage_phase = st.phase;
+            last_a = ab.at; last_a_phase = ab.phase;
+            st.next(n_stages);
+            ab.next(n_a);
+        }
+    }
+    // the last commits arrive on barriers of this CTA: it must not exit before
+    return warp_wait(empty + 8u * last_stage, last_stage_phase, abort_p) && warp_wait(a_empty + 8u * last_a, last_a_phase, abort_p);
+}
+
+constexpr int threads_of(int sets, int epi) { return 32 * (2 + kSetWarps * sets + epi); }
+
+// NC: columns (hidden rows) per epilogue warp; EPI: epilogue warps; SETS: sets of dequantising warps.
+template <int NC, int EPI, int SETS>
+__global__ void __launch_bounds__(threads_of(SETS, EPI), 1) w4_tensor_kernel(const __grid_constant__ TensorParams p)
+{
+    constexpr int N = NC * (EPI / 4);
     constexpr uint32_t kHiddenBytes = N * kBlock * 2;
     constexpr uint32_t kStage = kCodeBytes + kHiddenBytes;
     extern __shared__ unsigned char smem_tensor[];
@@ -137,9 +189,9 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_con
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int i = 0; i < kMaxStages; ++i) { mbar_init(full + 8u * i, 1); mbar_init(empty + 8u * i, kDequantWarps + 1); }
-        for (int i = 0; i < kMaxABlocks; ++i) { mbar_init(a_full + 8u * i, kDequantWarps); mbar_init(a_empty + 8u * i, 1); }
-        for (int i = 0; i < kMaxSlots; ++i) { mbar_init(acc_full + 8u * i, 1); mbar_init(acc_empty + 8u * i, kEpilogueWarps); }
+        for (int i = 0; i < kMaxStages; ++i) { mbar_init(full + 8u * i, 1); mbar_init(empty + 8u * i, kSetWarps + 1); }
+        for (int i = 0; i < kMaxABlocks; ++i) { mbar_init(a_full + 8u * i, kSetWarps); mbar_init(a_empty + 8u * i, 1); }
+        for (int i = 0; i < kMaxSlots; ++i) { mbar_init(acc_full + 8u * i, 1); mbar_init(acc_empty + 8u * i, EPI); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -183,75 +235,52 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_con
                 if (mbar_try(full + 8u * (q % n_stages), (q / n_stages) & 1u)) break;
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
-        Ring st, ab, slot;
-        slot.phase = 1;
-        bool ok = true;
-        uint32_t last_stage = 0, last_stage_phase = 0, last_a = 0, last_a_phase = 0;
-        const int mmas = p.group / 16;                  // MMAs per group
-        for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
-            int groups_left = p.groups;
-            for (int kb = 0; ok && kb < p.kblocks; ++kb, groups_left -= per_block) {
-                if (!warp_wait(full + 8u * st.at, st.phase, abort_p) || !warp_wait(a_full + 8u * ab.at, ab.phase, abort_p)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t b_lo = smem_desc_lo(tiles + st.at * kStage + kCodeBytes);
-                const uint32_t a = tmem + ab.at * kABlockCols;
-                const int n = min(per_block, groups_left);
-                for (int gi = 0; gi < n; ++gi) {
-                    if (!warp_wait(acc_empty + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
-                    tc_fence_after();
-                    if (elect_one()) {
-                        for (int m = 0; m < mmas; ++m) {
-                            const int kk = gi * mmas + m;           // 16-element slice of the block
-                            umma_from_tmem(tmem_acc + slot.at * N, a + kk * 8, b_lo + (kk >> 2) * (kHiddenBytes / 2 >> 4) + (kk & 3) * 2, p.idesc, m != 0);
-                        }
-                        umma_commit(acc_full + 8u * slot.at);
-                    }
-                    __syncwarp();
-                    slot.next(n_slots);
-                }
-                if (!ok) break;
-                if (elect_one()) {
-                    umma_commit(empty + 8u * st.at);
-                    umma_commit(a_empty + 8u * ab.at);
-                }
-                __syncwarp();
-                last_stage = st.at; last_stage_phase = st.phase;
-                last_a = ab.at; last_a_phase = ab.phase;
-                st.next(n_stages);
-                ab.next(n_a);
-            }
-        }
-        // the last commits arrive on barriers of this CTA: it must not exit before
-        if (ok) ok = warp_wait(empty + 8u * last_stage, last_stage_phase, abort_p) && warp_wait(a_empty + 8u * last_a, last_a_phase, abort_p);
+        bool ok;
+        if (per_block == 1) ok = issue_all<N, 1>(p, tiles, tmem, tmem_acc, full, empty, a_full, a_empty, acc_full, acc_empty, abort_p);
+        else if (per_block == 2) ok = issue_all<N, 2>(p, tiles, tmem, tmem_acc, full, empty, a_full, a_empty, acc_full, acc_empty, abort_p);
+        else ok = issue_all<N, 4>(p, tiles, tmem, tmem_acc, full, empty, a_full, a_empty, acc_full, acc_empty, abort_p);
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
-    } else if (warp < 2 + kDequantWarps) {
+    } else if (warp < 2 + kSetWarps * SETS) {
         // ------------------------------------------------------------------ dequantisers
-        const int quarter = warp & 3, half = (warp - 2) >> 2;
+        const int quarter = warp & 3, set = (warp - 2) >> 2;
         const int r = quarter * 32 + lane;              // row of the tile
         Ring st, ab;
         ab.phase = 1;
         bool ok = true;
         const uint32_t swizzle = (static_cast<uint32_t>(r) >> 1) & 3u;
+        int turn = 0;                                   // whose K block the next one is
         for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
             const size_t v = static_cast<size_t>(min(item / p.row_blocks * kTileV + r, p.V - 1));
             const unsigned char* zero = p.zeros ? p.zeros + v * p.groups : nullptr;
-            // the zero points of the two 32-element runs this thread expands, as loaded, two blocks ahead: arithmetic on a
-            // fresh load would wait for it
-            auto zero_of = [&](int kb, int run) -> uint32_t {
-                const int g = min(kb * per_block + (half * 2 + run) * 32 / p.group, p.groups - 1);
-                return zero ? __ldg(zero + g) : 8u;
+            // the zero points of a block's groups, as loaded, for this set's next block: arithmetic on a fresh load would
+            // wait for it
+            uint32_t z[4];
+            auto load_zeros = [&](int kb) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) z[i] = zero && i < per_block ? __ldg(zero + min(kb * per_block + i, p.groups - 1)) : 8u;
             };
-            uint32_t z0[2] = {zero_of(0, 0), zero_of(0, 1)}, z1[2] = {zero_of(1, 0), zero_of(1, 1)};
-            for (int kb = 0; kb < p.kblocks; ++kb) {
-                const uint32_t next[2] = {zero_of(kb + 2, 0), zero_of(kb + 2, 1)};
+            const int first = (set - turn + SETS) % SETS;
+            load_zeros(first);
+            for (int kb = 0; kb < p.kblocks; ++kb, turn = turn + 1 == SETS ? 0 : turn + 1) {
+                if (turn != set) {
+                    st.next(n_stages);
+                    ab.next(n_a);
+                    continue;
+                }
                 if (!warp_wait(full + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
-                uint32_t w[8];
+                uint32_t w[16];
                 const uint32_t row = tiles + st.at * kStage + static_cast<uint32_t>(r) * 64u;
 #pragma unroll
-                for (int c = 0; c < 2; ++c)
+                for (int c = 0; c < 4; ++c)
                     asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[4 * c]), "=r"(w[4 * c + 1]), "=r"(w[4 * c + 2]), "=r"(w[4 * c + 3])
-                                 : "r"(row + (((half * 2 + c) ^ swizzle) << 4)));
-                const uint32_t magic[2] = {0x43004300u | (z0[0] & 15u) * 0x00010001u, 0x43004300u | (z0[1] & 15u) * 0x00010001u};
+                                 : "r"(row + ((c ^ swizzle) << 4)));
+                uint32_t magic[4];                      // of the four runs of 32 elements
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t x = per_block == 1 ? z[0] : per_block == 2 ? z[i >> 1] : z[i];
+                    magic[i] = 0x43004300u | (x & 15u) * 0x00010001u;
+                }
+                load_zeros(kb + SETS);
                 uint32_t x[32];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -265,25 +294,32 @@ __global__ void __launch_bounds__(kThreads, 1) w4_tensor_kernel(const __grid_con
                 st.next(n_stages);
                 if (!warp_wait(a_empty + 8u * ab.at, ab.phase, abort_p)) { ok = false; break; }
                 tc_fence_after();
-                tmem_st32(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + ab.at * kABlockCols + half * 32, x);
+                const uint32_t a = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + ab.at * kABlockCols;
+                tmem_st32(a, x);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    uint32_t pairs[4];
+                    w4::expand(w[8 + i], magic[2 + (i >> 2)], pairs);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[4 * i + j] = pairs[j];
+                }
+                tmem_st32(a + 32, x);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive_local(a_full + 8u * ab.at);
                 ab.next(n_a);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) { z0[i] = z1[i]; z1[i] = next[i]; }
             }
         }
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
     } else {
         // ------------------------------------------------------------------ epilogue
-        const int quarter = warp & 3, half = (warp - 2 - kDequantWarps) >> 2;
+        const int quarter = warp & 3, share = (warp - 2 - kSetWarps * SETS) >> 2;
         Ring slot;
         bool ok = true;
-        const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + half * NC;
+        const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + share * NC;
         for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
-            const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * N + half * NC;
+            const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * N + share * NC;
             const __nv_bfloat16* scale = p.scales + static_cast<size_t>(min(v, p.V - 1)) * p.groups;
             float sum[NC];
 #pragma unroll
@@ -351,18 +387,19 @@ bool encode(CUtensorMap* map, CUtensorMapDataType type, const void* base, size_t
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int NC>
+template <int NC, int EPI, int SETS>
 cudaError_t launch_nc(TensorParams& p, int grid, cudaStream_t stream)
 {
-    constexpr size_t stage = kCodeBytes + static_cast<size_t>(2 * NC) * kBlock * 2;
+    constexpr int N = NC * (EPI / 4);
+    constexpr size_t stage = kCodeBytes + static_cast<size_t>(N) * kBlock * 2;
     p.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemLimit - 4096) / stage));
     const size_t smem = 1024 + p.stages * stage;
-    // tensor memory: two blocks of A at least, then as many accumulator slots as fit
-    p.a_blocks = 2 * NC * 4 + 4 * kABlockCols <= kTmemCols ? 4 : 2;
-    p.slots = std::min(kMaxSlots, (kTmemCols - p.a_blocks * kABlockCols) / (2 * NC));
-    cudaError_t e = cudaFuncSetAttribute(w4_tensor_kernel<NC>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    // tensor memory: four blocks of A if that leaves four accumulator slots, else two; then as many slots as fit
+    p.a_blocks = 4 * N + 4 * kABlockCols <= kTmemCols ? 4 : 2;
+    p.slots = std::min(kMaxSlots, (kTmemCols - p.a_blocks * kABlockCols) / N);
+    cudaError_t e = cudaFuncSetAttribute(w4_tensor_kernel<NC, EPI, SETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
-    w4_tensor_kernel<NC><<<grid, kThreads, smem, stream>>>(p);
+    w4_tensor_kernel<NC, EPI, SETS><<<grid, threads_of(SETS, EPI), smem, stream>>>(p);
     return cudaGetLastError();
 }
 
@@ -394,8 +431,7 @@ cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* dev
     p.status = device_status;
     p.row_blocks = (q.rows + kMaxRowsPerItem - 1) / kMaxRowsPerItem;
     const int cols = (q.rows + p.row_blocks - 1) / p.row_blocks;
-    const int nc = (cols + 15) / 16 * 8;                // N in steps of 16
-    const int n = nc <= 32 ? 2 * nc : nc <= 48 ? 96 : nc <= 64 ? 128 : 144;
+    const int n = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 96 ? 96 : cols <= 128 ? 128 : kMaxRowsPerItem;
     p.row_blocks = (q.rows + n - 1) / n;
     const long long items = static_cast<long long>((q.V + kTileV - 1) / kTileV) * p.row_blocks;
     if (items > 0x7fffffffLL) return cudaErrorInvalidValue;
@@ -407,13 +443,12 @@ cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* dev
         return cudaErrorInvalidValue;
     const int grid = std::min(sms, p.items);
     switch (n) {
-        case 16: return launch_nc<8>(p, grid, stream);
-        case 32: return launch_nc<16>(p, grid, stream);
-        case 48: return launch_nc<24>(p, grid, stream);
-        case 64: return launch_nc<32>(p, grid, stream);
-        case 96: return launch_nc<48>(p, grid, stream);
-        case 128: return launch_nc<64>(p, grid, stream);
-        default: return launch_nc<72>(p, grid, stream);
+        case 16: return launch_nc<16, 4, 3>(p, grid, stream);
+        case 32: return launch_nc<32, 4, 3>(p, grid, stream);
+        case 64: return launch_nc<64, 4, 3>(p, grid, stream);
+        case 96: return launch_nc<48, 8, 2>(p, grid, stream);
+        case 128: return launch_nc<64, 8, 2>(p, grid, stream);
+        default: return launch_nc<72, 8, 2>(p, grid, stream);
     }
 }
 
