@@ -70,6 +70,7 @@ struct StreamParams {
     int split;                          // warps per tile, a divisor of kWarpsS
     int chunks_per_warp;                // ceil(chunks / split)
     int tiles;
+    uint32_t exponent;                  // w4::kExponent
     void* out;
 };
 
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t x = __shfl_sync(0xffffffffu, sz[gi], g * 4 + i);
                         s[i] = __uint_as_float(x & 0xffff0000u);
-                        z[i] = 0x43004300u | (x & 15u) * 0x00010001u;
+                        z[i] = p.exponent | (x & 15u) * 0x00010001u;
                     }
                     float acc[2][NT][4];
 #pragma unroll
@@ -182,8 +183,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamPar
 #pragma unroll
                         for (int m = 0; m < 2; ++m) {
                             uint32_t lo[4], hi[4];
-                            w4::expand(x[2 * m][word], z[2 * m], lo);
-                            w4::expand(x[2 * m + 1][word], z[2 * m + 1], hi);
+                            w4::expand(x[2 * m][word], z[2 * m], p.exponent, lo);
+                            w4::expand(x[2 * m + 1][word], z[2 * m + 1], p.exponent, hi);
                             const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
@@ -276,6 +277,7 @@ cudaError_t launch_stream(const W4Problem& q, int nt, polyspec_dtype dt, cudaStr
     p.d = q.d;
     p.groups = q.d / q.group;
     p.out = q.out;
+    p.exponent = w4::kExponent;
     p.tiles = (q.V + kTileS - 1) / kTileS;
     const int chunks = (q.d + kChunk - 1) / kChunk;
     // as many warps per tile as leave each two chunks (the prefetch depth) to work on

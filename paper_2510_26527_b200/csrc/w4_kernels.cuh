@@ -22,12 +22,15 @@ cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* dev
 namespace w4 {
 
 // The eight weights of a word as four bf16 pairs (0,1) (2,3) (4,5) (6,7), the zero point subtracted.
-// `magic` holds 128 + z twice; 128 + q, 128 + z and q - z are all exact in bf16.
-__device__ __forceinline__ void expand(uint32_t word, uint32_t magic, uint32_t (&pairs)[4])
+// `magic` holds 128 + z twice; 128 + q, 128 + z and q - z are all exact in bf16.  `exponent` is kExponent, which callers pass
+// from a kernel parameter: a value the compiler cannot see stays in a register, so that mask and exponent are one three-input
+// instruction; as two immediates they took two (15 instead of 7 logic instructions per word, and those bound the kernels).
+constexpr uint32_t kExponent = 0x43004300u;
+__device__ __forceinline__ void expand(uint32_t word, uint32_t magic, uint32_t exponent, uint32_t (&pairs)[4])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t x = ((word >> (4 * i)) & 0x000f000fu) | 0x43004300u;
+        const uint32_t x = ((word >> (4 * i)) & 0x000f000fu) | exponent;
         asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(pairs[i]) : "r"(x), "r"(magic));
     }
 }

@@ -10,14 +10,15 @@
 //
 // Persistent, one CTA per SM; work items are (vocabulary tile, block of hidden rows), the row blocks of one tile neighbours so
 // that its codes come from L2 the second time.  Warp roles (18 warps):
-//   0        TMA producer: per K block of 128, the packed tile (128 rows x 64 bytes, 64-byte swizzle) and the hidden tile
-//            (two boxes of 64 elements, 128-byte swizzle)
+//   0        TMA producer: per K block, the packed tile (boxes of 128 rows x 64 bytes, 64-byte swizzle) and the hidden tile (boxes
+//            of 64 elements, 128-byte swizzle)
 //   1        MMA issuer; allocates and frees tensor memory
 //   then     dequantisers, in sets of four warps (one per lane quarter): a set takes every second or third K block, so that the
 //            latencies of one (shared-memory reads, tensor-memory stores, barriers) pass behind the arithmetic of another
 //   last     epilogue, one or two warps per lane quarter, each its share of the columns
-// Up to 64 rows, where expanding codes is what takes the time, three sets and four epilogue warps; above, two and eight.
-// Tensor memory: A blocks of 64 columns in a ring, then accumulator slots of N columns in a ring.
+// Tensor memory: A blocks in a ring, then accumulator slots in a ring; a slot holds `UNIT` groups.
+// With few rows an MMA is short and what a block costs is the MMA warp's own handshakes (some 80 cycles per wait that passes at
+// once, as much per commit): up to 64 rows, blocks of 256 elements, three sets and four epilogue warps; above, 128, two and eight.
 //
 // Every wait on an mbarrier is bounded: one that runs out raises an abort flag that all roles poll, sets POLYSPEC_ERR_TIMEOUT,
 // and the kernel still lets its copies land, frees tensor memory and returns.
@@ -36,12 +37,11 @@ namespace {
 using namespace tensordev;
 
 constexpr int kTileV = 128;
-constexpr int kBlock = 128;                             // K elements per block
-constexpr int kCodeBytes = kTileV * kBlock / 2;         // 8 KiB
+constexpr int kSub = 128;                               // K elements per box of codes
+constexpr int kSubBytes = kTileV * kSub / 2;            // 8 KiB
 constexpr int kSetWarps = 4;                            // dequantising warps per K block
 constexpr int kMaxStages = 12, kMaxSlots = 8, kMaxABlocks = 4;
 constexpr int kTmemCols = 512;
-constexpr int kABlockCols = kBlock / 2;                 // two bf16 per 32-bit column
 constexpr int kMaxRowsPerItem = 144;                    // an epilogue thread holds half of them as accumulators
 constexpr size_t kSmemLimit = 227 * 1024;
 
@@ -55,8 +55,7 @@ struct TensorParams {
     int rows, V, group, groups; // groups: of a whole row
     int kblocks;
     int row_blocks, items;
-    int stages, a_blocks, slots;
-    uint32_t idesc;
+    uint32_t idesc, exponent;
     int32_t* status;
 };
 
@@ -118,64 +117,102 @@ struct Ring {
     }
 };
 
+// Sizes of an instantiation.  NC: columns (hidden rows) per epilogue warp; EPI: epilogue warps; SETS: sets of dequantising warps;
+// BLOCK: K elements per block; UNIT: groups per accumulator slot.
+template <int NC_, int EPI_, int SETS_, int BLOCK_, int UNIT_>
+struct Shape {
+    static constexpr int NC = NC_, EPI = EPI_, SETS = SETS_, BLOCK = BLOCK_, UNIT = UNIT_;
+    static constexpr int N = NC * (EPI / 4);
+    static constexpr int kThreads = 32 * (2 + kSetWarps * SETS + EPI);
+    static constexpr int kSubs = BLOCK / kSub;
+    static constexpr uint32_t kCodeBytes = kSubs * kSubBytes, kBoxBytes = N * 128, kStage = kCodeBytes + BLOCK / 64 * kBoxBytes;
+    static constexpr int kACols = BLOCK / 2;                // two bf16 per 32-bit column
+    static constexpr int kSlotCols = UNIT * N;
+    static constexpr int kABlocks = 3 * kACols + 2 * kSlotCols <= kTmemCols ? 3 : 2;
+    static constexpr int kSlots = (kTmemCols - kABlocks * kACols) / kSlotCols < kMaxSlots ? (kTmemCols - kABlocks * kACols) / kSlotCols : kMaxSlots;
+    static constexpr int kStages = (kSmemLimit - 4096) / kStage < kMaxStages ? (kSmemLimit - 4096) / kStage : kMaxStages;
+    static constexpr size_t kSmem = 1024 + static_cast<size_t>(kStages) * kStage;
+    static_assert(kSlots >= 2 && kStages >= 3 && kStage % 1024 == 0 && kBoxBytes % 1024 == 0, "sizes");
+};
+
+struct Barriers { uint32_t full, empty, a_full, a_empty, acc_full, acc_empty; };
+
 // The MMA issuer's whole run.  The number of groups per K block is a template argument so that a block's MMAs are straight-line
-// code on uniform registers: with the loop bounds read from the parameters the issue alone took 750 cycles per block.
-template <int N, int GROUPS>
-__device__ __forceinline__ bool issue_all(const TensorParams& p, uint32_t tiles, uint32_t tmem, uint32_t tmem_acc, uint32_t full, uint32_t empty,
-                                          uint32_t a_full, uint32_t a_empty, uint32_t acc_full, uint32_t acc_empty, volatile int* abort_p)
+// code on uniform registers: with the loop bounds read from the parameters the issue alone took 750 cycles per 128 elements.
+// A full A block was made from the stage's codes after its copies, the hidden tile's among them, had landed: no wait for those.
+template <class S, int GROUPS>
+__device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers& bar, uint32_t tiles, uint32_t tmem, uint32_t tmem_acc, volatile int* abort_p)
 {
-    constexpr uint32_t kHiddenBytes = N * kBlock * 2, kStage = kCodeBytes + kHiddenBytes;
-    constexpr int kMmas = kBlock / 16 / GROUPS;         // per group
-    const uint32_t n_stages = p.stages, n_a = p.a_blocks, n_slots = p.slots;
+    constexpr int kMmas = S::BLOCK / 16 / GROUPS;       // per group
     Ring st, ab, slot;
     slot.phase = 1;
     uint32_t last_stage = 0, last_stage_phase = 0, last_a = 0, last_a_phase = 0;
     for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
         for (int kb = 0; kb < p.kblocks; ++kb) {
-            if (!warp_wait(full + 8u * st.at, st.phase, abort_p) || !warp_wait(a_full + 8u * ab.at, ab.phase, abort_p)) return false;
-            const uint32_t b_lo = smem_desc_lo(tiles + st.at * kStage + kCodeBytes);
-            const uint32_t a = tmem + ab.at * kABlockCols;
+            if (!warp_wait(bar.a_full + 8u * ab.at, ab.phase, abort_p)) return false;
+            const uint32_t b_lo = smem_desc_lo(tiles + st.at * S::kStage + S::kCodeBytes);
+            const uint32_t a = tmem + ab.at * S::kACols;
 #pragma unroll
-            for (int gi = 0; gi < GROUPS; ++gi) {
-                if (GROUPS > 1 && kb * GROUPS + gi >= p.groups) break;
-                if (!warp_wait(acc_empty + 8u * slot.at, slot.phase, abort_p)) return false;
+            for (int g0 = 0; g0 < GROUPS; g0 += S::UNIT) {
+                if (kb * GROUPS + g0 >= p.groups) break;
+                if (!warp_wait(bar.acc_empty + 8u * slot.at, slot.phase, abort_p)) return false;
                 tc_fence_after();
-                const uint32_t d = tmem_acc + slot.at * N;
+                const uint32_t d = tmem_acc + slot.at * S::kSlotCols;
                 if (elect_one()) {
 #pragma unroll
-                    for (int m = 0; m < kMmas; ++m) {
-                        const int kk = gi * kMmas + m;              // 16-element slice of the block
-                        umma_from_tmem(d, a + kk * 8, b_lo + (kk >> 2) * (kHiddenBytes / 2 >> 4) + (kk & 3) * 2, p.idesc, m != 0);
+                    for (int u = 0; u < S::UNIT && g0 + u < GROUPS; ++u) {
+                        if (kb * GROUPS + g0 + u >= p.groups) break;
+#pragma unroll
+                        for (int m = 0; m < kMmas; ++m) {
+                            const int kk = (g0 + u) * kMmas + m;        // 16-element slice of the block
+                            umma_from_tmem(d + u * S::N, a + kk * 8, b_lo + (kk >> 2) * (S::kBoxBytes >> 4) + (kk & 3) * 2, p.idesc, m != 0);
+                        }
                     }
-                    umma_commit(acc_full + 8u * slot.at);
+                    umma_commit(bar.acc_full + 8u * slot.at);
                 }
                 __syncwarp();
-                slot.next(n_slots);
+                slot.next(S::kSlots);
             }
             if (elect_one()) {
-                umma_commit(empty + 8u * st.at);
-                umma_commit(a_empty + 8u * ab.at);
+                umma_commit(bar.empty + 8u * st.at);
+                umma_commit(bar.a_empty + 8u * ab.at);
             }
             __syncwarp();
             last_stage = st.at; last_stage_phase = st.phase;
             last_a = ab.at; last_a_phase = ab.phase;
-            st.next(n_stages);
-            ab.next(n_a);
+            st.next(S::kStages);
+            ab.next(S::kABlocks);
         }
     }
     // the last commits arrive on barriers of this CTA: it must not exit before
-    return warp_wait(empty + 8u * last_stage, last_stage_phase, abort_p) && warp_wait(a_empty + 8u * last_a, last_a_phase, abort_p);
+    return warp_wait(bar.empty + 8u * last_stage, last_stage_phase, abort_p) && warp_wait(bar.a_empty + 8u * last_a, last_a_phase, abort_p);
 }
 
-constexpr int threads_of(int sets, int epi) { return 32 * (2 + kSetWarps * sets + epi); }
-
-// NC: columns (hidden rows) per epilogue warp; EPI: epilogue warps; SETS: sets of dequantising warps.
-template <int NC, int EPI, int SETS>
-__global__ void __launch_bounds__(threads_of(SETS, EPI), 1) w4_tensor_kernel(const __grid_constant__ TensorParams p)
+// An epilogue warp's sums of one slot: columns [0, NC) of each of `n` groups at t, scaled.
+template <class S>
+__device__ __forceinline__ void add_unit(float (&sum)[S::NC], uint32_t t, const __nv_bfloat16 (&scale)[S::UNIT], int n)
 {
-    constexpr int N = NC * (EPI / 4);
-    constexpr uint32_t kHiddenBytes = N * kBlock * 2;
-    constexpr uint32_t kStage = kCodeBytes + kHiddenBytes;
+#pragma unroll
+    for (int u = 0; u < S::UNIT; ++u) {
+        if (u >= n) break;
+        const float s = __bfloat162float(scale[u]);
+#pragma unroll
+        for (int c = 0; c < S::NC; c += 24) {
+            uint32_t x[24];
+#pragma unroll
+            for (int q = 0; q < 24; q += 8)
+                if (c + q < S::NC) tmem_ld8(t + u * S::N + c + q, x + q);
+            tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 24; ++i)
+                if (c + i < S::NC) sum[c + i] = fmaf(s, __uint_as_float(x[i]), sum[c + i]);
+        }
+    }
+}
+
+template <class S>
+__global__ void __launch_bounds__(S::kThreads, 1) w4_tensor_kernel(const __grid_constant__ TensorParams p)
+{
     extern __shared__ unsigned char smem_tensor[];
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
@@ -183,15 +220,19 @@ __global__ void __launch_bounds__(threads_of(SETS, EPI), 1) w4_tensor_kernel(con
 
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t tiles = (smem_addr(smem_tensor) + 1023u) & ~1023u;
-    const uint32_t full = smem_addr(barriers), empty = full + 8u * kMaxStages, a_full = empty + 8u * kMaxStages, a_empty = a_full + 8u * kMaxABlocks,
-                   acc_full = a_empty + 8u * kMaxABlocks, acc_empty = acc_full + 8u * kMaxSlots;
-    const uint32_t n_stages = p.stages, n_a = p.a_blocks, n_slots = p.slots;
+    Barriers bar;
+    bar.full = smem_addr(barriers);
+    bar.empty = bar.full + 8u * kMaxStages;
+    bar.a_full = bar.empty + 8u * kMaxStages;
+    bar.a_empty = bar.a_full + 8u * kMaxABlocks;
+    bar.acc_full = bar.a_empty + 8u * kMaxABlocks;
+    bar.acc_empty = bar.acc_full + 8u * kMaxSlots;
 
     if (threadIdx.x == 0) {
         abort_flag = 0;
-        for (int i = 0; i < kMaxStages; ++i) { mbar_init(full + 8u * i, 1); mbar_init(empty + 8u * i, kSetWarps + 1); }
-        for (int i = 0; i < kMaxABlocks; ++i) { mbar_init(a_full + 8u * i, kSetWarps); mbar_init(a_empty + 8u * i, 1); }
-        for (int i = 0; i < kMaxSlots; ++i) { mbar_init(acc_full + 8u * i, 1); mbar_init(acc_empty + 8u * i, EPI); }
+        for (int i = 0; i < kMaxStages; ++i) { mbar_init(bar.full + 8u * i, 1); mbar_init(bar.empty + 8u * i, kSetWarps + 1); }
+        for (int i = 0; i < kMaxABlocks; ++i) { mbar_init(bar.a_full + 8u * i, kSetWarps); mbar_init(bar.a_empty + 8u * i, 1); }
+        for (int i = 0; i < kMaxSlots; ++i) { mbar_init(bar.acc_full + 8u * i, 1); mbar_init(bar.acc_empty + 8u * i, S::EPI); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -202,51 +243,51 @@ __global__ void __launch_bounds__(threads_of(SETS, EPI), 1) w4_tensor_kernel(con
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot, tmem_acc = tmem + n_a * kABlockCols;
+    const uint32_t tmem = tmem_slot, tmem_acc = tmem + S::kABlocks * S::kACols;
     volatile int* abort_p = &abort_flag;
-    const int per_block = kBlock / p.group;             // groups per K block: 1, 2 or 4
+    const int per_sub = kSub / p.group;                 // groups per 128 elements: 1, 2 or 4
+    bool ok = true;
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
         Ring st;
         st.phase = 1;                                   // a fresh "empty" barrier passes a wait on parity 1
         uint32_t it = 0;
-        bool ok = true;
         for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
-            const int v0 = item / p.row_blocks * kTileV, row0 = item % p.row_blocks * N;
+            const int v0 = item / p.row_blocks * kTileV, row0 = item % p.row_blocks * S::N;
             for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-                if (!warp_wait(empty + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
-                const uint32_t bar = full + 8u * st.at, dst = tiles + st.at * kStage;
+                if (!warp_wait(bar.empty + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
+                const uint32_t full = bar.full + 8u * st.at, dst = tiles + st.at * S::kStage;
                 if (elect_one()) {
-                    mbar_expect_tx(bar, kStage);
-                    tma_load(dst, &p.map_codes, kb * (kBlock / 2), v0, bar);
-                    tma_load(dst + kCodeBytes, &p.map_hidden, kb * kBlock, row0, bar);
-                    tma_load(dst + kCodeBytes + kHiddenBytes / 2, &p.map_hidden, kb * kBlock + 64, row0, bar);
+                    mbar_expect_tx(full, S::kStage);
+#pragma unroll
+                    for (int i = 0; i < S::kSubs; ++i) tma_load(dst + i * kSubBytes, &p.map_codes, (kb * S::kSubs + i) * (kSub / 2), v0, full);
+#pragma unroll
+                    for (int i = 0; i < S::BLOCK / 64; ++i)
+                        tma_load(dst + S::kCodeBytes + i * S::kBoxBytes, &p.map_hidden, kb * S::BLOCK + i * 64, row0, full);
                 }
                 __syncwarp();
-                st.next(n_stages);
+                st.next(S::kStages);
             }
         }
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
         __syncwarp();
         // the copies must have landed before the CTA may exit, also when it gives up
-        for (uint32_t q = it > n_stages ? it - n_stages : 0u; q < it; ++q)
+        for (uint32_t q = it > S::kStages ? it - S::kStages : 0u; q < it; ++q)
             for (uint32_t i = 0; i < kSpinLimitG; ++i)
-                if (mbar_try(full + 8u * (q % n_stages), (q / n_stages) & 1u)) break;
+                if (mbar_try(bar.full + 8u * (q % S::kStages), (q / S::kStages) & 1u)) break;
     } else if (warp == 1) {
         // ------------------------------------------------------------------ MMA issuer
-        bool ok;
-        if (per_block == 1) ok = issue_all<N, 1>(p, tiles, tmem, tmem_acc, full, empty, a_full, a_empty, acc_full, acc_empty, abort_p);
-        else if (per_block == 2) ok = issue_all<N, 2>(p, tiles, tmem, tmem_acc, full, empty, a_full, a_empty, acc_full, acc_empty, abort_p);
-        else ok = issue_all<N, 4>(p, tiles, tmem, tmem_acc, full, empty, a_full, a_empty, acc_full, acc_empty, abort_p);
+        if (per_sub == 1) ok = issue_all<S, S::kSubs>(p, bar, tiles, tmem, tmem_acc, abort_p);
+        else if (per_sub == 2) ok = issue_all<S, 2 * S::kSubs>(p, bar, tiles, tmem, tmem_acc, abort_p);
+        else ok = issue_all<S, 4 * S::kSubs>(p, bar, tiles, tmem, tmem_acc, abort_p);
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
-    } else if (warp < 2 + kSetWarps * SETS) {
+    } else if (warp < 2 + kSetWarps * S::SETS) {
         // ------------------------------------------------------------------ dequantisers
         const int quarter = warp & 3, set = (warp - 2) >> 2;
         const int r = quarter * 32 + lane;              // row of the tile
         Ring st, ab;
         ab.phase = 1;
-        bool ok = true;
         const uint32_t swizzle = (static_cast<uint32_t>(r) >> 1) & 3u;
         int turn = 0;                                   // whose K block the next one is
         for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
@@ -254,106 +295,104 @@ __global__ void __launch_bounds__(threads_of(SETS, EPI), 1) w4_tensor_kernel(con
             const unsigned char* zero = p.zeros ? p.zeros + v * p.groups : nullptr;
             // the zero points of a block's groups, as loaded, for this set's next block: arithmetic on a fresh load would
             // wait for it
-            uint32_t z[4];
+            uint32_t z[4 * S::kSubs];
             auto load_zeros = [&](int kb) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) z[i] = zero && i < per_block ? __ldg(zero + min(kb * per_block + i, p.groups - 1)) : 8u;
+                for (int i = 0; i < 4 * S::kSubs; ++i)
+                    z[i] = zero && (i & 3) < per_sub ? __ldg(zero + min((kb * S::kSubs + (i >> 2)) * per_sub + (i & 3), p.groups - 1)) : 8u;
             };
-            const int first = (set - turn + SETS) % SETS;
-            load_zeros(first);
-            for (int kb = 0; kb < p.kblocks; ++kb, turn = turn + 1 == SETS ? 0 : turn + 1) {
+            load_zeros((set - turn + S::SETS) % S::SETS);
+            for (int kb = 0; kb < p.kblocks; ++kb, turn = turn + 1 == S::SETS ? 0 : turn + 1) {
                 if (turn != set) {
-                    st.next(n_stages);
-                    ab.next(n_a);
+                    st.next(S::kStages);
+                    ab.next(S::kABlocks);
                     continue;
                 }
-                if (!warp_wait(full + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
-                uint32_t w[16];
-                const uint32_t row = tiles + st.at * kStage + static_cast<uint32_t>(r) * 64u;
+                if (!warp_wait(bar.full + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
+                const uint32_t row = tiles + st.at * S::kStage + static_cast<uint32_t>(r) * 64u;
+                const uint32_t a = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + ab.at * S::kACols;
 #pragma unroll
-                for (int c = 0; c < 4; ++c)
-                    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[4 * c]), "=r"(w[4 * c + 1]), "=r"(w[4 * c + 2]), "=r"(w[4 * c + 3])
-                                 : "r"(row + ((c ^ swizzle) << 4)));
-                uint32_t magic[4];                      // of the four runs of 32 elements
+                for (int sub = 0; sub < S::kSubs; ++sub) {
+                    uint32_t w[16];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t x = per_block == 1 ? z[0] : per_block == 2 ? z[i >> 1] : z[i];
-                    magic[i] = 0x43004300u | (x & 15u) * 0x00010001u;
+                    for (int c = 0; c < 4; ++c)
+                        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
+                                     : "=r"(w[4 * c]), "=r"(w[4 * c + 1]), "=r"(w[4 * c + 2]), "=r"(w[4 * c + 3])
+                                     : "r"(row + sub * kSubBytes + ((c ^ swizzle) << 4)));
+                    uint32_t magic[4];                  // of the four runs of 32 elements
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t x = per_sub == 1 ? z[4 * sub] : per_sub == 2 ? z[4 * sub + (i >> 1)] : z[4 * sub + i];
+                        magic[i] = p.exponent | (x & 15u) * 0x00010001u;
+                    }
+                    if (sub == S::kSubs - 1) {
+                        load_zeros(kb + S::SETS);
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_local(bar.empty + 8u * st.at);           // the codes are in registers
+                    }
+                    if (sub == 0) {
+                        if (!warp_wait(bar.a_empty + 8u * ab.at, ab.phase, abort_p)) { ok = false; break; }
+                        tc_fence_after();
+                    }
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        uint32_t x[32];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t pairs[4];
+                            w4::expand(w[half * 8 + i], magic[half * 2 + (i >> 2)], p.exponent, pairs);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) x[4 * i + j] = pairs[j];
+                        }
+                        tmem_st32(a + sub * (kSub / 2) + half * 32, x);
+                    }
                 }
-                load_zeros(kb + SETS);
-                uint32_t x[32];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t pairs[4];
-                    w4::expand(w[i], magic[i >> 2], pairs);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[4 * i + j] = pairs[j];
-                }
-                __syncwarp();
-                if (lane == 0) mbar_arrive_local(empty + 8u * st.at);           // the codes are in registers
-                st.next(n_stages);
-                if (!warp_wait(a_empty + 8u * ab.at, ab.phase, abort_p)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t a = tmem + (static_cast<uint32_t>(quarter * 32) << 16) + ab.at * kABlockCols;
-                tmem_st32(a, x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    uint32_t pairs[4];
-                    w4::expand(w[8 + i], magic[2 + (i >> 2)], pairs);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[4 * i + j] = pairs[j];
-                }
-                tmem_st32(a + 32, x);
+                if (!ok) break;
+                st.next(S::kStages);
                 tmem_st_wait();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_local(a_full + 8u * ab.at);
-                ab.next(n_a);
+                if (lane == 0) mbar_arrive_local(bar.a_full + 8u * ab.at);
+                ab.next(S::kABlocks);
             }
         }
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
     } else {
         // ------------------------------------------------------------------ epilogue
-        const int quarter = warp & 3, share = (warp - 2 - kSetWarps * SETS) >> 2;
+        const int quarter = warp & 3, share = (warp - 2 - kSetWarps * S::SETS) >> 2;
         Ring slot;
-        bool ok = true;
-        const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + share * NC;
+        const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + share * S::NC;
         for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
-            const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * N + share * NC;
+            const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * S::N + share * S::NC;
             const __nv_bfloat16* scale = p.scales + static_cast<size_t>(min(v, p.V - 1)) * p.groups;
-            float sum[NC];
+            float sum[S::NC];
 #pragma unroll
-            for (int i = 0; i < NC; ++i) sum[i] = 0.0f;
-            // scales as loaded, two groups ahead (as the zero points above)
-            __nv_bfloat16 s0 = scale[0], s1 = scale[min(1, p.groups - 1)];
-            for (int g = 0; g < p.groups; ++g) {
-                const __nv_bfloat16 next = scale[min(g + 2, p.groups - 1)];
-                if (!warp_wait(acc_full + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
+            for (int i = 0; i < S::NC; ++i) sum[i] = 0.0f;
+            // scales as loaded, a slot's worth ahead (as the zero points above)
+            __nv_bfloat16 now[S::UNIT], next[S::UNIT];
+#pragma unroll
+            for (int u = 0; u < S::UNIT; ++u) {
+                now[u] = scale[min(u, p.groups - 1)];
+                next[u] = scale[min(S::UNIT + u, p.groups - 1)];
+            }
+            for (int g = 0; g < p.groups; g += S::UNIT) {
+                __nv_bfloat16 later[S::UNIT];
+#pragma unroll
+                for (int u = 0; u < S::UNIT; ++u) later[u] = scale[min(g + 2 * S::UNIT + u, p.groups - 1)];
+                if (!warp_wait(bar.acc_full + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t t = t0 + slot.at * N;
-                const float s = __bfloat162float(s0);
-#pragma unroll
-                for (int c = 0; c < NC; c += 24) {
-                    uint32_t x[24];
-#pragma unroll
-                    for (int q = 0; q < 24; q += 8)
-                        if (c + q < NC) tmem_ld8(t + c + q, x + q);
-                    tmem_ld_wait();
-#pragma unroll
-                    for (int i = 0; i < 24; ++i)
-                        if (c + i < NC) sum[c + i] = fmaf(s, __uint_as_float(x[i]), sum[c + i]);
-                }
+                add_unit<S>(sum, t0 + slot.at * S::kSlotCols, now, p.groups - g);
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive_local(acc_empty + 8u * slot.at);
-                slot.next(n_slots);
-                s0 = s1;
-                s1 = next;
+                if (lane == 0) mbar_arrive_local(bar.acc_empty + 8u * slot.at);
+                slot.next(S::kSlots);
+#pragma unroll
+                for (int u = 0; u < S::UNIT; ++u) { now[u] = next[u]; next[u] = later[u]; }
             }
             if (!ok || v >= p.V) continue;
-            const int n = min(NC, p.rows - row0);
+            const int n = min(S::NC, p.rows - row0);
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
+            for (int i = 0; i < S::NC; ++i) {
                 if (i >= n) continue;
                 const size_t at = static_cast<size_t>(row0 + i) * p.V + v;
                 if (p.out_bf16) w4::store_logit<POLYSPEC_BF16>(p.out, at, sum[i]);
@@ -387,19 +426,22 @@ bool encode(CUtensorMap* map, CUtensorMapDataType type, const void* base, size_t
                     CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int NC, int EPI, int SETS>
-cudaError_t launch_nc(TensorParams& p, int grid, cudaStream_t stream)
+template <class S>
+cudaError_t launch_shape(TensorParams& p, const W4Problem& q, int sms, cudaStream_t stream)
 {
-    constexpr int N = NC * (EPI / 4);
-    constexpr size_t stage = kCodeBytes + static_cast<size_t>(N) * kBlock * 2;
-    p.stages = static_cast<int>(std::min<size_t>(kMaxStages, (kSmemLimit - 4096) / stage));
-    const size_t smem = 1024 + p.stages * stage;
-    // tensor memory: four blocks of A if that leaves four accumulator slots, else two; then as many slots as fit
-    p.a_blocks = 4 * N + 4 * kABlockCols <= kTmemCols ? 4 : 2;
-    p.slots = std::min(kMaxSlots, (kTmemCols - p.a_blocks * kABlockCols) / N);
-    cudaError_t e = cudaFuncSetAttribute(w4_tensor_kernel<NC, EPI, SETS>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    p.kblocks = (q.d + S::BLOCK - 1) / S::BLOCK;
+    p.row_blocks = (q.rows + S::N - 1) / S::N;
+    const long long items = static_cast<long long>((q.V + kTileV - 1) / kTileV) * p.row_blocks;
+    if (items > 0x7fffffffLL - sms) return cudaErrorInvalidValue;
+    p.items = static_cast<int>(items);
+    // D fp32, A and B bf16, both K-major, M = 128, N
+    p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(S::N >> 3) << 17) | (static_cast<uint32_t>(kTileV >> 4) << 24);
+    if (!encode(&p.map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, q.codes, q.d / 2, q.V, q.d / 2, kSub / 2, kTileV, CU_TENSOR_MAP_SWIZZLE_64B) ||
+        !encode(&p.map_hidden, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, q.hidden, q.d, q.rows, static_cast<size_t>(q.d) * 2, 64, S::N, CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorInvalidValue;
+    cudaError_t e = cudaFuncSetAttribute(w4_tensor_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmem));
     if (e != cudaSuccess) return e;
-    w4_tensor_kernel<NC, EPI, SETS><<<grid, threads_of(SETS, EPI), smem, stream>>>(p);
+    w4_tensor_kernel<S><<<std::min(sms, p.items), S::kThreads, S::kSmem, stream>>>(p);
     return cudaGetLastError();
 }
 
@@ -427,29 +469,16 @@ cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* dev
     p.V = q.V;
     p.group = q.group;
     p.groups = q.d / q.group;
-    p.kblocks = (q.d + kBlock - 1) / kBlock;
     p.status = device_status;
-    p.row_blocks = (q.rows + kMaxRowsPerItem - 1) / kMaxRowsPerItem;
-    const int cols = (q.rows + p.row_blocks - 1) / p.row_blocks;
-    const int n = cols <= 16 ? 16 : cols <= 32 ? 32 : cols <= 64 ? 64 : cols <= 96 ? 96 : cols <= 128 ? 128 : kMaxRowsPerItem;
-    p.row_blocks = (q.rows + n - 1) / n;
-    const long long items = static_cast<long long>((q.V + kTileV - 1) / kTileV) * p.row_blocks;
-    if (items > 0x7fffffffLL) return cudaErrorInvalidValue;
-    p.items = static_cast<int>(items);
-    // D fp32, A and B bf16, both K-major, M = 128, N = n
-    p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(kTileV >> 4) << 24);
-    if (!encode(&p.map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, q.codes, q.d / 2, q.V, q.d / 2, kBlock / 2, kTileV, CU_TENSOR_MAP_SWIZZLE_64B) ||
-        !encode(&p.map_hidden, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, q.hidden, q.d, q.rows, static_cast<size_t>(q.d) * 2, 64, n, CU_TENSOR_MAP_SWIZZLE_128B))
-        return cudaErrorInvalidValue;
-    const int grid = std::min(sms, p.items);
-    switch (n) {
-        case 16: return launch_nc<16, 4, 3>(p, grid, stream);
-        case 32: return launch_nc<32, 4, 3>(p, grid, stream);
-        case 64: return launch_nc<64, 4, 3>(p, grid, stream);
-        case 96: return launch_nc<48, 8, 2>(p, grid, stream);
-        case 128: return launch_nc<64, 8, 2>(p, grid, stream);
-        default: return launch_nc<72, 8, 2>(p, grid, stream);
-    }
+    p.exponent = w4::kExponent;
+    // columns of an item: the rows cut evenly into blocks of at most 144, in the next size there is
+    const int blocks = (q.rows + kMaxRowsPerItem - 1) / kMaxRowsPerItem, cols = (q.rows + blocks - 1) / blocks;
+    if (cols <= 16) return launch_shape<Shape<16, 4, 3, 256, 2>>(p, q, sms, stream);
+    if (cols <= 32) return launch_shape<Shape<32, 4, 3, 256, 2>>(p, q, sms, stream);
+    if (cols <= 64) return launch_shape<Shape<64, 4, 3, 256, 1>>(p, q, sms, stream);
+    if (cols <= 96) return launch_shape<Shape<48, 8, 2, 128, 1>>(p, q, sms, stream);
+    if (cols <= 128) return launch_shape<Shape<64, 8, 2, 128, 1>>(p, q, sms, stream);
+    return launch_shape<Shape<72, 8, 2, 128, 1>>(p, q, sms, stream);
 }
 
 }  // namespace polyspec
