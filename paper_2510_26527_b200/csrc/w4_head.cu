@@ -8,18 +8,24 @@
 // subtraction for two weights).  A word holds its eight weights in the order 0 2 4 6 1 3 5 7 from bit 0 up, so that
 // (word >> 4 p) & 0x000f000f is the pair (2 p, 2 p + 1) as the matrix instructions want it.
 //
-// w4_stream_kernel, few rows: HBM-bound, every code is read once.  mma.sync.m16n8k16 with the vocabulary on the M axis:
-// codes go from global memory straight into the A fragments, nothing passes through shared memory but the hidden rows
-// (staged once per CTA in fragment order).  With at most 16 columns the tensor work is a small part of the time, and
-// tcgen05 would want the expanded weights written to tensor memory or shared memory first.
-// A tile is 32 vocabulary entries; `split` warps share a tile along d and add up through shared memory in a fixed order.
+// w4_stream_kernel, up to eight rows: HBM-bound, every code is read once.  mma.sync.m16n8k16 with the vocabulary on the M axis:
+// codes become A fragments in the registers of the lane that reads them.  With eight columns the tensor work is a small part of
+// the time, and tcgen05 would want the expanded weights written to tensor memory or shared memory first (w4_tensor.cu).
+// The codes are cut into pieces of 32 vocabulary entries (a tile) x 128 elements (2 KiB, one TMA box).  A CTA owns a contiguous
+// range of tiles and its warps equal, contiguous shares of the pieces of that range, whatever tile borders they cross, each
+// streamed through a private ring in shared memory: warps meet once, at the end, when the sums of tiles that several of them
+// worked on are added up in a fixed order.  (With whole tiles per team of warps the last round was a fifth of the time on 32000
+// entries, and a reduction with two barriers per tile cost as much again.)  The hidden rows are staged once per CTA in fragment
+// order.
+// Every wait on a copy is bounded: a warp whose wait runs out sets POLYSPEC_ERR_TIMEOUT and goes on without waiting, so that
+// the barrier at the end is still reached.
 #include <cuda_bf16.h>
 
 #include <algorithm>
 #include <mutex>
 
 #include "polyspec_kernels.cuh"
-#include "stream_device.cuh"
+#include "tensor_device.cuh"
 #include "w4_kernels.cuh"
 
 namespace polyspec {
@@ -28,7 +34,7 @@ namespace {
 constexpr int kWarpsS = 16;                     // warps per CTA, one CTA per SM
 constexpr int kThreadsS = 32 * kWarpsS;
 constexpr int kTileS = 32;                      // vocabulary entries per tile (two m16 tiles)
-constexpr int kStreamRows = 16;                 // more rows go to the tensor-core kernel
+constexpr int kStreamRows = 8;                  // more rows go to the tensor-core kernel
 constexpr int kChunk = 128;                     // d elements per step: 16 bytes of codes per lane and row
 
 __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -38,239 +44,324 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
         : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// The 16 bytes of codes a lane takes of one row and chunk: words 0..3.  Lane t of a quad takes, of every group of G
-// elements, G/4 consecutive ones: so that each MMA stays inside one group.
-template <int G>
-__device__ __forceinline__ uint4 load_codes(const uint32_t* row, int chunk, int t, int groups_left)
-{
-    uint4 w = make_uint4(0, 0, 0, 0);
-    const uint32_t* p = row + chunk * (kChunk / 8);
-    if (G == 128) {
-        w = streamdev::ld_stream(p + t * 4);
-    } else if (G == 64) {
-        uint2 x = make_uint2(0, 0), y = make_uint2(0, 0);
-        x = __ldg(reinterpret_cast<const uint2*>(p + t * 2));
-        if (groups_left > 1) y = __ldg(reinterpret_cast<const uint2*>(p + 8 + t * 2));
-        w = make_uint4(x.x, x.y, y.x, y.y);
-    } else {
-        w.x = __ldg(p + t);
-        if (groups_left > 1) w.y = __ldg(p + 4 + t);
-        if (groups_left > 2) w.z = __ldg(p + 8 + t);
-        if (groups_left > 3) w.w = __ldg(p + 12 + t);
-    }
-    return w;
-}
+using namespace tensordev;
+
+constexpr int kPieceBytes = kTileS * kChunk / 2;        // 2 KiB
+constexpr int kMaxRing = 6;
+constexpr int kTableGroups = 8;                         // groups whose scales and zero points a warp holds at a time
+constexpr int kTableWords = kTableGroups * 32;
+constexpr int kSums = 8;                                // accumulators per lane: two m16 tiles x four
 
 struct StreamParams {
+    CUtensorMap map_codes;              // [V, d / 2] bytes, box {64, 32}, 64-byte swizzle
     const __nv_bfloat16* hidden;
-    const uint32_t* codes;
-    const __nv_bfloat16* scales;
+    const unsigned short* scales;       // bf16 bits
     const unsigned char* zeros;         // or nullptr: 8
     int rows, V, d, groups;             // groups = d / G
-    int split;                          // warps per tile, a divisor of kWarpsS
-    int chunks_per_warp;                // ceil(chunks / split)
     int tiles;
+    int ring;                           // pieces in flight per warp
+    int vectors;                        // groups a multiple of eight, scales and zero points aligned for vector loads
     uint32_t exponent;                  // w4::kExponent
+    int32_t* status;
     void* out;
 };
 
-template <int G, int NT, int DT>
-__global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const StreamParams p)
+// The first of a group's products: nothing to add to.
+__device__ __forceinline__ void mma_bf16_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
+}
+
+// The codes a lane takes of one row of a piece, words 0..3.  Lane t of a quad takes, of every group of G elements, G/4
+// consecutive ones, so that each MMA stays inside one group.  `row` is the row's first byte; 16-byte chunk c of it lies at
+// chunk c ^ sw.
+template <int G>
+__device__ __forceinline__ void read_codes(uint32_t row, int t, uint32_t sw, uint32_t (&w)[4])
+{
+    if (G == 128) {
+        asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(row + ((t ^ sw) << 4)));
+    } else if (G == 64) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+            asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[2 * j]), "=r"(w[2 * j + 1]) : "r"(row + (((2 * j + (t >> 1)) ^ sw) << 4) + (t & 1) * 8));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[j]) : "r"(row + ((j ^ sw) << 4) + t * 4));
+    }
+}
+
+__device__ __forceinline__ void load_piece(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar)
+{
+    mbar_expect_tx(bar, kPieceBytes);
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+// The tile that piece s of a range of tiles from `first` on belongs to.
+__device__ __forceinline__ int tile_of(int first, long long s, int chunks) { return first + static_cast<int>(s / chunks); }
+
+template <int G, int DT>
+__global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_constant__ StreamParams p)
 {
     extern __shared__ uint4 smem_w4[];
+    __shared__ __align__(8) uint64_t barriers[kWarpsS * kMaxRing];
+    __shared__ int gave_up;
     constexpr int GPC = kChunk / G;             // groups per chunk
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int lane = threadIdx.x & 31, warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0);
     const int g = lane >> 2, t = lane & 3;
+    const uint32_t sw = static_cast<uint32_t>(g) >> 1;
     const int chunks = (p.d + kChunk - 1) / kChunk;
-    const int row0 = blockIdx.y * (NT * 8);     // first hidden row of this CTA
-    const int rows = min(NT * 8, p.rows - row0);
 
-    // hidden rows in fragment order: the 16 bytes of (chunk, n tile, word, lane) are the eight elements of row nt * 8 + g
-    // that multiply word `word` of the codes lane (g, t) holds
-    const int kept = chunks * NT * 4 * 32;
-    for (int i = threadIdx.x; i < kept; i += kThreadsS) {
-        const int l = i & 31, word = (i >> 5) & 3, nt = (i >> 7) % NT, c = (i >> 7) / NT;
-        const int n = nt * 8 + (l >> 2), q = l & 3;
+    // shared memory: the rings (1024-byte aligned), the scale tables, the hidden rows, the sums of a warp's first tile; those of
+    // its last tile go to its ring, which is idle by then
+    unsigned char* base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_w4) + 1023) & ~static_cast<uintptr_t>(1023));
+    uint32_t* table = reinterpret_cast<uint32_t*>(base + static_cast<size_t>(kWarpsS) * p.ring * kPieceBytes) + warp * kTableWords;
+    uint4* hidden = reinterpret_cast<uint4*>(base + static_cast<size_t>(kWarpsS) * (p.ring * kPieceBytes + kTableWords * 4));
+    float* joined = reinterpret_cast<float*>(hidden + chunks * 4 * 32);             // [kWarpsS][kSums][32]
+    auto sums_of = [&](int w, bool first) {
+        return first ? joined + w * (kSums * 32) : reinterpret_cast<float*>(base + static_cast<size_t>(w) * p.ring * kPieceBytes);
+    };
+    const uint32_t my_ring = smem_addr(base) + warp * p.ring * kPieceBytes;
+    const uint32_t bars = smem_addr(barriers) + warp * kMaxRing * 8u;
+
+    // tiles [t_first, t_first + n_tiles) are this CTA's, pieces [share(w), share(w + 1)) of them warp w's
+    const int t_first = static_cast<int>(static_cast<long long>(p.tiles) * blockIdx.x / gridDim.x);
+    const int n_tiles = static_cast<int>(static_cast<long long>(p.tiles) * (blockIdx.x + 1) / gridDim.x) - t_first;
+    const long long pieces = static_cast<long long>(n_tiles) * chunks;
+    auto share = [&](int w) { return pieces * w / kWarpsS; };
+    const long long s_first = share(warp), s_end = share(warp + 1);
+
+    if (lane == 0)
+        for (int i = 0; i < p.ring; ++i) mbar_init(bars + 8u * i, 1);
+    if (threadIdx.x == 0) gave_up = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    __syncwarp();
+    // what is read from here on, an earlier kernel of the stream may have written
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    int ask_tile = tile_of(t_first, s_first, chunks), ask_c = static_cast<int>(s_first % chunks), ask_at = 0;
+    long long ask_left = s_end - s_first;
+    auto ask = [&]() {
+        if (ask_left <= 0) return;
+        --ask_left;
+        if (elect_one()) load_piece(my_ring + ask_at * kPieceBytes, &p.map_codes, ask_c * (kChunk / 2), ask_tile * kTileS, bars + 8u * ask_at);
+        __syncwarp();
+        if (++ask_c == chunks) { ask_c = 0; ++ask_tile; }
+        if (++ask_at == p.ring) ask_at = 0;
+    };
+    for (int i = 0; i < p.ring; ++i) ask();
+
+    // Scales and zero points, kTableGroups groups of the tile's 32 entries at a time: lane l loads those of entry l, as vectors
+    // where the groups of a row are a multiple of eight (a lane that loads them group by group reads every 32-byte sector
+    // sixteen times over), one table ahead of its use; a table word is the scale's bits above 128 + z as bf16.
+    constexpr int kTableChunks = kTableGroups / GPC;
+    const bool vectors = p.vectors != 0;
+    uint4 raw_s = make_uint4(0, 0, 0, 0);
+    uint2 raw_z = make_uint2(0, 0);
+    auto load_raw = [&](int tile, int c) {
+        if (!vectors) return;
+        const size_t own = static_cast<size_t>(min(tile * kTileS + lane, p.V - 1)) * p.groups + c / kTableChunks * kTableGroups;
+        raw_s = __ldg(reinterpret_cast<const uint4*>(p.scales + own));
+        raw_z = p.zeros ? __ldg(reinterpret_cast<const uint2*>(p.zeros + own)) : make_uint2(0x08080808u, 0x08080808u);
+    };
+    auto fill_table = [&](int tile, int c) {
+        const int g0 = c / kTableChunks * kTableGroups;
+        const size_t own = static_cast<size_t>(min(tile * kTileS + lane, p.V - 1)) * p.groups;
+        __syncwarp();                           // the table before this one has been read
+#pragma unroll
+        for (int i = 0; i < kTableGroups; ++i) {
+            uint32_t sc, z;
+            if (vectors) {
+                const uint32_t pair = i < 2 ? raw_s.x : i < 4 ? raw_s.y : i < 6 ? raw_s.z : raw_s.w;
+                sc = (i & 1) ? pair >> 16 : pair;
+                z = (i < 4 ? raw_z.x : raw_z.y) >> (8 * (i & 3));
+            } else {
+                const int group = min(g0 + i, p.groups - 1);
+                sc = __ldg(p.scales + own + group);
+                z = p.zeros ? __ldg(p.zeros + own + group) : 8;
+            }
+            table[i * 32 + lane] = sc << 16 | 0x4300u | (z & 15u);
+        }
+        __syncwarp();
+    };
+    if (s_first < s_end) load_raw(tile_of(t_first, s_first, chunks), static_cast<int>(s_first % chunks));
+
+    // hidden rows in fragment order: the 16 bytes of (chunk, word, lane) are the eight elements of row g that multiply word
+    // `word` of the codes lane (g, t) holds
+    for (int i = threadIdx.x; i < chunks * 4 * 32; i += kThreadsS) {
+        const int l = i & 31, word = (i >> 5) & 3, c = i >> 7;
+        const int n = l >> 2, q = l & 3;
         const int k = c * kChunk + (G == 128 ? q * 32 + word * 8 : G == 64 ? (word >> 1) * 64 + q * 16 + (word & 1) * 8 : word * 32 + q * 8);
         uint4 x = make_uint4(0, 0, 0, 0);
-        if (n < rows && k < p.d) x = *reinterpret_cast<const uint4*>(p.hidden + static_cast<size_t>(row0 + n) * p.d + k);
-        smem_w4[i] = x;
+        if (n < p.rows && k < p.d) x = *reinterpret_cast<const uint4*>(p.hidden + static_cast<size_t>(n) * p.d + k);
+        hidden[i] = x;
     }
     __syncthreads();
 
-    const int team = warp / p.split, part = warp % p.split, teams = kWarpsS / p.split;
-    float* joined = reinterpret_cast<float*>(smem_w4 + kept);       // [2][kWarpsS][2 * NT * 4][32]
-    const int c_first = part * p.chunks_per_warp, c_end = min(chunks, c_first + p.chunks_per_warp);
-    uint32_t turn = 0;
-    for (int tile = blockIdx.x + team * gridDim.x; tile < p.tiles; tile += teams * gridDim.x, turn ^= 1u) {
-        const uint32_t* codes[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i)             // the lane's four entries: g, g + 8, g + 16, g + 24 (those past V read the last one)
-            codes[i] = p.codes + static_cast<size_t>(min(tile * kTileS + i * 8 + g, p.V - 1)) * (p.d / 8);
-        // scale and zero point of entry g + 8 t, which the quad's lanes hand one another when they use them
-        const size_t own = static_cast<size_t>(min(tile * kTileS + t * 8 + g, p.V - 1)) * p.groups;
-        struct Raw { unsigned short scale[GPC]; unsigned char zero[GPC]; };
-        auto load_raw = [&](int c) {
-            Raw r;
-#pragma unroll
-            for (int gi = 0; gi < GPC; ++gi) {
-                const int group = GPC == 1 ? c : min(c * GPC + gi, p.groups - 1);
-                r.scale[gi] = __ldg(reinterpret_cast<const unsigned short*>(p.scales) + own + group);
-                r.zero[gi] = p.zeros ? __ldg(p.zeros + own + group) : 8;
-            }
-            return r;
-        };
-        float sum[2][NT][4];
+    // entry (m, half) * 8 + g, row 2 t + (i & 1)
+    auto store = [&](int tile, int q, float x) {
+        const int i = q & 3, m = q >> 2;
+        const int v = tile * kTileS + m * 16 + (i >> 1) * 8 + g, n = 2 * t + (i & 1);
+        if (v < p.V && n < p.rows) w4::store_logit<DT>(p.out, static_cast<size_t>(n) * p.V + v, x);
+    };
+
+    uint32_t at = 0, phase = 0;
+    int tile = tile_of(t_first, s_first, chunks);
+    bool first_tile = true;
+    for (long long s = s_first; s < s_end; ++tile, first_tile = false) {
+        const int c_first = static_cast<int>(s % chunks);
+        const int c_end = static_cast<int>(s_end - s < chunks - c_first ? c_first + (s_end - s) : chunks);
+        s += c_end - c_first;
+        float sum[2][4];
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) sum[m][nt][i] = 0.0f;
+            for (int i = 0; i < 4; ++i) sum[m][i] = 0.0f;
 
-        constexpr int kAhead = 2;               // chunks of codes in flight
-        uint4 w[kAhead][4];
-        Raw raw[kAhead];
-#pragma unroll
-        for (int a = 0; a < kAhead; ++a)
-            if (c_first + a < c_end) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) w[a][i] = load_codes<G>(codes[i], c_first + a, t, p.groups - (c_first + a) * GPC);
-                raw[a] = load_raw(c_first + a);
+        for (int c = c_first; c < c_end; ++c) {
+            if (c == c_first || c % kTableChunks == 0) {
+                fill_table(tile, c);
+                const int next = (c / kTableChunks + 1) * kTableChunks;
+                if (next < c_end) load_raw(tile, next);
+                else if (s < s_end) load_raw(tile + 1, 0);
             }
-        for (int c0 = c_first; c0 < c_end; c0 += kAhead) {
+            if (!mbar_wait(bars + 8u * at, phase, &gave_up) && lane == 0) {
+                if (p.status) atomicCAS(p.status, 0, static_cast<int>(POLYSPEC_ERR_TIMEOUT));
+                *reinterpret_cast<volatile int*>(&gave_up) = 1;
+            }
+            __syncwarp();
+            uint32_t x[4][4];
 #pragma unroll
-            for (int a = 0; a < kAhead; ++a) {
-                const int c = c0 + a;
-                if (c >= c_end) break;
-                uint32_t x[4][4];
+            for (int i = 0; i < 4; ++i) read_codes<G>(my_ring + at * kPieceBytes + (i * 8 + g) * 64, t, sw, x[i]);
+            const uint4* hid = hidden + c * 4 * 32 + lane;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) { x[i][0] = w[a][i].x; x[i][1] = w[a][i].y; x[i][2] = w[a][i].z; x[i][3] = w[a][i].w; }
-                uint32_t sz[GPC];
+            for (int gi = 0; gi < GPC; ++gi) {
+                if (GPC > 1 && c * GPC + gi >= p.groups) break;
+                float sc[4];
+                uint32_t z[4];
 #pragma unroll
-                for (int gi = 0; gi < GPC; ++gi) sz[gi] = static_cast<uint32_t>(raw[a].scale[gi]) << 16 | (raw[a].zero[gi] & 15u);
-                if (c + kAhead < c_end) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) w[a][i] = load_codes<G>(codes[i], c + kAhead, t, p.groups - (c + kAhead) * GPC);
-                    raw[a] = load_raw(c + kAhead);
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t y = table[(c % kTableChunks * GPC + gi) * 32 + i * 8 + g];
+                    sc[i] = __uint_as_float(y & 0xffff0000u);
+                    z[i] = __byte_perm(y, 0, 0x1010);
                 }
-                const uint4* hid = smem_w4 + c * NT * 4 * 32 + lane;
+                float acc[2][4];
 #pragma unroll
-                for (int gi = 0; gi < GPC; ++gi) {
-                    const int group = c * GPC + gi;
-                    if (GPC > 1 && group >= p.groups) break;
-                    float s[4];
-                    uint32_t z[4];
+                for (int wi = 0; wi < 4 / GPC; ++wi) {
+                    const int word = gi * (4 / GPC) + wi;
+                    const uint4 h = hid[word * 32];
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t x = __shfl_sync(0xffffffffu, sz[gi], g * 4 + i);
-                        s[i] = __uint_as_float(x & 0xffff0000u);
-                        z[i] = p.exponent | (x & 15u) * 0x00010001u;
+                    for (int m = 0; m < 2; ++m) {
+                        uint32_t lo[4], hi[4];
+                        w4::expand(x[2 * m][word], z[2 * m], p.exponent, lo);
+                        w4::expand(x[2 * m + 1][word], z[2 * m + 1], p.exponent, hi);
+                        const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+                        if (wi == 0) mma_bf16_first(acc[m], a0, h.x, h.y);
+                        else mma_bf16(acc[m], a0, h.x, h.y);
+                        mma_bf16(acc[m], a1, h.z, h.w);
                     }
-                    float acc[2][NT][4];
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) acc[m][nt][i] = 0.0f;
-#pragma unroll
-                    for (int wi = 0; wi < 4 / GPC; ++wi) {
-                        const int word = gi * (4 / GPC) + wi;
-                        uint4 h[NT];
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt) h[nt] = hid[(nt * 4 + word) * 32];
-#pragma unroll
-                        for (int m = 0; m < 2; ++m) {
-                            uint32_t lo[4], hi[4];
-                            w4::expand(x[2 * m][word], z[2 * m], p.exponent, lo);
-                            w4::expand(x[2 * m + 1][word], z[2 * m + 1], p.exponent, hi);
-                            const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
-#pragma unroll
-                            for (int nt = 0; nt < NT; ++nt) {
-                                mma_bf16(acc[m][nt], a0, h[nt].x, h[nt].y);
-                                mma_bf16(acc[m][nt], a1, h[nt].z, h[nt].w);
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int m = 0; m < 2; ++m)
-#pragma unroll
-                        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) sum[m][nt][i] = fmaf(s[2 * m + (i >> 1)], acc[m][nt][i], sum[m][nt][i]);
                 }
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) sum[m][i] = fmaf(sc[2 * m + (i >> 1)], acc[m][i], sum[m][i]);
             }
+            __syncwarp();                       // every lane has read the piece
+            ask();
+            if (++at == static_cast<uint32_t>(p.ring)) { at = 0; phase ^= 1u; }
         }
-        // entry (m, half) * 8 + g, row nt * 8 + 2 t + (i & 1)
-        if (p.split > 1) {
-            float* mine = joined + (turn * kWarpsS + warp) * (2 * NT * 4 * 32);
+        const bool whole = c_end - c_first == chunks;
+        float* mine = sums_of(warp, first_tile) + lane;
 #pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) mine[((m * NT + nt) * 4 + i) * 32 + lane] = sum[m][nt][i];
-            asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * p.split) : "memory");
-            const float* all = joined + (turn * kWarpsS + team * p.split) * (2 * NT * 4 * 32);
-            for (int r = part; r < 2 * NT * 4; r += p.split) {
-                float x = 0.0f;
-                for (int q = 0; q < p.split; ++q) x += all[(q * 2 * NT * 4 + r) * 32 + lane];
-                const int i = r & 3, nt = (r >> 2) % NT, m = (r >> 2) / NT;
-                const int v = tile * kTileS + m * 16 + (i >> 1) * 8 + g, n = nt * 8 + 2 * t + (i & 1);
-                if (v < p.V && n < rows) w4::store_logit<DT>(p.out, static_cast<size_t>(row0 + n) * p.V + v, x);
-            }
-        } else {
-#pragma unroll
-            for (int m = 0; m < 2; ++m)
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int v = tile * kTileS + m * 16 + (i >> 1) * 8 + g, n = nt * 8 + 2 * t + (i & 1);
-                        if (v < p.V && n < rows) w4::store_logit<DT>(p.out, static_cast<size_t>(row0 + n) * p.V + v, sum[m][nt][i]);
-                    }
+        for (int q = 0; q < kSums; ++q) {
+            if (whole) store(tile, q, sum[q >> 2][q & 3]);
+            else mine[q * 32] = sum[q >> 2][q & 3];
         }
+    }
+    __syncthreads();
+    // tiles that several warps worked on: warp after warp in order
+    for (int i = warp; i < n_tiles; i += kWarpsS) {
+        const long long lo = static_cast<long long>(i) * chunks, hi = lo + chunks;
+        int w = static_cast<int>(lo * kWarpsS / pieces);
+        while (share(w + 1) <= lo) ++w;
+        while (share(w) > lo) --w;
+        if (share(w + 1) >= hi) continue;       // one warp's alone
+        float total[kSums];
+#pragma unroll
+        for (int q = 0; q < kSums; ++q) total[q] = 0.0f;
+        for (; w < kWarpsS && share(w) < hi; ++w) {
+            if (share(w) == share(w + 1)) continue;
+            const float* theirs = sums_of(w, share(w) >= lo) + lane;        // the warp's first tile, if its share begins in it
+#pragma unroll
+            for (int q = 0; q < kSums; ++q) total[q] += theirs[q * 32];
+        }
+#pragma unroll
+        for (int q = 0; q < kSums; ++q) store(t_first + i, q, total[q]);
     }
 }
 
 constexpr size_t kMaxSmem = 227 * 1024;
 
-size_t stream_smem(int d, int nt)
+// Shared memory with `ring` pieces per warp; the largest ring that fits is used, and two pieces are the least.
+size_t stream_smem(int d, int ring)
 {
     const size_t chunks = (d + kChunk - 1) / kChunk;
-    return chunks * nt * 4 * 512 + 2 * kWarpsS * (2 * nt * 4 * 32) * sizeof(float);
+    return 1024 + static_cast<size_t>(kWarpsS) * (ring * kPieceBytes + kTableWords * 4 + kSums * 32 * sizeof(float)) + chunks * 4 * 512;
+}
+int stream_ring(int d)
+{
+    int ring = kMaxRing;
+    while (ring > 0 && stream_smem(d, ring) + 2048 > kMaxSmem) --ring;
+    return ring;
 }
 
-template <int G, int NT, int DT>
-cudaError_t launch_stream_t(const StreamParams& p, int grid_y, int sms, cudaStream_t stream)
+template <int G, int DT>
+cudaError_t launch_stream_t(const StreamParams& p, int sms, cudaStream_t stream)
 {
-    const size_t smem = stream_smem(p.d, NT);
-    cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<G, NT, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    const size_t smem = stream_smem(p.d, p.ring);
+    cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<G, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
-    const dim3 grid(static_cast<unsigned>(std::min(sms, p.tiles)), static_cast<unsigned>(grid_y));
-    w4_stream_kernel<G, NT, DT><<<grid, kThreadsS, smem, stream>>>(p);
-    return cudaGetLastError();
+    // programmatic launch: the CTAs set up their barriers while the kernel before drains, and wait before their first read
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(std::min(sms, p.tiles)));
+    cfg.blockDim = dim3(kThreadsS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, w4_stream_kernel<G, DT>, p);
 }
 
 template <int G>
-cudaError_t launch_stream_g(const StreamParams& p, int nt, polyspec_dtype dt, int grid_y, int sms, cudaStream_t stream)
+cudaError_t launch_stream_g(const StreamParams& p, polyspec_dtype dt, int sms, cudaStream_t stream)
 {
-    if (dt == POLYSPEC_F32)
-        return nt == 1 ? launch_stream_t<G, 1, POLYSPEC_F32>(p, grid_y, sms, stream) : launch_stream_t<G, 2, POLYSPEC_F32>(p, grid_y, sms, stream);
-    return nt == 1 ? launch_stream_t<G, 1, POLYSPEC_BF16>(p, grid_y, sms, stream) : launch_stream_t<G, 2, POLYSPEC_BF16>(p, grid_y, sms, stream);
+    return dt == POLYSPEC_F32 ? launch_stream_t<G, POLYSPEC_F32>(p, sms, stream) : launch_stream_t<G, POLYSPEC_BF16>(p, sms, stream);
 }
 
-cudaError_t launch_stream(const W4Problem& q, int nt, polyspec_dtype dt, cudaStream_t stream)
+std::mutex g_mutex;
+EncodeTiledFn g_encode = nullptr;
+
+cudaError_t launch_stream(const W4Problem& q, polyspec_dtype dt, int32_t* device_status, cudaStream_t stream)
 {
+    {
+        std::lock_guard<std::mutex> lock(g_mutex);
+        if (!g_encode) {
+            const cudaError_t e = find_encoder(&g_encode);
+            if (e != cudaSuccess) return e;
+        }
+    }
     int dev = 0, sms = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
     StreamParams p;
     p.hidden = static_cast<const __nv_bfloat16*>(q.hidden);
-    p.codes = q.codes;
-    p.scales = static_cast<const __nv_bfloat16*>(q.scales);
+    p.scales = static_cast<const unsigned short*>(q.scales);
     p.zeros = q.zeros;
     p.rows = q.rows;
     p.V = q.V;
@@ -278,17 +369,19 @@ cudaError_t launch_stream(const W4Problem& q, int nt, polyspec_dtype dt, cudaStr
     p.groups = q.d / q.group;
     p.out = q.out;
     p.exponent = w4::kExponent;
+    p.status = device_status;
     p.tiles = (q.V + kTileS - 1) / kTileS;
-    const int chunks = (q.d + kChunk - 1) / kChunk;
-    // as many warps per tile as leave each two chunks (the prefetch depth) to work on
-    p.split = kWarpsS;
-    while (p.split > 1 && chunks < 2 * p.split) p.split >>= 1;
-    p.chunks_per_warp = (chunks + p.split - 1) / p.split;
-    const int grid_y = (q.rows + 8 * nt - 1) / (8 * nt);
+    p.ring = stream_ring(q.d);
+    p.vectors = p.groups % kTableGroups == 0 && (reinterpret_cast<uintptr_t>(q.scales) & 15u) == 0 && (reinterpret_cast<uintptr_t>(q.zeros) & 7u) == 0;
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(q.d / 2), static_cast<cuuint64_t>(q.V)}, pitch[1] = {static_cast<cuuint64_t>(q.d / 2)};
+    const cuuint32_t box[2] = {kChunk / 2, kTileS}, one[2] = {1, 1};
+    if (g_encode(&p.map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint32_t*>(q.codes), dims, pitch, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                 CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
+        return cudaErrorInvalidValue;
     switch (q.group) {
-        case 128: return launch_stream_g<128>(p, nt, dt, grid_y, sms, stream);
-        case 64: return launch_stream_g<64>(p, nt, dt, grid_y, sms, stream);
-        default: return launch_stream_g<32>(p, nt, dt, grid_y, sms, stream);
+        case 128: return launch_stream_g<128>(p, dt, sms, stream);
+        case 64: return launch_stream_g<64>(p, dt, sms, stream);
+        default: return launch_stream_g<32>(p, dt, sms, stream);
     }
 }
 
@@ -347,10 +440,9 @@ polyspec_status polyspec_lm_head_quantized(const void* hidden, const void* qweig
     q.group = group;
     q.out = logits;
     cudaStream_t s = static_cast<cudaStream_t>(cuda_stream);
-    if (rows > kStreamRows || stream_smem(d, rows > 8 ? 2 : 1) > kMaxSmem)
+    if (rows > kStreamRows || stream_ring(d) < 2)
         return cuda_failed(launch_w4_tensor(q, dt, device_status, s)) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
-    const int nt = rows > 8 ? 2 : 1;
-    return cuda_failed(launch_stream(q, nt, dt, s)) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
+    return cuda_failed(launch_stream(q, dt, device_status, s)) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }
 
 }  // extern "C"

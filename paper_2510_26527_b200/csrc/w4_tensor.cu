@@ -48,7 +48,7 @@ constexpr size_t kSmemLimit = 227 * 1024;
 struct TensorParams {
     CUtensorMap map_codes;      // [V, d / 2] bytes, box {64, 128}
     CUtensorMap map_hidden;     // [rows, d] bf16, box {64, N}
-    const __nv_bfloat16* scales;
+    const unsigned short* scales;       // bf16 bits
     const unsigned char* zeros;
     void* out;
     int out_bf16;
@@ -102,10 +102,27 @@ __device__ __forceinline__ void raise_abort(int* abort_flag, int32_t* status)
     *reinterpret_cast<volatile int*>(abort_flag) = 1;
 }
 
-// A bounded wait that the whole warp passes or the whole warp gives up (what follows are warp-wide instructions).
+// A bounded wait that the whole warp passes or the whole warp gives up (what follows are warp-wide instructions).  A try
+// suspends the warp for up to 20 microseconds: eighteen warps that poll in between take a quarter of the issue slots from
+// the ones that expand codes.
+constexpr uint32_t kSuspendNs = 20000, kTries = 100000;
+__device__ __forceinline__ bool try_suspended(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity), "r"(kSuspendNs) : "memory");
+    return ok != 0;
+}
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag)
 {
-    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
+    for (uint32_t i = 0; i < kTries; ++i) {
+        if (__all_sync(0xffffffffu, try_suspended(bar, parity))) return true;
+        if (__any_sync(0xffffffffu, *abort_flag)) return false;
+    }
+    return false;
 }
 
 // A position in a ring of n: its index and the parity a consumer waits for.
@@ -190,12 +207,12 @@ __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers&
 
 // An epilogue warp's sums of one slot: columns [0, NC) of each of `n` groups at t, scaled.
 template <class S>
-__device__ __forceinline__ void add_unit(float (&sum)[S::NC], uint32_t t, const __nv_bfloat16 (&scale)[S::UNIT], int n)
+__device__ __forceinline__ void add_unit(float (&sum)[S::NC], uint32_t t, const uint32_t (&scale)[S::UNIT], int n)
 {
 #pragma unroll
     for (int u = 0; u < S::UNIT; ++u) {
         if (u >= n) break;
-        const float s = __bfloat162float(scale[u]);
+        const float s = __uint_as_float(scale[u] << 16);
 #pragma unroll
         for (int c = 0; c < S::NC; c += 24) {
             uint32_t x[24];
@@ -364,21 +381,21 @@ __global__ void __launch_bounds__(S::kThreads, 1) w4_tensor_kernel(const __grid_
         const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + share * S::NC;
         for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
             const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * S::N + share * S::NC;
-            const __nv_bfloat16* scale = p.scales + static_cast<size_t>(min(v, p.V - 1)) * p.groups;
+            const unsigned short* scale = p.scales + static_cast<size_t>(min(v, p.V - 1)) * p.groups;
             float sum[S::NC];
 #pragma unroll
             for (int i = 0; i < S::NC; ++i) sum[i] = 0.0f;
-            // scales as loaded, a slot's worth ahead (as the zero points above)
-            __nv_bfloat16 now[S::UNIT], next[S::UNIT];
+            // scales as loaded, two slots ahead (as the zero points above; 32-bit variables, since 16-bit ones are packed on arrival)
+            uint32_t now[S::UNIT], next[S::UNIT];
 #pragma unroll
             for (int u = 0; u < S::UNIT; ++u) {
-                now[u] = scale[min(u, p.groups - 1)];
-                next[u] = scale[min(S::UNIT + u, p.groups - 1)];
+                now[u] = __ldg(scale + min(u, p.groups - 1));
+                next[u] = __ldg(scale + min(S::UNIT + u, p.groups - 1));
             }
             for (int g = 0; g < p.groups; g += S::UNIT) {
-                __nv_bfloat16 later[S::UNIT];
+                uint32_t later[S::UNIT];
 #pragma unroll
-                for (int u = 0; u < S::UNIT; ++u) later[u] = scale[min(g + 2 * S::UNIT + u, p.groups - 1)];
+                for (int u = 0; u < S::UNIT; ++u) later[u] = __ldg(scale + min(g + 2 * S::UNIT + u, p.groups - 1));
                 if (!warp_wait(bar.acc_full + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
                 tc_fence_after();
                 add_unit<S>(sum, t0 + slot.at * S::kSlotCols, now, p.groups - g);
@@ -461,7 +478,7 @@ cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* dev
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
     TensorParams p;
-    p.scales = static_cast<const __nv_bfloat16*>(q.scales);
+    p.scales = static_cast<const unsigned short*>(q.scales);
     p.zeros = q.zeros;
     p.out = q.out;
     p.out_bf16 = dt == POLYSPEC_BF16;

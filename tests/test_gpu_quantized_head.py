@@ -92,11 +92,12 @@ def test_writes_nothing_else_and_repeats(rows, V, d, group):
         assert (room[rows * V:] == -7.0).all()
         assert first is None or torch.equal(first, out)
         first = out.clone()
-    # a row's logits do not depend on where the vocabulary is cut
+    # slices of the vocabulary: the order in which a logit's partial sums are added depends on how the pieces fall to the
+    # warps, so each slice is held to the same bound as the whole rather than to the whole's bits
     cut = 1504
     for a, b in ((0, cut), (cut, V)):
         part, _ = binding.polyspec_lm_head_quantized(h, q[a:b].contiguous(), s[a:b].contiguous(), z[a:b].contiguous())
-        assert torch.equal(part, first[:, a:b])
+        _close(part, hidden, codes[a:b], scales[a:b], zp[a:b])
 
 
 def test_pack_layout_and_high_bits():
