@@ -99,9 +99,6 @@ __device__ __forceinline__ void load_piece(uint32_t dst, const CUtensorMap* map,
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
 
-// The tile that piece s of a range of tiles from `first` on belongs to.
-__device__ __forceinline__ int tile_of(int first, long long s, int chunks) { return first + static_cast<int>(s / chunks); }
-
 template <int G, int DT>
 __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_constant__ StreamParams p)
 {
@@ -127,11 +124,12 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
     const uint32_t bars = smem_addr(barriers) + warp * kMaxRing * 8u;
 
     // tiles [t_first, t_first + n_tiles) are this CTA's, pieces [share(w), share(w + 1)) of them warp w's
-    const int t_first = static_cast<int>(static_cast<long long>(p.tiles) * blockIdx.x / gridDim.x);
-    const int n_tiles = static_cast<int>(static_cast<long long>(p.tiles) * (blockIdx.x + 1) / gridDim.x) - t_first;
-    const long long pieces = static_cast<long long>(n_tiles) * chunks;
+    const int each = p.tiles / static_cast<int>(gridDim.x), more = p.tiles % static_cast<int>(gridDim.x), cta = blockIdx.x;
+    const int t_first = each * cta + min(cta, more), n_tiles = each + (cta < more ? 1 : 0);
+    const int pieces = n_tiles * chunks;        // at most 2^31 / 32 tiles x 64 chunks over all CTAs: 16 shares of one's fit 31 bits
     auto share = [&](int w) { return pieces * w / kWarpsS; };
-    const long long s_first = share(warp), s_end = share(warp + 1);
+    const int s_first = share(warp), s_end = share(warp + 1);
+    const int tile_first = t_first + s_first / chunks, c_start = s_first % chunks;
 
     if (lane == 0)
         for (int i = 0; i < p.ring; ++i) mbar_init(bars + 8u * i, 1);
@@ -141,8 +139,19 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
     __syncwarp();
     // what is read from here on, an earlier kernel of the stream may have written
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    int ask_tile = tile_of(t_first, s_first, chunks), ask_c = static_cast<int>(s_first % chunks), ask_at = 0;
-    long long ask_left = s_end - s_first;
+    // the hidden rows' loads go out first: behind the rings' requests they would wait for megabytes of codes
+    // (in row order, so that a warp asks for whole lines: 148 CTAs read the same ones)
+    constexpr int kBatch = 8;
+    const int row_vecs = p.d / 8, n_vecs = p.rows * row_vecs;
+    uint4 staged[kBatch];
+    auto load_hidden = [&](int i0) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u)
+            if (i0 + u * kThreadsS < n_vecs) staged[u] = reinterpret_cast<const uint4*>(p.hidden)[i0 + u * kThreadsS];
+    };
+    load_hidden(threadIdx.x);
+
+    int ask_tile = tile_first, ask_c = c_start, ask_at = 0, ask_left = s_end - s_first;
     auto ask = [&]() {
         if (ask_left <= 0) return;
         --ask_left;
@@ -170,33 +179,37 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
         const int g0 = c / kTableChunks * kTableGroups;
         const size_t own = static_cast<size_t>(min(tile * kTileS + lane, p.V - 1)) * p.groups;
         __syncwarp();                           // the table before this one has been read
+        if (vectors) {
+            const uint32_t pair[4] = {raw_s.x, raw_s.y, raw_s.z, raw_s.w}, z[2] = {raw_z.x & 0x0f0f0f0fu, raw_z.y & 0x0f0f0f0fu};
 #pragma unroll
-        for (int i = 0; i < kTableGroups; ++i) {
-            uint32_t sc, z;
-            if (vectors) {
-                const uint32_t pair = i < 2 ? raw_s.x : i < 4 ? raw_s.y : i < 6 ? raw_s.z : raw_s.w;
-                sc = (i & 1) ? pair >> 16 : pair;
-                z = (i < 4 ? raw_z.x : raw_z.y) >> (8 * (i & 3));
-            } else {
+            for (int i = 0; i < kTableGroups; ++i)          // scale above; below, 0x43 and the zero point's byte
+                table[i * 32 + lane] = __byte_perm(__byte_perm(z[i >> 2], 0x43u, 0x0040u | (i & 3)), pair[i >> 1], (i & 1) ? 0x7610 : 0x5410);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kTableGroups; ++i) {
                 const int group = min(g0 + i, p.groups - 1);
-                sc = __ldg(p.scales + own + group);
-                z = p.zeros ? __ldg(p.zeros + own + group) : 8;
+                table[i * 32 + lane] = static_cast<uint32_t>(__ldg(p.scales + own + group)) << 16 | 0x4300u | (p.zeros ? __ldg(p.zeros + own + group) & 15u : 8u);
             }
-            table[i * 32 + lane] = sc << 16 | 0x4300u | (z & 15u);
         }
         __syncwarp();
     };
-    if (s_first < s_end) load_raw(tile_of(t_first, s_first, chunks), static_cast<int>(s_first % chunks));
-
-    // hidden rows in fragment order: the 16 bytes of (chunk, word, lane) are the eight elements of row g that multiply word
-    // `word` of the codes lane (g, t) holds
-    for (int i = threadIdx.x; i < chunks * 4 * 32; i += kThreadsS) {
-        const int l = i & 31, word = (i >> 5) & 3, c = i >> 7;
-        const int n = l >> 2, q = l & 3;
-        const int k = c * kChunk + (G == 128 ? q * 32 + word * 8 : G == 64 ? (word >> 1) * 64 + q * 16 + (word & 1) * 8 : word * 32 + q * 8);
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (n < p.rows && k < p.d) x = *reinterpret_cast<const uint4*>(p.hidden + static_cast<size_t>(n) * p.d + k);
-        hidden[i] = x;
+    if (s_first < s_end) load_raw(tile_first, c_start);
+    // The fragment order: place (chunk, word, lane) holds the eight elements of row g that multiply word `word` of the codes lane
+    // (g, t) has.  Rows there are none of are zero, and so is what lies behind d.
+    for (int i = threadIdx.x; i < chunks * 4 * 32; i += kThreadsS)
+        if (((i & 31) >> 2) >= p.rows || (i >> 7) * kChunk + kChunk > p.d) hidden[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    for (int i0 = threadIdx.x; i0 < n_vecs;) {
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+            const int i = i0 + u * kThreadsS;
+            if (i >= n_vecs) break;
+            const int n = i / row_vecs, j = i - n * row_vecs, c = j / (kChunk / 8), e = j % (kChunk / 8);
+            const int word = G == 128 ? e % 4 : G == 64 ? e / 8 * 2 + e % 2 : e / 4, q = G == 128 ? e / 4 : G == 64 ? e % 8 / 2 : e % 4;
+            hidden[(c * 4 + word) * 32 + n * 4 + q] = staged[u];
+        }
+        i0 += kBatch * kThreadsS;
+        if (i0 < n_vecs) load_hidden(i0);
     }
     __syncthreads();
 
@@ -208,11 +221,10 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
     };
 
     uint32_t at = 0, phase = 0;
-    int tile = tile_of(t_first, s_first, chunks);
+    int tile = tile_first;
     bool first_tile = true;
-    for (long long s = s_first; s < s_end; ++tile, first_tile = false) {
-        const int c_first = static_cast<int>(s % chunks);
-        const int c_end = static_cast<int>(s_end - s < chunks - c_first ? c_first + (s_end - s) : chunks);
+    for (int s = s_first; s < s_end; ++tile, first_tile = false) {
+        const int c_first = first_tile ? c_start : 0, c_end = min(chunks, c_first + s_end - s);
         s += c_end - c_first;
         float sum[2][4];
 #pragma unroll
@@ -283,16 +295,15 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
     __syncthreads();
     // tiles that several warps worked on: warp after warp in order
     for (int i = warp; i < n_tiles; i += kWarpsS) {
-        const long long lo = static_cast<long long>(i) * chunks, hi = lo + chunks;
-        int w = static_cast<int>(lo * kWarpsS / pieces);
+        const int lo = i * chunks, hi = lo + chunks;
+        int w = 0;
         while (share(w + 1) <= lo) ++w;
-        while (share(w) > lo) --w;
-        if (share(w + 1) >= hi) continue;       // one warp's alone
+        if (share(w) <= lo && share(w + 1) >= hi) continue;             // one warp's alone
         float total[kSums];
 #pragma unroll
         for (int q = 0; q < kSums; ++q) total[q] = 0.0f;
         for (; w < kWarpsS && share(w) < hi; ++w) {
-            if (share(w) == share(w + 1)) continue;
+            if (share(w) == share(w + 1)) continue;     // nothing to do
             const float* theirs = sums_of(w, share(w) >= lo) + lane;        // the warp's first tile, if its share begins in it
 #pragma unroll
             for (int q = 0; q < kSums; ++q) total[q] += theirs[q * 32];
