@@ -10,11 +10,12 @@
 //
 // HBM-bound: every logit is read and written once, except that a vector of eight entries that the mask forbids as a whole
 // is written without being read, and that in place (out == logits) only what a control touches moves at all.
-// A CTA owns a slice of the vocabulary of one sequence and walks rows of the block.  It counts the history's tokens that
-// fall into its slice in shared memory once (a 32-bit word per entry: bits 31..29 flags, below them n(v)), and whoever is first to touch an
-// entry puts it on a list.  Rows are then streamed as vectors with nothing but the mask applied, and the few listed entries
-// are computed and stored one by one after them: a text of thousands of tokens touches a few entries of every 256 a warp
-// moves, so computing them where the vectors pass by had the whole warp take the slow path almost every time.
+// A CTA owns a slice of the vocabulary of one sequence and rows of the block.  It counts the history's tokens that fall into
+// its slice in shared memory (a 32-bit word per entry: bits 31..29 flags, below them n(v)), and whoever is first to touch an
+// entry puts it on a list.  The rows are streamed as vectors with nothing but the mask applied; then, behind one barrier, the
+// few listed entries of every row are computed from the logits as they were and stored over the vectors, a warp per row.  (A
+// text of thousands of tokens touches a few entries of every 256 that a warp moves: computing them where the vectors pass by
+// had the whole warp take the slow path almost every time, and a barrier per row cost a quarter of the time.)
 // Counting with integer atomics and adding listed biases in list order make the result independent of timing.
 #include <cuda_bf16.h>
 
@@ -200,6 +201,92 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
     __syncthreads();
 }
 
+// Rows j0 .. j1 of the slice as vectors; FULL: the slice has all its kThreads * VPT vectors.
+template <int DT, int VPT, bool FULL>
+__device__ __forceinline__ void stream_rows(const ControlParams& p, int b, int v0, int n, int j0, int j1, bool in_place)
+{
+    constexpr int kRows = 2;                            // rows in flight
+    const int tid = threadIdx.x;
+    const size_t first = static_cast<size_t>(b) * p.rows;
+    const unsigned char* mask = p.c.mask ? reinterpret_cast<const unsigned char*>(p.c.mask) + v0 / kVec + tid : nullptr;
+    auto inside = [&](int u) { return FULL || (u * kThreads + tid) * kVec < n; };
+    auto mask_of = [&](int j, uint32_t (&m)[kRows][VPT]) {
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int u = 0; u < VPT; ++u) {
+                m[r][u] = 0xffu;
+                if (mask && j + r < j1 && inside(u)) m[r][u] = mask[(first + j + r) * p.mask_bytes + u * kThreads];
+            }
+    };
+    uint32_t allowed[kRows][VPT];
+    mask_of(j0, allowed);
+    for (int j = j0; j < j1; j += kRows) {
+        Vec8<DT> z[kRows][VPT];
+        uint32_t next[kRows][VPT];
+        const size_t at = (first + j) * p.V + v0 + tid * kVec;
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int u = 0; u < VPT; ++u)
+                if (j + r < j1 && inside(u) && allowed[r][u] != 0 && (!in_place || allowed[r][u] != 0xffu))
+                    z[r][u].load(p.logits, at + static_cast<size_t>(r) * p.V + u * (kThreads * kVec));
+        mask_of(j + kRows, next);
+#pragma unroll
+        for (int r = 0; r < kRows; ++r)
+#pragma unroll
+            for (int u = 0; u < VPT; ++u) {
+                if (j + r < j1 && inside(u) && (!in_place || allowed[r][u] != 0xffu)) {
+                    if (allowed[r][u] != 0xffu) z[r][u].forbid(allowed[r][u]);
+                    z[r][u].store(p.out, at + static_cast<size_t>(r) * p.V + u * (kThreads * kVec));
+                }
+                allowed[r][u] = next[r][u];
+            }
+    }
+}
+
+// The listed entries of row j, entries start, start + step, ... of the list: four loads in flight.
+template <int DT>
+__device__ __forceinline__ void edit_row(const ControlParams& p, const Slice& s, int listed, int b, int v0, int j, int start, int step,
+                                         float r, float f, float pr)
+{
+    constexpr int kAhead = 4;
+    const size_t row = (static_cast<size_t>(b) * p.rows + j) * p.V + v0;
+    const unsigned char* mask = p.c.mask ? reinterpret_cast<const unsigned char*>(p.c.mask) + (static_cast<size_t>(b) * p.rows + j) * p.mask_bytes + v0 / kVec
+                                         : nullptr;
+    for (int i = start; i < listed; i += kAhead * step) {
+        int e[kAhead];
+        uint32_t w[kAhead], times[kAhead];
+        float x[kAhead];
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            w[q] = times[q] = 0;
+            e[q] = 0;
+            if (i + q * step < listed) {
+                e[q] = s.list[i + q * step];
+                w[q] = s.count[e[q]];
+                times[q] = w[q] & kCountMask;
+                if (w[q] & kDrafted)
+                    for (int d = 0; d < j; ++d) times[q] += s.draft[d] == e[q];
+                if (!times[q] && !(w[q] & (kSeenInPrompt | kBiased))) w[q] = 0;                     // drafted later than this row
+                else if (mask && !(mask[e[q] / kVec] >> (e[q] % kVec) & 1u)) w[q] = 0;
+            }
+        }
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+            if (w[q]) x[q] = load_logit<DT>(p.logits, row + e[q]);
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q) {
+            if (!w[q]) continue;
+            float y = x[q];
+            if (times[q] || (w[q] & kSeenInPrompt)) y = y > 0.0f ? y / r : y * r;
+            if (times[q]) y = y - f * static_cast<float>(times[q]) - pr;
+            if (w[q] & kBiased) y += s.bias[e[q]];
+            store_logit<DT>(p.out, row + e[q], y);
+        }
+    }
+}
+
 // VPT vectors of eight entries per thread: a slice of kThreads * VPT * 8 entries.
 // COUNTS: penalties or biases are there; otherwise only a mask.
 template <int DT, int VPT, bool COUNTS>
@@ -217,80 +304,35 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
     const int v0 = slice * kSlice;
     const int n = min(kSlice, p.V - v0);
     const int j0 = group * p.rows_per_group, j1 = min(p.rows, j0 + p.rows_per_group);
+    // In place, an edit of this CTA changes what it read: the edits come after the vectors, and every entry is edited once.
     const bool in_place = p.out == p.logits;
-    const unsigned char* mask = reinterpret_cast<const unsigned char*>(p.c.mask);
-    const bool streams = !in_place || mask;             // whether vectors move at all
+    if (!in_place || p.c.mask) {
+        if (n == kSlice) stream_rows<DT, VPT, true>(p, b, v0, n, j0, j1, in_place);
+        else stream_rows<DT, VPT, false>(p, b, v0, n, j0, j1, in_place);
+    }
+    if (!COUNTS) return;
 
+    const bool report = slice == 0 && group == 0;
     Slice s;
-    float r = 1.0f, f = 0.0f, pr = 0.0f;
-    int listed = 0;
-    if (COUNTS) {
-        const bool report = slice == 0 && group == 0;
-        s.count = reinterpret_cast<uint32_t*>(smem_controls);
-        s.list = reinterpret_cast<unsigned short*>(s.count + kSlice);
-        s.bias = p.c.bias_tokens ? reinterpret_cast<float*>(s.list + kSlice) : nullptr;
-        s.n_list = &n_list;
-        s.draft = drafted;
-        if (p.c.repetition) r = p.c.repetition[b];
-        if (p.c.frequency) f = p.c.frequency[b];
-        if (p.c.presence) pr = p.c.presence[b];
-        if (!(r > 0.0f)) {
-            if (report && tid == 0) bad_input(p.status);
-            r = 1.0f;
-        }
-        count_context(p, b, v0, n, report, s, drafted);
-        listed = n_list;
+    s.count = reinterpret_cast<uint32_t*>(smem_controls);
+    s.list = reinterpret_cast<unsigned short*>(s.count + kSlice);
+    s.bias = p.c.bias_tokens ? reinterpret_cast<float*>(s.list + kSlice) : nullptr;
+    s.n_list = &n_list;
+    s.draft = drafted;
+    float r = p.c.repetition ? p.c.repetition[b] : 1.0f;
+    const float f = p.c.frequency ? p.c.frequency[b] : 0.0f, pr = p.c.presence ? p.c.presence[b] : 0.0f;
+    if (!(r > 0.0f)) {
+        if (report && tid == 0) bad_input(p.status);
+        r = 1.0f;
     }
-
-    auto mask_of = [&](int j, uint32_t (&m)[VPT]) {
-#pragma unroll
-        for (int u = 0; u < VPT; ++u) {
-            const int e = (u * kThreads + tid) * kVec;
-            m[u] = 0xffu;
-            if (mask && j < j1 && e < n) m[u] = mask[(static_cast<size_t>(b) * p.rows + j) * p.mask_bytes + (v0 + e) / kVec];
-        }
-    };
-    uint32_t allowed[VPT];
-    mask_of(j0, allowed);
-    for (int j = j0; j < j1; ++j) {
-        const size_t row = (static_cast<size_t>(b) * p.rows + j) * p.V + v0;
-        if (streams) {
-            Vec8<DT> z[VPT];
-            uint32_t next[VPT];
-#pragma unroll
-            for (int u = 0; u < VPT; ++u) {
-                const int e = (u * kThreads + tid) * kVec;
-                if (e < n && allowed[u] != 0 && (!in_place || allowed[u] != 0xffu)) z[u].load(p.logits, row + e);
-            }
-            mask_of(j + 1, next);
-#pragma unroll
-            for (int u = 0; u < VPT; ++u) {
-                const int e = (u * kThreads + tid) * kVec;
-                if (e < n && (!in_place || allowed[u] != 0xffu)) {
-                    if (allowed[u] != 0xffu) z[u].forbid(allowed[u]);
-                    z[u].store(p.out, row + e);
-                }
-                allowed[u] = next[u];
-            }
-        }
-        if (COUNTS && listed) {
-            if (streams) __syncthreads();               // the listed entries are stored over the vectors
-            for (int i = tid; i < listed; i += kThreads) {
-                const int e = s.list[i];
-                const uint32_t w = s.count[e];
-                uint32_t times = w & kCountMask;
-                if (w & kDrafted)
-                    for (int q = 0; q < j; ++q) times += s.draft[q] == e;
-                if (!times && !(w & (kSeenInPrompt | kBiased))) continue;          // drafted later than this row
-                if (mask && !(mask[(static_cast<size_t>(b) * p.rows + j) * p.mask_bytes + (v0 + e) / 8] >> (e & 7) & 1u)) continue;
-                float x = load_logit<DT>(p.logits, row + e);
-                if (times || (w & kSeenInPrompt)) x = x > 0.0f ? x / r : x * r;
-                if (times) x = x - f * static_cast<float>(times) - pr;
-                if (w & kBiased) x += s.bias[e];
-                store_logit<DT>(p.out, row + e, x);
-            }
-        }
-    }
+    count_context(p, b, v0, n, report, s, drafted);     // its barriers also put the vectors before the edits
+    const int listed = n_list;
+    if (!listed) return;
+    // the CTA's warps over its rows: several per row where there are fewer rows than warps
+    constexpr int kWarps = kThreads / 32;
+    const int warp = tid >> 5, rows = j1 - j0, per_row = max(1, kWarps / rows);
+    if (warp >= rows * per_row) return;
+    for (int j = j0 + warp % rows; j < j1; j += kWarps) edit_row<DT>(p, s, listed, b, v0, j, (warp / rows) * 32 + (tid & 31), per_row * 32, r, f, pr);
 }
 
 template <int DT, int VPT>
@@ -318,14 +360,13 @@ template <int DT>
 cudaError_t launch_controls(ControlParams& p, bool counts, cudaStream_t stream)
 {
     // Few sequences: smaller slices, then fewer rows per CTA, until there are about eight CTAs for each of 148 SMs; many: the
-    // largest slice and all rows of a sequence, so that the history is counted as seldom as possible.  Without counts there
-    // is nothing to share between rows, and a CTA takes one.
+    // largest slice and all rows of a sequence, so that the history is counted as seldom as possible.
     const long long want = 8 * 148;
     auto ctas = [&](int vpt, int rpg) {
         const long long s = (p.V + kThreads * vpt * kVec - 1) / (kThreads * vpt * kVec);
         return s * ((p.rows + rpg - 1) / rpg) * p.B;
     };
-    int vpt = 2, rpg = counts ? p.rows : 1;
+    int vpt = 2, rpg = p.rows;
     while (vpt > 1 && ctas(vpt, rpg) < want) vpt >>= 1;
     while (rpg > 1 && ctas(vpt, rpg) < want) rpg = (rpg + 1) / 2;
     p.rows_per_group = rpg;

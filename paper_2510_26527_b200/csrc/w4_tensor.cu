@@ -55,6 +55,7 @@ struct TensorParams {
     int rows, V, group, groups; // groups: of a whole row
     int kblocks;
     int row_blocks, items;
+    int vectors;                // groups a multiple of eight, scales and zero points aligned for vector loads
     uint32_t idesc, exponent;
     int32_t* status;
 };
@@ -102,27 +103,11 @@ __device__ __forceinline__ void raise_abort(int* abort_flag, int32_t* status)
     *reinterpret_cast<volatile int*>(abort_flag) = 1;
 }
 
-// A bounded wait that the whole warp passes or the whole warp gives up (what follows are warp-wide instructions).  A try
-// suspends the warp for up to 20 microseconds: eighteen warps that poll in between take a quarter of the issue slots from
-// the ones that expand codes.
-constexpr uint32_t kSuspendNs = 20000, kTries = 100000;
-__device__ __forceinline__ bool try_suspended(uint32_t bar, uint32_t parity)
-{
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity), "r"(kSuspendNs) : "memory");
-    return ok != 0;
-}
+// A bounded wait that the whole warp passes or the whole warp gives up (what follows are warp-wide instructions).  Plain polls: with
+// a suspend-time hint on the tries, wake-ups came late and 288 rows took 95 instead of 90 microseconds.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag)
 {
-    for (uint32_t i = 0; i < kTries; ++i) {
-        if (__all_sync(0xffffffffu, try_suspended(bar, parity))) return true;
-        if (__any_sync(0xffffffffu, *abort_flag)) return false;
-    }
-    return false;
+    return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
 
 // A position in a ring of n: its index and the parity a consumer waits for.
@@ -205,6 +190,25 @@ __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers&
     return warp_wait(bar.empty + 8u * last_stage, last_stage_phase, abort_p) && warp_wait(bar.a_empty + 8u * last_a, last_a_phase, abort_p);
 }
 
+// Zero points, scales of the aligned run `run` of eight groups of one row, as vectors where rows hold a multiple of eight groups.
+__device__ __forceinline__ uint2 load_zeros8(const TensorParams& p, const unsigned char* zero, int run)
+{
+    if (!zero) return make_uint2(0x08080808u, 0x08080808u);
+    if (p.vectors) return __ldg(reinterpret_cast<const uint2*>(zero) + run);
+    uint32_t z[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) z[i >> 2] |= static_cast<uint32_t>(__ldg(zero + min(run * 8 + i, p.groups - 1))) << (8 * (i & 3));
+    return make_uint2(z[0], z[1]);
+}
+__device__ __forceinline__ uint4 load_scales8(const TensorParams& p, const unsigned short* scale, int run)
+{
+    if (p.vectors) return __ldg(reinterpret_cast<const uint4*>(scale) + run);
+    uint32_t s[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i >> 1] |= static_cast<uint32_t>(__ldg(scale + min(run * 8 + i, p.groups - 1))) << (16 * (i & 1));
+    return make_uint4(s[0], s[1], s[2], s[3]);
+}
+
 // An epilogue warp's sums of one slot: columns [0, NC) of each of `n` groups at t, scaled.
 template <class S>
 __device__ __forceinline__ void add_unit(float (&sum)[S::NC], uint32_t t, const uint32_t (&scale)[S::UNIT], int n)
@@ -212,7 +216,7 @@ __device__ __forceinline__ void add_unit(float (&sum)[S::NC], uint32_t t, const 
 #pragma unroll
     for (int u = 0; u < S::UNIT; ++u) {
         if (u >= n) break;
-        const float s = __uint_as_float(scale[u] << 16);
+        const float s = __uint_as_float(scale[u]);
 #pragma unroll
         for (int c = 0; c < S::NC; c += 24) {
             uint32_t x[24];
@@ -310,20 +314,22 @@ __global__ void __launch_bounds__(S::kThreads, 1) w4_tensor_kernel(const __grid_
         for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
             const size_t v = static_cast<size_t>(min(item / p.row_blocks * kTileV + r, p.V - 1));
             const unsigned char* zero = p.zeros ? p.zeros + v * p.groups : nullptr;
-            // the zero points of a block's groups, as loaded, for this set's next block: arithmetic on a fresh load would
-            // wait for it
-            uint32_t z[4 * S::kSubs];
-            auto load_zeros = [&](int kb) {
-#pragma unroll
-                for (int i = 0; i < 4 * S::kSubs; ++i)
-                    z[i] = zero && (i & 3) < per_sub ? __ldg(zero + min((kb * S::kSubs + (i >> 2)) * per_sub + (i & 3), p.groups - 1)) : 8u;
-            };
-            load_zeros((set - turn + S::SETS) % S::SETS);
+            // The zero points of the eight groups (an aligned run of them) that the next block of this set belongs to, loaded a
+            // turn ahead: arithmetic on a fresh load would wait for it.
+            constexpr int kBlockSubs = S::kSubs;
+            auto run_of = [&](int kb) { return min(kb * kBlockSubs * per_sub, p.groups - 1) / 8; };
+            int run_next = run_of((set - turn + S::SETS) % S::SETS);
+            uint2 z_next = load_zeros8(p, zero, run_next);
             for (int kb = 0; kb < p.kblocks; ++kb, turn = turn + 1 == S::SETS ? 0 : turn + 1) {
                 if (turn != set) {
                     st.next(S::kStages);
                     ab.next(S::kABlocks);
                     continue;
+                }
+                const uint2 z = z_next;
+                if (run_of(kb + S::SETS) != run_next) {
+                    run_next = run_of(kb + S::SETS);
+                    z_next = load_zeros8(p, zero, run_next);
                 }
                 if (!warp_wait(bar.full + 8u * st.at, st.phase, abort_p)) { ok = false; break; }
                 const uint32_t row = tiles + st.at * S::kStage + static_cast<uint32_t>(r) * 64u;
@@ -339,11 +345,12 @@ __global__ void __launch_bounds__(S::kThreads, 1) w4_tensor_kernel(const __grid_
                     uint32_t magic[4];                  // of the four runs of 32 elements
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint32_t x = per_sub == 1 ? z[4 * sub] : per_sub == 2 ? z[4 * sub + (i >> 1)] : z[4 * sub + i];
+                        // group of run i, counted from the aligned run of eight (32 i elements into sub-block `sub`)
+                        const uint32_t at = ((kb * S::kSubs + sub) * per_sub + (per_sub == 1 ? 0 : per_sub == 2 ? i >> 1 : i)) & 7u;
+                        const uint32_t x = (at & 4u ? z.y : z.x) >> (8u * (at & 3u));
                         magic[i] = p.exponent | (x & 15u) * 0x00010001u;
                     }
                     if (sub == S::kSubs - 1) {
-                        load_zeros(kb + S::SETS);
                         __syncwarp();
                         if (lane == 0) mbar_arrive_local(bar.empty + 8u * st.at);           // the codes are in registers
                     }
@@ -385,17 +392,19 @@ __global__ void __launch_bounds__(S::kThreads, 1) w4_tensor_kernel(const __grid_
             float sum[S::NC];
 #pragma unroll
             for (int i = 0; i < S::NC; ++i) sum[i] = 0.0f;
-            // scales as loaded, two slots ahead (as the zero points above; 32-bit variables, since 16-bit ones are packed on arrival)
-            uint32_t now[S::UNIT], next[S::UNIT];
-#pragma unroll
-            for (int u = 0; u < S::UNIT; ++u) {
-                now[u] = __ldg(scale + min(u, p.groups - 1));
-                next[u] = __ldg(scale + min(S::UNIT + u, p.groups - 1));
-            }
+            // scales in aligned runs of eight groups, the next run loaded while this one is used
+            uint4 run, run_next = load_scales8(p, scale, 0);
             for (int g = 0; g < p.groups; g += S::UNIT) {
-                uint32_t later[S::UNIT];
+                if ((g & 7) == 0) {
+                    run = run_next;
+                    if (g + 8 < p.groups) run_next = load_scales8(p, scale, g / 8 + 1);
+                }
+                uint32_t now[S::UNIT];
 #pragma unroll
-                for (int u = 0; u < S::UNIT; ++u) later[u] = __ldg(scale + min(g + 2 * S::UNIT + u, p.groups - 1));
+                for (int u = 0; u < S::UNIT; ++u) {
+                    const uint32_t at = (g + u) & 7, pair = at & 4 ? (at & 2 ? run.w : run.z) : (at & 2 ? run.y : run.x);
+                    now[u] = at & 1 ? pair & 0xffff0000u : pair << 16;
+                }
                 if (!warp_wait(bar.acc_full + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
                 tc_fence_after();
                 add_unit<S>(sum, t0 + slot.at * S::kSlotCols, now, p.groups - g);
@@ -403,8 +412,6 @@ __global__ void __launch_bounds__(S::kThreads, 1) w4_tensor_kernel(const __grid_
                 __syncwarp();
                 if (lane == 0) mbar_arrive_local(bar.acc_empty + 8u * slot.at);
                 slot.next(S::kSlots);
-#pragma unroll
-                for (int u = 0; u < S::UNIT; ++u) { now[u] = next[u]; next[u] = later[u]; }
             }
             if (!ok || v >= p.V) continue;
             const int n = min(S::NC, p.rows - row0);
@@ -488,11 +495,12 @@ cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* dev
     p.groups = q.d / q.group;
     p.status = device_status;
     p.exponent = w4::kExponent;
+    p.vectors = p.groups % 8 == 0 && (reinterpret_cast<uintptr_t>(q.scales) & 15u) == 0 && (reinterpret_cast<uintptr_t>(q.zeros) & 7u) == 0;
     // columns of an item: the rows cut evenly into blocks of at most 144, in the next size there is
     const int blocks = (q.rows + kMaxRowsPerItem - 1) / kMaxRowsPerItem, cols = (q.rows + blocks - 1) / blocks;
     if (cols <= 16) return launch_shape<Shape<16, 4, 3, 256, 2>>(p, q, sms, stream);
     if (cols <= 32) return launch_shape<Shape<32, 4, 3, 256, 2>>(p, q, sms, stream);
-    if (cols <= 64) return launch_shape<Shape<64, 4, 3, 256, 1>>(p, q, sms, stream);
+    if (cols <= 64) return launch_shape<Shape<32, 8, 2, 256, 1>>(p, q, sms, stream);
     if (cols <= 96) return launch_shape<Shape<48, 8, 2, 128, 1>>(p, q, sms, stream);
     if (cols <= 128) return launch_shape<Shape<64, 8, 2, 128, 1>>(p, q, sms, stream);
     return launch_shape<Shape<72, 8, 2, 128, 1>>(p, q, sms, stream);
