@@ -817,79 +817,95 @@ class ShardedChainCall:
 
 
 # ------------------------------------------------------------------ 4-bit LM head, sampling controls, cache pages
-class _On:
-    """The device and the stream of a call: every tensor contiguous on one CUDA device, which is made current while the call is
-    enqueued; what the call allocated stays alive for a stream other than the current one."""
-
-    def __init__(self, stream, *tensors):
-        self.device = None
-        for t in tensors:
-            if t is None:
-                continue
-            if not t.is_cuda or not t.is_contiguous():
+# These calls are short on the device (a few microseconds for one sequence), so the checks below read each tensor's device,
+# layout and type once and nothing else.
+def _one_device(*tensors) -> int:
+    """The one CUDA device all tensors are on, each contiguous."""
+    dev = -1
+    for t in tensors:
+        if t is not None:
+            d = t.get_device()
+            if d < 0 or not t.is_contiguous():
                 raise ValueError("device-pointer arguments must be contiguous CUDA tensors")
-            if self.device is None:
-                self.device = t.device
-            elif t.device != self.device:
-                raise ValueError("all tensors of a call must be on one device")
-        self.stream = stream
-        self._guard = None
-
-    def __enter__(self):
-        if torch.cuda.current_device() != self.device.index:
-            self._guard = torch.cuda.device(self.device)
-            self._guard.__enter__()
-        return self
-
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
-
-    def handle(self) -> int:
-        return _stream(self.stream)
-
-    def empty(self, shape, dtype) -> torch.Tensor:
-        """A tensor for the call's stream."""
-        if self.stream is None:
-            return torch.empty(shape, dtype=dtype, device=self.device)
-        s = self.stream if isinstance(self.stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.handle(), device=self.device)
-        with torch.cuda.stream(s):
-            return torch.empty(shape, dtype=dtype, device=self.device)
-
-    def status(self) -> torch.Tensor:
-        """A zeroed status word, zeroed on the call's stream."""
-        t = self.empty(1, torch.int32)
-        if self.stream is None:
-            return t.zero_()
-        s = self.stream if isinstance(self.stream, torch.cuda.Stream) else torch.cuda.ExternalStream(self.handle(), device=self.device)
-        with torch.cuda.stream(s):
-            return t.zero_()
+            if d != dev:
+                if dev >= 0:
+                    raise ValueError("all tensors of a call must be on one device")
+                dev = d
+    return dev
 
 
-def _typed(dtype, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.dtype != dtype:
+def _expect(name, t, dtype, shape=None):
+    if t is not None:
+        if t.dtype is not dtype:
             raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if shape is not None and t.shape != shape:
+            raise ValueError(f"shapes do not fit: {name} must be {list(shape)}, got {list(t.shape)}")
 
 
-def _status_arg(device_status):
-    if device_status is not None and (device_status.dtype != torch.int32 or device_status.numel() < 1):
-        raise TypeError("device_status must be an int32 tensor")
+def _on_stream(stream, dev: int):
+    """Context in which allocations belong to `stream` (a torch stream or a raw handle) of device `dev`."""
+    if stream is None:
+        return torch.cuda.device(dev)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(_stream(stream), device=torch.device("cuda", dev))
+    return torch.cuda.stream(stream)
+
+
+def _empty(shape, dtype, dev: int, stream) -> torch.Tensor:
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
+    with _on_stream(stream, dev):
+        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
+
+
+def _handle(stream, dev: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else _stream(stream)
+
+
+_status_words = {}          # (device, stream) -> status words zeroed on that stream and not handed out yet
+
+
+def _status_word(device_status, dev: int, stream) -> torch.Tensor:
+    """The caller's status word, or a fresh zeroed one.  Fresh ones are zeroed 256 at a time; while a graph is captured, and for a
+    stream other than the current one, each is a tensor of its own (a graph keeps alive what is allocated during its capture)."""
+    if device_status is not None:
+        return device_status
+    if stream is not None:
+        with _on_stream(stream, dev):
+            return torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", dev))
+    if torch._C._cuda_isCurrentStreamCapturing():
+        return torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", dev))
+    key = (dev, torch._C._cuda_getCurrentRawStream(dev))
+    try:
+        return _status_words[key].pop()
+    except (KeyError, IndexError):
+        words = list(torch.zeros(256, dtype=torch.int32, device=torch.device("cuda", dev)).split(1))
+        word = words.pop()
+        _status_words[key] = words
+        return word
+
+
+def _call(where: str, fn, dev: int, *args):
+    """fn(*args) with device `dev` current."""
+    if torch._C._cuda_getDevice() == dev:
+        st = fn(*args)
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args)
+    if st != OK:
+        raise PolyspecError(st, where)
 
 
 def polyspec_pack_quantized(codes, out=None, stream=None):
     """codes [V, d] uint8 (one 4-bit code per byte, d a multiple of 32) -> qweight [V, d/8] int32, the words
     polyspec_lm_head_quantized reads."""
-    lib = load_library()
-    _typed(torch.uint8, codes=codes)
-    _typed(torch.int32, out=out)
     V, d = codes.shape
-    with _On(stream, codes, out) as on:
-        if out is None:
-            out = on.empty((V, d // 8), torch.int32)
-        if tuple(out.shape) != (V, d // 8):
-            raise ValueError("out must be [V, d/8]")
-        _check(lib.polyspec_pack_quantized(_ptr(codes), V, d, _ptr(out), on.handle()), "polyspec_pack_quantized")
+    _expect("codes", codes, torch.uint8)
+    _expect("out", out, torch.int32, (V, d // 8))
+    dev = _one_device(codes, out)
+    if out is None:
+        out = _empty((V, d // 8), torch.int32, dev, stream)
+    _call("polyspec_pack_quantized", load_library().polyspec_pack_quantized, dev, codes.data_ptr(), V, d, out.data_ptr(), _handle(stream, dev))
     return out
 
 
@@ -897,26 +913,26 @@ def polyspec_lm_head_quantized(hidden, qweight, scales, zero_points=None, out=No
     """logits[r, v] = sum_d hidden[r, d] * scales[v, d // group] * (code[v, d] - zero_point[v, d // group]).
 
     hidden [rows, d] bf16, qweight [V, d/8] int32 (polyspec_pack_quantized), scales [V, d/group] bf16, zero_points
-    [V, d/group] uint8 or None (8 everywhere); out [rows, V] fp32 or bf16 (out_dtype, where out is not given)."""
-    lib = load_library()
-    _typed(torch.bfloat16, hidden=hidden, scales=scales)
-    _typed(torch.int32, qweight=qweight)
-    _typed(torch.uint8, zero_points=zero_points)
-    _status_arg(device_status)
+    [V, d/group] uint8 or None (8 everywhere); out [rows, V] fp32 or bf16 (out_dtype, where out is not given).
+    Returns (out, status word)."""
     rows, d = hidden.shape
     V, groups = scales.shape
-    if tuple(qweight.shape) != (V, d // 8) or groups < 1 or d % groups or (zero_points is not None and zero_points.shape != scales.shape):
+    _expect("hidden", hidden, torch.bfloat16)
+    _expect("scales", scales, torch.bfloat16)
+    _expect("qweight", qweight, torch.int32)
+    _expect("zero_points", zero_points, torch.uint8)
+    if qweight.shape != (V, d // 8) or groups < 1 or d % groups or (zero_points is not None and zero_points.shape != scales.shape):
         raise ValueError("shapes must be hidden [rows,d], qweight [V,d/8], scales [V,d/group], zero_points [V,d/group]")
-    with _On(stream, hidden, qweight, scales, zero_points, out, device_status) as on:
-        if out is None:
-            out = on.empty((rows, V), out_dtype)
-        if tuple(out.shape) != (rows, V):
-            raise ValueError("out must be [rows, V]")
-        dt = _dt(out)
-        if device_status is None:
-            device_status = on.status()
-        _check(lib.polyspec_lm_head_quantized(_ptr(hidden), _ptr(qweight), _ptr(scales), _ptr(zero_points), rows, V, d, d // groups, dt,
-                                              _ptr(out), _ptr(device_status), on.handle()), "polyspec_lm_head_quantized")
+    _expect("device_status", device_status, torch.int32)
+    dev = _one_device(hidden, qweight, scales, zero_points, out, device_status)
+    if out is None:
+        out = _empty((rows, V), out_dtype, dev, stream)
+    elif out.shape != (rows, V):
+        raise ValueError("out must be [rows, V]")
+    dt = _dt(out)
+    device_status = _status_word(device_status, dev, stream)
+    _call("polyspec_lm_head_quantized", load_library().polyspec_lm_head_quantized, dev, hidden.data_ptr(), qweight.data_ptr(),
+          scales.data_ptr(), _ptr(zero_points), rows, V, d, d // groups, dt, out.data_ptr(), device_status.data_ptr(), _handle(stream, dev))
     return out, device_status
 
 
@@ -929,46 +945,47 @@ def polyspec_process_logits(logits, draft_tokens=None, history=None, history_len
     draft_tokens [B, k >= rows-1], history [B, cap], history_len and prompt_len [B], bias_tokens [B, n]: int32; repetition,
     frequency, presence [B], bias_values [B, n]: float32; mask [B, rows, ceil(V/32)] int32 (bit v % 32 of word v // 32 set:
     allowed).  out: a tensor of its own (made if None) or logits itself.  Returns (out, status word)."""
-    lib = load_library()
     if logits.dim() != 3:
         raise ValueError("logits must be [B, rows, V]")
     B, rows, V = logits.shape
     dt = _dt(logits)
-    _typed(torch.int32, draft_tokens=draft_tokens, history=history, history_len=history_len, prompt_len=prompt_len, bias_tokens=bias_tokens,
-           mask=mask)
-    _typed(torch.float32, repetition=repetition, frequency=frequency, presence=presence, bias_values=bias_values)
-    _typed(logits.dtype, out=out)
-    _status_arg(device_status)
-    for name, t in (("history_len", history_len), ("prompt_len", prompt_len), ("repetition", repetition), ("frequency", frequency),
-                    ("presence", presence)):
-        if t is not None and tuple(t.shape) != (B,):
-            raise ValueError(f"{name} must be [B]")
-    if any(t is not None and (t.dim() != 2 or t.shape[0] != B) for t in (draft_tokens, history, bias_tokens)):
-        raise ValueError("draft_tokens, history and bias_tokens must be [B, n]")
-    if (bias_tokens is None) != (bias_values is None) or (bias_tokens is not None and bias_values.shape != bias_tokens.shape):
-        raise ValueError("bias_tokens and bias_values must have one shape")
-    if mask is not None and tuple(mask.shape) != (B, rows, (V + 31) // 32):
-        raise ValueError("mask must be [B, rows, ceil(V/32)]")
-    if out is not None and out.shape != logits.shape:
-        raise ValueError("out must have the shape of logits")
-    if history is None and (history_len is not None or prompt_len is not None):
+    i32, f32, per_seq = torch.int32, torch.float32, (B,)
+    k = cap = n_bias = 0
+    if draft_tokens is not None:
+        k = draft_tokens.shape[-1]
+        _expect("draft_tokens", draft_tokens, i32, (B, k))
+    if history is not None:
+        cap = history.shape[-1]
+        _expect("history", history, i32, (B, cap))
+        _expect("history_len", history_len, i32, per_seq)
+        _expect("prompt_len", prompt_len, i32, per_seq)
+        if cap == 0:
+            history = history_len = prompt_len = None
+    elif history_len is not None or prompt_len is not None:
         raise ValueError("history_len and prompt_len need a history")
-    if history is not None and history.shape[1] == 0:
-        history = history_len = prompt_len = None
-    if bias_tokens is not None and bias_tokens.shape[1] == 0:
-        bias_tokens = bias_values = None
-    with _On(stream, logits, draft_tokens, history, history_len, prompt_len, repetition, frequency, presence, bias_tokens, bias_values,
-             mask, out, device_status) as on:
-        if out is None:
-            out = on.empty(logits.shape, logits.dtype)
-        if device_status is None:
-            device_status = on.status()
-        c = LogitControls(_ptr(history), _ptr(history_len), _ptr(prompt_len), _ptr(repetition), _ptr(frequency), _ptr(presence),
-                          _ptr(bias_tokens), _ptr(bias_values), _ptr(mask), 0 if history is None else history.shape[1],
-                          0 if bias_tokens is None else bias_tokens.shape[1], int(vocab_begin), int(vocab_size))
-        _check(lib.polyspec_process_logits(_ptr(logits), ctypes.byref(c), _ptr(draft_tokens),
-                                           0 if draft_tokens is None else draft_tokens.shape[1], B, rows, V, dt, _ptr(out),
-                                           _ptr(device_status), on.handle()), "polyspec_process_logits")
+    _expect("repetition", repetition, f32, per_seq)
+    _expect("frequency", frequency, f32, per_seq)
+    _expect("presence", presence, f32, per_seq)
+    if (bias_tokens is None) != (bias_values is None):
+        raise ValueError("bias_tokens and bias_values go together")
+    if bias_tokens is not None:
+        n_bias = bias_tokens.shape[-1]
+        _expect("bias_tokens", bias_tokens, i32, (B, n_bias))
+        _expect("bias_values", bias_values, f32, (B, n_bias))
+        if n_bias == 0:
+            bias_tokens = bias_values = None
+    _expect("mask", mask, i32, (B, rows, (V + 31) // 32))
+    _expect("out", out, logits.dtype, logits.shape)
+    _expect("device_status", device_status, torch.int32)
+    dev = _one_device(logits, draft_tokens, history, history_len, prompt_len, repetition, frequency, presence, bias_tokens, bias_values,
+                      mask, out, device_status)
+    if out is None:
+        out = _empty(logits.shape, logits.dtype, dev, stream)
+    device_status = _status_word(device_status, dev, stream)
+    c = LogitControls(_ptr(history), _ptr(history_len), _ptr(prompt_len), _ptr(repetition), _ptr(frequency), _ptr(presence),
+                      _ptr(bias_tokens), _ptr(bias_values), _ptr(mask), cap, n_bias, vocab_begin, vocab_size)
+    _call("polyspec_process_logits", load_library().polyspec_process_logits, dev, logits.data_ptr(), c, _ptr(draft_tokens), k, B, rows, V,
+          dt, out.data_ptr(), device_status.data_ptr(), _handle(stream, dev))
     return out, device_status
 
 
@@ -981,38 +998,42 @@ def polyspec_cache_workspace(n_seqs: int, n_pages: int) -> int:
 class CachePages:
     """Page tables of one model's cache: table [n_seqs, max_pages], len [n_seqs], refs [n_pages] (int32) and free_bits
     [ceil(n_pages/32)] (int32), on the device.  CachePages.new allocates and initialises them; the constructor takes tensors
-    that hold a state already.  The calls' workspace is allocated at the first call that needs one."""
+    that hold a state already.  The calls' workspace is allocated at the first call that needs one and belongs to the state:
+    calls on one state are ordered anyway."""
 
     def __init__(self, table, len, refs, free_bits, page_tokens):
-        _typed(torch.int32, table=table, len=len, refs=refs, free_bits=free_bits)
         n_seqs, max_pages = table.shape
         n_pages = refs.numel()
-        if tuple(len.shape) != (n_seqs,) or refs.dim() != 1 or tuple(free_bits.shape) != ((n_pages + 31) // 32,):
-            raise ValueError("shapes must be table [n_seqs,max_pages], len [n_seqs], refs [n_pages], free_bits [ceil(n_pages/32)]")
-        _On(None, table, len, refs, free_bits)
+        _expect("table", table, torch.int32)
+        _expect("len", len, torch.int32, (n_seqs,))
+        _expect("refs", refs, torch.int32, (n_pages,))
+        _expect("free_bits", free_bits, torch.int32, ((n_pages + 31) // 32,))
+        self.dev = _one_device(table, len, refs, free_bits)
         self.table, self.len, self.refs, self.free_bits = table, len, refs, free_bits
         self.n_seqs, self.max_pages, self.n_pages, self.page_tokens = n_seqs, max_pages, n_pages, int(page_tokens)
-        self.c = CachePagesStruct(n_seqs, max_pages, n_pages, self.page_tokens, _ptr(table), _ptr(len), _ptr(refs), _ptr(free_bits))
+        self.c = CachePagesStruct(n_seqs, max_pages, n_pages, self.page_tokens, table.data_ptr(), len.data_ptr(), refs.data_ptr(),
+                                  free_bits.data_ptr())
         self._workspace = None
 
     @classmethod
     def new(cls, n_seqs, max_pages, n_pages, page_tokens, device="cuda", stream=None):
-        i32 = lambda *shape: torch.empty(shape, dtype=torch.int32, device=device)
+        device = torch.empty(0, device=device).device
+        i32 = lambda *shape: _empty(shape, torch.int32, device.index, stream)
         pages = cls(i32(n_seqs, max_pages), i32(n_seqs), i32(n_pages), i32((n_pages + 31) // 32), page_tokens)
-        with _On(stream, pages.table) as on:
-            _check(load_library().polyspec_cache_init(ctypes.byref(pages.c), on.handle()), "polyspec_cache_init")
+        _call("polyspec_cache_init", load_library().polyspec_cache_init, pages.dev, pages.c, _handle(stream, pages.dev))
         return pages
 
-    def workspace(self, on):
+    def workspace(self, stream=None):
         if self._workspace is None:
-            self._workspace = on.empty(polyspec_cache_workspace(self.n_seqs, self.n_pages), torch.uint8)
+            self._workspace = _empty(polyspec_cache_workspace(self.n_seqs, self.n_pages), torch.uint8, self.dev, stream)
         return self._workspace
 
 
-def _targets(pages, base, extra):
-    _typed(torch.int32, base=base, extra=extra)
-    if any(t is not None and tuple(t.shape) != (pages.n_seqs,) for t in (base, extra)):
-        raise ValueError("base and extra must be [n_seqs]")
+def _same_device(pages, *tensors):
+    dev = _one_device(*tensors)
+    if dev >= 0 and dev != pages.dev:
+        raise ValueError("all tensors of a call must be on one device")
+    return pages.dev
 
 
 def _pools(pages, pools):
@@ -1022,62 +1043,55 @@ def _pools(pages, pools):
     for t in pools:
         if t.dim() < 3 or t.shape[1] != pages.n_pages:
             raise ValueError("a pool must be [n_planes, n_pages, ...]")
-    return (CachePool * max(1, len(pools)))(*[CachePool(t.data_ptr(), t.shape[0], t.stride(1) * t.element_size()) for t in pools])
+    return (CachePool * len(pools))(*[CachePool(t.data_ptr(), t.shape[0], t.stride(1) * t.element_size()) for t in pools]) if pools else None
 
 
 def polyspec_cache_reserve(pages, base, extra=None, plus=0, pools=(), device_status=None, workspace=None, stream=None):
     """Grow every sequence to base[b] + extra[b] + plus tokens; a last page that others hold too is replaced by a copy of its
     own, in every pool ([n_planes, n_pages, ...] tensors).  pages.len tells what was granted.  Returns the status word."""
-    lib = load_library()
-    _targets(pages, base, extra)
-    _status_arg(device_status)
-    with _On(stream, pages.table, base, extra, workspace, device_status, *pools) as on:
-        if workspace is None:
-            workspace = pages.workspace(on)
-        if device_status is None:
-            device_status = on.status()
-        _check(lib.polyspec_cache_reserve(ctypes.byref(pages.c), _ptr(base), _ptr(extra), int(plus), _pools(pages, pools), len(pools),
-                                          _ptr(device_status), _ptr(workspace), workspace.numel(), on.handle()), "polyspec_cache_reserve")
+    _expect("base", base, torch.int32, (pages.n_seqs,))
+    _expect("extra", extra, torch.int32, (pages.n_seqs,))
+    _expect("device_status", device_status, torch.int32)
+    dev = _same_device(pages, base, extra, workspace, device_status, *pools)
+    if workspace is None:
+        workspace = pages.workspace(stream)
+    device_status = _status_word(device_status, dev, stream)
+    _call("polyspec_cache_reserve", load_library().polyspec_cache_reserve, dev, pages.c, base.data_ptr(), _ptr(extra), plus,
+          _pools(pages, pools), len(pools), device_status.data_ptr(), workspace.data_ptr(), workspace.nbytes, _handle(stream, dev))
     return device_status
 
 
 def polyspec_cache_rollback(pages, base, extra=None, plus=0, device_status=None, stream=None):
     """Let every sequence fall back to base[b] + extra[b] + plus tokens (never up); returns the status word."""
-    lib = load_library()
-    _targets(pages, base, extra)
-    _status_arg(device_status)
-    with _On(stream, pages.table, base, extra, device_status) as on:
-        if device_status is None:
-            device_status = on.status()
-        _check(lib.polyspec_cache_rollback(ctypes.byref(pages.c), _ptr(base), _ptr(extra), int(plus), _ptr(device_status), on.handle()),
-               "polyspec_cache_rollback")
+    _expect("base", base, torch.int32, (pages.n_seqs,))
+    _expect("extra", extra, torch.int32, (pages.n_seqs,))
+    _expect("device_status", device_status, torch.int32)
+    dev = _same_device(pages, base, extra, device_status)
+    device_status = _status_word(device_status, dev, stream)
+    _call("polyspec_cache_rollback", load_library().polyspec_cache_rollback, dev, pages.c, base.data_ptr(), _ptr(extra), plus,
+          device_status.data_ptr(), _handle(stream, dev))
     return device_status
 
 
 def polyspec_cache_fork(pages, src, dst, device_status=None, stream=None):
     """Sequence dst[i], which holds nothing, becomes a copy of src[i] on the same pages; returns the status word."""
-    lib = load_library()
-    _typed(torch.int32, src=src, dst=dst)
-    _status_arg(device_status)
-    if src.dim() != 1 or src.shape != dst.shape:
-        raise ValueError("src and dst must be [n]")
-    with _On(stream, pages.table, src, dst, device_status) as on:
-        if device_status is None:
-            device_status = on.status()
-        _check(lib.polyspec_cache_fork(ctypes.byref(pages.c), _ptr(src), _ptr(dst), src.numel(), _ptr(device_status), on.handle()),
-               "polyspec_cache_fork")
+    n = src.numel()
+    _expect("src", src, torch.int32, (n,))
+    _expect("dst", dst, torch.int32, (n,))
+    _expect("device_status", device_status, torch.int32)
+    dev = _same_device(pages, src, dst, device_status)
+    device_status = _status_word(device_status, dev, stream)
+    _call("polyspec_cache_fork", load_library().polyspec_cache_fork, dev, pages.c, src.data_ptr(), dst.data_ptr(), n,
+          device_status.data_ptr(), _handle(stream, dev))
     return device_status
 
 
 def polyspec_cache_compact(pages, pools=(), moved_to=None, workspace=None, stream=None):
     """Renumber the pages in use to 0 .. n_live-1, moving their contents in every pool; moved_to [n_pages] int32 takes the new
     numbers (-1 for free pages)."""
-    lib = load_library()
-    _typed(torch.int32, moved_to=moved_to)
-    if moved_to is not None and tuple(moved_to.shape) != (pages.n_pages,):
-        raise ValueError("moved_to must be [n_pages]")
-    with _On(stream, pages.table, moved_to, workspace, *pools) as on:
-        if workspace is None:
-            workspace = pages.workspace(on)
-        _check(lib.polyspec_cache_compact(ctypes.byref(pages.c), _pools(pages, pools), len(pools), _ptr(moved_to), _ptr(workspace),
-                                          workspace.numel(), on.handle()), "polyspec_cache_compact")
+    _expect("moved_to", moved_to, torch.int32, (pages.n_pages,))
+    dev = _same_device(pages, moved_to, workspace, *pools)
+    if workspace is None:
+        workspace = pages.workspace(stream)
+    _call("polyspec_cache_compact", load_library().polyspec_cache_compact, dev, pages.c, _pools(pages, pools), len(pools), _ptr(moved_to),
+          workspace.data_ptr(), workspace.nbytes, _handle(stream, dev))

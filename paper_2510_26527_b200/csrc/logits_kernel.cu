@@ -159,15 +159,29 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
             const unsigned at = static_cast<unsigned>(t) - first;
             if (t >= 0 && at < static_cast<unsigned>(n)) touch(at, i < prompt ? atomicOr(&s.count[at], kSeenInPrompt) : atomicAdd(&s.count[at], 1u));
         };
-        int i = tid;
-        for (; i + 7 * kThreads < len; i += 8 * kThreads) {
-            int t[8];
+        constexpr int kLoads = 4;
+        int done = 0;
+        if ((reinterpret_cast<uintptr_t>(text) & 15u) == 0) {           // sixteen tokens per thread in flight
+            const int4* quads = reinterpret_cast<const int4*>(text);
+            for (int q0 = 0; q0 < len / 4; q0 += kLoads * kThreads) {
+                int4 t[kLoads];
 #pragma unroll
-            for (int u = 0; u < 8; ++u) t[u] = text[i + u * kThreads];
+                for (int u = 0; u < kLoads; ++u) {
+                    t[u] = make_int4(-1, -1, -1, -1);
+                    if (q0 + u * kThreads + tid < len / 4) t[u] = quads[q0 + u * kThreads + tid];
+                }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) add(i + u * kThreads, t[u]);
+                for (int u = 0; u < kLoads; ++u) {
+                    const int i = (q0 + u * kThreads + tid) * 4;
+                    add(i, t[u].x);
+                    add(i + 1, t[u].y);
+                    add(i + 2, t[u].z);
+                    add(i + 3, t[u].w);
+                }
+            }
+            done = len / 4 * 4;
         }
-        for (; i < len; i += kThreads) add(i, text[i]);
+        for (int i = done + tid; i < len; i += kThreads) add(i, text[i]);
     }
     if (s.bias && tid >= kThreads - 32) {
         // one warp walks the list 32 biases at a time; those of one batch that name the same token are summed, in list order,
@@ -245,12 +259,12 @@ __device__ __forceinline__ void stream_rows(const ControlParams& p, int b, int v
     }
 }
 
-// The listed entries of row j, entries start, start + step, ... of the list: four loads in flight.
+// The listed entries of row j, entries start, start + step, ... of the list: two loads in flight (four took more registers than they saved time).
 template <int DT>
 __device__ __forceinline__ void edit_row(const ControlParams& p, const Slice& s, int listed, int b, int v0, int j, int start, int step,
                                          float r, float f, float pr)
 {
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 2;
     const size_t row = (static_cast<size_t>(b) * p.rows + j) * p.V + v0;
     const unsigned char* mask = p.c.mask ? reinterpret_cast<const unsigned char*>(p.c.mask) + (static_cast<size_t>(b) * p.rows + j) * p.mask_bytes + v0 / kVec
                                          : nullptr;
@@ -297,10 +311,12 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
     __shared__ int32_t drafted[kMaxK];
     constexpr int kSlice = kThreads * VPT * kVec;
     const int tid = threadIdx.x;
+    // sequences before slices: token ids are frequent at the low end, so that the slices with long lists start first (the other
+    // way round, the last of them ran alone at the end)
     int at = blockIdx.x;
-    const int slice = at % p.slices;
-    at /= p.slices;
-    const int group = at % p.row_groups, b = at / p.row_groups;
+    const int b = at % p.B;
+    at /= p.B;
+    const int group = at % p.row_groups, slice = at / p.row_groups;
     const int v0 = slice * kSlice;
     const int n = min(kSlice, p.V - v0);
     const int j0 = group * p.rows_per_group, j1 = min(p.rows, j0 + p.rows_per_group);

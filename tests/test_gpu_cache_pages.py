@@ -179,7 +179,7 @@ def test_captured_cycle():
     both.fork([0], [2])
     base, acc = both.pages.len.clone(), _i32([0, 1, 2, 3, 5])
     status = torch.zeros(1, dtype=torch.int32, device=DEV)
-    both.pages.workspace(binding._On(None, both.pages.table))
+    both.pages.workspace()
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
