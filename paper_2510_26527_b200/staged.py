@@ -12,7 +12,7 @@ committed and t advances.  One iteration of that loop, for every sequence of the
 and nothing in it comes back to the host: the loop reads one device counter (sequences still running) once
 every ``mu`` iterations, which is at most once per pass of M_1 for any sequence.  All verification and all
 bookkeeping run in the library's kernels; this module only sequences the calls and stands in for the model
-forwards.
+forwards.  Page tables of the models' caches, where given, are reserved and rolled back in the same loop.
 
 The stand-in: logits are indexed by position (row i of every model scores position i, whatever the tokens
 before it), so "running M_2 on positions s .. s+K" is a gather of rows s .. s+K of its table, done here with
@@ -38,9 +38,14 @@ class StagedBatch:
     drafts       [B, N] int32: the token M_3 proposes at each position
     u2           [B, R, K+1] float32: row r serves a sequence's r-th M_2 round
     u1           [B, C, MAX_BLOCK+1] float32: row c serves its c-th M_1 pass (slots 0..m-1 accept tests, slot MAX_BLOCK sampling)
+    caches       None, or {"M1" / "M2" / "M3": (binding.CachePages of B sequences, pools)}: page tables kept in step with the loop
+                 without a read-back.  Before a forward pass a model's cache has room for every token the pass is given (for row i
+                 the tokens before position i); after it, and after M_1's commit, it falls back to the tokens that stand and
+                 have been given to the model, all but the last one emitted.  A pool too small sets ERR_NO_PAGES in `status` and
+                 leaves that sequence's pages as they were; the loop itself reads nothing through them.
     """
 
-    def __init__(self, M1, M2, M3, drafts, u2, u1, K: int, mu: int, n_tokens: int, temperature: float):
+    def __init__(self, M1, M2, M3, drafts, u2, u1, K: int, mu: int, n_tokens: int, temperature: float, caches=None):
         self.lib = binding.load_library()
         for t in (M1, M2, M3, drafts, u2, u1):
             if not t.is_cuda or not t.is_contiguous():
@@ -76,6 +81,10 @@ class StagedBatch:
         self._b = torch.arange(B, device=dev).unsqueeze(1)
         self._ar2 = torch.arange(self.K + 1, device=dev).unsqueeze(0)
         self._ar1 = torch.arange(self.kcap + 1, device=dev).unsqueeze(0)
+        self.caches = dict(caches or {})
+        for name, (pages, _) in self.caches.items():
+            if name not in ("M1", "M2", "M3") or pages.n_seqs != B:
+                raise ValueError('caches must be {"M1" / "M2" / "M3": (pages of B sequences, pools)}')
         self.iterations = 0
         self.read_backs = 0
         self._check(self.lib.polyspec_staged_init(ctypes.byref(self.cstate), binding._stream(None)), "polyspec_staged_init")
@@ -90,11 +99,23 @@ class StagedBatch:
         idx = (pos.long().unsqueeze(1) + ar).clamp_(max=self.N - 1)
         return table[self._b, idx]
 
+    def _reserve(self, name, base, extra=None, plus=0):
+        if name in self.caches:
+            pages, pools = self.caches[name]
+            binding.polyspec_cache_reserve(pages, base, extra, plus, pools, device_status=self.status)
+
+    def _roll_back(self, *names):
+        for name in names:
+            if name in self.caches:
+                binding.polyspec_cache_rollback(self.caches[name][0], self.state["t"], self.state["cnt"], -1, device_status=self.status)
+
     def iteration(self):
         """One pass through the body of Algorithm 1's loop for every sequence; enqueues only."""
         lib, s, p, q = self.lib, ctypes.byref(self.cstate), binding._ptr, binding._stream(None)
         self._check(lib.polyspec_staged_round_begin(s, p(self.drafts), p(self.u2), p(self.pos2), p(self.tokens2), p(self.uniforms2),
                                                     p(self.block_len2), q), "polyspec_staged_round_begin")
+        self._reserve("M2", self.pos2, plus=self.K)
+        self._reserve("M3", self.pos2, plus=self.K)
         rows_p = self._forward(self.M2, self.pos2, self._ar2)
         rows_q = self._forward(self.M3, self.pos2, self._ar2[:, : self.K])
         binding.polyspec_verify_level(rows_p, rows_q, self.tokens2, self.uniforms2, self.temperature, block_len=self.block_len2,
@@ -102,12 +123,15 @@ class StagedBatch:
         self._check(lib.polyspec_staged_accumulate(s, p(self.tokens2), p(self.block_len2), p(self.out2["accepted_len"]),
                                                    p(self.out2["next_token"]), p(self.u1), p(self.pos1), p(self.tokens1),
                                                    p(self.uniforms1), p(self.block_len1), q), "polyspec_staged_accumulate")
+        self._roll_back("M2", "M3")
+        self._reserve("M1", self.pos1, self.block_len1)
         rows_p = self._forward(self.M1, self.pos1, self._ar1)
         rows_q = self._forward(self.M2, self.pos1, self._ar1[:, : self.kcap])
         binding.polyspec_verify_level(rows_p, rows_q, self.tokens1, self.uniforms1, self.temperature, block_len=self.block_len1,
                                       workspace=self.ws1, out=self.out1, device_status=self.status)
         self._check(lib.polyspec_staged_commit(s, p(self.block_len1), p(self.out1["accepted_len"]), p(self.out1["next_token"]), q),
                     "polyspec_staged_commit")
+        self._roll_back("M1", "M2", "M3")
         self.iterations += 1
 
     def run(self, max_iterations: int = 100000) -> Dict[str, torch.Tensor]:
@@ -127,6 +151,6 @@ class StagedBatch:
         return out
 
 
-def staged_decode_batch(M1, M2, M3, drafts, u2, u1, K, mu, n_tokens, temperature) -> Dict[str, torch.Tensor]:
+def staged_decode_batch(M1, M2, M3, drafts, u2, u1, K, mu, n_tokens, temperature, caches=None) -> Dict[str, torch.Tensor]:
     """Algorithm 1 from position 0 for every sequence of the batch; see StagedBatch."""
-    return StagedBatch(M1, M2, M3, drafts, u2, u1, K, mu, n_tokens, temperature).run()
+    return StagedBatch(M1, M2, M3, drafts, u2, u1, K, mu, n_tokens, temperature, caches).run()
