@@ -16,9 +16,11 @@
 //   then     dequantisers, in sets of four warps (one per lane quarter): a set takes every second or third K block, so that the
 //            latencies of one (shared-memory reads, tensor-memory stores, barriers) pass behind the arithmetic of another
 //   last     epilogue, one or two warps per lane quarter, each its share of the columns
-// Tensor memory: A blocks in a ring, then accumulator slots in a ring; a slot holds `UNIT` groups.
+// Tensor memory: A blocks in a ring, then accumulator slots in a ring; a slot takes as many of a block's groups as leave two
+// slots, so that small groups do not multiply the handshakes.
 // With few rows an MMA is short and what a block costs is the MMA warp's own handshakes (some 80 cycles per wait that passes at
-// once, as much per commit): up to 64 rows, blocks of 256 elements, three sets and four epilogue warps; above, 128, two and eight.
+// once, as much per commit): blocks of 256 elements up to 64 rows, 128 above.  From 64 rows on, half the time is the hidden
+// rows' way from L2: every tile of 128 entries reads all of them.
 //
 // Every wait on an mbarrier is bounded: one that runs out raises an abort flag that all roles poll, sets POLYSPEC_ERR_TIMEOUT,
 // and the kernel still lets its copies land, frees tensor memory and returns.
@@ -120,21 +122,30 @@ struct Ring {
 };
 
 // Sizes of an instantiation.  NC: columns (hidden rows) per epilogue warp; EPI: epilogue warps; SETS: sets of dequantising warps;
-// BLOCK: K elements per block; UNIT: groups per accumulator slot.
-template <int NC_, int EPI_, int SETS_, int BLOCK_, int UNIT_>
+// BLOCK: K elements per block; ABLOCKS: A blocks in tensor memory.
+template <int NC_, int EPI_, int SETS_, int BLOCK_, int ABLOCKS_>
 struct Shape {
-    static constexpr int NC = NC_, EPI = EPI_, SETS = SETS_, BLOCK = BLOCK_, UNIT = UNIT_;
+    static constexpr int NC = NC_, EPI = EPI_, SETS = SETS_, BLOCK = BLOCK_, kABlocks = ABLOCKS_;
     static constexpr int N = NC * (EPI / 4);
     static constexpr int kThreads = 32 * (2 + kSetWarps * SETS + EPI);
     static constexpr int kSubs = BLOCK / kSub;
     static constexpr uint32_t kCodeBytes = kSubs * kSubBytes, kBoxBytes = N * 128, kStage = kCodeBytes + BLOCK / 64 * kBoxBytes;
     static constexpr int kACols = BLOCK / 2;                // two bf16 per 32-bit column
-    static constexpr int kSlotCols = UNIT * N;
-    static constexpr int kABlocks = 3 * kACols + 2 * kSlotCols <= kTmemCols ? 3 : 2;
-    static constexpr int kSlots = (kTmemCols - kABlocks * kACols) / kSlotCols < kMaxSlots ? (kTmemCols - kABlocks * kACols) / kSlotCols : kMaxSlots;
+    static constexpr int kAccCols = kTmemCols - kABlocks * kACols;
     static constexpr int kStages = (kSmemLimit - 4096) / kStage < kMaxStages ? (kSmemLimit - 4096) / kStage : kMaxStages;
     static constexpr size_t kSmem = 1024 + static_cast<size_t>(kStages) * kStage;
-    static_assert(kSlots >= 2 && kStages >= 3 && kStage % 1024 == 0 && kBoxBytes % 1024 == 0, "sizes");
+    static_assert(2 * N <= kAccCols && kStages >= 3 && kStage % 1024 == 0 && kBoxBytes % 1024 == 0 && kABlocks <= kMaxABlocks, "sizes");
+    // A wait tells a phase from the one before it, not from the one two before.  A set that comes to block b has seen the MMAs of
+    // block b - SETS - kABlocks done.  So the A block of b was last used by b - kABlocks, whose own predecessor there must be
+    // among those: SETS <= kABlocks; and the stage of b by b - kStages, which must be among those or the set's own.
+    static_assert(SETS <= kABlocks && (kStages >= SETS + kABlocks || kStages % SETS == 0), "phases");
+};
+// With GROUPS groups in a K block: groups per slot, slots.
+template <class S, int GROUPS>
+struct Slots {
+    static constexpr int kUnit = GROUPS >= 4 && 8 * S::N <= S::kAccCols ? 4 : GROUPS >= 2 && 4 * S::N <= S::kAccCols ? 2 : 1;
+    static constexpr int kCols = kUnit * S::N;
+    static constexpr int kCount = S::kAccCols / kCols < kMaxSlots ? S::kAccCols / kCols : kMaxSlots;
 };
 
 struct Barriers { uint32_t full, empty, a_full, a_empty, acc_full, acc_empty; };
@@ -145,6 +156,7 @@ struct Barriers { uint32_t full, empty, a_full, a_empty, acc_full, acc_empty; };
 template <class S, int GROUPS>
 __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers& bar, uint32_t tiles, uint32_t tmem, uint32_t tmem_acc, volatile int* abort_p)
 {
+    using L = Slots<S, GROUPS>;
     constexpr int kMmas = S::BLOCK / 16 / GROUPS;       // per group
     Ring st, ab, slot;
     slot.phase = 1;
@@ -155,14 +167,14 @@ __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers&
             const uint32_t b_lo = smem_desc_lo(tiles + st.at * S::kStage + S::kCodeBytes);
             const uint32_t a = tmem + ab.at * S::kACols;
 #pragma unroll
-            for (int g0 = 0; g0 < GROUPS; g0 += S::UNIT) {
+            for (int g0 = 0; g0 < GROUPS; g0 += L::kUnit) {
                 if (kb * GROUPS + g0 >= p.groups) break;
                 if (!warp_wait(bar.acc_empty + 8u * slot.at, slot.phase, abort_p)) return false;
                 tc_fence_after();
-                const uint32_t d = tmem_acc + slot.at * S::kSlotCols;
+                const uint32_t d = tmem_acc + slot.at * L::kCols;
                 if (elect_one()) {
 #pragma unroll
-                    for (int u = 0; u < S::UNIT && g0 + u < GROUPS; ++u) {
+                    for (int u = 0; u < L::kUnit; ++u) {
                         if (kb * GROUPS + g0 + u >= p.groups) break;
 #pragma unroll
                         for (int m = 0; m < kMmas; ++m) {
@@ -173,7 +185,7 @@ __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers&
                     umma_commit(bar.acc_full + 8u * slot.at);
                 }
                 __syncwarp();
-                slot.next(S::kSlots);
+                slot.next(L::kCount);
             }
             if (elect_one()) {
                 umma_commit(bar.empty + 8u * st.at);
@@ -209,26 +221,69 @@ __device__ __forceinline__ uint4 load_scales8(const TensorParams& p, const unsig
     return make_uint4(s[0], s[1], s[2], s[3]);
 }
 
-// An epilogue warp's sums of one slot: columns [0, NC) of each of `n` groups at t, scaled.
-template <class S>
-__device__ __forceinline__ void add_unit(float (&sum)[S::NC], uint32_t t, const uint32_t (&scale)[S::UNIT], int n)
+// An epilogue warp's whole run: for every item, the groups in order, a slot at a time, scaled and added to the running sums.
+template <class S, int GROUPS>
+__device__ __forceinline__ bool run_epilogue(const TensorParams& p, const Barriers& bar, uint32_t tmem_acc, int quarter, int share, int lane,
+                                             volatile int* abort_p)
 {
+    using L = Slots<S, GROUPS>;
+    constexpr int kBatch = S::NC >= 48 ? 24 : 32;        // columns read at a time, as the registers allow
+    Ring slot;
+    const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + share * S::NC;
+    for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
+        const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * S::N + share * S::NC;
+        const unsigned short* scale = p.scales + static_cast<size_t>(min(v, p.V - 1)) * p.groups;
+        float sum[S::NC];
 #pragma unroll
-    for (int u = 0; u < S::UNIT; ++u) {
-        if (u >= n) break;
-        const float s = __uint_as_float(scale[u]);
+        for (int i = 0; i < S::NC; ++i) sum[i] = 0.0f;
+        // scales in aligned runs of eight groups, the next run loaded while this one is used
+        uint4 run = make_uint4(0, 0, 0, 0), run_next = load_scales8(p, scale, 0);
+        for (int g = 0; g < p.groups; g += L::kUnit) {
+            if ((g & 7) == 0) {
+                run = run_next;
+                if (g + 8 < p.groups) run_next = load_scales8(p, scale, g / 8 + 1);
+            }
+            float s[L::kUnit];
 #pragma unroll
-        for (int c = 0; c < S::NC; c += 24) {
-            uint32_t x[24];
+            for (int u = 0; u < L::kUnit; ++u) {
+                const uint32_t at = (g + u) & 7, pair = at & 4 ? (at & 2 ? run.w : run.z) : (at & 2 ? run.y : run.x);
+                s[u] = __uint_as_float(at & 1 ? pair & 0xffff0000u : pair << 16);
+            }
+            if (!warp_wait(bar.acc_full + 8u * slot.at, slot.phase, abort_p)) return false;
+            tc_fence_after();
+            const uint32_t t = t0 + slot.at * L::kCols;
+            const int left = p.groups - g;
 #pragma unroll
-            for (int q = 0; q < 24; q += 8)
-                if (c + q < S::NC) tmem_ld8(t + u * S::N + c + q, x + q);
-            tmem_ld_wait();
+            for (int c = 0; c < L::kUnit * S::NC; c += kBatch) {
+                uint32_t x[kBatch];
 #pragma unroll
-            for (int i = 0; i < 24; ++i)
-                if (c + i < S::NC) sum[c + i] = fmaf(s, __uint_as_float(x[i]), sum[c + i]);
+                for (int q = 0; q < kBatch; q += 8) {
+                    const int u = (c + q) / S::NC, col = (c + q) % S::NC;           // (compile-time)
+                    if (u < L::kUnit && (u == 0 || u < left)) tmem_ld8(t + u * S::N + col, x + q);
+                }
+                tmem_ld_wait();
+#pragma unroll
+                for (int q = 0; q < kBatch; ++q) {
+                    const int u = (c + q) / S::NC, col = (c + q) % S::NC;
+                    if (u < L::kUnit && (u == 0 || u < left)) sum[col] = fmaf(s[u], __uint_as_float(x[q]), sum[col]);
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_local(bar.acc_empty + 8u * slot.at);
+            slot.next(L::kCount);
+        }
+        if (v >= p.V) continue;
+        const int n = min(S::NC, p.rows - row0);
+#pragma unroll
+        for (int i = 0; i < S::NC; ++i) {
+            if (i >= n) continue;
+            const size_t at = static_cast<size_t>(row0 + i) * p.V + v;
+            if (p.out_bf16) w4::store_logit<POLYSPEC_BF16>(p.out, at, sum[i]);
+            else w4::store_logit<POLYSPEC_F32>(p.out, at, sum[i]);
         }
     }
+    return true;
 }
 
 template <class S>
@@ -384,45 +439,9 @@ __global__ void __launch_bounds__(S::kThreads, 1) w4_tensor_kernel(const __grid_
     } else {
         // ------------------------------------------------------------------ epilogue
         const int quarter = warp & 3, share = (warp - 2 - kSetWarps * S::SETS) >> 2;
-        Ring slot;
-        const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + share * S::NC;
-        for (int item = blockIdx.x; ok && item < p.items; item += gridDim.x) {
-            const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * S::N + share * S::NC;
-            const unsigned short* scale = p.scales + static_cast<size_t>(min(v, p.V - 1)) * p.groups;
-            float sum[S::NC];
-#pragma unroll
-            for (int i = 0; i < S::NC; ++i) sum[i] = 0.0f;
-            // scales in aligned runs of eight groups, the next run loaded while this one is used
-            uint4 run, run_next = load_scales8(p, scale, 0);
-            for (int g = 0; g < p.groups; g += S::UNIT) {
-                if ((g & 7) == 0) {
-                    run = run_next;
-                    if (g + 8 < p.groups) run_next = load_scales8(p, scale, g / 8 + 1);
-                }
-                uint32_t now[S::UNIT];
-#pragma unroll
-                for (int u = 0; u < S::UNIT; ++u) {
-                    const uint32_t at = (g + u) & 7, pair = at & 4 ? (at & 2 ? run.w : run.z) : (at & 2 ? run.y : run.x);
-                    now[u] = at & 1 ? pair & 0xffff0000u : pair << 16;
-                }
-                if (!warp_wait(bar.acc_full + 8u * slot.at, slot.phase, abort_p)) { ok = false; break; }
-                tc_fence_after();
-                add_unit<S>(sum, t0 + slot.at * S::kSlotCols, now, p.groups - g);
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_local(bar.acc_empty + 8u * slot.at);
-                slot.next(S::kSlots);
-            }
-            if (!ok || v >= p.V) continue;
-            const int n = min(S::NC, p.rows - row0);
-#pragma unroll
-            for (int i = 0; i < S::NC; ++i) {
-                if (i >= n) continue;
-                const size_t at = static_cast<size_t>(row0 + i) * p.V + v;
-                if (p.out_bf16) w4::store_logit<POLYSPEC_BF16>(p.out, at, sum[i]);
-                else w4::store_logit<POLYSPEC_F32>(p.out, at, sum[i]);
-            }
-        }
+        if (per_sub == 1) ok = run_epilogue<S, S::kSubs>(p, bar, tmem_acc, quarter, share, lane, abort_p);
+        else if (per_sub == 2) ok = run_epilogue<S, 2 * S::kSubs>(p, bar, tmem_acc, quarter, share, lane, abort_p);
+        else ok = run_epilogue<S, 4 * S::kSubs>(p, bar, tmem_acc, quarter, share, lane, abort_p);
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
     }
 
@@ -498,12 +517,13 @@ cudaError_t launch_w4_tensor(const W4Problem& q, polyspec_dtype dt, int32_t* dev
     p.vectors = p.groups % 8 == 0 && (reinterpret_cast<uintptr_t>(q.scales) & 15u) == 0 && (reinterpret_cast<uintptr_t>(q.zeros) & 7u) == 0;
     // columns of an item: the rows cut evenly into blocks of at most 144, in the next size there is
     const int blocks = (q.rows + kMaxRowsPerItem - 1) / kMaxRowsPerItem, cols = (q.rows + blocks - 1) / blocks;
-    if (cols <= 16) return launch_shape<Shape<16, 4, 3, 256, 2>>(p, q, sms, stream);
-    if (cols <= 32) return launch_shape<Shape<32, 4, 3, 256, 2>>(p, q, sms, stream);
-    if (cols <= 64) return launch_shape<Shape<32, 8, 2, 256, 1>>(p, q, sms, stream);
-    if (cols <= 96) return launch_shape<Shape<48, 8, 2, 128, 1>>(p, q, sms, stream);
-    if (cols <= 128) return launch_shape<Shape<64, 8, 2, 128, 1>>(p, q, sms, stream);
-    return launch_shape<Shape<72, 8, 2, 128, 1>>(p, q, sms, stream);
+    if (cols <= 16) return launch_shape<Shape<16, 4, 3, 256, 3>>(p, q, sms, stream);
+    if (cols <= 32) return launch_shape<Shape<32, 4, 2, 256, 2>>(p, q, sms, stream);
+    if (cols <= 48) return launch_shape<Shape<24, 8, 2, 256, 2>>(p, q, sms, stream);
+    if (cols <= 64) return launch_shape<Shape<32, 8, 2, 256, 2>>(p, q, sms, stream);
+    if (cols <= 96) return launch_shape<Shape<48, 8, 2, 128, 2>>(p, q, sms, stream);
+    if (cols <= 128) return launch_shape<Shape<64, 8, 2, 128, 3>>(p, q, sms, stream);
+    return launch_shape<Shape<72, 8, 2, 128, 3>>(p, q, sms, stream);
 }
 
 }  // namespace polyspec
