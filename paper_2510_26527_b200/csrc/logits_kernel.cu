@@ -11,8 +11,8 @@
 // HBM-bound: every logit is read and written once, except that a vector of eight entries that the mask forbids as a whole
 // is written without being read, and that in place (out == logits) only what a control touches moves at all.
 // A CTA owns a slice of the vocabulary of one sequence and rows of the block.  It counts the history's tokens that fall into
-// its slice in shared memory (a 32-bit word per entry: bits 31..29 flags, below them n(v)), and whoever is first to touch an
-// entry puts it on a list.  The rows are streamed as vectors with nothing but the mask applied; then, behind one barrier, the
+// its slice in shared memory (a word per entry, the top three bits flags, below them n(v); 16 bits where no count can pass 13,
+// so that slices of 8192 entries leave room for several CTAs), and whoever is first to touch an entry puts it on a list.  The rows are streamed as vectors with nothing but the mask applied; then, behind one barrier, the
 // few listed entries of every row are computed from the logits as they were and stored over the vectors, a warp per row.  (A
 // text of thousands of tokens touches a few entries of every 256 that a warp moves: computing them where the vectors pass by
 // had the whole warp take the slow path almost every time, and a barrier per row cost a quarter of the time.)
@@ -29,7 +29,28 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kVec = 8;                                 // entries per vector: one byte of the mask
-constexpr uint32_t kSeenInPrompt = 1u << 31, kBiased = 1u << 30, kDrafted = 1u << 29, kCountMask = kDrafted - 1;
+constexpr int kMaxVpt = 4;                              // vectors per thread at most
+constexpr int kSparseBiases = 256;                       // up to so many biases are kept as a list that edits search, more as an array
+constexpr int kMaxNarrow = (1 << 13) - 1;               // longest history whose counts fit 13 bits
+
+// The count words of a slice, 32 or 16 bits each (two to a 32-bit word, which the atomics work on: a count cannot carry over).
+template <bool WIDE> struct Counts;
+template <> struct Counts<true> {
+    static constexpr uint32_t kSeenInPrompt = 1u << 31, kBiased = 1u << 30, kDrafted = 1u << 29, kCountMask = kDrafted - 1;
+    static constexpr int kBytes = 4;
+    uint32_t* w;
+    __device__ __forceinline__ uint32_t get(int at) const { return w[at]; }
+    __device__ __forceinline__ uint32_t set(unsigned at, uint32_t flag) const { return atomicOr(&w[at], flag); }
+    __device__ __forceinline__ uint32_t add(unsigned at) const { return atomicAdd(&w[at], 1u); }
+};
+template <> struct Counts<false> {
+    static constexpr uint32_t kSeenInPrompt = 1u << 15, kBiased = 1u << 14, kDrafted = 1u << 13, kCountMask = kDrafted - 1;
+    static constexpr int kBytes = 2;
+    uint32_t* w;
+    __device__ __forceinline__ uint32_t get(int at) const { return reinterpret_cast<const unsigned short*>(w)[at]; }
+    __device__ __forceinline__ uint32_t set(unsigned at, uint32_t flag) const { return atomicOr(&w[at >> 1], flag << (16 * (at & 1))) >> (16 * (at & 1)) & 0xffffu; }
+    __device__ __forceinline__ uint32_t add(unsigned at) const { return atomicAdd(&w[at >> 1], 1u << (16 * (at & 1))) >> (16 * (at & 1)) & 0xffffu; }
+};
 
 struct ControlParams {
     const void* logits;
@@ -65,6 +86,7 @@ template <> struct Vec8<POLYSPEC_BF16> {
     uint4 a;
     __device__ __forceinline__ void load(const void* p, size_t e) { a = *reinterpret_cast<const uint4*>(static_cast<const char*>(p) + e * 2); }
     __device__ __forceinline__ void store(void* p, size_t e) const { *reinterpret_cast<uint4*>(static_cast<char*>(p) + e * 2) = a; }
+    __device__ __forceinline__ void fill_neg_inf() { a = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }
     // entries whose bit is clear become -inf, whatever they hold
     __device__ __forceinline__ void forbid(uint32_t allowed)
     {
@@ -90,6 +112,7 @@ template <> struct Vec8<POLYSPEC_F32> {
         q[0] = a;
         q[1] = b;
     }
+    __device__ __forceinline__ void fill_neg_inf() { a = b = make_uint4(0xff800000u, 0xff800000u, 0xff800000u, 0xff800000u); }
     __device__ __forceinline__ void forbid(uint32_t allowed)
     {
         const uint32_t lo = spread4(allowed), hi = spread4(allowed >> 4);
@@ -117,20 +140,32 @@ template <int DT> __device__ __forceinline__ void store_logit(void* p, size_t e,
 }
 
 // What a CTA knows of its slice.
+template <bool WIDE>
 struct Slice {
-    uint32_t* count;            // [slice]
-    float* bias;                // [slice] or nullptr
+    Counts<WIDE> count;         // [slice]
     unsigned short* list;       // [slice]: the touched entries
     int* n_list;
     const int32_t* draft;       // [rows - 1]: entries of the slice the drafted tokens are, -1 where they lie outside
+    float* bias;                // sums of the biases: [slice], or [min(n_bias, kSparseBiases)] for the entries in bias_at; or nullptr
+    unsigned short* bias_at;    // nullptr: bias is an array over the slice
+    int* n_bias_at;
+    __device__ __forceinline__ float bias_of(int e) const
+    {
+        if (!bias_at) return bias[e];
+        for (int i = 0; i < *n_bias_at; ++i)
+            if (bias_at[i] == e) return bias[i];
+        return 0.0f;
+    }
 };
 
 // One sequence's slice [v0, v0 + n) of the vocabulary, counted by the whole CTA.
-__device__ __forceinline__ void count_context(const ControlParams& p, int b, int v0, int n, bool report, const Slice& s, int32_t* drafted)
+template <bool WIDE>
+__device__ __forceinline__ void count_context(const ControlParams& p, int b, int v0, int n, bool report, const Slice<WIDE>& s, int32_t* drafted)
 {
+    using C = Counts<WIDE>;
     const int tid = threadIdx.x;
-    for (int i = tid; i < n / 4; i += kThreads) reinterpret_cast<uint4*>(s.count)[i] = make_uint4(0, 0, 0, 0);      // n is a multiple of 8
-    if (s.bias)
+    for (int i = tid; i < n * C::kBytes / 16; i += kThreads) reinterpret_cast<uint4*>(s.count.w)[i] = make_uint4(0, 0, 0, 0);   // n is a multiple of 8
+    if (s.bias && !s.bias_at)
         for (int i = tid; i < n / 4; i += kThreads) reinterpret_cast<uint4*>(s.bias)[i] = make_uint4(0, 0, 0, 0);
     if (tid == 0) *s.n_list = 0;
     __syncthreads();
@@ -145,7 +180,7 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
         const unsigned at = static_cast<unsigned>(t) - first;
         const bool mine = t >= 0 && at < static_cast<unsigned>(n);
         drafted[tid] = mine ? static_cast<int>(at) : -1;
-        if (mine) touch(at, atomicOr(&s.count[at], kDrafted));
+        if (mine) touch(at, s.count.set(at, C::kDrafted));
     }
     if (p.c.history) {
         int len = p.c.history_len ? p.c.history_len[b] : p.c.history_cap;
@@ -157,7 +192,7 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
         auto add = [&](int i, int t) {
             if (report && t >= p.c.vocab_size) bad_input(p.status);
             const unsigned at = static_cast<unsigned>(t) - first;
-            if (t >= 0 && at < static_cast<unsigned>(n)) touch(at, i < prompt ? atomicOr(&s.count[at], kSeenInPrompt) : atomicAdd(&s.count[at], 1u));
+            if (t >= 0 && at < static_cast<unsigned>(n)) touch(at, i < prompt ? s.count.set(at, C::kSeenInPrompt) : s.count.add(at));
         };
         constexpr int kLoads = 4;
         int done = 0;
@@ -189,6 +224,7 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
         const int lane = tid & 31;
         const int32_t* toks = p.c.bias_tokens + static_cast<size_t>(b) * p.c.n_bias;
         const float* vals = p.c.bias_values + static_cast<size_t>(b) * p.c.n_bias;
+        int kept = 0;                           // entries in bias_at
         for (int i0 = 0; i0 < p.c.n_bias; i0 += 32) {
             const int i = i0 + lane;
             const int t = i < p.c.n_bias ? toks[i] : -1;
@@ -199,18 +235,30 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
             const unsigned any = __ballot_sync(0xffffffffu, mine);
             if (!any) continue;
             const unsigned same = __match_any_sync(0xffffffffu, mine ? t : -1 - lane);
-            float sum = mine ? s.bias[at] : 0.0f;
+            int place = s.bias_at ? -1 : static_cast<int>(at);
+            if (mine && s.bias_at)
+                for (int q = 0; q < kept; ++q)
+                    if (s.bias_at[q] == at) place = q;
+            float sum = mine && place >= 0 ? s.bias[place] : 0.0f;
             for (unsigned left = any; left; left &= left - 1) {      // list order, every lane the same number of turns
                 const int src = __ffs(left) - 1;
                 const float y = __shfl_sync(0xffffffffu, x, src);
                 if (same >> src & 1u) sum += y;
             }
-            if (mine && lane == __ffs(same) - 1) {
-                s.bias[at] = sum;
-                touch(at, atomicOr(&s.count[at], kBiased));
+            const bool leads = mine && lane == __ffs(same) - 1;
+            const unsigned fresh = __ballot_sync(0xffffffffu, leads && place < 0);
+            if (leads) {
+                if (place < 0) {
+                    place = kept + __popc(fresh & ((1u << lane) - 1u));
+                    s.bias_at[place] = static_cast<unsigned short>(at);
+                }
+                s.bias[place] = sum;
+                touch(at, s.count.set(at, C::kBiased));
             }
+            kept += __popc(fresh);
             __syncwarp();
         }
+        if (s.bias_at && lane == 0) *s.n_bias_at = kept;
     }
     __syncthreads();
 }
@@ -219,7 +267,7 @@ __device__ __forceinline__ void count_context(const ControlParams& p, int b, int
 template <int DT, int VPT, bool FULL>
 __device__ __forceinline__ void stream_rows(const ControlParams& p, int b, int v0, int n, int j0, int j1, bool in_place)
 {
-    constexpr int kRows = 2;                            // rows in flight
+    constexpr int kRows = VPT >= 4 ? 1 : 2;             // rows in flight
     const int tid = threadIdx.x;
     const size_t first = static_cast<size_t>(b) * p.rows;
     const unsigned char* mask = p.c.mask ? reinterpret_cast<const unsigned char*>(p.c.mask) + v0 / kVec + tid : nullptr;
@@ -251,7 +299,8 @@ __device__ __forceinline__ void stream_rows(const ControlParams& p, int b, int v
 #pragma unroll
             for (int u = 0; u < VPT; ++u) {
                 if (j + r < j1 && inside(u) && (!in_place || allowed[r][u] != 0xffu)) {
-                    if (allowed[r][u] != 0xffu) z[r][u].forbid(allowed[r][u]);
+                    if (allowed[r][u] == 0) z[r][u].fill_neg_inf();
+                    else if (allowed[r][u] != 0xffu) z[r][u].forbid(allowed[r][u]);
                     z[r][u].store(p.out, at + static_cast<size_t>(r) * p.V + u * (kThreads * kVec));
                 }
                 allowed[r][u] = next[r][u];
@@ -260,10 +309,11 @@ __device__ __forceinline__ void stream_rows(const ControlParams& p, int b, int v
 }
 
 // The listed entries of row j, entries start, start + step, ... of the list: two loads in flight (four took more registers than they saved time).
-template <int DT>
-__device__ __forceinline__ void edit_row(const ControlParams& p, const Slice& s, int listed, int b, int v0, int j, int start, int step,
+template <int DT, bool WIDE>
+__device__ __forceinline__ void edit_row(const ControlParams& p, const Slice<WIDE>& s, int listed, int b, int v0, int j, int start, int step,
                                          float r, float f, float pr)
 {
+    using C = Counts<WIDE>;
     constexpr int kAhead = 2;
     const size_t row = (static_cast<size_t>(b) * p.rows + j) * p.V + v0;
     const unsigned char* mask = p.c.mask ? reinterpret_cast<const unsigned char*>(p.c.mask) + (static_cast<size_t>(b) * p.rows + j) * p.mask_bytes + v0 / kVec
@@ -278,11 +328,11 @@ __device__ __forceinline__ void edit_row(const ControlParams& p, const Slice& s,
             e[q] = 0;
             if (i + q * step < listed) {
                 e[q] = s.list[i + q * step];
-                w[q] = s.count[e[q]];
-                times[q] = w[q] & kCountMask;
-                if (w[q] & kDrafted)
+                w[q] = s.count.get(e[q]);
+                times[q] = w[q] & C::kCountMask;
+                if (w[q] & C::kDrafted)
                     for (int d = 0; d < j; ++d) times[q] += s.draft[d] == e[q];
-                if (!times[q] && !(w[q] & (kSeenInPrompt | kBiased))) w[q] = 0;                     // drafted later than this row
+                if (!times[q] && !(w[q] & (C::kSeenInPrompt | C::kBiased))) w[q] = 0;                     // drafted later than this row
                 else if (mask && !(mask[e[q] / kVec] >> (e[q] % kVec) & 1u)) w[q] = 0;
             }
         }
@@ -293,21 +343,21 @@ __device__ __forceinline__ void edit_row(const ControlParams& p, const Slice& s,
         for (int q = 0; q < kAhead; ++q) {
             if (!w[q]) continue;
             float y = x[q];
-            if (times[q] || (w[q] & kSeenInPrompt)) y = y > 0.0f ? y / r : y * r;
+            if (times[q] || (w[q] & C::kSeenInPrompt)) y = y > 0.0f ? y / r : y * r;
             if (times[q]) y = y - f * static_cast<float>(times[q]) - pr;
-            if (w[q] & kBiased) y += s.bias[e[q]];
+            if (w[q] & C::kBiased) y += s.bias_of(e[q]);
             store_logit<DT>(p.out, row + e[q], y);
         }
     }
 }
 
 // VPT vectors of eight entries per thread: a slice of kThreads * VPT * 8 entries.
-// COUNTS: penalties or biases are there; otherwise only a mask.
-template <int DT, int VPT, bool COUNTS>
-__global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
+// COUNTS: penalties or biases are there; otherwise only a mask.  WIDE: 32-bit counts.
+template <int DT, int VPT, bool COUNTS, bool WIDE>
+__global__ void __launch_bounds__(kThreads, 5) logits_kernel(const ControlParams p)
 {
     extern __shared__ uint4 smem_controls[];
-    __shared__ int n_list;
+    __shared__ int n_list, n_bias_at;
     __shared__ int32_t drafted[kMaxK];
     constexpr int kSlice = kThreads * VPT * kVec;
     const int tid = threadIdx.x;
@@ -329,11 +379,13 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
     if (!COUNTS) return;
 
     const bool report = slice == 0 && group == 0;
-    Slice s;
-    s.count = reinterpret_cast<uint32_t*>(smem_controls);
-    s.list = reinterpret_cast<unsigned short*>(s.count + kSlice);
-    s.bias = p.c.bias_tokens ? reinterpret_cast<float*>(s.list + kSlice) : nullptr;
+    Slice<WIDE> s;
+    s.count.w = reinterpret_cast<uint32_t*>(smem_controls);
+    s.bias = p.c.bias_tokens ? reinterpret_cast<float*>(reinterpret_cast<char*>(smem_controls) + kSlice * (Counts<WIDE>::kBytes + 2)) : nullptr;
+    s.list = reinterpret_cast<unsigned short*>(reinterpret_cast<char*>(smem_controls) + kSlice * Counts<WIDE>::kBytes);
+    s.bias_at = p.c.n_bias <= kSparseBiases ? reinterpret_cast<unsigned short*>(s.bias + kSparseBiases) : nullptr;
     s.n_list = &n_list;
+    s.n_bias_at = &n_bias_at;
     s.draft = drafted;
     float r = p.c.repetition ? p.c.repetition[b] : 1.0f;
     const float f = p.c.frequency ? p.c.frequency[b] : 0.0f, pr = p.c.presence ? p.c.presence[b] : 0.0f;
@@ -341,14 +393,14 @@ __global__ void __launch_bounds__(kThreads) logits_kernel(const ControlParams p)
         if (report && tid == 0) bad_input(p.status);
         r = 1.0f;
     }
-    count_context(p, b, v0, n, report, s, drafted);     // its barriers also put the vectors before the edits
+    count_context<WIDE>(p, b, v0, n, report, s, drafted);     // its barriers also put the vectors before the edits
     const int listed = n_list;
     if (!listed) return;
     // the CTA's warps over its rows: several per row where there are fewer rows than warps
     constexpr int kWarps = kThreads / 32;
     const int warp = tid >> 5, rows = j1 - j0, per_row = max(1, kWarps / rows);
     if (warp >= rows * per_row) return;
-    for (int j = j0 + warp % rows; j < j1; j += kWarps) edit_row<DT>(p, s, listed, b, v0, j, (warp / rows) * 32 + (tid & 31), per_row * 32, r, f, pr);
+    for (int j = j0 + warp % rows; j < j1; j += kWarps) edit_row<DT, WIDE>(p, s, listed, b, v0, j, (warp / rows) * 32 + (tid & 31), per_row * 32, r, f, pr);
 }
 
 template <int DT, int VPT>
@@ -359,33 +411,38 @@ cudaError_t launch_vpt(ControlParams& p, bool counts, cudaStream_t stream)
     p.row_groups = (p.rows + p.rows_per_group - 1) / p.rows_per_group;
     const long long blocks = static_cast<long long>(p.slices) * p.row_groups * p.B;
     if (blocks > 0x7fffffffLL) return cudaErrorInvalidValue;
-    const size_t smem = counts ? static_cast<size_t>(kSlice) * (p.c.bias_tokens ? 10 : 6) : 0;
-    if (counts) {
+    const bool wide = p.c.history && p.c.history_cap > kMaxNarrow;
+    const size_t biases = !p.c.bias_tokens ? 0 : p.c.n_bias <= kSparseBiases ? kSparseBiases * 6 : kSlice * 4;
+    const size_t smem = counts ? static_cast<size_t>(kSlice) * ((wide ? 4 : 2) + 2) + biases : 0;
+    auto launch = [&](auto kernel) {
         if (smem > 48 * 1024) {
-            cudaError_t e = cudaFuncSetAttribute(logits_kernel<DT, VPT, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
             if (e != cudaSuccess) return e;
         }
-        logits_kernel<DT, VPT, true><<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(p);
-    } else {
-        logits_kernel<DT, VPT, false><<<static_cast<unsigned>(blocks), kThreads, 0, stream>>>(p);
-    }
-    return cudaGetLastError();
+        kernel<<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(p);
+        return cudaGetLastError();
+    };
+    if (!counts) return launch(logits_kernel<DT, VPT, false, false>);
+    return wide ? launch(logits_kernel<DT, VPT, true, true>) : launch(logits_kernel<DT, VPT, true, false>);
 }
 
 template <int DT>
 cudaError_t launch_controls(ControlParams& p, bool counts, cudaStream_t stream)
 {
-    // Few sequences: smaller slices, then fewer rows per CTA, until there are about eight CTAs for each of 148 SMs; many: the
-    // largest slice and all rows of a sequence, so that the history is counted as seldom as possible.
-    const long long want = 8 * 148;
+    // Many sequences: the largest slices and all rows of a sequence, so that the history is counted as seldom as possible
+    // (256 x 5 rows of 152064: slices of 8192 entries 134 us, of 4096 168 us).  Fewer: smaller slices down to eight CTAs for
+    // each of 148 SMs, so that the ones with the longest lists do not run on alone (64 x 7 of 128256, texts of 4096: 4096
+    // entries 57 us, 8192 entries 78 us); then fewer rows per CTA down to four, since each CTA counts the history again
+    // (8 x 9 of 32000, texts of 2000: to four 9.6 us, to eight 13.2 us).
     auto ctas = [&](int vpt, int rpg) {
         const long long s = (p.V + kThreads * vpt * kVec - 1) / (kThreads * vpt * kVec);
         return s * ((p.rows + rpg - 1) / rpg) * p.B;
     };
-    int vpt = 2, rpg = p.rows;
-    while (vpt > 1 && ctas(vpt, rpg) < want) vpt >>= 1;
-    while (rpg > 1 && ctas(vpt, rpg) < want) rpg = (rpg + 1) / 2;
+    int vpt = kMaxVpt, rpg = p.rows;
+    while (vpt > 1 && ctas(vpt, rpg) < 8 * 148) vpt >>= 1;
+    while (rpg > 1 && ctas(vpt, rpg) < 4 * 148) rpg = (rpg + 1) / 2;
     p.rows_per_group = rpg;
+    if (vpt == 4) return launch_vpt<DT, 4>(p, counts, stream);
     return vpt == 2 ? launch_vpt<DT, 2>(p, counts, stream) : launch_vpt<DT, 1>(p, counts, stream);
 }
 
