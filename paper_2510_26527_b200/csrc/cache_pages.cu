@@ -11,6 +11,7 @@
 // Moving page contents is HBM-bound: warps copy 2 KiB pieces, four independent 16-byte loads per lane before the stores.
 #include <mutex>
 
+#include "launch.cuh"
 #include "polyspec_kernels.cuh"
 
 namespace polyspec {
@@ -139,6 +140,10 @@ __global__ void __launch_bounds__(kPlanThreads, 1) reserve_kernel(const polyspec
     const int per = (words + kPlanThreads - 1) / kPlanThreads;          // consecutive words of the free bitmap per thread
     const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
     if (tid == 0) { taken = 0; n_copies = 0; }
+    wait_for_stream();
+    // the first sequences' needs are read beside the bitmap: both are chains of dependent loads
+    Need first = {false, false, false, false, 0, 0, 0};
+    if (tid < s.n_seqs) first = need_of(s, base, extra, plus, tid);
     int mine = 0;
     for (int w = w0; w < w1; ++w) mine += __popc(s.free_bits[w]);
     int n_free, total;
@@ -148,8 +153,8 @@ __global__ void __launch_bounds__(kPlanThreads, 1) reserve_kernel(const polyspec
     int before = 0;
     for (int b0 = 0; b0 < s.n_seqs; b0 += kPlanThreads) {
         const int b = b0 + tid;
-        Need q = {false, false, false, false, 0, 0, 0};
-        if (b < s.n_seqs) q = need_of(s, base, extra, plus, b);
+        Need q = first;
+        if (b0 > 0) q = b < s.n_seqs ? need_of(s, base, extra, plus, b) : Need{false, false, false, false, 0, 0, 0};
         const int n = q.grow ? q.pages + (q.copy ? 1 : 0) : 0;
         // a running sum past the pool's size says no more than the pool's size does: it is held there, so it cannot overflow
         const int start = before + block_exclusive(min(n, s.n_pages + 1), sums, &total);
@@ -212,6 +217,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) reserve_kernel(const polyspec
 __global__ void rollback_kernel(const polyspec_cache_pages s, const int32_t* base, const int32_t* extra, int plus, int32_t* status)
 {
     const int b = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    wait_for_stream();
     if (b >= s.n_seqs) return;
     const long long to = target_len(base, extra, plus, b);
     const int len = held_len(s, b);
@@ -235,6 +241,7 @@ __global__ void rollback_kernel(const polyspec_cache_pages s, const int32_t* bas
 __global__ void fork_kernel(const polyspec_cache_pages s, const int32_t* src, const int32_t* dst, int n, int32_t* status)
 {
     const int i = blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    wait_for_stream();
     if (i >= n) return;
     const int from = src[i], to = dst[i];
     if (from < 0 && to < 0) return;                                     // an unused slot of the list
@@ -284,6 +291,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const polyspec
     const int per = (words + kPlanThreads - 1) / kPlanThreads;
     const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
     int mine = 0, n_free, n_moves;
+    wait_for_stream();
     for (int w = w0; w < w1; ++w) mine += __popc(s.free_bits[w]);
     block_exclusive(mine, sums, &n_free);
     const int n_live = s.n_pages - n_free;
@@ -339,6 +347,7 @@ struct Pools {
 // Copies the planned pages in every plane of every pool; a warp takes pieces of 2 KiB, four loads in flight per lane.
 __global__ void __launch_bounds__(256) move_kernel(const polyspec_cache_pages s, Plan plan, Pools pools, int rename)
 {
+    wait_for_stream();
     if (rename) rename_entries(s, plan);
     const int n = *plan.n_copies;
     const int lane = threadIdx.x & 31;
@@ -400,8 +409,7 @@ cudaError_t launch_move(const polyspec_cache_pages& s, const Plan& plan, const p
     cudaError_t e = cudaGetDevice(&dev);
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     if (e != cudaSuccess) return e;
-    move_kernel<<<sms * 8, 256, 0, stream>>>(s, plan, q, rename ? 1 : 0);
-    return cudaGetLastError();
+    return launch_early(move_kernel, dim3(static_cast<unsigned>(sms * 8)), 256, 0, stream, s, plan, q, rename ? 1 : 0);
 }
 
 }  // namespace
@@ -449,8 +457,7 @@ polyspec_status polyspec_cache_reserve(const polyspec_cache_pages* s, const int3
     if (st != POLYSPEC_OK) return st;
     const Plan plan = plan_of(workspace, s->n_seqs, s->n_pages);
     cudaStream_t q = static_cast<cudaStream_t>(cuda_stream);
-    reserve_kernel<<<1, kPlanThreads, 0, q>>>(*s, base, extra, plus, plan, device_status);
-    if (cuda_failed(cudaGetLastError())) return POLYSPEC_ERR_CUDA;
+    if (cuda_failed(launch_early(reserve_kernel, dim3(1), kPlanThreads, 0, q, *s, base, extra, plus, plan, device_status))) return POLYSPEC_ERR_CUDA;
     if (n_pools > 0 && cuda_failed(launch_move(*s, plan, pools, n_pools, false, q))) return POLYSPEC_ERR_CUDA;
     return POLYSPEC_OK;
 }
@@ -461,8 +468,9 @@ polyspec_status polyspec_cache_rollback(const polyspec_cache_pages* s, const int
     const polyspec_status st = check_pages(s);
     if (st != POLYSPEC_OK) return st;
     if (!base) return POLYSPEC_ERR_INVALID_ARG;
-    rollback_kernel<<<(s->n_seqs + 3) / 4, 128, 0, static_cast<cudaStream_t>(cuda_stream)>>>(*s, base, extra, plus, device_status);
-    return cuda_failed(cudaGetLastError()) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
+    const dim3 grid(static_cast<unsigned>((s->n_seqs + 3) / 4));
+    return cuda_failed(launch_early(rollback_kernel, grid, 128, 0, static_cast<cudaStream_t>(cuda_stream), *s, base, extra, plus, device_status))
+               ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }
 
 polyspec_status polyspec_cache_fork(const polyspec_cache_pages* s, const int32_t* src, const int32_t* dst, int n, int32_t* device_status,
@@ -471,8 +479,9 @@ polyspec_status polyspec_cache_fork(const polyspec_cache_pages* s, const int32_t
     const polyspec_status st = check_pages(s);
     if (st != POLYSPEC_OK) return st;
     if (!src || !dst || n < 1) return POLYSPEC_ERR_INVALID_ARG;
-    fork_kernel<<<(n + 3) / 4, 128, 0, static_cast<cudaStream_t>(cuda_stream)>>>(*s, src, dst, n, device_status);
-    return cuda_failed(cudaGetLastError()) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
+    const dim3 grid(static_cast<unsigned>((n + 3) / 4));
+    return cuda_failed(launch_early(fork_kernel, grid, 128, 0, static_cast<cudaStream_t>(cuda_stream), *s, src, dst, n, device_status))
+               ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }
 
 polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s, const polyspec_cache_pool* pools, int n_pools, int32_t* moved_to,
@@ -484,8 +493,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s, const poly
     if (st != POLYSPEC_OK) return st;
     const Plan plan = plan_of(workspace, s->n_seqs, s->n_pages);
     cudaStream_t q = static_cast<cudaStream_t>(cuda_stream);
-    compact_kernel<<<1, kPlanThreads, 0, q>>>(*s, plan, moved_to);
-    if (cuda_failed(cudaGetLastError())) return POLYSPEC_ERR_CUDA;
+    if (cuda_failed(launch_early(compact_kernel, dim3(1), kPlanThreads, 0, q, *s, plan, moved_to))) return POLYSPEC_ERR_CUDA;
     if (cuda_failed(launch_move(*s, plan, pools, n_pools, true, q))) return POLYSPEC_ERR_CUDA;
     return POLYSPEC_OK;
 }

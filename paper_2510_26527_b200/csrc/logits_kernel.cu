@@ -21,6 +21,7 @@
 
 #include <algorithm>
 
+#include "launch.cuh"
 #include "polyspec_kernels.cuh"
 #include "stream_device.cuh"
 
@@ -361,6 +362,7 @@ __global__ void __launch_bounds__(kThreads, 5) logits_kernel(const ControlParams
     __shared__ int32_t drafted[kMaxK];
     constexpr int kSlice = kThreads * VPT * kVec;
     const int tid = threadIdx.x;
+    wait_for_stream();
     // sequences before slices: token ids are frequent at the low end, so that the slices with long lists start first (the other
     // way round, the last of them ran alone at the end)
     int at = blockIdx.x;
@@ -419,8 +421,7 @@ cudaError_t launch_vpt(ControlParams& p, bool counts, cudaStream_t stream)
             const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
             if (e != cudaSuccess) return e;
         }
-        kernel<<<static_cast<unsigned>(blocks), kThreads, smem, stream>>>(p);
-        return cudaGetLastError();
+        return launch_early(kernel, dim3(static_cast<unsigned>(blocks)), kThreads, smem, stream, p);
     };
     if (!counts) return launch(logits_kernel<DT, VPT, false, false>);
     return wide ? launch(logits_kernel<DT, VPT, true, true>) : launch(logits_kernel<DT, VPT, true, false>);

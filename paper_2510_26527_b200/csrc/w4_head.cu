@@ -24,6 +24,7 @@
 #include <algorithm>
 #include <mutex>
 
+#include "launch.cuh"
 #include "polyspec_kernels.cuh"
 #include "tensor_device.cuh"
 #include "w4_kernels.cuh"
@@ -137,8 +138,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     __syncwarp();
-    // what is read from here on, an earlier kernel of the stream may have written
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    wait_for_stream();
     // the hidden rows' loads go out first: behind the rings' requests they would wait for megabytes of codes
     // (in row order, so that a warp asks for whole lines: 148 CTAs read the same ones)
     constexpr int kBatch = 8;
@@ -334,18 +334,7 @@ cudaError_t launch_stream_t(const StreamParams& p, int sms, cudaStream_t stream)
     const size_t smem = stream_smem(p.d, p.ring);
     cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<G, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
-    // programmatic launch: the CTAs set up their barriers while the kernel before drains, and wait before their first read
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(std::min(sms, p.tiles)));
-    cfg.blockDim = dim3(kThreadsS);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = stream;
-    cudaLaunchAttribute attr;
-    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, w4_stream_kernel<G, DT>, p);
+    return launch_early(w4_stream_kernel<G, DT>, dim3(static_cast<unsigned>(std::min(sms, p.tiles))), kThreadsS, smem, stream, p);
 }
 
 template <int G>

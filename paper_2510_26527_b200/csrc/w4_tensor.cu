@@ -29,6 +29,7 @@
 #include <algorithm>
 #include <mutex>
 
+#include "launch.cuh"
 #include "polyspec_kernels.cuh"
 #include "tensor_device.cuh"
 #include "w4_kernels.cuh"
@@ -323,6 +324,7 @@ __global__ void __launch_bounds__(S::kThreads, 1) w4_tensor_kernel(const __grid_
     volatile int* abort_p = &abort_flag;
     const int per_sub = kSub / p.group;                 // groups per 128 elements: 1, 2 or 4
     bool ok = true;
+    wait_for_stream();
 
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
@@ -484,8 +486,7 @@ cudaError_t launch_shape(TensorParams& p, const W4Problem& q, int sms, cudaStrea
         return cudaErrorInvalidValue;
     cudaError_t e = cudaFuncSetAttribute(w4_tensor_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmem));
     if (e != cudaSuccess) return e;
-    w4_tensor_kernel<S><<<std::min(sms, p.items), S::kThreads, S::kSmem, stream>>>(p);
-    return cudaGetLastError();
+    return launch_early(w4_tensor_kernel<S>, dim3(static_cast<unsigned>(std::min(sms, p.items))), S::kThreads, S::kSmem, stream, p);
 }
 
 }  // namespace
