@@ -991,7 +991,7 @@ def polyspec_process_logits(logits, draft_tokens=None, history=None, history_len
 
 def polyspec_cache_workspace(n_seqs: int, n_pages: int) -> int:
     n = ctypes.c_size_t(0)
-    _check(load_library().polyspec_cache_workspace(n_seqs, n_pages, ctypes.byref(n)), "polyspec_cache_workspace")
+    _check(load_library().polyspec_cache_workspace(n_seqs, n_pages, n), "polyspec_cache_workspace")
     return n.value
 
 
@@ -1002,12 +1002,13 @@ class CachePages:
     calls on one state are ordered anyway."""
 
     def __init__(self, table, len, refs, free_bits, page_tokens):
+        i32 = torch.int32
+        if table.dtype is not i32 or len.dtype is not i32 or refs.dtype is not i32 or free_bits.dtype is not i32:
+            raise TypeError("table, len, refs and free_bits must be int32")
         n_seqs, max_pages = table.shape
         n_pages = refs.numel()
-        _expect("table", table, torch.int32)
-        _expect("len", len, torch.int32, (n_seqs,))
-        _expect("refs", refs, torch.int32, (n_pages,))
-        _expect("free_bits", free_bits, torch.int32, ((n_pages + 31) // 32,))
+        if len.shape != (n_seqs,) or refs.dim() != 1 or free_bits.shape != ((n_pages + 31) // 32,):
+            raise ValueError("shapes must be table [n_seqs,max_pages], len [n_seqs], refs [n_pages], free_bits [ceil(n_pages/32)]")
         self.dev = _one_device(table, len, refs, free_bits)
         self.table, self.len, self.refs, self.free_bits = table, len, refs, free_bits
         self.n_seqs, self.max_pages, self.n_pages, self.page_tokens = n_seqs, max_pages, n_pages, int(page_tokens)
@@ -1036,6 +1037,14 @@ def _same_device(pages, *tensors):
     return pages.dev
 
 
+def _targets(pages, base, extra):
+    if base.dtype is not torch.int32 or (extra is not None and extra.dtype is not torch.int32):
+        raise TypeError("base and extra must be int32")
+    n = (pages.n_seqs,)
+    if base.shape != n or (extra is not None and extra.shape != n):
+        raise ValueError("base and extra must be [n_seqs]")
+
+
 def _pools(pages, pools):
     """pools: tensors [n_planes, n_pages, ...], each plane's page contiguous."""
     if len(pools) > CACHE_MAX_POOLS:
@@ -1049,8 +1058,7 @@ def _pools(pages, pools):
 def polyspec_cache_reserve(pages, base, extra=None, plus=0, pools=(), device_status=None, workspace=None, stream=None):
     """Grow every sequence to base[b] + extra[b] + plus tokens; a last page that others hold too is replaced by a copy of its
     own, in every pool ([n_planes, n_pages, ...] tensors).  pages.len tells what was granted.  Returns the status word."""
-    _expect("base", base, torch.int32, (pages.n_seqs,))
-    _expect("extra", extra, torch.int32, (pages.n_seqs,))
+    _targets(pages, base, extra)
     _expect("device_status", device_status, torch.int32)
     dev = _same_device(pages, base, extra, workspace, device_status, *pools)
     if workspace is None:
@@ -1063,8 +1071,7 @@ def polyspec_cache_reserve(pages, base, extra=None, plus=0, pools=(), device_sta
 
 def polyspec_cache_rollback(pages, base, extra=None, plus=0, device_status=None, stream=None):
     """Let every sequence fall back to base[b] + extra[b] + plus tokens (never up); returns the status word."""
-    _expect("base", base, torch.int32, (pages.n_seqs,))
-    _expect("extra", extra, torch.int32, (pages.n_seqs,))
+    _targets(pages, base, extra)
     _expect("device_status", device_status, torch.int32)
     dev = _same_device(pages, base, extra, device_status)
     device_status = _status_word(device_status, dev, stream)

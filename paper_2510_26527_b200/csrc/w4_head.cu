@@ -48,7 +48,7 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
 using namespace tensordev;
 
 constexpr int kPieceBytes = kTileS * kChunk / 2;        // 2 KiB
-constexpr int kMaxRing = 6;
+constexpr int kMaxRing = 2;                       // 64 KiB in flight per SM; six pieces put 28 MB of requests before the hidden rows and scales
 constexpr int kTableGroups = 8;                         // groups whose scales and zero points a warp holds at a time
 constexpr int kTableWords = kTableGroups * 32;
 constexpr int kSums = 8;                                // accumulators per lane: two m16 tiles x four
