@@ -113,6 +113,14 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
     return __all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag));
 }
 
+// The same for two barriers at once: what a passing wait costs is its latency, and the two overlap.
+__device__ __forceinline__ bool warp_wait2(uint32_t bar0, uint32_t parity0, uint32_t bar1, uint32_t parity1, volatile int* abort_flag)
+{
+    const bool first = mbar_try(bar0, parity0), second = mbar_try(bar1, parity1);
+    if (__all_sync(0xffffffffu, first && second)) return true;
+    return warp_wait(bar0, parity0, abort_flag) && warp_wait(bar1, parity1, abort_flag);
+}
+
 // A position in a ring of n: its index and the parity a consumer waits for.
 struct Ring {
     uint32_t at = 0, phase = 0;
@@ -154,6 +162,9 @@ struct Barriers { uint32_t full, empty, a_full, a_empty, acc_full, acc_empty; };
 // The MMA issuer's whole run.  The number of groups per K block is a template argument so that a block's MMAs are straight-line
 // code on uniform registers: with the loop bounds read from the parameters the issue alone took 750 cycles per 128 elements.
 // A full A block was made from the stage's codes after its copies, the hidden tile's among them, had landed: no wait for those.
+// One commit per slot is all the issuer signals with: whoever has seen a block's last slot full knows that its stage and its A
+// block have been read, and an epilogue warp hands both back (three commits a block, of some 60 cycles each, were on the
+// issuer's critical path).
 template <class S, int GROUPS>
 __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers& bar, uint32_t tiles, uint32_t tmem, uint32_t tmem_acc, volatile int* abort_p)
 {
@@ -161,22 +172,24 @@ __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers&
     constexpr int kMmas = S::BLOCK / 16 / GROUPS;       // per group
     Ring st, ab, slot;
     slot.phase = 1;
-    uint32_t last_stage = 0, last_stage_phase = 0, last_a = 0, last_a_phase = 0;
     for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
         for (int kb = 0; kb < p.kblocks; ++kb) {
-            if (!warp_wait(bar.a_full + 8u * ab.at, ab.phase, abort_p)) return false;
+            if (!warp_wait2(bar.a_full + 8u * ab.at, ab.phase, bar.acc_empty + 8u * slot.at, slot.phase, abort_p)) return false;
+            tc_fence_after();
             const uint32_t b_lo = smem_desc_lo(tiles + st.at * S::kStage + S::kCodeBytes);
             const uint32_t a = tmem + ab.at * S::kACols;
 #pragma unroll
             for (int g0 = 0; g0 < GROUPS; g0 += L::kUnit) {
                 if (kb * GROUPS + g0 >= p.groups) break;
-                if (!warp_wait(bar.acc_empty + 8u * slot.at, slot.phase, abort_p)) return false;
-                tc_fence_after();
+                if (g0 > 0) {
+                    if (!warp_wait(bar.acc_empty + 8u * slot.at, slot.phase, abort_p)) return false;
+                    tc_fence_after();
+                }
                 const uint32_t d = tmem_acc + slot.at * L::kCols;
                 if (elect_one()) {
 #pragma unroll
                     for (int u = 0; u < L::kUnit; ++u) {
-                        if (kb * GROUPS + g0 + u >= p.groups) break;
+                        if (u > 0 && kb * GROUPS + g0 + u >= p.groups) break;
 #pragma unroll
                         for (int m = 0; m < kMmas; ++m) {
                             const int kk = (g0 + u) * kMmas + m;        // 16-element slice of the block
@@ -188,19 +201,11 @@ __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers&
                 __syncwarp();
                 slot.next(L::kCount);
             }
-            if (elect_one()) {
-                umma_commit(bar.empty + 8u * st.at);
-                umma_commit(bar.a_empty + 8u * ab.at);
-            }
-            __syncwarp();
-            last_stage = st.at; last_stage_phase = st.phase;
-            last_a = ab.at; last_a_phase = ab.phase;
             st.next(S::kStages);
             ab.next(S::kABlocks);
         }
     }
-    // the last commits arrive on barriers of this CTA: it must not exit before
-    return warp_wait(bar.empty + 8u * last_stage, last_stage_phase, abort_p) && warp_wait(bar.a_empty + 8u * last_a, last_a_phase, abort_p);
+    return true;
 }
 
 // Zero points, scales of the aligned run `run` of eight groups of one row, as vectors where rows hold a multiple of eight groups.
@@ -229,7 +234,8 @@ __device__ __forceinline__ bool run_epilogue(const TensorParams& p, const Barrie
 {
     using L = Slots<S, GROUPS>;
     constexpr int kBatch = S::NC >= 48 ? 24 : 32;        // columns read at a time, as the registers allow
-    Ring slot;
+    Ring slot, st, ab;
+    const bool hands_back = quarter == 0 && share == 0;         // this warp returns stages and A blocks
     const uint32_t t0 = tmem_acc + (static_cast<uint32_t>(quarter * 32) << 16) + share * S::NC;
     for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
         const int v = item / p.row_blocks * kTileV + quarter * 32 + lane, row0 = item % p.row_blocks * S::N + share * S::NC;
@@ -252,6 +258,15 @@ __device__ __forceinline__ bool run_epilogue(const TensorParams& p, const Barrie
             }
             if (!warp_wait(bar.acc_full + 8u * slot.at, slot.phase, abort_p)) return false;
             tc_fence_after();
+            if (hands_back && ((g + L::kUnit) % GROUPS == 0 || g + L::kUnit >= p.groups)) {         // the block's last slot
+                tc_fence_before();
+                if (lane == 0) {
+                    mbar_arrive_local(bar.a_empty + 8u * ab.at);
+                    mbar_arrive_local(bar.empty + 8u * st.at);
+                }
+                st.next(S::kStages);
+                ab.next(S::kABlocks);
+            }
             const uint32_t t = t0 + slot.at * L::kCols;
             const int left = p.groups - g;
 #pragma unroll
