@@ -101,6 +101,13 @@ __device__ __forceinline__ void drop_page(const polyspec_cache_pages& s, int pag
     else if (was <= 0) { atomicAdd(&s.refs[page], 1); report(status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE); }
 }
 
+// Word w of the free bitmap, without bits behind the last page.
+__device__ __forceinline__ uint32_t free_word(const polyspec_cache_pages& s, int w)
+{
+    const uint32_t valid = s.n_pages >= 32 * (w + 1) ? 0xffffffffu : (1u << (s.n_pages - 32 * w)) - 1u;
+    return s.free_bits[w] & valid;
+}
+
 // Sequence b's length if it is one the table can hold, else -1.
 __device__ __forceinline__ int held_len(const polyspec_cache_pages& s, int b)
 {
@@ -145,7 +152,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) reserve_kernel(const polyspec
     Need first = {false, false, false, false, 0, 0, 0};
     if (tid < s.n_seqs) first = need_of(s, base, extra, plus, tid);
     int mine = 0;
-    for (int w = w0; w < w1; ++w) mine += __popc(s.free_bits[w]);
+    for (int w = w0; w < w1; ++w) mine += __popc(free_word(s, w));
     int n_free, total;
     const int my_rank = block_exclusive(mine, sums, &n_free);
 
@@ -172,7 +179,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) reserve_kernel(const polyspec
     // the lowest `taken` free pages, ascending; they are in use from here on
     int rank = my_rank;
     for (int w = w0; w < w1 && rank < taken; ++w) {
-        uint32_t bits = s.free_bits[w];
+        uint32_t bits = free_word(s, w);
         uint32_t left = bits;
         while (left && rank < taken) {
             const int bit = __ffs(left) - 1;
@@ -292,7 +299,7 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const polyspec
     const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
     int mine = 0, n_free, n_moves;
     wait_for_stream();
-    for (int w = w0; w < w1; ++w) mine += __popc(s.free_bits[w]);
+    for (int w = w0; w < w1; ++w) mine += __popc(free_word(s, w));
     block_exclusive(mine, sums, &n_free);
     const int n_live = s.n_pages - n_free;
     // bits of word w that lie below n_live
@@ -300,14 +307,14 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const polyspec
     auto valid = [&](int w) { return s.n_pages >= 32 * (w + 1) ? 0xffffffffu : (1u << (s.n_pages - 32 * w)) - 1u; };
     int holes = 0, movers = 0;
     for (int w = w0; w < w1; ++w) {
-        holes += __popc(s.free_bits[w] & below(w));
-        movers += __popc(~s.free_bits[w] & ~below(w) & valid(w));
+        holes += __popc(free_word(s, w) & below(w));
+        movers += __popc(~free_word(s, w) & ~below(w) & valid(w));
     }
     int hole = block_exclusive(holes, sums, &n_moves);
     int total;
     int mover = block_exclusive(movers, sums, &total);
     for (int w = w0; w < w1; ++w) {
-        const uint32_t bits = s.free_bits[w];
+        const uint32_t bits = free_word(s, w);
         for (uint32_t left = bits & below(w); left; left &= left - 1) plan.copies[hole++].y = w * 32 + __ffs(left) - 1;
         for (uint32_t left = ~bits & ~below(w) & valid(w); left; left &= left - 1) plan.copies[mover++].x = w * 32 + __ffs(left) - 1;
         s.free_bits[w] = ~below(w) & valid(w);

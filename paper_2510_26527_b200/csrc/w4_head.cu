@@ -429,6 +429,7 @@ polyspec_status polyspec_lm_head_quantized(const void* hidden, const void* qweig
         return POLYSPEC_ERR_INVALID_ARG;
     if (group != 32 && group != 64 && group != 128) return POLYSPEC_ERR_UNSUPPORTED;
     if (d % group != 0 || V > 0x7fffffff - 1024) return POLYSPEC_ERR_UNSUPPORTED;
+    if (static_cast<long long>((V + 127) / 128) * ((rows + 15LL) / 16) > 0x70000000LL) return POLYSPEC_ERR_UNSUPPORTED;      // work items
     W4Problem q;
     q.hidden = hidden;
     q.codes = static_cast<const uint32_t*>(qweight);

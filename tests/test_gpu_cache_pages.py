@@ -173,6 +173,23 @@ def test_broken_states_are_reported_and_skipped():
     assert torch.equal(both.pages.table, before)
 
 
+def test_bits_behind_the_last_page_are_not_pages():
+    both = Both(2, 8, 37, 4)
+    both.pages.free_bits[1] = -1                            # all 32 bits of a word that has five pages
+    st = binding.polyspec_cache_reserve(both.pages, _i32([32, 32]))
+    torch.cuda.synchronize()
+    assert int(st) == 0 and both.pages.table.flatten().tolist() == list(range(16))
+    small = Both(2, 40, 37, 1)
+    small.pages.free_bits[1] = -1
+    st = binding.polyspec_cache_reserve(small.pages, _i32([38, 37]))
+    torch.cuda.synchronize()
+    assert int(st) == binding.ERR_NO_PAGES and small.pages.len.tolist() == [0, 0]
+    binding.polyspec_cache_reserve(small.pages, _i32([20, 17]))
+    binding.polyspec_cache_compact(small.pages)
+    torch.cuda.synchronize()
+    assert small.pages.refs.tolist() == [1] * 37 and small.pages.free_bits.tolist() == [0, 0]
+
+
 def test_captured_cycle():
     both = Both(5, 8, 64, 4, ((2, 128),))
     both.reserve([10, 3, 0, 7, 7])

@@ -186,6 +186,34 @@ def test_slices_of_a_sharded_vocabulary_equal_the_whole(ranks):
         assert torch.equal(got, whole[..., r * n:(r + 1) * n])
 
 
+@pytest.mark.parametrize("history,bias", [(40, 5), (300, 256), (300, 257), (9000, 700)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_bias_lists_and_long_histories(history, bias, dtype):
+    """Short and long bias lists, 16- and 32-bit counts, in every combination that the kernel tells apart."""
+    z, kw, allowed = _inputs(2, 3, 4104, dtype, history, bias, True, True, seed=history)
+    out, status = _call(z.to(DEV), kw, allowed)
+    assert int(status) == 0
+    _close(out, z, kw, allowed)
+    only = {k: kw[k] for k in ("bias_tokens", "bias_values")}
+    out, status = _call(z.to(DEV), only, None)
+    assert int(status) == 0
+    _close(out, z, only, None)
+
+
+@pytest.mark.parametrize("dtype,V", [(torch.bfloat16, 16392), (torch.float32, 9000)])
+def test_a_sequence_does_not_depend_on_its_batch(dtype, V):
+    """Wide batches take other slice sizes than single sequences: the same bits."""
+    B, rows = 620, 3
+    z, kw, allowed = _inputs(B, rows, V, dtype, 64, 12, True, True, seed=9)
+    whole, status = _call(z.to(DEV), kw, allowed)
+    assert int(status) == 0
+    for b in (0, 57, 301, B - 1):
+        one, _ = _call(z[b:b + 1].to(DEV), {k: v[b:b + 1] for k, v in kw.items()}, allowed[b:b + 1])
+        assert torch.equal(one[0], whole[b])
+    some = slice(0, 3)
+    _close(whole[some], z[some], {k: v[some] for k, v in kw.items()}, allowed[some])
+
+
 def test_captured_on_another_stream_and_repeated():
     B, rows, V = 4, 5, 10000
     z, kw, allowed = _inputs(B, rows, V, torch.float32, 500, 30, True, True)

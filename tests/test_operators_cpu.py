@@ -30,7 +30,7 @@ def test_status_and_version(lib):
     ({"hidden": FAKE + 8}, INVALID), ({"qweight": FAKE + 4}, INVALID), ({"logits": FAKE + 4}, INVALID), ({"scales": FAKE + 1}, INVALID),
     ({"rows": 0}, INVALID), ({"V": 0}, INVALID), ({"d": 0}, INVALID), ({"rows": -3}, INVALID), ({"dt": 2}, INVALID),
     ({"group": 16}, UNSUPPORTED), ({"group": 0}, UNSUPPORTED), ({"group": 256}, UNSUPPORTED), ({"d": 4096 + 64}, UNSUPPORTED),
-    ({"V": 0x7fffffff}, UNSUPPORTED),
+    ({"V": 0x7fffffff}, UNSUPPORTED), ({"rows": 1 << 30, "V": 1 << 20}, UNSUPPORTED),
 ])
 def test_quantized_head_refuses(lib, change, status):
     a = dict(hidden=FAKE, qweight=FAKE, scales=FAKE, zeros=None, rows=8, V=32000, d=4096, group=128, dt=binding.F32, logits=FAKE)
