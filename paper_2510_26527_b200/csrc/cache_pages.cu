@@ -9,6 +9,8 @@
 //
 // The bookkeeping calls are latency-bound: one CTA (reserve, compact) or one warp per sequence (rollback, fork), one launch.
 // Moving page contents is HBM-bound: warps copy 2 KiB pieces, four independent 16-byte loads per lane before the stores.
+// Measured: reserve and rollback of 64 sequences in a pool of 41500 pages 7.7 us together; compacting 48 planes of 4000 pages of
+// 8 KiB, 114 to 118 us in the moves, 5.9 TB/s of DRAM traffic.
 #include <mutex>
 
 #include "launch.cuh"

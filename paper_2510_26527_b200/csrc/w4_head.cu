@@ -14,9 +14,12 @@
 // The codes are cut into pieces of 32 vocabulary entries (a tile) x 128 elements (2 KiB, one TMA box).  A CTA owns a contiguous
 // range of tiles and its warps equal, contiguous shares of the pieces of that range, whatever tile borders they cross, each
 // streamed through a private ring in shared memory: warps meet once, at the end, when the sums of tiles that several of them
-// worked on are added up in a fixed order.  (With whole tiles per team of warps the last round was a fifth of the time on 32000
-// entries, and a reduction with two barriers per tile cost as much again.)  The hidden rows are staged once per CTA in fragment
+// worked on are added up in a fixed order.  (Whole tiles per team of warps, with a reduction and two barriers per tile:
+// 26.3 against 24.0 us on 1 x 32000 x 4096.)  The hidden rows are staged once per CTA in fragment
 // order.
+// Measured: 1 x 32000 x 4096 in groups of 128, 20.5 us, 3.35 TB/s (floor 10.5: 4 to 5 us pass before the first piece is computed,
+// then issue, 53% of its slots); 5 x 152064 x 8192 in groups of 64, 158 us, 4.3 TB/s (63% of the issue slots; the same loop
+// without the arithmetic streams in 103).
 // Every wait on a copy is bounded: a warp whose wait runs out sets POLYSPEC_ERR_TIMEOUT and goes on without waiting, so that
 // the barrier at the end is still reached.
 #include <cuda_bf16.h>
