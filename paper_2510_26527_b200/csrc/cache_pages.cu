@@ -328,7 +328,6 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const polyspec
         const int2 m = plan.copies[i];
         s.refs[m.y] = s.refs[m.x];
         s.refs[m.x] = 0;
-        plan.pages[m.x] = m.y;
         if (moved_to) moved_to[m.x] = m.y;
     }
     if (tid == 0) {
@@ -337,14 +336,22 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const polyspec
     }
 }
 
-// Compact, tables: entries that name a page past the end are renamed.
+// Compact, tables: entries that name a page that moves are renamed.  The moves are sorted by the page they start from; an entry
+// past the end that names no such page (left behind a sequence's last one) stays as it is.
 __device__ __forceinline__ void rename_entries(const polyspec_cache_pages& s, const Plan& plan)
 {
-    const int n_live = plan.starts[0];
+    const int n_live = plan.starts[0], n_moves = *plan.n_copies;
     const long long n = static_cast<long long>(s.n_seqs) * s.max_pages, step = static_cast<long long>(gridDim.x) * blockDim.x;
     for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += step) {
         const int page = s.table[i];
-        if (page >= n_live && page < s.n_pages) s.table[i] = plan.pages[page];
+        if (page < n_live || page >= s.n_pages) continue;
+        int lo = 0, hi = n_moves;               // first move from `page` or later
+        while (lo < hi) {
+            const int mid = (lo + hi) >> 1;
+            if (plan.copies[mid].x < page) lo = mid + 1;
+            else hi = mid;
+        }
+        if (lo < n_moves && plan.copies[lo].x == page) s.table[i] = plan.copies[lo].y;
     }
 }
 

@@ -190,6 +190,24 @@ def test_bits_behind_the_last_page_are_not_pages():
     assert small.pages.refs.tolist() == [1] * 37 and small.pages.free_bits.tolist() == [0, 0]
 
 
+def test_compact_leaves_entries_behind_a_sequence_as_they_were():
+    """Table words behind the pages a sequence holds are no entries, whatever free page they name."""
+    both = Both(3, 8, 64, 4, ((2, 64),))
+    both.reserve([12, 12, 12])                              # pages 0-2, 3-5, 6-8
+    both.rollback([-1, 0, -1])                              # pages 3-5 are free: 6-8 move there
+    stale = [63, 40, 7, 20, 6]                              # 7 and 6 are in use and move; the others are free
+    both.pages.table[0, 3:] = _i32(stale)
+    both.pages.workspace().fill_(0x5a)                      # what an earlier call may have left
+    binding.polyspec_cache_compact(both.pages, pools=both.pools)
+    both.move(list(both.plain.compact().items()))
+    torch.cuda.synchronize()
+    table = both.pages.table.tolist()
+    assert table[0][:3] == [0, 1, 2] and table[2][:3] == [3, 4, 5]
+    assert [table[0][3], table[0][4], table[0][6]] == [63, 40, 20]
+    for got, want in zip(both.pools, both.copies):
+        assert (got.cpu().numpy() == want).all()
+
+
 def test_captured_cycle():
     both = Both(5, 8, 64, 4, ((2, 128),))
     both.reserve([10, 3, 0, 7, 7])
