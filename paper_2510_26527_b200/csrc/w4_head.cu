@@ -431,7 +431,7 @@ polyspec_status polyspec_lm_head_quantized(const void* hidden, const void* qweig
         (reinterpret_cast<uintptr_t>(logits) & 15u) != 0 || (reinterpret_cast<uintptr_t>(scales) & 1u) != 0)
         return POLYSPEC_ERR_INVALID_ARG;
     if (group != 32 && group != 64 && group != 128) return POLYSPEC_ERR_UNSUPPORTED;
-    if (d % group != 0 || V > 0x7fffffff - 1024) return POLYSPEC_ERR_UNSUPPORTED;
+    if (d % group != 0 || V > 0x7fffffff - 1024 || rows > 0x7fffffff - 1024) return POLYSPEC_ERR_UNSUPPORTED;     // a tile past the end counts on
     if (static_cast<long long>((V + 127) / 128) * ((rows + 15LL) / 16) > 0x70000000LL) return POLYSPEC_ERR_UNSUPPORTED;      // work items
     W4Problem q;
     q.hidden = hidden;

@@ -156,3 +156,61 @@ def test_captured_and_on_another_stream(rows):
     got, _ = binding.polyspec_lm_head_quantized(h2, q, s, z, stream=side)
     side.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("rows", [1, 5, 20, 150])
+@pytest.mark.parametrize("zeros", [True, False])
+def test_scales_and_zero_points_off_the_vector_boundary(rows, zeros):
+    """Eight groups a row, so that only the address keeps the vector loads away: same bits as from an aligned copy."""
+    hidden, codes, scales, zp = _case(rows, 300, 1024, 128, zeros, 31)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    q = binding.polyspec_pack_quantized(c)
+
+    def off(t):
+        if t is None:
+            return None
+        room = torch.empty(t.numel() + 1, dtype=t.dtype, device=DEV)
+        room[1:] = t.flatten()
+        return room[1:].view(t.shape)
+
+    want, _ = binding.polyspec_lm_head_quantized(h, q, s, z)
+    got, status = binding.polyspec_lm_head_quantized(h, q, off(s), off(z))
+    torch.cuda.synchronize()
+    assert int(status) == 0 and off(s).data_ptr() % 16 != 0
+    _close(got, hidden, codes, scales, zp)
+    assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("rows", [4, 40, 200])
+def test_two_calls_at_once_on_two_streams(rows):
+    cases = [_case(rows, 9001, 1024, 128, True, 41 + i) for i in range(2)]
+    args = []
+    for hidden, codes, scales, zp in cases:
+        h, c, s, z = _to(hidden, codes, scales, zp)
+        args.append((h, binding.polyspec_pack_quantized(c), s, z))
+    want = [binding.polyspec_lm_head_quantized(*a)[0] for a in args]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in args]
+    got = [[] for _ in args]
+    for _ in range(8):
+        for i, (a, side) in enumerate(zip(args, streams)):
+            got[i].append(binding.polyspec_lm_head_quantized(*a, stream=side))
+    torch.cuda.synchronize()
+    for outs, ref in zip(got, want):
+        for out, status in outs:
+            assert int(status) == 0 and torch.equal(out, ref)
+
+
+def test_output_offsets_past_32_bits():
+    """2.2 billion logits: the last rows are written where they belong, and nothing else is."""
+    V, d, rows = 152064, 32, 14500
+    hidden, codes, scales, zp = _case(rows, V, d, 32, True, 51)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    q = binding.polyspec_pack_quantized(c)
+    out, status = binding.polyspec_lm_head_quantized(h, q, s, z, out_dtype=torch.bfloat16)
+    torch.cuda.synchronize()
+    assert int(status) == 0 and out.numel() > 1 << 31
+    cols = torch.cat([torch.arange(200), torch.arange(V - 200, V)])
+    for at in (0, 7000, rows - 30):
+        part = out[at:at + 30][:, cols.to(DEV)]
+        _close(part, hidden[at:at + 30], codes[cols], scales[cols], zp[cols])

@@ -39,6 +39,12 @@ def test_quantized_head_refuses(lib, change, status):
                                           a["dt"], a["logits"], None, None) == status
 
 
+def test_quantized_head_refuses_counts_at_the_end_of_int(lib):
+    at = ctypes.c_void_p(1 << 20)                           # refused before it is read
+    for rows, V in ((0x7fffffff, 1), (1, 0x7fffffff)):
+        assert lib.polyspec_lm_head_quantized(at, at, at, None, rows, V, 32, 32, binding.F32, at, None, None) == binding.ERR_UNSUPPORTED
+
+
 def test_pack_refuses(lib):
     assert lib.polyspec_pack_quantized(None, 8, 32, FAKE, None) == INVALID
     assert lib.polyspec_pack_quantized(FAKE, 8, 32, None, None) == INVALID
