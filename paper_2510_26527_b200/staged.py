@@ -124,7 +124,8 @@ class StagedBatch:
                                                    p(self.out2["next_token"]), p(self.u1), p(self.pos1), p(self.tokens1),
                                                    p(self.uniforms1), p(self.block_len1), q), "polyspec_staged_accumulate")
         self._roll_back("M2", "M3")
-        self._reserve("M1", self.pos1, self.block_len1)
+        if "M1" in self.caches:                 # t + cnt tokens where its pass is due; below the length, so nothing, elsewhere
+            self._reserve("M1", (self.block_len1 > 0) * (self.pos1 + self.block_len1))
         rows_p = self._forward(self.M1, self.pos1, self._ar1)
         rows_q = self._forward(self.M2, self.pos1, self._ar1[:, : self.kcap])
         binding.polyspec_verify_level(rows_p, rows_q, self.tokens1, self.uniforms1, self.temperature, block_len=self.block_len1,

@@ -156,3 +156,27 @@ def test_staged_loop_reports_a_pool_too_small():
         _staged(5, 80, 256, 3, 5, 30, {"M2": (binding.CachePages.new(4, 30, 3, 4, DEV), [])})
     with pytest.raises(ValueError):
         _staged(5, 80, 256, 3, 5, 30, {"M4": (binding.CachePages.new(5, 30, 3, 4, DEV), [])})
+
+
+def _with_caches(loop, B, N, K, P=4):
+    most = (N + K + P) // P + 1
+    loop.caches = {m: (binding.CachePages.new(B, most, B * most, P, DEV), []) for m in ("M1", "M2", "M3")}
+    return {m: c for m, (c, _) in loop.caches.items()}
+
+
+def test_staged_loop_leaves_the_pages_of_a_model_that_sits_out():
+    """M_1's table stands still in every iteration in which its pass is not due."""
+    B, N, V, K, mu = 6, 120, 256, 3, 9
+    loop = _staged(B, N, V, K, mu, 50)
+    pages = _with_caches(loop, B, N, K)
+    waited = 0
+    while int(loop.state["remaining"]):
+        before = pages["M1"].len.tolist()
+        loop.iteration()
+        after, due = pages["M1"].len.tolist(), loop.block_len1.tolist()
+        for b in range(B):
+            if not due[b]:
+                assert after[b] == before[b], (b, before, after)
+                waited += 1
+        assert int(loop.status) == 0
+    assert waited > 3 * B
