@@ -115,7 +115,7 @@ class StagedBatch:
         self._check(lib.polyspec_staged_round_begin(s, p(self.drafts), p(self.u2), p(self.pos2), p(self.tokens2), p(self.uniforms2),
                                                     p(self.block_len2), q), "polyspec_staged_round_begin")
         self._reserve("M2", self.pos2, plus=self.K)
-        self._reserve("M3", self.pos2, plus=self.K)
+        self._reserve("M3", self.pos2, plus=self.K - 1)         # its last draft is not given back to it
         rows_p = self._forward(self.M2, self.pos2, self._ar2)
         rows_q = self._forward(self.M3, self.pos2, self._ar2[:, : self.K])
         binding.polyspec_verify_level(rows_p, rows_q, self.tokens2, self.uniforms2, self.temperature, block_len=self.block_len2,

@@ -180,3 +180,29 @@ def test_staged_loop_leaves_the_pages_of_a_model_that_sits_out():
                 waited += 1
         assert int(loop.status) == 0
     assert waited > 3 * B
+
+
+@pytest.mark.parametrize("K,mu", [(1, 4), (3, 5), (5, 1)])
+def test_staged_loop_lengths_are_the_tokens_each_model_was_given(K, mu):
+    """What a model was given, counted from the positions of its passes: rows p .. p + n of a pass take the tokens before p + n.
+    A length is as many of those as still stand, the last token emitted never among them."""
+    B, N, V = 6, 120, 256
+    loop = _staged(B, N, V, K, mu, 40)
+    loop.M3.copy_(loop.M2)                                  # q = p: M_2 accepts every draft
+    pages = _with_caches(loop, B, N, K)
+    want = {m: [0] * B for m in pages}
+    whole = 0
+    while int(loop.state["remaining"]):
+        loop.iteration()
+        torch.cuda.synchronize()
+        pos2, len2, pos1, len1 = (x.tolist() for x in (loop.pos2, loop.block_len2, loop.pos1, loop.block_len1))
+        stands = [max(t + c - 1, 0) for t, c in zip(loop.state["t"].tolist(), loop.state["cnt"].tolist())]
+        whole += sum(a == K for a, n in zip(loop.out2["accepted_len"].tolist(), len2) if n)
+        for b in range(B):
+            # M_3 drafts the K tokens (its last draft is not given back to it), M_2 scores K + 1 rows, M_1 len1 + 1 rows
+            given = {"M3": pos2[b] + K - 1 if len2[b] else 0, "M2": pos2[b] + K if len2[b] else 0, "M1": pos1[b] + len1[b] if len1[b] else 0}
+            for m in want:
+                want[m][b] = min(max(want[m][b], given[m]), stands[b])
+        for m, c in pages.items():
+            assert c.len.tolist() == want[m], m
+    assert whole > B and int(loop.status) == 0
