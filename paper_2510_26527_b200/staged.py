@@ -99,23 +99,27 @@ class StagedBatch:
         idx = (pos.long().unsqueeze(1) + ar).clamp_(max=self.N - 1)
         return table[self._b, idx]
 
-    def _reserve(self, name, base, extra=None, plus=0):
+    def _reserve(self, name, pos, block_len, plus):
+        """Room for pos + plus tokens of the sequences that take part in the pass; the others' target is 0, which reserves nothing."""
         if name in self.caches:
             pages, pools = self.caches[name]
-            binding.polyspec_cache_reserve(pages, base, extra, plus, pools, device_status=self.status)
+            binding.polyspec_cache_reserve(pages, (block_len > 0) * (pos + plus), pools=pools, device_status=self.status)
 
     def _roll_back(self, *names):
-        for name in names:
-            if name in self.caches:
-                binding.polyspec_cache_rollback(self.caches[name][0], self.state["t"], self.state["cnt"], -1, device_status=self.status)
+        """Back to all that stands but the last token emitted; to nothing where none was (a first round that failed)."""
+        names = [n for n in names if n in self.caches]
+        if names:
+            stands = (self.state["t"] + self.state["cnt"] - 1).clamp_(min=0)
+            for name in names:
+                binding.polyspec_cache_rollback(self.caches[name][0], stands, device_status=self.status)
 
     def iteration(self):
         """One pass through the body of Algorithm 1's loop for every sequence; enqueues only."""
         lib, s, p, q = self.lib, ctypes.byref(self.cstate), binding._ptr, binding._stream(None)
         self._check(lib.polyspec_staged_round_begin(s, p(self.drafts), p(self.u2), p(self.pos2), p(self.tokens2), p(self.uniforms2),
                                                     p(self.block_len2), q), "polyspec_staged_round_begin")
-        self._reserve("M2", self.pos2, plus=self.K)
-        self._reserve("M3", self.pos2, plus=self.K - 1)         # its last draft is not given back to it
+        self._reserve("M2", self.pos2, self.block_len2, self.K)
+        self._reserve("M3", self.pos2, self.block_len2, self.K - 1)         # its last draft is not given back to it
         rows_p = self._forward(self.M2, self.pos2, self._ar2)
         rows_q = self._forward(self.M3, self.pos2, self._ar2[:, : self.K])
         binding.polyspec_verify_level(rows_p, rows_q, self.tokens2, self.uniforms2, self.temperature, block_len=self.block_len2,
@@ -124,8 +128,7 @@ class StagedBatch:
                                                    p(self.out2["next_token"]), p(self.u1), p(self.pos1), p(self.tokens1),
                                                    p(self.uniforms1), p(self.block_len1), q), "polyspec_staged_accumulate")
         self._roll_back("M2", "M3")
-        if "M1" in self.caches:                 # t + cnt tokens where its pass is due; below the length, so nothing, elsewhere
-            self._reserve("M1", (self.block_len1 > 0) * (self.pos1 + self.block_len1))
+        self._reserve("M1", self.pos1, self.block_len1, self.block_len1)
         rows_p = self._forward(self.M1, self.pos1, self._ar1)
         rows_q = self._forward(self.M2, self.pos1, self._ar1[:, : self.kcap])
         binding.polyspec_verify_level(rows_p, rows_q, self.tokens1, self.uniforms1, self.temperature, block_len=self.block_len1,

@@ -206,3 +206,28 @@ def test_staged_loop_lengths_are_the_tokens_each_model_was_given(K, mu):
         for m, c in pages.items():
             assert c.len.tolist() == want[m], m
     assert whole > B and int(loop.status) == 0
+
+
+def test_staged_loop_sequences_out_of_the_loop_take_no_pages():
+    """Finished sequences keep their tables as they are; one that fails in its first round, or never had a round, holds nothing."""
+    B, N, V, K, mu = 5, 80, 256, 6, 1
+    loop = _staged(B, N, V, K, mu, 2)
+    loop.M2[3, : K + 1] = float("nan")
+    pages = _with_caches(loop, B, N, K)
+    done = [0] * B
+    for _ in range(12):
+        before = {m: c.len.tolist() for m, c in pages.items()}
+        loop.iteration()
+        for m, c in pages.items():
+            now = c.len.tolist()
+            assert [n for n, d in zip(now, done) if d] == [n for n, d in zip(before[m], done) if d], m
+        done = loop.state["done"].tolist()
+    assert all(done)
+    for c in pages.values():
+        assert int(c.len[3]) == 0 and int((c.table[3] >= 0).sum()) == 0
+        assert int(c.refs.sum()) == int(((c.len + 3) // 4).sum())
+    short = _staged(B, K, V, K, mu, 2)                      # a block and its bonus row do not fit into K positions
+    pages = _with_caches(short, B, K, K)
+    short.iteration()
+    assert all(short.state["done"].tolist())
+    assert all(int(c.len.abs().sum()) == 0 and int(c.refs.abs().sum()) == 0 for c in pages.values())
