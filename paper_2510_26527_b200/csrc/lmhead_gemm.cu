@@ -505,9 +505,11 @@ cudaError_t launch_lmhead(const LmHeadProblem* probs, int n, int V, float c, int
     e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+    // In every call, before the tensor maps are encoded: that is a driver call, which wants a context current in this host thread, and
+    // setting an attribute binds the device's where the thread has none yet.
+    e = cudaFuncSetAttribute(lmhead_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kGemmSmemBytes));
+    if (e != cudaSuccess) return e;
     if (!g_attr_set[dev]) {
-        e = cudaFuncSetAttribute(lmhead_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kGemmSmemBytes));
-        if (e != cudaSuccess) return e;
         int sms = 0;
         e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
         if (e != cudaSuccess) return e;

@@ -331,23 +331,34 @@ int stream_ring(int d)
     return ring;
 }
 
+std::mutex g_mutex;
+EncodeTiledFn g_encode = nullptr;
+
+// The tensor map of the codes.
+bool encode_codes(StreamParams& p, const uint32_t* codes)
+{
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(p.d / 2), static_cast<cuuint64_t>(p.V)}, pitch[1] = {static_cast<cuuint64_t>(p.d / 2)};
+    const cuuint32_t box[2] = {kChunk / 2, kTileS}, one[2] = {1, 1};
+    return g_encode(&p.map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint32_t*>(codes), dims, pitch, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 template <int G, int DT>
-cudaError_t launch_stream_t(const StreamParams& p, int sms, cudaStream_t stream)
+cudaError_t launch_stream_t(StreamParams& p, const uint32_t* codes, int sms, cudaStream_t stream)
 {
     const size_t smem = stream_smem(p.d, p.ring);
     cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<G, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
     if (e != cudaSuccess) return e;
+    // behind the attribute: encoding is a driver call, which wants a context current in this host thread, and setting one binds it
+    if (!encode_codes(p, codes)) return cudaErrorInvalidValue;
     return launch_early(w4_stream_kernel<G, DT>, dim3(static_cast<unsigned>(std::min(sms, p.tiles))), kThreadsS, smem, stream, p);
 }
 
 template <int G>
-cudaError_t launch_stream_g(const StreamParams& p, polyspec_dtype dt, int sms, cudaStream_t stream)
+cudaError_t launch_stream_g(StreamParams& p, const uint32_t* codes, polyspec_dtype dt, int sms, cudaStream_t stream)
 {
-    return dt == POLYSPEC_F32 ? launch_stream_t<G, POLYSPEC_F32>(p, sms, stream) : launch_stream_t<G, POLYSPEC_BF16>(p, sms, stream);
+    return dt == POLYSPEC_F32 ? launch_stream_t<G, POLYSPEC_F32>(p, codes, sms, stream) : launch_stream_t<G, POLYSPEC_BF16>(p, codes, sms, stream);
 }
-
-std::mutex g_mutex;
-EncodeTiledFn g_encode = nullptr;
 
 cudaError_t launch_stream(const W4Problem& q, polyspec_dtype dt, int32_t* device_status, cudaStream_t stream)
 {
@@ -376,15 +387,10 @@ cudaError_t launch_stream(const W4Problem& q, polyspec_dtype dt, int32_t* device
     p.tiles = (q.V + kTileS - 1) / kTileS;
     p.ring = stream_ring(q.d);
     p.vectors = p.groups % kTableGroups == 0 && (reinterpret_cast<uintptr_t>(q.scales) & 15u) == 0 && (reinterpret_cast<uintptr_t>(q.zeros) & 7u) == 0;
-    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(q.d / 2), static_cast<cuuint64_t>(q.V)}, pitch[1] = {static_cast<cuuint64_t>(q.d / 2)};
-    const cuuint32_t box[2] = {kChunk / 2, kTileS}, one[2] = {1, 1};
-    if (g_encode(&p.map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<uint32_t*>(q.codes), dims, pitch, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                 CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) != CUDA_SUCCESS)
-        return cudaErrorInvalidValue;
     switch (q.group) {
-        case 128: return launch_stream_g<128>(p, dt, sms, stream);
-        case 64: return launch_stream_g<64>(p, dt, sms, stream);
-        default: return launch_stream_g<32>(p, dt, sms, stream);
+        case 128: return launch_stream_g<128>(p, q.codes, dt, sms, stream);
+        case 64: return launch_stream_g<64>(p, q.codes, dt, sms, stream);
+        default: return launch_stream_g<32>(p, q.codes, dt, sms, stream);
     }
 }
 

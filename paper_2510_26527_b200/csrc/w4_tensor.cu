@@ -498,11 +498,12 @@ cudaError_t launch_shape(TensorParams& p, const W4Problem& q, int sms, cudaStrea
     p.items = static_cast<int>(items);
     // D fp32, A and B bf16, both K-major, M = 128, N
     p.idesc = (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(S::N >> 3) << 17) | (static_cast<uint32_t>(kTileV >> 4) << 24);
+    // before the encoding: that is a driver call, which wants a context current in this host thread, and this binds one
+    cudaError_t e = cudaFuncSetAttribute(w4_tensor_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmem));
+    if (e != cudaSuccess) return e;
     if (!encode(&p.map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, q.codes, q.d / 2, q.V, q.d / 2, kSub / 2, kTileV, CU_TENSOR_MAP_SWIZZLE_64B) ||
         !encode(&p.map_hidden, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, q.hidden, q.d, q.rows, static_cast<size_t>(q.d) * 2, 64, S::N, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
-    cudaError_t e = cudaFuncSetAttribute(w4_tensor_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmem));
-    if (e != cudaSuccess) return e;
     return launch_early(w4_tensor_kernel<S>, dim3(static_cast<unsigned>(std::min(sms, p.items))), S::kThreads, S::kSmem, stream, p);
 }
 

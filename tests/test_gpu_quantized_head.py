@@ -4,6 +4,8 @@ Tolerance per element: q - z is exact in bf16 and bf16 products are exact in fp3
 sum of G products takes at most G additions in any order, the sum over the groups one fused multiply-add each, each off by at
 most 2^-23 (an addition inside the tensor core may truncate) of a partial sum that the sum of magnitudes bounds: (G + groups)
 2^-23 sum |h| |w|.  A bf16 logit is rounded once more, by at most 2^-8 of its value."""
+import threading
+
 import pytest
 import torch
 
@@ -214,3 +216,22 @@ def test_output_offsets_past_32_bits():
     for at in (0, 7000, rows - 30):
         part = out[at:at + 30][:, cols.to(DEV)]
         _close(part, hidden[at:at + 30], codes[cols], scales[cols], zp[cols])
+
+
+@pytest.mark.parametrize("rows", [1, 40])
+def test_a_host_thread_without_a_context(rows):
+    """The C call as the first CUDA call of a thread, after another thread has made it already."""
+    hidden, codes, scales, zp = _case(rows, 200, 512, 128, True, 81)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    q = binding.polyspec_pack_quantized(c)
+    want, status = binding.polyspec_lm_head_quantized(h, q, s, z)
+    out = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    lib, stream, got = binding.load_library(), torch.cuda.current_stream().cuda_stream, []
+    args = (h.data_ptr(), q.data_ptr(), s.data_ptr(), z.data_ptr(), rows, 200, 512, 128, binding.F32, out.data_ptr(), status.data_ptr(), stream)
+    thread = threading.Thread(target=lambda: got.append(lib.polyspec_lm_head_quantized(*args)))
+    thread.start()
+    thread.join()
+    torch.cuda.synchronize()
+    assert got == [binding.OK] and int(status) == 0
+    assert torch.equal(out, want)

@@ -2,6 +2,8 @@
 so it can run on a side stream and be captured into a CUDA graph and replayed on new inputs (the way a
 serving loop removes launch overhead from the small, latency-bound calls).  Compared with plain calls
 of the same library on the same inputs: bit-exact, integers and floats alike."""
+import threading
+
 import pytest
 import torch
 
@@ -117,3 +119,21 @@ def test_fused_call_captured_in_a_graph_and_replayed_on_new_inputs():
         for k in want:
             assert torch.equal(call.out[k], want[k]), k
         assert int(call.device_status[0]) == 0
+
+
+def test_lm_head_from_a_host_thread_without_a_context():
+    """The C call as the first CUDA call of a thread, after another thread has made it already."""
+    g = torch.Generator(device=DEV).manual_seed(5)
+    hidden = torch.randn((8, 256), generator=g, device=DEV).to(torch.bfloat16)
+    W = torch.randn((300, 256), generator=g, device=DEV).to(torch.bfloat16)
+    want, status = binding.polyspec_lm_head(hidden, W)
+    out = torch.zeros_like(want)
+    torch.cuda.synchronize()
+    lib, stream, got = binding.load_library(), torch.cuda.current_stream().cuda_stream, []
+    args = (hidden.data_ptr(), W.data_ptr(), 8, 300, 256, out.data_ptr(), status.data_ptr(), stream)
+    thread = threading.Thread(target=lambda: got.append(lib.polyspec_lm_head(*args)))
+    thread.start()
+    thread.join()
+    torch.cuda.synchronize()
+    assert got == [binding.OK] and int(status) == 0
+    assert torch.equal(out, want)
