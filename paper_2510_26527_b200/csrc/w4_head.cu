@@ -316,7 +316,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
     }
 }
 
-constexpr size_t kMaxSmem = 227 * 1024;
+constexpr size_t kMaxSmem = 227 * 1024, kStaticRoom = 2048;
+constexpr size_t kMaxDynamic = kMaxSmem - kStaticRoom;          // of any call
 
 // Shared memory with `ring` pieces per warp; the largest ring that fits is used, and two pieces are the least.
 size_t stream_smem(int d, int ring)
@@ -327,7 +328,7 @@ size_t stream_smem(int d, int ring)
 int stream_ring(int d)
 {
     int ring = kMaxRing;
-    while (ring > 0 && stream_smem(d, ring) + 2048 > kMaxSmem) --ring;
+    while (ring > 0 && stream_smem(d, ring) > kMaxDynamic) --ring;
     return ring;
 }
 
@@ -347,7 +348,9 @@ template <int G, int DT>
 cudaError_t launch_stream_t(StreamParams& p, const uint32_t* codes, int sms, cudaStream_t stream)
 {
     const size_t smem = stream_smem(p.d, p.ring);
-    cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<G, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+    // The limit belongs to the kernel, not to the call: always the most that any call needs, so that a call for a narrow head in one
+    // host thread does not lower it between another thread's set-up and launch.
+    cudaError_t e = cudaFuncSetAttribute(w4_stream_kernel<G, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMaxDynamic));
     if (e != cudaSuccess) return e;
     // behind the attribute: encoding is a driver call, which wants a context current in this host thread, and setting one binds it
     if (!encode_codes(p, codes)) return cudaErrorInvalidValue;

@@ -213,3 +213,28 @@ def cdf_distance(weights, u, token):
     lo = (c[token] - w[token]) / total
     hi = c[token] / total
     return float(max(lo - u, u - hi, 0.0))
+
+
+def run_at_once(calls, times, threads=4):
+    """Each of `calls`, which return a status, `times` times in each of `threads` threads of its own, all at once; the statuses
+    other than 0 that came back."""
+    import sys
+    import threading
+    start = threading.Barrier(threads * len(calls))
+    bad = []
+
+    def loop(call):
+        start.wait()
+        bad.extend(st for st in (call() for _ in range(times)) if st != 0)
+
+    every = sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+    try:
+        workers = [threading.Thread(target=loop, args=(c,)) for c in calls for _ in range(threads)]
+        for w in workers:
+            w.start()
+        for w in workers:
+            w.join()
+    finally:
+        sys.setswitchinterval(every)
+    return bad

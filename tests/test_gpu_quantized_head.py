@@ -11,6 +11,7 @@ import torch
 
 from paper_2510_26527_b200 import binding, buildlib
 from tests import plain_operators as plain
+from tests.helpers import run_at_once
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -235,3 +236,22 @@ def test_a_host_thread_without_a_context(rows):
     torch.cuda.synchronize()
     assert got == [binding.OK] and int(status) == 0
     assert torch.equal(out, want)
+
+
+def test_threads_with_narrow_and_wide_heads():
+    """Same kernel, different shared memory: neither call may take the other's away between its set-up and its launch."""
+    lib, stream = binding.load_library(), torch.cuda.current_stream().cuda_stream
+    calls, kept = [], []
+    for i, (V, d) in enumerate([(64, 1024), (64, 8192)]):
+        hidden, codes, scales, zp = _case(4, V, d, 128, True, 61 + i)
+        h, c, s, z = _to(hidden, codes, scales, zp)
+        out, status, q = torch.empty((4, V), device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV), binding.polyspec_pack_quantized(c)
+        kept.append((out, status, h, q, s, z, (hidden, codes, scales, zp)))
+        args = (h.data_ptr(), q.data_ptr(), s.data_ptr(), z.data_ptr(), 4, V, d, 128, binding.F32, out.data_ptr(), status.data_ptr(), stream)
+        calls.append(lambda a=args: lib.polyspec_lm_head_quantized(*a))
+    torch.cuda.synchronize()
+    assert run_at_once(calls, 3000) == []
+    torch.cuda.synchronize()
+    for out, status, *_, case in kept:
+        assert int(status) == 0
+        _close(out, *case)
