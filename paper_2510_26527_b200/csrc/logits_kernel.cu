@@ -420,7 +420,10 @@ cudaError_t launch_vpt(ControlParams& p, bool counts, cudaStream_t stream)
     const size_t smem = counts ? static_cast<size_t>(kSlice) * ((wide ? 4 : 2) + 2) + biases : 0;
     auto launch = [&](auto kernel) {
         if (smem > 48 * 1024) {
-            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+            // the limit belongs to the kernel, not to the call: the most that any call of it needs, so that a call with a short bias
+            // list in one host thread does not lower it between another thread's set-up and launch
+            constexpr size_t kMost = kSlice * (4 + 2 + 4);
+            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kMost));
             if (e != cudaSuccess) return e;
         }
         return launch_early(kernel, dim3(static_cast<unsigned>(blocks)), kThreads, smem, stream, p);

@@ -9,6 +9,7 @@ import torch
 
 from paper_2510_26527_b200 import binding, buildlib
 from tests import plain_operators as plain
+from tests.helpers import run_at_once
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -250,3 +251,29 @@ def test_offsets_past_32_bits():
     assert z[-1, -1, -8:].tolist() == [2.0] * 5 + [1.0] + [2.0] * 2
     assert (z[:, :, V - 3] == torch.where(torch.arange(B * rows, device=DEV).view(B, rows) == B * rows - 1, 1.0, -1.0)).all()
     assert int((z != 0).sum()) == B * rows + 7
+
+
+def test_threads_with_short_and_long_bias_lists():
+    """Both take the widest slices with 32-bit counts and differ in shared memory only: neither may take the other's away."""
+    B, rows, V, cap = 300, 1, 32768, 8192
+    lib, stream = binding.load_library(), torch.cuda.current_stream().cuda_stream
+    z = torch.randn((B, rows, V), generator=torch.Generator(device=DEV).manual_seed(4), device=DEV).to(torch.bfloat16)
+    text = torch.arange(cap, device=DEV, dtype=torch.int32).repeat(B, 1)
+    length = torch.full((B,), 4, dtype=torch.int32, device=DEV)
+    calls, kept = [], []
+    for n in (8, 300):
+        kw = {"history": text, "history_len": length, "bias_tokens": torch.arange(n, device=DEV, dtype=torch.int32).repeat(B, 1),
+              "bias_values": torch.ones((B, n), device=DEV)}
+        out, status = torch.empty_like(z), torch.zeros(1, dtype=torch.int32, device=DEV)
+        c = binding.LogitControls(history=text.data_ptr(), history_len=length.data_ptr(), bias_tokens=kw["bias_tokens"].data_ptr(),
+                                  bias_values=kw["bias_values"].data_ptr(), history_cap=cap, n_bias=n)
+        kept.append((n, out, status, kw, c))
+        args = (z.data_ptr(), c, None, 0, B, rows, V, binding.BF16, out.data_ptr(), status.data_ptr(), stream)
+        calls.append(lambda a=args: lib.polyspec_process_logits(*a))
+    torch.cuda.synchronize()
+    assert run_at_once(calls, 400) == []
+    torch.cuda.synchronize()
+    for n, out, status, *_ in kept:
+        want = z.float()
+        want[..., :n] += 1.0
+        assert int(status) == 0 and torch.equal(out, want.to(torch.bfloat16))
