@@ -20,14 +20,15 @@
 // Measured: 1 x 32000 x 4096 in groups of 128, 20.5 us, 3.35 TB/s (floor 10.5: 4 to 5 us pass before the first piece is computed,
 // then issue, 53% of its slots); 5 x 152064 x 8192 in groups of 64, 158 us, 4.3 TB/s (63% of the issue slots; the same loop
 // without the arithmetic streams in 103).
-// Every wait on a copy is bounded: a warp whose wait runs out sets POLYSPEC_ERR_TIMEOUT and goes on without waiting, so that
-// the barrier at the end is still reached.
+// Every wait on a copy is bounded: a warp whose wait runs out sets POLYSPEC_ERR_TIMEOUT, asks for nothing more, waits (again with
+// a limit) for the copies it has on their way and goes to the barrier at the end.
 #include <cuda_bf16.h>
 
 #include <algorithm>
 #include <mutex>
 
 #include "launch.cuh"
+#include "piece_ring.cuh"
 #include "polyspec_kernels.cuh"
 #include "tensor_device.cuh"
 #include "w4_kernels.cuh"
@@ -154,14 +155,15 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
     };
     load_hidden(threadIdx.x);
 
-    int ask_tile = tile_first, ask_c = c_start, ask_at = 0, ask_left = s_end - s_first;
+    int ask_tile = tile_first, ask_c = c_start;
+    PieceRing ring(p.ring, s_end - s_first);
     auto ask = [&]() {
-        if (ask_left <= 0) return;
-        --ask_left;
-        if (elect_one()) load_piece(my_ring + ask_at * kPieceBytes, &p.map_codes, ask_c * (kChunk / 2), ask_tile * kTileS, bars + 8u * ask_at);
+        if (!ring.may_ask()) return;
+        if (elect_one())
+            load_piece(my_ring + ring.ask_at * kPieceBytes, &p.map_codes, ask_c * (kChunk / 2), ask_tile * kTileS, bars + 8u * ring.ask_at);
         __syncwarp();
         if (++ask_c == chunks) { ask_c = 0; ++ask_tile; }
-        if (++ask_at == p.ring) ask_at = 0;
+        ring.asked();
     };
     for (int i = 0; i < p.ring; ++i) ask();
 
@@ -223,9 +225,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
         if (v < p.V && n < p.rows) w4::store_logit<DT>(p.out, static_cast<size_t>(n) * p.V + v, x);
     };
 
-    uint32_t at = 0, phase = 0;
     int tile = tile_first;
-    bool first_tile = true;
+    bool first_tile = true, lost = false;
     for (int s = s_first; s < s_end; ++tile, first_tile = false) {
         const int c_first = first_tile ? c_start : 0, c_end = min(chunks, c_first + s_end - s);
         s += c_end - c_first;
@@ -242,14 +243,22 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
                 if (next < c_end) load_raw(tile, next);
                 else if (s < s_end) load_raw(tile + 1, 0);
             }
-            if (!mbar_wait(bars + 8u * at, phase, &gave_up) && lane == 0) {
-                if (p.status) atomicCAS(p.status, 0, static_cast<int>(POLYSPEC_ERR_TIMEOUT));
-                *reinterpret_cast<volatile int*>(&gave_up) = 1;
+            // landed, if one lane has seen it
+            if (!__any_sync(0xffffffffu, mbar_wait(bars + 8u * ring.at, ring.phase, &gave_up))) {
+                if (lane == 0) {
+                    if (p.status) atomicCAS(p.status, 0, static_cast<int>(POLYSPEC_ERR_TIMEOUT));
+                    *reinterpret_cast<volatile int*>(&gave_up) = 1;
+                }
+                ring.give_up([&](int slot, uint32_t parity) {
+                    for (uint32_t i = 0; i < kSpinLimitG && !mbar_try(bars + 8u * slot, parity); ++i) {}
+                });
+                lost = true;
+                break;
             }
             __syncwarp();
             uint32_t x[4][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) read_codes<G>(my_ring + at * kPieceBytes + (i * 8 + g) * 64, t, sw, x[i]);
+            for (int i = 0; i < 4; ++i) read_codes<G>(my_ring + ring.at * kPieceBytes + (i * 8 + g) * 64, t, sw, x[i]);
             const uint4* hid = hidden + c * 4 * 32 + lane;
 #pragma unroll
             for (int gi = 0; gi < GPC; ++gi) {
@@ -285,8 +294,9 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
             }
             __syncwarp();                       // every lane has read the piece
             ask();
-            if (++at == static_cast<uint32_t>(p.ring)) { at = 0; phase ^= 1u; }
+            ring.next();
         }
+        if (lost) break;
         const bool whole = c_end - c_first == chunks;
         float* mine = sums_of(warp, first_tile) + lane;
 #pragma unroll

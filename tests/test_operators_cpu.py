@@ -1,7 +1,9 @@
 """The 4-bit LM head, the sampling controls and the cache pages on a machine without a GPU: refusals at the C entry points and
 in the Python front end, and the plain page tables the GPU tests compare with."""
 import ctypes
+import os
 import random
+import subprocess
 
 import numpy as np
 import pytest
@@ -181,3 +183,13 @@ def test_mask_words():
     w = plain.mask_words(allowed)
     assert w.shape == (2, 3, 3)
     assert all(bool(w[b, j, v // 32] >> (v % 32) & 1) == allowed[b, j, v] for b in range(2) for j in range(3) for v in range(72))
+
+
+def test_streaming_ring_leaves_no_copy_on_its_way(tmp_path):
+    """The 4-bit head's ring on the host, given up at every point (a wait that runs out cannot be made to happen on the GPU)."""
+    exe = str(tmp_path / "piece_ring")
+    here = os.path.dirname(os.path.abspath(__file__))
+    subprocess.run(["g++", "-O1", "-std=c++17", "-Wall", "-Werror", "-fsanitize=address,undefined", "-I", buildlib.CSRC, "-o", exe,
+                    os.path.join(here, "piece_ring_driver.cpp")], check=True)
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert res.returncode == 0 and "0 failed checks" in res.stdout, res.stdout
