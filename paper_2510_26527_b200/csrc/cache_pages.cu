@@ -336,8 +336,9 @@ __global__ void __launch_bounds__(kPlanThreads, 1) compact_kernel(const polyspec
     }
 }
 
-// Compact, tables: entries that name a page that moves are renamed.  The moves are sorted by the page they start from; an entry
-// past the end that names no such page (left behind a sequence's last one) stays as it is.
+// Compact, tables: entries that name a page that moves are renamed; the moves are sorted by the page they start from.  Words behind
+// the pages of a sequence are no entries and stay as they are, whatever they name.  (Of a length that no table can hold nothing
+// follows: all words of that sequence count as entries, so that no page moves away from under one.)
 __device__ __forceinline__ void rename_entries(const polyspec_cache_pages& s, const Plan& plan)
 {
     const int n_live = plan.starts[0], n_moves = *plan.n_copies;
@@ -345,6 +346,8 @@ __device__ __forceinline__ void rename_entries(const polyspec_cache_pages& s, co
     for (long long i = static_cast<long long>(blockIdx.x) * blockDim.x + threadIdx.x; i < n; i += step) {
         const int page = s.table[i];
         if (page < n_live || page >= s.n_pages) continue;
+        const int b = static_cast<int>(i / s.max_pages), len = held_len(s, b);
+        if (len >= 0 && i - static_cast<long long>(b) * s.max_pages >= pages_for(len, s.page_tokens)) continue;
         int lo = 0, hi = n_moves;               // first move from `page` or later
         while (lo < hi) {
             const int mid = (lo + hi) >> 1;

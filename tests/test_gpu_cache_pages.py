@@ -241,3 +241,22 @@ def test_pool_offsets_past_32_bits():
     torch.cuda.synchronize()
     assert pages.table[1, 98:].tolist()[:2] == [998, 999]
     assert int(pool[1, 998, -1]) == 9 and (pool[1, 999] == 7).all() and int(pool[1, 998].sum()) == 9
+
+
+def test_compact_renames_no_word_behind_a_sequences_pages():
+    """Whatever such a word names, pages that move included."""
+    both = Both(4, 8, 64, 4, ((2, 64),))
+    both.reserve([12, 12, 12, 0])                           # pages 0-2, 3-5, 6-8
+    both.rollback([-1, 0, -1, -1])                          # 6-8 move to 3-5
+    tails = {0: (3, [8, 7, 6, 63, 3]), 1: (0, [6, 8, 7, -1, 99, 6, 0, -7]), 2: (3, [6, 6, 7, 8, 5]), 3: (0, [8] * 8)}
+    for b, (at, words) in tails.items():
+        both.pages.table[b, at:] = _i32(words)
+    binding.polyspec_cache_compact(both.pages, pools=both.pools)
+    both.move(list(both.plain.compact().items()))
+    torch.cuda.synchronize()
+    table = both.pages.table.tolist()
+    assert table[0][:3] == [0, 1, 2] and table[2][:3] == [3, 4, 5]
+    for b, (at, words) in tails.items():
+        assert table[b][at:] == words, b
+    for got, want in zip(both.pools, both.copies):
+        assert (got.cpu().numpy() == want).all()
