@@ -485,6 +485,7 @@ polyspec_status polyspec_process_logits(const void* logits, const polyspec_logit
  *        replaced by a copy of its own first (in every pool given).  A sequence for which the free pages, counted off in
  *        order, do not suffice stays as it was, with all after it that need a page (POLYSPEC_ERR_NO_PAGES in *device_status);
  *        so does one whose target exceeds max_pages * page_tokens (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE).  len tells what was granted.
+ *        Where several sequences stay as they were, the status is the first one's.
  *   polyspec_cache_rollback  sequences whose target is below their length (and not negative) fall back to it; pages wholly
  *        behind it are given back.  Others stay as they are.
  *   polyspec_cache_fork      for n pairs: sequence dst[i], which holds nothing, becomes a copy of src[i] that shares its pages.

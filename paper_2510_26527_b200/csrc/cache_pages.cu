@@ -144,11 +144,12 @@ __global__ void __launch_bounds__(kPlanThreads, 1) reserve_kernel(const polyspec
 {
     __shared__ int sums[33];
     __shared__ int taken, n_copies;
+    __shared__ unsigned long long failure;      // the lowest sequence that fails, above its status: one report, whoever comes first
     const int tid = threadIdx.x;
     const int words = (s.n_pages + 31) / 32;
     const int per = (words + kPlanThreads - 1) / kPlanThreads;          // consecutive words of the free bitmap per thread
     const int w0 = min(words, tid * per), w1 = min(words, w0 + per);
-    if (tid == 0) { taken = 0; n_copies = 0; }
+    if (tid == 0) { taken = 0; n_copies = 0; failure = ~0ull; }
     wait_for_stream();
     // the first sequences' needs are read beside the bitmap: both are chains of dependent loads
     Need first = {false, false, false, false, 0, 0, 0};
@@ -170,13 +171,14 @@ __global__ void __launch_bounds__(kPlanThreads, 1) reserve_kernel(const polyspec
         const bool ok = q.grow && (n == 0 || (start >= 0 && start <= n_free - n));
         if (b < s.n_seqs) {
             plan.starts[b] = ok ? (start << 1 | (q.copy ? 1 : 0)) : -1;
-            if (q.bad || q.too_long) report(status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
-            else if (q.grow && !ok) report(status, POLYSPEC_ERR_NO_PAGES);
+            const polyspec_status st = q.bad || q.too_long ? POLYSPEC_ERR_BAD_INPUT_ON_DEVICE : q.grow && !ok ? POLYSPEC_ERR_NO_PAGES : POLYSPEC_OK;
+            if (st != POLYSPEC_OK) atomicMin(&failure, static_cast<unsigned long long>(b) << 8 | st);
             if (ok && n > 0) atomicMax(&taken, start + n);
         }
         before = min(before + total, s.n_pages + 1);
     }
     __syncthreads();
+    if (tid == 0 && failure != ~0ull) report(status, static_cast<polyspec_status>(failure & 0xff));
 
     // the lowest `taken` free pages, ascending; they are in use from here on
     int rank = my_rank;

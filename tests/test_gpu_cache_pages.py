@@ -260,3 +260,17 @@ def test_compact_renames_no_word_behind_a_sequences_pages():
         assert table[b][at:] == words, b
     for got, want in zip(both.pools, both.copies):
         assert (got.cpu().numpy() == want).all()
+
+
+@pytest.mark.parametrize("far", [1, 2, 31, 40, 700, 1100])
+def test_reserve_reports_the_first_sequence_that_fails(far):
+    """A shortage and an over-long target in one call: the lower sequence's status, in one warp, across warps and across rounds."""
+    n = 1200
+    for short, long_ in ((0, far), (far, 0), (n - 1 - far, n - 1), (n - 1, n - 1 - far)):
+        pages = binding.CachePages.new(n, 4, 2, 4, DEV)
+        targets = [0] * n
+        targets[short], targets[long_] = 16, 17             # four pages where there are two; more than the table's sixteen tokens
+        for _ in range(3):
+            status = binding.polyspec_cache_reserve(pages, _i32(targets))
+            assert int(status) == (binding.ERR_NO_PAGES if short < long_ else binding.ERR_BAD_INPUT_ON_DEVICE), (short, long_)
+        assert int(pages.len.sum()) == 0
