@@ -380,9 +380,12 @@ __global__ void __launch_bounds__(kThreads, 5) logits_kernel(const ControlParams
         if (n == kSlice) stream_rows<DT, VPT, true>(p, b, v0, n, j0, j1, in_place);
         else stream_rows<DT, VPT, false>(p, b, v0, n, j0, j1, in_place);
     }
-    if (!COUNTS) return;
-
     const bool report = slice == 0 && group == 0;
+    if (!COUNTS) {                              // no entry is penalised, but a bad factor is reported all the same
+        if (report && tid == 0 && p.c.repetition && !(p.c.repetition[b] > 0.0f)) bad_input(p.status);
+        return;
+    }
+
     Slice<WIDE> s;
     s.count.w = reinterpret_cast<uint32_t*>(smem_controls);
     s.bias = p.c.bias_tokens ? reinterpret_cast<float*>(reinterpret_cast<char*>(smem_controls) + kSlice * (Counts<WIDE>::kBytes + 2)) : nullptr;

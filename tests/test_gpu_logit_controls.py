@@ -277,3 +277,20 @@ def test_threads_with_short_and_long_bias_lists():
         want = z.float()
         want[..., :n] += 1.0
         assert int(status) == 0 and torch.equal(out, want.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("value", [0.0, -1.0, float("nan")])
+def test_a_bad_repetition_is_reported_where_there_is_no_context(value):
+    """Without a history, a draft or biases no entry is penalised, but the factor is looked at all the same."""
+    B, rows, V = 3, 2, 5000
+    z, _, allowed = _inputs(B, rows, V, torch.bfloat16, mask=True)
+    for bad in range(B):
+        rep = np.ones(B, dtype=np.float32)
+        for masks in (allowed, None):
+            out, status = _call(z.to(DEV), {"repetition": rep}, masks)
+            assert int(status) == 0
+        rep[bad] = value
+        for masks in (allowed, None):
+            out, status = _call(z.to(DEV), {"repetition": rep}, masks)
+            assert int(status) == binding.ERR_BAD_INPUT_ON_DEVICE
+            _close(out, z, {}, masks)
