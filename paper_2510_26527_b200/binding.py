@@ -879,7 +879,8 @@ def _status_word(device_status, dev: int, stream) -> torch.Tensor:
     try:
         return _status_words[key].pop()
     except (KeyError, IndexError):
-        words = list(torch.zeros(256, dtype=torch.int32, device=torch.device("cuda", dev)).split(1))
+        with torch.inference_mode(False):       # words outlive the mode they are made under: later callers may write to theirs
+            words = list(torch.zeros(256, dtype=torch.int32, device=torch.device("cuda", dev)).split(1))
         word = words.pop()
         _status_words[key] = words
         return word

@@ -255,3 +255,16 @@ def test_threads_with_narrow_and_wide_heads():
     for out, status, *_, case in kept:
         assert int(status) == 0
         _close(out, *case)
+
+
+def test_a_status_word_made_under_inference_mode_can_be_written_outside():
+    hidden, codes, scales, zp = _case(2, 64, 128, 32, True, 71)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    q = binding.polyspec_pack_quantized(c)
+    binding._status_words.clear()
+    with torch.inference_mode():
+        binding.polyspec_lm_head_quantized(h, q, s, z)
+    _, status = binding.polyspec_lm_head_quantized(h, q, s, z)
+    status.zero_()
+    status.add_(1)
+    assert int(status) == 1
