@@ -847,7 +847,9 @@ def _on_stream(stream, dev: int):
     if stream is None:
         return torch.cuda.device(dev)
     if not isinstance(stream, torch.cuda.Stream):
-        stream = torch.cuda.ExternalStream(_stream(stream), device=torch.device("cuda", dev))
+        handle = _stream(stream)
+        # cudaStreamLegacy (1) is the default stream by another name, which torch refuses as an external one
+        stream = torch.cuda.ExternalStream(0 if handle == 1 else handle, device=torch.device("cuda", dev))
     return torch.cuda.stream(stream)
 
 

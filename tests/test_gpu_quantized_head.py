@@ -268,3 +268,14 @@ def test_a_status_word_made_under_inference_mode_can_be_written_outside():
     status.zero_()
     status.add_(1)
     assert int(status) == 1
+
+
+def test_raw_handles_of_the_default_stream():
+    """0 and cudaStreamLegacy (1) are the default stream."""
+    hidden, codes, scales, zp = _case(2, 64, 128, 32, True, 72)
+    h, c, s, z = _to(hidden, codes, scales, zp)
+    for handle in (0, 1):
+        out, status = binding.polyspec_lm_head_quantized(h, binding.polyspec_pack_quantized(c, stream=handle), s, z, stream=handle)
+        torch.cuda.synchronize()
+        assert int(status) == 0
+        _close(out, hidden, codes, scales, zp)
