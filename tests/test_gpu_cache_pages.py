@@ -274,3 +274,24 @@ def test_reserve_reports_the_first_sequence_that_fails(far):
             status = binding.polyspec_cache_reserve(pages, _i32(targets))
             assert int(status) == (binding.ERR_NO_PAGES if short < long_ else binding.ERR_BAD_INPUT_ON_DEVICE), (short, long_)
         assert int(pages.len.sum()) == 0
+
+
+@pytest.mark.parametrize("given", [False, True])
+def test_workspace_outlives_its_use_on_another_stream(given):
+    """The state's workspace, allocated on one stream and used on another, is not handed out again before that use is over."""
+    n_pages = 5003
+    keep = [torch.empty(1, device=DEV)]
+    side = torch.cuda.Stream()
+    pages = binding.CachePages.new(3, 40, n_pages, 4, DEV)
+    binding.polyspec_cache_reserve(pages, _i32([10, 20, 30]))
+    size, at = pages.workspace().nbytes, pages.workspace().data_ptr()
+    keep += [pages.table, pages.len, pages.refs, pages.free_bits]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(int(2e8))                         # a tenth of a second
+        binding.polyspec_cache_compact(pages, stream=side if given else None)
+    del pages
+    again = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    assert not side.query()
+    assert at not in [x.data_ptr() for x in again]
+    side.synchronize()
