@@ -1059,9 +1059,10 @@ def _pools(pages, pools):
     if len(pools) > CACHE_MAX_POOLS:
         raise ValueError(f"at most {CACHE_MAX_POOLS} pools")
     for t in pools:
-        if t.dim() < 3 or t.shape[1] != pages.n_pages:
+        if t.dim() < 3 or t.shape[0] < 1 or t.shape[1] != pages.n_pages:
             raise ValueError("a pool must be [n_planes, n_pages, ...]")
-    return (CachePool * len(pools))(*[CachePool(t.data_ptr(), t.shape[0], t.stride(1) * t.element_size()) for t in pools]) if pools else None
+    # (a stride says nothing of a dimension of size 1, so the size of a page is not read from it)
+    return (CachePool * len(pools))(*[CachePool(t.data_ptr(), t.shape[0], t.nbytes // (t.shape[0] * t.shape[1])) for t in pools]) if pools else None
 
 
 def polyspec_cache_reserve(pages, base, extra=None, plus=0, pools=(), device_status=None, workspace=None, stream=None):

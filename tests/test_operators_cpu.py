@@ -193,3 +193,16 @@ def test_streaming_ring_leaves_no_copy_on_its_way(tmp_path):
                     os.path.join(here, "piece_ring_driver.cpp")], check=True)
     res = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert res.returncode == 0 and "0 failed checks" in res.stdout, res.stdout
+
+
+@pytest.mark.parametrize("shape,strides", [((2, 1, 64), (64, 64, 1)), ((1, 1, 64), (64, 1, 1)), ((2, 1, 64), (64, 999, 1)), ((1, 5, 4, 8), (160, 32, 8, 1)),
+                                           ((3, 5, 32), (160, 32, 1))])
+def test_page_sizes_of_contiguous_pools(shape, strides):
+    """A contiguous tensor may have any stride in a dimension of size 1."""
+    t = torch.empty(200 + strides[0] * shape[0], dtype=torch.bfloat16).as_strided(shape, strides)
+    assert t.is_contiguous()
+    pages = type("Pages", (), {"n_pages": shape[1]})
+    (pool,) = binding._pools(pages, [t])
+    assert pool.n_planes == shape[0] and pool.page_bytes == 2 * t[0, 0].numel()
+    with pytest.raises(ValueError):
+        binding._pools(pages, [torch.empty((0,) + shape[1:])])
