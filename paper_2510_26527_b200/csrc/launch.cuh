@@ -1,5 +1,7 @@
 // Programmatic launch: the kernel's CTAs are set up while the kernel before it on the stream drains.  A kernel launched this way
-// calls wait_for_stream() before it touches memory; from there on everything earlier on the stream is done and visible.
+// calls wait_for_stream() before it touches memory; from there on everything earlier on the stream is done and visible.  What it
+// reads may have been written while it was resident already, so it uses no loads that promise read-only data (__ldg, ld.global.nc):
+// those may be moved over the wait and need not see such writes.
 #pragma once
 
 #include <cuda_runtime.h>

@@ -177,8 +177,8 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
     auto load_raw = [&](int tile, int c) {
         if (!vectors) return;
         const size_t own = static_cast<size_t>(min(tile * kTileS + lane, p.V - 1)) * p.groups + c / kTableChunks * kTableGroups;
-        raw_s = __ldg(reinterpret_cast<const uint4*>(p.scales + own));
-        raw_z = p.zeros ? __ldg(reinterpret_cast<const uint2*>(p.zeros + own)) : make_uint2(0x08080808u, 0x08080808u);
+        raw_s = *reinterpret_cast<const uint4*>(p.scales + own);
+        raw_z = p.zeros ? *reinterpret_cast<const uint2*>(p.zeros + own) : make_uint2(0x08080808u, 0x08080808u);
     };
     auto fill_table = [&](int tile, int c) {
         const int g0 = c / kTableChunks * kTableGroups;
@@ -193,7 +193,7 @@ __global__ void __launch_bounds__(kThreadsS, 1) w4_stream_kernel(const __grid_co
 #pragma unroll
             for (int i = 0; i < kTableGroups; ++i) {
                 const int group = min(g0 + i, p.groups - 1);
-                table[i * 32 + lane] = static_cast<uint32_t>(__ldg(p.scales + own + group)) << 16 | 0x4300u | (p.zeros ? __ldg(p.zeros + own + group) & 15u : 8u);
+                table[i * 32 + lane] = static_cast<uint32_t>(p.scales[own + group]) << 16 | 0x4300u | (p.zeros ? p.zeros[own + group] & 15u : 8u);
             }
         }
         __syncwarp();

@@ -214,18 +214,18 @@ __device__ __forceinline__ bool issue_all(const TensorParams& p, const Barriers&
 __device__ __forceinline__ uint2 load_zeros8(const TensorParams& p, const unsigned char* zero, int run)
 {
     if (!zero) return make_uint2(0x08080808u, 0x08080808u);
-    if (p.vectors) return __ldg(reinterpret_cast<const uint2*>(zero) + run);
+    if (p.vectors) return reinterpret_cast<const uint2*>(zero)[run];
     uint32_t z[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) z[i >> 2] |= static_cast<uint32_t>(__ldg(zero + min(run * 8 + i, p.groups - 1))) << (8 * (i & 3));
+    for (int i = 0; i < 8; ++i) z[i >> 2] |= static_cast<uint32_t>(zero[min(run * 8 + i, p.groups - 1)]) << (8 * (i & 3));
     return make_uint2(z[0], z[1]);
 }
 __device__ __forceinline__ uint4 load_scales8(const TensorParams& p, const unsigned short* scale, int run)
 {
-    if (p.vectors) return __ldg(reinterpret_cast<const uint4*>(scale) + run);
+    if (p.vectors) return reinterpret_cast<const uint4*>(scale)[run];
     uint32_t s[4] = {0, 0, 0, 0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i >> 1] |= static_cast<uint32_t>(__ldg(scale + min(run * 8 + i, p.groups - 1))) << (16 * (i & 1));
+    for (int i = 0; i < 8; ++i) s[i >> 1] |= static_cast<uint32_t>(scale[min(run * 8 + i, p.groups - 1)]) << (16 * (i & 1));
     return make_uint4(s[0], s[1], s[2], s[3]);
 }
 

@@ -279,3 +279,21 @@ def test_raw_handles_of_the_default_stream():
         torch.cuda.synchronize()
         assert int(status) == 0
         _close(out, hidden, codes, scales, zp)
+
+
+@pytest.mark.parametrize("rows", [1, 8, 40, 200])
+@pytest.mark.parametrize("V,d,group", [(300, 1024, 128), (9001, 1056, 32)])
+def test_every_input_written_by_the_kernel_before(rows, V, d, group):
+    """The kernel is set up while the one before it drains; what that one writes last is what is read."""
+    cases = [_to(*_case(rows, V, d, group, True, 91 + i)) for i in range(2)]
+    cases = [[h, binding.polyspec_pack_quantized(c), s, z] for h, c, s, z in cases]
+    want = [binding.polyspec_lm_head_quantized(*a)[0] for a in cases]
+    now = [t.clone() for t in cases[0]]
+    got = []
+    for n in range(24):
+        for which in range(4):                              # another input written last each time
+            for i in range(4):
+                now[(which + 1 + i) % 4].copy_(cases[n % 2][(which + 1 + i) % 4])
+            got.append((n % 2, binding.polyspec_lm_head_quantized(*now)[0]))
+    torch.cuda.synchronize()
+    assert all(torch.equal(out, want[i]) for i, out in got)
