@@ -400,7 +400,7 @@ __global__ void __launch_bounds__(256) move_kernel(const polyspec_cache_pages s,
 polyspec_status check_pages(const polyspec_cache_pages* s)
 {
     if (!s || s->n_seqs < 1 || s->max_pages < 1 || s->n_pages < 1 || s->page_tokens < 1) return POLYSPEC_ERR_INVALID_ARG;
-    if (!s->table || !s->len || !s->refs || !s->free_bits) return POLYSPEC_ERR_INVALID_ARG;
+    if (!s->table || !s->len || !s->refs || !s->free_bits || !aligned4(s->table, s->len, s->refs, s->free_bits)) return POLYSPEC_ERR_INVALID_ARG;
     if (static_cast<long long>(s->max_pages) * s->page_tokens > 0x7fffffffLL || s->n_pages > kMaxPages) return POLYSPEC_ERR_UNSUPPORTED;
     return POLYSPEC_OK;
 }
@@ -474,7 +474,7 @@ polyspec_status polyspec_cache_reserve(const polyspec_cache_pages* s, const int3
 {
     polyspec_status st = check_pages(s);
     if (st == POLYSPEC_OK) st = check_pools(pools, n_pools);
-    if (st == POLYSPEC_OK) st = base ? check_plan(s, workspace, workspace_bytes) : POLYSPEC_ERR_INVALID_ARG;
+    if (st == POLYSPEC_OK) st = base && aligned4(base, extra, device_status) ? check_plan(s, workspace, workspace_bytes) : POLYSPEC_ERR_INVALID_ARG;
     if (st != POLYSPEC_OK) return st;
     const Plan plan = plan_of(workspace, s->n_seqs, s->n_pages);
     cudaStream_t q = static_cast<cudaStream_t>(cuda_stream);
@@ -488,7 +488,7 @@ polyspec_status polyspec_cache_rollback(const polyspec_cache_pages* s, const int
 {
     const polyspec_status st = check_pages(s);
     if (st != POLYSPEC_OK) return st;
-    if (!base) return POLYSPEC_ERR_INVALID_ARG;
+    if (!base || !aligned4(base, extra, device_status)) return POLYSPEC_ERR_INVALID_ARG;
     const dim3 grid(static_cast<unsigned>((s->n_seqs + 3) / 4));
     return cuda_failed(launch_early(rollback_kernel, grid, 128, 0, static_cast<cudaStream_t>(cuda_stream), *s, base, extra, plus, device_status))
                ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
@@ -499,7 +499,7 @@ polyspec_status polyspec_cache_fork(const polyspec_cache_pages* s, const int32_t
 {
     const polyspec_status st = check_pages(s);
     if (st != POLYSPEC_OK) return st;
-    if (!src || !dst || n < 1) return POLYSPEC_ERR_INVALID_ARG;
+    if (!src || !dst || n < 1 || !aligned4(src, dst, device_status)) return POLYSPEC_ERR_INVALID_ARG;
     const dim3 grid(static_cast<unsigned>((n + 3) / 4));
     return cuda_failed(launch_early(fork_kernel, grid, 128, 0, static_cast<cudaStream_t>(cuda_stream), *s, src, dst, n, device_status))
                ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
@@ -510,7 +510,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s, const poly
 {
     polyspec_status st = check_pages(s);
     if (st == POLYSPEC_OK) st = check_pools(pools, n_pools);
-    if (st == POLYSPEC_OK) st = check_plan(s, workspace, workspace_bytes);
+    if (st == POLYSPEC_OK) st = aligned4(moved_to) ? check_plan(s, workspace, workspace_bytes) : POLYSPEC_ERR_INVALID_ARG;
     if (st != POLYSPEC_OK) return st;
     const Plan plan = plan_of(workspace, s->n_seqs, s->n_pages);
     cudaStream_t q = static_cast<cudaStream_t>(cuda_stream);

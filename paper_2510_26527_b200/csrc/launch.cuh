@@ -6,7 +6,13 @@
 
 #include <cuda_runtime.h>
 
+#include <cstdint>
+
 namespace polyspec {
+
+// Every pointer is a multiple of four or null: what arrays of 32-bit words need.
+template <class... P>
+inline bool aligned4(const P*... p) { return ((reinterpret_cast<uintptr_t>(p) | ...) & 3u) == 0; }
 
 __device__ __forceinline__ void wait_for_stream() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

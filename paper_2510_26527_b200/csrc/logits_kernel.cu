@@ -477,7 +477,9 @@ extern "C" polyspec_status polyspec_process_logits(
     if (p.c.history && p.c.history_cap < 1) return POLYSPEC_ERR_INVALID_ARG;
     if ((p.c.bias_tokens != nullptr) != (p.c.bias_values != nullptr)) return POLYSPEC_ERR_INVALID_ARG;
     if (p.c.bias_tokens && p.c.n_bias < 1) return POLYSPEC_ERR_INVALID_ARG;
-    if ((reinterpret_cast<uintptr_t>(p.c.mask) & 3u) != 0) return POLYSPEC_ERR_INVALID_ARG;
+    if (!aligned4(p.c.history, p.c.history_len, p.c.prompt_len, p.c.repetition, p.c.frequency, p.c.presence, p.c.bias_tokens, p.c.bias_values, p.c.mask,
+                  draft_tokens, device_status))
+        return POLYSPEC_ERR_INVALID_ARG;
     const size_t bytes = static_cast<size_t>(B) * rows * V * (dt == POLYSPEC_BF16 ? 2 : 4);
     const uintptr_t a = reinterpret_cast<uintptr_t>(logits), o = reinterpret_cast<uintptr_t>(out);
     if (a != o && a < o + bytes && o < a + bytes) return POLYSPEC_ERR_INVALID_ARG;        // the same buffer, or none of it

@@ -447,7 +447,7 @@ polyspec_status polyspec_lm_head_quantized(const void* hidden, const void* qweig
     if (!hidden || !qweight || !scales || !logits || rows <= 0 || V <= 0 || d <= 0) return POLYSPEC_ERR_INVALID_ARG;
     if (dt != POLYSPEC_F32 && dt != POLYSPEC_BF16) return POLYSPEC_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(hidden) & 15u) != 0 || (reinterpret_cast<uintptr_t>(qweight) & 15u) != 0 ||
-        (reinterpret_cast<uintptr_t>(logits) & 15u) != 0 || (reinterpret_cast<uintptr_t>(scales) & 1u) != 0)
+        (reinterpret_cast<uintptr_t>(logits) & 15u) != 0 || (reinterpret_cast<uintptr_t>(scales) & 1u) != 0 || !aligned4(device_status))
         return POLYSPEC_ERR_INVALID_ARG;
     if (group != 32 && group != 64 && group != 128) return POLYSPEC_ERR_UNSUPPORTED;
     if (d % group != 0 || V > 0x7fffffff - 1024 || rows > 0x7fffffff - 1024) return POLYSPEC_ERR_UNSUPPORTED;     // a tile past the end counts on

@@ -206,3 +206,32 @@ def test_page_sizes_of_contiguous_pools(shape, strides):
     assert pool.n_planes == shape[0] and pool.page_bytes == 2 * t[0, 0].numel()
     with pytest.raises(ValueError):
         binding._pools(pages, [torch.empty((0,) + shape[1:])])
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_arrays_of_words_off_their_boundary_are_refused(lib, off):
+    at, big = FAKE + off, 1 << 40
+    head = lambda status: lib.polyspec_lm_head_quantized(FAKE, FAKE, FAKE, None, 8, 32000, 4096, 128, binding.F32, FAKE, status, None)
+    assert head(at) == INVALID
+
+    def controls(draft=None, status=None, **fields):
+        c = binding.LogitControls(history_cap=5, n_bias=3, **fields)
+        return lib.polyspec_process_logits(FAKE, ctypes.byref(c), draft, 3, 2, 4, 1000, binding.BF16, FAKE + big, status, None)
+
+    assert controls(draft=at) == INVALID and controls(status=at) == INVALID
+    for name in ("history", "history_len", "prompt_len", "repetition", "frequency", "presence", "mask"):
+        assert controls(**{name: at}) == INVALID, name
+    assert controls(bias_tokens=at, bias_values=FAKE) == INVALID and controls(bias_tokens=FAKE, bias_values=at) == INVALID
+
+    def pages(s, base=FAKE, extra=None, moved_to=None, status=None):
+        return (lib.polyspec_cache_reserve(s, base, extra, 0, None, 0, status, FAKE, big, None), lib.polyspec_cache_rollback(s, base, extra, 0, status, None),
+                lib.polyspec_cache_fork(s, base, FAKE, 1, status, None), lib.polyspec_cache_fork(s, FAKE, base, 1, status, None))
+
+    for name in ("table", "len", "refs", "free_bits"):
+        s = _pages(**{name: at})
+        assert pages(s) == (INVALID,) * 4 and lib.polyspec_cache_init(s, None) == INVALID
+        assert lib.polyspec_cache_compact(s, None, 0, None, FAKE, big, None) == INVALID
+    s = _pages()
+    assert pages(s, base=at) == (INVALID,) * 4 and pages(s, status=at) == (INVALID,) * 4
+    assert pages(s, extra=at)[:2] == (INVALID,) * 2
+    assert lib.polyspec_cache_compact(s, None, 0, at, FAKE, big, None) == INVALID
