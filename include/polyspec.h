@@ -415,8 +415,10 @@ polyspec_status polyspec_staged_commit(const polyspec_staged_state* s /* host */
  *   zero_points  [V, d/group] bytes, or NULL for 8 everywhere; the low four bits of a byte count
  *   logits       out [rows, V] fp32 or bf16 (logits_dt), 16-byte aligned; any V
  *   q - z is multiplied exactly, a group's sum and the sum over the groups are held in fp32; bf16 logits are rounded once.
- *   The result of a row does not depend on timing.  No workspace; nothing outside [rows, V] is written.
- *   device_status as in polyspec_lm_head.
+ *   The result of a row does not depend on timing.  The order in which a logit's partial sums are added depends on the sizes: up to
+ *   eight rows and above are two kernels, and up to eight rows it changes with V.  So a row in a larger batch, or a slice of the
+ *   vocabulary, equals the whole within fp32 rounding, not bit for bit.
+ *   No workspace; nothing outside [rows, V] is written.  device_status as in polyspec_lm_head.
  */
 polyspec_status polyspec_pack_quantized(const void* codes /* [V, d] bytes, 16-byte aligned, low four bits count */, int V, int d /* a multiple of 32 */,
                                  void* qweight /* out [V, d/8] words */, void* cuda_stream);
@@ -439,7 +441,7 @@ polyspec_status polyspec_lm_head_quantized(const void* hidden, const void* qweig
  *
  *   logits [B, rows, V] fp32 or bf16, out [B, rows, V]: either the same buffer (in place) or one that does not overlap it;
  *   both 16-byte aligned, V a multiple of 8
- *   draft_tokens [B, k] or NULL (every row then has the history alone as its context), rows <= k + 1
+ *   draft_tokens [B, k] or NULL (every row then has the history alone as its context), k <= POLYSPEC_MAX_K, rows <= k + 1
  *   controls (host struct of device pointers; a NULL pointer leaves that control out):
  *     history       [B, history_cap] token ids; history_len [B] (NULL: history_cap), prompt_len [B] (NULL: 0): the first
  *                   prompt_len tokens are the prompt, which counts for the repetition penalty only
@@ -493,7 +495,7 @@ polyspec_status polyspec_process_logits(const void* logits, const polyspec_logit
  *        tokens, src is a dst of the list, or an earlier pair has the same dst.
  *   polyspec_cache_compact   moves pages so that those in use are numbered 0 .. n_live-1: the i-th used page from n_live on
  *        goes to the i-th free page below n_live, its contents in every pool with it; tables follow.  moved_to [n_pages] (or
- *        NULL): the new number of every page in use, -1 for free ones.
+ *        NULL): the new number of every page in use, -1 for free ones.  Table words behind a sequence's pages stay as they are.
  *   Reserve and compact need a workspace of polyspec_cache_workspace bytes.  Calls on one state must be ordered by the
  *   caller (one stream); the outcome depends on the state alone.  A page number out of range or a reference too many found on
  *   the way is skipped and reported as POLYSPEC_ERR_BAD_INPUT_ON_DEVICE.

@@ -17,7 +17,8 @@
 // text of thousands of tokens touches a few entries of every 256 that a warp moves: computing them where the vectors pass by
 // had the whole warp take the slow path almost every time, 116 us on 64 x 7 rows of 128256; a barrier per row 75, one barrier 68.)
 // Measured, bf16: 64 x 7 x 128256, texts of 4096: 57 us, 4.0 TB/s of the bytes it needs; 256 x 5 x 152064 with masks: 134 us, 4.6;
-// masks alone in place, 64 x 7 x 128256: 31 us.
+// masks alone in place, 64 x 7 x 128256: 31 us.  fp32, to which slices and occupancy were not fitted (slices of 4096 entries and more
+// spill registers): 64 x 7 x 128256, texts of 4096: 117 us, 3.9 TB/s; 128 x 5 x 152064 with masks: 145 us, 4.2.
 // Counting with integer atomics and adding listed biases in list order make the result independent of timing.
 #include <cuda_bf16.h>
 

@@ -17,9 +17,10 @@
 // worked on are added up in a fixed order.  (Whole tiles per team of warps, with a reduction and two barriers per tile:
 // 26.3 against 24.0 us on 1 x 32000 x 4096.)  The hidden rows are staged once per CTA in fragment
 // order.
-// Measured: 1 x 32000 x 4096 in groups of 128, 20.5 us, 3.35 TB/s (floor 10.5: 4 to 5 us pass before the first piece is computed,
-// then issue, 53% of its slots); 5 x 152064 x 8192 in groups of 64, 158 us, 4.3 TB/s (63% of the issue slots; the same loop
-// without the arithmetic streams in 103).
+// Measured as a replayed graph: 1 x 32000 x 4096 in groups of 128, 20.5 us, 3.35 TB/s (floor 10.5; 4 to 5 us pass before the first
+// piece is computed); 5 x 152064 x 8192 in groups of 64, 158 us, 4.3 TB/s (173 us, 3.9 TB/s in calls queued by the host; the same
+// loop without the arithmetic streams in 103).  Neither memory (51 and 66%) nor issue (53 and 64% of the slots) is full: a warp takes
+// one piece at a time through one dependent chain of wait, shared loads, expansion and MMA.
 // Every wait on a copy is bounded: a warp whose wait runs out sets POLYSPEC_ERR_TIMEOUT, asks for nothing more, waits (again with
 // a limit) for the copies it has on their way and goes to the barrier at the end.
 #include <cuda_bf16.h>
@@ -52,7 +53,9 @@ __device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], 
 using namespace tensordev;
 
 constexpr int kPieceBytes = kTileS * kChunk / 2;        // 2 KiB
-constexpr int kMaxRing = 2;                       // 64 KiB in flight per SM; six pieces put 28 MB of requests before the hidden rows and scales
+// 64 KiB in flight per SM.  On 1 x 32000 x 4096 and 5 x 12807 x 2080, the sizes it was chosen on, six pieces put 28 MB of requests
+// before the hidden rows and scales; longer runs were not swept.
+constexpr int kMaxRing = 2;
 constexpr int kTableGroups = 8;                         // groups whose scales and zero points a warp holds at a time
 constexpr int kTableWords = kTableGroups * 32;
 constexpr int kSums = 8;                                // accumulators per lane: two m16 tiles x four

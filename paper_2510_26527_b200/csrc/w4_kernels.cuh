@@ -24,7 +24,7 @@ namespace w4 {
 // The eight weights of a word as four bf16 pairs (0,1) (2,3) (4,5) (6,7), the zero point subtracted.
 // `magic` holds 128 + z twice; 128 + q, 128 + z and q - z are all exact in bf16.  `exponent` is kExponent, which callers pass
 // from a kernel parameter: a value the compiler cannot see stays in a register, so that mask and exponent are one three-input
-// instruction; as two immediates they took two (15 instead of 7 logic instructions per word, and those bound the kernels).
+// instruction; as two immediates they are two.
 constexpr uint32_t kExponent = 0x43004300u;
 __device__ __forceinline__ void expand(uint32_t word, uint32_t magic, uint32_t exponent, uint32_t (&pairs)[4])
 {

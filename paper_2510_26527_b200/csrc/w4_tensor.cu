@@ -20,9 +20,10 @@
 // slots, so that small groups do not multiply the handshakes.
 // With few rows an MMA is short and what a block costs is the MMA warp's own handshakes (some 90 cycles per wait that passes at
 // once, by time stamps): blocks of 256 elements up to 64 rows, 128 above.
-// Measured, 32000 x 4096 in groups of 128: 9 rows 23.3 us (57% of the issue slots), 288 rows 83 us, 906 TFLOP/s (tensor pipe 40%,
-// issue slots 60%; every tile of 128 entries reads all hidden rows, 0.62 GB from L2); 37 x 12807 x 2080 in groups of 32 17.1 us
-// (101 tiles on 148 SMs).
+// Measured as a replayed graph, 32000 x 4096 in groups of 128: 9 rows 23.3 us, 288 rows 83 us, 909 TFLOP/s (95 us, 793 TFLOP/s in calls
+// queued by the host; tensor pipe 40%, issue slots 60%; every tile of 128 entries reads all hidden rows, 0.58 GB from L2);
+// 37 x 12807 x 2080 in groups of 32 17.1 us (101 tiles on 148 SMs).  The shapes were chosen on groups of 128; small groups leave
+// fewer MMAs to each slot's handshake: 288 rows 123 us in groups of 64, 203 us in groups of 32; 64 rows 32 us, in groups of 32 57 us.
 //
 // Every wait on an mbarrier is bounded: one that runs out raises an abort flag that all roles poll, sets POLYSPEC_ERR_TIMEOUT,
 // and the kernel still lets its copies land, frees tensor memory and returns.

@@ -40,9 +40,10 @@ class StagedBatch:
     u1           [B, C, MAX_BLOCK+1] float32: row c serves its c-th M_1 pass (slots 0..m-1 accept tests, slot MAX_BLOCK sampling)
     caches       None, or {"M1" / "M2" / "M3": (binding.CachePages of B sequences, pools)}: page tables kept in step with the loop
                  without a read-back.  Before a forward pass a model's cache has room for every token the pass is given (for row i
-                 the tokens before position i); after it, and after M_1's commit, it falls back to the tokens that stand and
-                 have been given to the model, all but the last one emitted.  A pool too small sets ERR_NO_PAGES in `status` and
-                 leaves that sequence's pages as they were; the loop itself reads nothing through them.
+                 the tokens before position i); after it, and after M_1's commit, it falls back to those of them that stand, the last
+                 token emitted never among them.  Sequences that sit a pass out (M_1's below the threshold, those that are done) are
+                 left as they are.  A pool too small sets ERR_NO_PAGES in `status` and leaves that sequence's pages as they were; the
+                 loop itself reads nothing through them.
     """
 
     def __init__(self, M1, M2, M3, drafts, u2, u1, K: int, mu: int, n_tokens: int, temperature: float, caches=None):
