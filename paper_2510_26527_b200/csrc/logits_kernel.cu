@@ -375,18 +375,17 @@ __global__ void __launch_bounds__(kThreads, 5) logits_kernel(const ControlParams
     const int v0 = slice * kSlice;
     const int n = min(kSlice, p.V - v0);
     const int j0 = group * p.rows_per_group, j1 = min(p.rows, j0 + p.rows_per_group);
+    // Without a context no entry is penalised, but a bad factor is reported all the same (here, where no vectors are in registers).
+    if (!COUNTS && slice == 0 && group == 0 && tid == 0 && p.c.repetition && !(p.c.repetition[b] > 0.0f)) bad_input(p.status);
     // In place, an edit of this CTA changes what it read: the edits come after the vectors, and every entry is edited once.
     const bool in_place = p.out == p.logits;
     if (!in_place || p.c.mask) {
         if (n == kSlice) stream_rows<DT, VPT, true>(p, b, v0, n, j0, j1, in_place);
         else stream_rows<DT, VPT, false>(p, b, v0, n, j0, j1, in_place);
     }
-    const bool report = slice == 0 && group == 0;
-    if (!COUNTS) {                              // no entry is penalised, but a bad factor is reported all the same
-        if (report && tid == 0 && p.c.repetition && !(p.c.repetition[b] > 0.0f)) bad_input(p.status);
-        return;
-    }
+    if (!COUNTS) return;
 
+    const bool report = slice == 0 && group == 0;
     Slice<WIDE> s;
     s.count.w = reinterpret_cast<uint32_t*>(smem_controls);
     s.bias = p.c.bias_tokens ? reinterpret_cast<float*>(reinterpret_cast<char*>(smem_controls) + kSlice * (Counts<WIDE>::kBytes + 2)) : nullptr;
