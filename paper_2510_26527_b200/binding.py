@@ -1002,9 +1002,9 @@ class CachePages:
     """Page tables of one model's cache: table [n_seqs, max_pages], len [n_seqs], refs [n_pages] (int32) and free_bits
     [ceil(n_pages/32)] (int32), on the device.  CachePages.new allocates and initialises them; the constructor takes tensors
     that hold a state already.  The calls' workspace is allocated at the first call that needs one and belongs to the state:
-    calls on one state are ordered anyway.  torch streams that it is used on besides the one it was allocated on are recorded, so
-    that its memory is not handed out again before their work is done; for raw handles, which may be destroyed before the state is, and
-    for the state's tensors that is the caller's to see to."""
+    calls on one state are ordered anyway.  Streams of torch's own that it is used on besides the one it was allocated on are
+    recorded, so that its memory is not handed out again before their work is done; for raw handles and external streams, which may be
+    destroyed before the state is, and for the state's tensors that is the caller's to see to."""
 
     def __init__(self, table, len, refs, free_bits, page_tokens):
         i32 = torch.int32
@@ -1019,7 +1019,7 @@ class CachePages:
         self.n_seqs, self.max_pages, self.n_pages, self.page_tokens = n_seqs, max_pages, n_pages, int(page_tokens)
         self.c = CachePagesStruct(n_seqs, max_pages, n_pages, self.page_tokens, table.data_ptr(), len.data_ptr(), refs.data_ptr(),
                                   free_bits.data_ptr())
-        self._workspace, self._workspace_streams = None, set()
+        self._workspace, self._workspace_streams = None, set()          # the streams it belongs to: allocated on, recorded
 
     @classmethod
     def new(cls, n_seqs, max_pages, n_pages, page_tokens, device="cuda", stream=None):
@@ -1033,9 +1033,12 @@ class CachePages:
         handle = _handle(stream, self.dev)
         if self._workspace is None:
             self._workspace = _empty(polyspec_cache_workspace(self.n_seqs, self.n_pages), torch.uint8, self.dev, stream)
+            self._workspace_streams = {handle}
         elif handle not in self._workspace_streams and (stream is None or isinstance(stream, torch.cuda.Stream)):
-            self._workspace.record_stream(torch.cuda.current_stream(self.dev) if stream is None else stream)
-        self._workspace_streams.add(handle)
+            used = torch.cuda.current_stream(self.dev) if stream is None else stream
+            if handle == 0 or used.stream_id != handle:     # an external stream's id is its handle
+                self._workspace.record_stream(used)
+                self._workspace_streams.add(handle)
         return self._workspace
 
 

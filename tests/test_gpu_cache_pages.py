@@ -1,4 +1,5 @@
 """Cache pages against the plain tables: every array equal after every call, and the contents of the pools with them."""
+import ctypes
 import random
 
 import numpy as np
@@ -295,3 +296,29 @@ def test_workspace_outlives_its_use_on_another_stream(given):
     assert not side.query()
     assert at not in [x.data_ptr() for x in again]
     side.synchronize()
+
+
+@pytest.mark.parametrize("how", ["current", "external", "raw"])
+def test_a_state_outlives_an_external_stream_it_was_used_on(how, monkeypatch):
+    """Nothing is recorded for a stream that is not torch's: the state may be dropped after the stream is gone."""
+    recorded = []
+    monkeypatch.setattr(torch.Tensor, "record_stream", lambda self, stream: recorded.append(stream))
+    both = Both(3, 8, 64, 4)
+    both.reserve([10, 20, 30])
+    handle, cudart = ctypes.c_ulonglong(0), torch.cuda.cudart()
+    assert int(cudart.cudaStreamCreate(ctypes.addressof(handle))) == 0
+    torch.cuda.synchronize()
+    external = torch.cuda.ExternalStream(handle.value)
+    if how == "current":
+        with torch.cuda.stream(external):
+            binding.polyspec_cache_compact(both.pages)
+    else:
+        binding.polyspec_cache_compact(both.pages, stream=external if how == "external" else handle.value)
+    both.plain.compact()
+    both.check(None)
+    assert int(cudart.cudaStreamDestroy(handle.value)) == 0
+    assert recorded == []
+    side = torch.cuda.Stream()
+    binding.polyspec_cache_compact(both.pages, stream=side)
+    both.check(None)
+    assert recorded == [side]
