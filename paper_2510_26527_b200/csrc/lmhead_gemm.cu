@@ -463,8 +463,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) lmh
 
 std::mutex g_init_mutex;
 EncodeTiledFn g_encode = nullptr;
-bool g_attr_set[64] = {false};
-int g_pairs[64] = {0};      // CTA pairs the device can hold at once
+int g_pairs[64] = {0};      // CTA pairs the device can hold at once; 0: not looked at yet
 
 cudaError_t get_encoder() { return g_encode ? cudaSuccess : find_encoder(&g_encode); }
 
@@ -509,7 +508,7 @@ cudaError_t launch_lmhead(const LmHeadProblem* probs, int n, int V, float c, int
     // setting an attribute binds the device's where the thread has none yet.
     e = cudaFuncSetAttribute(lmhead_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kGemmSmemBytes));
     if (e != cudaSuccess) return e;
-    if (!g_attr_set[dev]) {
+    if (g_pairs[dev] == 0) {
         int sms = 0;
         e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
         if (e != cudaSuccess) return e;
@@ -530,7 +529,6 @@ cudaError_t launch_lmhead(const LmHeadProblem* probs, int n, int V, float c, int
             clusters = sms / 2;
         }
         g_pairs[dev] = clusters < sms / 2 ? clusters : sms / 2;
-        g_attr_set[dev] = true;
     }
 
     GemmParams p;

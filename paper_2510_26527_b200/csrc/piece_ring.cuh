@@ -1,7 +1,7 @@
 // The turns of a ring of shared-memory slots that one warp fills with asynchronous copies and empties in the same order: which
 // slot the next copy goes to, which one is waited for next and with what parity, and how many copies are on their way.  The user
 // asks `size` times at the start, and then once for each copy used, before next(): so a slot asked into is always free.  No CUDA
-// in it but the qualifiers: tests/piece_ring_driver.cpp plays it on the host.
+// in it but the qualifiers, so that it can be played on the host.
 #pragma once
 
 #include <cstdint>
