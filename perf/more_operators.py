@@ -393,8 +393,8 @@ PLAIN = {"rotate": _plain_rotate, "prompt": _plain_prompt, "append": _plain_appe
 # ------------------------------------------------------------------ the package's calls
 def _own_rotate(s):
     from paper_2510_26527_b200 import binding
-    q, k, _ = binding.polyspec_rotate_heads(s["q"], s["k"], s["positions"], s["frequencies"], s["q_weight"], s["k_weight"], interleaved=s["interleaved"],
-                                            q_out=s["q_out"], k_out=s["k_out"])
+    q, k = binding.polyspec_rotate_heads(s["q"], s["k"], s["positions"], s["frequencies"], s["q_weight"], s["k_weight"], interleaved=s["interleaved"],
+                                         q_out=s["q_out"], k_out=s["k_out"])
     return {"q": q, "k": k}
 
 
