@@ -524,6 +524,101 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
                                        int32_t* moved_to, void* workspace, size_t workspace_bytes, void* cuda_stream);
 
 /*
+ * A model's attention around the cache pages: what its pass over a prompt or a block needs between its projections and its LM head.
+ * All of it takes rows of heads in bf16: [rows, heads, head_dim] with the heads of a row behind one another and `stride` elements from
+ * row to row (a multiple of 8, at least heads * head_dim), 16-byte aligned, so that queries, keys and values may be parts of the rows of
+ * one fused projection.  Outputs of heads are contiguous.
+ *
+ * polyspec_rotate_heads -- norm of every query and key head and its rotation by position, in one pass:
+ *     y = weight ? x / sqrt(mean(x^2) + eps) * weight : x
+ *     (a, b) -> (a cos - b sin, a sin + b cos),  angle = positions[row] * frequencies[i],
+ *   (a, b) the elements (i, i + rotary_dim/2), or (2i, 2i + 1) if interleaved, of the first rotary_dim of a head; the others stay.
+ *   In fp32 (the angle's turns in fp64), rounded once to bf16.
+ *   q [rows, q_heads, head_dim], k [rows, kv_heads, head_dim]; k may be NULL (kv_heads 0)
+ *   positions [rows] (any int32), frequencies [rotary_dim/2] fp32, in radians per position
+ *   q_weight, k_weight [head_dim] bf16, or NULL: no norm.  eps >= 0
+ *   head_dim and rotary_dim multiples of 16, rotary_dim <= head_dim <= 256 (0: no rotation, positions and frequencies unread)
+ *   q_out, k_out  out, row strides of their own; either the rows of q, k themselves (in place) or rows that overlap none of the inputs.
+ *
+ * polyspec_prompt_attention -- causal attention over whole prompts, packed one behind the other:
+ *     out[i, h] = sum_{j <= i} softmax_j(scale * q[i, h] . k[j, h / (q_heads/kv_heads)]) v[j, .]   i, j rows of one prompt
+ *   rows_at [n_seqs + 1]: prompt b is the rows rows_at[b] .. rows_at[b + 1]-1 (none if equal); rows outside all of them are neither read into
+ *   a result nor written.  q_heads a multiple of kv_heads; head_dim 64 or 128; scale finite
+ *   out [rows, q_heads, head_dim]; lse out [rows, q_heads] fp32 or NULL: the natural logarithm of the softmax's denominator.
+ *   Products of bf16, sums and softmax in fp32; weights are rounded to bf16 for their product with the values.  Keys and values behind a
+ *   row never reach it, NaN and infinities included.  Row numbers that decrease or lie outside 0 .. rows make the prompt empty
+ *   (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE in *device_status); POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.
+ *
+ * Caches held in 4 bits.  One plane of a pool holds one layer's keys or values; a token's head is head_dim codes with one scale and one
+ * offset (bf16): value = scale * code + offset, scale > 0.  A page of polyspec_cache_pages (page_tokens a multiple of 8, at most 32768) is
+ * [kv_heads, page_tokens / 8] units of 8 tokens; a unit is head_dim 32-bit words of codes, then 8 pairs (scale, offset):
+ * page_bytes = kv_heads * (page_tokens / 8) * (4 head_dim + 32).  Code e of eight neighbours is in the four bits from bit
+ * 4 * (e / 2) + 16 * (e % 2) on of their word.  Word w of token r lies at r * head_dim/8 + w in a unit of keys; in a unit of values, with
+ * w = 8 h + g, at (8 g + r) * head_dim/64 + h (where the attention's matrix instructions want it).
+ * A pool [2 * layers, n_pages, page_bytes] serves reserve, compact and evict as it is; the calls of one layer take its two
+ * planes, keys then values.
+ *
+ * Which rows are whose in append, attention and weigh: sequence b has the rows rows_at[b] .., rows_at[b + 1] - rows_at[b] of them or the
+ * first n_rows[b] (NULL: all); its row i stands at slot base[b] + (extra ? extra[b] : 0) + i of its cache.  Reserve comes first: a row
+ * whose slot is not below len[b] is not written or attends to nothing (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE), as are the rows of a sequence
+ * whose numbers make no sense.
+ *
+ * polyspec_cache_append -- keys and values of new rows into their slots:  offset = min(x), scale = the smallest bf16 number
+ *   >= (max(x) - offset) / 15 (1 if that is 0), code = (x - offset) / scale rounded to the nearest, ties to even, at most 15; differences and
+ *   quotients in fp32.  Of x with NaN, infinities or a range past fp32: every value NaN.
+ *   k_held, v_held  out [rows, kv_heads, head_dim] bf16 or NULL: the values the pages now stand for
+ *   weights         [n_seqs, max_pages * page_tokens] fp32 or NULL: set to 0 at the new slots
+ *   A page that other sequences hold too is not written (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE).
+ *
+ * polyspec_cache_attention -- the rows of a block over the cache, each row over the slots up to its own:
+ *     out[i, h] = sum_{j <= slot(i)} softmax_j(scale * q[i, h] . K[j, h / (q_heads/kv_heads)]) V[j, .]
+ *   head_dim 64 or 128, any number of rows; out, lse as in polyspec_prompt_attention; a row that attends to nothing gets zeros and -inf.  Codes are
+ *   multiplied as whole numbers, scales and offsets applied to fp32 sums; softmax weights are rounded to fp16 for their product
+ *   with the codes.  The order of the sums depends on the lengths and on the batch.
+ *   Workspace of polyspec_cache_attention_workspace bytes.
+ *
+ * polyspec_cache_weigh -- adds to every cached token the attention weight that the rows gave it, over all heads:
+ *     weights[b, j] = keep * weights[b, j] + sum_{i, h} exp(scale * q[i, h] . K[j, .] - lse[i, h])   for j < len[b]
+ *   with lse of polyspec_cache_attention on the same rows (n_rows may be fewer: only the rows that were accepted).  The sum over rows and
+ *   heads has a fixed order.
+ *
+ * polyspec_cache_evict -- sequences of more than budget[b] tokens (budget[b] >= 0) keep the first `first`, the last `recent` and, of those between, the ones of
+ *   largest weight (the lower slot of equal ones; NaN below everything) until budget[b] are left.  What is kept moves together in
+ *   every plane of the pool and in the weights, in order; pages wholly behind are given back, len follows.  What lies behind the kept tokens in
+ *   a page or in the weights stays as it is.  A sequence stays as it was (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE) if its budget is below first + recent, or
+ *   if a page from the first changed slot on is held by others too.
+ *   kept_from  out [n_seqs, max_pages * page_tokens] or NULL: the slot each kept token of a shortened sequence had, -1 behind them;
+ *              sequences that were not shortened get -1 throughout.
+ *   Workspace of polyspec_cache_evict_workspace bytes.
+ */
+polyspec_status polyspec_rotate_heads(const void* q, long long q_stride, int q_heads, const void* k, long long k_stride, int kv_heads,
+                                      int rows, int head_dim, int rotary_dim, int interleaved, const int32_t* positions,
+                                      const float* frequencies, const void* q_weight, const void* k_weight, float eps,
+                                      void* q_out, long long q_out_stride, void* k_out, long long k_out_stride, void* cuda_stream);
+polyspec_status polyspec_prompt_attention(const void* q, long long q_stride, const void* k, long long k_stride, const void* v, long long v_stride,
+                                          const int32_t* rows_at, int n_seqs, int rows, int q_heads, int kv_heads, int head_dim, float scale,
+                                          void* out, float* lse, int32_t* device_status, void* cuda_stream);
+typedef struct {
+    const int32_t *rows_at, *n_rows, *base, *extra;     /* device; n_rows and extra may be NULL */
+    int rows;                                           /* rows of the tensors of heads */
+} polyspec_block_rows;
+polyspec_status polyspec_cache_append(const polyspec_cache_pages* s /* host */, const polyspec_block_rows* r /* host */,
+                                      const void* k, long long k_stride, const void* v, long long v_stride, int kv_heads, int head_dim,
+                                      void* pool, void* k_held, void* v_held, float* weights, int32_t* device_status, void* cuda_stream);
+polyspec_status polyspec_cache_attention_workspace(int q_heads, int kv_heads, int head_dim, size_t* bytes /* host out */);
+polyspec_status polyspec_cache_attention(const polyspec_cache_pages* s /* host */, const polyspec_block_rows* r /* host */,
+                                         const void* q, long long q_stride, int q_heads, int kv_heads, int head_dim, float scale,
+                                         const void* pool, void* out, float* lse, int32_t* device_status,
+                                         void* workspace, size_t workspace_bytes, void* cuda_stream);
+polyspec_status polyspec_cache_weigh(const polyspec_cache_pages* s /* host */, const polyspec_block_rows* r /* host */,
+                                     const void* q, long long q_stride, int q_heads, int kv_heads, int head_dim, float scale,
+                                     const void* pool, const float* lse, float keep, float* weights, int32_t* device_status, void* cuda_stream);
+polyspec_status polyspec_cache_evict_workspace(int n_seqs, int max_pages, int page_tokens, size_t* bytes /* host out */);
+polyspec_status polyspec_cache_evict(const polyspec_cache_pages* s /* host */, const int32_t* budget, int first, int recent, float* weights,
+                                     void* pool, int n_planes, int kv_heads, int head_dim, int32_t* kept_from, int32_t* device_status,
+                                     void* workspace, size_t workspace_bytes, void* cuda_stream);
+
+/*
  * polyspec_verify_level_static -- polyspec_verify_level without a workspace argument.
  * (The paper has no counterpart to this call; it exists for integration reasons only.)
  *

@@ -222,7 +222,7 @@ const char* polyspec_status_string(polyspec_status s)
     return "unknown status";
 }
 
-int polyspec_version(void) { return 400; }      // 0.4.0: 4-bit LM head, sampling controls on logits, cache pages in the ABI
+int polyspec_version(void) { return 500; }      // 0.5.0: head rotation, prompt attention, 4-bit cache pages (append, attention, weights, eviction) in the ABI
 
 const char* polyspec_last_cuda_error(void) { return cudaGetErrorString(g_last_cuda_error); }
 

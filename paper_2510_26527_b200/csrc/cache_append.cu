@@ -1,0 +1,143 @@
+// Keys and values of new rows into a cache's 4-bit pages: per token and head an offset, a scale and a code per element.
+//
+//   offset = min(x), scale = (max(x) - offset) / 15 rounded up to bf16, code = rint((x - offset) / scale)
+//
+// A word of eight codes is one lane's 16-byte vector, a head head_dim / 8 lanes; keys and values of a row's head are neighbours in a warp.
+// Rounding the scale up keeps every code at 15 or below, so nothing is cut off.
+#include <cuda_bf16.h>
+
+#include "kv_pages.cuh"
+
+namespace polyspec {
+namespace {
+
+constexpr int kThreads = 256;
+
+struct AppendParams {
+    polyspec_cache_pages s;
+    polyspec_block_rows r;
+    const __nv_bfloat16 *k, *v;
+    long long k_stride, v_stride;
+    unsigned char* pool;
+    size_t page_bytes;
+    __nv_bfloat16 *k_held, *v_held;
+    float* weights;
+    int32_t* status;
+    int kv_heads;
+};
+
+// D: head_dim.  A CTA has a row; its teams of D / 8 lanes take turns over (head, keys or values).
+template <int D>
+__global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
+{
+    constexpr int kLanes = D / 8;
+    __shared__ int found;
+    wait_for_stream();
+    const int row = blockIdx.x;
+    if (row == 0)               // numbers that make no sense are reported even where no row belongs to them
+        for (int b = threadIdx.x; b < p.s.n_seqs; b += kThreads)
+            if (kv::seq_rows(p.s, p.r, b).bad) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
+    const int b = kv::find_seq(p.r.rows_at, p.s.n_seqs, row, &found);
+    if (b < 0) return;
+    const kv::SeqRows q = kv::seq_rows(p.s, p.r, b);
+    const int i = row - q.row0;
+    if (i >= q.granted) return;
+    const int slot = q.base + i, P = p.s.page_tokens;
+    const int page = p.s.table[static_cast<size_t>(b) * p.s.max_pages + slot / P];
+    if (page < 0 || page >= p.s.n_pages || p.s.refs[page] > 1) {
+        if (threadIdx.x == 0) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
+        return;
+    }
+    if (p.weights && threadIdx.x == 0) p.weights[static_cast<size_t>(b) * p.s.max_pages * P + slot] = 0.0f;
+    const int at = slot % P, unit = at / kv::kUnit, r = at % kv::kUnit, w = threadIdx.x % kLanes;
+    // (whole warps go round together: the exchange below is warp-wide)
+    for (int j0 = 0; j0 < 2 * p.kv_heads; j0 += kThreads / kLanes) {
+        const int j = j0 + threadIdx.x / kLanes, head = j >> 1, values = j & 1;
+        const bool live = head < p.kv_heads;
+        float x[8];
+        if (live) {
+            const __nv_bfloat16* from = (values ? p.v + row * p.v_stride : p.k + row * p.k_stride) + head * D;
+            const uint4 raw = reinterpret_cast<const uint4*>(from)[w];
+            x[0] = __uint_as_float(raw.x << 16); x[1] = __uint_as_float(raw.x & 0xffff0000u);
+            x[2] = __uint_as_float(raw.y << 16); x[3] = __uint_as_float(raw.y & 0xffff0000u);
+            x[4] = __uint_as_float(raw.z << 16); x[5] = __uint_as_float(raw.z & 0xffff0000u);
+            x[6] = __uint_as_float(raw.w << 16); x[7] = __uint_as_float(raw.w & 0xffff0000u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+        }
+        float lo = x[0], hi = x[0];
+        bool nan = false;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            lo = fminf(lo, x[e]);
+            hi = fmaxf(hi, x[e]);
+            nan = nan || !(fabsf(x[e]) <= 3.4e38f);
+        }
+#pragma unroll
+        for (int d = 1; d < kLanes; d <<= 1) {
+            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+        }
+        const uint32_t bad = __ballot_sync(0xffffffffu, nan);
+        const uint32_t team = ((1ull << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
+        float offset = lo + 0.0f;                       // (not -0)
+        const float range = hi - offset;
+        const uint32_t up = (__float_as_uint(__fdiv_rn(range, 15.0f)) + 0xffffu) & 0xffff0000u;
+        float scale = up ? __uint_as_float(up) : 1.0f;
+        const bool broken = (bad & team) || !(range <= 3.4e38f);
+        if (broken) scale = offset = __uint_as_float(0x7fc00000u);
+        uint32_t word = 0, held[4];
+        float y[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int code = broken ? 0 : min(15, static_cast<int>(rintf(__fdiv_rn(x[e] - offset, scale))));
+            word |= static_cast<uint32_t>(code) << (4 * (e / 2) + 16 * (e % 2));
+            y[e] = __fadd_rn(__fmul_rn(scale, static_cast<float>(code)), offset);
+        }
+        if (!live) continue;
+        unsigned char* plane = p.pool + (values ? static_cast<size_t>(p.s.n_pages) * p.page_bytes : 0);
+        uint32_t* to = reinterpret_cast<uint32_t*>(plane + page * p.page_bytes + static_cast<size_t>(head * (P / kv::kUnit) + unit) * kv::unit_bytes(D));
+        to[values ? kv::value_word(r, w, D) : kv::key_word(r, w, D)] = word;
+        if (w == 0) to[D + r] = (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
+        __nv_bfloat16* out = values ? p.v_held : p.k_held;
+        if (out) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 z = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
+                held[e] = *reinterpret_cast<const uint32_t*>(&z);
+            }
+            reinterpret_cast<uint4*>(out + (static_cast<size_t>(row) * p.kv_heads + head) * D)[w] = make_uint4(held[0], held[1], held[2], held[3]);
+        }
+    }
+}
+
+}  // namespace
+}  // namespace polyspec
+
+using namespace polyspec;
+
+extern "C" polyspec_status polyspec_cache_append(const polyspec_cache_pages* s, const polyspec_block_rows* r, const void* k, long long k_stride,
+                                                 const void* v, long long v_stride, int kv_heads, int head_dim, void* pool, void* k_held,
+                                                 void* v_held, float* weights, int32_t* device_status, void* cuda_stream)
+{
+    polyspec_status st = kv::check_state(s);
+    if (st == POLYSPEC_OK) st = kv::check_rows(r);
+    if (st == POLYSPEC_OK) st = kv::check_heads(kv_heads, kv_heads, head_dim);
+    if (st != POLYSPEC_OK) return st;
+    if (!kv::rows_ok(k, k_stride, kv_heads, head_dim) || !kv::rows_ok(v, v_stride, kv_heads, head_dim)) return POLYSPEC_ERR_INVALID_ARG;
+    if (!pool || !kv::aligned16(pool) || !kv::aligned16(k_held) || !kv::aligned16(v_held) || !aligned4(weights, device_status)) return POLYSPEC_ERR_INVALID_ARG;
+    AppendParams p;
+    p.s = *s; p.r = *r;
+    p.k = static_cast<const __nv_bfloat16*>(k); p.v = static_cast<const __nv_bfloat16*>(v);
+    p.k_stride = k_stride; p.v_stride = v_stride;
+    p.pool = static_cast<unsigned char*>(pool);
+    p.page_bytes = kv::page_bytes(*s, kv_heads, head_dim);
+    p.k_held = static_cast<__nv_bfloat16*>(k_held); p.v_held = static_cast<__nv_bfloat16*>(v_held);
+    p.weights = weights; p.status = device_status; p.kv_heads = kv_heads;
+    const dim3 grid(static_cast<unsigned>(r->rows));
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    const cudaError_t e = head_dim == 128 ? launch_early(append_kernel<128>, grid, kThreads, 0, stream, p)
+                                          : launch_early(append_kernel<64>, grid, kThreads, 0, stream, p);
+    return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
+}

@@ -1,0 +1,322 @@
+// Shortening caches to a budget by accumulated attention weight: of the tokens between the first few and the last few the
+// heaviest stay, what stays moves together in every plane, pages behind it are given back.
+//
+// Two launches.  The first, one CTA per sequence, finds the weight of the last token that stays (radix selection over the weights' bits,
+// four passes of eight bits), lists the slots that stay in order, moves the weights, gives pages back.  The second moves the contents:
+// a CTA per sequence, plane and head goes through the kept tokens in order, kBatch at a time.  A token never moves up, so a batch that has been
+// read before it is written overwrites nothing that a later batch reads.
+// Moving is HBM-bound: each token that moves is read and written once.
+#include "kv_pages.cuh"
+
+namespace polyspec {
+namespace {
+
+constexpr int kSelectThreads = 1024;
+constexpr int kMoveThreads = 256;
+
+struct EvictPlan {
+    int32_t* head;          // [n_seqs, 4]: first new slot whose token moves, tokens kept (0: sequence stays as it is)
+    int32_t* from;          // [n_seqs, cap]: the slot that kept token i had
+    float* weights;         // [n_seqs, cap]: its weight
+    int32_t* pages;         // [n_seqs, max_pages]: the table as it was
+};
+
+inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+size_t evict_bytes(int n_seqs, int max_pages, int page_tokens)
+{
+    const size_t n = n_seqs, cap = static_cast<size_t>(max_pages) * page_tokens;
+    return align256(n * 16) + 2 * align256(n * cap * 4) + align256(n * max_pages * 4);
+}
+EvictPlan evict_plan(void* workspace, int n_seqs, int max_pages, int page_tokens)
+{
+    const size_t n = n_seqs, cap = static_cast<size_t>(max_pages) * page_tokens;
+    char* w = static_cast<char*>(workspace);
+    EvictPlan p;
+    p.head = reinterpret_cast<int32_t*>(w);
+    w += align256(n * 16);
+    p.from = reinterpret_cast<int32_t*>(w);
+    w += align256(n * cap * 4);
+    p.weights = reinterpret_cast<float*>(w);
+    w += align256(n * cap * 4);
+    p.pages = reinterpret_cast<int32_t*>(w);
+    return p;
+}
+
+// Order of weights as order of unsigned numbers; both zeros alike, NaN below everything.
+__device__ __forceinline__ uint32_t weight_key(float w)
+{
+    if (w != w) return 0;
+    const uint32_t u = __float_as_uint(w + 0.0f);
+    return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+// Exclusive prefix sums of two counts over the CTA; every thread calls it.
+__device__ __forceinline__ int2 block_exclusive2(int2 x, int2* sums /* shared, 32 */, int2* total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int2 inc = x;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int a = __shfl_up_sync(0xffffffffu, inc.x, d), b = __shfl_up_sync(0xffffffffu, inc.y, d);
+        if (lane >= d) { inc.x += a; inc.y += b; }
+    }
+    __syncthreads();
+    if (lane == 31) sums[warp] = inc;
+    __syncthreads();
+    if (warp == 0) {
+        int2 s = sums[lane];
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int a = __shfl_up_sync(0xffffffffu, s.x, d), b = __shfl_up_sync(0xffffffffu, s.y, d);
+            if (lane >= d) { s.x += a; s.y += b; }
+        }
+        sums[lane] = s;
+    }
+    __syncthreads();
+    *total = sums[31];
+    const int2 before = warp ? sums[warp - 1] : make_int2(0, 0);
+    return make_int2(inc.x - x.x + before.x, inc.y - x.y + before.y);
+}
+
+__global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const polyspec_cache_pages s, const int32_t* budgets, int first, int recent,
+                                                                         float* weights, EvictPlan plan, int32_t* kept_from, int32_t* status)
+{
+    __shared__ int hist[256];
+    __shared__ int2 sums[32];
+    __shared__ uint32_t prefix;
+    __shared__ int left, first_moved, shared_page;
+    const int b = blockIdx.x, tid = threadIdx.x;
+    const size_t cap = static_cast<size_t>(s.max_pages) * s.page_tokens;
+    float* w = weights + b * cap;
+    int32_t* row = s.table + static_cast<size_t>(b) * s.max_pages;
+    int32_t* from = plan.from + b * cap;
+    wait_for_stream();
+    const int len = s.len[b], budget = budgets[b];
+    if (tid == 0) { plan.head[4 * b] = 0; plan.head[4 * b + 1] = 0; }
+    bool stays = budget < 0 || len <= budget;
+    if (len < 0 || len > static_cast<long long>(cap) || (!stays && budget < static_cast<long long>(first) + recent)) {
+        if (tid == 0) kv::report(status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
+        stays = true;
+    }
+    if (kept_from)
+        for (size_t i = tid; i < cap; i += kSelectThreads) kept_from[b * cap + i] = -1;
+    if (stays) return;
+
+    // of the slots first .. len - recent - 1 the `need` heaviest stay
+    const int end = len - recent, need = budget - first - recent;
+    uint32_t bits = 0;                          // the leading bits of the last one's weight, as far as they are known
+    int ties = need;                            // how many of equal leading bits stay
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (tid < 256) hist[tid] = 0;
+        __syncthreads();
+        for (int i = first + tid; i < end; i += kSelectThreads) {
+            const uint32_t key = weight_key(w[i]);
+            if (shift == 24 || key >> (shift + 8) == bits) {
+                // (weights of one size share their leading bits: one add per warp and digit)
+                const uint32_t digit = key >> shift & 255u, peers = __match_any_sync(__activemask(), digit);
+                if ((tid & 31) == __ffs(peers) - 1) atomicAdd(&hist[digit], __popc(peers));
+            }
+        }
+        __syncthreads();
+        if (tid < 32) {                         // from the top digit down, eight digits a lane
+            int sum = 0;
+            for (int d = 0; d < 8; ++d) sum += hist[255 - tid * 8 - d];
+            int inc = sum;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, inc, d);
+                if (tid >= d) inc += y;
+            }
+            int above = inc - sum;
+            if (above < ties && ties <= inc) {
+                int d = 255 - tid * 8;
+                while (above + hist[d] < ties) above += hist[d--];
+                prefix = bits << 8 | d;
+                left = ties - above;
+            }
+            if (tid == 0 && ties == 0) { prefix = 0xffffffffu; left = 0; }
+        }
+        __syncthreads();
+        if (ties == 0) { bits = 0xffffffffu; break; }
+        bits = prefix;
+        ties = left;
+    }
+    // (with none to keep, no key is above ~0, which no number has)
+
+    // slots in order, a run per thread: above the last one's weight, and equal to it
+    const int per = (len + kSelectThreads - 1) / kSelectThreads;
+    const int i0 = min(len, tid * per), i1 = min(len, i0 + per);
+    auto state = [&](int i) {                   // 2 stays, 1 equal, 0 goes
+        if (i < first || i >= end) return 2;
+        const uint32_t key = weight_key(w[i]);
+        return key > bits ? 2 : key == bits && need > 0 ? 1 : 0;
+    };
+    int2 mine = make_int2(0, 0), total;
+    for (int i = i0; i < i1; ++i) {
+        const int st = state(i);
+        mine.x += st == 2;
+        mine.y += st == 1;
+    }
+    if (tid == 0) { first_moved = budget; shared_page = 0; }
+    const int2 before = block_exclusive2(mine, sums, &total);
+    int equal = before.y, at = before.x + min(before.y, ties);
+    int moved = budget;
+    for (int i = i0; i < i1; ++i) {
+        const int st = state(i);
+        if (st == 2 || (st == 1 && equal < ties)) {
+            if (at < budget) {
+                from[at] = i;
+                plan.weights[b * cap + at] = w[i];
+                if (at != i) moved = min(moved, at);
+            }
+            ++at;
+        }
+        equal += st == 1;
+    }
+    if (moved < budget) atomicMin(&first_moved, moved);
+    __syncthreads();
+
+    // nobody else may hold a page that changes; pages wholly behind what stays only lose this sequence's hold
+    const int P = s.page_tokens, keep_pages = (budget + P - 1) / P, held = (len + P - 1) / P;
+    for (int i = tid; i < held; i += kSelectThreads) {
+        const int page = row[i];
+        const bool there = page >= 0 && page < s.n_pages;
+        if (!there || (i >= first_moved / P && i < keep_pages && s.refs[page] > 1)) shared_page = 1;
+        plan.pages[static_cast<size_t>(b) * s.max_pages + i] = page;
+    }
+    __syncthreads();
+    if (shared_page) {
+        if (tid == 0) kv::report(status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
+        return;
+    }
+    for (int i = first_moved + tid; i < budget; i += kSelectThreads) w[i] = plan.weights[b * cap + i];
+    if (kept_from)
+        for (int i = tid; i < budget; i += kSelectThreads) kept_from[b * cap + i] = from[i];
+    for (int i = keep_pages + tid; i < held; i += kSelectThreads) {
+        const int page = row[i];
+        const int was = atomicSub(&s.refs[page], 1);
+        if (was == 1) atomicOr(&s.free_bits[page >> 5], 1u << (page & 31));
+        else if (was <= 0) { atomicAdd(&s.refs[page], 1); kv::report(status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE); }
+        row[i] = -1;
+    }
+    if (tid == 0) {
+        s.len[b] = budget;
+        plan.head[4 * b] = first_moved;
+        plan.head[4 * b + 1] = budget;
+    }
+}
+
+// D: head_dim.  blockIdx.x: head and plane, blockIdx.y: sequence.
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec_cache_pages s, EvictPlan plan, unsigned char* pool, size_t page_bytes,
+                                                                  int kv_heads)
+{
+    constexpr int kBatch = kMoveThreads;        // tokens at a time
+    constexpr int kPieces = D / 32;             // 16-byte pieces of a token's codes
+    const int b = blockIdx.y, plane = blockIdx.x / kv_heads, head = blockIdx.x % kv_heads, tid = threadIdx.x;
+    const bool values = plane & 1;
+    const int P = s.page_tokens, units = P / kv::kUnit;
+    const size_t cap = static_cast<size_t>(s.max_pages) * P;
+    const int32_t* from = plan.from + b * cap;
+    const int32_t* pages = plan.pages + static_cast<size_t>(b) * s.max_pages;
+    unsigned char* data = pool + static_cast<size_t>(plane) * s.n_pages * page_bytes;
+    wait_for_stream();
+    const int begin = plan.head[4 * b], end = plan.head[4 * b + 1];
+    auto unit_of = [&](int slot) {
+        return data + pages[slot / P] * page_bytes + static_cast<size_t>(head * units + slot % P / kv::kUnit) * kv::unit_bytes(D);
+    };
+    for (int i0 = begin; i0 < end; i0 += kBatch) {
+        const int n = min(kBatch, end - i0);
+        if (!values) {
+            uint4 x[kPieces];
+            uint32_t pair = 0;
+#pragma unroll
+            for (int u = 0; u < kPieces; ++u) {
+                const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
+                if (t < n) {
+                    const int slot = from[i0 + t];
+                    x[u] = reinterpret_cast<const uint4*>(unit_of(slot))[slot % kv::kUnit * kPieces + part];
+                }
+            }
+            if (tid < n) {
+                const int slot = from[i0 + tid];
+                pair = reinterpret_cast<const uint32_t*>(unit_of(slot))[D + slot % kv::kUnit];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < kPieces; ++u) {
+                const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
+                if (t < n) reinterpret_cast<uint4*>(unit_of(i0 + t))[(i0 + t) % kv::kUnit * kPieces + part] = x[u];
+            }
+            if (tid < n) reinterpret_cast<uint32_t*>(unit_of(i0 + tid))[D + (i0 + tid) % kv::kUnit] = pair;
+        } else {
+            // the D / 64 words of one group of lanes: (8 h + g, token) for all h
+            using Piece = typename std::conditional<D == 128, uint2, uint32_t>::type;
+            Piece x[8];
+            uint32_t pair = 0;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int item = u * kMoveThreads + tid, t = item / 8, g = item % 8;
+                if (t < n) {
+                    const int slot = from[i0 + t];
+                    x[u] = reinterpret_cast<const Piece*>(unit_of(slot))[8 * g + slot % kv::kUnit];
+                }
+            }
+            if (tid < n) {
+                const int slot = from[i0 + tid];
+                pair = reinterpret_cast<const uint32_t*>(unit_of(slot))[D + slot % kv::kUnit];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int item = u * kMoveThreads + tid, t = item / 8, g = item % 8;
+                if (t < n) reinterpret_cast<Piece*>(unit_of(i0 + t))[8 * g + (i0 + t) % kv::kUnit] = x[u];
+            }
+            if (tid < n) reinterpret_cast<uint32_t*>(unit_of(i0 + tid))[D + (i0 + tid) % kv::kUnit] = pair;
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace
+}  // namespace polyspec
+
+using namespace polyspec;
+
+extern "C" {
+
+polyspec_status polyspec_cache_evict_workspace(int n_seqs, int max_pages, int page_tokens, size_t* bytes)
+{
+    if (!bytes || n_seqs < 1 || max_pages < 1 || page_tokens < 1) return POLYSPEC_ERR_INVALID_ARG;
+    if (static_cast<long long>(max_pages) * page_tokens > 0x7fffffffLL) return POLYSPEC_ERR_UNSUPPORTED;
+    *bytes = evict_bytes(n_seqs, max_pages, page_tokens);
+    return POLYSPEC_OK;
+}
+
+polyspec_status polyspec_cache_evict(const polyspec_cache_pages* s, const int32_t* budget, int first, int recent, float* weights, void* pool,
+                                     int n_planes, int kv_heads, int head_dim, int32_t* kept_from, int32_t* device_status, void* workspace,
+                                     size_t workspace_bytes, void* cuda_stream)
+{
+    polyspec_status st = kv::check_state(s);
+    if (st == POLYSPEC_OK) st = kv::check_heads(kv_heads, kv_heads, head_dim);
+    if (st != POLYSPEC_OK) return st;
+    if (!budget || first < 0 || recent < 0 || !weights || !pool || !kv::aligned16(pool) || n_planes < 2 || n_planes % 2) return POLYSPEC_ERR_INVALID_ARG;
+    if (!aligned4(budget, weights, kept_from, device_status)) return POLYSPEC_ERR_INVALID_ARG;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return POLYSPEC_ERR_INVALID_ARG;
+    if (s->n_seqs > 65535 || static_cast<long long>(n_planes) * kv_heads > 0x7fffffffLL) return POLYSPEC_ERR_UNSUPPORTED;
+    if (workspace_bytes < evict_bytes(s->n_seqs, s->max_pages, s->page_tokens)) return POLYSPEC_ERR_WORKSPACE;
+    const EvictPlan plan = evict_plan(workspace, s->n_seqs, s->max_pages, s->page_tokens);
+    cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+    cudaError_t e = launch_early(evict_select_kernel, dim3(static_cast<unsigned>(s->n_seqs)), kSelectThreads, 0, stream, *s, budget, first, recent,
+                                 weights, plan, kept_from, device_status);
+    if (e == cudaSuccess) {
+        const dim3 grid(static_cast<unsigned>(n_planes * kv_heads), static_cast<unsigned>(s->n_seqs));
+        unsigned char* data = static_cast<unsigned char*>(pool);
+        const size_t bytes = kv::page_bytes(*s, kv_heads, head_dim);
+        e = head_dim == 128 ? launch_early(evict_move_kernel<128>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads)
+                            : launch_early(evict_move_kernel<64>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads);
+    }
+    return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
+}
+
+}  // extern "C"
