@@ -543,7 +543,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  * polyspec_prompt_attention -- causal attention over whole prompts, packed one behind the other:
  *     out[i, h] = sum_{j <= i} softmax_j(scale * q[i, h] . k[j, h / (q_heads/kv_heads)]) v[j, .]   i, j rows of one prompt
  *   rows_at [n_seqs + 1]: prompt b is the rows rows_at[b] .. rows_at[b + 1]-1 (none if equal); rows outside all of them are neither read into
- *   a result nor written.  q_heads a multiple of kv_heads; head_dim 64 or 128; scale finite
+ *   a result nor written.  q_heads a multiple of kv_heads; head_dim 64 or 128; 0 <= scale <= 1e30
  *   out [rows, q_heads, head_dim]; lse out [rows, q_heads] fp32 or NULL: the natural logarithm of the softmax's denominator.
  *   Products of bf16, sums and softmax in fp32; weights are rounded to bf16 for their product with the values.  Keys and values behind a
  *   row never reach it, NaN and infinities included.  Row numbers that decrease or lie outside 0 .. rows make the prompt empty

@@ -53,7 +53,7 @@ PROMPT = dict(q=FAKE, q_stride=6144, k=FAKE, k_stride=6144, v=FAKE, v_stride=614
 @pytest.mark.parametrize("change,status", [
     ({"q": None}, INVALID), ({"k": None}, INVALID), ({"v": None}, INVALID), ({"rows_at": None}, INVALID), ({"out": None}, INVALID), ({"out": FAKE + 8}, INVALID),
     ({"v": FAKE + 8}, INVALID), ({"lse": FAKE + 2}, INVALID), ({"n_seqs": 0}, INVALID), ({"rows": 0}, INVALID), ({"q_heads": 0}, INVALID), ({"kv_heads": 0}, INVALID),
-    ({"q_stride": 4095}, INVALID), ({"k_stride": 1020}, INVALID), ({"scale": float("nan")}, INVALID), ({"scale": float("inf")}, INVALID),
+    ({"q_stride": 4095}, INVALID), ({"k_stride": 1020}, INVALID), ({"scale": float("nan")}, INVALID), ({"scale": float("inf")}, INVALID), ({"scale": -0.1}, INVALID),
     ({"kv_heads": 5}, UNSUPPORTED), ({"d": 96}, UNSUPPORTED), ({"d": 256}, UNSUPPORTED), ({"rows": 1 << 25}, UNSUPPORTED), ({"q_heads": 2048, "kv_heads": 2048}, UNSUPPORTED),
     ({"n_seqs": (1 << 20) + 1}, UNSUPPORTED),
 ])
