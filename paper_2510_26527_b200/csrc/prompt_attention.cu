@@ -117,6 +117,32 @@ __device__ __forceinline__ float ex2(float x)
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float x;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(b), "f"(c));
+    return x;
+}
+// Pairs of fp32 numbers in one instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+    return x;
+}
+__device__ __forceinline__ void unpair(uint64_t x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t x;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b)
 {
     uint32_t x;
@@ -156,7 +182,7 @@ struct Ring {
 template <class S>
 struct Bars {
     static constexpr int kFull = 0, kEmpty = kFull + S::STAGES, kClean = kEmpty + S::STAGES, kQFull = kClean + S::STAGES, kQEmpty = kQFull + 2,
-                         kSFull = kQEmpty + 1, kPReady = kSFull + 2, kOFull = kPReady + 2, kItemFull = kOFull + 2, kItemEmpty = kItemFull + kSlots,
+                         kSFull = kQEmpty + 1, kPReady = kSFull + 2, kPHalf = kPReady + 2, kOFull = kPHalf + 2, kItemFull = kOFull + 2, kItemEmpty = kItemFull + kSlots,
                          kCount = kItemEmpty + kSlots;
 };
 
@@ -226,7 +252,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     if (threadIdx.x == 0) {
         abort_flag = 0;
         for (int i = 0; i < B::kCount; ++i) {
-            const bool empty = i >= B::kEmpty && i < B::kEmpty + NS, ready = i >= B::kPReady && i < B::kPReady + 2;
+            const bool empty = i >= B::kEmpty && i < B::kEmpty + NS, ready = i >= B::kPReady && i < B::kPHalf + 2;
             mbar_init(bar(i), i >= B::kItemEmpty ? 11 : empty ? 2 : ready ? 4 : 1);
         }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -244,7 +270,6 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
     bool ok = true;
     Ring slot;                                                  // of the item at hand
     wait_for_stream();
-
     // the next item for everyone but the scheduler
     auto take = [&](Item* it) {
         if (!warp_wait(bar(B::kItemFull + slot.at), slot.phase, abort_p)) return false;
@@ -257,6 +282,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         slot.next(kSlots);
     };
 
+    // 384 threads were launched with 168 registers each; a softmax thread holds a row of 128 scores: 128 * 88 + 256 * 208 = 384 * 168
+    if (warp < 4) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 0) {
         // ------------------------------------------------------------------ TMA producer
         Ring st;
@@ -327,12 +355,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             }
         };
         // O of tile `which` += P V with the values in `stage`: 64-element columns of values lie a box apart, groups of 8 keys 1024 bytes
-        auto product_o = [&](int which, uint32_t stage, bool first) {
+        auto product_o = [&](int which, uint32_t stage, bool first, int half) {
             const uint32_t addr = ring_tiles + stage * S::TILE;
             const uint32_t b = ((addr & 0x3ffffu) >> 4) | (S::BOX >> 4 << 16);
 #pragma unroll
-            for (int k = 0; k < kTileRows / 16; ++k)
+            for (int i = 0; i < kTileRows / 32; ++i) {
+                const int k = half * (kTileRows / 32) + i;
                 umma_ts(tmem_o + which * 128, tmem + which * kTileRows + k * 8, b + k * (2048 >> 4), S::IDESC_O, !first || k != 0);
+            }
         };
         while (ok) {
             if (!take(&it)) { ok = false; break; }
@@ -381,13 +411,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                     const int mine = which ? steps_b : steps_a;
                     const bool live = j < mine;
                     if (live) {
+                        if (!wait(B::kPHalf + which, p_phase[which])) break;
+                        tc_fence_after();
+                        if (elect_one()) product_o(which, v_stage, j == 0, 0);
+                        __syncwarp();
                         if (!wait(B::kPReady + which, p_phase[which])) break;
                         p_phase[which] ^= 1u;
                         tc_fence_after();
                     }
                     if (elect_one()) {
                         if (live) {
-                            product_o(which, v_stage, j == 0);
+                            product_o(which, v_stage, j == 0, 1);
                             if (j + 1 == mine) umma_commit(bar(B::kOFull + which));
                         }
                         if (which == 1) umma_commit(bar(B::kEmpty + v_stage));
@@ -419,7 +453,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
         }
         most = __reduce_max_sync(0xffffffffu, most);
         Cursor c = {most - 1, 0};
-        for (int n = blockIdx.x;; n += gridDim.x) {
+        // to and fro over the CTAs, so that none gets the longest item of every round
+        for (int round = 0;; ++round) {
+            const int n = round * gridDim.x + (round & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
             const int2 t = find_tile(p, c, n / p.pairs, lane);
             Item it = {0, 0, 0, 0, 0, 0, 0, 0, 0};
             if (t.x >= 0) {
@@ -451,7 +487,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             if (t.x < 0) break;
         }
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
-    } else if (warp == 3) {
+    } else {
         // ------------------------------------------------------------------ values that are not finite
         Ring st, clean;
         Item it;
@@ -501,7 +537,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
             if (ok) give_back();
         }
         if (!ok && lane == 0) raise_abort(&abort_flag, p.status);
+    }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         // ------------------------------------------------------------------ softmax and epilogue
         const int which = (warp - 4) >> 2, quarter = warp & 3, r = quarter * 32 + lane;
         const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
@@ -529,8 +567,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                 }
                 float top[4] = {s[0], s[1], s[2], s[3]};
 #pragma unroll
-                for (int i = 4; i < kTileRows; ++i) top[i & 3] = fmaxf(top[i & 3], s[i]);
-                const float most = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+                for (int i = 4; i + 1 < kTileRows; i += 2) top[i >> 1 & 3] = max3(top[i >> 1 & 3], s[i], s[i + 1]);
+                const float most = fmaxf(max3(top[0], top[1], top[2]), top[3]);
                 if (j == 0) m = most;
                 else if (__any_sync(0xffffffffu, (most - m) * c > kSlack)) {
                     const float to = fmaxf(m, most), by = to == m ? 1.0f : ex2((m - to) * c);
@@ -547,24 +585,32 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                     }
                 }
                 const float mc = m == -INFINITY ? 0.0f : m * c;
-                float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                const uint64_t c2 = pair(c, c), mc2 = pair(-mc, -mc);
+                uint64_t sum0 = 0, sum1 = 0;                    // two pairs of zeros
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     uint32_t x[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        const float a = ex2(fmaf(s[64 * h + 2 * i], c, -mc)), b = ex2(fmaf(s[64 * h + 2 * i + 1], c, -mc));
-                        sum[(2 * i) & 3] += a;
-                        sum[(2 * i + 1) & 3] += b;
+                        float a, b;
+                        unpair(fma2(pair(s[64 * h + 2 * i], s[64 * h + 2 * i + 1]), c2, mc2), &a, &b);
+                        a = ex2(a);
+                        b = ex2(b);
+                        if (i & 1) sum1 = add2(sum1, pair(a, b));
+                        else sum0 = add2(sum0, pair(a, b));
                         x[i] = pack_bf16(a, b);
                     }
                     tmem_st32(s_at + 32 * h, x);
+                    tmem_st_wait();
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_local(bar((h ? B::kPReady : B::kPHalf) + which));
                 }
-                l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
-                tmem_st_wait();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive_local(bar(B::kPReady + which));
+                {
+                    float a, b;
+                    unpair(add2(sum0, sum1), &a, &b);
+                    l += a + b;
+                }
             }
             if (!ok) break;
             if (steps) {
