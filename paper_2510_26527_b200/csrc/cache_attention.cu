@@ -14,19 +14,27 @@
 // where pairs of tokens have to be brought together (values).  Queries are scaled by a power of two into fp16's upper range, where their
 // bf16 digits are exact down to 2^-28 of the block's largest.
 //
-// mma.sync on 16 rows: a block's rows times the heads that share a key head, 4 to 36 of them, fill a tile; tcgen05's tiles of 128
-// rows would be mostly empty, and its operands would have to be expanded through shared or tensor memory.
+// mma.sync with tokens and elements as the 16 rows of its A operand and the block's rows as its 8 columns: a block's rows times the heads that
+// share a key head are 4 to 36, so the columns are well filled, a lane has the scales of two tokens only, and softmax weights change from the first
+// product's layout to the second's with one movmatrix per 8 x 8.  (tcgen05's tiles of 128 rows would be mostly empty, and its operands would have to
+// be expanded through shared or tensor memory.)
 //
 // Work: (sequence, key head, row tile) are segments of `steps` of 16 tokens per warp; the steps of all segments, one after the other, are cut into equal
-// shares, one per CTA, whatever the lengths.  Each warp streams its tiles through a ring of its own (cp.async) and keeps maximum,
-// sums and the output tile in registers; a segment's warps meet once at its end.  A segment that crosses CTAs leaves partial
+// shares, one per CTA, whatever the lengths.  Each warp streams its tiles through a ring of its own (bulk copies, one or two units at a time) and keeps
+// maximum, sums and the output tile in registers; a segment's warps meet once at its end.  A segment that crosses CTAs leaves partial
 // results, which a second kernel joins.
 #include <cuda_fp16.h>
 
 #include "kv_pages.cuh"
+#include "tensor_device.cuh"
 
 namespace polyspec {
 namespace {
+
+using tensordev::mbar_expect_tx;
+using tensordev::mbar_init;
+using tensordev::mbar_try;
+using tensordev::smem_addr;
 
 constexpr int kMaxCtas = 304;                   // CTAs that the workspace has room for
 constexpr float kNone = -3.0e38f;               // a maximum over nothing
@@ -46,7 +54,7 @@ struct AttendParams {
     unsigned short* out;
     float* lse;
     float* partial;                             // [2 * CTAs][rows of a tile][head_dim + 2]
-    int4* joins;                                // [CTAs]: (parts, sequence, key head, row tile) of the segment that begins there and ends elsewhere
+    int4* joins;                                // [CTAs]: (parts, sequence * 64 + row groups, key head, first row) of the segment that begins there and ends elsewhere
     int32_t* status;
 };
 
@@ -59,13 +67,13 @@ __device__ __forceinline__ float ex2(float x)
 __device__ __forceinline__ float lg2(float x)
 {
     float y;
-    asm("lg2.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ float rcp(float x)
 {
     float y;
-    asm("rcp.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t half2_bits(float a, float b)
@@ -91,35 +99,36 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
 // Pair i (0..3) of a word's codes as two fp16 numbers: elements 2i, 2i+1 for keys.  Odd pairs come 16-fold.
 __device__ __forceinline__ uint32_t code_pair(uint32_t word, int i) { return (i >= 2 ? word >> 8 : word) & (i & 1 ? 0x00f000f0u : 0x000f000fu); }
 
-__device__ __forceinline__ void copy16(uint32_t to, const void* from, bool there)
+// The 8 x 8 matrix of 16-bit numbers whose rows the lanes hold in pairs, transposed.
+__device__ __forceinline__ uint32_t transpose(uint32_t x)
 {
-    const int n = there ? 16 : 0;               // 0: the piece is filled with zeros, nothing is read
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(from), "r"(n) : "memory");
+    uint32_t y;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
-__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void copy_bulk(uint32_t to, const void* from, uint32_t bytes, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(to), "l"(from), "r"(bytes), "r"(bar) : "memory");
+}
 
-// Rows of a tile as the A operand of the first product.  The element order inside a step of 16 follows the codes' (words are dealt out to lanes
-// whole); elements whose codes come 16-fold are divided by 16.  Thread `item` holds eight elements of one row.
+// Rows of a tile as the B operand of the first product, [8-row groups][D / 16][32 lanes] pairs of words.  The element order inside a step of 16
+// follows the codes' (words are dealt out to lanes whole); elements whose codes come 16-fold are divided by 16.  x: eight elements of row r.
 template <int D>
-__device__ __forceinline__ void store_fragment(uint32_t* frag /* [tiles][D / 16][32][4] */, int r, int word, const float* x, float by)
+__device__ __forceinline__ void store_fragment(uint32_t* frag, int r, int word, const float* x, float by)
 {
     constexpr int kWords = D / 32;              // words of a token per lane
-    const int t = word / kWords, w = word % kWords, lane = (r & 7) * 4 + t, reg = (r >> 3) & 1;
-    uint32_t* to = frag + (((r >> 4) * (D / 16) + 2 * w) * 32 + lane) * 4 + reg;
+    const int t = word / kWords, w = word % kWords, lane = (r & 7) * 4 + t;
+    uint2* to = reinterpret_cast<uint2*>(frag) + ((r >> 3) * (D / 16) + 2 * w) * 32 + lane;
     const float by16 = by * 0.0625f;
-    to[0] = half2_bits(x[0] * by, x[1] * by);
-    to[2] = half2_bits(x[2] * by16, x[3] * by16);
-    to[128] = half2_bits(x[4] * by, x[5] * by);
-    to[130] = half2_bits(x[6] * by16, x[7] * by16);
+    to[0] = make_uint2(half2_bits(x[0] * by, x[1] * by), half2_bits(x[2] * by16, x[3] * by16));
+    to[32] = make_uint2(half2_bits(x[4] * by, x[5] * by), half2_bits(x[6] * by16, x[7] * by16));
 }
 
-// The rows of a tile into shared memory, by all THREADS of a CTA.  Row r of a tile is row (tile * ROWS + r) / group of the block, head
-// kv_head * group + (tile * ROWS + r) % group.  sums[r] = scale * log2(e) * sum of the row; *factor = what a product of fragments and codes
-// is multiplied with.  Ends with the CTA in step.
+// The rows of a tile into shared memory, by all THREADS of a CTA: rows row0 .. row0 + ROWS - 1 of (row of the block, head of the group), zeros from
+// `end` on.  sums[r] = scale * log2(e) * sum of the row; *factor = what a product of fragments and codes is multiplied with.  Ends with the CTA in step.
 template <int D, int ROWS, int THREADS>
-__device__ __forceinline__ void load_rows(const AttendParams& p, const kv::SeqRows& q, int kv_head, int tile, uint32_t* frag, float* sums, float* warp_max,
-                                          float* factor)
+__device__ __forceinline__ void load_rows(const AttendParams& p, const kv::SeqRows& q, int kv_head, int row0, int end, uint32_t* frag, float* sums,
+                                          float* warp_max, float* factor)
 {
     constexpr int kVecs = D / 8, kItems = ROWS * kVecs, kPer = (kItems + THREADS - 1) / THREADS;
     static_assert(kItems % THREADS == 0 || (kPer == 1 && kItems % 32 == 0), "whole warps take part or none");
@@ -127,9 +136,9 @@ __device__ __forceinline__ void load_rows(const AttendParams& p, const kv::SeqRo
     float top = 0.0f;
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
-        const int item = u * THREADS + threadIdx.x, r = tile * ROWS + item / kVecs, i = r / p.group;
+        const int item = u * THREADS + threadIdx.x, r = row0 + item / kVecs, i = r / p.group;
         raw[u] = make_uint4(0, 0, 0, 0);
-        if (item < kItems && i < q.n) raw[u] = *reinterpret_cast<const uint4*>(p.q + (q.row0 + i) * p.q_stride + (kv_head * p.group + r % p.group) * D + item % kVecs * 8);
+        if (item < kItems && r < end) raw[u] = *reinterpret_cast<const uint4*>(p.q + (q.row0 + i) * p.q_stride + (kv_head * p.group + r % p.group) * D + item % kVecs * 8);
         const uint32_t* x = reinterpret_cast<const uint32_t*>(&raw[u]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -164,27 +173,31 @@ __device__ __forceinline__ void load_rows(const AttendParams& p, const kv::SeqRo
     __syncthreads();
 }
 
-// What a CTA's share of the steps is, and where in it a cursor stands.
-struct Segment { int b, head, tile, tiles, steps; kv::SeqRows q; };
+// A segment, and where in the list of them a cursor stands: row tile `tile` of `tiles` with tile_rows rows each (a multiple of 8; rows times heads of the
+// group are dealt out evenly), `steps` steps over the tokens.
+struct Segment { int b, head, tile, tiles, tile_rows, steps; kv::SeqRows q; };
 
 template <int ROWS, int STEP>
 __device__ __forceinline__ void seq_segments(const AttendParams& p, Segment& g)
 {
-    g.tiles = (g.q.n * p.group + ROWS - 1) / ROWS;
+    const int groups = (g.q.n * p.group + 7) / 8;
+    g.tiles = (groups + ROWS / 8 - 1) / (ROWS / 8);
+    g.tile_rows = g.tiles ? (groups + g.tiles - 1) / g.tiles * 8 : 8;
     g.steps = max(1, (g.q.base + g.q.granted + STEP - 1) / STEP);
 }
 
 // Slots that row i of a block attends to: up to its own, none if that was not granted.
 __device__ __forceinline__ int row_limit(const kv::SeqRows& q, int i) { return i < q.granted ? q.base + i + 1 : 0; }
 
-template <int D_, int MT_, int WARPS_, int STAGES_, int CTAS_>
+// NT: groups of 8 rows in a tile.
+template <int D_, int NT_, int WARPS_, int STAGES_, int CTAS_>
 struct Shape {
-    static constexpr int D = D_, MT = MT_, WARPS = WARPS_, STAGES = STAGES_, CTAS = CTAS_;
-    static constexpr int THREADS = WARPS * 32, ROWS = MT * 16, STEP = WARPS * 16;       // STEP: tokens
-    static constexpr int UB = kv::unit_bytes(D), STAGE = 4 * UB;
-    static constexpr int FRAG = MT * (D / 16) * 512;                                    // bytes
+    static constexpr int D = D_, NT = NT_, WARPS = WARPS_, STAGES = STAGES_, CTAS = CTAS_;
+    static constexpr int THREADS = WARPS * 32, ROWS = NT * 8, STEP = WARPS * 16;        // STEP: tokens
+    static constexpr int UB = kv::unit_bytes(D), STAGE = 4 * UB, M = D / 16;            // M: 16-element groups of the output
+    static constexpr int FRAG = NT * (D / 16) * 256;                                    // bytes
     static constexpr int RING = WARPS * STAGES * STAGE;
-    static constexpr int MERGE = WARPS / 2 * MT * (D / 8) * 512;
+    static constexpr int MERGE = WARPS / 2 * NT * M * 512;
     static constexpr size_t SMEM = FRAG + RING + MERGE;
     static constexpr int PART = ROWS * (D + 2);                                         // floats of a partial result
     static_assert(SMEM * CTAS <= 220 * 1024, "shared memory");
@@ -240,17 +253,16 @@ __device__ __forceinline__ void next_segment(const AttendParams& p, Segment& g)
     if (++g.head < p.kv_heads) return;
     g.head = 0;
     do {
-        if (++g.b >= p.s.n_seqs) { g.tiles = 0; g.steps = 0x7fffffff; g.q = kv::SeqRows{0, 0, 0, 0, 0, false}; return; }
+        if (++g.b >= p.s.n_seqs) { g.tiles = 0; g.tile_rows = 8; g.steps = 0x7fffffff; g.q = kv::SeqRows{0, 0, 0, 0, 0, false}; return; }
         g.q = kv::seq_rows(p.s, p.r, g.b);
         seq_segments<S::ROWS, S::STEP>(p, g);
     } while (g.tiles == 0);
 }
 
 // Tokens that some row of the segment attends to.
-template <class S>
 __device__ __forceinline__ int visible(const AttendParams& p, const Segment& g)
 {
-    const int first = g.tile * S::ROWS / p.group, last = min(g.q.n - 1, (g.tile * S::ROWS + S::ROWS - 1) / p.group);
+    const int first = g.tile * g.tile_rows / p.group, last = min(g.q.n - 1, (g.tile * g.tile_rows + g.tile_rows - 1) / p.group);
     return first < g.q.granted ? row_limit(g.q, min(last, g.q.granted - 1)) : 0;
 }
 
@@ -272,19 +284,180 @@ __device__ __forceinline__ void store_out(const AttendParams& p, const kv::SeqRo
     if (d0 == 0 && p.lse) p.lse[at] = none ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
 }
 
+// What a warp keeps of its tile: output (elements x rows, in the codes' form), per row the reference of the exponentials (a maximum less kLift), the sums of
+// p and of p vo.  NT groups of 8 rows; a lane has rows 2 t4 and 2 t4 + 1 of each.
+template <class S>
+struct Running { float o[S::NT][S::M][4], ref[S::NT][2], l[S::NT][2], lo[S::NT][2]; bool started; };
+
+// 16 tokens, of which the stage at `at` has keys and values, for the first L groups of rows.  masked: some row does not see some token, or a unit could not be
+// read (bad).  q0: the rows' fragments where they stay in registers (one group).
+template <class S, int L>
+__device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>& run, const unsigned char* at, const uint32_t* frag, const uint2* q0, const float* sums,
+                                              float factor, bool masked, uint32_t bad, int key0, const Segment& seg, int lane)
+{
+    constexpr int D = S::D, KS = D / 16, M = S::M, UB = S::UB, WORDS = D / 32, H = D / 64;
+    const int g8 = lane >> 2, t4 = lane & 3;
+    // codes of keys, and the first product: tokens x rows
+    uint32_t kw[2][WORDS];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        if (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(at + u * UB + lane * 16);
+            kw[u][0] = x.x; kw[u][1] = x.y; kw[u][WORDS - 2] = x.z; kw[u][WORDS - 1] = x.w;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(at + u * UB + lane * 8);
+            kw[u][0] = x.x; kw[u][1] = x.y;
+        }
+    }
+    float sc[L][4];
+#pragma unroll
+    for (int n = 0; n < L; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+        const uint32_t a0 = code_pair(kw[0][s >> 1], 2 * (s & 1)), a1 = code_pair(kw[1][s >> 1], 2 * (s & 1));
+        const uint32_t a2 = code_pair(kw[0][s >> 1], 2 * (s & 1) + 1), a3 = code_pair(kw[1][s >> 1], 2 * (s & 1) + 1);
+#pragma unroll
+        for (int n = 0; n < L; ++n) {
+            const uint2 b = S::NT == 1 ? q0[S::NT == 1 ? s : 0] : reinterpret_cast<const uint2*>(frag)[(n * KS + s) * 32 + lane];
+            mma(sc[n], a0, a1, a2, a3, b.x, b.y);
+        }
+    }
+    // scales and offsets of the lane's tokens g8 and g8 + 8
+    float ks[2], ko[2], lv[2], iv[2], ov[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        const uint32_t kp = *reinterpret_cast<const uint32_t*>(at + u * UB + 4 * D + g8 * 4);
+        const uint32_t vp = *reinterpret_cast<const uint32_t*>(at + (2 + u) * UB + 4 * D + g8 * 4);
+        ks[u] = low(kp) * factor;
+        ko[u] = high(kp);
+        const float vs = low(vp);
+        lv[u] = lg2(vs);
+        iv[u] = rcp(vs);
+        ov[u] = high(vp) * iv[u];
+    }
+    // exponents, less the references
+    float most = -INFINITY;
+#pragma unroll
+    for (int n = 0; n < L; ++n) {
+        const float2 sq = *reinterpret_cast<const float2*>(&sums[n * 8 + 2 * t4]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            sc[n][2 * u] = fmaf(sc[n][2 * u], ks[u], fmaf(sq.x, ko[u], lv[u]) - run.ref[n][0]);
+            sc[n][2 * u + 1] = fmaf(sc[n][2 * u + 1], ks[u], fmaf(sq.y, ko[u], lv[u]) - run.ref[n][1]);
+        }
+    }
+    uint32_t hidden = 0;                        // bit 4 n + 2 u + j
+    if (masked) {
+#pragma unroll
+        for (int n = 0; n < L; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int limit = row_limit(seg.q, (seg.tile * seg.tile_rows + n * 8 + 2 * t4 + j) / p.group);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    if (key0 + 8 * u + g8 >= limit || (bad >> u & 1u)) {
+                        hidden |= 1u << (4 * n + 2 * u + j);
+                        sc[n][2 * u + j] = -INFINITY;
+                    }
+            }
+    }
+#pragma unroll
+    for (int n = 0; n < L; ++n) most = fmaxf(most, fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])));
+    // the first tokens set the references; after that sums are rescaled only when a maximum has risen by 2^8 since the last time
+    if (__any_sync(0xffffffffu, !run.started || most > kLift + kSlack)) {
+        const bool first = !run.started;
+#pragma unroll
+        for (int n = 0; n < L; ++n)
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float top = fmaxf(sc[n][j], sc[n][2 + j]);
+#pragma unroll
+                for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                // (a row that sees none of its warp's first tokens sees none of the later ones either)
+                const float up = first ? (top == -INFINITY ? 0.0f : top - kLift) : fmaxf(top - kLift, 0.0f), by = first ? 1.0f : ex2(-up);
+                sc[n][j] -= up;
+                sc[n][2 + j] -= up;
+                run.ref[n][j] += up;
+                run.l[n][j] *= by;
+                run.lo[n][j] *= by;
+#pragma unroll
+                for (int i = 0; i < M; ++i) { run.o[n][i][j] *= by; run.o[n][i][2 + j] *= by; }
+            }
+        run.started = true;
+    }
+    uint32_t pr[L][2];
+#pragma unroll
+    for (int n = 0; n < L; ++n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[n][i] = ex2(sc[n][i]);
+        pr[n][0] = transpose(half2_bits(sc[n][0], sc[n][1]));
+        pr[n][1] = transpose(half2_bits(sc[n][2], sc[n][3]));
+    }
+    if (!masked) {
+#pragma unroll
+        for (int n = 0; n < L; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                run.l[n][i & 1] = fmaf(sc[n][i], iv[i >> 1], run.l[n][i & 1]);
+                run.lo[n][i & 1] = fmaf(sc[n][i], ov[i >> 1], run.lo[n][i & 1]);
+            }
+    } else {                                    // scales behind what a row sees may be anything
+#pragma unroll
+        for (int n = 0; n < L; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (!(hidden >> (4 * n + i) & 1u)) {
+                    run.l[n][i & 1] = fmaf(sc[n][i], iv[i >> 1], run.l[n][i & 1]);
+                    run.lo[n][i & 1] = fmaf(sc[n][i], ov[i >> 1], run.lo[n][i & 1]);
+                }
+    }
+    // codes of values: words of tokens 2 t4 and 2 t4 + 1, paired by token, and the second product: elements x rows
+    uint32_t even[2][H], odd[2][H];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+        if (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(at + (2 + u) * UB + lane * 16);
+            even[u][0] = __byte_perm(x.x, x.z, 0x5410); odd[u][0] = __byte_perm(x.x, x.z, 0x7632);
+            even[u][H - 1] = __byte_perm(x.y, x.w, 0x5410); odd[u][H - 1] = __byte_perm(x.y, x.w, 0x7632);
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(at + (2 + u) * UB + lane * 8);
+            even[u][0] = __byte_perm(x.x, x.y, 0x5410); odd[u][0] = __byte_perm(x.x, x.y, 0x7632);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < M; ++i) {
+        // the product's rows: elements 8 g8 + i and 64 + 8 g8 + i, or of narrow heads 8 g8 + i and 8 g8 + 4 + i
+        const int e0 = i, e1 = D == 128 ? i : i + 4, h1 = H - 1;
+        const uint32_t a0 = code_pair(e0 & 1 ? odd[0][0] : even[0][0], e0 >> 1), a1 = code_pair(e1 & 1 ? odd[0][h1] : even[0][h1], e1 >> 1);
+        const uint32_t a2 = code_pair(e0 & 1 ? odd[1][0] : even[1][0], e0 >> 1), a3 = code_pair(e1 & 1 ? odd[1][h1] : even[1][h1], e1 >> 1);
+#pragma unroll
+        for (int n = 0; n < L; ++n) mma(run.o[n][i], a0, a1, a2, a3, pr[n][0], pr[n][1]);
+    }
+}
+
 template <class S>
 __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const AttendParams p)
 {
-    constexpr int D = S::D, MT = S::MT, W = S::WARPS, NS = S::STAGES, KS = D / 16, NT = D / 8, UB = S::UB, WORDS = D / 32, H = D / 64;
+    constexpr int D = S::D, NT = S::NT, W = S::WARPS, NS = S::STAGES, KS = D / 16, M = S::M, UB = S::UB, H = D / 64;
     extern __shared__ __align__(16) unsigned char smem[];
     __shared__ long long warp_sums[W], hit_at;
     __shared__ int hit;
-    __shared__ float warp_max[W], sums[S::ROWS], sm_m[W][S::ROWS], sm_l[W][S::ROWS], sm_o[W][S::ROWS];
+    __shared__ __align__(16) float sums[S::ROWS];            // read in pairs
+    __shared__ float warp_max[W], sm_m[W][S::ROWS], sm_l[W][S::ROWS], sm_o[W][S::ROWS];
+    __shared__ __align__(8) uint64_t barriers[W * NS];
+    __shared__ Segment mine, produced[W];       // the segment at hand; the one that each warp's copies have come to
+    __shared__ int produced_visible[W];
     uint32_t* frag = reinterpret_cast<uint32_t*>(smem);
     float4* merge = reinterpret_cast<float4*>(smem + S::FRAG + S::RING);
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3;
     unsigned char* ring = smem + S::FRAG + warp * NS * S::STAGE;
-    const uint32_t ring_at = static_cast<uint32_t>(__cvta_generic_to_shared(ring));
+    const uint32_t ring_at = smem_addr(ring), bar_at = smem_addr(&barriers[warp * NS]);
+    if (lane == 0) {
+        for (int i = 0; i < NS; ++i) mbar_init(bar_at + 8u * i, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncwarp();
     wait_for_stream();
 
     // this CTA's share [s0, s1) of all steps
@@ -296,18 +469,21 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
     if (blockIdx.x >= ctas) return;
     const long long s0 = total * blockIdx.x / ctas, s1 = total * (blockIdx.x + 1) / ctas;
     locate<S>(p, s0, &seq, &within, warp_sums, &hit, &hit_at);
-    Segment mine;                                // the consumer's
-    mine.b = seq;
-    mine.q = kv::seq_rows(p.s, p.r, seq);
-    seq_segments<S::ROWS, S::STEP>(p, mine);
-    int step = static_cast<int>(within % mine.steps);
+    int step;
     {
-        const int n = static_cast<int>(within / mine.steps);
-        mine.head = n / mine.tiles;
-        mine.tile = n % mine.tiles;
+        Segment g;
+        g.b = seq;
+        g.q = kv::seq_rows(p.s, p.r, seq);
+        seq_segments<S::ROWS, S::STEP>(p, g);
+        step = static_cast<int>(within % g.steps);
+        const int n = static_cast<int>(within / g.steps);
+        g.head = n / g.tiles;
+        g.tile = n % g.tiles;
+        if (threadIdx.x == 0) mine = g;
+        if (lane == 0) { produced[warp] = g; produced_visible[warp] = visible(p, g); }
+        __syncthreads();
     }
-    Segment ahead = mine;                       // the producer's
-    int ahead_step = step, ahead_visible = visible<S>(p, ahead);
+    int ahead_step = step, ahead_steps = mine.steps;
     const int n_steps = static_cast<int>(s1 - s0);
 
     // lane 2k + u: unit u of the warp's k-th tile from here on, as a number of units in a plane, or ~0
@@ -319,7 +495,8 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
         if (unit_k == 16) {
             const long long slot = (static_cast<long long>(ahead_step + (lane >> 1)) * W + warp) * 16 + (lane & 1) * 8;
             unit_numbers = 0xffffffffu;
-            if (slot < ahead_visible) {
+            if (slot < produced_visible[warp]) {
+                const Segment& ahead = produced[warp];
                 const int unit = static_cast<int>(slot >> 3), at = unit / p.units_per_page;
                 const int page = p.s.table[static_cast<size_t>(ahead.b) * p.s.max_pages + at];
                 if (page >= 0 && page < p.s.n_pages)
@@ -329,338 +506,218 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
             }
             unit_k = 0;
         }
-        const uint32_t to = ring_at + stage * S::STAGE;
         const uint32_t u0 = __shfl_sync(0xffffffffu, unit_numbers, 2 * unit_k), u1 = __shfl_sync(0xffffffffu, unit_numbers, 2 * unit_k + 1);
-        const bool there0 = u0 != 0xffffffffu, there1 = u1 != 0xffffffffu;
-        const unsigned char* k0 = p.pool + static_cast<size_t>(there0 ? u0 : 0) * UB;
-        const unsigned char* k1 = p.pool + static_cast<size_t>(there1 ? u1 : 0) * UB;
-        bad_units = (bad_units & ~(3u << (2 * stage))) | ((there0 ? 0u : 1u) | (there1 ? 0u : 2u)) << (2 * stage);
-        if (D == 128) {
-            copy16(to + lane * 16, k0 + lane * 16, there0);
-            copy16(to + UB + lane * 16, k1 + lane * 16, there1);
-            copy16(to + 2 * UB + lane * 16, k0 + p.plane_bytes + lane * 16, there0);
-            copy16(to + 3 * UB + lane * 16, k1 + p.plane_bytes + lane * 16, there1);
-        } else {
-            const int o = (lane & 15) * 16;
-            const unsigned char* k = lane < 16 ? k0 : k1;
-            const bool there = lane < 16 ? there0 : there1;
-            copy16(to + (lane >> 4) * UB + o, k + o, there);
-            copy16(to + (2 + (lane >> 4)) * UB + o, k + p.plane_bytes + o, there);
-        }
-        if (lane < 8) {                         // scales and offsets: two pieces of each unit
-            const int n = lane >> 1, o = 4 * D + (lane & 1) * 16;
-            copy16(to + n * UB + o, (n & 1 ? k1 : k0) + (n >> 1 ? p.plane_bytes : 0) + o, n & 1 ? there1 : there0);
+        const uint32_t there = (u0 != 0xffffffffu ? 1u : 0u) | (u1 != 0xffffffffu ? 2u : 0u);
+        bad_units = (bad_units & ~(3u << (2 * stage))) | (3u ^ there) << (2 * stage);
+        if (lane == 0) {
+            const uint32_t to = ring_at + stage * S::STAGE, bar = bar_at + 8u * stage;
+            const unsigned char* k0 = p.pool + static_cast<size_t>(u0) * UB;
+            mbar_expect_tx(bar, (there == 3u ? 4 : there ? 2 : 0) * UB);
+            if (there == 3u && u1 == u0 + 1) {
+                copy_bulk(to, k0, 2 * UB, bar);
+                copy_bulk(to + 2 * UB, k0 + p.plane_bytes, 2 * UB, bar);
+            } else {
+                if (there & 1u) {
+                    copy_bulk(to, k0, UB, bar);
+                    copy_bulk(to + 2 * UB, k0 + p.plane_bytes, UB, bar);
+                }
+                if (there & 2u) {
+                    const unsigned char* k1 = p.pool + static_cast<size_t>(u1) * UB;
+                    copy_bulk(to + UB, k1, UB, bar);
+                    copy_bulk(to + 3 * UB, k1 + p.plane_bytes, UB, bar);
+                }
+            }
         }
         ++unit_k;
-        if (++ahead_step == ahead.steps) {
-            next_segment<S>(p, ahead);
+        if (++ahead_step == ahead_steps) {
+            __syncwarp();
+            if (lane == 0) {
+                Segment g = produced[warp];
+                next_segment<S>(p, g);
+                produced[warp] = g;
+                produced_visible[warp] = visible(p, g);
+            }
+            __syncwarp();
             ahead_step = 0;
-            ahead_visible = visible<S>(p, ahead);
+            ahead_steps = produced[warp].steps;
             unit_k = 16;
         }
     };
 
     int issued = 0;
-    for (; issued < NS - 1; ++issued) {
-        if (issued < n_steps) issue(issued);
-        copies_end();
-    }
+    for (; issued < NS - 1 && issued < n_steps; ++issued) issue(issued);
 
-    float o[MT][NT][4], m[MT][2], l[MT][2], lo[MT][2];
-    int limit[MT][2];
-    int seen = 0, done = 0, stage = 0;          // done: steps
-    bool from_start = step == 0;
+    Running<S> run;
+    static_assert(NT <= 4, "groups");
+    uint2 q0[NT == 1 ? KS : 1];                 // of a tile of one group of rows the fragments stay in registers
+    int seen = 0, live = 0, done = 0, stage = 0;        // done: steps; live: groups of rows
+    uint32_t phase = 0;
+    bool from_start = step == 0, fresh = true, ok = true;
     float factor = 0.0f;
-    bool fresh = true;
+    int steps = 0, all_see = 0;                 // of the segment; tokens that every row sees
     while (done < n_steps) {
         if (fresh) {
-            load_rows<D, S::ROWS, S::THREADS>(p, mine.q, mine.head, mine.tile, frag, sums, warp_max, &factor);
-            seen = visible<S>(p, mine);
+            __syncthreads();                    // the segment has been written
+            steps = mine.steps;
+            all_see = mine.q.base + 1;
+            const int row0 = mine.tile * mine.tile_rows, end = min(mine.q.n * p.group, row0 + mine.tile_rows);
+            load_rows<D, S::ROWS, S::THREADS>(p, mine.q, mine.head, row0, end, frag, sums, warp_max, &factor);
+            live = (end - row0 + 7) / 8;
+            seen = visible(p, mine);
+            if (NT == 1) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
+                for (int s = 0; s < KS; ++s) q0[NT == 1 ? s : 0] = reinterpret_cast<const uint2*>(frag)[s * 32 + lane];
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const int r = mine.tile * S::ROWS + i * 16 + j * 8 + g8;
-                    limit[i][j] = row_limit(mine.q, r / p.group);
-                    m[i][j] = kNone;
-                    l[i][j] = lo[i][j] = 0.0f;
+                    run.ref[n][j] = 0.0f;
+                    run.l[n][j] = run.lo[n][j] = 0.0f;
                 }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) o[i][n][0] = o[i][n][1] = o[i][n][2] = o[i][n][3] = 0.0f;
+                for (int i = 0; i < M; ++i) run.o[n][i][0] = run.o[n][i][1] = run.o[n][i][2] = run.o[n][i][3] = 0.0f;
             }
+            run.started = false;
             fresh = false;
         }
-        copies_wait<NS - 2>();
-        __syncwarp();
+        if (ok) {                               // a bounded wait, passed or given up by the whole warp
+            uint32_t i = 0;
+            while (i < tensordev::kSpinLimitG && !mbar_try(bar_at + 8u * stage, phase)) ++i;
+            ok = __all_sync(0xffffffffu, i < tensordev::kSpinLimitG);
+        }
         const int key0 = (step * W + warp) * 16;
-        if (key0 < seen) {
+        const uint32_t bad = bad_units >> (2 * stage) & 3u;
+        if (key0 < seen && ok && bad != 3u) {
             const unsigned char* at = ring + stage * S::STAGE;
-            // codes of keys, and the first product
-            uint32_t kw[2][WORDS];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (D == 128) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(at + u * UB + lane * 16);
-                    kw[u][0] = x.x; kw[u][1] = x.y; kw[u][WORDS - 2] = x.z; kw[u][WORDS - 1] = x.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(at + u * UB + lane * 8);
-                    kw[u][0] = x.x; kw[u][1] = x.y;
-                }
-            }
-            float sc[MT][2][4];
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) sc[i][u][0] = sc[i][u][1] = sc[i][u][2] = sc[i][u][3] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                uint32_t b[2][2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    b[u][0] = code_pair(kw[u][s >> 1], 2 * (s & 1));
-                    b[u][1] = code_pair(kw[u][s >> 1], 2 * (s & 1) + 1);
-                }
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const uint4 a = *reinterpret_cast<const uint4*>(frag + ((i * KS + s) * 32 + lane) * 4);
-                    mma(sc[i][0], a.x, a.y, a.z, a.w, b[0][0], b[0][1]);
-                    mma(sc[i][1], a.x, a.y, a.z, a.w, b[1][0], b[1][1]);
-                }
-            }
-            // scales and offsets of the lane's four tokens: 8u + 2 t4 + j
-            float ks[2][2], ko[2][2], lv[2][2], iv[2][2], ov[2][2];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint2 kp = *reinterpret_cast<const uint2*>(at + u * UB + 4 * D + t4 * 8);
-                const uint2 vp = *reinterpret_cast<const uint2*>(at + (2 + u) * UB + 4 * D + t4 * 8);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    ks[u][j] = low(j ? kp.y : kp.x) * factor;
-                    ko[u][j] = high(j ? kp.y : kp.x);
-                    const float vs = low(j ? vp.y : vp.x);
-                    lv[u][j] = lg2(vs);
-                    iv[u][j] = rcp(vs);
-                    ov[u][j] = high(j ? vp.y : vp.x) * iv[u][j];
-                }
-            }
-            // masked: some row does not see some token of the tile, or a page could not be read
-            const uint32_t bad = bad_units >> (2 * stage) & 3u;
-            const bool masked = key0 + 16 > mine.q.base + 1 || bad;
-            uint32_t pr[MT][4];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {                           // rows g8 and g8 + 8
-                    const float sq = sums[i * 16 + j * 8 + g8];
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-                        for (int c = 0; c < 2; ++c)
-                            sc[i][u][2 * j + c] = fmaf(sc[i][u][2 * j + c], ks[u][c], fmaf(sq, ko[u][c], lv[u][c]));
-                    }
-                }
-                uint32_t hidden = 0;                                    // bit 4 u + 2 j + c
-                if (masked) {
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int j = 0; j < 2; ++j)
-#pragma unroll
-                            for (int c = 0; c < 2; ++c)
-                                if (key0 + 8 * u + 2 * t4 + c >= limit[i][j] || (bad >> u & 1u)) {
-                                    hidden |= 1u << (4 * u + 2 * j + c);
-                                    sc[i][u][2 * j + c] = -INFINITY;
-                                }
-                }
-                const float top0 = fmaxf(fmaxf(sc[i][0][0], sc[i][0][1]), fmaxf(sc[i][1][0], sc[i][1][1]));
-                const float top1 = fmaxf(fmaxf(sc[i][0][2], sc[i][0][3]), fmaxf(sc[i][1][2], sc[i][1][3]));
-                // sums are rescaled only when the maximum has risen by 2^8 since the last time
-                if (__any_sync(0xffffffffu, top0 > m[i][0] + kSlack || top1 > m[i][1] + kSlack)) {
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        float top = j ? top1 : top0;
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                        const float to = fmaxf(m[i][j], top), by = ex2(m[i][j] - to);
-                        m[i][j] = to;
-                        l[i][j] *= by;
-                        lo[i][j] *= by;
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) { o[i][n][2 * j] *= by; o[i][n][2 * j + 1] *= by; }
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float ref = m[i][j] - kLift;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) sc[i][u][2 * j + c] = ex2(sc[i][u][2 * j + c] - ref);
-                    if (!masked) {
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int c = 0; c < 2; ++c) {
-                                l[i][j] = fmaf(sc[i][u][2 * j + c], iv[u][c], l[i][j]);
-                                lo[i][j] = fmaf(sc[i][u][2 * j + c], ov[u][c], lo[i][j]);
-                            }
-                    } else {                    // scales behind what a row sees may be anything
-#pragma unroll
-                        for (int u = 0; u < 2; ++u)
-#pragma unroll
-                            for (int c = 0; c < 2; ++c)
-                                if (!(hidden >> (4 * u + 2 * j + c) & 1u)) {
-                                    l[i][j] = fmaf(sc[i][u][2 * j + c], iv[u][c], l[i][j]);
-                                    lo[i][j] = fmaf(sc[i][u][2 * j + c], ov[u][c], lo[i][j]);
-                                }
-                    }
-                }
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    pr[i][2 * u] = half2_bits(sc[i][u][0], sc[i][u][1]);
-                    pr[i][2 * u + 1] = half2_bits(sc[i][u][2], sc[i][u][3]);
-                }
-            }
-            // codes of values: words of the lane's two tokens, paired by token, and the second product
-            uint32_t vw[2][2][H];
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                if (D == 128) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(at + (2 + u) * UB + lane * 16);
-                    vw[u][0][0] = x.x; vw[u][0][H - 1] = x.y; vw[u][1][0] = x.z; vw[u][1][H - 1] = x.w;
-                } else {
-                    const uint2 x = *reinterpret_cast<const uint2*>(at + (2 + u) * UB + lane * 8);
-                    vw[u][0][0] = x.x; vw[u][1][0] = x.y;
-                }
-            }
-#pragma unroll
-            for (int h = 0; h < H; ++h) {
-                uint32_t even[2], odd[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    even[u] = __byte_perm(vw[u][0][h], vw[u][1][h], 0x5410);
-                    odd[u] = __byte_perm(vw[u][0][h], vw[u][1][h], 0x7632);
-                }
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t b0 = code_pair(e & 1 ? odd[0] : even[0], e >> 1), b1 = code_pair(e & 1 ? odd[1] : even[1], e >> 1);
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) mma(o[i][h * 8 + e], pr[i][0], pr[i][1], pr[i][2], pr[i][3], b0, b1);
-                }
-            }
+            const bool masked = key0 + 16 > all_see || bad;
+            // (code of its own for each number of groups: what is not there costs nothing, and what is there is straight-line code)
+            if (NT == 1 || live == 1) attend_tokens<S, 1>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
+            else if (NT == 2 || live == 2) attend_tokens<S, NT < 2 ? 1 : 2>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
+            else if (NT == 3 || live == 3) attend_tokens<S, NT < 3 ? 1 : 3>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
+            else attend_tokens<S, NT < 4 ? 1 : 4>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
         }
         __syncwarp();
         // the stage that was read before this one is free again
-        {
-            const int to = stage == 0 ? NS - 1 : stage - 1;
-            if (issued < n_steps) issue(to);
-            ++issued;
-            copies_end();
-        }
-        stage = stage + 1 == NS ? 0 : stage + 1;
+        if (issued < n_steps && ok) { issue(stage == 0 ? NS - 1 : stage - 1); ++issued; }
+        if (++stage == NS) { stage = 0; phase ^= 1u; }
         ++done;
         ++step;
-        if (step < mine.steps && done < n_steps) continue;
+        if (step < steps && done < n_steps) continue;
 
         // the segment, or this CTA's part of it, is done: its warps meet
-        const bool whole = from_start && step == mine.steps;
+        const bool whole = from_start && step == steps;
+        const int row0 = mine.tile * mine.tile_rows, end = min(mine.q.n * p.group, row0 + mine.tile_rows);
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
 #pragma unroll
-                for (int d = 1; d < 4; d <<= 1) {
-                    l[i][j] += __shfl_xor_sync(0xffffffffu, l[i][j], d);
-                    lo[i][j] += __shfl_xor_sync(0xffffffffu, lo[i][j], d);
+                for (int d = 4; d < 32; d <<= 1) {
+                    run.l[n][j] += __shfl_xor_sync(0xffffffffu, run.l[n][j], d);
+                    run.lo[n][j] += __shfl_xor_sync(0xffffffffu, run.lo[n][j], d);
                 }
-                if (t4 == 0) sm_m[warp][i * 16 + j * 8 + g8] = m[i][j];
+                if (run.l[n][j] == 0.0f) run.ref[n][j] = kNone;         // saw nothing
+                if (g8 == 0) sm_m[warp][n * 8 + 2 * t4 + j] = run.ref[n][j];
             }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int r = i * 16 + j * 8 + g8;
+                const int r = n * 8 + 2 * t4 + j;
                 float top = kNone;
 #pragma unroll
                 for (int w = 0; w < W; ++w) top = fmaxf(top, sm_m[w][r]);
-                const float by = ex2(m[i][j] - top);
-                if (t4 == 0) { sm_l[warp][r] = l[i][j] * by; sm_o[warp][r] = lo[i][j] * by; }
-                m[i][j] = top;
+                const float by = ex2(run.ref[n][j] - top);
+                if (g8 == 0) { sm_l[warp][r] = run.l[n][j] * by; sm_o[warp][r] = run.lo[n][j] * by; }
 #pragma unroll
-                for (int n = 0; n < NT; ++n) { o[i][n][2 * j] *= by; o[i][n][2 * j + 1] *= by; }
+                for (int i = 0; i < M; ++i) { run.o[n][i][j] *= by; run.o[n][i][2 + j] *= by; }
             }
         if (warp >= W / 2) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int n = 0; n < NT; ++n)
-                    merge[(((warp - W / 2) * MT + i) * NT + n) * 32 + lane] = make_float4(o[i][n][0], o[i][n][1], o[i][n][2], o[i][n][3]);
+                for (int i = 0; i < M; ++i)
+                    merge[(((warp - W / 2) * NT + n) * M + i) * 32 + lane] = make_float4(run.o[n][i][0], run.o[n][i][1], run.o[n][i][2], run.o[n][i][3]);
         }
         __syncthreads();
         if (warp < W / 2) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    float4* at = &merge[((warp * MT + i) * NT + n) * 32 + lane];
+                for (int i = 0; i < M; ++i) {
+                    float4* at = &merge[((warp * NT + n) * M + i) * 32 + lane];
                     const float4 x = *at;
-                    *at = make_float4(o[i][n][0] + x.x, o[i][n][1] + x.y, o[i][n][2] + x.z, o[i][n][3] + x.w);
+                    *at = make_float4(run.o[n][i][0] + x.x, run.o[n][i][1] + x.y, run.o[n][i][2] + x.z, run.o[n][i][3] + x.w);
                 }
         }
         __syncthreads();
-        // lane and half of the head: elements 64 h + 16 t4 .. + 15 of rows g8 and g8 + 8
-        for (int item = threadIdx.x; item < MT * H * 32; item += S::THREADS) {
-            const int ln = item & 31, h = item >> 5 & (H - 1), i = item / (32 * H), g = ln >> 2, t = ln & 3;
-            float x[4][8];
+        // a thread per (group of rows, lane): rows 2 t and 2 t + 1, elements 8 g .. 8 g + 7 of each half of the head
+        for (int item = threadIdx.x; item < NT * 32; item += S::THREADS) {
+            const int ln = item & 31, n = item >> 5, g = ln >> 2, t = ln & 3;
+            float x[2][H][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
+            for (int i = 0; i < M; ++i) {
                 float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
                 for (int w = 0; w < W / 2; ++w) {
-                    const float4 y = merge[((w * MT + i) * NT + h * 8 + e) * 32 + ln];
+                    const float4 y = merge[((w * NT + n) * M + i) * 32 + ln];
                     sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
                 }
-                const float by = e & 2 ? 1048576.0f : 16777216.0f;      // 2^20, 2^24: what the codes' form left out
-                x[0][e] = sum.x * by; x[1][e] = sum.y * by; x[2][e] = sum.z * by; x[3][e] = sum.w * by;
+                const float by = i & 2 ? 1048576.0f : 16777216.0f;      // 2^20, 2^24: what the codes' form left out
+                const int h1 = H - 1, e1 = D == 128 ? i : i + 4;
+                x[0][0][i] = sum.x * by; x[1][0][i] = sum.y * by; x[0][h1][e1] = sum.z * by; x[1][h1][e1] = sum.w * by;
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int r = i * 16 + j * 8 + g;
+                const int r = n * 8 + 2 * t + j;
+                if (row0 + r >= end) continue;
                 float top = kNone, lt = 0.0f, ot = 0.0f;
 #pragma unroll
                 for (int w = 0; w < W; ++w) { top = fmaxf(top, sm_m[w][r]); lt += sm_l[w][r]; ot += sm_o[w][r]; }
 #pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float* y = x[2 * j + c];
+                for (int h = 0; h < H; ++h) {
+                    float* y = x[j][h];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) y[e] += ot;
-                    const int d0 = 64 * h + 16 * t + 8 * c;
+                    const int d0 = 64 * h + 8 * g;
                     if (whole) {
-                        store_out(p, mine.q, mine.head, mine.tile * S::ROWS + r, D, d0, y, top - kLift, lt);
-                    } else if ((mine.tile * S::ROWS + r) / p.group < mine.q.n) {
+                        store_out(p, mine.q, mine.head, row0 + r, D, d0, y, top, lt);
+                    } else {
                         float* part = p.partial + static_cast<size_t>(2 * blockIdx.x + (from_start ? 1 : 0)) * S::PART;
                         reinterpret_cast<float4*>(part + r * D + d0)[0] = make_float4(y[0], y[1], y[2], y[3]);
                         reinterpret_cast<float4*>(part + r * D + d0)[1] = make_float4(y[4], y[5], y[6], y[7]);
-                        if (d0 == 0) { part[S::ROWS * D + 2 * r] = top - kLift; part[S::ROWS * D + 2 * r + 1] = lt; }
+                        if (d0 == 0) { part[S::ROWS * D + 2 * r] = top; part[S::ROWS * D + 2 * r + 1] = lt; }
                     }
                 }
             }
         }
         if (!whole && from_start && threadIdx.x == 0) {
             // the CTAs that the rest of the segment falls to
-            const long long last = s1 - step + mine.steps - 1;          // its last step
-            const int end = static_cast<int>(((last + 1) * ctas - 1) / total);
-            p.joins[blockIdx.x] = make_int4(end - static_cast<int>(blockIdx.x) + 1, mine.b, mine.head, mine.tile);
+            const long long last = s1 - step + steps - 1;          // its last step
+            const int at = static_cast<int>(((last + 1) * ctas - 1) / total);
+            p.joins[blockIdx.x] = make_int4(at - static_cast<int>(blockIdx.x) + 1, mine.b << 6 | mine.tile_rows / 8, mine.head, row0);
         }
-        if (step == mine.steps) {
-            next_segment<S>(p, mine);
+        __syncthreads();
+        if (step == steps) {
+            if (threadIdx.x == 0 && done < n_steps) {
+                Segment g = mine;
+                next_segment<S>(p, g);
+                mine = g;
+            }
             step = 0;
         }
         from_start = true;
         fresh = true;
     }
-    copies_wait<0>();
+    // gave up: what is still on its way lands before the CTA exits
+    if (!ok) {
+        if (lane == 0 && p.status) atomicCAS(p.status, 0, static_cast<int>(POLYSPEC_ERR_TIMEOUT));
+        for (int k = max(0, issued - NS); k < issued; ++k)
+            for (uint32_t i = 0; i < tensordev::kSpinLimitG; ++i)
+                if (mbar_try(bar_at + 8u * (k % NS), static_cast<uint32_t>(k / NS) & 1u)) break;
+    }
 }
 
 // Joins the parts of the segment that begins in CTA blockIdx.x and ends in a later one, in order.
@@ -671,10 +728,11 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p)
     wait_for_stream();
     const int4 job = p.joins[blockIdx.x];
     if (job.x == 0) return;
-    const kv::SeqRows q = kv::seq_rows(p.s, p.r, job.y);
+    const kv::SeqRows q = kv::seq_rows(p.s, p.r, job.y >> 6);
+    const int job_rows = (job.y & 63) * 8;
     for (int item = threadIdx.x; item < S::ROWS * kVecs; item += 256) {
         const int r = item / kVecs, d0 = item % kVecs * 8;
-        if ((job.w * S::ROWS + r) / p.group >= q.n) continue;
+        if (job.w + r >= q.n * p.group || r >= job_rows) continue;
         float x[8], m = kNone, l = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.0f;
@@ -688,7 +746,7 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p)
             x[0] = fmaf(x[0], was, a.x * is); x[1] = fmaf(x[1], was, a.y * is); x[2] = fmaf(x[2], was, a.z * is); x[3] = fmaf(x[3], was, a.w * is);
             x[4] = fmaf(x[4], was, b.x * is); x[5] = fmaf(x[5], was, b.y * is); x[6] = fmaf(x[6], was, b.z * is); x[7] = fmaf(x[7], was, b.w * is);
         }
-        store_out(p, q, job.z, job.w * S::ROWS + r, D, d0, x, m, l);
+        store_out(p, q, job.z, job.w + r, D, d0, x, m, l);
     }
 }
 
@@ -706,7 +764,7 @@ cudaError_t launch_attend(const AttendParams& p, cudaStream_t stream)
     return e;
 }
 
-constexpr int kMaxRows = 32;                    // rows of the largest tile
+constexpr int kMaxRows = 40;                    // rows of the largest tile
 inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 inline size_t attend_bytes(int head_dim) { return align256(kMaxCtas * sizeof(int4)) + static_cast<size_t>(2 * kMaxCtas) * kMaxRows * (head_dim + 2) * 4; }
 
@@ -720,13 +778,13 @@ struct WeighParams {
 
 constexpr int kWeighWarps = 8, kWeighTokens = kWeighWarps * 16;
 
-// A CTA has 128 tokens of a sequence, a warp 16 of them: keys only, once per head and row tile, the products as in attend_kernel.  Sums stay in a
-// lane's registers over all heads and rows; the lanes of one token meet at the end.  So every sum has one order.
+// A CTA has 128 tokens of a sequence, a warp 16 of them: keys only, once per head, the products as in attend_kernel.  Sums stay in a lane's registers
+// over all heads and rows; the lanes of one token meet at the end.  So every sum has one order.
 template <int D>
 __global__ void __launch_bounds__(kWeighWarps * 32) weigh_kernel(const WeighParams w)
 {
-    constexpr int KS = D / 16, UB = kv::unit_bytes(D), WORDS = D / 32, ROWS = 32, MT = 2, THREADS = kWeighWarps * 32;
-    __shared__ __align__(16) uint32_t frag[MT * KS * 128];
+    constexpr int KS = D / 16, UB = kv::unit_bytes(D), WORDS = D / 32, NT = 4, ROWS = NT * 8, THREADS = kWeighWarps * 32;
+    __shared__ __align__(16) uint32_t frag[NT * KS * 64];
     __shared__ float warp_max[kWeighWarps], sums[ROWS];
     const AttendParams& p = w.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3, b = blockIdx.y;
@@ -746,15 +804,13 @@ __global__ void __launch_bounds__(kWeighWarps * 32) weigh_kernel(const WeighPara
             else if (lane == 0) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
         }
     }
-    float acc[2][2] = {{0.0f, 0.0f}, {0.0f, 0.0f}};
-    const int tiles = (q.n * p.group + ROWS - 1) / ROWS;
+    float acc[2] = {0.0f, 0.0f};                // tokens g8, g8 + 8
+    const int rows = q.granted * p.group;
     for (int head = 0; head < p.kv_heads; ++head) {
-        // the head's keys stay in registers over its row tiles
-        uint32_t kw[2][WORDS];
-        uint2 kp[2];
+        // the head's keys stay in registers over its rows
+        uint32_t kw[2][WORDS], kp[2] = {0, 0};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            kp[u] = make_uint2(0, 0);
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) kw[u][i] = 0;
             if (unit[u] != 0xffffffffu) {
@@ -764,61 +820,49 @@ __global__ void __launch_bounds__(kWeighWarps * 32) weigh_kernel(const WeighPara
                     const uint2 x = *reinterpret_cast<const uint2*>(at + lane * (WORDS * 4) + i * 4);
                     kw[u][i] = x.x; kw[u][i + 1] = x.y;
                 }
-                kp[u] = *reinterpret_cast<const uint2*>(at + 4 * D + t4 * 8);
+                kp[u] = *reinterpret_cast<const uint32_t*>(at + 4 * D + g8 * 4);
             }
         }
-        for (int tile = 0; tile < tiles; ++tile) {
+        for (int row0 = 0; row0 < rows; row0 += ROWS) {
             float factor;
             __syncthreads();                    // the rows of the tile before have been read
-            load_rows<D, ROWS, THREADS>(p, q, head, tile, frag, sums, warp_max, &factor);
-            float sc[MT][2][4];
+            load_rows<D, ROWS, THREADS>(p, q, head, row0, rows, frag, sums, warp_max, &factor);
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int n = 0; n < NT; ++n) {
+                if (row0 + n * 8 >= rows) break;
+                float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                for (int u = 0; u < 2; ++u) sc[i][u][0] = sc[i][u][1] = sc[i][u][2] = sc[i][u][3] = 0.0f;
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-#pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    const uint4 a = *reinterpret_cast<const uint4*>(frag + ((i * KS + s) * 32 + lane) * 4);
-#pragma unroll
-                    for (int u = 0; u < 2; ++u)
-                        mma(sc[i][u], a.x, a.y, a.z, a.w, code_pair(kw[u][s >> 1], 2 * (s & 1)), code_pair(kw[u][s >> 1], 2 * (s & 1) + 1));
+                for (int s = 0; s < KS; ++s) {
+                    const uint2 x = reinterpret_cast<const uint2*>(frag)[(n * KS + s) * 32 + lane];
+                    mma(sc, code_pair(kw[0][s >> 1], 2 * (s & 1)), code_pair(kw[1][s >> 1], 2 * (s & 1)), code_pair(kw[0][s >> 1], 2 * (s & 1) + 1),
+                        code_pair(kw[1][s >> 1], 2 * (s & 1) + 1), x.x, x.y);
                 }
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    const int r = tile * ROWS + i * 16 + j * 8 + g8, row = r / p.group;
-                    const int limit = row < q.n ? row_limit(q, row) : 0;
-                    if (limit == 0) continue;
+                    const int r = row0 + n * 8 + 2 * t4 + j, row = r / p.group;
+                    if (r >= rows) continue;
+                    const int limit = row_limit(q, row);
                     const float lse = w.lse[static_cast<size_t>(q.row0 + row) * p.q_heads + head * p.group + r % p.group] * 1.44269504088896340736f;
-                    const float sq = sums[i * 16 + j * 8 + g8];
+                    const float sq = sums[n * 8 + 2 * t4 + j];
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        if (unit[u] == 0xffffffffu) continue;
-#pragma unroll
-                        for (int c = 0; c < 2; ++c) {
-                            const uint32_t pair = c ? kp[u].y : kp[u].x;
-                            const float x = fmaf(sc[i][u][2 * j + c], low(pair) * factor, sq * high(pair));
-                            if (key0 + 8 * u + 2 * t4 + c < limit) acc[u][c] += ex2(x - lse);
-                        }
+                        const float x = fmaf(sc[2 * u + j], low(kp[u]) * factor, sq * high(kp[u]));
+                        if (unit[u] != 0xffffffffu && key0 + 8 * u + g8 < limit) acc[u] += ex2(x - lse);
                     }
                 }
+            }
         }
     }
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) acc[u][c] += __shfl_xor_sync(0xffffffffu, acc[u][c], d);
-            const int slot = key0 + 8 * u + 2 * t4 + c;
-            if (g8 == 0 && slot < q.len) {
-                float* to = w.weights + static_cast<size_t>(b) * p.s.max_pages * p.s.page_tokens + slot;
-                *to = fmaf(w.keep, *to, acc[u][c]);
-            }
+    for (int u = 0; u < 2; ++u) {
+        acc[u] += __shfl_xor_sync(0xffffffffu, acc[u], 1);
+        acc[u] += __shfl_xor_sync(0xffffffffu, acc[u], 2);
+        const int slot = key0 + 8 * u + g8;
+        if (t4 == 0 && slot < q.len) {
+            float* to = w.weights + static_cast<size_t>(b) * p.s.max_pages * p.s.page_tokens + slot;
+            *to = fmaf(w.keep, *to, acc[u]);
         }
+    }
 }
 
 polyspec_status fill(AttendParams* p, const polyspec_cache_pages* s, const polyspec_block_rows* r, const void* q, long long q_stride, int q_heads,
@@ -831,6 +875,7 @@ polyspec_status fill(AttendParams* p, const polyspec_cache_pages* s, const polys
     if (!kv::rows_ok(q, q_stride, q_heads, head_dim) || !pool || !kv::aligned16(pool) || !aligned4(device_status)) return POLYSPEC_ERR_INVALID_ARG;
     if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return POLYSPEC_ERR_INVALID_ARG;
     const size_t bytes = kv::page_bytes(*s, kv_heads, head_dim);
+    if (s->n_seqs > (1 << 24)) return POLYSPEC_ERR_UNSUPPORTED;
     if (s->n_pages * (bytes / kv::unit_bytes(head_dim)) >= 0xffffffffull) return POLYSPEC_ERR_UNSUPPORTED;      // units of a plane are counted in 32 bits
     p->s = *s;
     p->r = *r;
@@ -876,11 +921,15 @@ polyspec_status polyspec_cache_attention(const polyspec_cache_pages* s, const po
     p.joins = static_cast<int4*>(workspace);
     p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(kMaxCtas * sizeof(int4)));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    // rows of a sequence times the heads that share a key head, on average: more than one tile of 16, and two tiles share the codes' expansion
-    const bool wide = static_cast<long long>(r->rows) * p.group > 16LL * s->n_seqs;
+    // rows of a sequence times the heads that share a key head, on average
+    const long long rows = (static_cast<long long>(r->rows) * p.group + s->n_seqs - 1) / s->n_seqs;
     cudaError_t e;
-    if (head_dim == 128) e = wide ? launch_attend<Shape<128, 2, 4, 5, 2>>(p, stream) : launch_attend<Shape<128, 1, 8, 4, 2>>(p, stream);
-    else e = wide ? launch_attend<Shape<64, 2, 8, 4, 2>>(p, stream) : launch_attend<Shape<64, 1, 8, 5, 2>>(p, stream);
+    if (head_dim == 128)
+        e = rows <= 8 ? launch_attend<Shape<128, 1, 8, 4, 2>>(p, stream) : rows <= 16 ? launch_attend<Shape<128, 2, 8, 4, 2>>(p, stream)
+                                                                         : launch_attend<Shape<128, 4, 4, 6, 2>>(p, stream);
+    else
+        e = rows <= 8 ? launch_attend<Shape<64, 1, 8, 6, 2>>(p, stream) : rows <= 16 ? launch_attend<Shape<64, 2, 8, 6, 2>>(p, stream)
+                                                                        : launch_attend<Shape<64, 4, 8, 5, 2>>(p, stream);
     return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }
 
