@@ -19,8 +19,8 @@
 // product's layout to the second's with one movmatrix per 8 x 8.  (tcgen05's tiles of 128 rows would be mostly empty, and its operands would have to
 // be expanded through shared or tensor memory.)
 //
-// Work: (sequence, key head, row tile) are segments of `steps` of 16 tokens per warp; the steps of all segments, one after the other, are cut into equal
-// shares, one per CTA, whatever the lengths.  Each warp streams its tiles through a ring of its own (bulk copies, one or two units at a time) and keeps
+// Work: (sequence, key head, row tile) are segments of `steps` of 32 tokens per warp; the steps of all segments, one after the other, are cut into equal
+// shares, one per CTA, whatever the lengths; what a segment costs besides its steps counts as kOverhead of them.  Each warp streams its tiles through a ring of its own (bulk copies of one or two units) and keeps
 // maximum, sums and the output tile in registers; a segment's warps meet once at its end.  A segment that crosses CTAs leaves partial
 // results, which a second kernel joins.
 #include <cuda_fp16.h>
@@ -36,7 +36,8 @@ using tensordev::mbar_init;
 using tensordev::mbar_try;
 using tensordev::smem_addr;
 
-constexpr int kMaxCtas = 304;                   // CTAs that the workspace has room for
+constexpr int kMaxCtas = 608;                   // CTAs that the workspace has room for
+constexpr int kOverhead = 4;                    // steps' worth of work that a segment costs besides its steps: its rows, the meeting of its warps
 constexpr float kNone = -3.0e38f;               // a maximum over nothing
 constexpr float kLift = 7.0f;                   // p' is kept 2^7 above 1 at the maximum, out of fp16's subnormals
 constexpr float kSlack = 8.0f;                  // and may rise to 2^15 before sums are rescaled
@@ -193,8 +194,8 @@ __device__ __forceinline__ int row_limit(const kv::SeqRows& q, int i) { return i
 template <int D_, int NT_, int WARPS_, int STAGES_, int CTAS_>
 struct Shape {
     static constexpr int D = D_, NT = NT_, WARPS = WARPS_, STAGES = STAGES_, CTAS = CTAS_;
-    static constexpr int THREADS = WARPS * 32, ROWS = NT * 8, STEP = WARPS * 16;        // STEP: tokens
-    static constexpr int UB = kv::unit_bytes(D), STAGE = 4 * UB, M = D / 16;            // M: 16-element groups of the output
+    static constexpr int THREADS = WARPS * 32, ROWS = NT * 8, STEP = WARPS * 32;        // STEP: tokens
+    static constexpr int UB = kv::unit_bytes(D), STAGE = 8 * UB, M = D / 16;            // M: 16-element groups of the output
     static constexpr int FRAG = NT * (D / 16) * 256;                                    // bytes
     static constexpr int RING = WARPS * STAGES * STAGE;
     static constexpr int MERGE = WARPS / 2 * NT * M * 512;
@@ -203,7 +204,8 @@ struct Shape {
     static_assert(SMEM * CTAS <= 220 * 1024, "shared memory");
 };
 
-// Where the steps of sequence b begin among all sequences' steps: the sequence that holds step `at`, or the total.  Every thread calls it.
+// All sequences' steps and overheads one behind the other: the sequence that holds place `at`, the place within it; returns the total.  Every thread
+// calls it.
 template <class S>
 __device__ __forceinline__ long long locate(const AttendParams& p, long long at, int* seq, long long* within, long long* warp_sums, int* hit, long long* hit_at)
 {
@@ -218,7 +220,7 @@ __device__ __forceinline__ long long locate(const AttendParams& p, long long at,
             g.q = kv::seq_rows(p.s, p.r, b);
             if (g.q.bad && blockIdx.x == 0) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
             seq_segments<S::ROWS, S::STEP>(p, g);
-            n = static_cast<long long>(g.tiles) * g.steps * p.kv_heads;
+            n = static_cast<long long>(g.tiles) * (g.steps + kOverhead) * p.kv_heads;
         }
         long long inc = n;
 #pragma unroll
@@ -289,80 +291,85 @@ __device__ __forceinline__ void store_out(const AttendParams& p, const kv::SeqRo
 template <class S>
 struct Running { float o[S::NT][S::M][4], ref[S::NT][2], l[S::NT][2], lo[S::NT][2]; bool started; };
 
-// 16 tokens, of which the stage at `at` has keys and values, for the first L groups of rows.  masked: some row does not see some token, or a unit could not be
+// 16 * T tokens from token 16 * t0 of a stage on, for the first L groups of rows.  `at`: the stage, 4 units of keys, 4 of values.  masked: some row does not see some token, or a unit could not be
 // read (bad).  q0: the rows' fragments where they stay in registers (one group).
-template <class S, int L>
-__device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>& run, const unsigned char* at, const uint32_t* frag, const uint2* q0, const float* sums,
+template <class S, int L, int T>
+__device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>& run, const unsigned char* at, int t0, const uint32_t* frag, const uint2* q0, const float* sums,
                                               float factor, bool masked, uint32_t bad, int key0, const Segment& seg, int lane)
 {
     constexpr int D = S::D, KS = D / 16, M = S::M, UB = S::UB, WORDS = D / 32, H = D / 64;
     const int g8 = lane >> 2, t4 = lane & 3;
     // codes of keys, and the first product: tokens x rows
-    uint32_t kw[2][WORDS];
+    float sc[T][L][4];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        if (D == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(at + u * UB + lane * 16);
-            kw[u][0] = x.x; kw[u][1] = x.y; kw[u][WORDS - 2] = x.z; kw[u][WORDS - 1] = x.w;
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(at + u * UB + lane * 8);
-            kw[u][0] = x.x; kw[u][1] = x.y;
-        }
-    }
-    float sc[L][4];
-#pragma unroll
-    for (int n = 0; n < L; ++n) sc[n][0] = sc[n][1] = sc[n][2] = sc[n][3] = 0.0f;
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-        const uint32_t a0 = code_pair(kw[0][s >> 1], 2 * (s & 1)), a1 = code_pair(kw[1][s >> 1], 2 * (s & 1));
-        const uint32_t a2 = code_pair(kw[0][s >> 1], 2 * (s & 1) + 1), a3 = code_pair(kw[1][s >> 1], 2 * (s & 1) + 1);
-#pragma unroll
-        for (int n = 0; n < L; ++n) {
-            const uint2 b = S::NT == 1 ? q0[S::NT == 1 ? s : 0] : reinterpret_cast<const uint2*>(frag)[(n * KS + s) * 32 + lane];
-            mma(sc[n], a0, a1, a2, a3, b.x, b.y);
-        }
-    }
-    // scales and offsets of the lane's tokens g8 and g8 + 8
-    float ks[2], ko[2], lv[2], iv[2], ov[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const uint32_t kp = *reinterpret_cast<const uint32_t*>(at + u * UB + 4 * D + g8 * 4);
-        const uint32_t vp = *reinterpret_cast<const uint32_t*>(at + (2 + u) * UB + 4 * D + g8 * 4);
-        ks[u] = low(kp) * factor;
-        ko[u] = high(kp);
-        const float vs = low(vp);
-        lv[u] = lg2(vs);
-        iv[u] = rcp(vs);
-        ov[u] = high(vp) * iv[u];
-    }
-    // exponents, less the references
-    float most = -INFINITY;
-#pragma unroll
-    for (int n = 0; n < L; ++n) {
-        const float2 sq = *reinterpret_cast<const float2*>(&sums[n * 8 + 2 * t4]);
+    for (int v = 0; v < T; ++v) {
+        uint32_t kw[2][WORDS];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            sc[n][2 * u] = fmaf(sc[n][2 * u], ks[u], fmaf(sq.x, ko[u], lv[u]) - run.ref[n][0]);
-            sc[n][2 * u + 1] = fmaf(sc[n][2 * u + 1], ks[u], fmaf(sq.y, ko[u], lv[u]) - run.ref[n][1]);
+            const unsigned char* unit = at + (2 * (t0 + v) + u) * UB;
+            if (D == 128) {
+                const uint4 x = *reinterpret_cast<const uint4*>(unit + lane * 16);
+                kw[u][0] = x.x; kw[u][1] = x.y; kw[u][WORDS - 2] = x.z; kw[u][WORDS - 1] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(unit + lane * 8);
+                kw[u][0] = x.x; kw[u][1] = x.y;
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < L; ++n) sc[v][n][0] = sc[v][n][1] = sc[v][n][2] = sc[v][n][3] = 0.0f;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+            const uint32_t a0 = code_pair(kw[0][s >> 1], 2 * (s & 1)), a1 = code_pair(kw[1][s >> 1], 2 * (s & 1));
+            const uint32_t a2 = code_pair(kw[0][s >> 1], 2 * (s & 1) + 1), a3 = code_pair(kw[1][s >> 1], 2 * (s & 1) + 1);
+#pragma unroll
+            for (int n = 0; n < L; ++n) {
+                const uint2 b = S::NT == 1 ? q0[S::NT == 1 ? s : 0] : reinterpret_cast<const uint2*>(frag)[(n * KS + s) * 32 + lane];
+                mma(sc[v][n], a0, a1, a2, a3, b.x, b.y);
+            }
         }
     }
-    uint32_t hidden = 0;                        // bit 4 n + 2 u + j
+    // scales and offsets of the lane's tokens g8 and g8 + 8; exponents, less the references
+    float iv[T][2], ov[T][2], most = -INFINITY;
+#pragma unroll
+    for (int v = 0; v < T; ++v) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const unsigned char* pairs = at + (2 * (t0 + v) + u) * UB + 4 * D + g8 * 4;
+            const uint32_t kp = *reinterpret_cast<const uint32_t*>(pairs), vp = *reinterpret_cast<const uint32_t*>(pairs + 4 * UB);
+            const float ks = low(kp) * factor, ko = high(kp), vs = low(vp), lv = lg2(vs);
+            iv[v][u] = rcp(vs);
+            ov[v][u] = high(vp) * iv[v][u];
+#pragma unroll
+            for (int n = 0; n < L; ++n) {
+                const float2 sq = *reinterpret_cast<const float2*>(&sums[n * 8 + 2 * t4]);
+                sc[v][n][2 * u] = fmaf(sc[v][n][2 * u], ks, fmaf(sq.x, ko, lv) - run.ref[n][0]);
+                sc[v][n][2 * u + 1] = fmaf(sc[v][n][2 * u + 1], ks, fmaf(sq.y, ko, lv) - run.ref[n][1]);
+            }
+        }
+    }
+    uint32_t hidden[T];                         // bit 4 n + 2 u + j
     if (masked) {
 #pragma unroll
-        for (int n = 0; n < L; ++n)
+        for (int v = 0; v < T; ++v) {
+            hidden[v] = 0;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const int limit = row_limit(seg.q, (seg.tile * seg.tile_rows + n * 8 + 2 * t4 + j) / p.group);
+            for (int n = 0; n < L; ++n)
 #pragma unroll
-                for (int u = 0; u < 2; ++u)
-                    if (key0 + 8 * u + g8 >= limit || (bad >> u & 1u)) {
-                        hidden |= 1u << (4 * n + 2 * u + j);
-                        sc[n][2 * u + j] = -INFINITY;
-                    }
-            }
+                for (int j = 0; j < 2; ++j) {
+                    const int limit = row_limit(seg.q, (seg.tile * seg.tile_rows + n * 8 + 2 * t4 + j) / p.group);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+                        if (key0 + 16 * (t0 + v) + 8 * u + g8 >= limit || (bad >> (2 * (t0 + v) + u) & 1u)) {
+                            hidden[v] |= 1u << (4 * n + 2 * u + j);
+                            sc[v][n][2 * u + j] = -INFINITY;
+                        }
+                }
+        }
     }
 #pragma unroll
-    for (int n = 0; n < L; ++n) most = fmaxf(most, fmaxf(fmaxf(sc[n][0], sc[n][1]), fmaxf(sc[n][2], sc[n][3])));
+    for (int v = 0; v < T; ++v)
+#pragma unroll
+        for (int n = 0; n < L; ++n) most = fmaxf(most, fmaxf(fmaxf(sc[v][n][0], sc[v][n][1]), fmaxf(sc[v][n][2], sc[v][n][3])));
     // the first tokens set the references; after that sums are rescaled only when a maximum has risen by 2^8 since the last time
     if (__any_sync(0xffffffffu, !run.started || most > kLift + kSlack)) {
         const bool first = !run.started;
@@ -370,13 +377,15 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
         for (int n = 0; n < L; ++n)
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                float top = fmaxf(sc[n][j], sc[n][2 + j]);
+                float top = -INFINITY;
+#pragma unroll
+                for (int v = 0; v < T; ++v) top = fmaxf(top, fmaxf(sc[v][n][j], sc[v][n][2 + j]));
 #pragma unroll
                 for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
                 // (a row that sees none of its warp's first tokens sees none of the later ones either)
                 const float up = first ? (top == -INFINITY ? 0.0f : top - kLift) : fmaxf(top - kLift, 0.0f), by = first ? 1.0f : ex2(-up);
-                sc[n][j] -= up;
-                sc[n][2 + j] -= up;
+#pragma unroll
+                for (int v = 0; v < T; ++v) { sc[v][n][j] -= up; sc[v][n][2 + j] -= up; }
                 run.ref[n][j] += up;
                 run.l[n][j] *= by;
                 run.lo[n][j] *= by;
@@ -385,53 +394,63 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
             }
         run.started = true;
     }
-    uint32_t pr[L][2];
+    uint32_t pr[T][L][2];
 #pragma unroll
-    for (int n = 0; n < L; ++n) {
+    for (int v = 0; v < T; ++v)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sc[n][i] = ex2(sc[n][i]);
-        pr[n][0] = transpose(half2_bits(sc[n][0], sc[n][1]));
-        pr[n][1] = transpose(half2_bits(sc[n][2], sc[n][3]));
-    }
+        for (int n = 0; n < L; ++n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sc[v][n][i] = ex2(sc[v][n][i]);
+            pr[v][n][0] = transpose(half2_bits(sc[v][n][0], sc[v][n][1]));
+            pr[v][n][1] = transpose(half2_bits(sc[v][n][2], sc[v][n][3]));
+        }
     if (!masked) {
 #pragma unroll
-        for (int n = 0; n < L; ++n)
+        for (int v = 0; v < T; ++v)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                run.l[n][i & 1] = fmaf(sc[n][i], iv[i >> 1], run.l[n][i & 1]);
-                run.lo[n][i & 1] = fmaf(sc[n][i], ov[i >> 1], run.lo[n][i & 1]);
-            }
+            for (int n = 0; n < L; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    run.l[n][i & 1] = fmaf(sc[v][n][i], iv[v][i >> 1], run.l[n][i & 1]);
+                    run.lo[n][i & 1] = fmaf(sc[v][n][i], ov[v][i >> 1], run.lo[n][i & 1]);
+                }
     } else {                                    // scales behind what a row sees may be anything
 #pragma unroll
-        for (int n = 0; n < L; ++n)
+        for (int v = 0; v < T; ++v)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (!(hidden >> (4 * n + i) & 1u)) {
-                    run.l[n][i & 1] = fmaf(sc[n][i], iv[i >> 1], run.l[n][i & 1]);
-                    run.lo[n][i & 1] = fmaf(sc[n][i], ov[i >> 1], run.lo[n][i & 1]);
-                }
+            for (int n = 0; n < L; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (!(hidden[v] >> (4 * n + i) & 1u)) {
+                        run.l[n][i & 1] = fmaf(sc[v][n][i], iv[v][i >> 1], run.l[n][i & 1]);
+                        run.lo[n][i & 1] = fmaf(sc[v][n][i], ov[v][i >> 1], run.lo[n][i & 1]);
+                    }
     }
     // codes of values: words of tokens 2 t4 and 2 t4 + 1, paired by token, and the second product: elements x rows
-    uint32_t even[2][H], odd[2][H];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        if (D == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(at + (2 + u) * UB + lane * 16);
-            even[u][0] = __byte_perm(x.x, x.z, 0x5410); odd[u][0] = __byte_perm(x.x, x.z, 0x7632);
-            even[u][H - 1] = __byte_perm(x.y, x.w, 0x5410); odd[u][H - 1] = __byte_perm(x.y, x.w, 0x7632);
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(at + (2 + u) * UB + lane * 8);
-            even[u][0] = __byte_perm(x.x, x.y, 0x5410); odd[u][0] = __byte_perm(x.x, x.y, 0x7632);
+    for (int v = 0; v < T; ++v) {
+        uint32_t even[2][H], odd[2][H];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const unsigned char* unit = at + (4 + 2 * (t0 + v) + u) * UB;
+            if (D == 128) {
+                const uint4 x = *reinterpret_cast<const uint4*>(unit + lane * 16);
+                even[u][0] = __byte_perm(x.x, x.z, 0x5410); odd[u][0] = __byte_perm(x.x, x.z, 0x7632);
+                even[u][H - 1] = __byte_perm(x.y, x.w, 0x5410); odd[u][H - 1] = __byte_perm(x.y, x.w, 0x7632);
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(unit + lane * 8);
+                even[u][0] = __byte_perm(x.x, x.y, 0x5410); odd[u][0] = __byte_perm(x.x, x.y, 0x7632);
+            }
         }
-    }
 #pragma unroll
-    for (int i = 0; i < M; ++i) {
-        // the product's rows: elements 8 g8 + i and 64 + 8 g8 + i, or of narrow heads 8 g8 + i and 8 g8 + 4 + i
-        const int e0 = i, e1 = D == 128 ? i : i + 4, h1 = H - 1;
-        const uint32_t a0 = code_pair(e0 & 1 ? odd[0][0] : even[0][0], e0 >> 1), a1 = code_pair(e1 & 1 ? odd[0][h1] : even[0][h1], e1 >> 1);
-        const uint32_t a2 = code_pair(e0 & 1 ? odd[1][0] : even[1][0], e0 >> 1), a3 = code_pair(e1 & 1 ? odd[1][h1] : even[1][h1], e1 >> 1);
+        for (int i = 0; i < M; ++i) {
+            // the product's rows: elements 8 g8 + i and 64 + 8 g8 + i, or of narrow heads 8 g8 + i and 8 g8 + 4 + i
+            const int e0 = i, e1 = D == 128 ? i : i + 4, h1 = H - 1;
+            const uint32_t a0 = code_pair(e0 & 1 ? odd[0][0] : even[0][0], e0 >> 1), a1 = code_pair(e1 & 1 ? odd[0][h1] : even[0][h1], e1 >> 1);
+            const uint32_t a2 = code_pair(e0 & 1 ? odd[1][0] : even[1][0], e0 >> 1), a3 = code_pair(e1 & 1 ? odd[1][h1] : even[1][h1], e1 >> 1);
 #pragma unroll
-        for (int n = 0; n < L; ++n) mma(run.o[n][i], a0, a1, a2, a3, pr[n][0], pr[n][1]);
+            for (int n = 0; n < L; ++n) mma(run.o[n][i], a0, a1, a2, a3, pr[v][n][0], pr[v][n][1]);
+        }
     }
 }
 
@@ -469,31 +488,34 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
     if (blockIdx.x >= ctas) return;
     const long long s0 = total * blockIdx.x / ctas, s1 = total * (blockIdx.x + 1) / ctas;
     locate<S>(p, s0, &seq, &within, warp_sums, &hit, &hit_at);
-    int step;
+    int step, left;                             // left: places up to s1 (a step's, and an overhead's at each new segment)
     {
         Segment g;
         g.b = seq;
         g.q = kv::seq_rows(p.s, p.r, seq);
         seq_segments<S::ROWS, S::STEP>(p, g);
-        step = static_cast<int>(within % g.steps);
-        const int n = static_cast<int>(within / g.steps);
+        const int span = g.steps + kOverhead, n = static_cast<int>(within / span);
         g.head = n / g.tiles;
         g.tile = n % g.tiles;
+        const int into = static_cast<int>(within % span) - kOverhead;       // negative: before the segment's first step
+        step = max(into, 0);
+        left = static_cast<int>(s1 - s0) + min(into, 0);
+        if (left <= 0) return;
         if (threadIdx.x == 0) mine = g;
         if (lane == 0) { produced[warp] = g; produced_visible[warp] = visible(p, g); }
         __syncthreads();
     }
-    int ahead_step = step, ahead_steps = mine.steps;
-    const int n_steps = static_cast<int>(s1 - s0);
+    int ahead_step = step, ahead_steps = mine.steps, ahead_left = left;
 
-    // lane 2k + u: unit u of the warp's k-th tile from here on, as a number of units in a plane, or ~0
+    // lane 4 k + u: unit u of the warp's k-th stage from here on, as a number of units in a plane, or ~0
     uint32_t unit_numbers = 0;
-    int unit_k = 16;                            // tiles of `unit_numbers` that are used up
-    uint32_t bad_units = 0;                     // bit 2 stage + u: nothing could be read there
+    int unit_k = 8;                             // stages of `unit_numbers` that are used up
+    uint32_t bad_units = 0;                     // bit 4 stage + u: nothing could be read there
 
+    // Copies of the next stage: lanes 0 .. 3 a unit of keys each, 4 .. 7 of values; a unit that follows its even neighbour's in memory goes with it.
     auto issue = [&](int stage) {
-        if (unit_k == 16) {
-            const long long slot = (static_cast<long long>(ahead_step + (lane >> 1)) * W + warp) * 16 + (lane & 1) * 8;
+        if (unit_k == 8) {
+            const long long slot = (static_cast<long long>(ahead_step + (lane >> 2)) * W + warp) * 32 + (lane & 3) * 8;
             unit_numbers = 0xffffffffu;
             if (slot < produced_visible[warp]) {
                 const Segment& ahead = produced[warp];
@@ -506,29 +528,19 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
             }
             unit_k = 0;
         }
-        const uint32_t u0 = __shfl_sync(0xffffffffu, unit_numbers, 2 * unit_k), u1 = __shfl_sync(0xffffffffu, unit_numbers, 2 * unit_k + 1);
-        const uint32_t there = (u0 != 0xffffffffu ? 1u : 0u) | (u1 != 0xffffffffu ? 2u : 0u);
-        bad_units = (bad_units & ~(3u << (2 * stage))) | (3u ^ there) << (2 * stage);
-        if (lane == 0) {
-            const uint32_t to = ring_at + stage * S::STAGE, bar = bar_at + 8u * stage;
-            const unsigned char* k0 = p.pool + static_cast<size_t>(u0) * UB;
-            mbar_expect_tx(bar, (there == 3u ? 4 : there ? 2 : 0) * UB);
-            if (there == 3u && u1 == u0 + 1) {
-                copy_bulk(to, k0, 2 * UB, bar);
-                copy_bulk(to + 2 * UB, k0 + p.plane_bytes, 2 * UB, bar);
-            } else {
-                if (there & 1u) {
-                    copy_bulk(to, k0, UB, bar);
-                    copy_bulk(to + 2 * UB, k0 + p.plane_bytes, UB, bar);
-                }
-                if (there & 2u) {
-                    const unsigned char* k1 = p.pool + static_cast<size_t>(u1) * UB;
-                    copy_bulk(to + UB, k1, UB, bar);
-                    copy_bulk(to + 3 * UB, k1 + p.plane_bytes, UB, bar);
-                }
-            }
-        }
+        const uint32_t number = __shfl_sync(0xffffffffu, unit_numbers, 4 * unit_k + (lane & 3));
+        const uint32_t neighbour = __shfl_xor_sync(0xffffffffu, number, 1);
+        const bool there = number != 0xffffffffu, odd = lane & 1;
+        const bool together = odd ? number == neighbour + 1 && neighbour != 0xffffffffu : neighbour == number + 1 && there && neighbour != 0xffffffffu;
+        const uint32_t units = __ballot_sync(0xffffffffu, there) & 15u;
+        bad_units = (bad_units & ~(15u << (4 * stage))) | (15u ^ units) << (4 * stage);
+        const uint32_t bar = bar_at + 8u * stage;
+        if (lane == 0) mbar_expect_tx(bar, 2 * UB * __popc(units));
+        __syncwarp();
+        if (lane < 8 && there && !(odd && together))
+            copy_bulk(ring_at + stage * S::STAGE + lane * UB, p.pool + static_cast<size_t>(number) * UB + (lane < 4 ? 0 : p.plane_bytes), together ? 2 * UB : UB, bar);
         ++unit_k;
+        --ahead_left;
         if (++ahead_step == ahead_steps) {
             __syncwarp();
             if (lane == 0) {
@@ -540,22 +552,23 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
             __syncwarp();
             ahead_step = 0;
             ahead_steps = produced[warp].steps;
-            unit_k = 16;
+            ahead_left -= kOverhead;
+            unit_k = 8;
         }
     };
 
     int issued = 0;
-    for (; issued < NS - 1 && issued < n_steps; ++issued) issue(issued);
+    for (; issued < NS - 1 && ahead_left > 0; ++issued) issue(issued);
 
     Running<S> run;
-    static_assert(NT <= 4, "groups");
+    static_assert(NT <= 2, "groups");
     uint2 q0[NT == 1 ? KS : 1];                 // of a tile of one group of rows the fragments stay in registers
-    int seen = 0, live = 0, done = 0, stage = 0;        // done: steps; live: groups of rows
+    int seen = 0, live = 0, stage = 0;          // live: groups of rows
     uint32_t phase = 0;
     bool from_start = step == 0, fresh = true, ok = true;
     float factor = 0.0f;
     int steps = 0, all_see = 0;                 // of the segment; tokens that every row sees
-    while (done < n_steps) {
+    while (left > 0) {
         if (fresh) {
             __syncthreads();                    // the segment has been written
             steps = mine.steps;
@@ -586,24 +599,30 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
             while (i < tensordev::kSpinLimitG && !mbar_try(bar_at + 8u * stage, phase)) ++i;
             ok = __all_sync(0xffffffffu, i < tensordev::kSpinLimitG);
         }
-        const int key0 = (step * W + warp) * 16;
-        const uint32_t bad = bad_units >> (2 * stage) & 3u;
-        if (key0 < seen && ok && bad != 3u) {
+        const int key0 = (step * W + warp) * 32;
+        const uint32_t bad = bad_units >> (4 * stage) & 15u;
+        if (key0 < seen && ok && bad != 15u) {
             const unsigned char* at = ring + stage * S::STAGE;
-            const bool masked = key0 + 16 > all_see || bad;
-            // (code of its own for each number of groups: what is not there costs nothing, and what is there is straight-line code)
-            if (NT == 1 || live == 1) attend_tokens<S, 1>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
-            else if (NT == 2 || live == 2) attend_tokens<S, NT < 2 ? 1 : 2>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
-            else if (NT == 3 || live == 3) attend_tokens<S, NT < 3 ? 1 : 3>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
-            else attend_tokens<S, NT < 4 ? 1 : 4>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
+            const bool masked = key0 + 32 > all_see || bad;
+            if (NT == 1) {
+                attend_tokens<S, 1, 2>(p, run, at, 0, frag, q0, sums, factor, masked, bad, key0, mine, lane);
+            } else {
+#pragma unroll 1
+                for (int t0 = 0; t0 < 2; ++t0) {
+                    if ((bad >> (2 * t0) & 3u) == 3u) continue;
+                    // (code of its own for each number of groups: what is not there costs nothing, and what is there is straight-line code)
+                    if (live == 1) attend_tokens<S, 1, 1>(p, run, at, t0, frag, q0, sums, factor, masked, bad, key0, mine, lane);
+                    else attend_tokens<S, NT, 1>(p, run, at, t0, frag, q0, sums, factor, masked, bad, key0, mine, lane);
+                }
+            }
         }
         __syncwarp();
         // the stage that was read before this one is free again
-        if (issued < n_steps && ok) { issue(stage == 0 ? NS - 1 : stage - 1); ++issued; }
+        if (ahead_left > 0 && ok) { issue(stage == 0 ? NS - 1 : stage - 1); ++issued; }
         if (++stage == NS) { stage = 0; phase ^= 1u; }
-        ++done;
+        --left;
         ++step;
-        if (step < steps && done < n_steps) continue;
+        if (step < steps && left > 0) continue;
 
         // the segment, or this CTA's part of it, is done: its warps meet
         const bool whole = from_start && step == steps;
@@ -695,13 +714,14 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
         }
         if (!whole && from_start && threadIdx.x == 0) {
             // the CTAs that the rest of the segment falls to
-            const long long last = s1 - step + steps - 1;          // its last step
+            const long long last = s1 + (steps - step) - 1;             // the place of its last step
             const int at = static_cast<int>(((last + 1) * ctas - 1) / total);
             p.joins[blockIdx.x] = make_int4(at - static_cast<int>(blockIdx.x) + 1, mine.b << 6 | mine.tile_rows / 8, mine.head, row0);
         }
         __syncthreads();
         if (step == steps) {
-            if (threadIdx.x == 0 && done < n_steps) {
+            left -= kOverhead;
+            if (threadIdx.x == 0 && left > 0) {
                 Segment g = mine;
                 next_segment<S>(p, g);
                 mine = g;
@@ -764,7 +784,7 @@ cudaError_t launch_attend(const AttendParams& p, cudaStream_t stream)
     return e;
 }
 
-constexpr int kMaxRows = 40;                    // rows of the largest tile
+constexpr int kMaxRows = 16;                    // rows of the largest tile
 inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 inline size_t attend_bytes(int head_dim) { return align256(kMaxCtas * sizeof(int4)) + static_cast<size_t>(2 * kMaxCtas) * kMaxRows * (head_dim + 2) * 4; }
 
@@ -921,15 +941,11 @@ polyspec_status polyspec_cache_attention(const polyspec_cache_pages* s, const po
     p.joins = static_cast<int4*>(workspace);
     p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(kMaxCtas * sizeof(int4)));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    // rows of a sequence times the heads that share a key head, on average
-    const long long rows = (static_cast<long long>(r->rows) * p.group + s->n_seqs - 1) / s->n_seqs;
+    // rows of a sequence times the heads that share a key head, on average: one group of 8 rows, or tiles of two
+    const bool few = static_cast<long long>(r->rows) * p.group <= 8LL * s->n_seqs;
     cudaError_t e;
-    if (head_dim == 128)
-        e = rows <= 8 ? launch_attend<Shape<128, 1, 8, 4, 2>>(p, stream) : rows <= 16 ? launch_attend<Shape<128, 2, 8, 4, 2>>(p, stream)
-                                                                         : launch_attend<Shape<128, 4, 4, 6, 2>>(p, stream);
-    else
-        e = rows <= 8 ? launch_attend<Shape<64, 1, 8, 6, 2>>(p, stream) : rows <= 16 ? launch_attend<Shape<64, 2, 8, 6, 2>>(p, stream)
-                                                                        : launch_attend<Shape<64, 4, 8, 5, 2>>(p, stream);
+    if (head_dim == 128) e = few ? launch_attend<Shape<128, 1, 8, 2, 2>>(p, stream) : launch_attend<Shape<128, 2, 4, 3, 3>>(p, stream);
+    else e = few ? launch_attend<Shape<64, 1, 8, 3, 2>>(p, stream) : launch_attend<Shape<64, 2, 8, 3, 2>>(p, stream);
     return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }
 
