@@ -26,90 +26,129 @@ struct AppendParams {
     int kv_heads;
 };
 
-// D: head_dim.  A CTA has a row; its teams of D / 8 lanes take turns over (head, keys or values).
-template <int D>
+// D: head_dim.  A CTA has ROWS rows; its teams of D / 8 lanes take turns over (row, head, keys or values), kAhead items at a time, whose loads are on
+// their way while the rows' places are looked up (a chain of four loads: sequence, length, page, its holders).
+template <int D, int ROWS>
 __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
 {
-    constexpr int kLanes = D / 8;
-    __shared__ int found;
+    constexpr int kLanes = D / 8, kTeams = kThreads / kLanes, kAhead = 4;
+    __shared__ int found[ROWS];
+    __shared__ uint32_t units[ROWS];            // the row's unit of head 0, or ~0: not written
+    __shared__ int tokens[ROWS];                // its token of the unit
     wait_for_stream();
-    const int row = blockIdx.x;
-    if (row == 0)               // numbers that make no sense are reported even where no row belongs to them
-        for (int b = threadIdx.x; b < p.s.n_seqs; b += kThreads)
+    const int row0 = blockIdx.x * ROWS, tid = threadIdx.x, w = tid % kLanes, team = tid / kLanes;
+    const int per_row = 2 * p.kv_heads, items = min(ROWS, p.r.rows - row0) * per_row;
+    uint4 raw[kAhead];
+    auto load = [&](int first) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int item = first + u * kTeams + team, row = row0 + item / per_row, j = item % per_row;
+            raw[u] = make_uint4(0, 0, 0, 0);
+            if (item < items) raw[u] = reinterpret_cast<const uint4*>((j & 1 ? p.v + row * p.v_stride : p.k + row * p.k_stride) + (j >> 1) * D)[w];
+        }
+    };
+    load(0);
+    if (row0 == 0)              // numbers that make no sense are reported even where no row belongs to them
+        for (int b = tid; b < p.s.n_seqs; b += kThreads)
             if (kv::seq_rows(p.s, p.r, b).bad) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
-    const int b = kv::find_seq(p.r.rows_at, p.s.n_seqs, row, &found);
-    if (b < 0) return;
-    const kv::SeqRows q = kv::seq_rows(p.s, p.r, b);
-    const int i = row - q.row0;
-    if (i >= q.granted) return;
-    const int slot = q.base + i, P = p.s.page_tokens;
-    const int page = p.s.table[static_cast<size_t>(b) * p.s.max_pages + slot / P];
-    if (page < 0 || page >= p.s.n_pages || p.s.refs[page] > 1) {
-        if (threadIdx.x == 0) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
-        return;
+    if (tid < ROWS) found[tid] = -1;
+    __syncthreads();
+    for (int b = tid; b < p.s.n_seqs; b += kThreads) {
+        const int lo = p.r.rows_at[b], hi = p.r.rows_at[b + 1];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i)
+            if (lo <= row0 + i && row0 + i < hi) atomicMax(&found[i], b);
     }
-    if (p.weights && threadIdx.x == 0) p.weights[static_cast<size_t>(b) * p.s.max_pages * P + slot] = 0.0f;
-    const int at = slot % P, unit = at / kv::kUnit, r = at % kv::kUnit, w = threadIdx.x % kLanes;
-    // (whole warps go round together: the exchange below is warp-wide)
-    for (int j0 = 0; j0 < 2 * p.kv_heads; j0 += kThreads / kLanes) {
-        const int j = j0 + threadIdx.x / kLanes, head = j >> 1, values = j & 1;
-        const bool live = head < p.kv_heads;
-        float x[8];
-        if (live) {
-            const __nv_bfloat16* from = (values ? p.v + row * p.v_stride : p.k + row * p.k_stride) + head * D;
-            const uint4 raw = reinterpret_cast<const uint4*>(from)[w];
-            x[0] = __uint_as_float(raw.x << 16); x[1] = __uint_as_float(raw.x & 0xffff0000u);
-            x[2] = __uint_as_float(raw.y << 16); x[3] = __uint_as_float(raw.y & 0xffff0000u);
-            x[4] = __uint_as_float(raw.z << 16); x[5] = __uint_as_float(raw.z & 0xffff0000u);
-            x[6] = __uint_as_float(raw.w << 16); x[7] = __uint_as_float(raw.w & 0xffff0000u);
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-        }
-        float lo = x[0], hi = x[0];
-        bool nan = false;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            lo = fminf(lo, x[e]);
-            hi = fmaxf(hi, x[e]);
-            nan = nan || !(fabsf(x[e]) <= 3.4e38f);
-        }
-#pragma unroll
-        for (int d = 1; d < kLanes; d <<= 1) {
-            lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-            hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-        }
-        const uint32_t bad = __ballot_sync(0xffffffffu, nan);
-        const uint32_t team = ((1ull << kLanes) - 1u) << ((threadIdx.x & 31) / kLanes * kLanes);
-        float offset = lo + 0.0f;                       // (not -0)
-        const float range = hi - offset;
-        const uint32_t up = (__float_as_uint(__fdiv_rn(range, 15.0f)) + 0xffffu) & 0xffff0000u;
-        float scale = up ? __uint_as_float(up) : 1.0f;
-        const bool broken = (bad & team) || !(range <= 3.4e38f);
-        if (broken) scale = offset = __uint_as_float(0x7fc00000u);
-        uint32_t word = 0, held[4];
-        float y[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int code = broken ? 0 : min(15, static_cast<int>(rintf(__fdiv_rn(x[e] - offset, scale))));
-            word |= static_cast<uint32_t>(code) << (4 * (e / 2) + 16 * (e % 2));
-            y[e] = __fadd_rn(__fmul_rn(scale, static_cast<float>(code)), offset);
-        }
-        if (!live) continue;
-        unsigned char* plane = p.pool + (values ? static_cast<size_t>(p.s.n_pages) * p.page_bytes : 0);
-        uint32_t* to = reinterpret_cast<uint32_t*>(plane + page * p.page_bytes + static_cast<size_t>(head * (P / kv::kUnit) + unit) * kv::unit_bytes(D));
-        to[values ? kv::value_word(r, w, D) : kv::key_word(r, w, D)] = word;
-        if (w == 0) to[D + r] = (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
-        __nv_bfloat16* out = values ? p.v_held : p.k_held;
-        if (out) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const __nv_bfloat162 z = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
-                held[e] = *reinterpret_cast<const uint32_t*>(&z);
+    __syncthreads();
+    const int P = p.s.page_tokens, per_page = P / kv::kUnit;
+    if (tid < ROWS) {
+        const int b = found[tid];
+        units[tid] = 0xffffffffu;
+        if (b >= 0) {
+            const kv::SeqRows q = kv::seq_rows(p.s, p.r, b);
+            const int i = row0 + tid - q.row0;
+            if (i < q.granted) {
+                const int slot = q.base + i, at = slot / P;
+                const int page = p.s.table[static_cast<size_t>(b) * p.s.max_pages + at];
+                if (page < 0 || page >= p.s.n_pages || p.s.refs[page] > 1) {
+                    kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
+                } else {
+                    units[tid] = static_cast<uint32_t>(page) * p.kv_heads * per_page + (slot - at * P) / kv::kUnit;
+                    tokens[tid] = slot % kv::kUnit;
+                    if (p.weights) p.weights[static_cast<size_t>(b) * p.s.max_pages * P + slot] = 0.0f;
+                }
             }
-            reinterpret_cast<uint4*>(out + (static_cast<size_t>(row) * p.kv_heads + head) * D)[w] = make_uint4(held[0], held[1], held[2], held[3]);
         }
     }
+    __syncthreads();
+    // (whole warps go round together: the exchange below is warp-wide)
+    for (int first = 0; first < items; first += kAhead * kTeams) {
+        if (first > 0) load(first);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int item = first + u * kTeams + team;
+            if (first + u * kTeams >= items) break;
+            const int i = min(item, items - 1) / per_row, j = item % per_row, head = j >> 1, values = j & 1;
+            const bool live = item < items && units[i] != 0xffffffffu;
+            float x[8];
+            x[0] = __uint_as_float(raw[u].x << 16); x[1] = __uint_as_float(raw[u].x & 0xffff0000u);
+            x[2] = __uint_as_float(raw[u].y << 16); x[3] = __uint_as_float(raw[u].y & 0xffff0000u);
+            x[4] = __uint_as_float(raw[u].z << 16); x[5] = __uint_as_float(raw[u].z & 0xffff0000u);
+            x[6] = __uint_as_float(raw[u].w << 16); x[7] = __uint_as_float(raw[u].w & 0xffff0000u);
+            float lo = x[0], hi = x[0];
+            bool nan = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                lo = fminf(lo, x[e]);
+                hi = fmaxf(hi, x[e]);
+                nan = nan || !(fabsf(x[e]) <= 3.4e38f);
+            }
+#pragma unroll
+            for (int d = 1; d < kLanes; d <<= 1) {
+                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
+                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
+            }
+            const uint32_t bad = __ballot_sync(0xffffffffu, nan);
+            const uint32_t mates = ((1ull << kLanes) - 1u) << ((tid & 31) / kLanes * kLanes);
+            float offset = lo + 0.0f;                       // (not -0)
+            const float range = hi - offset;
+            const uint32_t up = (__float_as_uint(__fdiv_rn(range, 15.0f)) + 0xffffu) & 0xffff0000u;
+            float scale = up ? __uint_as_float(up) : 1.0f;
+            const bool broken = (bad & mates) || !(range <= 3.4e38f);
+            if (broken) scale = offset = __uint_as_float(0x7fc00000u);
+            uint32_t word = 0, held[4];
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int code = broken ? 0 : min(15, static_cast<int>(rintf(__fdiv_rn(x[e] - offset, scale))));
+                word |= static_cast<uint32_t>(code) << (4 * (e / 2) + 16 * (e % 2));
+                y[e] = __fadd_rn(__fmul_rn(scale, static_cast<float>(code)), offset);
+            }
+            if (!live) continue;
+            unsigned char* plane = p.pool + (values ? static_cast<size_t>(p.s.n_pages) * p.page_bytes : 0);
+            uint32_t* to = reinterpret_cast<uint32_t*>(plane + static_cast<size_t>(units[i] + static_cast<uint32_t>(head * per_page)) * kv::unit_bytes(D));
+            const int r = tokens[i];
+            to[values ? kv::value_word(r, w, D) : kv::key_word(r, w, D)] = word;
+            if (w == 0) to[D + r] = (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
+            __nv_bfloat16* out = values ? p.v_held : p.k_held;
+            if (out) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const __nv_bfloat162 z = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
+                    held[e] = *reinterpret_cast<const uint32_t*>(&z);
+                }
+                reinterpret_cast<uint4*>(out + (static_cast<size_t>(row0 + i) * p.kv_heads + head) * D)[w] = make_uint4(held[0], held[1], held[2], held[3]);
+            }
+        }
+    }
+}
+
+template <int D>
+cudaError_t launch_append(const AppendParams& p, cudaStream_t stream)
+{
+    // four rows share the look-up of their places where there are rows enough for all SMs
+    if (p.r.rows >= 4096) return launch_early(append_kernel<D, 4>, dim3(static_cast<unsigned>((p.r.rows + 3) / 4)), kThreads, 0, stream, p);
+    return launch_early(append_kernel<D, 1>, dim3(static_cast<unsigned>(p.r.rows)), kThreads, 0, stream, p);
 }
 
 }  // namespace
@@ -135,9 +174,8 @@ extern "C" polyspec_status polyspec_cache_append(const polyspec_cache_pages* s, 
     p.page_bytes = kv::page_bytes(*s, kv_heads, head_dim);
     p.k_held = static_cast<__nv_bfloat16*>(k_held); p.v_held = static_cast<__nv_bfloat16*>(v_held);
     p.weights = weights; p.status = device_status; p.kv_heads = kv_heads;
-    const dim3 grid(static_cast<unsigned>(r->rows));
+    if (s->n_pages * (p.page_bytes / kv::unit_bytes(head_dim)) >= 0xffffffffull) return POLYSPEC_ERR_UNSUPPORTED;       // units of a plane are counted in 32 bits
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    const cudaError_t e = head_dim == 128 ? launch_early(append_kernel<128>, grid, kThreads, 0, stream, p)
-                                          : launch_early(append_kernel<64>, grid, kThreads, 0, stream, p);
+    const cudaError_t e = head_dim == 128 ? launch_append<128>(p, stream) : launch_append<64>(p, stream);
     return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }

@@ -3,9 +3,12 @@
 //
 // Two launches.  The first, one CTA per sequence, finds the weight of the last token that stays (radix selection over the weights' bits,
 // four passes of eight bits), lists the slots that stay in order, moves the weights, gives pages back.  The second moves the contents:
-// a CTA per sequence, plane and head goes through the kept tokens in order, kBatch at a time.  A token never moves up, so a batch that has been
+// a CTA per sequence, head and run of planes goes through the kept tokens in order, kBatch at a time.  A token never moves up, so a batch that has been
 // read before it is written overwrites nothing that a later batch reads.
 // Moving is HBM-bound: each token that moves is read and written once.
+#include <algorithm>
+#include <type_traits>
+
 #include "kv_pages.cuh"
 
 namespace polyspec {
@@ -13,6 +16,7 @@ namespace {
 
 constexpr int kSelectThreads = 1024;
 constexpr int kMoveThreads = 256;
+constexpr int kKeyRoom = 49152;                 // longest cache whose weights are held in shared memory
 
 struct EvictPlan {
     int32_t* head;          // [n_seqs, 4]: first new slot whose token moves, tokens kept (0: sequence stays as it is)
@@ -79,8 +83,9 @@ __device__ __forceinline__ int2 block_exclusive2(int2 x, int2* sums /* shared, 3
 }
 
 __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const polyspec_cache_pages s, const int32_t* budgets, int first, int recent,
-                                                                         float* weights, EvictPlan plan, int32_t* kept_from, int32_t* status)
+                                                                         float* weights, EvictPlan plan, int32_t* kept_from, int32_t* status, int key_room)
 {
+    extern __shared__ uint32_t keys[];          // of the slots, where there is room for all
     __shared__ int hist[256];
     __shared__ int2 sums[32];
     __shared__ uint32_t prefix;
@@ -102,6 +107,13 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
         for (size_t i = tid; i < cap; i += kSelectThreads) kept_from[b * cap + i] = -1;
     if (stays) return;
 
+    const bool in_keys = len <= key_room;
+    if (in_keys) {
+        for (int i = tid; i < len; i += kSelectThreads) keys[i] = weight_key(w[i]);
+        __syncthreads();
+    }
+    auto key_of = [&](int i) { return in_keys ? keys[i] : weight_key(w[i]); };
+
     // of the slots first .. len - recent - 1 the `need` heaviest stay
     const int end = len - recent, need = budget - first - recent;
     uint32_t bits = 0;                          // the leading bits of the last one's weight, as far as they are known
@@ -110,7 +122,7 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
         if (tid < 256) hist[tid] = 0;
         __syncthreads();
         for (int i = first + tid; i < end; i += kSelectThreads) {
-            const uint32_t key = weight_key(w[i]);
+            const uint32_t key = key_of(i);
             if (shift == 24 || key >> (shift + 8) == bits) {
                 // (weights of one size share their leading bits: one add per warp and digit)
                 const uint32_t digit = key >> shift & 255u, peers = __match_any_sync(__activemask(), digit);
@@ -148,7 +160,7 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
     const int i0 = min(len, tid * per), i1 = min(len, i0 + per);
     auto state = [&](int i) {                   // 2 stays, 1 equal, 0 goes
         if (i < first || i >= end) return 2;
-        const uint32_t key = weight_key(w[i]);
+        const uint32_t key = key_of(i);
         return key > bits ? 2 : key == bits && need > 0 ? 1 : 0;
     };
     int2 mine = make_int2(0, 0), total;
@@ -206,75 +218,73 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
     }
 }
 
-// D: head_dim.  blockIdx.x: head and plane, blockIdx.y: sequence.
+// D: head_dim.  blockIdx.x: key head and a run of planes, blockIdx.y: sequence.  Where a batch's tokens come from and go to is found once for all of the
+// CTA's planes (divisions by the page's size took more time than the copies), a batch ahead of its use.
 template <int D>
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec_cache_pages s, EvictPlan plan, unsigned char* pool, size_t page_bytes,
-                                                                  int kv_heads)
+                                                                  int kv_heads, int n_planes, int run)
 {
     constexpr int kBatch = kMoveThreads;        // tokens at a time
     constexpr int kPieces = D / 32;             // 16-byte pieces of a token's codes
-    const int b = blockIdx.y, plane = blockIdx.x / kv_heads, head = blockIdx.x % kv_heads, tid = threadIdx.x;
-    const bool values = plane & 1;
+    constexpr int UB = kv::unit_bytes(D);
+    using Piece = typename std::conditional<D == 128, uint2, uint32_t>::type;         // the D / 64 words of one group of lanes
+    __shared__ uint2 places[2][2][kBatch];      // [turn][from, to]: unit of the plane, token of the unit
+    const int b = blockIdx.y, head = blockIdx.x % kv_heads, plane0 = blockIdx.x / kv_heads * run, planes = min(run, n_planes - plane0), tid = threadIdx.x;
     const int P = s.page_tokens, units = P / kv::kUnit;
     const size_t cap = static_cast<size_t>(s.max_pages) * P;
     const int32_t* from = plan.from + b * cap;
     const int32_t* pages = plan.pages + static_cast<size_t>(b) * s.max_pages;
-    unsigned char* data = pool + static_cast<size_t>(plane) * s.n_pages * page_bytes;
     wait_for_stream();
     const int begin = plan.head[4 * b], end = plan.head[4 * b + 1];
-    auto unit_of = [&](int slot) {
-        return data + pages[slot / P] * page_bytes + static_cast<size_t>(head * units + slot % P / kv::kUnit) * kv::unit_bytes(D);
+    if (begin >= end) return;
+    auto place = [&](int slot) {
+        const int unit = slot / kv::kUnit, at = unit / units;
+        return make_uint2((static_cast<uint32_t>(pages[at]) * kv_heads + head) * units + (unit - at * units), slot % kv::kUnit);
     };
-    for (int i0 = begin; i0 < end; i0 += kBatch) {
-        const int n = min(kBatch, end - i0);
-        if (!values) {
-            uint4 x[kPieces];
-            uint32_t pair = 0;
-#pragma unroll
-            for (int u = 0; u < kPieces; ++u) {
-                const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
-                if (t < n) {
-                    const int slot = from[i0 + t];
-                    x[u] = reinterpret_cast<const uint4*>(unit_of(slot))[slot % kv::kUnit * kPieces + part];
-                }
-            }
-            if (tid < n) {
-                const int slot = from[i0 + tid];
-                pair = reinterpret_cast<const uint32_t*>(unit_of(slot))[D + slot % kv::kUnit];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u < kPieces; ++u) {
-                const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
-                if (t < n) reinterpret_cast<uint4*>(unit_of(i0 + t))[(i0 + t) % kv::kUnit * kPieces + part] = x[u];
-            }
-            if (tid < n) reinterpret_cast<uint32_t*>(unit_of(i0 + tid))[D + (i0 + tid) % kv::kUnit] = pair;
-        } else {
-            // the D / 64 words of one group of lanes: (8 h + g, token) for all h
-            using Piece = typename std::conditional<D == 128, uint2, uint32_t>::type;
-            Piece x[8];
-            uint32_t pair = 0;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int item = u * kMoveThreads + tid, t = item / 8, g = item % 8;
-                if (t < n) {
-                    const int slot = from[i0 + t];
-                    x[u] = reinterpret_cast<const Piece*>(unit_of(slot))[8 * g + slot % kv::kUnit];
-                }
-            }
-            if (tid < n) {
-                const int slot = from[i0 + tid];
-                pair = reinterpret_cast<const uint32_t*>(unit_of(slot))[D + slot % kv::kUnit];
-            }
-            __syncthreads();
-#pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int item = u * kMoveThreads + tid, t = item / 8, g = item % 8;
-                if (t < n) reinterpret_cast<Piece*>(unit_of(i0 + t))[8 * g + (i0 + t) % kv::kUnit] = x[u];
-            }
-            if (tid < n) reinterpret_cast<uint32_t*>(unit_of(i0 + tid))[D + (i0 + tid) % kv::kUnit] = pair;
+    auto find = [&](int turn, int i) {
+        if (i + tid < end) {
+            places[turn][0][tid] = place(from[i + tid]);
+            places[turn][1][tid] = place(i + tid);
         }
-        __syncthreads();
+    };
+    find(0, begin);
+    __syncthreads();
+    int turn = 0;
+    for (int i0 = begin; i0 < end; i0 += kBatch, turn ^= 1) {
+        const int n = min(kBatch, end - i0);
+        const uint2 (*at)[kBatch] = places[turn];
+        for (int k = 0; k < planes; ++k) {
+            unsigned char* data = pool + static_cast<size_t>(plane0 + k) * s.n_pages * page_bytes;
+            auto unit = [&](int which, int t) { return data + static_cast<size_t>(at[which][t].x) * UB; };
+            uint32_t pair = 0;
+            if (tid < n) pair = reinterpret_cast<const uint32_t*>(unit(0, tid))[D + at[0][tid].y];
+            if (k == 0) find(turn ^ 1, i0 + kBatch);
+            if (!((plane0 + k) & 1)) {
+                uint4 x[kPieces];
+#pragma unroll
+                for (int u = 0; u < kPieces; ++u) {
+                    const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
+                    if (t < n) x[u] = reinterpret_cast<const uint4*>(unit(0, t))[at[0][t].y * kPieces + part];
+                }
+                __syncthreads();                // everything of the batch has been read
+#pragma unroll
+                for (int u = 0; u < kPieces; ++u) {
+                    const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
+                    if (t < n) reinterpret_cast<uint4*>(unit(1, t))[at[1][t].y * kPieces + part] = x[u];
+                }
+            } else {
+                Piece x[8];
+#pragma unroll
+                for (int u = 0; u < 8; ++u) {   // neighbouring lanes have neighbouring tokens: a group's words of a unit are neighbours
+                    if (tid < n) x[u] = reinterpret_cast<const Piece*>(unit(0, tid))[8 * u + at[0][tid].y];
+                }
+                __syncthreads();
+#pragma unroll
+                for (int u = 0; u < 8; ++u)
+                    if (tid < n) reinterpret_cast<Piece*>(unit(1, tid))[8 * u + at[1][tid].y] = x[u];
+            }
+            if (tid < n) reinterpret_cast<uint32_t*>(unit(1, tid))[D + at[1][tid].y] = pair;
+        }
     }
 }
 
@@ -303,18 +313,26 @@ polyspec_status polyspec_cache_evict(const polyspec_cache_pages* s, const int32_
     if (!budget || first < 0 || recent < 0 || !weights || !pool || !kv::aligned16(pool) || n_planes < 2 || n_planes % 2) return POLYSPEC_ERR_INVALID_ARG;
     if (!aligned4(budget, weights, kept_from, device_status)) return POLYSPEC_ERR_INVALID_ARG;
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return POLYSPEC_ERR_INVALID_ARG;
+    if (s->n_pages * (kv::page_bytes(*s, kv_heads, head_dim) / kv::unit_bytes(head_dim)) >= 0xffffffffull) return POLYSPEC_ERR_UNSUPPORTED;
     if (s->n_seqs > 65535 || static_cast<long long>(n_planes) * kv_heads > 0x7fffffffLL) return POLYSPEC_ERR_UNSUPPORTED;
     if (workspace_bytes < evict_bytes(s->n_seqs, s->max_pages, s->page_tokens)) return POLYSPEC_ERR_WORKSPACE;
     const EvictPlan plan = evict_plan(workspace, s->n_seqs, s->max_pages, s->page_tokens);
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    cudaError_t e = launch_early(evict_select_kernel, dim3(static_cast<unsigned>(s->n_seqs)), kSelectThreads, 0, stream, *s, budget, first, recent,
-                                 weights, plan, kept_from, device_status);
+    const size_t cap = static_cast<size_t>(s->max_pages) * s->page_tokens;
+    const int room = cap <= kKeyRoom ? static_cast<int>(cap) : 0;
+    cudaError_t e = cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kKeyRoom * 4);
+    if (e == cudaSuccess)
+        e = launch_early(evict_select_kernel, dim3(static_cast<unsigned>(s->n_seqs)), kSelectThreads, static_cast<size_t>(room) * 4, stream, *s, budget, first,
+                         recent, weights, plan, kept_from, device_status, room);
     if (e == cudaSuccess) {
-        const dim3 grid(static_cast<unsigned>(n_planes * kv_heads), static_cast<unsigned>(s->n_seqs));
+        // planes per CTA: as many as leave some thousand CTAs
+        const long long all = static_cast<long long>(n_planes) * kv_heads * s->n_seqs;
+        const int run = static_cast<int>(std::max<long long>(1, std::min<long long>(n_planes, all / 2048)));
+        const dim3 grid(static_cast<unsigned>((n_planes + run - 1) / run * kv_heads), static_cast<unsigned>(s->n_seqs));
         unsigned char* data = static_cast<unsigned char*>(pool);
         const size_t bytes = kv::page_bytes(*s, kv_heads, head_dim);
-        e = head_dim == 128 ? launch_early(evict_move_kernel<128>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads)
-                            : launch_early(evict_move_kernel<64>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads);
+        e = head_dim == 128 ? launch_early(evict_move_kernel<128>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads, n_planes, run)
+                            : launch_early(evict_move_kernel<64>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads, n_planes, run);
     }
     return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }

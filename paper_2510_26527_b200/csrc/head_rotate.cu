@@ -58,31 +58,48 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
     const bool turned = chunk * 8 < p.rotary, halves = turned && !p.interleaved;
     const int v0 = halves ? at : chunk, v1 = halves ? at + half : chunk + 1;
     wait_for_stream();
-    if (row >= p.rows) return;
+    if (row >= p.rows) return;                  // (whole warps)
 
     float c[8], s[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) { c[i] = 1.0f; s[i] = 0.0f; }
-    if (turned && mine) {
+    if (p.rotary) {
+        // the lanes that stand at one place of different heads share its eight angles
+        constexpr int kOwn = kHeads < 8 ? 8 / kHeads : 1;
         const double turns = static_cast<double>(p.positions[row]) * 0.15915494309189533577;       // 1 / 2 pi
+        float cs[kOwn], sn[kOwn];
+#pragma unroll
+        for (int i = 0; i < kOwn; ++i) {
+            const int k = at * 8 + (slot * kOwn + i) % 8;
+            const double x = turns * p.frequencies[min(k, p.rotary / 2 - 1)];
+            sincospif(2.0f * static_cast<float>(x - rint(x)), &sn[i], &cs[i]);
+        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const double x = turns * p.frequencies[at * 8 + i];
-            sincospif(2.0f * static_cast<float>(x - rint(x)), &s[i], &c[i]);
+            const float a = __shfl_sync(0xffffffffu, cs[i % kOwn], i / kOwn * L + at), b = __shfl_sync(0xffffffffu, sn[i % kOwn], i / kOwn * L + at);
+            if (turned) { c[i] = a; s[i] = b; }
         }
     }
     const int heads = p.q_heads + p.kv_heads;
+    auto load = [&](int h, uint4& r0, uint4& r1) {
+        r0 = r1 = make_uint4(0, 0, 0, 0);
+        if (mine && h < heads) {
+            const bool is_q = h < p.q_heads;
+            const uint4* x = reinterpret_cast<const uint4*>((is_q ? p.q + row * p.q_stride + h * p.head_dim : p.k + row * p.k_stride + (h - p.q_heads) * p.head_dim));
+            r0 = x[v0];
+            r1 = x[v1];
+        }
+    };
+    uint4 r0, r1, n0, n1;                       // the heads at hand, the next ones
+    load(part * kHeads + slot, n0, n1);
     for (int h0 = part * kHeads; h0 < heads; h0 += p.parts * kHeads) {
         const int h = h0 + slot;
         const bool live = mine && h < heads, is_q = h < p.q_heads;
         const __nv_bfloat16* weight = is_q ? p.q_weight : p.k_weight;
         const int head = is_q ? h : h - p.q_heads;
-        uint4 r0 = make_uint4(0, 0, 0, 0), r1 = r0;
-        if (live) {
-            const uint4* x = reinterpret_cast<const uint4*>((is_q ? p.q + row * p.q_stride : p.k + row * p.k_stride) + head * p.head_dim);
-            r0 = x[v0];
-            r1 = x[v1];
-        }
+        r0 = n0;
+        r1 = n1;
+        load(h + p.parts * kHeads, n0, n1);
         float a[8], b[8];
         unpack(r0, a);
         unpack(r1, b);

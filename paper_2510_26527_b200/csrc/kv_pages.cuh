@@ -54,18 +54,6 @@ __device__ __forceinline__ SeqRows seq_rows(const polyspec_cache_pages& s, const
     return q;
 }
 
-// The sequence that row `row` lies in, or -1: the last one that begins at or before it, if the rows begin in order.  Every thread of
-// the CTA calls it; `found` is a shared word.
-__device__ __forceinline__ int find_seq(const int32_t* rows_at, int n_seqs, int row, int* found)
-{
-    if (threadIdx.x == 0) *found = -1;
-    __syncthreads();
-    for (int b = threadIdx.x; b < n_seqs; b += blockDim.x)
-        if (rows_at[b] <= row && row < rows_at[b + 1]) atomicMax(found, b);
-    __syncthreads();
-    return *found;
-}
-
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 // Rows of heads: stride at least a row, a multiple of eight elements, 16-byte aligned.
