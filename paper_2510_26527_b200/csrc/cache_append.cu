@@ -116,19 +116,36 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
             float scale = up ? __uint_as_float(up) : 1.0f;
             const bool broken = (bad & mates) || !(range <= 3.4e38f);
             if (broken) scale = offset = __uint_as_float(0x7fc00000u);
+            const float inv = __frcp_rn(scale), near = scale * 0.49999f;
             uint32_t word = 0, held[4];
             float y[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int code = broken ? 0 : min(15, static_cast<int>(rintf(__fdiv_rn(x[e] - offset, scale))));
-                word |= static_cast<uint32_t>(code) << (4 * (e / 2) + 16 * (e % 2));
-                y[e] = __fadd_rn(__fmul_rn(scale, static_cast<float>(code)), offset);
+                // the nearest whole number, by adding 1.5 * 2^23; the quotient itself is only divided out where the remainder says that it is near the
+                // middle between two
+                const float a = x[e] - offset;
+                float t = __fadd_rn(__fmul_rn(a, inv), 12582912.0f), code = t - 12582912.0f;
+                if (!(fabsf(fmaf(-code, scale, a)) <= near)) {
+                    t = __fadd_rn(__fdiv_rn(a, scale), 12582912.0f);
+                    code = t - 12582912.0f;
+                }
+                word |= (__float_as_uint(t) & 15u) << (4 * (e / 2) + 16 * (e % 2));
+                y[e] = __fadd_rn(__fmul_rn(scale, code), offset);
             }
+            if (broken) {
+                word = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = scale;
+            }
+            // words 8 h + g of a row's values are neighbours for all h: lanes of lower words store both
+            const uint32_t other = __shfl_xor_sync(0xffffffffu, word, 8);
             if (!live) continue;
             unsigned char* plane = p.pool + (values ? static_cast<size_t>(p.s.n_pages) * p.page_bytes : 0);
             uint32_t* to = reinterpret_cast<uint32_t*>(plane + static_cast<size_t>(units[i] + static_cast<uint32_t>(head * per_page)) * kv::unit_bytes(D));
             const int r = tokens[i];
-            to[values ? kv::value_word(r, w, D) : kv::key_word(r, w, D)] = word;
+            if (!values) to[kv::key_word(r, w, D)] = word;
+            else if (D == 64) to[kv::value_word(r, w, D)] = word;
+            else if (w < 8) *reinterpret_cast<uint2*>(to + kv::value_word(r, w, D)) = make_uint2(word, other);
             if (w == 0) to[D + r] = (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
             __nv_bfloat16* out = values ? p.v_held : p.k_held;
             if (out) {

@@ -125,6 +125,14 @@ __device__ __forceinline__ void store_fragment(uint32_t* frag, int r, int word, 
     to[32] = make_uint2(half2_bits(x[4] * by, x[5] * by), half2_bits(x[6] * by16, x[7] * by16));
 }
 
+// The power of two that brings numbers of up to `top` in size into [2^14, 2^15), and what their products with codes (which bring 2^-24) are to be multiplied with.
+__device__ __forceinline__ float row_scale(const AttendParams& p, float top, float* factor)
+{
+    const int k = top > 0.0f ? max(-100, static_cast<int>(__float_as_uint(top) >> 23) - 127) : 0;          // top in [2^k, 2^(k+1))
+    *factor = p.scale_log2 * __uint_as_float(static_cast<uint32_t>(min(254, 10 + k + 127)) << 23);
+    return __uint_as_float(static_cast<uint32_t>(14 - k + 127) << 23);
+}
+
 // The rows of a tile into shared memory, by all THREADS of a CTA: rows row0 .. row0 + ROWS - 1 of (row of the block, head of the group), zeros from
 // `end` on.  sums[r] = scale * log2(e) * sum of the row; *factor = what a product of fragments and codes is multiplied with.  Ends with the CTA in step.
 template <int D, int ROWS, int THREADS>
@@ -154,10 +162,7 @@ __device__ __forceinline__ void load_rows(const AttendParams& p, const kv::SeqRo
     __syncthreads();
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) top = fmaxf(top, warp_max[w]);
-    // top in [2^k, 2^(k+1)): by 2^(14-k) into [2^14, 2^15); codes bring 2^-24
-    const int k = top > 0.0f ? max(-100, static_cast<int>(__float_as_uint(top) >> 23) - 127) : 0;
-    const float by = __uint_as_float(static_cast<uint32_t>(14 - k + 127) << 23);
-    *factor = p.scale_log2 * __uint_as_float(static_cast<uint32_t>(min(254, 10 + k + 127)) << 23);
+    const float by = row_scale(p, top, factor);
 #pragma unroll
     for (int u = 0; u < kPer; ++u) {
         const int item = u * THREADS + threadIdx.x, r = item / kVecs;
@@ -796,16 +801,17 @@ struct WeighParams {
     float* weights;
 };
 
-constexpr int kWeighWarps = 8, kWeighTokens = kWeighWarps * 16;
+constexpr int kWeighWarps = 8, kWeighTokens = kWeighWarps * 16, kWeighGroups = 16;
 
-// A CTA has 128 tokens of a sequence, a warp 16 of them: keys only, once per head, the products as in attend_kernel.  Sums stay in a lane's registers
-// over all heads and rows; the lanes of one token meet at the end.  So every sum has one order.
+// A CTA has 128 tokens of a sequence, a warp 16 of them: keys only, the products as in attend_kernel.  The rows of all heads come in chunks of 16
+// groups of 8 (as many heads as that holds), so that the CTA seldom has to meet; a head's keys are loaded while the one before is multiplied.
+// Sums stay in a lane's registers over all heads and rows; the lanes of one token meet at the end.  So every sum has one order.
 template <int D>
 __global__ void __launch_bounds__(kWeighWarps * 32) weigh_kernel(const WeighParams w)
 {
-    constexpr int KS = D / 16, UB = kv::unit_bytes(D), WORDS = D / 32, NT = 4, ROWS = NT * 8, THREADS = kWeighWarps * 32;
-    __shared__ __align__(16) uint32_t frag[NT * KS * 64];
-    __shared__ float warp_max[kWeighWarps], sums[ROWS];
+    constexpr int KS = D / 16, UB = kv::unit_bytes(D), WORDS = D / 32, G = kWeighGroups, THREADS = kWeighWarps * 32, kVecs = D / 8;
+    __shared__ __align__(16) uint32_t frag[G * KS * 64];
+    __shared__ __align__(16) float4 of_row[G * 8];             // factor, scaled sum, logarithm of the denominator (base 2), first slot it does not see
     const AttendParams& p = w.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g8 = lane >> 2, t4 = lane & 3, b = blockIdx.y;
     wait_for_stream();
@@ -824,51 +830,87 @@ __global__ void __launch_bounds__(kWeighWarps * 32) weigh_kernel(const WeighPara
             else if (lane == 0) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
         }
     }
-    float acc[2] = {0.0f, 0.0f};                // tokens g8, g8 + 8
-    const int rows = q.granted * p.group;
-    for (int head = 0; head < p.kv_heads; ++head) {
-        // the head's keys stay in registers over its rows
-        uint32_t kw[2][WORDS], kp[2] = {0, 0};
+    const int rows = q.granted * p.group, head_groups = (rows + 7) / 8, groups = head_groups * p.kv_heads;        // a head's rows in groups of 8
+    // the next head's keys; zeros where there are none
+    uint32_t next[2][WORDS], next_pair[2];
+    auto load_keys = [&](int head) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
+            next_pair[u] = 0;
 #pragma unroll
-            for (int i = 0; i < WORDS; ++i) kw[u][i] = 0;
-            if (unit[u] != 0xffffffffu) {
+            for (int i = 0; i < WORDS; ++i) next[u][i] = 0;
+            if (unit[u] != 0xffffffffu && head < p.kv_heads) {
                 const unsigned char* at = p.pool + (static_cast<size_t>(unit[u]) + static_cast<size_t>(head) * p.units_per_page) * UB;
 #pragma unroll
                 for (int i = 0; i < WORDS; i += 2) {
                     const uint2 x = *reinterpret_cast<const uint2*>(at + lane * (WORDS * 4) + i * 4);
-                    kw[u][i] = x.x; kw[u][i + 1] = x.y;
+                    next[u][i] = x.x; next[u][i + 1] = x.y;
                 }
-                kp[u] = *reinterpret_cast<const uint32_t*>(at + 4 * D + g8 * 4);
+                next_pair[u] = *reinterpret_cast<const uint32_t*>(at + 4 * D + g8 * 4);
             }
         }
-        for (int row0 = 0; row0 < rows; row0 += ROWS) {
+    };
+    if (groups) load_keys(0);
+    uint32_t kw[2][WORDS], kp[2];
+    float acc[2] = {0.0f, 0.0f};                // tokens g8, g8 + 8
+    int head = -1;
+    for (int group0 = 0; group0 < groups; group0 += G) {
+        const int n_groups = min(G, groups - group0);
+        __syncthreads();                        // the rows of the chunk before have been read
+        // a row per kVecs lanes: into fragments, scaled by a power of two of its own into fp16's upper range
+        for (int item = threadIdx.x; item < n_groups * 8 * kVecs; item += THREADS) {
+            const int n = item / (8 * kVecs), r = item / kVecs & 7, h = (group0 + n) / head_groups, row = (group0 + n) % head_groups * 8 + r;
+            const int i = row / p.group, of = h * p.group + row % p.group;
+            uint4 raw = make_uint4(0, 0, 0, 0);
+            float lse = 0.0f;
+            if (row < rows) {
+                raw = *reinterpret_cast<const uint4*>(p.q + (q.row0 + i) * p.q_stride + of * D + item % kVecs * 8);
+                lse = w.lse[static_cast<size_t>(q.row0 + i) * p.q_heads + of] * 1.44269504088896340736f;
+            }
+            const uint32_t* y = reinterpret_cast<const uint32_t*>(&raw);
+            float x[8], sum = 0.0f, top = 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { x[2 * e] = low(y[e]); x[2 * e + 1] = high(y[e]); sum += x[2 * e] + x[2 * e + 1]; }
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (fabsf(x[e]) <= 3.4e38f) top = fmaxf(top, fabsf(x[e]));
+#pragma unroll
+            for (int d = 1; d < kVecs; d <<= 1) {
+                sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            }
             float factor;
-            __syncthreads();                    // the rows of the tile before have been read
-            load_rows<D, ROWS, THREADS>(p, q, head, row0, rows, frag, sums, warp_max, &factor);
+            const float by = row_scale(p, top, &factor);
+            store_fragment<D>(frag, n * 8 + r, item % kVecs, x, by);
+            if (item % kVecs == 0) of_row[n * 8 + r] = make_float4(factor, sum * p.scale_log2, lse, __int_as_float(row < rows ? row_limit(q, i) : 0));
+        }
+        __syncthreads();
+        for (int n = 0; n < n_groups; ++n) {
+            const int h = (group0 + n) / head_groups;
+            if (h != head) {
+                head = h;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if (row0 + n * 8 >= rows) break;
-                float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                for (int u = 0; u < 2; ++u) {
+                    kp[u] = next_pair[u];
 #pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const uint2 x = reinterpret_cast<const uint2*>(frag)[(n * KS + s) * 32 + lane];
-                    mma(sc, code_pair(kw[0][s >> 1], 2 * (s & 1)), code_pair(kw[1][s >> 1], 2 * (s & 1)), code_pair(kw[0][s >> 1], 2 * (s & 1) + 1),
-                        code_pair(kw[1][s >> 1], 2 * (s & 1) + 1), x.x, x.y);
+                    for (int i = 0; i < WORDS; ++i) kw[u][i] = next[u][i];
                 }
+                load_keys(head + 1);
+            }
+            float sc[4] = {0.0f, 0.0f, 0.0f, 0.0f}, sd[4] = {0.0f, 0.0f, 0.0f, 0.0f};         // (two chains of products)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int r = row0 + n * 8 + 2 * t4 + j, row = r / p.group;
-                    if (r >= rows) continue;
-                    const int limit = row_limit(q, row);
-                    const float lse = w.lse[static_cast<size_t>(q.row0 + row) * p.q_heads + head * p.group + r % p.group] * 1.44269504088896340736f;
-                    const float sq = sums[n * 8 + 2 * t4 + j];
+            for (int s = 0; s < KS; ++s) {
+                const uint2 x = reinterpret_cast<const uint2*>(frag)[(n * KS + s) * 32 + lane];
+                mma(s & 1 ? sd : sc, code_pair(kw[0][s >> 1], 2 * (s & 1)), code_pair(kw[1][s >> 1], 2 * (s & 1)), code_pair(kw[0][s >> 1], 2 * (s & 1) + 1),
+                    code_pair(kw[1][s >> 1], 2 * (s & 1) + 1), x.x, x.y);
+            }
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const float x = fmaf(sc[2 * u + j], low(kp[u]) * factor, sq * high(kp[u]));
-                        if (unit[u] != 0xffffffffu && key0 + 8 * u + g8 < limit) acc[u] += ex2(x - lse);
-                    }
+            for (int j = 0; j < 2; ++j) {
+                const float4 row = of_row[n * 8 + 2 * t4 + j];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float x = fmaf(sc[2 * u + j] + sd[2 * u + j], low(kp[u]) * row.x, fmaf(row.y, high(kp[u]), -row.z));
+                    if (unit[u] != 0xffffffffu && key0 + 8 * u + g8 < __float_as_int(row.w)) acc[u] += ex2(x);
                 }
             }
         }
