@@ -755,11 +755,6 @@ polyspec_status fill(AttendParams* p, const polyspec_cache_pages* s, const polys
     p->pool = static_cast<const unsigned char*>(pool);
     p->plane_bytes = bytes * s->n_pages;
     p->units_per_page = s->page_tokens / kv::kUnit;
-    // with 2^k >= units_per_page the product's error stays below 2^28 * 2^k, one unit of the shifted-out part
-    int k = 0;
-    while ((1 << k) < p->units_per_page) ++k;
-    p->div_shift = 28 + k;
-    p->div_magic = ((1ull << p->div_shift) + p->units_per_page - 1) / p->units_per_page;
     p->status = device_status;
     p->out = nullptr; p->lse = nullptr; p->partial = nullptr; p->joins = nullptr;
     return POLYSPEC_OK;

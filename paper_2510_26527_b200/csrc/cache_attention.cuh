@@ -23,8 +23,7 @@ struct AttendParams {
     float scale_log2;                           // scale * log2(e)
     const unsigned char* pool;
     size_t plane_bytes;
-    int units_per_page, div_shift;
-    unsigned long long div_magic;               // unit / units_per_page = unit * div_magic >> div_shift, for units below 2^28
+    int units_per_page;
     unsigned short* out;
     float* lse;
     float* partial;                             // [2 * CTAs][rows of a tile][head_dim + 2]

@@ -16,9 +16,6 @@
 //   12-19  softmax, a thread per token and every other group of 8 rows; at the end of a part the output, a thread per element
 // What bounds it is shared memory: per step 32 KB of values written and read, queries and weights, some 900 cycles of its 128 bytes per cycle.
 #include <cuda.h>
-#ifndef KA
-#define KA 2
-#endif
 
 #include "cache_attention.cuh"
 #include "tensor_device.cuh"
@@ -34,8 +31,7 @@ struct Wide {
     static constexpr int OVERHEAD = 4;          // steps' worth of work that a segment costs besides its steps
     static constexpr int PART = ROWS * (D + 2);
     static constexpr uint32_t QBOX = ROWS * 128, QTILE = 2 * QBOX, VBOX = 128 * 128, VTILE = 2 * VBOX, PTILE = 128 * 128;
-    static constexpr int PITCH = 132;           // floats of a row of the scratch: tokens, and room so that rows start in different banks
-    static constexpr size_t SMEM = 1024 + 2 * (QTILE + VTILE + PTILE) + 2 * ROWS * PITCH * 4;
+    static constexpr size_t SMEM = 1024 + 2 * (QTILE + VTILE + PTILE);
     // tensor memory: two blocks of keys, two of scores, the output
     static constexpr uint32_t KCOLS = 64, S0 = 128, SCOLS = 64, O0 = 256, COLS = 512;
 };
@@ -118,14 +114,11 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
 struct Units {
     const int32_t* table;
     uint32_t head_unit, page_units;             // of the page's units the head's first; units of a page over all heads
-    unsigned long long magic;                   // unit / per_page as a product, exact for all units of a table
-    int per_page, n_pages, seen, shift;
+    int per_page, n_pages, seen;
     __device__ __forceinline__ void start(const AttendParams& p, const Part& part)
     {
         table = p.s.table + static_cast<size_t>(part.b) * p.s.max_pages;
         per_page = p.units_per_page;
-        magic = p.div_magic;
-        shift = p.div_shift;
         n_pages = p.s.n_pages;
         head_unit = static_cast<uint32_t>(part.head) * per_page;
         page_units = static_cast<uint32_t>(p.kv_heads) * per_page;
@@ -135,7 +128,7 @@ struct Units {
     __device__ __forceinline__ int2 look(long long slot) const
     {
         if (slot >= seen) return make_int2(0, -1);
-        const int unit = static_cast<int>(slot >> 3), at = static_cast<int>(unit * magic >> shift);
+        const int unit = static_cast<int>(slot >> 3), at = unit / per_page;
         return make_int2(table[at], unit - at * per_page);
     }
     __device__ __forceinline__ bool broken(int2 x) const { return x.y >= 0 && (x.x < 0 || x.x >= n_pages); }
@@ -154,13 +147,12 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
     __shared__ long long warp_sums[S::WARPS], hit_at;
     __shared__ Part parts[2];
     __shared__ __align__(16) float sums[2][S::ROWS], refs[S::ROWS];            // read four at a time
-    __shared__ float factors[2], ups[S::ROWS], bys[S::ROWS], total_l[S::ROWS], total_o[S::ROWS];
+    __shared__ float factors[2], tops[4][S::ROWS], parts_l[4][S::ROWS], parts_o[4][S::ROWS];
     __shared__ int limits[2][S::ROWS];
     __shared__ long long places[2][S::ROWS];    // of the rows, in [rows, q_heads]
     __shared__ __align__(8) uint64_t barriers[Bars::kCount];
     const int warp = __shfl_sync(0xffffffffu, static_cast<int>(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t q_tiles = (smem_addr(smem_wide) + 1023u) & ~1023u, v_tiles = q_tiles + 2 * S::QTILE, p_tiles = v_tiles + 2 * S::VTILE;
-    float* scratch = reinterpret_cast<float*>(smem_wide + (p_tiles + 2 * S::PTILE - smem_addr(smem_wide)));       // [2][rows][PITCH]
     const uint32_t bars = smem_addr(barriers);
     auto bar = [&](int n) { return bars + 8u * n; };
 
@@ -369,7 +361,7 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
     } else if (warp < 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
         const int quarter = warp & 3;
-        constexpr int kAhead = KA;              // steps whose codes are on their way
+        constexpr int kAhead = 3;               // steps whose codes are on their way
         if (warp < 8) {
             // ------------------------------------------------------------------ keys, a thread per token
             const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
@@ -379,7 +371,7 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
                 Units units;
                 units.start(p, part);
                 const int token = quarter * 32 + lane;
-                uint4 x[kAhead + 1][4];         // the step at hand and the next ones
+                uint4 x[kAhead][4];
                 int2 next = make_int2(0, -1);
                 auto look = [&](int j) { return j < part.steps ? units.look(static_cast<long long>(part.step0 + j) * 128 + token) : make_int2(0, -1); };
                 auto load = [&](uint4* to, int j) {
@@ -392,28 +384,29 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
                 next = look(0);
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) load(x[u], u);
-#pragma unroll 1
-                for (int j = 0; j < part.steps; ++j, ++n) {
-                    const uint32_t at = n & 1, use = n >> 1 & 1;
-                    load(x[kAhead], j + kAhead);
-                    if (!warp_wait(bar(Bars::kKFree + at), use ^ 1, abort_p)) { ok = false; break; }
-                    tc_fence_after();
+                for (int j0 = 0; j0 < part.steps && ok; j0 += kAhead) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t words[4] = {x[0][i].x, x[0][i].y, x[0][i].z, x[0][i].w};
-                        uint32_t y[16];
+                    for (int u = 0; u < kAhead; ++u) {
+                        if (j0 + u >= part.steps) break;
+                        const uint32_t at = n & 1, use = n >> 1 & 1;
+                        if (!warp_wait(bar(Bars::kKFree + at), use ^ 1, abort_p)) { ok = false; break; }
+                        tc_fence_after();
 #pragma unroll
-                        for (int w = 0; w < 16; ++w) y[w] = code_pair(words[w >> 2], w & 3);
-                        tmem_st16(tmem + at * S::KCOLS + lanes + i * 16, y);
+                        for (int i = 0; i < 4; ++i) {
+                            const uint4 v = x[u][i];
+                            const uint32_t words[4] = {v.x, v.y, v.z, v.w};
+                            uint32_t y[16];
+#pragma unroll
+                            for (int w = 0; w < 16; ++w) y[w] = code_pair(words[w >> 2], w & 3);
+                            tmem_st16(tmem + at * S::KCOLS + lanes + i * 16, y);
+                        }
+                        load(x[u], j0 + u + kAhead);
+                        tmem_st_wait();
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_local(bar(Bars::kKFull + at));
+                        ++n;
                     }
-#pragma unroll
-                    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x[u][i] = x[u + 1][i];
-                    tmem_st_wait();
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_local(bar(Bars::kKFull + at));
                 }
                 if (ok) give_back();
             }
@@ -425,7 +418,7 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
                 if (part.steps == 0) break;
                 Units units;
                 units.start(p, part);
-                uint2 x[kAhead + 1][8];
+                uint2 x[kAhead][8];
                 int2 next = make_int2(0, -1);   // of the unit that lane & 3 stands for
                 auto look = [&](int j) { return j < part.steps ? units.look(static_cast<long long>(part.step0 + j) * 128 + quarter * 32 + (lane & 3) * 8) : make_int2(0, -1); };
                 auto load = [&](uint2* to, int j) {
@@ -442,28 +435,28 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
                 next = look(0);
 #pragma unroll
                 for (int u = 0; u < kAhead; ++u) load(x[u], u);
-#pragma unroll 1
-                for (int j = 0; j < part.steps; ++j, ++n) {
-                    const uint32_t at = n & 1, use = n >> 1 & 1;
-                    load(x[kAhead], j + kAhead);
-                    if (!warp_wait(bar(Bars::kVFree + at), use ^ 1, abort_p)) { ok = false; break; }
-                    const uint32_t to = v_tiles + at * S::VTILE + (quarter * 32 + r) * 128;
+                for (int j0 = 0; j0 < part.steps && ok; j0 += kAhead) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
+                    for (int u = 0; u < kAhead; ++u) {
+                        if (j0 + u >= part.steps) break;
+                        const uint32_t at = n & 1, use = n >> 1 & 1;
+                        if (!warp_wait(bar(Bars::kVFree + at), use ^ 1, abort_p)) { ok = false; break; }
+                        const uint32_t to = v_tiles + at * S::VTILE + (quarter * 32 + r) * 128;
 #pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const uint2 w = x[0][2 * i + k];
-                            const uint32_t chunk = to + i * 1024 + (((g + 4 * k) ^ r) << 4);
-                            st_shared16(chunk, code_pair(w.x, 0), code_pair(w.x, 1), code_pair(w.x, 2), code_pair(w.x, 3));
-                            st_shared16(chunk + S::VBOX, code_pair(w.y, 0), code_pair(w.y, 1), code_pair(w.y, 2), code_pair(w.y, 3));
-                        }
+                        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                    for (int u = 0; u < kAhead; ++u)
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[u][i] = x[u + 1][i];
-                    proxy_fence();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_local(bar(Bars::kVFull + at));
+                            for (int k = 0; k < 2; ++k) {
+                                const uint2 w = x[u][2 * i + k];
+                                const uint32_t chunk = to + i * 1024 + (((g + 4 * k) ^ r) << 4);
+                                st_shared16(chunk, code_pair(w.x, 0), code_pair(w.x, 1), code_pair(w.x, 2), code_pair(w.x, 3));
+                                st_shared16(chunk + S::VBOX, code_pair(w.y, 0), code_pair(w.y, 1), code_pair(w.y, 2), code_pair(w.y, 3));
+                            }
+                        load(x[u], j0 + u + kAhead);
+                        proxy_fence();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_local(bar(Bars::kVFull + at));
+                        ++n;
+                    }
                 }
                 if (ok) give_back();
             }
@@ -534,8 +527,8 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
                         float4 sum[2], ref[2];
                         sum[0] = *reinterpret_cast<const float4*>(&sums[slot][r0]); sum[1] = *reinterpret_cast<const float4*>(&sums[slot][r0 + 4]);
                         ref[0] = *reinterpret_cast<const float4*>(&refs[r0]); ref[1] = *reinterpret_cast<const float4*>(&refs[r0 + 4]);
-                        const float sq[8] = {sum[0].x, sum[0].y, sum[0].z, sum[0].w, sum[1].x, sum[1].y, sum[1].z, sum[1].w};
-                        const float rf[8] = {ref[0].x, ref[0].y, ref[0].z, ref[0].w, ref[1].x, ref[1].y, ref[1].z, ref[1].w};
+                        const float* sq = &sum[0].x;
+                        const float* rf = &ref[0].x;
 #pragma unroll
                         for (int e = 0; e < 8; ++e) x[c][e] = fmaf(x[c][e], ks, fmaf(sq[e], ko, lv) - rf[e]);
                         if (__builtin_expect(masked, 0)) {
@@ -549,57 +542,52 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
                 // the first tokens set the references; after that sums are rescaled only when a maximum has risen by 2^kSlack
                 if (__builtin_expect(meet_any(!ok || !started || most > kLift + kSlack), 0)) {
                     if (meet_any(!ok)) { ok = false; break; }
-                    // through shared memory, a row per warp at a time: seldom run, so short rather than fast (straight-line code of 24 rows a thread cost
-                    // some 20 microseconds in instruction fetches alone)
-#pragma unroll
-                    for (int c = 0; c < C; ++c)
-                        if (2 * c + turn < groups) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) scratch[((2 * c + turn) * 8 + e) * S::PITCH + token] = x[c][e];
-                        }
-                    meet_any(false);
-                    bool some = false;
-#pragma unroll 1
-                    for (int r = warp - 12; r < part.live; r += 8) {
-                        const float4 y = *reinterpret_cast<const float4*>(&scratch[r * S::PITCH + lane * 4]);
-                        float top = fmaxf(fmaxf(y.x, y.y), fmaxf(y.z, y.w));
-#pragma unroll
-                        for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                        // (a row that sees none of the first tokens sees none of the later ones either)
-                        const float up = !started ? (top == -INFINITY ? 0.0f : top - kLift) : fmaxf(top - kLift, 0.0f);
-                        some = some || top > -INFINITY;
-                        if (lane == 0) { ups[r] = up; bys[r] = started ? ex2(-up) : 1.0f; refs[r] += up; }
-                    }
-                    some = meet_any(some);
-                    // the output of the steps before: finished, then rescaled by the threads that stand for its elements
-                    if (j > 0) ok = ok && warp_wait(bar(Bars::kPFree + (at ^ 1)), (n - 1) >> 1 & 1, abort_p);
-                    tc_fence_after();
 #pragma unroll
                     for (int c = 0; c < C; ++c)
                         if (2 * c + turn < groups) {
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
-                                const int r = (2 * c + turn) * 8 + e;
-                                if (r >= part.live) break;
-                                x[c][e] -= ups[r];
-                                l[c][e] *= bys[r];
-                                lo[c][e] *= bys[r];
+                                float top = x[c][e];
+#pragma unroll
+                                for (int d = 16; d; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                                if (lane == 0) tops[quarter][(2 * c + turn) * 8 + e] = top;
                             }
                         }
-                    if (j > 0) {
-#pragma unroll 1
-                        for (int c = turn; c < groups; c += 2) {
-                            float o[8];
-                            tmem_ld8(tmem + S::O0 + lanes + c * 8, o);
-                            tmem_ld_wait();
+                    meet_any(false);
+                    // the output of the steps before: finished, then rescaled by the threads that stand for its elements
+                    if (j > 0) ok = ok && warp_wait(bar(Bars::kPFree + (at ^ 1)), (n - 1) >> 1 & 1, abort_p);
+                    tc_fence_after();
+                    bool some = false;
+                    for (int r = 0; r < part.live; ++r) some = some || fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r])) > -INFINITY;
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) o[e] *= bys[c * 8 + e];
-                            tmem_st8(tmem + S::O0 + lanes + c * 8, o);
+                    for (int c = 0; c < C; ++c)
+                        if (2 * c + turn < groups) {
+                            float o[8];
+                            if (j > 0) {
+                                tmem_ld8(tmem + S::O0 + lanes + (2 * c + turn) * 8, o);
+                                tmem_ld_wait();
+                            }
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) {
+                                const int r = (2 * c + turn) * 8 + e;
+                                const float top = fmaxf(fmaxf(tops[0][r], tops[1][r]), fmaxf(tops[2][r], tops[3][r]));
+                                // (a row that sees none of the first tokens sees none of the later ones either)
+                                const float up = !started ? (top == -INFINITY ? 0.0f : top - kLift) : fmaxf(top - kLift, 0.0f), by = started ? ex2(-up) : 1.0f;
+                                x[c][e] -= up;
+                                l[c][e] *= by;
+                                lo[c][e] *= by;
+                                o[e] *= by;
+                            }
+                            if (j > 0) tmem_st8(tmem + S::O0 + lanes + (2 * c + turn) * 8, o);
                         }
-                        tmem_st_wait();
-                    }
+                    tmem_st_wait();
                     tc_fence_before();
-                    meet_any(false);            // (the next ones overwrite what has been read here)
+                    meet_any(false);            // everyone has read the references
+                    if (turn == 0 && token < part.live) {
+                        const float top = fmaxf(fmaxf(tops[0][token], tops[1][token]), fmaxf(tops[2][token], tops[3][token]));
+                        refs[token] += !started ? (top == -INFINITY ? 0.0f : top - kLift) : fmaxf(top - kLift, 0.0f);
+                    }
+                    meet_any(false);
                     started = started || some;
                 }
                 ok = ok && warp_wait(bar(Bars::kPFree + at), use ^ 1, abort_p);
@@ -634,29 +622,20 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
             o_phase ^= 1u;
             if (meet_any(!ok)) { ok = false; break; }
             tc_fence_after();
-            // sums over the tokens, the same way
+            // sums over the tokens
 #pragma unroll
             for (int c = 0; c < C; ++c)
                 if (2 * c + turn < groups) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
-                        scratch[((2 * c + turn) * 8 + e) * S::PITCH + token] = l[c][e];
-                        scratch[(S::ROWS + (2 * c + turn) * 8 + e) * S::PITCH + token] = lo[c][e];
+#pragma unroll
+                        for (int d = 16; d; d >>= 1) {
+                            l[c][e] += __shfl_xor_sync(0xffffffffu, l[c][e], d);
+                            lo[c][e] += __shfl_xor_sync(0xffffffffu, lo[c][e], d);
+                        }
+                        if (lane == 0) { parts_l[quarter][(2 * c + turn) * 8 + e] = l[c][e]; parts_o[quarter][(2 * c + turn) * 8 + e] = lo[c][e]; }
                     }
                 }
-            meet_any(false);
-#pragma unroll 1
-            for (int r = warp - 12; r < part.live; r += 8) {
-                const float4 y = *reinterpret_cast<const float4*>(&scratch[r * S::PITCH + lane * 4]);
-                const float4 z = *reinterpret_cast<const float4*>(&scratch[(S::ROWS + r) * S::PITCH + lane * 4]);
-                float lt = (y.x + y.y) + (y.z + y.w), ot = (z.x + z.y) + (z.z + z.w);
-#pragma unroll
-                for (int d = 16; d; d >>= 1) {
-                    lt += __shfl_xor_sync(0xffffffffu, lt, d);
-                    ot += __shfl_xor_sync(0xffffffffu, ot, d);
-                }
-                if (lane == 0) { total_l[r] = lt; total_o[r] = ot; }
-            }
             meet_any(false);
             const bool whole = part.starts && part.ends;
             const float by = token & 2 ? 1048576.0f : 16777216.0f;      // 2^20, 2^24: what the codes' form left out
@@ -670,7 +649,9 @@ __global__ void __launch_bounds__(Wide::THREADS, 1) attend_wide_kernel(const Att
                 for (int e = 0; e < 8; ++e) {
                     const int r = c * 8 + e;
                     if (r >= part.live) continue;
-                    const float lt = total_l[r], y = fmaf(o[e], by, total_o[r]);
+                    const float lt = (parts_l[0][r] + parts_l[1][r]) + (parts_l[2][r] + parts_l[3][r]);
+                    const float ot = (parts_o[0][r] + parts_o[1][r]) + (parts_o[2][r] + parts_o[3][r]);
+                    const float y = fmaf(o[e], by, ot);
                     if (whole) {
                         const bool none = limits[slot][r] == 0;
                         p.out[places[slot][r] * S::D + token] = none ? 0 : static_cast<unsigned short>(bf16x2_bits(y / lt, 0.0f) & 0xffffu);
