@@ -20,26 +20,85 @@
 // be expanded through shared or tensor memory.)
 //
 // Work: (sequence, key head, row tile) are segments of `steps` of 32 tokens per warp; the steps of all segments, one after the other, are cut into equal
-// shares, one per CTA, whatever the lengths; what a segment costs besides its steps counts as OVERHEAD of them.  Each warp streams its tiles through a ring of its own (bulk copies of one or two units) and keeps
+// shares, one per CTA, whatever the lengths; what a segment costs besides its steps counts as kOverhead of them.  Each warp streams its tiles through a ring of its own (bulk copies of one or two units) and keeps
 // maximum, sums and the output tile in registers; a segment's warps meet once at its end.  A segment that crosses CTAs leaves partial
 // results, which a second kernel joins.
-#include "cache_attention.cuh"
+#include <cuda_fp16.h>
+
+#include "kv_pages.cuh"
 #include "tensor_device.cuh"
 
 namespace polyspec {
 namespace {
 
-using namespace attend;
 using tensordev::mbar_expect_tx;
 using tensordev::mbar_init;
 using tensordev::mbar_try;
 using tensordev::smem_addr;
+
+constexpr int kMaxCtas = 608;                   // CTAs that the workspace has room for
+constexpr int kOverhead = 4;                    // steps' worth of work that a segment costs besides its steps: its rows, the meeting of its warps
+constexpr float kNone = -3.0e38f;               // a maximum over nothing
+constexpr float kLift = 7.0f;                   // p' is kept 2^7 above 1 at the maximum, out of fp16's subnormals
+constexpr float kSlack = 8.0f;                  // and may rise to 2^15 before sums are rescaled
+
+struct AttendParams {
+    polyspec_cache_pages s;
+    polyspec_block_rows r;
+    const unsigned short* q;                    // bf16 bits
+    long long q_stride;
+    int q_heads, kv_heads, group;
+    float scale_log2;                           // scale * log2(e)
+    const unsigned char* pool;
+    size_t plane_bytes;
+    int units_per_page;
+    unsigned short* out;
+    float* lse;
+    float* partial;                             // [2 * CTAs][rows of a tile][head_dim + 2]
+    int4* joins;                                // [CTAs]: (parts, sequence * 64 + row groups, key head, first row) of the segment that begins there and ends elsewhere
+    int32_t* status;
+};
+
+__device__ __forceinline__ float ex2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float lg2(float x)
+{
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float rcp(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t half2_bits(float a, float b)
+{
+    const __half2 x = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&x);
+}
+__device__ __forceinline__ uint32_t bf16x2_bits(float a, float b)
+{
+    uint32_t x;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(b), "f"(a));
+    return x;
+}
+__device__ __forceinline__ float low(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ __forceinline__ float high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
 
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
 {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+
+// Pair i (0..3) of a word's codes as two fp16 numbers: elements 2i, 2i+1 for keys.  Odd pairs come 16-fold.
+__device__ __forceinline__ uint32_t code_pair(uint32_t word, int i) { return (i >= 2 ? word >> 8 : word) & (i & 1 ? 0x00f000f0u : 0x000f000fu); }
 
 // The 8 x 8 matrix of 16-bit numbers whose rows the lanes hold in pairs, transposed.
 __device__ __forceinline__ uint32_t transpose(uint32_t x)
@@ -64,6 +123,14 @@ __device__ __forceinline__ void store_fragment(uint32_t* frag, int r, int word, 
     const float by16 = by * 0.0625f;
     to[0] = make_uint2(half2_bits(x[0] * by, x[1] * by), half2_bits(x[2] * by16, x[3] * by16));
     to[32] = make_uint2(half2_bits(x[4] * by, x[5] * by), half2_bits(x[6] * by16, x[7] * by16));
+}
+
+// The power of two that brings numbers of up to `top` in size into [2^14, 2^15), and what their products with codes (which bring 2^-24) are to be multiplied with.
+__device__ __forceinline__ float row_scale(const AttendParams& p, float top, float* factor)
+{
+    const int k = top > 0.0f ? max(-100, static_cast<int>(__float_as_uint(top) >> 23) - 127) : 0;          // top in [2^k, 2^(k+1))
+    *factor = p.scale_log2 * __uint_as_float(static_cast<uint32_t>(min(254, 10 + k + 127)) << 23);
+    return __uint_as_float(static_cast<uint32_t>(14 - k + 127) << 23);
 }
 
 // The rows of a tile into shared memory, by all THREADS of a CTA: rows row0 .. row0 + ROWS - 1 of (row of the block, head of the group), zeros from
@@ -112,12 +179,27 @@ __device__ __forceinline__ void load_rows(const AttendParams& p, const kv::SeqRo
     __syncthreads();
 }
 
+// A segment, and where in the list of them a cursor stands: row tile `tile` of `tiles` with tile_rows rows each (a multiple of 8; rows times heads of the
+// group are dealt out evenly), `steps` steps over the tokens.
+struct Segment { int b, head, tile, tiles, tile_rows, steps; kv::SeqRows q; };
+
+template <int ROWS, int STEP>
+__device__ __forceinline__ void seq_segments(const AttendParams& p, Segment& g)
+{
+    const int groups = (g.q.n * p.group + 7) / 8;
+    g.tiles = (groups + ROWS / 8 - 1) / (ROWS / 8);
+    g.tile_rows = g.tiles ? (groups + g.tiles - 1) / g.tiles * 8 : 8;
+    g.steps = max(1, (g.q.base + g.q.granted + STEP - 1) / STEP);
+}
+
+// Slots that row i of a block attends to: up to its own, none if that was not granted.
+__device__ __forceinline__ int row_limit(const kv::SeqRows& q, int i) { return i < q.granted ? q.base + i + 1 : 0; }
+
 // NT: groups of 8 rows in a tile.
 template <int D_, int NT_, int WARPS_, int STAGES_, int CTAS_>
 struct Shape {
     static constexpr int D = D_, NT = NT_, WARPS = WARPS_, STAGES = STAGES_, CTAS = CTAS_;
     static constexpr int THREADS = WARPS * 32, ROWS = NT * 8, STEP = WARPS * 32;        // STEP: tokens
-    static constexpr int OVERHEAD = 4;          // steps' worth of work that a segment costs besides its steps: its rows, the meeting of its warps
     static constexpr int UB = kv::unit_bytes(D), STAGE = 8 * UB, M = D / 16;            // M: 16-element groups of the output
     static constexpr int FRAG = NT * (D / 16) * 256;                                    // bytes
     static constexpr int RING = WARPS * STAGES * STAGE;
@@ -126,6 +208,88 @@ struct Shape {
     static constexpr int PART = ROWS * (D + 2);                                         // floats of a partial result
     static_assert(SMEM * CTAS <= 220 * 1024, "shared memory");
 };
+
+// All sequences' steps and overheads one behind the other: the sequence that holds place `at`, the place within it; returns the total.  Every thread
+// calls it.
+template <class S>
+__device__ __forceinline__ long long locate(const AttendParams& p, long long at, int* seq, long long* within, long long* warp_sums, int* hit, long long* hit_at)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    long long carry = 0;
+    if (threadIdx.x == 0) *hit = -1;
+    for (int b0 = 0; b0 < p.s.n_seqs; b0 += S::THREADS) {
+        const int b = b0 + threadIdx.x;
+        long long n = 0;
+        if (b < p.s.n_seqs) {
+            Segment g;
+            g.q = kv::seq_rows(p.s, p.r, b);
+            if (g.q.bad && blockIdx.x == 0) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
+            seq_segments<S::ROWS, S::STEP>(p, g);
+            n = static_cast<long long>(g.tiles) * (g.steps + kOverhead) * p.kv_heads;
+        }
+        long long inc = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long y = __shfl_up_sync(0xffffffffu, inc, d);
+            if (lane >= d) inc += y;
+        }
+        __syncthreads();
+        if (lane == 31) warp_sums[warp] = inc;
+        __syncthreads();
+        long long before = carry;
+        for (int w = 0; w < S::WARPS; ++w) {
+            if (w < warp) before += warp_sums[w];
+            carry += warp_sums[w];
+        }
+        const long long start = before + inc - n;
+        if (n > 0 && start <= at && at < start + n) { *hit = b; *hit_at = at - start; }
+    }
+    __syncthreads();
+    *seq = *hit;
+    *within = *hit_at;
+    __syncthreads();
+    return carry;
+}
+
+// A cursor over segments: the next (row tile, then head, then sequence with rows).
+template <class S>
+__device__ __forceinline__ void next_segment(const AttendParams& p, Segment& g)
+{
+    if (++g.tile < g.tiles) return;
+    g.tile = 0;
+    if (++g.head < p.kv_heads) return;
+    g.head = 0;
+    do {
+        if (++g.b >= p.s.n_seqs) { g.tiles = 0; g.tile_rows = 8; g.steps = 0x7fffffff; g.q = kv::SeqRows{0, 0, 0, 0, 0, false}; return; }
+        g.q = kv::seq_rows(p.s, p.r, g.b);
+        seq_segments<S::ROWS, S::STEP>(p, g);
+    } while (g.tiles == 0);
+}
+
+// Tokens that some row of the segment attends to.
+__device__ __forceinline__ int visible(const AttendParams& p, const Segment& g)
+{
+    const int first = g.tile * g.tile_rows / p.group, last = min(g.q.n - 1, (g.tile * g.tile_rows + g.tile_rows - 1) / p.group);
+    return first < g.q.granted ? row_limit(g.q, min(last, g.q.granted - 1)) : 0;
+}
+
+// Normalised outputs of eight neighbouring elements of a row.
+__device__ __forceinline__ void store_out(const AttendParams& p, const kv::SeqRows& q, int kv_head, int r, int D, int d0, const float* x, float m, float l)
+{
+    const int i = r / p.group;
+    if (i >= q.n) return;
+    const size_t at = static_cast<size_t>(q.row0 + i) * p.q_heads + kv_head * p.group + r % p.group;
+    const bool none = row_limit(q, i) == 0;
+    const float inv = none ? 0.0f : 1.0f / l;
+    uint4 y;
+    y.x = bf16x2_bits(x[0] * inv, x[1] * inv);
+    y.y = bf16x2_bits(x[2] * inv, x[3] * inv);
+    y.z = bf16x2_bits(x[4] * inv, x[5] * inv);
+    y.w = bf16x2_bits(x[6] * inv, x[7] * inv);
+    if (none) y = make_uint4(0, 0, 0, 0);
+    *reinterpret_cast<uint4*>(p.out + at * D + d0) = y;
+    if (d0 == 0 && p.lse) p.lse[at] = none ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
+}
 
 // What a warp keeps of its tile: output (elements x rows, in the codes' form), per row the reference of the exponentials (a maximum less kLift), the sums of
 // p and of p vo.  NT groups of 8 rows; a lane has rows 2 t4 and 2 t4 + 1 of each.
@@ -211,7 +375,7 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
     for (int v = 0; v < T; ++v)
 #pragma unroll
         for (int n = 0; n < L; ++n) most = fmaxf(most, fmaxf(fmaxf(sc[v][n][0], sc[v][n][1]), fmaxf(sc[v][n][2], sc[v][n][3])));
-    // the first tokens set the references; after that sums are rescaled only when a maximum has risen by 2^kSlack since the last time
+    // the first tokens set the references; after that sums are rescaled only when a maximum has risen by 2^8 since the last time
     if (__any_sync(0xffffffffu, !run.started || most > kLift + kSlack)) {
         const bool first = !run.started;
 #pragma unroll
@@ -335,10 +499,10 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
         g.b = seq;
         g.q = kv::seq_rows(p.s, p.r, seq);
         seq_segments<S::ROWS, S::STEP>(p, g);
-        const int span = g.steps + S::OVERHEAD, n = static_cast<int>(within / span);
+        const int span = g.steps + kOverhead, n = static_cast<int>(within / span);
         g.head = n / g.tiles;
         g.tile = n % g.tiles;
-        const int into = static_cast<int>(within % span) - S::OVERHEAD;       // negative: before the segment's first step
+        const int into = static_cast<int>(within % span) - kOverhead;       // negative: before the segment's first step
         step = max(into, 0);
         left = static_cast<int>(s1 - s0) + min(into, 0);
         if (left <= 0) return;
@@ -393,7 +557,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
             __syncwarp();
             ahead_step = 0;
             ahead_steps = produced[warp].steps;
-            ahead_left -= S::OVERHEAD;
+            ahead_left -= kOverhead;
             unit_k = 8;
         }
     };
@@ -448,7 +612,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
             if (NT == 1) {
                 attend_tokens<S, 1, 2>(p, run, at, 0, frag, q0, sums, factor, masked, bad, key0, mine, lane);
             } else {
-#pragma unroll
+#pragma unroll 1
                 for (int t0 = 0; t0 < 2; ++t0) {
                     if ((bad >> (2 * t0) & 3u) == 3u) continue;
                     // (code of its own for each number of groups: what is not there costs nothing, and what is there is straight-line code)
@@ -561,7 +725,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
         }
         __syncthreads();
         if (step == steps) {
-            left -= S::OVERHEAD;
+            left -= kOverhead;
             if (threadIdx.x == 0 && left > 0) {
                 Segment g = mine;
                 next_segment<S>(p, g);
@@ -581,6 +745,36 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
     }
 }
 
+// Joins the parts of the segment that begins in CTA blockIdx.x and ends in a later one, in order.
+template <class S>
+__global__ void __launch_bounds__(256) join_kernel(const AttendParams p)
+{
+    constexpr int D = S::D, kVecs = D / 8;
+    wait_for_stream();
+    const int4 job = p.joins[blockIdx.x];
+    if (job.x == 0) return;
+    const kv::SeqRows q = kv::seq_rows(p.s, p.r, job.y >> 6);
+    const int job_rows = (job.y & 63) * 8;
+    for (int item = threadIdx.x; item < S::ROWS * kVecs; item += 256) {
+        const int r = item / kVecs, d0 = item % kVecs * 8;
+        if (job.w + r >= q.n * p.group || r >= job_rows) continue;
+        float x[8], m = kNone, l = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.0f;
+        for (int k = 0; k < job.x; ++k) {
+            const float* part = p.partial + static_cast<size_t>(k ? 2 * (blockIdx.x + k) : 2 * blockIdx.x + 1) * S::PART;
+            const float2 ml = *reinterpret_cast<const float2*>(part + S::ROWS * D + 2 * r);
+            const float4 a = reinterpret_cast<const float4*>(part + r * D + d0)[0], b = reinterpret_cast<const float4*>(part + r * D + d0)[1];
+            const float to = fmaxf(m, ml.x), was = ex2(m - to), is = ex2(ml.x - to);
+            m = to;
+            l = fmaf(l, was, ml.y * is);
+            x[0] = fmaf(x[0], was, a.x * is); x[1] = fmaf(x[1], was, a.y * is); x[2] = fmaf(x[2], was, a.z * is); x[3] = fmaf(x[3], was, a.w * is);
+            x[4] = fmaf(x[4], was, b.x * is); x[5] = fmaf(x[5], was, b.y * is); x[6] = fmaf(x[6], was, b.z * is); x[7] = fmaf(x[7], was, b.w * is);
+        }
+        store_out(p, q, job.z, job.w + r, D, d0, x, m, l);
+    }
+}
+
 template <class S>
 cudaError_t launch_attend(const AttendParams& p, cudaStream_t stream)
 {
@@ -595,7 +789,7 @@ cudaError_t launch_attend(const AttendParams& p, cudaStream_t stream)
     return e;
 }
 
-constexpr int kMaxRows = kWideRows;             // rows of the largest tile
+constexpr int kMaxRows = 16;                    // rows of the largest tile
 inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 inline size_t attend_bytes(int head_dim) { return align256(kMaxCtas * sizeof(int4)) + static_cast<size_t>(2 * kMaxCtas) * kMaxRows * (head_dim + 2) * 4; }
 
@@ -743,8 +937,7 @@ polyspec_status fill(AttendParams* p, const polyspec_cache_pages* s, const polys
     if (!kv::rows_ok(q, q_stride, q_heads, head_dim) || !pool || !kv::aligned16(pool) || !aligned4(device_status)) return POLYSPEC_ERR_INVALID_ARG;
     if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return POLYSPEC_ERR_INVALID_ARG;
     const size_t bytes = kv::page_bytes(*s, kv_heads, head_dim);
-    // (steps of up to 256 tokens past the end are counted in int)
-    if (s->n_seqs > (1 << 24) || static_cast<long long>(s->max_pages) * s->page_tokens > 0x7fffff00LL) return POLYSPEC_ERR_UNSUPPORTED;
+    if (s->n_seqs > (1 << 24)) return POLYSPEC_ERR_UNSUPPORTED;
     if (s->n_pages * (bytes / kv::unit_bytes(head_dim)) >= 0xffffffffull) return POLYSPEC_ERR_UNSUPPORTED;      // units of a plane are counted in 32 bits
     p->s = *s;
     p->r = *r;
@@ -793,7 +986,7 @@ polyspec_status polyspec_cache_attention(const polyspec_cache_pages* s, const po
     // rows of a sequence times the heads that share a key head, on average: one group of 8 rows, or tiles of two
     const bool few = static_cast<long long>(r->rows) * p.group <= 8LL * s->n_seqs;
     cudaError_t e;
-    if (head_dim == 128) e = few ? launch_attend<Shape<128, 1, 8, 2, 2>>(p, stream) : launch_attend_wide(p, stream);
+    if (head_dim == 128) e = few ? launch_attend<Shape<128, 1, 8, 2, 2>>(p, stream) : launch_attend<Shape<128, 2, 4, 3, 3>>(p, stream);
     else e = few ? launch_attend<Shape<64, 1, 8, 3, 2>>(p, stream) : launch_attend<Shape<64, 2, 8, 3, 2>>(p, stream);
     return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }
