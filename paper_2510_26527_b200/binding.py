@@ -7,6 +7,7 @@ library cannot be loaded the functions raise: there is no fallback path.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Sequence
 
@@ -879,11 +880,16 @@ def _on_stream(stream, dev: int):
     return torch.cuda.stream(stream)
 
 
+@functools.lru_cache(maxsize=None)
+def _device(dev: int) -> torch.device:
+    return torch.device("cuda", dev)
+
+
 def _empty(shape, dtype, dev: int, stream) -> torch.Tensor:
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
+        return torch.empty(shape, dtype=dtype, device=_device(dev))
     with _on_stream(stream, dev):
-        return torch.empty(shape, dtype=dtype, device=torch.device("cuda", dev))
+        return torch.empty(shape, dtype=dtype, device=_device(dev))
 
 
 def _handle(stream, dev: int) -> int:
@@ -1144,31 +1150,38 @@ def polyspec_cache_compact(pages, pools=(), moved_to=None, workspace=None, strea
 
 
 # ------------------------------------------------------------------ a model's attention around the cache pages
-def _head_rows(name, t, rows=None, heads=None, d=None) -> int:
-    """Checks rows of heads, [rows, heads, d] bf16 whose rows may lie apart (parts of a fused projection); returns the row stride."""
-    if t.dtype is not torch.bfloat16:
+# (Short calls again: each tensor's type, shape, strides and device are read once.)
+_BF16, _F32T, _I32T = torch.bfloat16, torch.float32, torch.int32
+
+
+def _head_rows(name, t, shape, dev):
+    """Checks rows of heads, [rows, heads, head_dim] bf16 whose rows may lie apart (parts of a fused projection), of a given shape or (None) any;
+    dev: the device of the call's other tensors, -1 for the first.  Returns (row stride, device)."""
+    if t.dtype is not _BF16:
         raise TypeError(f"{name} must be torch.bfloat16, got {t.dtype}")
-    if t.dim() != 3:
-        raise ValueError(f"{name} must be [rows, heads, head_dim]")
-    shape, stride = t.shape, t.stride()
-    if (rows is not None and shape[0] != rows) or (heads is not None and shape[1] != heads) or (d is not None and shape[2] != d):
-        raise ValueError(f"shapes do not fit: {name} must be {[x for x in (rows, heads, d)]}, got {list(shape)}")
-    if not t.is_cuda or (shape[2] > 1 and stride[2] != 1) or (shape[1] > 1 and stride[1] != shape[2]):
-        raise ValueError(f"{name} must be a CUDA tensor with the heads of a row behind one another")
+    size = t.shape
+    if len(size) != 3 or (shape is not None and size != shape):
+        raise ValueError(f"shapes do not fit: {name} must be {'[rows, heads, head_dim]' if shape is None else list(shape)}, got {list(size)}")
+    stride, at = t.stride(), t.get_device()
     # (a stride says nothing of a dimension of size 1)
-    return stride[0] if shape[0] > 1 else shape[1] * shape[2]
+    if at < 0 or (stride[2] != 1 and size[2] > 1) or (stride[1] != size[2] and size[1] > 1):
+        raise ValueError(f"{name} must be a CUDA tensor with the heads of a row behind one another")
+    if at != dev and dev >= 0:
+        raise ValueError("all tensors of a call must be on one device")
+    return (stride[0] if size[0] > 1 else size[1] * size[2]), at
 
 
-def _head_device(dev: int, *tensors) -> int:
-    """The device of rows of heads, which need not be contiguous, and of the other tensors of a call (dev, -1: there are none)."""
-    for t in tensors:
-        if t is not None:
-            d = t.get_device()
-            if dev < 0:
-                dev = d
-            elif d != dev:
-                raise ValueError("all tensors of a call must be on one device")
-    return dev
+def _flat(name, t, dtype, shape, dev):
+    """Checks a contiguous tensor of a call on device dev; returns its address, None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"shapes do not fit: {name} must be {list(shape)}, got {list(t.shape)}")
+    if t.get_device() != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous tensor on the device of the call's other tensors")
+    return t.data_ptr()
 
 
 def polyspec_rotate_heads(q, k, positions, frequencies, q_weight=None, k_weight=None, interleaved=False, eps=1e-6, q_out=None, k_out=None, stream=None):
@@ -1177,32 +1190,33 @@ def polyspec_rotate_heads(q, k, positions, frequencies, q_weight=None, k_weight=
 
     bf16; rows may lie apart, as parts of one projection's rows do.  positions [rows] int32, frequencies [rotary/2] fp32, weights [d] bf16.
     q_out, k_out: tensors of their own (made if None) or q and k themselves.  Returns (q_out, k_out)."""
-    rows, heads, d = q.shape
-    qs = _head_rows("q", q)
-    ks = kv_heads = kos = 0
-    rotary = 0 if frequencies is None else 2 * frequencies.numel()
-    if rotary:
+    qs, dev = _head_rows("q", q, None, -1)
+    shape = rows, heads, d = q.shape
+    ks = kv_heads = kos = rotary = 0
+    k_ptr = k_out_ptr = None
+    if frequencies is not None:
+        rotary = 2 * frequencies.numel()
         if positions is None:
             raise ValueError("frequencies need positions")
-        _expect("positions", positions, torch.int32, (rows,))
-        _expect("frequencies", frequencies, torch.float32, (rotary // 2,))
-    _expect("q_weight", q_weight, torch.bfloat16, (d,))
-    _expect("k_weight", k_weight, torch.bfloat16, (d,))
-    dev = _head_device(_one_device(positions, frequencies, q_weight, k_weight), q, k, q_out, k_out)
     if q_out is None:
-        q_out = _empty((rows, heads, d), torch.bfloat16, dev, stream)
-    qos = _head_rows("q_out", q_out, rows, heads, d)
+        q_out = _empty(shape, _BF16, dev, stream)
+    qos = _head_rows("q_out", q_out, shape, dev)[0]
     if k is not None:
-        kv_heads = k.shape[1] if k.dim() == 3 else 0
-        ks = _head_rows("k", k, rows, kv_heads, d)
+        ks = _head_rows("k", k, None, dev)[0]
+        k_shape = k.shape
+        kv_heads = k_shape[1]
+        if k_shape[0] != rows or k_shape[2] != d:
+            raise ValueError("shapes do not fit: k must be [rows, kv_heads, head_dim]")
         if k_out is None:
-            k_out = _empty((rows, kv_heads, d), torch.bfloat16, dev, stream)
-        kos = _head_rows("k_out", k_out, rows, kv_heads, d)
+            k_out = _empty(k_shape, _BF16, dev, stream)
+        kos = _head_rows("k_out", k_out, k_shape, dev)[0]
+        k_ptr, k_out_ptr = k.data_ptr(), k_out.data_ptr()
     elif k_out is not None:
         raise ValueError("k_out needs k")
-    _call("polyspec_rotate_heads", load_library().polyspec_rotate_heads, dev, q.data_ptr(), qs, heads, _ptr(k), ks, kv_heads, rows, d, rotary,
-          int(bool(interleaved)), _ptr(positions) if rotary else None, _ptr(frequencies) if rotary else None, _ptr(q_weight), _ptr(k_weight), eps,
-          q_out.data_ptr(), qos, _ptr(k_out), kos, _handle(stream, dev))
+    _call("polyspec_rotate_heads", load_library().polyspec_rotate_heads, dev, q.data_ptr(), qs, heads, k_ptr, ks, kv_heads, rows, d, rotary,
+          1 if interleaved else 0, _flat("positions", positions, _I32T, (rows,), dev) if rotary else None,
+          _flat("frequencies", frequencies, _F32T, (rotary // 2,), dev) if rotary else None, _flat("q_weight", q_weight, _BF16, (d,), dev),
+          _flat("k_weight", k_weight, _BF16, (d,), dev), eps, q_out.data_ptr(), qos, k_out_ptr, kos, _handle(stream, dev))
     return q_out, k_out
 
 
@@ -1210,23 +1224,24 @@ def polyspec_prompt_attention(q, k, v, rows_at, scale=None, out=None, lse=None, 
     """Causal attention over packed prompts: prompt b is the rows rows_at[b] .. rows_at[b + 1] - 1 of q [rows, q_heads, d], k and v
     [rows, kv_heads, d] (bf16; rows may lie apart).  scale: d ** -0.5 where None.  out [rows, q_heads, d] bf16 and, where given, lse
     [rows, q_heads] fp32 are contiguous.  Returns (out, lse, status word)."""
-    rows, heads, d = q.shape
-    qs = _head_rows("q", q)
-    kv_heads = k.shape[1] if k.dim() == 3 else 0
-    ks, vs = _head_rows("k", k, rows, kv_heads, d), _head_rows("v", v, rows, kv_heads, d)
-    _expect("rows_at", rows_at, torch.int32)
+    qs, dev = _head_rows("q", q, None, -1)
+    shape = rows, heads, d = q.shape
+    ks = _head_rows("k", k, None, dev)[0]
+    k_shape = k.shape
+    kv_heads = k_shape[1]
+    if k_shape[0] != rows or k_shape[2] != d:
+        raise ValueError("shapes do not fit: k must be [rows, kv_heads, head_dim]")
+    vs = _head_rows("v", v, k_shape, dev)[0]
     if rows_at.dim() != 1 or rows_at.shape[0] < 2:
         raise ValueError("rows_at must be [n_seqs + 1]")
-    _expect("out", out, torch.bfloat16, (rows, heads, d))
-    _expect("lse", lse, torch.float32, (rows, heads))
-    _expect("device_status", device_status, torch.int32)
-    dev = _head_device(_one_device(rows_at, out, lse, device_status), q, k, v)
     if out is None:
-        out = _empty((rows, heads, d), torch.bfloat16, dev, stream)
+        out = _empty(shape, _BF16, dev, stream)
+    n_seqs = rows_at.shape[0] - 1
     device_status = _status_word(device_status, dev, stream)
     _call("polyspec_prompt_attention", load_library().polyspec_prompt_attention, dev, q.data_ptr(), qs, k.data_ptr(), ks, v.data_ptr(), vs,
-          rows_at.data_ptr(), rows_at.shape[0] - 1, rows, heads, kv_heads, d, d ** -0.5 if scale is None else scale, out.data_ptr(), _ptr(lse),
-          device_status.data_ptr(), _handle(stream, dev))
+          _flat("rows_at", rows_at, _I32T, (n_seqs + 1,), dev), n_seqs, rows, heads, kv_heads, d, d ** -0.5 if scale is None else scale,
+          _flat("out", out, _BF16, shape, dev), _flat("lse", lse, _F32T, (rows, heads), dev), _flat("device_status", device_status, _I32T, (1,), dev),
+          _handle(stream, dev))
     return out, lse, device_status
 
 
@@ -1236,21 +1251,22 @@ def cache_page_bytes(kv_heads: int, d: int, page_tokens: int) -> int:
 
 
 def _block_rows(pages, rows, rows_at, base, extra, n_rows):
-    n = pages.n_seqs
-    i32 = torch.int32
-    if rows_at.dtype is not i32 or base.dtype is not i32 or (extra is not None and extra.dtype is not i32) or (n_rows is not None and n_rows.dtype is not i32):
-        raise TypeError("rows_at, base, extra and n_rows must be int32")
-    if rows_at.shape != (n + 1,) or base.shape != (n,) or (extra is not None and extra.shape != (n,)) or (n_rows is not None and n_rows.shape != (n,)):
-        raise ValueError("rows_at must be [n_seqs + 1]; base, extra and n_rows [n_seqs]")
-    return BlockRows(rows_at.data_ptr(), _ptr(n_rows), base.data_ptr(), _ptr(extra), rows)
+    n, dev = pages.n_seqs, pages.dev
+    per_seq = (n,)
+    return BlockRows(_flat("rows_at", rows_at, _I32T, (n + 1,), dev), _flat("n_rows", n_rows, _I32T, per_seq, dev), _flat("base", base, _I32T, per_seq, dev),
+                     _flat("extra", extra, _I32T, per_seq, dev), rows)
 
 
-def _layer_pool(pages, pool, kv_heads, d, planes=2):
-    """pool: [planes, n_pages, page bytes] of any type; the planes of one layer (keys, values) or of all."""
-    if pool.dim() < 3 or pool.shape[1] != pages.n_pages or (pool.shape[0] != 2 if planes == 2 else pool.shape[0] < 2 or pool.shape[0] % 2):
-        raise ValueError("a layer's pool must be [2, n_pages, ...]: keys, values" if planes == 2 else "a pool must be [2 * layers, n_pages, ...]")
-    if pool.nbytes != pool.shape[0] * pages.n_pages * cache_page_bytes(kv_heads, d, pages.page_tokens):
+def _layer_pool(pages, pool, kv_heads, d, layers=False):
+    """pool: [planes, n_pages, ...] of any type; the planes of one layer (keys, values) or of all.  Returns its address."""
+    size = pool.shape
+    if len(size) < 3 or size[1] != pages.n_pages or (size[0] < 2 or size[0] % 2 if layers else size[0] != 2):
+        raise ValueError("a pool must be [2 * layers, n_pages, ...]" if layers else "a layer's pool must be [2, n_pages, ...]: keys, values")
+    if pool.numel() * pool.element_size() != size[0] * size[1] * cache_page_bytes(kv_heads, d, pages.page_tokens):
         raise ValueError("a page must have kv_heads * (page_tokens / 8) * (4 * head_dim + 32) bytes")
+    if pool.get_device() != pages.dev or not pool.is_contiguous():
+        raise ValueError("pool must be a contiguous tensor on the device of the pages")
+    return pool.data_ptr()
 
 
 def polyspec_cache_append(pages, k, v, pool, rows_at, base, extra=None, n_rows=None, k_held=None, v_held=None, weights=None, device_status=None, stream=None):
@@ -1259,21 +1275,20 @@ def polyspec_cache_append(pages, k, v, pool, rows_at, base, extra=None, n_rows=N
     Sequence b has the rows rows_at[b] .. (rows_at[b+1] - rows_at[b] of them, or the first n_rows[b]); its row i goes to slot base[b] +
     extra[b] + i, which must have been reserved.  k_held, v_held [rows, kv_heads, d] bf16 take the values the pages now stand for; weights
     [n_seqs, max_pages * page_tokens] fp32 become 0 at the new slots.  Returns the status word."""
-    rows, kv_heads, d = k.shape
-    ks, vs = _head_rows("k", k), _head_rows("v", v, rows, kv_heads, d)
+    dev = pages.dev
+    ks = _head_rows("k", k, None, dev)[0]
+    shape = rows, kv_heads, d = k.shape
+    vs = _head_rows("v", v, shape, dev)[0]
     r = _block_rows(pages, rows, rows_at, base, extra, n_rows)
-    _layer_pool(pages, pool, kv_heads, d)
-    _expect("k_held", k_held, torch.bfloat16, (rows, kv_heads, d))
-    _expect("v_held", v_held, torch.bfloat16, (rows, kv_heads, d))
-    _expect("weights", weights, torch.float32, (pages.n_seqs, pages.max_pages * pages.page_tokens))
-    _expect("device_status", device_status, torch.int32)
-    dev = _head_device(_same_device(pages, rows_at, base, extra, n_rows, pool, k_held, v_held, weights, device_status), k, v)
     device_status = _status_word(device_status, dev, stream)
     _call("polyspec_cache_append", load_library().polyspec_cache_append, dev, pages.c, r, k.data_ptr(), ks, v.data_ptr(), vs, kv_heads, d,
-          pool.data_ptr(), _ptr(k_held), _ptr(v_held), _ptr(weights), device_status.data_ptr(), _handle(stream, dev))
+          _layer_pool(pages, pool, kv_heads, d), _flat("k_held", k_held, _BF16, shape, dev), _flat("v_held", v_held, _BF16, shape, dev),
+          _flat("weights", weights, _F32T, (pages.n_seqs, pages.max_pages * pages.page_tokens), dev),
+          _flat("device_status", device_status, _I32T, (1,), dev), _handle(stream, dev))
     return device_status
 
 
+@functools.lru_cache(maxsize=256)       # (a function of the sizes alone)
 def polyspec_cache_attention_workspace(q_heads: int, kv_heads: int, d: int) -> int:
     n = ctypes.c_size_t(0)
     _check(load_library().polyspec_cache_attention_workspace(q_heads, kv_heads, d, n), "polyspec_cache_attention_workspace")
@@ -1287,42 +1302,40 @@ def polyspec_cache_attention(pages, q, pool, kv_heads, rows_at, base, extra=None
 
     out [rows, q_heads, d] bf16; lse, where given, [rows, q_heads] fp32.  The workspace is the caller's or a fresh one of the call's stream.
     Returns (out, lse, status word)."""
-    rows, heads, d = q.shape
-    qs = _head_rows("q", q)
+    dev = pages.dev
+    qs = _head_rows("q", q, None, dev)[0]
+    shape = rows, heads, d = q.shape
     r = _block_rows(pages, rows, rows_at, base, extra, n_rows)
-    _layer_pool(pages, pool, kv_heads, d)
-    _expect("out", out, torch.bfloat16, (rows, heads, d))
-    _expect("lse", lse, torch.float32, (rows, heads))
-    _expect("device_status", device_status, torch.int32)
-    dev = _head_device(_same_device(pages, rows_at, base, extra, n_rows, pool, out, lse, device_status, workspace), q)
+    pool_ptr = _layer_pool(pages, pool, kv_heads, d)
     if out is None:
-        out = _empty((rows, heads, d), torch.bfloat16, dev, stream)
+        out = _empty(shape, _BF16, dev, stream)
     if workspace is None:
         workspace = _empty((polyspec_cache_attention_workspace(heads, kv_heads, d),), torch.uint8, dev, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the device of the pages")
     device_status = _status_word(device_status, dev, stream)
     _call("polyspec_cache_attention", load_library().polyspec_cache_attention, dev, pages.c, r, q.data_ptr(), qs, heads, kv_heads, d,
-          d ** -0.5 if scale is None else scale, pool.data_ptr(), out.data_ptr(), _ptr(lse), device_status.data_ptr(), workspace.data_ptr(),
-          workspace.nbytes, _handle(stream, dev))
+          d ** -0.5 if scale is None else scale, pool_ptr, _flat("out", out, _BF16, shape, dev), _flat("lse", lse, _F32T, (rows, heads), dev),
+          _flat("device_status", device_status, _I32T, (1,), dev), workspace.data_ptr(), workspace.nbytes, _handle(stream, dev))
     return out, lse, device_status
 
 
 def polyspec_cache_weigh(pages, q, pool, kv_heads, rows_at, base, lse, weights, extra=None, n_rows=None, scale=None, keep=1.0, device_status=None, stream=None):
     """weights [n_seqs, max_pages * page_tokens] fp32 = keep * weights + the attention weight that the rows gave each cached token, over all heads;
     lse [rows, q_heads] of polyspec_cache_attention on the same rows, n_rows how many of a sequence's rows count.  Returns the status word."""
+    dev = pages.dev
+    qs = _head_rows("q", q, None, dev)[0]
     rows, heads, d = q.shape
-    qs = _head_rows("q", q)
     r = _block_rows(pages, rows, rows_at, base, extra, n_rows)
-    _layer_pool(pages, pool, kv_heads, d)
-    _expect("lse", lse, torch.float32, (rows, heads))
-    _expect("weights", weights, torch.float32, (pages.n_seqs, pages.max_pages * pages.page_tokens))
-    _expect("device_status", device_status, torch.int32)
-    dev = _head_device(_same_device(pages, rows_at, base, extra, n_rows, pool, lse, weights, device_status), q)
     device_status = _status_word(device_status, dev, stream)
     _call("polyspec_cache_weigh", load_library().polyspec_cache_weigh, dev, pages.c, r, q.data_ptr(), qs, heads, kv_heads, d,
-          d ** -0.5 if scale is None else scale, pool.data_ptr(), lse.data_ptr(), keep, weights.data_ptr(), device_status.data_ptr(), _handle(stream, dev))
+          d ** -0.5 if scale is None else scale, _layer_pool(pages, pool, kv_heads, d), _flat("lse", lse, _F32T, (rows, heads), dev), keep,
+          _flat("weights", weights, _F32T, (pages.n_seqs, pages.max_pages * pages.page_tokens), dev),
+          _flat("device_status", device_status, _I32T, (1,), dev), _handle(stream, dev))
     return device_status
 
 
+@functools.lru_cache(maxsize=256)
 def polyspec_cache_evict_workspace(n_seqs: int, max_pages: int, page_tokens: int) -> int:
     n = ctypes.c_size_t(0)
     _check(load_library().polyspec_cache_evict_workspace(n_seqs, max_pages, page_tokens, n), "polyspec_cache_evict_workspace")
@@ -1333,16 +1346,14 @@ def polyspec_cache_evict(pages, budget, weights, pool, kv_heads, d, first=0, rec
     """Cut sequences of more than budget[b] tokens (budget [n_seqs] int32; negative: left alone) to budget[b]: the first `first`, the last `recent` and the
     heaviest between stay and move together in every plane of pool [2 * layers, n_pages, ...] and in weights [n_seqs, max_pages * page_tokens].
     pages.len tells what is left, kept_from (int32, like weights) the slots the kept tokens had.  Returns the status word."""
-    shape = (pages.n_seqs, pages.max_pages * pages.page_tokens)
-    _expect("budget", budget, torch.int32, (pages.n_seqs,))
-    _expect("weights", weights, torch.float32, shape)
-    _expect("kept_from", kept_from, torch.int32, shape)
-    _layer_pool(pages, pool, kv_heads, d, planes=None)
-    _expect("device_status", device_status, torch.int32)
-    dev = _same_device(pages, budget, weights, pool, kept_from, device_status, workspace)
+    dev, shape = pages.dev, (pages.n_seqs, pages.max_pages * pages.page_tokens)
+    pool_ptr = _layer_pool(pages, pool, kv_heads, d, layers=True)
     if workspace is None:
         workspace = _empty((polyspec_cache_evict_workspace(pages.n_seqs, pages.max_pages, pages.page_tokens),), torch.uint8, dev, stream)
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the device of the pages")
     device_status = _status_word(device_status, dev, stream)
-    _call("polyspec_cache_evict", load_library().polyspec_cache_evict, dev, pages.c, budget.data_ptr(), first, recent, weights.data_ptr(), pool.data_ptr(),
-          pool.shape[0], kv_heads, d, _ptr(kept_from), device_status.data_ptr(), workspace.data_ptr(), workspace.nbytes, _handle(stream, dev))
+    _call("polyspec_cache_evict", load_library().polyspec_cache_evict, dev, pages.c, _flat("budget", budget, _I32T, (pages.n_seqs,), dev), first, recent,
+          _flat("weights", weights, _F32T, shape, dev), pool_ptr, pool.shape[0], kv_heads, d, _flat("kept_from", kept_from, _I32T, shape, dev),
+          _flat("device_status", device_status, _I32T, (1,), dev), workspace.data_ptr(), workspace.nbytes, _handle(stream, dev))
     return device_status
