@@ -550,7 +550,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *   (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE in *device_status); POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.
  *
  * Caches held in 4 bits.  One plane of a pool holds one layer's keys or values; a token's head is head_dim codes with one scale and one
- * offset (bf16): value = scale * code + offset, scale > 0.  A page of polyspec_cache_pages (page_tokens a multiple of 8, at most 32768) is
+ * offset (bf16): value = scale * code + offset, scale a normal number > 0.  A page of polyspec_cache_pages (page_tokens a multiple of 8, at most 32768) is
  * [kv_heads, page_tokens / 8] units of 8 tokens; a unit is head_dim 32-bit words of codes, then 8 pairs (scale, offset):
  * page_bytes = kv_heads * (page_tokens / 8) * (4 head_dim + 32).  Code e of eight neighbours is in the four bits from bit
  * 4 * (e / 2) + 16 * (e % 2) on of their word.  Word w of token r lies at r * head_dim/8 + w in a unit of keys; in a unit of values, with
@@ -563,8 +563,8 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  * whose slot is not below len[b] is not written or attends to nothing (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE), as are the rows of a sequence
  * whose numbers make no sense.
  *
- * polyspec_cache_append -- keys and values of new rows into their slots:  offset = min(x), scale = the smallest bf16 number
- *   >= (max(x) - offset) / 15 (1 if that is 0), code = (x - offset) / scale rounded to the nearest, ties to even, at most 15; differences and
+ * polyspec_cache_append -- keys and values of new rows into their slots:  offset = min(x), scale = the smallest normal bf16
+ *   number >= (max(x) - offset) / 15 (1 if that is 0), code = (x - offset) / scale rounded to the nearest, ties to even, at most 15; differences and
  *   quotients in fp32.  Of x with NaN, infinities or a range past fp32: every value NaN.
  *   k_held, v_held  out [rows, kv_heads, head_dim] bf16 or NULL: the values the pages now stand for
  *   weights         [n_seqs, max_pages * page_tokens] fp32 or NULL: set to 0 at the new slots

@@ -13,6 +13,13 @@ namespace {
 
 constexpr int kThreads = 256;
 
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
+{
+    uint32_t x;
+    asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(a), "r"(b));
+    return x;
+}
+
 struct AppendParams {
     polyspec_cache_pages s;
     polyspec_block_rows r;
@@ -95,28 +102,23 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
             x[2] = __uint_as_float(raw[u].y << 16); x[3] = __uint_as_float(raw[u].y & 0xffff0000u);
             x[4] = __uint_as_float(raw[u].z << 16); x[5] = __uint_as_float(raw[u].z & 0xffff0000u);
             x[6] = __uint_as_float(raw[u].w << 16); x[7] = __uint_as_float(raw[u].w & 0xffff0000u);
-            float lo = x[0], hi = x[0];
-            bool nan = false;
+            // largest element and largest of the negated ones, two bf16 per instruction, NaN sticking
+            const uint32_t sign = 0x80008000u;
+            const uint32_t top = max2(max2(raw[u].x, raw[u].y), max2(raw[u].z, raw[u].w));
+            const uint32_t bottom = max2(max2(raw[u].x ^ sign, raw[u].y ^ sign), max2(raw[u].z ^ sign, raw[u].w ^ sign));
+            uint32_t ends = max2(__byte_perm(top, bottom, 0x5410), __byte_perm(top, bottom, 0x7632));
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                lo = fminf(lo, x[e]);
-                hi = fmaxf(hi, x[e]);
-                nan = nan || !(fabsf(x[e]) <= 3.4e38f);
-            }
-#pragma unroll
-            for (int d = 1; d < kLanes; d <<= 1) {
-                lo = fminf(lo, __shfl_xor_sync(0xffffffffu, lo, d));
-                hi = fmaxf(hi, __shfl_xor_sync(0xffffffffu, hi, d));
-            }
-            const uint32_t bad = __ballot_sync(0xffffffffu, nan);
-            const uint32_t mates = ((1ull << kLanes) - 1u) << ((tid & 31) / kLanes * kLanes);
-            float offset = lo + 0.0f;                       // (not -0)
-            const float range = hi - offset;
-            const uint32_t up = (__float_as_uint(__fdiv_rn(range, 15.0f)) + 0xffffu) & 0xffff0000u;
-            float scale = up ? __uint_as_float(up) : 1.0f;
-            const bool broken = (bad & mates) || !(range <= 3.4e38f);
+            for (int d = 1; d < kLanes; d <<= 1) ends = max2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
+            float offset = __uint_as_float((ends ^ sign) & 0xffff0000u) + 0.0f;         // (not -0)
+            const float range = __uint_as_float(ends << 16) - offset;
+            // range / 15, of which only the bits above the last sixteen are wanted, rounded up: the product says which they are unless it is next to one of their steps
+            float step = range * (1.0f / 15.0f);
+            if (((__float_as_uint(step) + 8u) & 0xffffu) < 17u) step = __fdiv_rn(range, 15.0f);
+            const uint32_t up = (__float_as_uint(step) + 0xffffu) & 0xffff0000u;
+            float scale = up ? fmaxf(__uint_as_float(up), 1.17549435e-38f) : 1.0f;      // at least the smallest normal number
+            const bool broken = !(range <= 3.4e38f);
             if (broken) scale = offset = __uint_as_float(0x7fc00000u);
-            const float inv = __frcp_rn(scale), near = scale * 0.49999f;
+            const float inv = __fdividef(1.0f, scale), near = scale * 0.49999f;
             uint32_t word = 0, held[4];
             float y[8];
 #pragma unroll

@@ -45,7 +45,7 @@ def quantise(x):
     with np.errstate(all="ignore"):
         step = ((hi - lo) / np.float32(15)).astype(np.float32)
         up = ((step.view(np.uint32) + np.uint32(0xffff)) & np.uint32(0xffff0000)).view(np.float32)
-        up = np.where(up == 0, np.float32(1), up)
+        up = np.where(up == 0, np.float32(1), np.maximum(up, np.float32(2.0 ** -126)))
         code = np.rint(((x - lo[..., None]) / up[..., None]).astype(np.float32))
         broken = ~np.isfinite(x).all(-1) | ~np.isfinite(hi - lo)
         code = np.where(broken[..., None], 0, np.minimum(code, 15)).astype(np.int64)
