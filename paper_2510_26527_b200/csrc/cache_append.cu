@@ -38,15 +38,15 @@ struct AppendParams {
 template <int D, int ROWS>
 __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
 {
-    constexpr int kLanes = D / 8, kTeams = kThreads / kLanes, kAhead = 4;
+    constexpr int kLanes = D / 8, kTeams = kThreads / kLanes, kAhead = 2;
     __shared__ int found[ROWS];
     __shared__ uint32_t units[ROWS];            // the row's unit of head 0, or ~0: not written
     __shared__ int tokens[ROWS];                // its token of the unit
     wait_for_stream();
     const int row0 = blockIdx.x * ROWS, tid = threadIdx.x, w = tid % kLanes, team = tid / kLanes;
     const int per_row = 2 * p.kv_heads, items = min(ROWS, p.r.rows - row0) * per_row;
-    uint4 raw[kAhead];
-    auto load = [&](int first) {
+    uint4 raw[kAhead], coming[kAhead];
+    auto load = [&](uint4* raw, int first) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int item = first + u * kTeams + team, row = row0 + item / per_row, j = item % per_row;
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
             if (item < items) raw[u] = reinterpret_cast<const uint4*>((j & 1 ? p.v + row * p.v_stride : p.k + row * p.k_stride) + (j >> 1) * D)[w];
         }
     };
-    load(0);
+    load(coming, 0);
     if (row0 == 0)              // numbers that make no sense are reported even where no row belongs to them
         for (int b = tid; b < p.s.n_seqs; b += kThreads)
             if (kv::seq_rows(p.s, p.r, b).bad) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
@@ -90,7 +90,9 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
     __syncthreads();
     // (whole warps go round together: the exchange below is warp-wide)
     for (int first = 0; first < items; first += kAhead * kTeams) {
-        if (first > 0) load(first);
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) raw[u] = coming[u];
+        if (first + kAhead * kTeams < items) load(coming, first + kAhead * kTeams);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int item = first + u * kTeams + team;
@@ -165,8 +167,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
 template <int D>
 cudaError_t launch_append(const AppendParams& p, cudaStream_t stream)
 {
-    // four rows share the look-up of their places where there are rows enough for all SMs
-    if (p.r.rows >= 4096) return launch_early(append_kernel<D, 4>, dim3(static_cast<unsigned>((p.r.rows + 3) / 4)), kThreads, 0, stream, p);
+    // eight rows share the look-up of their places where there are rows enough for all SMs
+    if (p.r.rows >= 4096) return launch_early(append_kernel<D, 8>, dim3(static_cast<unsigned>((p.r.rows + 7) / 8)), kThreads, 0, stream, p);
     return launch_early(append_kernel<D, 1>, dim3(static_cast<unsigned>(p.r.rows)), kThreads, 0, stream, p);
 }
 

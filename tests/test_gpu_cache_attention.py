@@ -478,3 +478,219 @@ def test_prompt_bad_row_numbers():
     out = torch.full((20, 2, 64), 9.0, dtype=torch.bfloat16, device=DEV)
     _, _, st = binding.polyspec_prompt_attention(q, q, q, _i32([4, 4, 4]), out=out)
     assert int(st) == 0 and (out == 9).all()
+
+
+# ------------------------------------------------------------------ many sequences, several calls at once, one whole run
+def test_more_sequences_than_a_block_has_threads():
+    """The cursors over sequences go round more than once; every third sequence has no rows."""
+    n, heads, kv, d, P = 700, 2, 1, 64, 8
+    counts = [0 if b % 3 == 2 else 1 + b % 2 for b in range(n)]
+    lens = [3 + b % 11 if c else b % 4 for b, c in enumerate(counts)]
+    c = plain.Cache(lens, kv, d, P, 190)
+    at, base = _starts(counts), [x - k for x, k in zip(lens, counts)]
+    q = _normal(191, at[-1], heads, d)
+    pages, on = c.to(DEV), c.words_on(c.pool(), DEV)
+    lse = torch.zeros((at[-1], heads), device=DEV)
+    out, _, st = binding.polyspec_cache_attention(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse=lse)
+    want, want_lse, tol, tol_lse, weights, tol_w = plain.attend(c, q.float().numpy(), at, base)
+    _close(out, want, tol)
+    _close(lse, want_lse, tol_lse)
+    w = torch.zeros((n, c.cap), device=DEV)
+    binding.polyspec_cache_weigh(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse, w)
+    for b in range(n):
+        _close(w[b, : lens[b]], weights[b], tol_w[b])
+    assert int(st) == 0
+    x = _normal(192, at[-1], kv, d)
+    st = binding.polyspec_cache_append(pages, x.to(DEV), x.to(DEV), on, _i32(at), _i32(base))
+    assert int(st) == 0
+    pool = on.cpu().numpy().view(np.uint32).reshape(2, c.n_pages, kv, P // 8, d + 8)
+    code, scale, offset, _ = plain.quantise(x.float().numpy())
+    for p in range(2):
+        want_pool = pool.copy()
+        for b, k in enumerate(counts):
+            c.put(want_pool, p, b, range(base[b], base[b] + k), code[at[b]:at[b] + k], scale[at[b]:at[b] + k], offset[at[b]:at[b] + k])
+        assert (want_pool[p] == pool[p]).all()
+    lens = [30 + 40 * (b % 5) for b in range(300)]
+    at = _starts(lens)
+    q, k, v = _normal(193, at[-1], 2, 64), _normal(194, at[-1], 1, 64), _normal(195, at[-1], 1, 64)
+    out, _, st = binding.polyspec_prompt_attention(q.to(DEV), k.to(DEV), v.to(DEV), _i32(at))
+    want, _, tol, _ = plain.prompt(*(x.float().numpy() for x in (q, k, v)), at)
+    _close(out, want, tol)
+    assert int(st) == 0
+
+
+def test_a_page_larger_than_a_cache_and_wide_groups():
+    """One page of 1024 tokens; 48 query heads on one key head, so that a sequence's rows fill several tiles."""
+    lens, counts, heads, kv, P = [1000, 37], [3, 2], 48, 1, 1024
+    for d in (64, 128):
+        c = plain.Cache(lens, kv, d, P, 200)
+        at, base = _starts(counts), [997, 35]
+        q = _normal(201, 5, heads, d)
+        lse = torch.zeros((5, heads), device=DEV)
+        pages, on = c.to(DEV), c.words_on(c.pool(), DEV)
+        out, _, st = binding.polyspec_cache_attention(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse=lse)
+        want, want_lse, tol, tol_lse, weights, tol_w = plain.attend(c, q.float().numpy(), at, base)
+        _close(out, want, tol)
+        _close(lse, want_lse, tol_lse)
+        w = torch.zeros((2, c.cap), device=DEV)
+        binding.polyspec_cache_weigh(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse, w)
+        for b in range(2):
+            _close(w[b, : lens[b]], weights[b], tol_w[b])
+
+
+def test_two_calls_at_once_on_two_streams():
+    """Attention of two layers, prompts and evictions side by side: nothing is shared between calls but what they are given."""
+    lens, counts, heads, kv, d, P = [900, 300], [4, 4], 8, 2, 128, 16
+    c = plain.Cache(lens, kv, d, P, 210)
+    at, base = _i32(_starts(counts)), _i32(n - k for n, k in zip(lens, counts))
+    pages, on = c.to(DEV), c.words_on(c.pool(4), DEV)
+    q = [_normal(211 + i, 8, heads, d).to(DEV) for i in range(2)]
+    prompt = _normal(213, 500, 4, 128).to(DEV)
+    ends = _i32([0, 300, 500])
+    alone = [binding.polyspec_cache_attention(pages, q[i], on[2 * i:2 * i + 2], kv, at, base)[0].clone() for i in range(2)]
+    alone_prompt = binding.polyspec_prompt_attention(prompt, prompt, prompt, ends)[0].clone()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        got = []
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got.append(binding.polyspec_cache_attention(pages, q[i], on[2 * i:2 * i + 2], kv, at, base)[0])
+        with torch.cuda.stream(streams[2]):
+            got.append(binding.polyspec_prompt_attention(prompt, prompt, prompt, ends)[0])
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], alone[0]) and torch.equal(got[1], alone[1]) and torch.equal(got[2], alone_prompt)
+
+
+def test_front_end_refuses_layouts_it_cannot_take():
+    c = plain.Cache([9], 2, 64, 8, 220)
+    pages, on = c.to(DEV), c.words_on(c.pool(), DEV)
+    x = torch.zeros((9, 2, 64), dtype=torch.bfloat16, device=DEV)
+    at, base = _i32([0, 9]), _i32([0])
+    with pytest.raises(ValueError):
+        binding.polyspec_cache_append(pages, x.transpose(0, 1), x, on, at, base)
+    with pytest.raises(ValueError):
+        binding.polyspec_cache_append(pages, x[:, :, ::2], x[:, :, ::2], on, at, base)
+    with pytest.raises(ValueError):
+        binding.polyspec_cache_append(pages, x, x, on[:1], at, base)
+    with pytest.raises(ValueError):
+        binding.polyspec_cache_attention(pages, x, on[:, :, :100], 2, at, base)
+    with pytest.raises(ValueError):
+        binding.polyspec_cache_attention(pages, x, on, 2, _i32([0, 3, 9]), base)
+    with pytest.raises(TypeError):
+        binding.polyspec_cache_attention(pages, x, on, 2, at.long(), base)
+    with pytest.raises(TypeError):
+        binding.polyspec_cache_weigh(pages, x, on, 2, at, base, torch.zeros((9, 2), device=DEV).double(), torch.zeros((1, c.cap), device=DEV))
+    with pytest.raises(ValueError):
+        binding.polyspec_cache_evict(pages, _i32([4]), torch.zeros((1, c.cap + 8), device=DEV), on, 2, 64)
+    with pytest.raises(ValueError):
+        binding.polyspec_prompt_attention(x, x, x, _i32([0]))
+    with pytest.raises(ValueError):
+        binding.polyspec_rotate_heads(x, None, None, torch.ones(32, device=DEV))
+    with pytest.raises(binding.PolyspecError):
+        binding.polyspec_rotate_heads(x[:, :, :8].contiguous(), None, None, None)
+
+
+class Run:
+    """A model's layer over a batch: prompts, then blocks of drafted tokens of which some are accepted, the cache kept to a budget."""
+
+    def __init__(self, lens, heads, kv, d, P, seed):
+        self.lens, self.heads, self.kv, self.d, self.P = lens, heads, kv, d, P
+        self.rng = np.random.default_rng(seed)
+        self.seed = seed
+        B, most = len(lens), max(lens) + 80
+        self.pages = binding.CachePages.new(B, -(-most // P), B * (-(-most // P)), P, DEV)
+        self.pool = torch.zeros((2, self.pages.n_pages, binding.cache_page_bytes(kv, d, P)), dtype=torch.uint8, device=DEV)
+        self.weights = torch.zeros((B, self.pages.max_pages * P), device=DEV)
+        self.status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        self.freq = torch.from_numpy((10000.0 ** -(np.arange(d // 2) / (d // 2))).astype(np.float32)).to(DEV)
+        self.norm = [(_normal(seed + i, d).float() * 0.1 + 1).to(torch.bfloat16).to(DEV) for i in range(2)]
+        self.text = list(lens)                                          # positions: eviction does not move them
+        # what the cache stands for, and the weights, in plain arrays
+        self.codes = [[np.zeros((0, kv, d), int) for _ in lens] for _ in range(2)]
+        self.scale = [[np.zeros((0, kv), np.float32) for _ in lens] for _ in range(2)]
+        self.offset = [[np.zeros((0, kv), np.float32) for _ in lens] for _ in range(2)]
+        self.w = [np.zeros(0) for _ in lens]
+
+    def rows(self, counts):
+        """A projection of new rows, rotated at their positions; the cache's room and its new tokens."""
+        self.seed += 10
+        H, K, d = self.heads, self.kv, self.d
+        at = _starts(counts)
+        qkv = _normal(self.seed, at[-1], H + 2 * K, d).to(DEV)
+        q, k, v = qkv.split([H, K, K], 1)
+        pos = np.concatenate([np.arange(t - n, t) for t, n in zip(self.text, counts)]).astype(np.int32)
+        before = qkv.float().cpu().numpy()
+        binding.polyspec_rotate_heads(q, k, torch.from_numpy(pos).to(DEV), self.freq, self.norm[0], self.norm[1], q_out=q, k_out=k)
+        for x, part, w in ((q, before[:, :H], 0), (k, before[:, H:H + K], 1)):
+            _close(x, *plain.rotate(part, self.norm[w].float().cpu().numpy(), pos, self.freq.cpu().numpy(), False))
+        held = [len(x) for x in self.w]
+        base = _i32(held)
+        binding.polyspec_cache_reserve(self.pages, base, extra=_i32(counts), device_status=self.status)
+        binding.polyspec_cache_append(self.pages, k, v, self.pool, _i32(at), base, weights=self.weights, device_status=self.status)
+        for p, x in enumerate((k, v)):
+            code, scale, offset, _ = plain.quantise(x.float().cpu().numpy())
+            for b, n in enumerate(counts):
+                s = slice(at[b], at[b] + n)
+                for have, new in ((self.codes, code), (self.scale, scale), (self.offset, offset)):
+                    have[p][b] = np.concatenate([have[p][b], new[s]])
+        for b, n in enumerate(counts):
+            self.w[b] = np.concatenate([self.w[b], np.zeros(n)])
+        return at, q, k, v, held, base
+
+    def cache(self):
+        c = plain.Cache.__new__(plain.Cache)
+        c.kv, c.d, c.P, c.lens = self.kv, self.d, self.P, [len(x) for x in self.w]
+        c.codes, c.scale, c.offset = self.codes, self.scale, self.offset
+        return c
+
+    def prompt(self):
+        at, q, k, v, _, _ = self.rows(self.lens)
+        out, _, _ = binding.polyspec_prompt_attention(q, k, v, _i32(at), device_status=self.status)
+        want, _, tol, _ = plain.prompt(*(x.float().cpu().numpy() for x in (q, k, v)), at)
+        _close(out, want, tol)
+
+    def block(self, counts):
+        self.text = [t + n for t, n in zip(self.text, counts)]
+        at, q, _, _, held, base = self.rows(counts)
+        lse = torch.zeros((at[-1], self.heads), device=DEV)
+        out, _, _ = binding.polyspec_cache_attention(self.pages, q, self.pool, self.kv, _i32(at), base, lse=lse, device_status=self.status)
+        c, qn = self.cache(), q.float().cpu().numpy()
+        want, want_lse, tol, tol_lse, _, _ = plain.attend(c, qn, at, held)
+        _close(out, want, tol)
+        _close(lse, want_lse, tol_lse)
+        accepted = [int(self.rng.integers(0, n + 1)) for n in counts]
+        kept = _i32(accepted)
+        binding.polyspec_cache_weigh(self.pages, q, self.pool, self.kv, _i32(at), base, lse, self.weights, n_rows=kept, device_status=self.status)
+        binding.polyspec_cache_rollback(self.pages, base, kept, device_status=self.status)
+        _, _, _, _, more, tol_w = plain.attend(c, qn, at, held, n_rows=accepted)
+        self.text = [t - n + a for t, n, a in zip(self.text, counts, accepted)]
+        for b, a in enumerate(accepted):
+            m = held[b] + a
+            for have in (self.codes, self.scale, self.offset):
+                for p in range(2):
+                    have[p][b] = have[p][b][:m]
+            _close(self.weights[b, :m], (self.w[b] + more[b])[:m], (tol_w[b] + 4 * plain.U32 * (self.w[b] + more[b]))[:m])
+            self.w[b] = self.weights[b, :m].double().cpu().numpy()          # (the next comparison starts from what is there)
+
+    def evict(self, budget):
+        binding.polyspec_cache_evict(self.pages, _i32([budget] * len(self.lens)), self.weights, self.pool, self.kv, self.d, first=2, recent=8, device_status=self.status)
+        for b in range(len(self.lens)):
+            keep = plain.evict_slots(self.w[b].astype(np.float32), len(self.w[b]), budget, 2, 8)
+            if keep is not None:
+                self.w[b] = self.w[b][keep]
+                for have in (self.codes, self.scale, self.offset):
+                    for p in range(2):
+                        have[p][b] = have[p][b][keep]
+        assert self.pages.len.tolist() == [len(x) for x in self.w]
+
+
+@pytest.mark.parametrize("lens,heads,kv,d,P", [([70, 33, 1], 4, 2, 64, 8), ([150, 40], 8, 2, 128, 16), ([130, 5, 64], 12, 4, 128, 24)])
+def test_a_whole_run(lens, heads, kv, d, P):
+    run = Run(lens, heads, kv, d, P, 300)
+    run.prompt()
+    for i in range(4):
+        run.block([1 + (b + i) % 6 for b in range(len(lens))])
+        if i % 2:
+            run.evict(40)
+    assert int(run.status) == 0
