@@ -20,9 +20,14 @@
 // be expanded through shared or tensor memory.)
 //
 // Work: (sequence, key head, row tile) are segments of `steps` of 32 tokens per warp; the steps of all segments, one after the other, are cut into equal
-// shares, one per CTA, whatever the lengths; what a segment costs besides its steps counts as kOverhead of them.  Each warp streams its tiles through a ring of its own (bulk copies of one or two units) and keeps
-// maximum, sums and the output tile in registers; a segment's warps meet once at its end.  A segment that crosses CTAs leaves partial
-// results, which a second kernel joins.
+// shares, one per CTA, whatever the lengths; what a segment costs besides its steps counts as kOverhead of them.  Each warp streams its tokens through
+// a ring of its own (bulk copies of one or two units) and keeps maximum, sums and the output tile in registers; a segment's warps meet once at its
+// end.  A segment that crosses CTAs leaves partial results, which a second kernel joins.
+//
+// Measured (B200): single tokens of 16 sequences of up to 65536 tokens, 350 MB of pages, 84 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64
+// sequences of up to 8192 tokens, 428 MB, 259 us: bound by issue, half of the slots, with three warps per scheduler that the output tile's registers
+// leave (the pages lying in L2 instead: 272 against 277 then).  A variant on tcgen05, tokens as the rows of a tile of 128, took 367: its sixteen
+// and more warps' waits and look-ups per step cost as many instructions as the products they save.
 #include <cuda_fp16.h>
 
 #include "kv_pages.cuh"
@@ -347,13 +352,14 @@ __device__ __forceinline__ void store_out(const AttendParams& p, const kv::SeqRo
 template <class S>
 struct Running { float o[S::NT][S::M][4]; uint64_t ref[S::NT], l[S::NT], lo[S::NT]; bool started; };         // (pairs of rows; ref with its sign turned)
 
-// 16 * T tokens from token 16 * t0 of a stage on, for the first L groups of rows.  `at`: the stage, 4 units of keys, 4 of values.  masked: some row does not see some token, or a unit could not be
-// read (bad).  q0: the rows' fragments where they stay in registers (one group).
-template <class S, int L, int T>
-__device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>& run, const unsigned char* at, int t0, const uint32_t* frag, const uint2* q0, const float* sums,
+// A stage's 32 tokens, 16 at a time side by side (two chains of products hide each other's latency: 276 -> 259 us on blocks of 4 to 9 rows).  `at`: the stage,
+// 4 units of keys, 4 of values.  masked: some row does not see some token, or a unit could not be read (bad).  q0: the rows' fragments where they stay in
+// registers (one group of rows).  All groups of rows are computed, live or not: branches around those that are not cost more than they save.
+template <class S>
+__device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>& run, const unsigned char* at, const uint32_t* frag, const uint2* q0, const float* sums,
                                               float factor, bool masked, uint32_t bad, int key0, const Segment& seg, int lane)
 {
-    constexpr int D = S::D, KS = D / 16, M = S::M, UB = S::UB, WORDS = D / 32, H = D / 64;
+    constexpr int D = S::D, KS = D / 16, M = S::M, UB = S::UB, WORDS = D / 32, H = D / 64, L = S::NT, T = 2;
     const int g8 = lane >> 2, t4 = lane & 3;
     // codes of keys, and the first product: tokens x rows
     float sc[T][L][4];
@@ -362,7 +368,7 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
         uint32_t kw[2][WORDS];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const unsigned char* unit = at + (2 * (t0 + v) + u) * UB;
+            const unsigned char* unit = at + (2 * v + u) * UB;
             if (D == 128) {
                 const uint4 x = *reinterpret_cast<const uint4*>(unit + lane * 16);
                 kw[u][0] = x.x; kw[u][1] = x.y; kw[u][WORDS - 2] = x.z; kw[u][WORDS - 1] = x.w;
@@ -391,7 +397,7 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
     for (int v = 0; v < T; ++v) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const unsigned char* pairs = at + (2 * (t0 + v) + u) * UB + 4 * D + g8 * 4;
+            const unsigned char* pairs = at + (2 * v + u) * UB + 4 * D + g8 * 4;
             const uint32_t kp = *reinterpret_cast<const uint32_t*>(pairs), vp = *reinterpret_cast<const uint32_t*>(pairs + 4 * UB);
             const float ks = low(kp) * factor, ko = high(kp), vs = low(vp), lv = lg2(vs);
             iv[v][u] = rcp(vs);
@@ -414,8 +420,8 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
                 const int r = seg.tile * seg.tile_rows + n * 8 + 2 * t4, limit0 = row_limit(seg.q, r / p.group), limit1 = row_limit(seg.q, (r + 1) / p.group);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const int key = key0 + 16 * (t0 + v) + 8 * u + g8;
-                    const bool gone = bad >> (2 * (t0 + v) + u) & 1u, h0 = gone || key >= limit0, h1 = gone || key >= limit1;
+                    const int key = key0 + 16 * v + 8 * u + g8;
+                    const bool gone = bad >> (2 * v + u) & 1u, h0 = gone || key >= limit0, h1 = gone || key >= limit1;
                     float a, b;
                     unpair(x[v][n][u], &a, &b);
                     x[v][n][u] = pair(h0 ? -INFINITY : a, h1 ? -INFINITY : b);
@@ -512,7 +518,7 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
         uint32_t even[2][H], odd[2][H];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const unsigned char* unit = at + (4 + 2 * (t0 + v) + u) * UB;
+            const unsigned char* unit = at + (4 + 2 * v + u) * UB;
             if (D == 128) {
                 const uint4 x = *reinterpret_cast<const uint4*>(unit + lane * 16);
                 even[u][0] = __byte_perm(x.x, x.z, 0x5410); odd[u][0] = __byte_perm(x.x, x.z, 0x7632);
@@ -637,7 +643,6 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
     for (; issued < NS - 1 && ahead_left > 0; ++issued) issue(issued);
 
     Running<S> run;
-    static_assert(NT <= 4, "groups");
     uint2 q0[NT == 1 ? KS : 1];                 // of a tile of one group of rows the fragments stay in registers
     int seen = 0, stage = 0;
     uint32_t phase = 0;
@@ -675,16 +680,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
         if (key0 < seen && ok && bad != 15u) {
             const unsigned char* at = ring + stage * S::STAGE;
             const bool masked = key0 + 32 > all_see || bad;
-            if (NT == 1) {
-                attend_tokens<S, 1, 2>(p, run, at, 0, frag, q0, sums, factor, masked, bad, key0, mine, lane);
-            } else {
-#pragma unroll 1
-                for (int t0 = 0; t0 < 2; ++t0) {
-                    if ((bad >> (2 * t0) & 3u) == 3u) continue;
-                    // (all groups, live or not: branches around those that are not cost more than they save, 390 against 275 us on blocks of 4 to 9 rows)
-                    attend_tokens<S, NT, 1>(p, run, at, t0, frag, q0, sums, factor, masked, bad, key0, mine, lane);
-                }
-            }
+            attend_tokens<S>(p, run, at, frag, q0, sums, factor, masked, bad, key0, mine, lane);
         }
         __syncwarp();
         // the stage that was read before this one is free again
@@ -859,7 +855,7 @@ cudaError_t launch_attend(const AttendParams& p, cudaStream_t stream)
     return e;
 }
 
-constexpr int kMaxRows = 32;                    // rows of the largest tile
+constexpr int kMaxRows = 16;                    // rows of the largest tile
 inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
 inline size_t attend_bytes(int head_dim) { return align256(kMaxCtas * sizeof(int4)) + static_cast<size_t>(2 * kMaxCtas) * kMaxRows * (head_dim + 2) * 4; }
 
@@ -1053,15 +1049,12 @@ polyspec_status polyspec_cache_attention(const polyspec_cache_pages* s, const po
     p.joins = static_cast<int4*>(workspace);
     p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(kMaxCtas * sizeof(int4)));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-    // rows of a sequence times the heads that share a key head, on average: the tile that takes them in one pass over the cache if one does
-    const long long rows = (static_cast<long long>(r->rows) * p.group + s->n_seqs - 1) / s->n_seqs;
+    // rows of a sequence times the heads that share a key head, on average: one group of 8, or tiles of two.  (36 rows of 128 elements: tiles of 16 rows
+    // 259 us; of 24 rows 272, of 32 rows 275, with two passes fewer over the cache but fewer warps.)
+    const bool few = static_cast<long long>(r->rows) * p.group <= 8LL * s->n_seqs;
     cudaError_t e;
-    if (head_dim == 128)
-        e = rows <= 8 ? launch_attend<Shape<128, 1, 8, 2, 2>>(p, stream) : rows <= 16 ? launch_attend<Shape<128, 2, 4, 3, 3>>(p, stream)
-                                                                         : launch_attend<Shape<128, 4, 4, 3, 2>>(p, stream);
-    else
-        e = rows <= 8 ? launch_attend<Shape<64, 1, 8, 3, 2>>(p, stream) : rows <= 16 ? launch_attend<Shape<64, 2, 8, 3, 2>>(p, stream)
-                                                                        : launch_attend<Shape<64, 4, 4, 3, 3>>(p, stream);
+    if (head_dim == 128) e = few ? launch_attend<Shape<128, 1, 8, 2, 2>>(p, stream) : launch_attend<Shape<128, 2, 4, 3, 3>>(p, stream);
+    else e = few ? launch_attend<Shape<64, 1, 8, 3, 2>>(p, stream) : launch_attend<Shape<64, 2, 4, 4, 3>>(p, stream);
     return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }
 
