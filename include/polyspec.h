@@ -525,7 +525,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
 
 /*
  * A model's attention around the cache pages: what its pass over a prompt or a block needs between its projections and its LM head.
- * All of it takes rows of heads in bf16: [rows, heads, head_dim] with the heads of a row behind one another and `stride` elements from
+ * At most 2^24 rows, and in attention 1024 query heads.  All of it takes rows of heads in bf16: [rows, heads, head_dim] with the heads of a row behind one another and `stride` elements from
  * row to row (a multiple of 8, at least heads * head_dim), 16-byte aligned, so that queries, keys and values may be parts of the rows of
  * one fused projection.  Outputs of heads are contiguous.
  *
@@ -550,8 +550,8 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *   (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE in *device_status); POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.
  *
  * Caches held in 4 bits.  One plane of a pool holds one layer's keys or values; a token's head is head_dim codes with one scale and one
- * offset (bf16): value = scale * code + offset, scale a normal number > 0.  A page of polyspec_cache_pages (page_tokens a multiple of 8, at most 32768) is
- * [kv_heads, page_tokens / 8] units of 8 tokens; a unit is head_dim 32-bit words of codes, then 8 pairs (scale, offset):
+ * offset (bf16): value = scale * code + offset, scale a normal number > 0.  A page of polyspec_cache_pages (page_tokens a multiple of 8, at most 32768,
+ * and max_pages * page_tokens at most 2^31 - 2^16) is [kv_heads, page_tokens / 8] units of 8 tokens; a unit is head_dim 32-bit words of codes, then 8 pairs (scale, offset):
  * page_bytes = kv_heads * (page_tokens / 8) * (4 head_dim + 32).  Code e of eight neighbours is in the four bits from bit
  * 4 * (e / 2) + 16 * (e % 2) on of their word.  Word w of token r lies at r * head_dim/8 + w in a unit of keys; in a unit of values, with
  * w = 8 h + g, at (8 g + r) * head_dim/64 + h (where the attention's matrix instructions want it).
@@ -576,6 +576,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *   multiplied as whole numbers, scales and offsets applied to fp32 sums; softmax weights are rounded to fp16 for their product
  *   with the codes.  The order of the sums depends on the lengths and on the batch.
  *   Workspace of polyspec_cache_attention_workspace bytes.
+ *   POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.
  *
  * polyspec_cache_weigh -- adds to every cached token the attention weight that the rows gave it, over all heads:
  *     weights[b, j] = keep * weights[b, j] + sum_{i, h} exp(scale * q[i, h] . K[j, .] - lse[i, h])   for j < len[b]
@@ -586,7 +587,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *   largest weight (the lower slot of equal ones; NaN below everything) until budget[b] are left.  What is kept moves together in
  *   every plane of the pool and in the weights, in order; pages wholly behind are given back, len follows.  What lies behind the kept tokens in
  *   a page or in the weights stays as it is.  A sequence stays as it was (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE) if its budget is below first + recent, or
- *   if a page from the first changed slot on is held by others too.
+ *   if a page from the first changed slot on is held by others too, as the holds were before the call.
  *   kept_from  out [n_seqs, max_pages * page_tokens] or NULL: the slot each kept token of a shortened sequence had, -1 behind them;
  *              sequences that were not shortened get -1 throughout.
  *   Workspace of polyspec_cache_evict_workspace bytes.

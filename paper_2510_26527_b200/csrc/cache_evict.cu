@@ -2,8 +2,7 @@
 // heaviest stay, what stays moves together in every plane, pages behind it are given back.
 //
 // Two launches.  The first, one CTA per sequence, finds the weight of the last token that stays (radix selection over the weights' bits,
-// four passes of eight bits), lists the slots that stay in order, moves the weights, gives pages back.  The second moves the contents:
-// a CTA per sequence, head and run of planes goes through the kept tokens in order, kBatch at a time.  A token never moves up, so a batch that has been
+// four passes of eight bits), lists the slots that stay in order, moves the weights, lists the slots that stay in order, moves the weights.  The second gives pages back and moves the contents: per sequence, head and run of planes goes through the kept tokens in order, kBatch at a time.  A token never moves up, so a batch that has been
 // read before it is written overwrites nothing that a later batch reads.
 // Moving is HBM-bound: each token that moves is read and written once.
 #include <algorithm>
@@ -19,7 +18,7 @@ constexpr int kMoveThreads = 256;
 constexpr int kKeyRoom = 49152;                 // longest cache whose weights are held in shared memory
 
 struct EvictPlan {
-    int32_t* head;          // [n_seqs, 4]: first new slot whose token moves, tokens kept (0: sequence stays as it is)
+    int32_t* head;          // [n_seqs, 4]: first new slot whose token moves, tokens kept, first page that goes, pages held (0, 0, 0, 0: sequence stays as it is)
     int32_t* from;          // [n_seqs, cap]: the slot that kept token i had
     float* weights;         // [n_seqs, cap]: its weight
     int32_t* pages;         // [n_seqs, max_pages]: the table as it was
@@ -93,11 +92,11 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
     const int b = blockIdx.x, tid = threadIdx.x;
     const size_t cap = static_cast<size_t>(s.max_pages) * s.page_tokens;
     float* w = weights + b * cap;
-    int32_t* row = s.table + static_cast<size_t>(b) * s.max_pages;
+    const int32_t* row = s.table + static_cast<size_t>(b) * s.max_pages;
     int32_t* from = plan.from + b * cap;
     wait_for_stream();
     const int len = s.len[b], budget = budgets[b];
-    if (tid == 0) { plan.head[4 * b] = 0; plan.head[4 * b + 1] = 0; }
+    if (tid < 4) plan.head[4 * b + tid] = 0;
     bool stays = budget < 0 || len <= budget;
     if (len < 0 || len > static_cast<long long>(cap) || (!stays && budget < static_cast<long long>(first) + recent)) {
         if (tid == 0) kv::report(status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
@@ -121,13 +120,16 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
     for (int shift = 24; shift >= 0; shift -= 8) {
         if (tid < 256) hist[tid] = 0;
         __syncthreads();
-        for (int i = first + tid; i < end; i += kSelectThreads) {
-            const uint32_t key = key_of(i);
-            if (shift == 24 || key >> (shift + 8) == bits) {
-                // (weights of one size share their leading bits: one add per warp and digit)
-                const uint32_t digit = key >> shift & 255u, peers = __match_any_sync(__activemask(), digit);
-                if ((tid & 31) == __ffs(peers) - 1) atomicAdd(&hist[digit], __popc(peers));
+        for (int i0 = first + (tid & ~31); i0 < end; i0 += kSelectThreads) {
+            const int i = i0 + (tid & 31);
+            uint32_t digit = 256;               // of no interest
+            if (i < end) {
+                const uint32_t key = key_of(i);
+                if (shift == 24 || key >> (shift + 8) == bits) digit = key >> shift & 255u;
             }
+            // (weights of one size share their leading bits: one add per warp and digit)
+            const uint32_t peers = __match_any_sync(0xffffffffu, digit);
+            if (digit < 256 && (tid & 31) == __ffs(peers) - 1) atomicAdd(&hist[digit], __popc(peers));
         }
         __syncthreads();
         if (tid < 32) {                         // from the top digit down, eight digits a lane
@@ -188,7 +190,8 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
     if (moved < budget) atomicMin(&first_moved, moved);
     __syncthreads();
 
-    // nobody else may hold a page that changes; pages wholly behind what stays only lose this sequence's hold
+    // nobody else may hold a page that changes; pages wholly behind what stays only lose this sequence's hold, in the second launch: until then every
+    // sequence sees the holds as they were, whichever CTA comes first
     const int P = s.page_tokens, keep_pages = (budget + P - 1) / P, held = (len + P - 1) / P;
     for (int i = tid; i < held; i += kSelectThreads) {
         const int page = row[i];
@@ -204,17 +207,12 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
     for (int i = first_moved + tid; i < budget; i += kSelectThreads) w[i] = plan.weights[b * cap + i];
     if (kept_from)
         for (int i = tid; i < budget; i += kSelectThreads) kept_from[b * cap + i] = from[i];
-    for (int i = keep_pages + tid; i < held; i += kSelectThreads) {
-        const int page = row[i];
-        const int was = atomicSub(&s.refs[page], 1);
-        if (was == 1) atomicOr(&s.free_bits[page >> 5], 1u << (page & 31));
-        else if (was <= 0) { atomicAdd(&s.refs[page], 1); kv::report(status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE); }
-        row[i] = -1;
-    }
     if (tid == 0) {
         s.len[b] = budget;
         plan.head[4 * b] = first_moved;
         plan.head[4 * b + 1] = budget;
+        plan.head[4 * b + 2] = keep_pages;
+        plan.head[4 * b + 3] = held;
     }
 }
 
@@ -222,7 +220,7 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
 // CTA's planes (divisions by the page's size took more time than the copies), a batch ahead of its use.
 template <int D>
 __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec_cache_pages s, EvictPlan plan, unsigned char* pool, size_t page_bytes,
-                                                                  int kv_heads, int n_planes, int run)
+                                                                  int kv_heads, int n_planes, int run, int32_t* status)
 {
     constexpr int kBatch = kMoveThreads;        // tokens at a time
     constexpr int kPieces = D / 32;             // 16-byte pieces of a token's codes
@@ -236,6 +234,13 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec
     const int32_t* pages = plan.pages + static_cast<size_t>(b) * s.max_pages;
     wait_for_stream();
     const int begin = plan.head[4 * b], end = plan.head[4 * b + 1];
+    if (blockIdx.x == 0)                        // the sequence's hold on what lies wholly behind
+        for (int i = plan.head[4 * b + 2] + tid; i < plan.head[4 * b + 3]; i += kMoveThreads) {
+            const int page = pages[i], was = atomicSub(&s.refs[page], 1);
+            if (was == 1) atomicOr(&s.free_bits[page >> 5], 1u << (page & 31));
+            else if (was <= 0) { atomicAdd(&s.refs[page], 1); kv::report(status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE); }
+            s.table[static_cast<size_t>(b) * s.max_pages + i] = -1;
+        }
     if (begin >= end) return;
     auto place = [&](int slot) {
         const int unit = slot / kv::kUnit, at = unit / units;
@@ -298,7 +303,7 @@ extern "C" {
 polyspec_status polyspec_cache_evict_workspace(int n_seqs, int max_pages, int page_tokens, size_t* bytes)
 {
     if (!bytes || n_seqs < 1 || max_pages < 1 || page_tokens < 1) return POLYSPEC_ERR_INVALID_ARG;
-    if (static_cast<long long>(max_pages) * page_tokens > 0x7fffffffLL) return POLYSPEC_ERR_UNSUPPORTED;
+    if (static_cast<long long>(max_pages) * page_tokens > kv::kMostTokens) return POLYSPEC_ERR_UNSUPPORTED;
     *bytes = evict_bytes(n_seqs, max_pages, page_tokens);
     return POLYSPEC_OK;
 }
@@ -331,8 +336,8 @@ polyspec_status polyspec_cache_evict(const polyspec_cache_pages* s, const int32_
         const dim3 grid(static_cast<unsigned>((n_planes + run - 1) / run * kv_heads), static_cast<unsigned>(s->n_seqs));
         unsigned char* data = static_cast<unsigned char*>(pool);
         const size_t bytes = kv::page_bytes(*s, kv_heads, head_dim);
-        e = head_dim == 128 ? launch_early(evict_move_kernel<128>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads, n_planes, run)
-                            : launch_early(evict_move_kernel<64>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads, n_planes, run);
+        e = head_dim == 128 ? launch_early(evict_move_kernel<128>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads, n_planes, run, device_status)
+                            : launch_early(evict_move_kernel<64>, grid, kMoveThreads, 0, stream, *s, plan, data, bytes, kv_heads, n_planes, run, device_status);
     }
     return cuda_failed(e) ? POLYSPEC_ERR_CUDA : POLYSPEC_OK;
 }

@@ -12,6 +12,7 @@ namespace polyspec {
 namespace kv {
 
 constexpr int kUnit = 8;                        // tokens of a unit
+constexpr long long kMostTokens = 0x7fff0000;   // of a sequence: counters may run past its end by a CTA's step
 
 __host__ __device__ constexpr int unit_bytes(int head_dim) { return 4 * head_dim + 4 * kUnit; }
 inline size_t page_bytes(const polyspec_cache_pages& s, int kv_heads, int head_dim)
@@ -66,7 +67,7 @@ inline polyspec_status check_state(const polyspec_cache_pages* s)
 {
     if (!s || s->n_seqs < 1 || s->max_pages < 1 || s->n_pages < 1 || s->page_tokens < 1) return POLYSPEC_ERR_INVALID_ARG;
     if (!s->table || !s->len || !s->refs || !s->free_bits || !aligned4(s->table, s->len, s->refs, s->free_bits)) return POLYSPEC_ERR_INVALID_ARG;
-    if (static_cast<long long>(s->max_pages) * s->page_tokens > 0x7fffffffLL || s->n_pages > (1 << 20)) return POLYSPEC_ERR_UNSUPPORTED;
+    if (static_cast<long long>(s->max_pages) * s->page_tokens > kMostTokens || s->n_pages > (1 << 20)) return POLYSPEC_ERR_UNSUPPORTED;
     return s->page_tokens % kUnit || s->page_tokens > 32768 ? POLYSPEC_ERR_UNSUPPORTED : POLYSPEC_OK;
 }
 

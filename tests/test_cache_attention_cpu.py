@@ -95,6 +95,13 @@ def test_calls_on_pages_refuse_bad_states(lib, change, status):
     assert lib.polyspec_cache_evict(_pages(**change), FAKE, 0, 0, FAKE, FAKE, 2, 4, 128, None, None, FAKE, BIG, None) == status
 
 
+def test_calls_on_pages_refuse_caches_whose_ends_counters_would_pass(lib):
+    assert _all_calls(lib, _pages(max_pages=65535, page_tokens=32768), _rows()) == {UNSUPPORTED}
+    assert lib.polyspec_cache_evict(_pages(max_pages=65535, page_tokens=32768), FAKE, 0, 0, FAKE, FAKE, 2, 4, 128, None, None, FAKE, BIG, None) == UNSUPPORTED
+    assert lib.polyspec_cache_evict_workspace(4, 65535, 32768, ctypes.byref(ctypes.c_size_t(0))) == UNSUPPORTED
+    assert lib.polyspec_cache_evict_workspace(4, 65534, 32768, ctypes.byref(ctypes.c_size_t(0))) == binding.OK
+
+
 @pytest.mark.parametrize("change,status", [
     ({"rows_at": None}, INVALID), ({"base": None}, INVALID), ({"rows": 0}, INVALID), ({"n_rows": FAKE + 1}, INVALID), ({"extra": FAKE + 2}, INVALID), ({"rows": 1 << 25}, UNSUPPORTED),
 ])

@@ -413,6 +413,36 @@ def test_evict_leaves_sequences_whose_pages_others_hold():
     assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
 
 
+def test_evict_of_two_holders_of_a_page_at_once():
+    # a page that changes in sequence 2 k lies behind what sequence 2 k + 1 keeps, and some of what that keeps comes from it: whichever is looked at
+    # first, the page has two holders, 2 k stays as it was
+    pairs, kv, d, P = 100, 2, 64, 8
+    c = plain.Cache([64] * (2 * pairs), kv, d, P, 145)
+    w = np.zeros((2 * pairs, c.cap), np.float32)
+    for b in range(0, 2 * pairs, 2):
+        c.refs[c.table[b, 5]] = 0
+        c.table[b, 5] = c.table[b + 1, 7]
+        c.refs[c.table[b, 5]] = 2
+        for p in range(2):
+            for x in (c.codes, c.scale, c.offset):
+                x[p][b][40:48] = x[p][b + 1][56:64]
+        w[b, :36], w[b, 44:64] = 1, 1                       # of a budget of 56; slots 36 .. change
+        w[b + 1, :8], w[b + 1, 40:64] = 1, 1                # of a budget of 32; slots 8 .. change
+    pages, pool = c.to(DEV), c.pool()
+    on = c.words_on(pool, DEV)
+    st = binding.polyspec_cache_evict(pages, _i32([56, 32] * pairs), torch.from_numpy(w).to(DEV), on, kv, d)
+    assert int(st) == BAD
+    assert pages.len.tolist() == [64, 32] * pairs
+    for b in range(1, 2 * pairs, 2):
+        for p in range(2):
+            c.put(pool, p, b, range(8, 32), c.codes[p][b][40:64], c.scale[p][b][40:64], c.offset[p][b][40:64])
+        c.refs[c.table[b, 4:8]] -= 1
+        c.table[b, 4:8] = -1
+    assert (pages.table.cpu().numpy() == c.table).all() and (pages.refs.cpu().numpy() == c.refs).all()
+    assert (pages.free_bits.cpu().numpy() == c.free_bits()).all()
+    assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
+
+
 # ------------------------------------------------------------------ prompts
 @pytest.mark.parametrize("lens,heads,kv,d", [
     ([1], 1, 1, 64), ([1, 2, 3], 4, 2, 128), ([127, 128, 129], 2, 1, 128), ([300, 0, 5], 3, 3, 64), ([513], 6, 2, 128), ([64, 65, 63, 255, 257], 8, 2, 64),
