@@ -109,6 +109,14 @@ __device__ __forceinline__ void tmem_st32(uint32_t addr, const uint32_t* r)
           "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]),
           "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
 }
+// Waits for loads from tensor memory; what they filled is not used before.
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait(float (&r)[N])
+{
+    tensordev::tmem_ld_wait();
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+f"(r[i]));
+}
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 __device__ __forceinline__ float ex2(float x)
@@ -164,7 +172,7 @@ __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatil
         if (mbar_try(bar, parity)) { ok = true; break; }
         if ((i & 63u) == 63u) {
             if (*abort_flag) break;
-            if (i >= 4096u) __nanosleep(500);
+            if (i >= 4096u) __nanosleep(i >= 65536u ? 4000 : 500);
         }
     }
     return __all_sync(0xffffffffu, ok);
@@ -559,7 +567,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                 float s[kTileRows];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) tmem_ld32(s_at + i * 32, s + i * 32);
-                tmem_ld_wait();
+                tmem_ld_wait(s);
                 if (j + 1 == steps) {
 #pragma unroll
                     for (int i = 0; i < kTileRows; ++i)
@@ -578,7 +586,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                     for (int i = 0; i < D / 32; ++i) {
                         float o[32];
                         tmem_ld32(o_at + i * 32, o);
-                        tmem_ld_wait();
+                        tmem_ld_wait(o);
 #pragma unroll
                         for (int e = 0; e < 32; ++e) o[e] *= by;
                         tmem_st32(o_at + i * 32, reinterpret_cast<const uint32_t*>(o));
@@ -625,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                 for (int i = 0; i < D / 32; ++i) {
                     float o[32];
                     tmem_ld32(o_at + i * 32, o);
-                    tmem_ld_wait();
+                    tmem_ld_wait(o);
                     if (dirty && live) {
                         // the values that were replaced by 0, from the first key that was watched up to the row's own
                         const int first = it.begin + (it.row_a - it.begin) / kTileRows * kTileRows;
