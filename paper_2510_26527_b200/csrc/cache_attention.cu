@@ -827,15 +827,34 @@ __global__ void __launch_bounds__(256) join_kernel(const AttendParams p)
         float x[8], m = kNone, l = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-        for (int k = 0; k < job.x; ++k) {
-            const float* part = p.partial + static_cast<size_t>(k ? 2 * (blockIdx.x + k) : 2 * blockIdx.x + 1) * S::PART;
-            const float2 ml = *reinterpret_cast<const float2*>(part + S::ROWS * D + 2 * r);
-            const float4 a = reinterpret_cast<const float4*>(part + r * D + d0)[0], b = reinterpret_cast<const float4*>(part + r * D + d0)[1];
-            const float to = fmaxf(m, ml.x), was = ex2(m - to), is = ex2(ml.x - to);
+        // eight parts' numbers are on their way at a time: single tokens over a few thousand have a part per 256 of them
+        for (int k0 = 0; k0 < job.x; k0 += 8) {
+            float2 ml[8];
+            float4 a[8], b[8];
+            float to = m;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const int k = min(k0 + u, job.x - 1);
+                const float* part = p.partial + static_cast<size_t>(k ? 2 * (blockIdx.x + k) : 2 * blockIdx.x + 1) * S::PART;
+                ml[u] = *reinterpret_cast<const float2*>(part + S::ROWS * D + 2 * r);
+                a[u] = reinterpret_cast<const float4*>(part + r * D + d0)[0];
+                b[u] = reinterpret_cast<const float4*>(part + r * D + d0)[1];
+            }
+#pragma unroll
+            for (int u = 0; u < 8; ++u) to = fmaxf(to, ml[u].x);
+            const float was = ex2(m - to);
             m = to;
-            l = fmaf(l, was, ml.y * is);
-            x[0] = fmaf(x[0], was, a.x * is); x[1] = fmaf(x[1], was, a.y * is); x[2] = fmaf(x[2], was, a.z * is); x[3] = fmaf(x[3], was, a.w * is);
-            x[4] = fmaf(x[4], was, b.x * is); x[5] = fmaf(x[5], was, b.y * is); x[6] = fmaf(x[6], was, b.z * is); x[7] = fmaf(x[7], was, b.w * is);
+            l *= was;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= was;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (k0 + u >= job.x) break;
+                const float is = ex2(ml[u].x - to);
+                l = fmaf(ml[u].y, is, l);
+                x[0] = fmaf(a[u].x, is, x[0]); x[1] = fmaf(a[u].y, is, x[1]); x[2] = fmaf(a[u].z, is, x[2]); x[3] = fmaf(a[u].w, is, x[3]);
+                x[4] = fmaf(b[u].x, is, x[4]); x[5] = fmaf(b[u].y, is, x[5]); x[6] = fmaf(b[u].z, is, x[6]); x[7] = fmaf(b[u].w, is, x[7]);
+            }
         }
         store_out(p, q, job.z, job.w + r, D, d0, x, m, l);
     }
