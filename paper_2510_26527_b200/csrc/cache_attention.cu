@@ -60,7 +60,8 @@ struct AttendParams {
     unsigned short* out;
     float* lse;
     float* partial;                             // [2 * CTAs][rows of a tile][head_dim + 2]
-    int4* joins;                                // [CTAs]: (parts, sequence * 64 + row groups, key head, first row) of the segment that begins there and ends elsewhere
+    int4* joins;                                // [2 * CTAs]: of the segment that begins in a CTA and ends elsewhere (parts, rows of its tile, key head, first row), its
+                                                // sequence's rows (first row of the tensors, rows, slot, granted)
     int32_t* status;
 };
 
@@ -565,7 +566,7 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
     __syncwarp();
     wait_for_stream();
 
-    if (threadIdx.x == 0) p.joins[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (threadIdx.x == 0) p.joins[2 * blockIdx.x] = make_int4(0, 0, 0, 0);
     Share share;
     if (!find_share<S>(p, &found, warp_sums, share)) return;
     const long long s0 = share.begin, s1 = share.end, total = share.total, ctas = share.ctas, within = share.within;
@@ -787,7 +788,8 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
             // the CTAs that the rest of the segment falls to
             const long long last = s1 + (steps - step) - 1;             // the place of its last step
             const int at = static_cast<int>(((last + 1) * ctas - 1) / total);
-            p.joins[blockIdx.x] = make_int4(at - static_cast<int>(blockIdx.x) + 1, mine.b << 6 | mine.tile_rows / 8, mine.head, row0);
+            p.joins[2 * blockIdx.x] = make_int4(at - static_cast<int>(blockIdx.x) + 1, mine.tile_rows, mine.head, row0);
+            p.joins[2 * blockIdx.x + 1] = make_int4(mine.q.row0, mine.q.n, mine.q.base, mine.q.granted);
         }
         __syncthreads();
         if (step == steps) {
@@ -811,52 +813,72 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
     }
 }
 
-// Joins the parts of the segment that begins in CTA blockIdx.x and ends in a later one, in order.
+// Joins the parts of the segment that begins in CTA blockIdx.x and ends in a later one.  A lane takes eight elements of a row, eight parts on their way at
+// a time; of more parts (single tokens over a few thousand: one per 256 of them) four lanes take every fourth.
 template <class S>
 __global__ void __launch_bounds__(256) join_kernel(const AttendParams p)
 {
-    constexpr int D = S::D, kVecs = D / 8;
+    constexpr int D = S::D, kVecs = D / 8, kAhead = 8;
     wait_for_stream();
-    const int4 job = p.joins[blockIdx.x];
+    const int4 job = p.joins[2 * blockIdx.x], rows = p.joins[2 * blockIdx.x + 1];
     if (job.x == 0) return;
-    const kv::SeqRows q = kv::seq_rows(p.s, p.r, job.y >> 6);
-    const int job_rows = (job.y & 63) * 8;
-    for (int item = threadIdx.x; item < S::ROWS * kVecs; item += 256) {
+    const kv::SeqRows q = {rows.x, rows.y, rows.w, rows.z, 0, false};
+    const int share = job.x > kAhead ? 4 : 1, slice = threadIdx.x % share;
+    for (int item = threadIdx.x / share; item < S::ROWS * kVecs; item += 256 / share) {        // (whole warps)
         const int r = item / kVecs, d0 = item % kVecs * 8;
-        if (job.w + r >= q.n * p.group || r >= job_rows) continue;
+        const bool live = job.w + r < q.n * p.group && r < job.y;
         float x[8], m = kNone, l = 0.0f;
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = 0.0f;
-        // eight parts' numbers are on their way at a time: single tokens over a few thousand have a part per 256 of them
-        for (int k0 = 0; k0 < job.x; k0 += 8) {
-            float2 ml[8];
-            float4 a[8], b[8];
+        for (int k0 = slice; live && k0 < job.x; k0 += share * kAhead) {
+            float2 ml[kAhead];
+            float4 a[kAhead], b[kAhead];
             float to = m;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                const int k = min(k0 + u, job.x - 1);
-                const float* part = p.partial + static_cast<size_t>(k ? 2 * (blockIdx.x + k) : 2 * blockIdx.x + 1) * S::PART;
-                ml[u] = *reinterpret_cast<const float2*>(part + S::ROWS * D + 2 * r);
-                a[u] = reinterpret_cast<const float4*>(part + r * D + d0)[0];
-                b[u] = reinterpret_cast<const float4*>(part + r * D + d0)[1];
+            for (int u = 0; u < kAhead; ++u) {
+                const int k = k0 + share * u;
+                if (k < job.x) {
+                    const float* part = p.partial + static_cast<size_t>(k ? 2 * (blockIdx.x + k) : 2 * blockIdx.x + 1) * S::PART;
+                    ml[u] = *reinterpret_cast<const float2*>(part + S::ROWS * D + 2 * r);
+                    a[u] = reinterpret_cast<const float4*>(part + r * D + d0)[0];
+                    b[u] = reinterpret_cast<const float4*>(part + r * D + d0)[1];
+                } else {
+                    ml[u] = make_float2(kNone, 0.0f);
+                    a[u] = b[u] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                }
             }
 #pragma unroll
-            for (int u = 0; u < 8; ++u) to = fmaxf(to, ml[u].x);
+            for (int u = 0; u < kAhead; ++u) to = fmaxf(to, ml[u].x);
             const float was = ex2(m - to);
             m = to;
             l *= was;
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[e] *= was;
 #pragma unroll
-            for (int u = 0; u < 8; ++u) {
-                if (k0 + u >= job.x) break;
+            for (int u = 0; u < kAhead; ++u) {
                 const float is = ex2(ml[u].x - to);
                 l = fmaf(ml[u].y, is, l);
                 x[0] = fmaf(a[u].x, is, x[0]); x[1] = fmaf(a[u].y, is, x[1]); x[2] = fmaf(a[u].z, is, x[2]); x[3] = fmaf(a[u].w, is, x[3]);
                 x[4] = fmaf(b[u].x, is, x[4]); x[5] = fmaf(b[u].y, is, x[5]); x[6] = fmaf(b[u].z, is, x[6]); x[7] = fmaf(b[u].w, is, x[7]);
             }
         }
-        store_out(p, q, job.z, job.w + r, D, d0, x, m, l);
+        if (share > 1) {
+            float top = m;
+#pragma unroll
+            for (int d = 1; d < 4; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+            const float by = ex2(m - top);
+            m = top;
+            l *= by;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] *= by;
+#pragma unroll
+            for (int d = 1; d < 4; d <<= 1) {
+                l += __shfl_xor_sync(0xffffffffu, l, d);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] += __shfl_xor_sync(0xffffffffu, x[e], d);
+            }
+        }
+        if (live && slice == 0) store_out(p, q, job.z, job.w + r, D, d0, x, m, l);
     }
 }
 
@@ -876,7 +898,7 @@ cudaError_t launch_attend(const AttendParams& p, cudaStream_t stream)
 
 constexpr int kMaxRows = 16;                    // rows of the largest tile
 inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-inline size_t attend_bytes(int head_dim) { return align256(kMaxCtas * sizeof(int4)) + static_cast<size_t>(2 * kMaxCtas) * kMaxRows * (head_dim + 2) * 4; }
+inline size_t attend_bytes(int head_dim) { return align256(2 * kMaxCtas * sizeof(int4)) + static_cast<size_t>(2 * kMaxCtas) * kMaxRows * (head_dim + 2) * 4; }
 
 // ---- accumulated weights: w[j] = keep * w[j] + sum over heads and rows of 2^(s2[r, j] - lse2[r])
 struct WeighParams {
@@ -1066,7 +1088,7 @@ polyspec_status polyspec_cache_attention(const polyspec_cache_pages* s, const po
     p.out = static_cast<unsigned short*>(out);
     p.lse = lse;
     p.joins = static_cast<int4*>(workspace);
-    p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(kMaxCtas * sizeof(int4)));
+    p.partial = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(2 * kMaxCtas * sizeof(int4)));
     cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
     // rows of a sequence times the heads that share a key head, on average: one group of 8, or tiles of two.  (36 rows of 128 elements: tiles of 16 rows
     // 259 us; of 24 rows 272, of 32 rows 275, with two passes fewer over the cache but fewer warps.)
