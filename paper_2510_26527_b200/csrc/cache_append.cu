@@ -12,11 +12,40 @@ namespace polyspec {
 namespace {
 
 constexpr int kThreads = 256;
+// 1.5 * 2^23 as bits (the form of whole numbers below), at the places of all eight codes of a word
+constexpr uint32_t kMagicSum = 0x4b400000u * 0x11111111u;
 
 __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
 {
     uint32_t x;
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(a), "r"(b));
+    return x;
+}
+
+__device__ __forceinline__ float max3_abs(float a, float b, float c)
+{
+    float x;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
+    return x;
+}
+// Pairs of fp32 numbers in one instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+    return x;
+}
+__device__ __forceinline__ void unpair(uint64_t x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t x;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
     return x;
 }
 
@@ -46,15 +75,26 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
     const int row0 = blockIdx.x * ROWS, tid = threadIdx.x, w = tid % kLanes, team = tid / kLanes;
     const int per_row = 2 * p.kv_heads, items = min(ROWS, p.r.rows - row0) * per_row;
     uint4 raw[kAhead], coming[kAhead];
-    auto load = [&](uint4* raw, int first) {
+    // an item's row of the CTA and its number in the row; a turn further on without a division
+    struct At { int i, j; };
+    const int turn_rows = kTeams / per_row, turn_rest = kTeams % per_row;
+    auto next = [&](At& at) {
+        at.i += turn_rows;
+        at.j += turn_rest;
+        if (at.j >= per_row) { at.j -= per_row; ++at.i; }
+    };
+    const int rows = min(ROWS, p.r.rows - row0);
+    const __nv_bfloat16 *k_rows = p.k + row0 * p.k_stride + w * 8, *v_rows = p.v + row0 * p.v_stride + w * 8;
+    At read = {team / per_row, team % per_row}, at = read;
+    auto load = [&](uint4* raw) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int item = first + u * kTeams + team, row = row0 + item / per_row, j = item % per_row;
             raw[u] = make_uint4(0, 0, 0, 0);
-            if (item < items) raw[u] = reinterpret_cast<const uint4*>((j & 1 ? p.v + row * p.v_stride : p.k + row * p.k_stride) + (j >> 1) * D)[w];
+            if (read.i < rows) raw[u] = *reinterpret_cast<const uint4*>((read.j & 1 ? v_rows + read.i * p.v_stride : k_rows + read.i * p.k_stride) + (read.j >> 1) * D);
+            next(read);
         }
     };
-    load(coming, 0);
+    load(coming);
     if (row0 == 0)              // numbers that make no sense are reported even where no row belongs to them
         for (int b = tid; b < p.s.n_seqs; b += kThreads)
             if (kv::seq_rows(p.s, p.r, b).bad) kv::report(p.status, POLYSPEC_ERR_BAD_INPUT_ON_DEVICE);
@@ -92,18 +132,18 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
     for (int first = 0; first < items; first += kAhead * kTeams) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) raw[u] = coming[u];
-        if (first + kAhead * kTeams < items) load(coming, first + kAhead * kTeams);
+        if (first + kAhead * kTeams < items) load(coming);
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int item = first + u * kTeams + team;
             if (first + u * kTeams >= items) break;
-            const int i = min(item, items - 1) / per_row, j = item % per_row, head = j >> 1, values = j & 1;
-            const bool live = item < items && units[i] != 0xffffffffu;
-            float x[8];
-            x[0] = __uint_as_float(raw[u].x << 16); x[1] = __uint_as_float(raw[u].x & 0xffff0000u);
-            x[2] = __uint_as_float(raw[u].y << 16); x[3] = __uint_as_float(raw[u].y & 0xffff0000u);
-            x[4] = __uint_as_float(raw[u].z << 16); x[5] = __uint_as_float(raw[u].z & 0xffff0000u);
-            x[6] = __uint_as_float(raw[u].w << 16); x[7] = __uint_as_float(raw[u].w & 0xffff0000u);
+            const int i = min(at.i, rows - 1), head = at.j >> 1, values = at.j & 1;
+            const bool live = at.i < rows && units[i] != 0xffffffffu;
+            next(at);
+            uint64_t x[4];                      // neighbours in pairs
+            x[0] = pair(__uint_as_float(raw[u].x << 16), __uint_as_float(raw[u].x & 0xffff0000u));
+            x[1] = pair(__uint_as_float(raw[u].y << 16), __uint_as_float(raw[u].y & 0xffff0000u));
+            x[2] = pair(__uint_as_float(raw[u].z << 16), __uint_as_float(raw[u].z & 0xffff0000u));
+            x[3] = pair(__uint_as_float(raw[u].w << 16), __uint_as_float(raw[u].w & 0xffff0000u));
             // largest element and largest of the negated ones, two bf16 per instruction, NaN sticking
             const uint32_t sign = 0x80008000u;
             const uint32_t top = max2(max2(raw[u].x, raw[u].y), max2(raw[u].z, raw[u].w));
@@ -121,26 +161,37 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
             const bool broken = !(range <= 3.4e38f);
             if (broken) scale = offset = __uint_as_float(0x7fc00000u);
             const float inv = __fdividef(1.0f, scale), near = scale * 0.49999f;
-            uint32_t word = 0, held[4];
-            float y[8];
+            // the nearest whole number to a product, by adding 1.5 * 2^23; quotients themselves are only divided out where a remainder says that one is near
+            // the middle between two
+            const float magic = 12582912.0f;
+            const uint64_t inv2 = pair(inv, inv), scale2 = pair(-scale, -scale), less = pair(-offset, -offset), more = pair(magic, magic), back = pair(-magic, -magic);
+            uint64_t a[4], t[4];
+            float rest = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                // the nearest whole number, by adding 1.5 * 2^23; the quotient itself is only divided out where the remainder says that it is near the
-                // middle between two
-                const float a = x[e] - offset;
-                float t = __fadd_rn(__fmul_rn(a, inv), 12582912.0f), code = t - 12582912.0f;
-                if (!(fabsf(fmaf(-code, scale, a)) <= near)) {
-                    t = __fadd_rn(__fdiv_rn(a, scale), 12582912.0f);
-                    code = t - 12582912.0f;
+            for (int e = 0; e < 4; ++e) {
+                a[e] = add2(x[e], less);
+                t[e] = fma2(a[e], inv2, more);
+                float r0, r1;
+                unpair(fma2(add2(t[e], back), scale2, a[e]), &r0, &r1);
+                rest = max3_abs(rest, r0, r1);
+            }
+            if (rest > near) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float a0, a1;
+                    unpair(a[e], &a0, &a1);
+                    t[e] = pair(__fadd_rn(__fdiv_rn(a0, scale), magic), __fadd_rn(__fdiv_rn(a1, scale), magic));
                 }
-                word |= (__float_as_uint(t) & 15u) << (4 * (e / 2) + 16 * (e % 2));
-                y[e] = __fadd_rn(__fmul_rn(scale, code), offset);
             }
-            if (broken) {
-                word = 0;
+            uint32_t word = 0;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = scale;
+            for (int e = 0; e < 4; ++e) {
+                float t0, t1;
+                unpair(t[e], &t0, &t1);
+                word += (__float_as_uint(t0) << (4 * e)) + (__float_as_uint(t1) << (4 * e + 16));
             }
+            word -= kMagicSum;
+            if (broken) word = 0;
             // words 8 h + g of a row's values are neighbours for all h: lanes of lower words store both
             const uint32_t other = __shfl_xor_sync(0xffffffffu, word, 8);
             if (!live) continue;
@@ -153,9 +204,12 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
             if (w == 0) to[D + r] = (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
             __nv_bfloat16* out = values ? p.v_held : p.k_held;
             if (out) {
+                uint32_t held[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const __nv_bfloat162 z = __floats2bfloat162_rn(y[2 * e], y[2 * e + 1]);
+                    float y0, y1;               // (a scale of 8 bits times a code is exact; a NaN scale makes all of them NaN)
+                    unpair(fma2(add2(t[e], back), pair(scale, scale), pair(offset, offset)), &y0, &y1);
+                    const __nv_bfloat162 z = __floats2bfloat162_rn(y0, y1);
                     held[e] = *reinterpret_cast<const uint32_t*>(&z);
                 }
                 reinterpret_cast<uint4*>(out + (static_cast<size_t>(row0 + i) * p.kv_heads + head) * D)[w] = make_uint4(held[0], held[1], held[2], held[3]);
