@@ -2,8 +2,13 @@
 //
 //   offset = min(x), scale = (max(x) - offset) / 15 rounded up to bf16, code = rint((x - offset) / scale)
 //
-// A word of eight codes is one lane's 16-byte vector, a head head_dim / 8 lanes; keys and values of a row's head are neighbours in a warp.
-// Rounding the scale up keeps every code at 15 or below, so nothing is cut off.
+// A word of eight codes is one 16-byte vector of a head.  A lane takes two, half a head apart (in units of values their words are neighbours), a head
+// head_dim / 16 lanes: what is computed once per head and lane (ends, scale, addresses) costs as much as the codes themselves, so half as many lanes are
+// faster (54 -> 47 us at the size below).  Rounding the scale up keeps every code at 15 or below, so nothing is cut off.
+//
+// Measured (B200): 17600 rows of 8 heads of 128, 72 MB in and as much of held values out, 19 MB of codes: 43 us, 3.7 TB/s, by issue (72% of the slots) more than
+// by memory (25 us); four rows per CTA of 128 threads (eight of 256 threads 47, four of 64 threads 44).  A block of 420 rows 5.0 us: the chain of loads that finds
+// a row's place.
 #include <cuda_bf16.h>
 
 #include "kv_pages.cuh"
@@ -11,7 +16,7 @@
 namespace polyspec {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 128;
 // 1.5 * 2^23 as bits (the form of whole numbers below), at the places of all eight codes of a word
 constexpr uint32_t kMagicSum = 0x4b400000u * 0x11111111u;
 
@@ -62,19 +67,19 @@ struct AppendParams {
     int kv_heads;
 };
 
-// D: head_dim.  A CTA has ROWS rows; its teams of D / 8 lanes take turns over (row, head, keys or values), kAhead items at a time, whose loads are on
+// D: head_dim.  A CTA has ROWS rows; its teams of D / 16 lanes take turns over (row, head, keys or values), an item ahead with their loads; the first are on
 // their way while the rows' places are looked up (a chain of four loads: sequence, length, page, its holders).
 template <int D, int ROWS>
 __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
 {
-    constexpr int kLanes = D / 8, kTeams = kThreads / kLanes, kAhead = 2;
+    constexpr int kLanes = D / 16, kTeams = kThreads / kLanes;
     __shared__ int found[ROWS];
     __shared__ uint32_t units[ROWS];            // the row's unit of head 0, or ~0: not written
     __shared__ int tokens[ROWS];                // its token of the unit
     wait_for_stream();
     const int row0 = blockIdx.x * ROWS, tid = threadIdx.x, w = tid % kLanes, team = tid / kLanes;
     const int per_row = 2 * p.kv_heads, items = min(ROWS, p.r.rows - row0) * per_row;
-    uint4 raw[kAhead], coming[kAhead];
+    uint4 raw[2], coming[2];
     // an item's row of the CTA and its number in the row; a turn further on without a division
     struct At { int i, j; };
     const int turn_rows = kTeams / per_row, turn_rest = kTeams % per_row;
@@ -87,12 +92,13 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
     const __nv_bfloat16 *k_rows = p.k + row0 * p.k_stride + w * 8, *v_rows = p.v + row0 * p.v_stride + w * 8;
     At read = {team / per_row, team % per_row}, at = read;
     auto load = [&](uint4* raw) {
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            raw[u] = make_uint4(0, 0, 0, 0);
-            if (read.i < rows) raw[u] = *reinterpret_cast<const uint4*>((read.j & 1 ? v_rows + read.i * p.v_stride : k_rows + read.i * p.k_stride) + (read.j >> 1) * D);
-            next(read);
+        raw[0] = raw[1] = make_uint4(0, 0, 0, 0);
+        if (read.i < rows) {
+            const uint4* from = reinterpret_cast<const uint4*>((read.j & 1 ? v_rows + read.i * p.v_stride : k_rows + read.i * p.k_stride) + (read.j >> 1) * D);
+            raw[0] = from[0];
+            raw[1] = from[kLanes];
         }
+        next(read);
     };
     load(coming);
     if (row0 == 0)              // numbers that make no sense are reported even where no row belongs to them
@@ -129,91 +135,87 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
     }
     __syncthreads();
     // (whole warps go round together: the exchange below is warp-wide)
-    for (int first = 0; first < items; first += kAhead * kTeams) {
+    for (int first = 0; first < items; first += kTeams) {
+        raw[0] = coming[0];
+        raw[1] = coming[1];
+        if (first + kTeams < items) load(coming);
+        const int i = min(at.i, rows - 1), head = at.j >> 1, values = at.j & 1;
+        const bool live = at.i < rows && units[i] != 0xffffffffu;
+        next(at);
+        const uint32_t z[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
+        // largest element and largest of the negated ones, two bf16 per instruction, NaN sticking
+        const uint32_t sign = 0x80008000u;
+        uint32_t top = z[0], bottom = z[0] ^ sign;
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) raw[u] = coming[u];
-        if (first + kAhead * kTeams < items) load(coming);
+        for (int e = 1; e < 8; ++e) { top = max2(top, z[e]); bottom = max2(bottom, z[e] ^ sign); }
+        uint32_t ends = max2(__byte_perm(top, bottom, 0x5410), __byte_perm(top, bottom, 0x7632));
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (first + u * kTeams >= items) break;
-            const int i = min(at.i, rows - 1), head = at.j >> 1, values = at.j & 1;
-            const bool live = at.i < rows && units[i] != 0xffffffffu;
-            next(at);
-            uint64_t x[4];                      // neighbours in pairs
-            x[0] = pair(__uint_as_float(raw[u].x << 16), __uint_as_float(raw[u].x & 0xffff0000u));
-            x[1] = pair(__uint_as_float(raw[u].y << 16), __uint_as_float(raw[u].y & 0xffff0000u));
-            x[2] = pair(__uint_as_float(raw[u].z << 16), __uint_as_float(raw[u].z & 0xffff0000u));
-            x[3] = pair(__uint_as_float(raw[u].w << 16), __uint_as_float(raw[u].w & 0xffff0000u));
-            // largest element and largest of the negated ones, two bf16 per instruction, NaN sticking
-            const uint32_t sign = 0x80008000u;
-            const uint32_t top = max2(max2(raw[u].x, raw[u].y), max2(raw[u].z, raw[u].w));
-            const uint32_t bottom = max2(max2(raw[u].x ^ sign, raw[u].y ^ sign), max2(raw[u].z ^ sign, raw[u].w ^ sign));
-            uint32_t ends = max2(__byte_perm(top, bottom, 0x5410), __byte_perm(top, bottom, 0x7632));
+        for (int d = 1; d < kLanes; d <<= 1) ends = max2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
+        float offset = __uint_as_float((ends ^ sign) & 0xffff0000u) + 0.0f;         // (not -0)
+        const float range = __uint_as_float(ends << 16) - offset;
+        // range / 15, of which only the bits above the last sixteen are wanted, rounded up: the product says which they are unless it is next to one of their steps
+        float step = range * (1.0f / 15.0f);
+        if (((__float_as_uint(step) + 8u) & 0xffffu) < 17u) step = __fdiv_rn(range, 15.0f);
+        const uint32_t up = (__float_as_uint(step) + 0xffffu) & 0xffff0000u;
+        float scale = up ? fmaxf(__uint_as_float(up), 1.17549435e-38f) : 1.0f;      // at least the smallest normal number
+        const bool broken = !(range <= 3.4e38f);
+        if (broken) scale = offset = __uint_as_float(0x7fc00000u);
+        const float inv = __fdividef(1.0f, scale), near = scale * 0.49999f;
+        // the nearest whole number to a product, by adding 1.5 * 2^23; quotients themselves are only divided out where a remainder says that one is near
+        // the middle between two
+        const float magic = 12582912.0f;
+        const uint64_t inv2 = pair(inv, inv), scale2 = pair(-scale, -scale), less = pair(-offset, -offset), more = pair(magic, magic), back = pair(-magic, -magic);
+        uint64_t a[8], t[8];
+        float rest = 0.0f;
 #pragma unroll
-            for (int d = 1; d < kLanes; d <<= 1) ends = max2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
-            float offset = __uint_as_float((ends ^ sign) & 0xffff0000u) + 0.0f;         // (not -0)
-            const float range = __uint_as_float(ends << 16) - offset;
-            // range / 15, of which only the bits above the last sixteen are wanted, rounded up: the product says which they are unless it is next to one of their steps
-            float step = range * (1.0f / 15.0f);
-            if (((__float_as_uint(step) + 8u) & 0xffffu) < 17u) step = __fdiv_rn(range, 15.0f);
-            const uint32_t up = (__float_as_uint(step) + 0xffffu) & 0xffff0000u;
-            float scale = up ? fmaxf(__uint_as_float(up), 1.17549435e-38f) : 1.0f;      // at least the smallest normal number
-            const bool broken = !(range <= 3.4e38f);
-            if (broken) scale = offset = __uint_as_float(0x7fc00000u);
-            const float inv = __fdividef(1.0f, scale), near = scale * 0.49999f;
-            // the nearest whole number to a product, by adding 1.5 * 2^23; quotients themselves are only divided out where a remainder says that one is near
-            // the middle between two
-            const float magic = 12582912.0f;
-            const uint64_t inv2 = pair(inv, inv), scale2 = pair(-scale, -scale), less = pair(-offset, -offset), more = pair(magic, magic), back = pair(-magic, -magic);
-            uint64_t a[4], t[4];
-            float rest = 0.0f;
+        for (int e = 0; e < 8; ++e) {
+            a[e] = add2(pair(__uint_as_float(z[e] << 16), __uint_as_float(z[e] & 0xffff0000u)), less);
+            t[e] = fma2(a[e], inv2, more);
+            float r0, r1;
+            unpair(fma2(add2(t[e], back), scale2, a[e]), &r0, &r1);
+            rest = max3_abs(rest, r0, r1);
+        }
+        if (rest > near) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                a[e] = add2(x[e], less);
-                t[e] = fma2(a[e], inv2, more);
-                float r0, r1;
-                unpair(fma2(add2(t[e], back), scale2, a[e]), &r0, &r1);
-                rest = max3_abs(rest, r0, r1);
+            for (int e = 0; e < 8; ++e) {
+                float a0, a1;
+                unpair(a[e], &a0, &a1);
+                t[e] = pair(__fadd_rn(__fdiv_rn(a0, scale), magic), __fadd_rn(__fdiv_rn(a1, scale), magic));
             }
-            if (rest > near) {
+        }
+        if (!live) continue;
+        uint32_t words[2] = {0, 0};
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float a0, a1;
-                    unpair(a[e], &a0, &a1);
-                    t[e] = pair(__fadd_rn(__fdiv_rn(a0, scale), magic), __fadd_rn(__fdiv_rn(a1, scale), magic));
-                }
-            }
-            uint32_t word = 0;
+        for (int e = 0; e < 8; ++e) {
+            float t0, t1;
+            unpair(t[e], &t0, &t1);
+            words[e >> 2] += (__float_as_uint(t0) << (4 * (e & 3))) + (__float_as_uint(t1) << (4 * (e & 3) + 16));
+        }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                float t0, t1;
-                unpair(t[e], &t0, &t1);
-                word += (__float_as_uint(t0) << (4 * e)) + (__float_as_uint(t1) << (4 * e + 16));
-            }
-            word -= kMagicSum;
-            if (broken) word = 0;
-            // words 8 h + g of a row's values are neighbours for all h: lanes of lower words store both
-            const uint32_t other = __shfl_xor_sync(0xffffffffu, word, 8);
-            if (!live) continue;
-            unsigned char* plane = p.pool + (values ? static_cast<size_t>(p.s.n_pages) * p.page_bytes : 0);
-            uint32_t* to = reinterpret_cast<uint32_t*>(plane + static_cast<size_t>(units[i] + static_cast<uint32_t>(head * per_page)) * kv::unit_bytes(D));
-            const int r = tokens[i];
-            if (!values) to[kv::key_word(r, w, D)] = word;
-            else if (D == 64) to[kv::value_word(r, w, D)] = word;
-            else if (w < 8) *reinterpret_cast<uint2*>(to + kv::value_word(r, w, D)) = make_uint2(word, other);
-            if (w == 0) to[D + r] = (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
-            __nv_bfloat16* out = values ? p.v_held : p.k_held;
-            if (out) {
-                uint32_t held[4];
+        for (int h = 0; h < 2; ++h) words[h] = broken ? 0 : words[h] - kMagicSum;
+        unsigned char* plane = p.pool + (values ? static_cast<size_t>(p.s.n_pages) * p.page_bytes : 0);
+        uint32_t* to = reinterpret_cast<uint32_t*>(plane + static_cast<size_t>(units[i] + static_cast<uint32_t>(head * per_page)) * kv::unit_bytes(D));
+        const int r = tokens[i];
+        if (D == 128 && values) {
+            *reinterpret_cast<uint2*>(to + kv::value_word(r, w, D)) = make_uint2(words[0], words[1]);
+        } else {
+            to[values ? kv::value_word(r, w, D) : kv::key_word(r, w, D)] = words[0];
+            to[values ? kv::value_word(r, w + kLanes, D) : kv::key_word(r, w + kLanes, D)] = words[1];
+        }
+        if (w == 0) to[D + r] = (__float_as_uint(scale) >> 16) | (__float_as_uint(offset) & 0xffff0000u);
+        __nv_bfloat16* out = values ? p.v_held : p.k_held;
+        if (out) {
+            uint32_t held[8];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float y0, y1;               // (a scale of 8 bits times a code is exact; a NaN scale makes all of them NaN)
-                    unpair(fma2(add2(t[e], back), pair(scale, scale), pair(offset, offset)), &y0, &y1);
-                    const __nv_bfloat162 z = __floats2bfloat162_rn(y0, y1);
-                    held[e] = *reinterpret_cast<const uint32_t*>(&z);
-                }
-                reinterpret_cast<uint4*>(out + (static_cast<size_t>(row0 + i) * p.kv_heads + head) * D)[w] = make_uint4(held[0], held[1], held[2], held[3]);
+            for (int e = 0; e < 8; ++e) {
+                float y0, y1;               // (a scale of 8 bits times a code is exact; a NaN scale makes all of them NaN)
+                unpair(fma2(add2(t[e], back), pair(scale, scale), pair(offset, offset)), &y0, &y1);
+                const __nv_bfloat162 y = __floats2bfloat162_rn(y0, y1);
+                held[e] = *reinterpret_cast<const uint32_t*>(&y);
             }
+            uint4* held_to = reinterpret_cast<uint4*>(out + (static_cast<size_t>(row0 + i) * p.kv_heads + head) * D) + w;
+            held_to[0] = make_uint4(held[0], held[1], held[2], held[3]);
+            held_to[kLanes] = make_uint4(held[4], held[5], held[6], held[7]);
         }
     }
 }
@@ -221,8 +223,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
 template <int D>
 cudaError_t launch_append(const AppendParams& p, cudaStream_t stream)
 {
-    // eight rows share the look-up of their places where there are rows enough for all SMs
-    if (p.r.rows >= 4096) return launch_early(append_kernel<D, 8>, dim3(static_cast<unsigned>((p.r.rows + 7) / 8)), kThreads, 0, stream, p);
+    // four rows share the look-up of their places where there are rows enough for all SMs
+    if (p.r.rows >= 4096) return launch_early(append_kernel<D, 4>, dim3(static_cast<unsigned>((p.r.rows + 3) / 4)), kThreads, 0, stream, p);
     return launch_early(append_kernel<D, 1>, dim3(static_cast<unsigned>(p.r.rows)), kThreads, 0, stream, p);
 }
 
