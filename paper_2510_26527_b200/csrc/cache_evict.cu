@@ -252,45 +252,68 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec
             places[turn][1][tid] = place(i + tid);
         }
     };
+    // An item is a batch of one plane.  The next one's loads are under way while this one's are waited for and stored: what they read lies behind what
+    // this one writes, or in another plane.
+    struct Held { uint4 codes[kPieces]; uint32_t pair; };       // keys: pieces of tokens; values: a token's words, in the order of their groups
+    struct At { int i0, k, turn; };                             // batch, plane of the run, which half of `places`
+    auto unit = [&](const At& at, int which, int t) {
+        return pool + (static_cast<size_t>(plane0 + at.k) * s.n_pages * page_bytes + static_cast<size_t>(places[at.turn][which][t].x) * UB);
+    };
+    auto next = [&](At& at) {
+        if (++at.k < planes) return;
+        at.k = 0;
+        at.i0 += kBatch;
+        at.turn ^= 1;
+    };
+    auto load = [&](const At& at, Held& x) {
+        const int n = min(kBatch, end - at.i0);
+        if (tid < n) x.pair = reinterpret_cast<const uint32_t*>(unit(at, 0, tid))[D + places[at.turn][0][tid].y];
+        if (!((plane0 + at.k) & 1)) {
+#pragma unroll
+            for (int u = 0; u < kPieces; ++u) {
+                const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
+                if (t < n) x.codes[u] = reinterpret_cast<const uint4*>(unit(at, 0, t))[places[at.turn][0][t].y * kPieces + part];
+            }
+        } else if (tid < n) {                   // neighbouring lanes have neighbouring tokens: a group's words of a unit are neighbours
+            const Piece* from = reinterpret_cast<const Piece*>(unit(at, 0, tid)) + places[at.turn][0][tid].y;
+            Piece* y = reinterpret_cast<Piece*>(x.codes);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) y[u] = from[8 * u];
+        }
+    };
+    auto store = [&](const At& at, const Held& x) {
+        const int n = min(kBatch, end - at.i0);
+        if (!((plane0 + at.k) & 1)) {
+#pragma unroll
+            for (int u = 0; u < kPieces; ++u) {
+                const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
+                if (t < n) reinterpret_cast<uint4*>(unit(at, 1, t))[places[at.turn][1][t].y * kPieces + part] = x.codes[u];
+            }
+        } else if (tid < n) {
+            Piece* to = reinterpret_cast<Piece*>(unit(at, 1, tid)) + places[at.turn][1][tid].y;
+            const Piece* y = reinterpret_cast<const Piece*>(x.codes);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) to[8 * u] = y[u];
+        }
+        if (tid < n) reinterpret_cast<uint32_t*>(unit(at, 1, tid))[D + places[at.turn][1][tid].y] = x.pair;
+    };
+    Held one, two;
+    At at = {begin, 0, 0};
     find(0, begin);
     __syncthreads();
-    int turn = 0;
-    for (int i0 = begin; i0 < end; i0 += kBatch, turn ^= 1) {
-        const int n = min(kBatch, end - i0);
-        const uint2 (*at)[kBatch] = places[turn];
-        for (int k = 0; k < planes; ++k) {
-            unsigned char* data = pool + static_cast<size_t>(plane0 + k) * s.n_pages * page_bytes;
-            auto unit = [&](int which, int t) { return data + static_cast<size_t>(at[which][t].x) * UB; };
-            uint32_t pair = 0;
-            if (tid < n) pair = reinterpret_cast<const uint32_t*>(unit(0, tid))[D + at[0][tid].y];
-            if (k == 0) find(turn ^ 1, i0 + kBatch);
-            if (!((plane0 + k) & 1)) {
-                uint4 x[kPieces];
-#pragma unroll
-                for (int u = 0; u < kPieces; ++u) {
-                    const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
-                    if (t < n) x[u] = reinterpret_cast<const uint4*>(unit(0, t))[at[0][t].y * kPieces + part];
-                }
-                __syncthreads();                // everything of the batch has been read
-#pragma unroll
-                for (int u = 0; u < kPieces; ++u) {
-                    const int item = u * kMoveThreads + tid, t = item / kPieces, part = item % kPieces;
-                    if (t < n) reinterpret_cast<uint4*>(unit(1, t))[at[1][t].y * kPieces + part] = x[u];
-                }
-            } else {
-                Piece x[8];
-#pragma unroll
-                for (int u = 0; u < 8; ++u) {   // neighbouring lanes have neighbouring tokens: a group's words of a unit are neighbours
-                    if (tid < n) x[u] = reinterpret_cast<const Piece*>(unit(0, tid))[8 * u + at[0][tid].y];
-                }
-                __syncthreads();
-#pragma unroll
-                for (int u = 0; u < 8; ++u)
-                    if (tid < n) reinterpret_cast<Piece*>(unit(1, tid))[8 * u + at[1][tid].y] = x[u];
-            }
-            if (tid < n) reinterpret_cast<uint32_t*>(unit(1, tid))[D + at[1][tid].y] = pair;
-        }
-    }
+    load(at, one);
+    auto step = [&](Held& mine, Held& coming) {
+        At ahead = at;
+        next(ahead);
+        if (ahead.k == 0) find(ahead.turn, ahead.i0);           // (the half that the batch before this one had)
+        __syncthreads();                        // everything of this item has been read; the next places are known
+        if (ahead.i0 < end) load(ahead, coming);
+        store(at, mine);
+        at = ahead;
+        if (at.k == 0) __syncthreads();         // this batch's places have been used
+        return at.i0 < end;
+    };
+    while (step(one, two) && step(two, one)) {}
 }
 
 }  // namespace

@@ -7,6 +7,9 @@
 // the only exchange, and the 8 angles of a lane are the same for every head that it meets in a row.
 // Angles in turns: position * frequency / 2 pi in fp64, the whole turns taken off, the rest to sincospi in fp32.  (A position of a million
 // times a frequency of 1 leaves fp32 an error of 0.06 radians.)
+//
+// HBM-bound where there are many rows.  Measured (B200): 8192 rows of 40 heads of 128, 168 MB: 34 us, 4.9 TB/s (a copy of as much 25.6; more heads ahead took
+// registers and were slower, 38); a block of 9 rows 1.9 us, the launch and two loads.
 #include <cuda_bf16.h>
 
 #include "kv_pages.cuh"
@@ -27,28 +30,42 @@ struct RotateParams {
     float eps;
 };
 
-__device__ __forceinline__ void unpack(const uint4& r, float* z)
+// Pairs of fp32 numbers in one instruction.
+__device__ __forceinline__ uint64_t pair(float a, float b)
 {
-    z[0] = __uint_as_float(r.x << 16); z[1] = __uint_as_float(r.x & 0xffff0000u);
-    z[2] = __uint_as_float(r.y << 16); z[3] = __uint_as_float(r.y & 0xffff0000u);
-    z[4] = __uint_as_float(r.z << 16); z[5] = __uint_as_float(r.z & 0xffff0000u);
-    z[6] = __uint_as_float(r.w << 16); z[7] = __uint_as_float(r.w & 0xffff0000u);
+    uint64_t x;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
+    return x;
 }
-__device__ __forceinline__ uint32_t pack2(float a, float b)
+__device__ __forceinline__ void unpair(uint64_t x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
 {
-    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&x);
+    uint64_t x;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
+    return x;
 }
-__device__ __forceinline__ uint4 pack(const float* z)
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
 {
-    return make_uint4(pack2(z[0], z[1]), pack2(z[2], z[3]), pack2(z[4], z[5]), pack2(z[6], z[7]));
+    uint64_t x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
 }
+__device__ __forceinline__ uint64_t pair_of(uint32_t x) { return pair(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
+__device__ __forceinline__ void unpack(const uint4& r, uint64_t* z) { z[0] = pair_of(r.x); z[1] = pair_of(r.y); z[2] = pair_of(r.z); z[3] = pair_of(r.w); }
+__device__ __forceinline__ uint32_t pack2(uint64_t x)
+{
+    float a, b;
+    unpair(x, &a, &b);
+    const __nv_bfloat162 y = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&y);
+}
+__device__ __forceinline__ uint4 pack(const uint64_t* z) { return make_uint4(pack2(z[0]), pack2(z[1]), pack2(z[2]), pack2(z[3])); }
 
 // L lanes per head (a power of two, at least head_dim / 16).
 template <int L>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
 {
-    constexpr int kHeads = 32 / L;              // heads a warp holds at a time
+    constexpr int kHeads = 32 / L; // heads a warp holds at a time
     const int lane = threadIdx.x & 31, at = lane % L, slot = lane / L;
     const long long item = static_cast<long long>(blockIdx.x) * (kThreads / 32) + (threadIdx.x >> 5);
     const int row = static_cast<int>(item / p.parts), part = static_cast<int>(item % p.parts);
@@ -59,6 +76,20 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
     const int v0 = halves ? at : chunk, v1 = halves ? at + half : chunk + 1;
     wait_for_stream();
     if (row >= p.rows) return;                  // (whole warps)
+
+    const int heads = p.q_heads + p.kv_heads;
+    const __nv_bfloat16 *q_row = p.q + row * p.q_stride, *k_row = p.k + row * p.k_stride - p.q_heads * p.head_dim;
+    __nv_bfloat16 *q_to = p.q_out + row * p.q_out_stride, *k_to = p.k_out + row * p.k_out_stride - p.q_heads * p.head_dim;
+    auto load = [&](int h, uint4& r0, uint4& r1) {
+        r0 = r1 = make_uint4(0, 0, 0, 0);
+        if (mine && h < heads) {
+            const uint4* x = reinterpret_cast<const uint4*>((h < p.q_heads ? q_row : k_row) + h * p.head_dim);
+            r0 = x[v0];
+            r1 = x[v1];
+        }
+    };
+    uint4 n0, n1;                               // the next heads: on their way while the angles are computed
+    load(part * kHeads + slot, n0, n1);
 
     float c[8], s[8];
 #pragma unroll
@@ -80,63 +111,69 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
             if (turned) { c[i] = a; s[i] = b; }
         }
     }
-    const int heads = p.q_heads + p.kv_heads;
-    auto load = [&](int h, uint4& r0, uint4& r1) {
-        r0 = r1 = make_uint4(0, 0, 0, 0);
-        if (mine && h < heads) {
-            const bool is_q = h < p.q_heads;
-            const uint4* x = reinterpret_cast<const uint4*>((is_q ? p.q + row * p.q_stride + h * p.head_dim : p.k + row * p.k_stride + (h - p.q_heads) * p.head_dim));
-            r0 = x[v0];
-            r1 = x[v1];
-        }
-    };
-    uint4 r0, r1, n0, n1;                       // the heads at hand, the next ones
-    load(part * kHeads + slot, n0, n1);
+    uint4 weight[2][2];                         // of queries, of keys
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const uint4* from = reinterpret_cast<const uint4*>(i ? p.k_weight : p.q_weight);
+        weight[i][0] = weight[i][1] = make_uint4(0, 0, 0, 0);
+        if (from && mine) { weight[i][0] = from[v0]; weight[i][1] = from[v1]; }
+    }
+    uint64_t c2[4], s2[4], n2[4];               // of the rotation by halves: cosines, sines, sines with their sign turned
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        c2[i] = pair(c[2 * i], c[2 * i + 1]);
+        s2[i] = pair(s[2 * i], s[2 * i + 1]);
+        n2[i] = pair(-s[2 * i], -s[2 * i + 1]);
+    }
+    const float over = 1.0f / p.head_dim;
     for (int h0 = part * kHeads; h0 < heads; h0 += p.parts * kHeads) {
         const int h = h0 + slot;
         const bool live = mine && h < heads, is_q = h < p.q_heads;
-        const __nv_bfloat16* weight = is_q ? p.q_weight : p.k_weight;
-        const int head = is_q ? h : h - p.q_heads;
-        r0 = n0;
-        r1 = n1;
+        const uint4 r0 = n0, r1 = n1;
         load(h + p.parts * kHeads, n0, n1);
-        float a[8], b[8];
+        uint64_t a[4], b[4];
         unpack(r0, a);
         unpack(r1, b);
-        float sum = 0.0f;
+        if (p.q_weight || p.k_weight) {
+            uint64_t both = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(a[i], a[i], fmaf(b[i], b[i], sum));
+            for (int i = 0; i < 4; ++i) both = fma2(a[i], a[i], fma2(b[i], b[i], both));
+            float sum, odd;
+            unpair(both, &sum, &odd);
+            sum += odd;
 #pragma unroll
-        for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (!live) continue;
-        if (weight) {
-            const float norm = 1.0f / sqrtf(sum / p.head_dim + p.eps);
-            float w[8];
-            unpack(reinterpret_cast<const uint4*>(weight)[v0], w);
+            for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+            const float norm = 1.0f / sqrtf(sum * over + p.eps);
+            if (is_q ? p.q_weight : p.k_weight) {
+                uint64_t w[4];
+                const uint64_t norm2 = pair(norm, norm);
+                unpack(is_q ? weight[0][0] : weight[1][0], w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) a[i] *= norm * w[i];
-            unpack(reinterpret_cast<const uint4*>(weight)[v1], w);
+                for (int i = 0; i < 4; ++i) a[i] = mul2(a[i], mul2(norm2, w[i]));
+                unpack(is_q ? weight[0][1] : weight[1][1], w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) b[i] *= norm * w[i];
+                for (int i = 0; i < 4; ++i) b[i] = mul2(b[i], mul2(norm2, w[i]));
+            }
         }
+        if (!live) continue;
         if (halves) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float x = a[i], y = b[i];
-                a[i] = x * c[i] - y * s[i];
-                b[i] = x * s[i] + y * c[i];
+            for (int i = 0; i < 4; ++i) {
+                const uint64_t x = a[i], y = b[i];
+                a[i] = fma2(x, c2[i], mul2(y, n2[i]));
+                b[i] = fma2(x, s2[i], mul2(y, c2[i]));
             }
         } else if (turned) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float x = a[2 * i], y = a[2 * i + 1], z = b[2 * i], w = b[2 * i + 1];
-                a[2 * i] = x * c[i] - y * s[i];
-                a[2 * i + 1] = x * s[i] + y * c[i];
-                b[2 * i] = z * c[i + 4] - w * s[i + 4];
-                b[2 * i + 1] = z * s[i + 4] + w * c[i + 4];
+                float x, y, z, w;
+                unpair(a[i], &x, &y);
+                unpair(b[i], &z, &w);
+                a[i] = pair(x * c[i] - y * s[i], x * s[i] + y * c[i]);
+                b[i] = pair(z * c[i + 4] - w * s[i + 4], z * s[i + 4] + w * c[i + 4]);
             }
         }
-        uint4* y = reinterpret_cast<uint4*>((is_q ? p.q_out + row * p.q_out_stride : p.k_out + row * p.k_out_stride) + head * p.head_dim);
+        uint4* y = reinterpret_cast<uint4*>((is_q ? q_to : k_to) + h * p.head_dim);
         y[v0] = pack(a);
         y[v1] = pack(b);
     }
