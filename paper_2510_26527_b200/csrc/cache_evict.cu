@@ -2,9 +2,13 @@
 // heaviest stay, what stays moves together in every plane, pages behind it are given back.
 //
 // Two launches.  The first, one CTA per sequence, finds the weight of the last token that stays (radix selection over the weights' bits,
-// four passes of eight bits), lists the slots that stay in order, moves the weights, lists the slots that stay in order, moves the weights.  The second gives pages back and moves the contents: per sequence, head and run of planes goes through the kept tokens in order, kBatch at a time.  A token never moves up, so a batch that has been
+// four passes of eight bits), lists the slots that stay in order, moves the weights.  The second gives pages back and moves the contents: a CTA
+// per sequence, head and run of planes goes through the kept tokens in order, kBatch at a time.  A token never moves up, so a batch that has been
 // read before it is written overwrites nothing that a later batch reads.
-// Moving is HBM-bound: each token that moves is read and written once.
+//
+// Moving is HBM-bound: each token that moves is read and written once, and of a unit of values that keeps any token everything is read (four neighbours
+// share a sector).  Measured (B200): one sequence of 4300 tokens cut to 4096 in 64 planes of 8 heads of 128, 285 MB, 60.5 us, some 13 of them the first launch's
+// chain of passes; 32 sequences of up to 2048 cut to 1024 in 64 planes of 4 heads 279 us, of which the moves are 260: 1.57 GB in and out, 6.0 TB/s.
 #include <algorithm>
 #include <type_traits>
 
