@@ -50,19 +50,43 @@ __device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
     asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
     return x;
 }
-__device__ __forceinline__ uint64_t pair_of(uint32_t x) { return pair(__uint_as_float(x << 16), __uint_as_float(x & 0xffff0000u)); }
-__device__ __forceinline__ void unpack(const uint4& r, uint64_t* z) { z[0] = pair_of(r.x); z[1] = pair_of(r.y); z[2] = pair_of(r.z); z[3] = pair_of(r.w); }
-__device__ __forceinline__ uint32_t pack2(uint64_t x)
+__device__ __forceinline__ float low(uint32_t x) { return __uint_as_float(x << 16); }
+__device__ __forceinline__ float high(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
+// A lane's two vectors as the first and the second numbers of its eight pairs, two pairs to a 64-bit number: partners are the vectors themselves, or
+// neighbours in them.
+template <bool NEIGHBOURS>
+__device__ __forceinline__ void unpack(const uint4& r0, const uint4& r1, uint64_t* a, uint64_t* b)
 {
-    float a, b;
-    unpair(x, &a, &b);
-    const __nv_bfloat162 y = __floats2bfloat162_rn(a, b);
-    return *reinterpret_cast<const uint32_t*>(&y);
+    const uint32_t x[8] = {r0.x, r0.y, r0.z, r0.w, r1.x, r1.y, r1.z, r1.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = NEIGHBOURS ? pair(low(x[2 * i]), low(x[2 * i + 1])) : pair(low(x[i]), high(x[i]));
+        b[i] = NEIGHBOURS ? pair(high(x[2 * i]), high(x[2 * i + 1])) : pair(low(x[4 + i]), high(x[4 + i]));
+    }
 }
-__device__ __forceinline__ uint4 pack(const uint64_t* z) { return make_uint4(pack2(z[0]), pack2(z[1]), pack2(z[2]), pack2(z[3])); }
+__device__ __forceinline__ uint32_t pack2(float a, float b)
+{
+    const __nv_bfloat162 x = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&x);
+}
+template <bool NEIGHBOURS>
+__device__ __forceinline__ void pack(const uint64_t* a, const uint64_t* b, uint4& r0, uint4& r1)
+{
+    uint32_t x[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float a0, a1, b0, b1;
+        unpair(a[i], &a0, &a1);
+        unpair(b[i], &b0, &b1);
+        x[NEIGHBOURS ? 2 * i : i] = NEIGHBOURS ? pack2(a0, b0) : pack2(a0, a1);
+        x[NEIGHBOURS ? 2 * i + 1 : 4 + i] = NEIGHBOURS ? pack2(a1, b1) : pack2(b0, b1);
+    }
+    r0 = make_uint4(x[0], x[1], x[2], x[3]);
+    r1 = make_uint4(x[4], x[5], x[6], x[7]);
+}
 
-// L lanes per head (a power of two, at least head_dim / 16).
-template <int L>
+// L lanes per head (a power of two, at least head_dim / 16); NEIGHBOURS: neighbours are rotated together.
+template <int L, bool NEIGHBOURS>
 __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
 {
     constexpr int kHeads = 32 / L; // heads a warp holds at a time
@@ -72,7 +96,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
     const int vectors = p.head_dim / 8, half = p.rotary / 16, chunk = 2 * at;
     const bool mine = chunk < vectors;
     // the lane's two vectors: partners of a rotation by halves, else neighbours
-    const bool turned = chunk * 8 < p.rotary, halves = turned && !p.interleaved;
+    const bool turned = chunk * 8 < p.rotary, halves = turned && !NEIGHBOURS;
     const int v0 = halves ? at : chunk, v1 = halves ? at + half : chunk + 1;
     wait_for_stream();
     if (row >= p.rows) return;                  // (whole warps)
@@ -118,7 +142,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
         weight[i][0] = weight[i][1] = make_uint4(0, 0, 0, 0);
         if (from && mine) { weight[i][0] = from[v0]; weight[i][1] = from[v1]; }
     }
-    uint64_t c2[4], s2[4], n2[4];               // of the rotation by halves: cosines, sines, sines with their sign turned
+    uint64_t c2[4], s2[4], n2[4];               // cosines, sines, sines with their sign turned
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         c2[i] = pair(c[2 * i], c[2 * i + 1]);
@@ -132,8 +156,7 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
         const uint4 r0 = n0, r1 = n1;
         load(h + p.parts * kHeads, n0, n1);
         uint64_t a[4], b[4];
-        unpack(r0, a);
-        unpack(r1, b);
+        unpack<NEIGHBOURS>(r0, r1, a, b);
         if (p.q_weight || p.k_weight) {
             uint64_t both = 0;
 #pragma unroll
@@ -145,37 +168,30 @@ __global__ void __launch_bounds__(kThreads) rotate_kernel(const RotateParams p)
             for (int d = 1; d < L; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
             const float norm = 1.0f / sqrtf(sum * over + p.eps);
             if (is_q ? p.q_weight : p.k_weight) {
-                uint64_t w[4];
+                uint64_t w[4], v[4];
                 const uint64_t norm2 = pair(norm, norm);
-                unpack(is_q ? weight[0][0] : weight[1][0], w);
+                unpack<NEIGHBOURS>(is_q ? weight[0][0] : weight[1][0], is_q ? weight[0][1] : weight[1][1], w, v);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) a[i] = mul2(a[i], mul2(norm2, w[i]));
-                unpack(is_q ? weight[0][1] : weight[1][1], w);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) b[i] = mul2(b[i], mul2(norm2, w[i]));
+                for (int i = 0; i < 4; ++i) {
+                    a[i] = mul2(a[i], mul2(norm2, w[i]));
+                    b[i] = mul2(b[i], mul2(norm2, v[i]));
+                }
             }
         }
         if (!live) continue;
-        if (halves) {
+        if (turned) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const uint64_t x = a[i], y = b[i];
                 a[i] = fma2(x, c2[i], mul2(y, n2[i]));
                 b[i] = fma2(x, s2[i], mul2(y, c2[i]));
             }
-        } else if (turned) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float x, y, z, w;
-                unpair(a[i], &x, &y);
-                unpair(b[i], &z, &w);
-                a[i] = pair(x * c[i] - y * s[i], x * s[i] + y * c[i]);
-                b[i] = pair(z * c[i + 4] - w * s[i + 4], z * s[i + 4] + w * c[i + 4]);
-            }
         }
         uint4* y = reinterpret_cast<uint4*>((is_q ? q_to : k_to) + h * p.head_dim);
-        y[v0] = pack(a);
-        y[v1] = pack(b);
+        uint4 y0, y1;
+        pack<NEIGHBOURS>(a, b, y0, y1);
+        y[v0] = y0;
+        y[v1] = y1;
     }
 }
 
@@ -183,7 +199,8 @@ template <int L>
 cudaError_t launch(const RotateParams& p, cudaStream_t stream)
 {
     const long long warps = static_cast<long long>(p.rows) * p.parts;
-    return launch_early(rotate_kernel<L>, dim3(static_cast<unsigned>((warps + kThreads / 32 - 1) / (kThreads / 32))), kThreads, 0, stream, p);
+    const dim3 grid(static_cast<unsigned>((warps + kThreads / 32 - 1) / (kThreads / 32)));
+    return p.interleaved ? launch_early(rotate_kernel<L, true>, grid, kThreads, 0, stream, p) : launch_early(rotate_kernel<L, false>, grid, kThreads, 0, stream, p);
 }
 
 }  // namespace
