@@ -27,12 +27,6 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
     return x;
 }
 
-__device__ __forceinline__ float max3_abs(float a, float b, float c)
-{
-    float x;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(fabsf(b)), "f"(fabsf(c)));
-    return x;
-}
 // Pairs of fp32 numbers in one instruction.
 __device__ __forceinline__ uint64_t pair(float a, float b)
 {
@@ -51,6 +45,19 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
 {
     uint64_t x;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t x;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
+    return x;
+}
+
+__device__ __forceinline__ uint32_t min2(uint32_t a, uint32_t b)
+{
+    uint32_t x;
+    asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(a), "r"(b));
     return x;
 }
 
@@ -143,11 +150,12 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
         const bool live = at.i < rows && units[i] != 0xffffffffu;
         next(at);
         const uint32_t z[8] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w, raw[1].x, raw[1].y, raw[1].z, raw[1].w};
-        // largest element and largest of the negated ones, two bf16 per instruction, NaN sticking
+        // largest element and, negated, smallest, two bf16 per instruction, NaN sticking
         const uint32_t sign = 0x80008000u;
-        uint32_t top = z[0], bottom = z[0] ^ sign;
+        uint32_t top = z[0], bottom = z[0];
 #pragma unroll
-        for (int e = 1; e < 8; ++e) { top = max2(top, z[e]); bottom = max2(bottom, z[e] ^ sign); }
+        for (int e = 1; e < 8; ++e) { top = max2(top, z[e]); bottom = min2(bottom, z[e]); }
+        bottom ^= sign;
         uint32_t ends = max2(__byte_perm(top, bottom, 0x5410), __byte_perm(top, bottom, 0x7632));
 #pragma unroll
         for (int d = 1; d < kLanes; d <<= 1) ends = max2(ends, __shfl_xor_sync(0xffffffffu, ends, d));
@@ -160,28 +168,21 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
         float scale = up ? fmaxf(__uint_as_float(up), 1.17549435e-38f) : 1.0f;      // at least the smallest normal number
         const bool broken = !(range <= 3.4e38f);
         if (broken) scale = offset = __uint_as_float(0x7fc00000u);
-        const float inv = __fdividef(1.0f, scale), near = scale * 0.49999f;
-        // the nearest whole number to a product, by adding 1.5 * 2^23; quotients themselves are only divided out where a remainder says that one is near
-        // the middle between two
-        const float magic = 12582912.0f;
-        const uint64_t inv2 = pair(inv, inv), scale2 = pair(-scale, -scale), less = pair(-offset, -offset), more = pair(magic, magic), back = pair(-magic, -magic);
-        uint64_t a[8], t[8];
-        float rest = 0.0f;
+        // Quotients as a division rounds them, by Markstein's correction: with the reciprocal rounded to nearest, q' = a * inv, r = a - q' * scale (exact),
+        // q = q' + r * inv.  (Numbers this coarse often lie in the very middle between two codes: an approximate quotient would not do, and a look at the
+        // remainders, with a division where they are near the half, divided almost always.)  Then the nearest whole number, by adding 1.5 * 2^23.
+        const float magic = 12582912.0f, inv = __frcp_rn(scale);
+        const uint64_t inv2 = pair(inv, inv), minus = pair(-scale, -scale), less = pair(-offset, -offset), more = pair(magic, magic), back = pair(-magic, -magic);
+        uint64_t t[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            a[e] = add2(pair(__uint_as_float(z[e] << 16), __uint_as_float(z[e] & 0xffff0000u)), less);
-            t[e] = fma2(a[e], inv2, more);
-            float r0, r1;
-            unpair(fma2(add2(t[e], back), scale2, a[e]), &r0, &r1);
-            rest = max3_abs(rest, r0, r1);
+            const uint64_t a = add2(pair(__uint_as_float(z[e] << 16), __uint_as_float(z[e] & 0xffff0000u)), less), q = mul2(a, inv2);
+            t[e] = add2(fma2(fma2(q, minus, a), inv2, q), more);
         }
-        if (rest > near) {
+        if (scale < 1e-25f) {                   // remainders would leave the normal numbers
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                float a0, a1;
-                unpair(a[e], &a0, &a1);
-                t[e] = pair(__fadd_rn(__fdiv_rn(a0, scale), magic), __fadd_rn(__fdiv_rn(a1, scale), magic));
-            }
+            for (int e = 0; e < 8; ++e)
+                t[e] = pair(__fadd_rn(__fdiv_rn(__uint_as_float(z[e] << 16) - offset, scale), magic), __fadd_rn(__fdiv_rn(__uint_as_float(z[e] & 0xffff0000u) - offset, scale), magic));
         }
         if (!live) continue;
         uint32_t words[2] = {0, 0};

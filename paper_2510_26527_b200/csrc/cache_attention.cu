@@ -24,7 +24,8 @@
 // a ring of its own (bulk copies of one or two units) and keeps maximum, sums and the output tile in registers; a segment's warps meet once at its
 // end.  A segment that crosses CTAs leaves partial results, which a second kernel joins.
 //
-// Measured (B200): single tokens of 16 sequences of up to 65536 tokens, 350 MB of pages, 84 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64
+// Measured (B200): one token over 4000 11.6 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of pages,
+// 83 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64
 // sequences of up to 8192 tokens, 428 MB, 259 us: bound by issue, half of the slots, with three warps per scheduler that the output tile's registers
 // leave (the pages lying in L2 instead: 272 against 277 then).  A variant on tcgen05, tokens as the rows of a tile of 128, took 367: its sixteen
 // and more warps' waits and look-ups per step cost as many instructions as the products they save.
@@ -913,6 +914,7 @@ constexpr int kWeighWarps = 8, kWeighTokens = kWeighWarps * 16, kWeighGroups = 1
 // A CTA has 128 tokens of a sequence, a warp 16 of them: keys only, the products as in attend_kernel.  The rows of all heads come in chunks of 16
 // groups of 8 (as many heads as that holds), so that the CTA seldom has to meet; a head's keys are loaded while the one before is multiplied.
 // Sums stay in a lane's registers over all heads and rows; the lanes of one token meet at the end.  So every sum has one order.
+// Issue-bound: 25 rows x 4 key heads of 64, 33 sequences of up to 3000 tokens 20 us (64 or 96 tokens per CTA: 2 us more, rows are brought in more often; 192: the same).
 template <int D>
 __global__ void __launch_bounds__(kWeighWarps * 32) weigh_kernel(const WeighParams w)
 {

@@ -8,8 +8,8 @@
 // Angles in turns: position * frequency / 2 pi in fp64, the whole turns taken off, the rest to sincospi in fp32.  (A position of a million
 // times a frequency of 1 leaves fp32 an error of 0.06 radians.)
 //
-// HBM-bound where there are many rows.  Measured (B200): 8192 rows of 40 heads of 128, 168 MB: 34 us, 4.9 TB/s (a copy of as much 25.6; more heads ahead took
-// registers and were slower, 38); a block of 9 rows 1.9 us, the launch and two loads.
+// HBM-bound where there are many rows.  Measured (B200): 8195 rows of 40 heads of 128, 168 MB: 33.8 us, 5.0 TB/s (a copy of as much 25.6; two heads ahead
+// instead of one take registers, 38 us); a block of 9 rows 1.8 us, the launch and two loads.
 #include <cuda_bf16.h>
 
 #include "kv_pages.cuh"
@@ -17,7 +17,7 @@
 namespace polyspec {
 namespace {
 
-constexpr int kThreads = 128;
+constexpr int kThreads = 64;                    // (128: 34.3 us at the size above, 256: 40)
 
 struct RotateParams {
     const __nv_bfloat16 *q, *k, *q_weight, *k_weight;

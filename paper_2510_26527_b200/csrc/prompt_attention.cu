@@ -15,6 +15,12 @@
 //         are not finite are replaced by 0 there; if there were any, the epilogue adds them to the rows that see them
 //   4-7   softmax and epilogue of tile A, a thread per row;  8-11 the same for tile B
 // A row's maximum is only followed when it has risen by 2^8: sums and output are then rescaled, by the row's own threads.
+//
+// Measured (B200): prompts of 8192, 2500, 1111 and 389 rows, 32 heads of 128 over 8: 507 us, 1208 TFLOP/s, 0.74 of a library product's burst (575 us where a
+// long run is held at the power cap).  Bound by the softmax and the products taking turns: tensor and exponential pipes are each active 60% of the time.  Half
+// or a quarter of the exponentials as polynomials on the FMA pipe moved nothing or cost time; without the split of registers between roles scores spill
+// (3300 us); weights handed over in halves and items to and fro over the CTAs were worth 577 -> 524, what is loaded from tensor memory pinned behind its wait
+// 524 -> 507.  Prompts of a few hundred rows: 11 us, a launch with the longest item's four steps.
 #include <cuda.h>
 #include <cuda_bf16.h>
 

@@ -124,6 +124,23 @@ def test_append(lens, counts, kv, d, P):
     assert (weights.cpu().numpy() == want_w).all()
 
 
+def test_append_of_numbers_in_the_middle_between_codes_and_of_all_sizes():
+    # whole numbers times powers of two: many quotients lie in the very middle, the smallest scales are the smallest normal number
+    n, kv, d, P = 700, 3, 128, 16
+    rng = np.random.default_rng(23)
+    c = plain.Cache([n], kv, d, P, 24)
+    x = [torch.from_numpy(np.ldexp(rng.integers(-(2 ** rng.integers(1, 8, (n, kv, 1))), 2 ** rng.integers(1, 8, (n, kv, 1)) + 1, (n, kv, d)).astype(np.float32),
+                                   rng.integers(-126, 112, (n, kv, 1))).astype(np.float32)).to(torch.bfloat16) for _ in range(2)]
+    pool = c.empty_pool()
+    pages, on = c.to(DEV), c.words_on(pool, DEV)
+    st = binding.polyspec_cache_append(pages, x[0].to(DEV), x[1].to(DEV), on, _i32([0, n]), _i32([0]))
+    assert int(st) == 0
+    for p in range(2):
+        code, scale, offset, _ = plain.quantise(x[p].float().numpy())
+        c.put(pool, p, 0, range(n), code, scale, offset)
+    assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
+
+
 def test_append_takes_a_padded_batch_and_parts_of_a_projection():
     """n_rows below the rows given; base in two parts; rows before the first and behind the last sequence; strided rows."""
     lens, counts, kv, d, P = [30, 8, 21], [5, 5, 5], 2, 128, 16
