@@ -6,9 +6,8 @@
 // head_dim / 16 lanes: what is computed once per head and lane (ends, scale, addresses) costs as much as the codes themselves, so half as many lanes are
 // faster (54 -> 47 us at the size below).  Rounding the scale up keeps every code at 15 or below, so nothing is cut off.
 //
-// Measured (B200): 17600 rows of 8 heads of 128, 72 MB in and as much of held values out, 19 MB of codes: 43 us, 3.7 TB/s, by issue (72% of the slots) more than
-// by memory (25 us); four rows per CTA of 128 threads (eight of 256 threads 47, four of 64 threads 44).  A block of 420 rows 5.0 us: the chain of loads that finds
-// a row's place.
+// Measured (B200): 17500 rows of 8 heads of 128, 72 MB in and as much of held values out, 19 MB of codes: 36 us, 4.5 TB/s (a copy of as much 25); four rows per CTA
+// of 128 threads (two or eight rows 38, eight of 256 threads 39, four of 64 threads 37).  A block of 420 rows 4.4 us: the chain of loads that finds a row's place.
 #include <cuda_bf16.h>
 
 #include "kv_pages.cuh"
