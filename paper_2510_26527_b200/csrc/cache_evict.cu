@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec
     constexpr int kPieces = D / 32;             // 16-byte pieces of a token's codes
     constexpr int UB = kv::unit_bytes(D);
     using Piece = typename std::conditional<D == 128, uint2, uint32_t>::type;         // the D / 64 words of one group of lanes
-    __shared__ uint2 places[2][2][kBatch];      // [turn][from, to]: unit of the plane, token of the unit
+    __shared__ uint2 places[3][2][kBatch];      // [turn][from, to]: unit of the plane, token of the unit; of three batches in a row
     const int b = blockIdx.y, head = blockIdx.x % kv_heads, plane0 = blockIdx.x / kv_heads * run, planes = min(run, n_planes - plane0), tid = threadIdx.x;
     const int P = s.page_tokens, units = P / kv::kUnit;
     const size_t cap = static_cast<size_t>(s.max_pages) * P;
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec
         return make_uint2((static_cast<uint32_t>(pages[at]) * kv_heads + head) * units + (unit - at * units), slot % kv::kUnit);
     };
     auto find = [&](int turn, int i) {
-        if (i + tid < end) {
+        if (i < end - tid) {
             places[turn][0][tid] = place(from[i + tid]);
             places[turn][1][tid] = place(i + tid);
         }
@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec
     // An item is a batch of one plane.  The next one's loads are under way while this one's are waited for and stored: what they read lies behind what
     // this one writes, or in another plane.
     struct Held { uint4 codes[kPieces]; uint32_t pair; };       // keys: pieces of tokens; values: a token's words, in the order of their groups
-    struct At { int i0, k, turn; };                             // batch, plane of the run, which half of `places`
+    struct At { int i0, k, turn; };                             // batch, plane of the run, which third of `places`
     auto unit = [&](const At& at, int which, int t) {
         return pool + (static_cast<size_t>(plane0 + at.k) * s.n_pages * page_bytes + static_cast<size_t>(places[at.turn][which][t].x) * UB);
     };
@@ -267,7 +267,7 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec
         if (++at.k < planes) return;
         at.k = 0;
         at.i0 += kBatch;
-        at.turn ^= 1;
+        at.turn = at.turn == 2 ? 0 : at.turn + 1;
     };
     auto load = [&](const At& at, Held& x) {
         const int n = min(kBatch, end - at.i0);
@@ -306,15 +306,16 @@ __global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const polyspec
     find(0, begin);
     __syncthreads();
     load(at, one);
+    find(1, begin + kBatch);
     auto step = [&](Held& mine, Held& coming) {
         At ahead = at;
         next(ahead);
-        if (ahead.k == 0) find(ahead.turn, ahead.i0);           // (the half that the batch before this one had)
-        __syncthreads();                        // everything of this item has been read; the next places are known
+        __syncthreads();                        // everything of this item has been read; the next batch's places are known
         if (ahead.i0 < end) load(ahead, coming);
+        // the places of the batch after that, by the time of the loads: they take the third of the batch before this one, which all threads have stored
+        if (ahead.k == 0) find(ahead.turn == 2 ? 0 : ahead.turn + 1, ahead.i0 + kBatch);
         store(at, mine);
         at = ahead;
-        if (at.k == 0) __syncthreads();         // this batch's places have been used
         return at.i0 < end;
     };
     while (step(one, two) && step(two, one)) {}
