@@ -24,11 +24,10 @@
 // a ring of its own (bulk copies of one or two units) and keeps maximum, sums and the output tile in registers; a segment's warps meet once at its
 // end.  A segment that crosses CTAs leaves partial results, which a second kernel joins.
 //
-// Measured (B200): one token over 4000 11.6 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of pages,
-// 83 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64
-// sequences of up to 8192 tokens, 428 MB, 259 us: bound by issue, half of the slots, with three warps per scheduler that the output tile's registers
-// leave (the pages lying in L2 instead: 272 against 277 then).  A variant on tcgen05, tokens as the rows of a tile of 128, took 367: its sixteen
-// and more warps' waits and look-ups per step cost as many instructions as the products they save.
+// Measured (B200): one token over 4000 11.6 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
+// pages, 83 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64 sequences of up to 8192 tokens, 428 MB, 259 us: bound by issue, half of the slots, with
+// three warps per scheduler that the output tile's registers leave (with the pages in L2 hardly less: 272 against 277 of an earlier form).  A variant on tcgen05, tokens
+// as the rows of a tile of 128, took 367: its sixteen and more warps' waits and look-ups per step cost as many instructions as the products they save.
 #include <cuda_fp16.h>
 
 #include "kv_pages.cuh"
@@ -1046,7 +1045,6 @@ polyspec_status fill(AttendParams* p, const polyspec_cache_pages* s, const polys
     if (!kv::rows_ok(q, q_stride, q_heads, head_dim) || !pool || !kv::aligned16(pool) || !aligned4(device_status)) return POLYSPEC_ERR_INVALID_ARG;
     if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return POLYSPEC_ERR_INVALID_ARG;
     const size_t bytes = kv::page_bytes(*s, kv_heads, head_dim);
-    if (s->n_seqs > (1 << 24)) return POLYSPEC_ERR_UNSUPPORTED;
     if (s->n_pages * (bytes / kv::unit_bytes(head_dim)) >= 0xffffffffull) return POLYSPEC_ERR_UNSUPPORTED;      // units of a plane are counted in 32 bits
     p->s = *s;
     p->r = *r;
