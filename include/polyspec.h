@@ -573,8 +573,9 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  * polyspec_cache_attention -- the rows of a block over the cache, each row over the slots up to its own:
  *     out[i, h] = sum_{j <= slot(i)} softmax_j(scale * q[i, h] . K[j, h / (q_heads/kv_heads)]) V[j, .]
  *   head_dim 64 or 128, any number of rows; out, lse as in polyspec_prompt_attention; a row that attends to nothing gets zeros and -inf.  Codes are
- *   multiplied as whole numbers, scales and offsets applied to fp32 sums; softmax weights are rounded to fp16 for their product
- *   with the codes.  The order of the sums depends on the lengths and on the batch.
+ *   multiplied as whole numbers, scales and offsets applied to fp32 sums.  Weights times the values' scales are rounded to fp16 for their product with the
+ *   codes: each is off by 2^-11 of itself at most, or by 2^-28 of its row's largest.  lse, and with it the weights of polyspec_cache_weigh, depends on keys alone.
+ *   Values are at most some 2^96 in size: sums over the tokens stay within fp32.  The order of the sums depends on the lengths and on the batch.
  *   Workspace of polyspec_cache_attention_workspace bytes.
  *   POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.
  *

@@ -4,9 +4,9 @@
 //
 // The matrix instructions multiply codes, never dequantised numbers:
 //   s[r, j] = ks[j] * (q[r] . ck[j]) + ko[j] * sum(q[r])                        one product and one FMA per (row, token)
-//   out[r]  = (sum_j p'[r, j] cv[j] + sum_j p[r, j] vo[j]) / sum_j p[r, j],     p' = p * vs[j]
-// p' comes out of the exponential itself: 2^(s + log2 vs[j] - m), with m the running maximum of s + log2 vs, so that it is at its most
-// accurate where it counts; p = p' / vs[j].
+//   out[r]  = (sum_j (p[r, j] vs[j]) cv[j] + sum_j p[r, j] vo[j]) / sum_j p[r, j],     p = 2^(s - m)
+// with m near the running maximum of s.  p and both sums of p are fp32; only the products p vs are rounded, to fp16, times a power of two that
+// keeps a row's largest at 2^3 or more: what it loses of the others is small beside the largest, whatever their scales.
 //
 // A code is an fp16 number without any arithmetic: four bits under a mask are a subnormal, code * 2^-24, and the same mask four
 // bits higher gives 16 * code * 2^-24.  Matrix instructions multiply subnormals exactly; the 16 goes into the query's elements
@@ -24,8 +24,8 @@
 // a ring of its own (bulk copies of one or two units) and keeps maximum, sums and the output tile in registers; a segment's warps meet once at its
 // end.  A segment that crosses CTAs leaves partial results, which a second kernel joins.
 //
-// Measured (B200): one token over 4000 11.6 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
-// pages, 83 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64 sequences of up to 8192 tokens, 428 MB, 259 us: bound by issue, half of the slots, with
+// Measured (B200): one token over 4000 12.0 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
+// pages, 84 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64 sequences of up to 8192 tokens, 428 MB, 258 us: bound by issue, half of the slots, with
 // three warps per scheduler that the output tile's registers leave (with the pages in L2 hardly less: 272 against 277 of an earlier form).  A variant on tcgen05, tokens
 // as the rows of a tile of 128, took 367: its sixteen and more warps' waits and look-ups per step cost as many instructions as the products they save.
 #include <cuda_fp16.h>
@@ -44,8 +44,10 @@ using tensordev::smem_addr;
 constexpr int kMaxCtas = 608;                   // CTAs that the workspace has room for
 constexpr int kOverhead = 4;                    // steps' worth of work that a segment costs besides its steps: its rows, the meeting of its warps
 constexpr float kNone = -3.0e38f;               // a maximum over nothing
-constexpr float kLift = 3.0f;                   // p' is 2^3 at the maximum that the reference was taken from
+constexpr float kLift = 3.0f;                   // a row's largest product of weight and scale is 2^3 when its reference is set
 constexpr float kSlack = 12.0f;                 // and may rise to 2^15, near fp16's end, before sums are rescaled
+constexpr float kTame = 40.0f;                  // scales from 2^-40 to 2^40 need no units: a weight that is lost below 2^-126 is 2^-49 of the largest at most
+constexpr float kMostUnit = 126.0f;             // units are 2^-126 to 2^126
 
 struct AttendParams {
     polyspec_cache_pages s;
@@ -75,12 +77,6 @@ __device__ __forceinline__ float lg2(float x)
 {
     float y;
     asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float rcp(float x)
-{
-    float y;
-    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t half2_bits(float a, float b)
@@ -348,10 +344,129 @@ __device__ __forceinline__ void store_out(const AttendParams& p, const kv::SeqRo
     if (d0 == 0 && p.lse) p.lse[at] = none ? -INFINITY : (m + log2f(l)) * 0.69314718055994530942f;
 }
 
-// What a warp keeps of its tile: output (elements x rows, in the codes' form), per row the reference of the exponentials (a maximum less kLift), the sums of
-// p and of p vo.  NT groups of 8 rows; a lane has rows 2 t4 and 2 t4 + 1 of each.
+// What a warp keeps of its tile.  Per row: the reference of the weights p = 2^(score - reference), with its sign turned; their sum l and the sum lo of p vo; and the
+// output, elements x rows in the codes' form, the sum of p vs unit cv.  A power of two, `unit`, is 1 as long as one reference serves both: then it brings p vs into
+// fp16's range, and p is within 2^60 of 1.  Where scales are too far from 1 for that the reference follows the weights alone, and the unit the products.
+// NT groups of 8 rows; a lane has rows 2 t4 and 2 t4 + 1 of each, as pairs.
 template <class S>
-struct Running { float o[S::NT][S::M][4]; uint64_t ref[S::NT], l[S::NT], lo[S::NT]; bool started; };         // (pairs of rows; ref with its sign turned)
+struct Running { float o[S::NT][S::M][4]; uint64_t ref[S::NT], unit[S::NT], l[S::NT], lo[S::NT]; bool started, units; };
+
+__device__ __forceinline__ float exponent(float x) { return static_cast<float>(static_cast<int>(__float_as_uint(x) >> 23 & 255u) - 127); }
+
+// The largest of a row's numbers, over its tokens.
+template <int T>
+__device__ __forceinline__ float row_max(const float (&y)[T][2], float top)
+{
+#pragma unroll
+    for (int v = 0; v < T; ++v) top = max3(top, y[v][0], y[v][1]);
+#pragma unroll
+    for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    return top;
+}
+
+// Rows' references rise by `up`: exponents, sums and output follow, the output by a factor of its own.
+template <class S, int T>
+__device__ __forceinline__ void follow(Running<S>& run, uint64_t (&x)[T][S::NT][2], int n, const float (&up)[2], const float (&by)[2], const float (&by_o)[2])
+{
+    const uint64_t less = pair(-up[0], -up[1]), by2 = pair(by[0], by[1]);
+#pragma unroll
+    for (int v = 0; v < T; ++v) { x[v][n][0] = add2(x[v][n][0], less); x[v][n][1] = add2(x[v][n][1], less); }
+    run.ref[n] = add2(run.ref[n], less);
+    run.l[n] = mul2(run.l[n], by2);
+    run.lo[n] = mul2(run.lo[n], by2);
+#pragma unroll
+    for (int i = 0; i < S::M; ++i) { run.o[n][i][0] *= by_o[0]; run.o[n][i][1] *= by_o[1]; run.o[n][i][2] *= by_o[0]; run.o[n][i][3] *= by_o[1]; }
+}
+
+// References and units that fit the tokens at hand: x, exponents of their weights, less the old references (-inf: not seen), and vs, the values' scales.
+// (A row that sees none of its warp's first tokens sees none of the later ones either.)
+template <class S, int T>
+__device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T][S::NT][2], const float (&vs)[T][2])
+{
+    const bool first = !run.started;
+    float lv[T][2];
+    bool tame = !run.units;
+#pragma unroll
+    for (int v = 0; v < T; ++v)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float most = -INFINITY;
+#pragma unroll
+            for (int n = 0; n < S::NT; ++n) {
+                float a, b;
+                unpair(x[v][n][u], &a, &b);
+                most = max3(most, a, b);
+            }
+            lv[v][u] = lg2(vs[v][u]);
+            tame = tame && (most == -INFINITY || !(fabsf(lv[v][u]) > kTame));
+        }
+    run.started = true;
+    if (__builtin_expect(__all_sync(0xffffffffu, tame), 1)) {
+#pragma unroll
+        for (int n = 0; n < S::NT; ++n) {
+            float up[2], by[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float y[T][2];
+#pragma unroll
+                for (int v = 0; v < T; ++v)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        float a, b;
+                        unpair(x[v][n][u], &a, &b);
+                        y[v][u] = (j ? b : a) == -INFINITY ? -INFINITY : (j ? b : a) + lv[v][u];
+                    }
+                const float top = row_max(y, -INFINITY);            // the largest product is 2^top
+                up[j] = top == -INFINITY ? 0.0f : first ? top - kLift : fmaxf(top - kLift, 0.0f);
+                by[j] = first ? 1.0f : ex2(-up[j]);
+            }
+            run.unit[n] = pair(1.0f, 1.0f);
+            follow<S, T>(run, x, n, up, by, by);
+        }
+        return;
+    }
+    bool units = false;
+#pragma unroll
+    for (int n = 0; n < S::NT; ++n) {
+        float up[2], by[2], by_o[2], unit[2], l[2];
+        unpair(run.unit[n], &unit[0], &unit[1]);
+        unpair(run.l[n], &l[0], &l[1]);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            // The row's largest weight, of these tokens or (by their sum) of those before, is 2^top; these tokens' largest product 2^h of that, in the output's
+            // unit 2^(top + h + e).
+            float y[T][2], w[T][2];
+#pragma unroll
+            for (int v = 0; v < T; ++v)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    float a, b;
+                    unpair(x[v][n][u], &a, &b);
+                    y[v][u] = j ? b : a;
+                }
+            float top = row_max(y, l[j] > 0.0f ? log2f(l[j]) : -INFINITY);
+            top = top == -INFINITY ? 0.0f : ceilf(top);
+#pragma unroll
+            for (int v = 0; v < T; ++v)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) w[v][u] = ex2(y[v][u] - top) * vs[v][u];
+            const float heavy = row_max(w, 0.0f), h = exponent(heavy), e = first ? 0.0f : exponent(unit[j]);
+            const bool none = first && heavy == 0.0f, anew = !none && (first || top + h + e > kLift + 5.0f);
+            // with a unit of 1 the largest weight would be 2^most; else it becomes 2^-5
+            const float most = anew ? kLift - h : top + e, fall = anew ? top + h + e - kLift : 0.0f;
+            const bool one = none || fabsf(most) <= kTame;
+            const float wanted = one ? 0.0f : most + 5.0f, to = fminf(fmaxf(wanted, -kMostUnit), kMostUnit);
+            up[j] = one && !none ? top - most : top + 5.0f;
+            unit[j] = __uint_as_float(static_cast<uint32_t>(static_cast<int>(to) + 127) << 23);
+            by[j] = first ? 1.0f : ex2(-up[j]);
+            by_o[j] = first ? 1.0f : ex2(to - wanted - fall);
+            units = units || !one;
+        }
+        run.unit[n] = pair(unit[0], unit[1]);
+        follow<S, T>(run, x, n, up, by, by_o);
+    }
+    run.units = __any_sync(0xffffffffu, units);
+}
 
 // A stage's 32 tokens, 16 at a time side by side (two chains of products hide each other's latency: 276 -> 259 us on blocks of 4 to 9 rows).  `at`: the stage,
 // 4 units of keys, 4 of values.  masked: some row does not see some token, or a unit could not be read (bad).  q0: the rows' fragments where they stay in
@@ -391,31 +506,31 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
             }
         }
     }
-    // scales and offsets of the lane's tokens g8 and g8 + 8; exponents, less the references, rows in pairs
+    // scales and offsets of the lane's tokens g8 and g8 + 8; exponents of their weights, less the references, rows in pairs
     uint64_t x[T][L][2];
-    float iv[T][2], ov[T][2], most = -INFINITY;
+    float vs[T][2], vo[T][2], most = -INFINITY, scale = 0x1p-45f;       // (a scale that keeps weights below 2^60 where it bounds the products)
 #pragma unroll
     for (int v = 0; v < T; ++v) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const unsigned char* pairs = at + (2 * v + u) * UB + 4 * D + g8 * 4;
             const uint32_t kp = *reinterpret_cast<const uint32_t*>(pairs), vp = *reinterpret_cast<const uint32_t*>(pairs + 4 * UB);
-            const float ks = low(kp) * factor, ko = high(kp), vs = low(vp), lv = lg2(vs);
-            iv[v][u] = rcp(vs);
-            ov[v][u] = high(vp) * iv[v][u];
-            const uint64_t ks2 = pair(ks, ks), ko2 = pair(ko, ko), lv2 = pair(lv, lv);
+            const float ks = low(kp) * factor, ko = high(kp);
+            vs[v][u] = low(vp);
+            vo[v][u] = high(vp);
+            const uint64_t ks2 = pair(ks, ks), ko2 = pair(ko, ko);
 #pragma unroll
             for (int n = 0; n < L; ++n) {
                 const uint64_t sq = *reinterpret_cast<const uint64_t*>(&sums[n * 8 + 2 * t4]);
-                x[v][n][u] = fma2(pair(sc[v][n][2 * u], sc[v][n][2 * u + 1]), ks2, fma2(sq, ko2, add2(lv2, run.ref[n])));
+                x[v][n][u] = fma2(pair(sc[v][n][2 * u], sc[v][n][2 * u + 1]), ks2, fma2(sq, ko2, run.ref[n]));
             }
         }
+        scale = max3(scale, vs[v][0], vs[v][1]);
     }
-    uint32_t hidden[T];                         // bit 4 n + 2 u + j
+    uint32_t hidden[T] = {};                    // bit 4 n + 2 u + j
     if (__builtin_expect(masked, 0)) {
 #pragma unroll
         for (int v = 0; v < T; ++v) {
-            hidden[v] = 0;
 #pragma unroll
             for (int n = 0; n < L; ++n) {
                 const int r = seg.tile * seg.tile_rows + n * 8 + 2 * t4, limit0 = row_limit(seg.q, r / p.group), limit1 = row_limit(seg.q, (r + 1) / p.group);
@@ -441,76 +556,42 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
                 unpair(x[v][n][u], &a, &b);
                 most = max3(most, a, b);
             }
-    // the first tokens set the references; after that sums are rescaled only when a maximum has risen by 2^kSlack since the last time
-    if (__builtin_expect(__any_sync(0xffffffffu, !run.started || most > kLift + kSlack), 0)) {
-        const bool first = !run.started;
-#pragma unroll
-        for (int n = 0; n < L; ++n) {
-            float up[2], by[2];
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                float top = -INFINITY;
-#pragma unroll
-                for (int v = 0; v < T; ++v)
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        float a, b;
-                        unpair(x[v][n][u], &a, &b);
-                        top = fmaxf(top, j ? b : a);
-                    }
-#pragma unroll
-                for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-                // (a row that sees none of its warp's first tokens sees none of the later ones either)
-                up[j] = first ? (top == -INFINITY ? 0.0f : top - kLift) : fmaxf(top - kLift, 0.0f);
-                by[j] = first ? 1.0f : ex2(-up[j]);
-            }
-            const uint64_t less = pair(-up[0], -up[1]), by2 = pair(by[0], by[1]);
-#pragma unroll
-            for (int v = 0; v < T; ++v) { x[v][n][0] = add2(x[v][n][0], less); x[v][n][1] = add2(x[v][n][1], less); }
-            run.ref[n] = add2(run.ref[n], less);
-            run.l[n] = mul2(run.l[n], by2);
-            run.lo[n] = mul2(run.lo[n], by2);
-#pragma unroll
-            for (int i = 0; i < M; ++i) { run.o[n][i][0] *= by[0]; run.o[n][i][1] *= by[1]; run.o[n][i][2] *= by[0]; run.o[n][i][3] *= by[1]; }
-        }
-        run.started = true;
-    }
+    // The first tokens set the references; after that sums are rescaled only when a product may have risen by 2^kSlack since the last time, by a bound of the largest
+    // weight and the largest scale of a lane's tokens.  With units every stage is looked at exactly.
+    if (__builtin_expect(__any_sync(0xffffffffu, !run.started || run.units || most + lg2(scale) > kLift + kSlack), 0)) set_references<S, T>(run, x, vs);
     uint32_t pr[T][L][2];
-#pragma unroll
-    for (int v = 0; v < T; ++v)
-#pragma unroll
-        for (int n = 0; n < L; ++n)
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                float a, b;
-                unpair(x[v][n][u], &a, &b);
-                a = ex2(a);
-                b = ex2(b);
-                pr[v][n][u] = transpose(half2_bits(a, b));
-                x[v][n][u] = pair(a, b);
-            }
-    if (__builtin_expect(!masked, 1)) {
+    if (__builtin_expect(!masked && !run.units, 1)) {
 #pragma unroll
         for (int v = 0; v < T; ++v)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint64_t iv2 = pair(iv[v][u], iv[v][u]), ov2 = pair(ov[v][u], ov[v][u]);
+                const uint64_t vs2 = pair(vs[v][u], vs[v][u]), vo2 = pair(vo[v][u], vo[v][u]);
 #pragma unroll
                 for (int n = 0; n < L; ++n) {
-                    run.l[n] = fma2(x[v][n][u], iv2, run.l[n]);
-                    run.lo[n] = fma2(x[v][n][u], ov2, run.lo[n]);
+                    float a, b;
+                    unpair(x[v][n][u], &a, &b);
+                    const uint64_t weight = pair(ex2(a), ex2(b));
+                    run.l[n] = add2(run.l[n], weight);
+                    run.lo[n] = fma2(weight, vo2, run.lo[n]);
+                    unpair(mul2(weight, vs2), &a, &b);
+                    pr[v][n][u] = transpose(half2_bits(a, b));
                 }
             }
-    } else {                                    // scales behind what a row sees may be anything
+    } else {                                    // scales and offsets behind what a row sees may be anything
 #pragma unroll
         for (int v = 0; v < T; ++v)
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int n = 0; n < L; ++n) {
-                    const bool s0 = !(hidden[v] >> (4 * n + 2 * u) & 1u), s1 = !(hidden[v] >> (4 * n + 2 * u) & 2u);
-                    run.l[n] = fma2(x[v][n][u], pair(s0 ? iv[v][u] : 0.0f, s1 ? iv[v][u] : 0.0f), run.l[n]);
-                    run.lo[n] = fma2(x[v][n][u], pair(s0 ? ov[v][u] : 0.0f, s1 ? ov[v][u] : 0.0f), run.lo[n]);
+                    const bool h0 = hidden[v] >> (4 * n + 2 * u) & 1u, h1 = hidden[v] >> (4 * n + 2 * u) & 2u;
+                    float a, b;
+                    unpair(x[v][n][u], &a, &b);
+                    const uint64_t weight = pair(ex2(a), ex2(b));
+                    run.l[n] = add2(run.l[n], weight);
+                    run.lo[n] = fma2(weight, pair(h0 ? 0.0f : vo[v][u], h1 ? 0.0f : vo[v][u]), run.lo[n]);
+                    unpair(mul2(mul2(weight, pair(h0 ? 0.0f : vs[v][u], h1 ? 0.0f : vs[v][u])), run.unit[n]), &a, &b);
+                    pr[v][n][u] = transpose(half2_bits(a, b));
                 }
     }
     // codes of values: words of tokens 2 t4 and 2 t4 + 1, paired by token, and the second product: elements x rows
@@ -664,11 +745,11 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
             }
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
-                run.ref[n] = run.l[n] = run.lo[n] = 0;
+                run.ref[n] = run.unit[n] = run.l[n] = run.lo[n] = 0;
 #pragma unroll
                 for (int i = 0; i < M; ++i) run.o[n][i][0] = run.o[n][i][1] = run.o[n][i][2] = run.o[n][i][3] = 0.0f;
             }
-            run.started = false;
+            run.started = run.units = false;
             fresh = false;
         }
         if (ok) {                               // a bounded wait, passed or given up by the whole warp
@@ -713,7 +794,9 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
         }
         __syncthreads();
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n) {
+            float unit[2];
+            unpair(run.unit[n], &unit[0], &unit[1]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
                 const int r = n * 8 + 2 * t4 + j;
@@ -722,9 +805,16 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
                 for (int w = 0; w < W; ++w) top = fmaxf(top, sm_m[w][r]);
                 const float by = ex2(ref[n][j] - top);
                 if (g8 == 0) { sm_l[warp][r] = l[n][j] * by; sm_o[warp][r] = lo[n][j] * by; }
+                // out of the unit, and with what the codes' form left out: 2^24, for 16-fold codes 2^20
+                const float inverse = __uint_as_float(0x7f000000u - __float_as_uint(unit[j])), even = by * 16777216.0f, odd = by * 1048576.0f;
 #pragma unroll
-                for (int i = 0; i < M; ++i) { run.o[n][i][j] *= by; run.o[n][i][2 + j] *= by; }
+                for (int i = 0; i < M; ++i) {
+                    const float whole = i & 2 ? odd : even;
+                    run.o[n][i][j] = run.o[n][i][j] * whole * inverse;
+                    run.o[n][i][2 + j] = run.o[n][i][2 + j] * whole * inverse;
+                }
             }
+        }
         if (warp >= W / 2) {
 #pragma unroll
             for (int n = 0; n < NT; ++n)
@@ -756,9 +846,8 @@ __global__ void __launch_bounds__(S::THREADS, S::CTAS) attend_kernel(const Atten
                     const float4 y = merge[((w * NT + n) * M + i) * 32 + ln];
                     sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
                 }
-                const float by = i & 2 ? 1048576.0f : 16777216.0f;      // 2^20, 2^24: what the codes' form left out
                 const int h1 = H - 1, e1 = D == 128 ? i : i + 4;
-                x[0][0][i] = sum.x * by; x[1][0][i] = sum.y * by; x[0][h1][e1] = sum.z * by; x[1][h1][e1] = sum.w * by;
+                x[0][0][i] = sum.x; x[1][0][i] = sum.y; x[0][h1][e1] = sum.z; x[1][h1][e1] = sum.w;
             }
 #pragma unroll
             for (int j = 0; j < 2; ++j) {

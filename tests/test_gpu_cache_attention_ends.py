@@ -1,0 +1,110 @@
+"""Calls on 4-bit caches at the ends of what they take: scales of values far apart, heads of equal elements, rows that attend to nothing, ranges at the
+end of fp32, tables of many tokens, shared pages, several calls at once.  Against 64-bit arithmetic."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2510_26527_b200 import binding, buildlib
+from tests import plain_attention as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BAD = binding.ERR_BAD_INPUT_ON_DEVICE
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    buildlib.build()
+    binding.load_library()
+    assert torch.cuda.is_available()
+
+
+def _i32(x):
+    return torch.tensor(list(x), dtype=torch.int32, device=DEV)
+
+
+def _normal(seed, *shape):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16)
+
+
+def _close(got, want, tol):
+    got = got.detach().cpu().double().numpy()
+    same = (got == want) | (np.isnan(got) & np.isnan(want))
+    with np.errstate(invalid="ignore"):
+        off = np.abs(got - want) - tol
+    assert (same | (off <= 0)).all(), (float(np.nanmax(np.where(same, -1, off))), np.argwhere(~same & ~(off <= 0))[:4])
+
+
+def _starts(counts):
+    return np.concatenate([[0], np.cumsum(counts)]).astype(int).tolist()
+
+
+# ------------------------------------------------------------------ attention: scales of values
+def _finest(c, q, at, base):
+    """What the second product's weights, fp16 numbers of an absolute half step of 2^-25, may add to each output: 15 times that per token, where the
+    largest weight times scale of a token with a code above 0 is held as 2^3 at least, or, where scales are too small for that, 1 as 2^121."""
+    rows, heads, d = q.shape
+    add = np.zeros((rows, heads, 1))
+    for b in range(len(c.lens)):
+        for row in range(at[b], at[b + 1]):
+            m = base[b] + row - at[b] + 1
+            for h in range(heads):
+                g = h // (heads // c.kv)
+                s = d ** -0.5 * (c.value(0, b)[:m, g] @ q[row, h].astype(np.float64))
+                p = np.exp(s - s.max())
+                p /= p.sum()
+                real = c.codes[1][b][:m, g].any(-1)
+                add[row, h] = m * (15 * 2.0 ** -28 * max([0.0, *(p * c.scale[1][b][:m, g])[real]]) + 2.0 ** -142)
+    return add
+
+
+SHAPES = [([1], 4, 4), ([1, 1], 16, 2), ([9], 8, 2), ([5, 3], 12, 3)]         # rows of a block, query heads, key heads: one group of 8 rows, or more
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("counts,heads,kv", SHAPES)
+@pytest.mark.parametrize("lo,hi", [(-126, 96), (-126, -118), (-70, -50), (80, 96)])
+def test_softmax_does_not_depend_on_the_scales_of_values(d, counts, heads, kv, lo, hi):
+    lens = [150 + 40 * b for b in range(len(counts))]
+    c = plain.Cache(lens, kv, d, 16, 400)
+    for b, n in enumerate(lens):
+        c.scale[1][b] = plain.bf16(np.exp2(c.rng.uniform(lo, hi, (n, kv))))
+        c.offset[1][b] = plain.bf16(c.scale[1][b] * (-7.5 + c.rng.standard_normal((n, kv))))
+    at, base = _starts(counts), [n - k for n, k in zip(lens, counts)]
+    q = _normal(401, at[-1], heads, d)
+    pages, on = c.to(DEV), c.words_on(c.pool(), DEV)
+    lse = torch.zeros((at[-1], heads), device=DEV)
+    out, _, st = binding.polyspec_cache_attention(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse=lse)
+    assert int(st) == 0
+    qn = q.float().numpy()
+    want, want_lse, tol, tol_lse, weights, tol_w = plain.attend(c, qn, at, base)
+    _close(lse, want_lse, tol_lse)
+    _close(out, want, tol + _finest(c, qn, at, base))
+    w = torch.zeros((len(lens), c.cap), device=DEV)
+    binding.polyspec_cache_weigh(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse, w)
+    for b, n in enumerate(lens):
+        _close(w[b, :n], weights[b], tol_w[b] + 4 * plain.U32 * (1 + weights[b]))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("tiny", [-126, -100, -60])
+@pytest.mark.parametrize("kind", ["equal scores", "offsets"])
+def test_tokens_of_tiny_scales_keep_their_weight(d, tiny, kind):
+    """Two tokens of equal scores, one with a tiny scale beside an ordinary one; or many with a tiny scale and an offset of any size."""
+    n = 2 if kind == "equal scores" else 90
+    c = plain.Cache([n], 2, d, 8, 410)
+    c.scale[1][0][:1 if n == 2 else n] = 2.0 ** tiny
+    c.offset[1][0][:] = plain.bf16(np.exp2(c.rng.uniform(-10, 60, (n, 2))) * c.rng.choice([-1, 1], (n, 2)))
+    if n == 2:
+        c.scale[1][0][1] = 16.0
+        c.offset[1][0][:] = 0.0
+        for x in (c.codes[0][0], c.scale[0][0], c.offset[0][0]):
+            x[1] = x[0]
+    q = _normal(411, 1, 4, d)
+    lse = torch.zeros((1, 4), device=DEV)
+    out, _, st = binding.polyspec_cache_attention(c.to(DEV), q.to(DEV), c.words_on(c.pool(), DEV), 2, _i32([0, 1]), _i32([n - 1]), lse=lse)
+    assert int(st) == 0
+    qn = q.float().numpy()
+    want, want_lse, tol, tol_lse, _, _ = plain.attend(c, qn, [0, 1], [n - 1])
+    _close(lse, want_lse, tol_lse)
+    _close(out, want, tol + _finest(c, qn, [0, 1], [n - 1]))
