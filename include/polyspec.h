@@ -574,7 +574,8 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *     out[i, h] = sum_{j <= slot(i)} softmax_j(scale * q[i, h] . K[j, h / (q_heads/kv_heads)]) V[j, .]
  *   head_dim 64 or 128, any number of rows; out, lse as in polyspec_prompt_attention; a row that attends to nothing gets zeros and -inf.  Codes are
  *   multiplied as whole numbers, scales and offsets applied to fp32 sums.  Weights times the values' scales are rounded to fp16 for their product with the
- *   codes: each is off by 2^-11 of itself at most, or by 2^-28 of its row's largest.  lse, and with it the weights of polyspec_cache_weigh, depends on keys alone.
+ *   codes: each is off by 2^-11 of itself at most, or by 2^-28 of its row's largest (heads of
+ *   equal elements, all codes 0, aside).  lse, and with it the weights of polyspec_cache_weigh, depends on keys alone.
  *   Values are at most some 2^96 in size: sums over the tokens stay within fp32.  The order of the sums depends on the lengths and on the batch.
  *   Workspace of polyspec_cache_attention_workspace bytes.
  *   POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.

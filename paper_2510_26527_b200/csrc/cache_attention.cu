@@ -24,8 +24,8 @@
 // a ring of its own (bulk copies of one or two units) and keeps maximum, sums and the output tile in registers; a segment's warps meet once at its
 // end.  A segment that crosses CTAs leaves partial results, which a second kernel joins.
 //
-// Measured (B200): one token over 4000 12.0 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
-// pages, 84 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64 sequences of up to 8192 tokens, 428 MB, 258 us: bound by issue, half of the slots, with
+// Measured (B200): one token over 4000 12.3 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
+// pages, 84 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64 sequences of up to 8192 tokens, 428 MB, 260 us: bound by issue, half of the slots, with
 // three warps per scheduler that the output tile's registers leave (with the pages in L2 hardly less: 272 against 277 of an earlier form).  A variant on tcgen05, tokens
 // as the rows of a tile of 128, took 367: its sixteen and more warps' waits and look-ups per step cost as many instructions as the products they save.
 #include <cuda_fp16.h>
@@ -379,13 +379,48 @@ __device__ __forceinline__ void follow(Running<S>& run, uint64_t (&x)[T][S::NT][
 }
 
 // References and units that fit the tokens at hand: x, exponents of their weights, less the old references (-inf: not seen), and vs, the values' scales.
-// (A row that sees none of its warp's first tokens sees none of the later ones either.)
+// (A row that sees none of its warp's first tokens sees none of the later ones either.)  A head of equal elements has codes of 0 and a scale that says nothing, 1 from
+// the append: it gets a scale of 0, or it would take the bits of others that are smaller.  `values`: the stage's units.
 template <class S, int T>
-__device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T][S::NT][2], const float (&vs)[T][2])
+__device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T][S::NT][2], float (&vs)[T][2], const unsigned char* values, int lane)
 {
+    // a lane has words of tokens 2 t4 and 2 t4 + 1 here, of token g8 elsewhere
+    constexpr int kWords = S::D / 64;
+    uint32_t some[T][2][2];
+    bool zeros = false;
+#pragma unroll
+    for (int v = 0; v < T; ++v)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const uint32_t* words = reinterpret_cast<const uint32_t*>(values + (2 * v + u) * S::UB) + lane * 2 * kWords;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                some[v][u][i] = kWords == 2 ? words[2 * i] | words[2 * i + 1] : words[i];
+                zeros = zeros || some[v][u][i] == 0;
+            }
+        }
     const bool first = !run.started;
     float lv[T][2];
     bool tame = !run.units;
+#pragma unroll
+    for (int v = 0; v < T; ++v) { lv[v][0] = lg2(vs[v][0]); lv[v][1] = lg2(vs[v][1]); }
+    if (__any_sync(0xffffffffu, zeros)) {
+#pragma unroll
+        for (int v = 0; v < T; ++v)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                uint32_t tokens[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    tokens[i] = __ballot_sync(0xffffffffu, some[v][u][i] != 0);
+                    tokens[i] |= tokens[i] >> 16;
+                    tokens[i] |= tokens[i] >> 8;
+                    tokens[i] |= tokens[i] >> 4;
+                }
+                const int token = lane >> 2;
+                if (!((token & 1 ? tokens[1] : tokens[0]) >> (token >> 1) & 1u) && vs[v][u] <= 3.4e38f) { vs[v][u] = 0.0f; lv[v][u] = -kTame; }
+            }
+    }
 #pragma unroll
     for (int v = 0; v < T; ++v)
 #pragma unroll
@@ -397,7 +432,6 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
                 unpair(x[v][n][u], &a, &b);
                 most = max3(most, a, b);
             }
-            lv[v][u] = lg2(vs[v][u]);
             tame = tame && (most == -INFINITY || !(fabsf(lv[v][u]) > kTame));
         }
     run.started = true;
@@ -558,7 +592,7 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
             }
     // The first tokens set the references; after that sums are rescaled only when a product may have risen by 2^kSlack since the last time, by a bound of the largest
     // weight and the largest scale of a lane's tokens.  With units every stage is looked at exactly.
-    if (__builtin_expect(__any_sync(0xffffffffu, !run.started || run.units || most + lg2(scale) > kLift + kSlack), 0)) set_references<S, T>(run, x, vs);
+    if (__builtin_expect(__any_sync(0xffffffffu, !run.started || run.units || most + lg2(scale) > kLift + kSlack), 0)) set_references<S, T>(run, x, vs, at + 4 * UB, lane);
     uint32_t pr[T][L][2];
     if (__builtin_expect(!masked && !run.units, 1)) {
 #pragma unroll

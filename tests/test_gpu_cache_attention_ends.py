@@ -108,3 +108,33 @@ def test_tokens_of_tiny_scales_keep_their_weight(d, tiny, kind):
     want, want_lse, tol, tol_lse, _, _ = plain.attend(c, qn, [0, 1], [n - 1])
     _close(lse, want_lse, tol_lse)
     _close(out, want, tol + _finest(c, qn, [0, 1], [n - 1]))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("counts,heads,kv", [([1], 2, 2), ([9], 4, 1), ([3, 1], 8, 2)])
+@pytest.mark.parametrize("at_slot,scale,value,size", [(0, 1.0, 0.0, 0.0006), (8000, 1.0, 0.0, 0.0006), (5000, 64.0, 0.0, 0.009), (0, 1.0, 0.25, 0.009)])
+def test_a_head_of_equal_elements_takes_no_bits_from_the_others(d, counts, heads, kv, at_slot, scale, value, size):
+    """A token whose values are all the same (all of its codes 0) has 0.99 of the weight, over thousands of small ones."""
+    lens = [8192 - 100 * b for b in range(len(counts))]
+    c = plain.Cache(lens, kv, d, 64, 420, scale=(0.01, 0.02))
+    at, base = _starts(counts), [n - k for n, k in zip(lens, counts)]
+    q = _normal(421, 1, kv, d).repeat_interleave(heads // kv, 1).repeat(at[-1], 1, 1)           # one direction for each key head's rows
+    qn = q.float().numpy()
+    for b, n in enumerate(lens):
+        c.scale[1][b] = plain.bf16(c.rng.uniform(0.6 * size, size, (n, kv)))
+        c.offset[1][b] = plain.bf16(c.scale[1][b] * (-7.5 + c.rng.standard_normal((n, kv))))
+        slot = min(at_slot, base[b])
+        for g in range(kv):
+            x = qn[0, g * (heads // kv)].astype(np.float64)
+            s = d ** -0.5 * (c.value(0, b)[:, g] @ x)
+            target = np.log(99.0) + np.log(np.exp(s - s.max()).sum()) + s.max()
+            c.codes[0][b][slot, g] = np.where(x > 0, 15, 0)
+            c.scale[0][b][slot, g] = plain.bf16(target / (d ** -0.5 * 7.5 * np.abs(x).sum()))
+            c.offset[0][b][slot, g] = plain.bf16(-7.5 * c.scale[0][b][slot, g])
+            c.codes[1][b][slot, g], c.scale[1][b][slot, g], c.offset[1][b][slot, g] = 0, scale, value
+    lse = torch.zeros((at[-1], heads), device=DEV)
+    out, _, st = binding.polyspec_cache_attention(c.to(DEV), q.to(DEV), c.words_on(c.pool(), DEV), kv, _i32(at), _i32(base), lse=lse)
+    assert int(st) == 0
+    want, want_lse, tol, tol_lse, _, _ = plain.attend(c, qn, at, base)
+    _close(lse, want_lse, tol_lse)
+    _close(out, want, tol + _finest(c, qn, at, base))
