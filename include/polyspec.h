@@ -560,8 +560,8 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *
  * Which rows are whose in append, attention and weigh: sequence b has the rows rows_at[b] .., rows_at[b + 1] - rows_at[b] of them or the
  * first n_rows[b] (NULL: all); its row i stands at slot base[b] + (extra ? extra[b] : 0) + i of its cache.  Reserve comes first: a row
- * whose slot is not below len[b] is not written or attends to nothing (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE), as are the rows of a sequence
- * whose numbers make no sense.
+ * whose slot is not below len[b] is not written or attends to nothing (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE), as are the rows of a sequence whose len or
+ * base makes no sense, and all rows between the row numbers of one whose n_rows does not.  Row numbers that decrease or lie outside 0 .. rows leave the sequence without rows.
  *
  * polyspec_cache_append -- keys and values of new rows into their slots:  offset = min(x), scale = the smallest normal bf16
  *   number >= (max(x) - offset) / 15 (1 if that is 0), code = (x - offset) / scale rounded to the nearest, ties to even, at most 15; differences and

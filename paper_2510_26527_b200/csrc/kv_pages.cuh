@@ -33,7 +33,7 @@ __device__ __forceinline__ void report(int32_t* status, polyspec_status what)
 }
 
 // One sequence's rows of a block and its cache: rows row0 .. row0 + n - 1 stand at slots base .. base + n - 1, of which the first
-// `granted` are below len.  n is 0 where the numbers make no sense.
+// `granted` are below len.  None is where base or len makes no sense, nor, of all rows between its row numbers, where n_rows does not; n is 0 where those make none.
 struct SeqRows { int row0, n, granted, base, len; bool bad; };
 __device__ __forceinline__ SeqRows seq_rows(const polyspec_cache_pages& s, const polyspec_block_rows& r, int b)
 {
@@ -41,14 +41,12 @@ __device__ __forceinline__ SeqRows seq_rows(const polyspec_cache_pages& s, const
     const int row0 = r.rows_at[b], end = r.rows_at[b + 1], len = s.len[b];
     const int n = r.n_rows ? r.n_rows[b] : end - row0;
     const long long base = static_cast<long long>(r.base[b]) + (r.extra ? r.extra[b] : 0);
-    if (row0 < 0 || end < row0 || end > r.rows || n < 0 || n > end - row0 || len < 0 || len > s.max_pages * s.page_tokens) {
-        q.bad = true;
-        return q;
-    }
+    if (row0 < 0 || end < row0 || end > r.rows) { q.bad = true; return q; }
     q.row0 = row0;
+    q.n = n < 0 || n > end - row0 ? end - row0 : n;
+    if (q.n != n || len < 0 || len > s.max_pages * s.page_tokens) { q.bad = true; return q; }
     q.len = len;
-    if (base < 0) { q.bad = n > 0; q.n = n; return q; }         // rows that stand nowhere attend to nothing
-    q.n = n;
+    if (base < 0) { q.bad = n > 0; return q; }                  // rows that stand nowhere attend to nothing
     q.granted = base >= len ? 0 : min(n, static_cast<int>(len - base));
     q.base = static_cast<int>(min(base, static_cast<long long>(len)));
     q.bad = q.granted < n;

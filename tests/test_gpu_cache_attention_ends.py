@@ -138,3 +138,35 @@ def test_a_head_of_equal_elements_takes_no_bits_from_the_others(d, counts, heads
     want, want_lse, tol, tol_lse, _, _ = plain.attend(c, qn, at, base)
     _close(lse, want_lse, tol_lse)
     _close(out, want, tol + _finest(c, qn, at, base))
+
+
+# ------------------------------------------------------------------ rows that attend to nothing
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("change", [{"n_rows": [3, 4, 3]}, {"n_rows": [3, -1, 3]}, {"n_rows": [3, 2, 3], "len": -1}, {"len": -1}, {"len": 1 << 20}, {"base": -4}, {"base": 2 ** 31 - 1}])
+def test_every_row_of_a_sequence_whose_numbers_make_no_sense_gets_zeros(d, change):
+    c = plain.Cache([20, 9, 33], 2, d, 8, 430)
+    at, base, n_rows = [0, 3, 6, 9], [17, 6, 30], change.get("n_rows")
+    q = _normal(431, 9, 4, d)
+    want, want_lse, tol, tol_lse, weights, tol_w = plain.attend(c, q.float().numpy(), at, base)
+    want[3:6], want_lse[3:6], tol[3:6], tol_lse[3:6] = 0, -np.inf, 0, 0
+    if n_rows == [3, 2, 3]:                                 # the row that belongs to nobody stays
+        want[5], want_lse[5] = 9, 9
+    pages, on = c.to(DEV), c.words_on(c.pool(), DEV)
+    base[1] = change.get("base", base[1])
+    pages.len[1] = change.get("len", 9)
+    n_rows = None if n_rows is None else _i32(n_rows)
+    out = torch.full((9, 4, d), 9.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((9, 4), 9.0, device=DEV)
+    _, _, st = binding.polyspec_cache_attention(pages, q.to(DEV), on, 2, _i32(at), _i32(base), n_rows=n_rows, out=out, lse=lse)
+    assert int(st) == BAD
+    _close(out, want, tol)
+    _close(lse, want_lse, tol_lse)
+    w = torch.full((3, c.cap), 2.0, device=DEV)
+    assert int(binding.polyspec_cache_weigh(pages, q.to(DEV), on, 2, _i32(at), _i32(base), lse, w, n_rows=n_rows)) == BAD
+    for b in (0, 2):
+        _close(w[b, :c.lens[b]], 2 + weights[b], tol_w[b] + 4 * plain.U32 * (2 + weights[b]))
+    assert (w[1] == 2).all()
+    x, before = _normal(432, 9, 2, d).to(DEV), on.clone()
+    assert int(binding.polyspec_cache_append(pages, x, x, on, _i32(at), _i32(base), n_rows=n_rows)) == BAD
+    held = torch.from_numpy(c.table[1][c.table[1] >= 0].astype(np.int64)).to(DEV)
+    assert torch.equal(on[:, held], before[:, held])
