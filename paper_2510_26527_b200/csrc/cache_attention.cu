@@ -326,13 +326,13 @@ __device__ __forceinline__ int visible(const AttendParams& p, const Segment& g)
     return first < g.q.granted ? row_limit(g.q, min(last, g.q.granted - 1)) : 0;
 }
 
-// Normalised outputs of eight neighbouring elements of a row.
+// Normalised outputs of eight neighbouring elements of a row; zeros where it attends to nothing, or none of what it attends to could be read.
 __device__ __forceinline__ void store_out(const AttendParams& p, const kv::SeqRows& q, int kv_head, int r, int D, int d0, const float* x, float m, float l)
 {
     const int i = r / p.group;
     if (i >= q.n) return;
     const size_t at = static_cast<size_t>(q.row0 + i) * p.q_heads + kv_head * p.group + r % p.group;
-    const bool none = row_limit(q, i) == 0;
+    const bool none = row_limit(q, i) == 0 || l == 0.0f;
     const float inv = none ? 0.0f : 1.0f / l;
     uint4 y;
     y.x = bf16x2_bits(x[0] * inv, x[1] * inv);

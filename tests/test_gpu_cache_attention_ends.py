@@ -170,3 +170,24 @@ def test_every_row_of_a_sequence_whose_numbers_make_no_sense_gets_zeros(d, chang
     assert int(binding.polyspec_cache_append(pages, x, x, on, _i32(at), _i32(base), n_rows=n_rows)) == BAD
     held = torch.from_numpy(c.table[1][c.table[1] >= 0].astype(np.int64)).to(DEV)
     assert torch.equal(on[:, held], before[:, held])
+
+
+@pytest.mark.parametrize("counts,heads,kv", [([1, 1], 2, 2), ([4, 2], 16, 2)])
+def test_rows_none_of_whose_pages_can_be_read_get_zeros(counts, heads, kv):
+    lens, d, P = [40, 300], 128, 8
+    for unreadable in ([0], [1], [0, 1]):
+        c = plain.Cache(lens, kv, d, P, 440)
+        at, base = _starts(counts), [n - k for n, k in zip(lens, counts)]
+        q = _normal(441, at[-1], heads, d)
+        want, want_lse, tol, tol_lse, _, _ = plain.attend(c, q.float().numpy(), at, base)
+        pages, on = c.to(DEV), c.words_on(c.pool(), DEV)
+        for b in unreadable:
+            pages.table[b] = c.n_pages + 3
+            rows = slice(at[b], at[b + 1])
+            want[rows], want_lse[rows], tol[rows], tol_lse[rows] = 0, -np.inf, 0, 0
+        out = torch.full((at[-1], heads, d), 9.0, dtype=torch.bfloat16, device=DEV)
+        lse = torch.full((at[-1], heads), 9.0, device=DEV)
+        _, _, st = binding.polyspec_cache_attention(pages, q.to(DEV), on, kv, _i32(at), _i32(base), out=out, lse=lse)
+        assert int(st) == BAD
+        _close(out, want, tol)
+        _close(lse, want_lse, tol_lse)
