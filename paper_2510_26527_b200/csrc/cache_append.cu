@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams p)
         if (((__float_as_uint(step) + 8u) & 0xffffu) < 17u) step = __fdiv_rn(range, 15.0f);
         const uint32_t up = (__float_as_uint(step) + 0xffffu) & 0xffff0000u;
         float scale = up ? fmaxf(__uint_as_float(up), 1.17549435e-38f) : 1.0f;      // at least the smallest normal number
-        const bool broken = !(range <= 3.4e38f);
+        const bool broken = !(range < INFINITY);
         if (broken) scale = offset = __uint_as_float(0x7fc00000u);
         // Quotients as a division rounds them, by Markstein's correction: with the reciprocal rounded to nearest, q' = a * inv, r = a - q' * scale (exact),
         // q = q' + r * inv.  (Numbers this coarse often lie in the very middle between two codes: an approximate quotient would not do, and a look at the

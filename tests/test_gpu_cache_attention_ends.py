@@ -191,3 +191,30 @@ def test_rows_none_of_whose_pages_can_be_read_get_zeros(counts, heads, kv):
         assert int(st) == BAD
         _close(out, want, tol)
         _close(lse, want_lse, tol_lse)
+
+
+# ------------------------------------------------------------------ append, queries: ends of the number range
+@pytest.mark.parametrize("d", [64, 128])
+def test_append_of_ranges_up_to_the_end_of_fp32(d):
+    """Ranges between 3.39e38 and the largest finite number have codes; beyond it every value is NaN."""
+    n, kv = 24, 2
+    c = plain.Cache([n], kv, d, 8, 450)
+    x = _normal(451, n, kv, d).float() * 1e37
+    top = torch.tensor(3.3895313892515355e38)
+    x[:, :, 3] = top
+    low = -torch.linspace(0.9e36, 2.1e36, n).view(n, 1)
+    x = torch.maximum(x, low.unsqueeze(-1))
+    x[:, :, 7] = low
+    x = x.to(torch.bfloat16)
+    code, scale, offset, back = plain.quantise(x.float().numpy())
+    ranges = x.float().amax(-1) - x.float().amin(-1)
+    assert (ranges.isfinite() & (ranges > 3.4e38)).any() and ranges.isinf().any()
+    pool = c.empty_pool()
+    pages, on = c.to(DEV), c.words_on(pool, DEV)
+    held = torch.zeros((n, kv, d), dtype=torch.bfloat16, device=DEV)
+    assert int(binding.polyspec_cache_append(pages, x.to(DEV), x.to(DEV), on, _i32([0, n]), _i32([0]), k_held=held)) == 0
+    for p in range(2):
+        c.put(pool, p, 0, range(n), code, scale, offset)
+    assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
+    got = held.float().cpu().numpy()
+    assert ((got == back) | (np.isnan(got) & np.isnan(back))).all()
