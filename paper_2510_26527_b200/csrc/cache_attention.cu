@@ -25,7 +25,7 @@
 // end.  A segment that crosses CTAs leaves partial results, which a second kernel joins.
 //
 // Measured (B200): one token over 4000 12.3 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
-// pages, 84 us, 4.2 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64 sequences of up to 8192 tokens, 428 MB, 260 us: bound by issue, half of the slots, with
+// pages, 84.5 us, 4.1 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64 sequences of up to 8192 tokens, 428 MB, 261 us: bound by issue, half of the slots, with
 // three warps per scheduler that the output tile's registers leave (with the pages in L2 hardly less: 272 against 277 of an earlier form).  A variant on tcgen05, tokens
 // as the rows of a tile of 128, took 367: its sixteen and more warps' waits and look-ups per step cost as many instructions as the products they save.
 #include <cuda_fp16.h>
@@ -164,7 +164,7 @@ __device__ __forceinline__ void store_fragment(uint32_t* frag, int r, int word, 
 __device__ __forceinline__ float row_scale(const AttendParams& p, float top, float* factor)
 {
     const int k = top > 0.0f ? max(-100, static_cast<int>(__float_as_uint(top) >> 23) - 127) : 0;          // top in [2^k, 2^(k+1))
-    *factor = p.scale_log2 * __uint_as_float(static_cast<uint32_t>(min(254, 10 + k + 127)) << 23);
+    *factor = p.scale_log2 * 1024.0f * __uint_as_float(static_cast<uint32_t>(k + 127) << 23);              // (2^(10 + k) alone may be past fp32)
     return __uint_as_float(static_cast<uint32_t>(14 - k + 127) << 23);
 }
 
@@ -205,11 +205,11 @@ __device__ __forceinline__ void load_rows(const AttendParams& p, const kv::SeqRo
         const uint32_t* y = reinterpret_cast<const uint32_t*>(&raw[u]);
         float x[8], sum = 0.0f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) { x[2 * e] = low(y[e]); x[2 * e + 1] = high(y[e]); sum += x[2 * e] + x[2 * e + 1]; }
+        for (int e = 0; e < 4; ++e) { x[2 * e] = low(y[e]); x[2 * e + 1] = high(y[e]); sum = fmaf(x[2 * e], p.scale_log2, fmaf(x[2 * e + 1], p.scale_log2, sum)); }
         store_fragment<D>(frag, r, item % kVecs, x, by);
 #pragma unroll
         for (int d = 1; d < kVecs; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (item % kVecs == 0) sums[r] = sum * p.scale_log2;
+        if (item % kVecs == 0) sums[r] = sum;
     }
     __syncthreads();
 }
@@ -1101,7 +1101,7 @@ __global__ void __launch_bounds__(kWeighWarps * 32) weigh_kernel(const WeighPara
             const uint32_t* y = reinterpret_cast<const uint32_t*>(&raw);
             float x[8], sum = 0.0f, top = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { x[2 * e] = low(y[e]); x[2 * e + 1] = high(y[e]); sum += x[2 * e] + x[2 * e + 1]; }
+            for (int e = 0; e < 4; ++e) { x[2 * e] = low(y[e]); x[2 * e + 1] = high(y[e]); sum = fmaf(x[2 * e], p.scale_log2, fmaf(x[2 * e + 1], p.scale_log2, sum)); }
 #pragma unroll
             for (int e = 0; e < 8; ++e)
                 if (fabsf(x[e]) <= 3.4e38f) top = fmaxf(top, fabsf(x[e]));
@@ -1113,7 +1113,7 @@ __global__ void __launch_bounds__(kWeighWarps * 32) weigh_kernel(const WeighPara
             float factor;
             const float by = row_scale(p, top, &factor);
             store_fragment<D>(frag, n * 8 + r, item % kVecs, x, by);
-            if (item % kVecs == 0) of_row[n * 8 + r] = make_float4(factor, sum * p.scale_log2, lse, __int_as_float(row < rows ? row_limit(q, i) : 0));
+            if (item % kVecs == 0) of_row[n * 8 + r] = make_float4(factor, sum, lse, __int_as_float(row < rows ? row_limit(q, i) : 0));
         }
         __syncthreads();
         for (int n = 0; n < n_groups; ++n) {

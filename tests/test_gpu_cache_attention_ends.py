@@ -218,3 +218,24 @@ def test_append_of_ranges_up_to_the_end_of_fp32(d):
     assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
     got = held.float().cpu().numpy()
     assert ((got == back) | (np.isnan(got) & np.isnan(back))).all()
+
+
+@pytest.mark.parametrize("counts,heads,kv", [([1], 4, 4), ([9], 8, 2)])
+@pytest.mark.parametrize("power", [60, 117, 118, 126])
+def test_large_queries_with_a_small_scale(counts, heads, kv, power):
+    n, d = 70, 128
+    c = plain.Cache([n], kv, d, 16, 460)
+    at, base = _starts(counts), [n - counts[0]]
+    q = (_normal(461, at[-1], heads, d).float().clamp(-1.9, 1.9) * 2.0 ** power).to(torch.bfloat16)
+    q[:, :, 0] = 2.0 ** power * 1.5
+    scale = d ** -0.5 * 2.0 ** -power
+    pages, on = c.to(DEV), c.words_on(c.pool(), DEV)
+    lse = torch.zeros((at[-1], heads), device=DEV)
+    out, _, st = binding.polyspec_cache_attention(pages, q.to(DEV), on, kv, _i32(at), _i32(base), scale=scale, lse=lse)
+    assert int(st) == 0
+    want, want_lse, tol, tol_lse, weights, tol_w = plain.attend(c, q.float().numpy(), at, base, scale=scale)
+    _close(out, want, tol)
+    _close(lse, want_lse, tol_lse)
+    w = torch.zeros((1, c.cap), device=DEV)
+    binding.polyspec_cache_weigh(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse, w, scale=scale)
+    _close(w[0, :n], weights[0], tol_w[0] + 4 * plain.U32 * (1 + weights[0]))
