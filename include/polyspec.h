@@ -572,7 +572,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *
  * polyspec_cache_attention -- the rows of a block over the cache, each row over the slots up to its own:
  *     out[i, h] = sum_{j <= slot(i)} softmax_j(scale * q[i, h] . K[j, h / (q_heads/kv_heads)]) V[j, .]
- *   head_dim 64 or 128, any number of rows; out, lse as in polyspec_prompt_attention; a row that attends to nothing, or to no page that can be read
+ *   head_dim 64 or 128, any number of rows; -1e30 <= scale <= 1e30 (it may be negative here and in weigh); out, lse as in polyspec_prompt_attention; a row that attends to nothing, or to no page that can be read
  *   (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE: pages that cannot be read are left out), gets zeros and -inf.  Codes are
  *   multiplied as whole numbers, scales and offsets applied to fp32 sums.  Weights times the values' scales are rounded to fp16 for their product with the
  *   codes: each is off by 2^-11 of itself at most, or by 2^-28 of its row's largest (heads of

@@ -1166,7 +1166,7 @@ polyspec_status fill(AttendParams* p, const polyspec_cache_pages* s, const polys
     if (st == POLYSPEC_OK) st = kv::check_heads(q_heads, kv_heads, head_dim);
     if (st != POLYSPEC_OK) return st;
     if (!kv::rows_ok(q, q_stride, q_heads, head_dim) || !pool || !kv::aligned16(pool) || !aligned4(device_status)) return POLYSPEC_ERR_INVALID_ARG;
-    if (!(scale >= -3.0e38f && scale <= 3.0e38f)) return POLYSPEC_ERR_INVALID_ARG;
+    if (!(scale >= -1.0e30f && scale <= 1.0e30f)) return POLYSPEC_ERR_INVALID_ARG;
     const size_t bytes = kv::page_bytes(*s, kv_heads, head_dim);
     if (s->n_pages * (bytes / kv::unit_bytes(head_dim)) >= 0xffffffffull) return POLYSPEC_ERR_UNSUPPORTED;      // units of a plane are counted in 32 bits
     p->s = *s;

@@ -239,3 +239,22 @@ def test_large_queries_with_a_small_scale(counts, heads, kv, power):
     w = torch.zeros((1, c.cap), device=DEV)
     binding.polyspec_cache_weigh(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse, w, scale=scale)
     _close(w[0, :n], weights[0], tol_w[0] + 4 * plain.U32 * (1 + weights[0]))
+
+
+@pytest.mark.parametrize("counts,heads,kv", [([1], 4, 4), ([9], 8, 2)])
+@pytest.mark.parametrize("scale", [-0.11, 0.0])
+def test_scales_below_and_at_zero(counts, heads, kv, scale):
+    n, d = 150, 64
+    c = plain.Cache([n], kv, d, 16, 465)
+    at, base = _starts(counts), [n - counts[0]]
+    q = _normal(466, at[-1], heads, d)
+    pages, on = c.to(DEV), c.words_on(c.pool(), DEV)
+    lse = torch.zeros((at[-1], heads), device=DEV)
+    out, _, st = binding.polyspec_cache_attention(pages, q.to(DEV), on, kv, _i32(at), _i32(base), scale=scale, lse=lse)
+    assert int(st) == 0
+    want, want_lse, tol, tol_lse, weights, tol_w = plain.attend(c, q.float().numpy(), at, base, scale=scale)
+    _close(out, want, tol)
+    _close(lse, want_lse, tol_lse)
+    w = torch.zeros((1, c.cap), device=DEV)
+    binding.polyspec_cache_weigh(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse, w, scale=scale)
+    _close(w[0, :n], weights[0], tol_w[0] + 4 * plain.U32 * (1 + weights[0]))
