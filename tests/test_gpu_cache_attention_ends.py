@@ -258,3 +258,33 @@ def test_scales_below_and_at_zero(counts, heads, kv, scale):
     w = torch.zeros((1, c.cap), device=DEV)
     binding.polyspec_cache_weigh(pages, q.to(DEV), on, kv, _i32(at), _i32(base), lse, w, scale=scale)
     _close(w[0, :n], weights[0], tol_w[0] + 4 * plain.U32 * (1 + weights[0]))
+
+
+# ------------------------------------------------------------------ eviction
+def test_evict_with_tables_of_more_tokens_than_shared_memory_holds():
+    """Tables for 50048 tokens: a sequence of 50001, whose weights are read from memory, and a short one, whose weights fit."""
+    lens, budget, kv, d, P = [50001, 700], [1500, 90], 1, 64, 64
+    c = plain.Cache(lens, kv, d, P, 470, max_tokens=50048)
+    w = np.random.default_rng(471).integers(0, 500, (2, c.cap)).astype(np.float32)
+    w[:, ::9] = np.nan
+    pages, pool = c.to(DEV), c.pool()
+    on, won = c.words_on(pool, DEV), torch.from_numpy(w.copy()).to(DEV)
+    kept_from = torch.full((2, c.cap), 5, dtype=torch.int32, device=DEV)
+    assert int(binding.polyspec_cache_evict(pages, _i32(budget), won, on, kv, d, first=3, recent=40, kept_from=kept_from)) == 0
+    assert pages.len.tolist() == budget
+    want_from = np.full((2, c.cap), -1)
+    for b in range(2):
+        keep = plain.evict_slots(w[b], lens[b], budget[b], 3, 40)
+        moved = [i for i, j in enumerate(keep) if i != j]
+        old = [keep[i] for i in moved]
+        for p in range(2):
+            c.put(pool, p, b, moved, c.codes[p][b][old], c.scale[p][b][old], c.offset[p][b][old])
+        w[b, : len(keep)] = w[b, keep]
+        want_from[b, : len(keep)] = keep
+        c.refs[c.table[b, -(-budget[b] // P):-(-lens[b] // P)]] -= 1
+        c.table[b, -(-budget[b] // P):] = -1
+    assert (kept_from.cpu().numpy() == want_from).all()
+    assert (won.cpu().numpy().view(np.uint32) == w.view(np.uint32)).all()
+    assert (pages.table.cpu().numpy() == c.table).all() and (pages.refs.cpu().numpy() == c.refs).all()
+    assert (pages.free_bits.cpu().numpy() == c.free_bits()).all()
+    assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
