@@ -196,13 +196,13 @@ __global__ void __launch_bounds__(kSelectThreads, 1) evict_select_kernel(const p
     if (moved < budget) atomicMin(&first_moved, moved);
     __syncthreads();
 
-    // nobody else may hold a page that changes; pages wholly behind what stays only lose this sequence's hold, in the second launch: until then every
+    // nobody else may hold a page that changes (none does where nothing moves); pages wholly behind what stays only lose this sequence's hold, in the second launch: until then every
     // sequence sees the holds as they were, whichever CTA comes first
     const int P = s.page_tokens, keep_pages = (budget + P - 1) / P, held = (len + P - 1) / P;
     for (int i = tid; i < held; i += kSelectThreads) {
         const int page = row[i];
         const bool there = page >= 0 && page < s.n_pages;
-        if (!there || (i >= first_moved / P && i < keep_pages && s.refs[page] > 1)) shared_page = 1;
+        if (!there || (first_moved < budget && i >= first_moved / P && i < keep_pages && s.refs[page] > 1)) shared_page = 1;
         plan.pages[static_cast<size_t>(b) * s.max_pages + i] = page;
     }
     __syncthreads();

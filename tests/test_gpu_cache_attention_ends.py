@@ -288,3 +288,28 @@ def test_evict_with_tables_of_more_tokens_than_shared_memory_holds():
     assert (pages.table.cpu().numpy() == c.table).all() and (pages.refs.cpu().numpy() == c.refs).all()
     assert (pages.free_bits.cpu().numpy() == c.free_bits()).all()
     assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
+
+
+def test_evict_where_nothing_moves_does_not_look_at_shared_pages():
+    """The heaviest tokens are the first: sequences are cut behind them, a last page that is kept in part may be held by others."""
+    lens, kv, d, P = [64, 64, 64], 2, 64, 8
+    c = plain.Cache(lens, kv, d, P, 480)
+    w = np.tile(np.arange(c.cap, dtype=np.float32)[::-1], (3, 1)).copy()
+    budget = [44, 40, 44]
+    w[2, 50] = 1000.0                                       # here one token moves, into the shared page
+    for b in range(3):
+        c.refs[c.table[b, 5]] = 2
+    c.refs[c.table[0, 7]] = 3
+    pages, pool = c.to(DEV), c.pool()
+    on, won = c.words_on(pool, DEV), torch.from_numpy(w.copy()).to(DEV)
+    kept_from = torch.full((3, c.cap), 5, dtype=torch.int32, device=DEV)
+    assert int(binding.polyspec_cache_evict(pages, _i32(budget), won, on, kv, d, kept_from=kept_from)) == BAD
+    assert pages.len.tolist() == [44, 40, 64]
+    for b in range(2):
+        c.refs[c.table[b, -(-budget[b] // P):]] -= 1
+        c.table[b, -(-budget[b] // P):] = -1
+        assert (kept_from[b].cpu().numpy() == [i if i < budget[b] else -1 for i in range(c.cap)]).all()
+    assert (kept_from[2] == -1).all()
+    assert (pages.table.cpu().numpy() == c.table).all() and (pages.refs.cpu().numpy() == c.refs).all()
+    assert (won.cpu().numpy() == w).all()
+    assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
