@@ -313,3 +313,38 @@ def test_evict_where_nothing_moves_does_not_look_at_shared_pages():
     assert (pages.table.cpu().numpy() == c.table).all() and (pages.refs.cpu().numpy() == c.refs).all()
     assert (won.cpu().numpy() == w).all()
     assert (on.cpu().numpy().view(np.uint32).reshape(pool.shape) == pool).all()
+
+
+def test_evictions_side_by_side_with_attention():
+    """Two caches shortened on two streams while a third and a fourth are attended to: each as if it were alone."""
+    kv, d, P = 2, 128, 16
+    lens = [900, 300, 1500, 40]
+    budget = _i32([200, 300, 700, 39])
+
+    def state(seed):
+        c = plain.Cache(lens, kv, d, P, seed)
+        w = torch.rand((len(lens), c.cap), generator=torch.Generator().manual_seed(seed)).to(DEV)
+        return c.to(DEV), c.words_on(c.pool(4), DEV), w
+
+    at, base = _i32(_starts([3] * 4)), _i32(n - 3 for n in lens)
+    q = [_normal(490 + i, 12, 8, d).to(DEV) for i in range(2)]
+    readers = [state(492 + i) for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(4)]
+    evict = lambda s: binding.polyspec_cache_evict(s[0], budget, s[2], s[1], kv, d, first=2, recent=20)
+    attend = lambda i: binding.polyspec_cache_attention(readers[i][0], q[i], readers[i][1][:2], kv, at, base)[0]
+    alone, alone_out = [state(494 + i) for i in range(2)], [attend(i).clone() for i in range(2)]
+    for s in alone:
+        assert int(evict(s)) == 0
+    for _ in range(5):
+        cut, got = [state(494 + i) for i in range(2)], []
+        torch.cuda.synchronize()
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                evict(cut[i])
+            with torch.cuda.stream(streams[2 + i]):
+                got.append(attend(i))
+        torch.cuda.synchronize()
+        for i in range(2):
+            for name in ("table", "len", "refs", "free_bits"):
+                assert torch.equal(getattr(cut[i][0], name), getattr(alone[i][0], name))
+            assert torch.equal(cut[i][1], alone[i][1]) and torch.equal(cut[i][2], alone[i][2]) and torch.equal(got[i], alone_out[i])
