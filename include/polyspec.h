@@ -545,7 +545,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *   rows_at [n_seqs + 1]: prompt b is the rows rows_at[b] .. rows_at[b + 1]-1 (none if equal); rows outside all of them are neither read into
  *   a result nor written.  q_heads a multiple of kv_heads; head_dim 64 or 128; 0 <= scale <= 1e30
  *   out [rows, q_heads, head_dim]; lse out [rows, q_heads] fp32 or NULL: the natural logarithm of the softmax's denominator.
- *   Products of bf16, sums and softmax in fp32; weights are rounded to bf16 for their product with the values.  Keys and values behind a
+ *   Products of bf16, sums and softmax in fp32 (values are at most 2^64 in size); weights are rounded to bf16 for their product with the values.  Keys and values behind a
  *   row never reach it, NaN and infinities included.  Row numbers that decrease or lie outside 0 .. rows make the prompt empty
  *   (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE in *device_status); POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.
  *
@@ -577,7 +577,7 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *   multiplied as whole numbers, scales and offsets applied to fp32 sums.  Weights times the values' scales are rounded to fp16 for their product with the
  *   codes: each is off by 2^-11 of itself at most, or by 2^-28 of its row's largest (heads of
  *   equal elements, all codes 0, aside).  lse, and with it the weights of polyspec_cache_weigh, depends on keys alone.
- *   Values are at most some 2^96 in size: sums over the tokens stay within fp32.  The order of the sums depends on the lengths and on the batch.
+ *   Values are at most 2^64 in size: sums of weights times values stay within fp32.  The order of the sums depends on the lengths and on the batch.
  *   Workspace of polyspec_cache_attention_workspace bytes.
  *   POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.
  *

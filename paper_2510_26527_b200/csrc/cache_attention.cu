@@ -46,7 +46,9 @@ constexpr int kOverhead = 4;                    // steps' worth of work that a s
 constexpr float kNone = -3.0e38f;               // a maximum over nothing
 constexpr float kLift = 3.0f;                   // a row's largest product of weight and scale is 2^3 when its reference is set
 constexpr float kSlack = 12.0f;                 // and may rise to 2^15, near fp16's end, before sums are rescaled
-constexpr float kTame = 40.0f;                  // scales from 2^-40 to 2^40 need no units: a weight that is lost below 2^-126 is 2^-49 of the largest at most
+// Scales from 2^-24 to 2^40 need no units: the largest weight is between 2^-37 and 2^27 when the reference is set (so what is lost below 2^-126 is 2^-89 of it at most),
+// and weights stay below 2^39, which leaves values of up to 2^64 room for their sums in fp32.
+constexpr float kLeastScale = -24.0f, kMostScale = 40.0f;
 constexpr float kMostUnit = 126.0f;             // units are 2^-126 to 2^126
 
 struct AttendParams {
@@ -346,7 +348,7 @@ __device__ __forceinline__ void store_out(const AttendParams& p, const kv::SeqRo
 
 // What a warp keeps of its tile.  Per row: the reference of the weights p = 2^(score - reference), with its sign turned; their sum l and the sum lo of p vo; and the
 // output, elements x rows in the codes' form, the sum of p vs unit cv.  A power of two, `unit`, is 1 as long as one reference serves both: then it brings p vs into
-// fp16's range, and p is within 2^60 of 1.  Where scales are too far from 1 for that the reference follows the weights alone, and the unit the products.
+// fp16's range.  Where scales are too far from 1 for that the reference follows the weights alone, and the unit the products.
 // NT groups of 8 rows; a lane has rows 2 t4 and 2 t4 + 1 of each, as pairs.
 template <class S>
 struct Running { float o[S::NT][S::M][4]; uint64_t ref[S::NT], unit[S::NT], l[S::NT], lo[S::NT]; bool started, units; };
@@ -418,7 +420,7 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
                     tokens[i] |= tokens[i] >> 4;
                 }
                 const int token = lane >> 2;
-                if (!((token & 1 ? tokens[1] : tokens[0]) >> (token >> 1) & 1u) && vs[v][u] <= 3.4e38f) { vs[v][u] = 0.0f; lv[v][u] = -kTame; }
+                if (!((token & 1 ? tokens[1] : tokens[0]) >> (token >> 1) & 1u) && vs[v][u] <= 3.4e38f) { vs[v][u] = 0.0f; lv[v][u] = kLeastScale; }
             }
     }
 #pragma unroll
@@ -432,7 +434,7 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
                 unpair(x[v][n][u], &a, &b);
                 most = max3(most, a, b);
             }
-            tame = tame && (most == -INFINITY || !(fabsf(lv[v][u]) > kTame));
+            tame = tame && (most == -INFINITY || !(lv[v][u] < kLeastScale || lv[v][u] > kMostScale));
         }
     run.started = true;
     if (__builtin_expect(__all_sync(0xffffffffu, tame), 1)) {
@@ -448,7 +450,7 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
                     for (int u = 0; u < 2; ++u) {
                         float a, b;
                         unpair(x[v][n][u], &a, &b);
-                        y[v][u] = (j ? b : a) == -INFINITY ? -INFINITY : (j ? b : a) + lv[v][u];
+                        y[v][u] = (j ? b : a) + lv[v][u];           // (NaN, of a hidden token's scale, is never the largest)
                     }
                 const float top = row_max(y, -INFINITY);            // the largest product is 2^top
                 up[j] = top == -INFINITY ? 0.0f : first ? top - kLift : fmaxf(top - kLift, 0.0f);
@@ -488,7 +490,7 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
             const bool none = first && heavy == 0.0f, anew = !none && (first || top + h + e > kLift + 5.0f);
             // with a unit of 1 the largest weight would be 2^most; else it becomes 2^-5
             const float most = anew ? kLift - h : top + e, fall = anew ? top + h + e - kLift : 0.0f;
-            const bool one = none || fabsf(most) <= kTame;
+            const bool one = none || (most >= kLift - kMostScale && most <= kLift - kLeastScale);
             const float wanted = one ? 0.0f : most + 5.0f, to = fminf(fmaxf(wanted, -kMostUnit), kMostUnit);
             up[j] = one && !none ? top - most : top + 5.0f;
             unit[j] = __uint_as_float(static_cast<uint32_t>(static_cast<int>(to) + 127) << 23);
@@ -542,7 +544,7 @@ __device__ __forceinline__ void attend_tokens(const AttendParams& p, Running<S>&
     }
     // scales and offsets of the lane's tokens g8 and g8 + 8; exponents of their weights, less the references, rows in pairs
     uint64_t x[T][L][2];
-    float vs[T][2], vo[T][2], most = -INFINITY, scale = 0x1p-45f;       // (a scale that keeps weights below 2^60 where it bounds the products)
+    float vs[T][2], vo[T][2], most = -INFINITY, scale = 0x1p-24f;       // (the least: so the bound below holds weights under 2^39, too)
 #pragma unroll
     for (int v = 0; v < T; ++v) {
 #pragma unroll

@@ -140,6 +140,28 @@ def test_a_head_of_equal_elements_takes_no_bits_from_the_others(d, counts, heads
     _close(out, want, tol + _finest(c, qn, at, base))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("counts,heads,kv", [([1], 2, 2), ([9], 4, 1)])
+@pytest.mark.parametrize("scale", [2.0 ** -126, 2.0 ** -45, 2.0 ** -23, 1.0])
+def test_values_of_up_to_2_to_the_64th(d, counts, heads, kv, scale):
+    """Offsets near 2^64 of either sign with any scale; half of the heads have codes of 0 throughout."""
+    n = 3000
+    c = plain.Cache([n], kv, d, 64, 425)
+    c.scale[1][0][:] = scale
+    c.offset[1][0][:] = plain.bf16(c.rng.uniform(-1, 1, (n, kv)) * 2.0 ** 64)
+    c.codes[1][0][c.rng.random((n, kv)) < 0.5] = 0
+    c.codes[1][0][:40] = 0
+    at, base = _starts(counts), [n - counts[0]]
+    q = _normal(426, at[-1], heads, d)
+    lse = torch.zeros((at[-1], heads), device=DEV)
+    out, _, st = binding.polyspec_cache_attention(c.to(DEV), q.to(DEV), c.words_on(c.pool(), DEV), kv, _i32(at), _i32(base), lse=lse)
+    assert int(st) == 0
+    qn = q.float().numpy()
+    want, want_lse, tol, tol_lse, _, _ = plain.attend(c, qn, at, base)
+    _close(lse, want_lse, tol_lse)
+    _close(out, want, tol + _finest(c, qn, at, base))
+
+
 # ------------------------------------------------------------------ rows that attend to nothing
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("change", [{"n_rows": [3, 4, 3]}, {"n_rows": [3, -1, 3]}, {"n_rows": [3, 2, 3], "len": -1}, {"len": -1}, {"len": 1 << 20}, {"base": -4}, {"base": 2 ** 31 - 1}])
