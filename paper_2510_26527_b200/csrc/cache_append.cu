@@ -11,9 +11,12 @@
 #include <cuda_bf16.h>
 
 #include "kv_pages.cuh"
+#include "number_pairs.cuh"
 
 namespace polyspec {
 namespace {
+
+using namespace numbers;
 
 constexpr int kThreads = 128;
 // 1.5 * 2^23 as bits (the form of whole numbers below), at the places of all eight codes of a word
@@ -23,33 +26,6 @@ __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b)
 {
     uint32_t x;
     asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(x) : "r"(a), "r"(b));
-    return x;
-}
-
-// Pairs of fp32 numbers in one instruction.
-__device__ __forceinline__ uint64_t pair(float a, float b)
-{
-    uint64_t x;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
-    return x;
-}
-__device__ __forceinline__ void unpair(uint64_t x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t x;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
-    return x;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t x;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
-    return x;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t x;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
     return x;
 }
 

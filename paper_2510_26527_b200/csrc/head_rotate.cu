@@ -13,9 +13,12 @@
 #include <cuda_bf16.h>
 
 #include "kv_pages.cuh"
+#include "number_pairs.cuh"
 
 namespace polyspec {
 namespace {
+
+using namespace numbers;
 
 constexpr int kThreads = 64;                    // (128: 34.3 us at the size above, 256: 40)
 
@@ -30,28 +33,6 @@ struct RotateParams {
     float eps;
 };
 
-// Pairs of fp32 numbers in one instruction.
-__device__ __forceinline__ uint64_t pair(float a, float b)
-{
-    uint64_t x;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
-    return x;
-}
-__device__ __forceinline__ void unpair(uint64_t x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t x;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
-    return x;
-}
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t x;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
-    return x;
-}
-__device__ __forceinline__ float low(uint32_t x) { return __uint_as_float(x << 16); }
-__device__ __forceinline__ float high(uint32_t x) { return __uint_as_float(x & 0xffff0000u); }
 // A lane's two vectors as the first and the second numbers of its eight pairs, two pairs to a 64-bit number: partners are the vectors themselves, or
 // neighbours in them.
 template <bool NEIGHBOURS>

@@ -28,10 +28,13 @@
 #include <mutex>
 
 #include "kv_pages.cuh"
+#include "number_pairs.cuh"
 #include "tensor_device.cuh"
 
 namespace polyspec {
 namespace {
+
+using namespace numbers;
 
 using namespace tensordev;
 
@@ -124,45 +127,6 @@ __device__ __forceinline__ void tmem_ld_wait(float (&r)[N])
     for (int i = 0; i < N; ++i) asm volatile("" : "+f"(r[i]));
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-__device__ __forceinline__ float ex2(float x)
-{
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float x;
-    asm("max.f32 %0, %1, %2, %3;" : "=f"(x) : "f"(a), "f"(b), "f"(c));
-    return x;
-}
-// Pairs of fp32 numbers in one instruction.
-__device__ __forceinline__ uint64_t pair(float a, float b)
-{
-    uint64_t x;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a), "f"(b));
-    return x;
-}
-__device__ __forceinline__ void unpair(uint64_t x, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(x)); }
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t x;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(x) : "l"(a), "l"(b), "l"(c));
-    return x;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t x;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(a), "l"(b));
-    return x;
-}
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b)
-{
-    uint32_t x;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(x) : "f"(b), "f"(a));
-    return x;
-}
 
 __device__ __forceinline__ void raise_abort(int* abort_flag, int32_t* status)
 {
@@ -612,7 +576,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                         b = ex2(b);
                         if (i & 1) sum1 = add2(sum1, pair(a, b));
                         else sum0 = add2(sum0, pair(a, b));
-                        x[i] = pack_bf16(a, b);
+                        x[i] = bf16x2_bits(a, b);
                     }
                     tmem_st32(s_at + 32 * h, x);
                     tmem_st_wait();
@@ -654,8 +618,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompt_kernel(const __grid_consta
                         uint4* to = reinterpret_cast<uint4*>(p.out + at * D + i * 32);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
-                            to[e] = make_uint4(pack_bf16(o[8 * e] * inv, o[8 * e + 1] * inv), pack_bf16(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
-                                               pack_bf16(o[8 * e + 4] * inv, o[8 * e + 5] * inv), pack_bf16(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
+                            to[e] = make_uint4(bf16x2_bits(o[8 * e] * inv, o[8 * e + 1] * inv), bf16x2_bits(o[8 * e + 2] * inv, o[8 * e + 3] * inv),
+                                               bf16x2_bits(o[8 * e + 4] * inv, o[8 * e + 5] * inv), bf16x2_bits(o[8 * e + 6] * inv, o[8 * e + 7] * inv));
                     }
                 }
                 if (live && p.lse) p.lse[at] = (m * c + log2f(l)) * 0.69314718055994530942f;
