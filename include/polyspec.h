@@ -589,8 +589,8 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  * polyspec_cache_evict -- sequences of more than budget[b] tokens (budget[b] >= 0) keep the first `first`, the last `recent` and, of those between, the ones of
  *   largest weight (the lower slot of equal ones; NaN below everything) until budget[b] are left.  What is kept moves together in
  *   every plane of the pool and in the weights, in order; pages wholly behind are given back, len follows.  What lies behind the kept tokens in
- *   a page or in the weights stays as it is.  A sequence stays as it was (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE) if its budget is below first + recent, or
- *   if a page that keeps tokens from the first changed slot on is held by others too, as the holds were before the call.  (Pages wholly behind only lose the
+ *   a page or in the weights stays as it is.  A sequence stays as it was (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE) if its budget is below first + recent,
+ *   if one of its page numbers makes no sense, or if a page that keeps tokens from the first changed slot on is held by others too, as the holds were before the call.  (Pages wholly behind only lose the
  *   sequence's hold, and where the kept tokens are the first ones no slot changes.)
  *   kept_from  out [n_seqs, max_pages * page_tokens] or NULL: the slot each kept token of a shortened sequence had, -1 behind them;
  *              sequences that were not shortened get -1 throughout.

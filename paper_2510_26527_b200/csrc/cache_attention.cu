@@ -24,10 +24,11 @@
 // a ring of its own (bulk copies of one or two units) and keeps maximum, sums and the output tile in registers; a segment's warps meet once at its
 // end.  A segment that crosses CTAs leaves partial results, which a second kernel joins.
 //
-// Measured (B200): one token over 4000 12.3 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
-// pages, 84.5 us, 4.1 TB/s (the copies alone 60); blocks of 4 to 9 rows of 64 sequences of up to 8192 tokens, 428 MB, 261 us: bound by issue, half of the slots, with
-// three warps per scheduler that the output tile's registers leave (with the pages in L2 hardly less: 272 against 277 of an earlier form).  A variant on tcgen05, tokens
-// as the rows of a tile of 128, took 367: its sixteen and more warps' waits and look-ups per step cost as many instructions as the products they save.
+// Measured (B200): one token over 4000 12.5 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
+// pages, 84.5 us, 4.1 TB/s (the copies alone 60; with two stages none is under way while a warp computes); blocks of 4 to 9 rows of 64 sequences of up to 8192
+// tokens, 428 MB, 262 us: bound by the latency of products, exponentials and products one behind the other, half of the issue slots used, with three warps per
+// scheduler that the output tile's registers leave (with the pages in L2 hardly less: 272 against 277 of an earlier form).  A variant on tcgen05, tokens as
+// the rows of a tile of 128, took 367: its sixteen and more warps' waits and look-ups per step cost as many instructions as the products they save.
 #include <cuda_fp16.h>
 
 #include "kv_pages.cuh"

@@ -7,8 +7,8 @@
 // read before it is written overwrites nothing that a later batch reads.
 //
 // Moving is HBM-bound: each token that moves is read and written once, and of a unit of values that keeps any token everything is read (four neighbours
-// share a sector).  Measured (B200): one sequence of 4300 tokens cut to 4096 in 64 planes of 8 heads of 128, 285 MB, 73 us, some 14 of them the first launch's
-// chain of passes; 32 sequences of up to 2048 cut to 1024 in 64 planes of 4 heads 279 us, of which the moves are 260: 1.57 GB in and out, 6.0 TB/s.
+// share a sector).  Measured (B200): one sequence of 4300 tokens cut to 4096 in 64 planes of 8 heads of 128, 285 MB, 76 us, some 14 of them the first launch's
+// chain of passes; 32 sequences of up to 2048 cut to 1024 in 64 planes of 4 heads 276 us, of which the moves are 260: 1.57 GB in and out, 6.0 TB/s.
 #include <algorithm>
 #include <type_traits>
 

@@ -69,7 +69,7 @@ inline polyspec_status check_state(const polyspec_cache_pages* s)
     return s->page_tokens % kUnit || s->page_tokens > 32768 ? POLYSPEC_ERR_UNSUPPORTED : POLYSPEC_OK;
 }
 
-// (rows * heads stays far below 2^31: the largest row counts are refused)
+// (a sequence's rows times the heads of a group, which kernels count in 32 bits, would take 256 GB of queries to reach 2^31)
 inline polyspec_status check_rows(const polyspec_block_rows* r)
 {
     if (!r || !r->rows_at || !r->base || r->rows < 1 || !aligned4(r->rows_at, r->n_rows, r->base, r->extra)) return POLYSPEC_ERR_INVALID_ARG;

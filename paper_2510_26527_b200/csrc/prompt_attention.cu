@@ -20,7 +20,8 @@
 // long run is held at the power cap).  Bound by the softmax and the products taking turns: tensor and exponential pipes are each active 60% of the time.  Half
 // or a quarter of the exponentials as polynomials on the FMA pipe moved nothing or cost time; without the split of registers between roles scores spill
 // (3300 us); weights handed over in halves and items to and fro over the CTAs were worth 577 -> 524, what is loaded from tensor memory pinned behind its wait
-// 524 -> 507.  Prompts of a few hundred rows: 11 us, a launch with the longest item's four steps.
+// 524 -> 507.  Prompts of a few hundred rows: 11 us, a launch and the longest item's steps one after the other (three for
+// 384 rows of groups of odd size, without a tile B, so with half of the softmax warps idle).
 #include <cuda.h>
 #include <cuda_bf16.h>
 
