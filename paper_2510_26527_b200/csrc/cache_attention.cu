@@ -26,7 +26,7 @@
 //
 // Measured (B200): one token over 4000 12.5 us, most of it two launches' dependent look-ups; single tokens of 16 sequences of up to 65536 tokens, 350 MB of
 // pages, 84.5 us, 4.1 TB/s (the copies alone 60; with two stages none is under way while a warp computes); blocks of 4 to 9 rows of 64 sequences of up to 8192
-// tokens, 428 MB, 262 us: bound by the latency of products, exponentials and products one behind the other, half of the issue slots used, with three warps per
+// tokens, 428 MB, 263 us: bound by the latency of products, exponentials and products one behind the other, half of the issue slots used, with three warps per
 // scheduler that the output tile's registers leave (with the pages in L2 hardly less: 272 against 277 of an earlier form).  A variant on tcgen05, tokens as
 // the rows of a tile of 128, took 367: its sixteen and more warps' waits and look-ups per step cost as many instructions as the products they save.
 #include <cuda_fp16.h>
@@ -333,7 +333,7 @@ __device__ __forceinline__ void follow(Running<S>& run, uint64_t (&x)[T][S::NT][
 
 // References and units that fit the tokens at hand: x, exponents of their weights, less the old references (-inf: not seen), and vs, the values' scales.
 // (A row that sees none of its warp's first tokens sees none of the later ones either.)  A head of equal elements has codes of 0 and a scale that says nothing, 1 from
-// the append: it gets a scale of 0, or it would take the bits of others that are smaller.  `values`: the stage's units.
+// the append: it gets a scale of 0 (lv: -inf), or it would take the bits of others that are smaller.  `values`: the stage's units.
 template <class S, int T>
 __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T][S::NT][2], float (&vs)[T][2], const unsigned char* values, int lane)
 {
@@ -371,7 +371,7 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
                     tokens[i] |= tokens[i] >> 4;
                 }
                 const int token = lane >> 2;
-                if (!((token & 1 ? tokens[1] : tokens[0]) >> (token >> 1) & 1u) && vs[v][u] <= 3.4e38f) { vs[v][u] = 0.0f; lv[v][u] = kLeastScale; }
+                if (!((token & 1 ? tokens[1] : tokens[0]) >> (token >> 1) & 1u) && vs[v][u] <= 3.4e38f) { vs[v][u] = 0.0f; lv[v][u] = -INFINITY; }
             }
     }
 #pragma unroll
@@ -421,7 +421,7 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             // The row's largest weight, of these tokens or (by their sum) of those before, is 2^top; these tokens' largest product 2^h of that, in the output's
-            // unit 2^(top + h + e).
+            // unit 2^(top + h + e).  Before a row's first product its unit is the largest.
             float y[T][2], w[T][2];
 #pragma unroll
             for (int v = 0; v < T; ++v)
@@ -431,8 +431,9 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
                     unpair(x[v][n][u], &a, &b);
                     y[v][u] = j ? b : a;
                 }
-            float top = row_max(y, l[j] > 0.0f ? log2f(l[j]) : -INFINITY);
-            top = top == -INFINITY ? 0.0f : ceilf(top);
+            float top = row_max(y, lg2(l[j]));           // (-inf where there were none)
+            const bool sees = top > -INFINITY;
+            top = sees ? ceilf(top) : 0.0f;
 #pragma unroll
             for (int v = 0; v < T; ++v)
 #pragma unroll
@@ -441,8 +442,8 @@ __device__ __forceinline__ void set_references(Running<S>& run, uint64_t (&x)[T]
             const bool none = first && heavy == 0.0f, anew = !none && (first || top + h + e > kLift + 5.0f);
             // with a unit of 1 the largest weight would be 2^most; else it becomes 2^-5
             const float most = anew ? kLift - h : top + e, fall = anew ? top + h + e - kLift : 0.0f;
-            const bool one = none || (most >= kLift - kMostScale && most <= kLift - kLeastScale);
-            const float wanted = one ? 0.0f : most + 5.0f, to = fminf(fmaxf(wanted, -kMostUnit), kMostUnit);
+            const bool one = none ? !sees : most >= kLift - kMostScale && most <= kLift - kLeastScale;
+            const float wanted = one ? 0.0f : none ? kMostUnit : most + 5.0f, to = fminf(fmaxf(wanted, -kMostUnit), kMostUnit);
             up[j] = one && !none ? top - most : top + 5.0f;
             unit[j] = __uint_as_float(static_cast<uint32_t>(static_cast<int>(to) + 127) << 23);
             by[j] = first ? 1.0f : ex2(-up[j]);

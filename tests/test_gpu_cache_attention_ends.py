@@ -162,6 +162,31 @@ def test_values_of_up_to_2_to_the_64th(d, counts, heads, kv, scale):
     _close(out, want, tol + _finest(c, qn, at, base))
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("counts,heads,kv", [([1], 2, 2), ([9], 4, 1)])
+@pytest.mark.parametrize("more", [10, 25, 45, 70])
+@pytest.mark.parametrize("equal", [[0], [2000], list(range(300)), list(range(0, 2990, 3))], ids=["first", "middle", "many first", "every third"])
+def test_a_head_of_equal_elements_of_any_weight(d, counts, heads, kv, more, equal):
+    """Zero-valued tokens whose weights are 2^more of the others': these are all that the output is made of."""
+    n = 3000
+    c = plain.Cache([n], kv, d, 64, 427, scale=(0.01, 0.02))
+    at, base = _starts(counts), [n - counts[0]]
+    q = _normal(428, 1, kv, d).repeat_interleave(heads // kv, 1).repeat(at[-1], 1, 1)           # one direction for each key head's rows
+    qn = q.float().numpy()
+    for g in range(kv):
+        x = qn[0, g * (heads // kv)].astype(np.float64)
+        c.codes[0][0][equal, g] = np.where(x > 0, 15, 0)
+        c.scale[0][0][equal, g] = plain.bf16(more * np.log(2.0) / (d ** -0.5 * 7.5 * np.abs(x).sum()))
+        c.offset[0][0][equal, g] = plain.bf16(-7.5 * c.scale[0][0][equal, g])
+        c.codes[1][0][equal, g], c.scale[1][0][equal, g], c.offset[1][0][equal, g] = 0, 1.0, 0.0
+    lse = torch.zeros((at[-1], heads), device=DEV)
+    out, _, st = binding.polyspec_cache_attention(c.to(DEV), q.to(DEV), c.words_on(c.pool(), DEV), kv, _i32(at), _i32(base), lse=lse)
+    assert int(st) == 0
+    want, want_lse, tol, tol_lse, _, _ = plain.attend(c, qn, at, base)
+    _close(lse, want_lse, tol_lse)
+    _close(out, want, tol + _finest(c, qn, at, base))
+
+
 # ------------------------------------------------------------------ rows that attend to nothing
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("change", [{"n_rows": [3, 4, 3]}, {"n_rows": [3, -1, 3]}, {"n_rows": [3, 2, 3], "len": -1}, {"len": -1}, {"len": 1 << 20}, {"base": -4}, {"base": 2 ** 31 - 1}])
