@@ -560,8 +560,9 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *
  * Which rows are whose in append, attention and weigh: sequence b has the rows rows_at[b] .., rows_at[b + 1] - rows_at[b] of them or the
  * first n_rows[b] (NULL: all); its row i stands at slot base[b] + (extra ? extra[b] : 0) + i of its cache.  Reserve comes first: a row
- * whose slot is not below len[b] is not written or attends to nothing (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE), as are the rows of a sequence whose len or
- * base makes no sense, and all rows between the row numbers of one whose n_rows does not.  Row numbers that decrease or lie outside 0 .. rows leave the sequence without rows.
+ * whose slot is not below len[b] is not written or attends to nothing (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE), as are the rows of a sequence
+ * whose len or base makes no sense, and all rows between the row numbers of one whose n_rows does not.  Row numbers that decrease or lie
+ * outside 0 .. rows leave the sequence without rows.
  *
  * polyspec_cache_append -- keys and values of new rows into their slots:  offset = min(x), scale = the smallest normal bf16
  *   number >= (max(x) - offset) / 15 (1 if that is 0), code = (x - offset) / scale rounded to the nearest, ties to even, at most 15; differences and
@@ -572,12 +573,13 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *
  * polyspec_cache_attention -- the rows of a block over the cache, each row over the slots up to its own:
  *     out[i, h] = sum_{j <= slot(i)} softmax_j(scale * q[i, h] . K[j, h / (q_heads/kv_heads)]) V[j, .]
- *   head_dim 64 or 128, any number of rows; -1e30 <= scale <= 1e30 (it may be negative here and in weigh); out, lse as in polyspec_prompt_attention; a row that attends to nothing, or to no page that can be read
- *   (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE: pages that cannot be read are left out), gets zeros and -inf.  Codes are
- *   multiplied as whole numbers, scales and offsets applied to fp32 sums.  Weights times the values' scales are rounded to fp16 for their product with the
- *   codes: each is off by 2^-11 of itself at most, or by 2^-28 of its row's largest (heads of
- *   equal elements, all codes 0, aside).  lse, and with it the weights of polyspec_cache_weigh, depends on keys alone.
- *   Values are at most 2^64 in size: sums of weights times values stay within fp32.  The order of the sums depends on the lengths and on the batch.
+ *   head_dim 64 or 128, any number of rows; -1e30 <= scale <= 1e30 (it may be negative here and in weigh); out, lse as in
+ *   polyspec_prompt_attention; a row that attends to nothing, or to no page that can be read (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE: pages that
+ *   cannot be read are left out), gets zeros and -inf.  Codes are multiplied as whole numbers, scales and offsets applied to fp32 sums.
+ *   Weights times the values' scales are rounded to fp16 for their product with the codes: each is off by 2^-11 of itself at most, or by
+ *   2^-28 of its row's largest, heads of equal elements (all codes 0) aside (2^-20 where all its scales are below 2^-118).  lse, and with it
+ *   the weights of polyspec_cache_weigh, depends on queries and keys alone.  Values are at most 2^64 in size: sums of weights times values
+ *   stay within fp32.  The order of the sums depends on the lengths and on the batch.
  *   Workspace of polyspec_cache_attention_workspace bytes.
  *   POLYSPEC_ERR_TIMEOUT as in polyspec_lm_head.
  *
@@ -590,8 +592,8 @@ polyspec_status polyspec_cache_compact(const polyspec_cache_pages* s /* host */,
  *   largest weight (the lower slot of equal ones; NaN below everything) until budget[b] are left.  What is kept moves together in
  *   every plane of the pool and in the weights, in order; pages wholly behind are given back, len follows.  What lies behind the kept tokens in
  *   a page or in the weights stays as it is.  A sequence stays as it was (POLYSPEC_ERR_BAD_INPUT_ON_DEVICE) if its budget is below first + recent,
- *   if one of its page numbers makes no sense, or if a page that keeps tokens from the first changed slot on is held by others too, as the holds were before the call.  (Pages wholly behind only lose the
- *   sequence's hold, and where the kept tokens are the first ones no slot changes.)
+ *   if one of its page numbers makes no sense, or if a page that keeps tokens from the first changed slot on is held by others too, as the
+ *   holds were before the call.  (Pages wholly behind only lose the sequence's hold, and where the kept tokens are the first ones no slot changes.)
  *   kept_from  out [n_seqs, max_pages * page_tokens] or NULL: the slot each kept token of a shortened sequence had, -1 behind them;
  *              sequences that were not shortened get -1 throughout.
  *   Workspace of polyspec_cache_evict_workspace bytes.
